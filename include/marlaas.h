@@ -58,7 +58,7 @@ enum {
 };
 
 enum {
-    MARLAAS_FLAG_ACCUMULATE = 1u,     /* backward: dA_t, dB_t += instead of overwrite */
+    MARLAAS_FLAG_ACCUMULATE = 1u,     /* backward: dA_t, dB_t += instead of overwrite; marlaas_policy_loss: stats += */
     MARLAAS_FLAG_HOST_TABLE = 2u,     /* seg_offsets / seg_slot are HOST arrays: validated on the host, then copied
                                          into the workspace in stream order (not while the stream is being captured:
                                          refused with MARLAAS_ERR_INVALID_ARG) */
@@ -71,6 +71,8 @@ enum {
                                          projections of one decoder layer, which all see the same mixed batch.  The
                                          caller vouches for the condition; batches of at most 1024 tokens ignore the
                                          flag (their plan is built inside the first kernel anyway). */
+    MARLAAS_FLAG_TOKEN_MEAN = 64u,    /* marlaas_group_advantages: every active token of a tenant weighs the same */
+    MARLAAS_FLAG_NO_STD = 128u,       /* marlaas_group_advantages: rewards are centred, not divided by their deviation */
     MARLAAS_FLAG_OVERLAP_PREVIOUS = 32u /* forward, decode-shaped batches (at most 1024 tokens): the caller states that the
                                          work submitted to the stream immediately before this call -- typically the same
                                          layer's call for another micro-batch of a serving loop that interleaves two --
@@ -282,6 +284,106 @@ marlaas_status_t marlaas_lora_build_index(marlaas_pool_t* pool, int64_t T, const
                                           int32_t* tok_slot, int32_t* slot_count, int32_t* slot_offset,
                                           int32_t* perm, void* workspace, size_t workspace_bytes,
                                           uint32_t flags, void* cuda_stream);
+
+/* ---- the policy update around the layer (Algorithm 1, training branch; Experimental setup: GRPO) ----
+ * rewards -> advantages and token weights -> clipped loss with KL term, whose gradient by the logits is the dy of the
+ * output projection's marlaas_lora_backward -> AdamW with 8-bit moments committed into the pool.  The sequences of a
+ * batch are the segments of its segment table; `pool` supplies the device, the slots and the status word. */
+
+enum { MARLAAS_DTYPE_BF16 = 0, MARLAAS_DTYPE_F32 = 1 };    /* element type of logits and of their gradient */
+enum { MARLAAS_MAX_VOCABULARY = 262144 };
+enum { MARLAAS_POLICY_STATS = 8 };                         /* columns of marlaas_policy_loss's stats */
+
+/* Bytes of workspace that marlaas_group_advantages and marlaas_policy_loss need for a batch of T tokens in num_segments
+ * segments and num_groups groups (0 for the loss); 256-byte aligned, contents need not be preserved. */
+size_t marlaas_policy_workspace_bytes(const marlaas_pool_t* pool, int64_t T, int32_t num_segments, int32_t num_groups);
+
+/* Group-relative advantages and token weights.  Segment i of `seg` is sequence i with reward r_i; group g is the
+ * sequences [group_offsets[g], group_offsets[g+1]) (the answers to one prompt).  With d_i = r_i - r_first(g), mean and
+ * population variance over the group,
+ *     a_i = (d_i - mean d) / (sqrt(var d) + eps)          (MARLAAS_FLAG_NO_STD: a_i = d_i - mean d)
+ * A group whose rewards are all alike has advantages of exactly 0.  A token is active if its target is >= 0:
+ *     adv = a_i,  weight = 1 / (N_t len_i)                (MARLAAS_FLAG_TOKEN_MEAN: weight = 1 / M_t)
+ * with len_i the active tokens of its sequence, N_t the sequences of its tenant (slot) that have any, M_t the active
+ * tokens of its tenant; slot -1 counts as one more tenant.  Inactive tokens get 0 and 0.  The weights of a tenant with an
+ * active token sum to 1.  rewards fp32 [S], group_offsets int32 [G+1] (0 .. S, non-decreasing; on the device, or on the
+ * HOST with MARLAAS_FLAG_HOST_TABLE like the segment table), targets int32 [T]; outputs fp32 seq_adv [S], adv [T],
+ * weight [T], each may be NULL.  A device table that is not as described is reported by marlaas_check_status
+ * (MARLAAS_ERR_BAD_SEGMENT_TABLE, MARLAAS_ERR_DEVICE_BAD_INDEX); the outputs are then unspecified. */
+marlaas_status_t marlaas_group_advantages(marlaas_pool_t* pool, int64_t T, const marlaas_segments_t* seg,
+                                          const float* rewards, int32_t num_groups, const int32_t* group_offsets,
+                                          const int32_t* targets, float eps, float* seq_adv, float* adv, float* weight,
+                                          void* workspace, size_t workspace_bytes, uint32_t flags, void* cuda_stream);
+
+/* Log-probabilities of the target tokens under softmax(logits * inv_temperature), and the entropy of that distribution:
+ * the behaviour policy's values at rollout, the reference policy's in training.  logits [T][V] of `dtype`, leading
+ * dimension ld, rows on 16-byte boundaries (ld a multiple of 8 for bf16, of 4 for fp32; V is any number from 1 to
+ * MARLAAS_MAX_VOCABULARY).  targets int32 [T]; logp fp32 [T]; entropy fp32 [T] or NULL.
+ *  - A row with a negative target is ignored: it is not read, logp and entropy are 0.
+ *  - Logits of -inf have probability 0.  A row whose logits are all -inf has no distribution: logp and entropy are 0.
+ *  - A row with a NaN or +inf gets NaN.
+ *  - A target >= V is reported by marlaas_check_status (MARLAAS_ERR_DEVICE_BAD_INDEX) and its row is ignored. */
+marlaas_status_t marlaas_token_logprobs(marlaas_pool_t* pool, int64_t T, int64_t V, const void* logits, int64_t ld,
+                                        int32_t dtype, const int32_t* targets, float inv_temperature, float* logp,
+                                        float* entropy, uint32_t flags, void* cuda_stream);
+
+/* The clipped policy loss with KL and entropy terms, and its gradient by the logits, in one pass over them.  With logp
+ * and the entropy H of token i as above, A = adv[i], w = weight[i]:
+ *     ratio = exp(logp - old_logp[i])      pg = -min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A)
+ *     d = ref_logp[i] - logp               kl = exp(d) - d - 1
+ *     loss = sum_i w (pg + kl_coef kl - entropy_coef H)
+ *     dlogits[i] = grad_scale * d loss / d logits[i]
+ * where a clipped token's pg has no gradient.  dlogits: [T][V] of `dtype` with leading dimension lddl, rows on 16-byte
+ * boundaries; NULL = not wanted; dlogits == logits with lddl == ld overwrites the logits, any other overlap is refused.
+ * Columns from V to the leading dimension are left alone.  logp: fp32 [T] or NULL.
+ * Rows that marlaas_token_logprobs ignores, and tokens of weight 0 whatever their other values, contribute nothing: their
+ * gradient is 0.  ref_logp may be NULL if kl_coef is 0.
+ * stats: fp32 [capacity + 1][MARLAAS_POLICY_STATS], per slot (last row: slot -1) the sums over its tokens of
+ *     w (pg + kl_coef kl - entropy_coef H), w pg, w kl, w H, w ratio, w [clipped], w, 1
+ * (with weights that sum to 1, the first six are the tenant's means); written, or added to with MARLAAS_FLAG_ACCUMULATE,
+ * in a fixed order of the sums.  A token of an ill-formed device table counts as slot -1 and is reported. */
+typedef struct marlaas_policy_loss {
+    float clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale;
+} marlaas_policy_loss_t;
+marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V, const void* logits, int64_t ld,
+                                     int32_t dtype, const int32_t* targets, const marlaas_segments_t* seg,
+                                     const float* old_logp, const float* ref_logp, const float* adv, const float* weight,
+                                     const marlaas_policy_loss_t* hp, void* dlogits, int64_t lddl, float* logp,
+                                     float* stats, void* workspace, size_t workspace_bytes, uint32_t flags,
+                                     void* cuda_stream);
+
+/* AdamW and commit as marlaas_adapter_pool_adamw_commit, with both moments held in 8 bits: 2.06 bytes per element
+ * instead of 8, and 18 bytes moved per element instead of 30.  The moments of a matrix of n elements are
+ * marlaas_adamw_compact_state_bytes(n) bytes: for every 256 consecutive elements a block of 528 bytes, 16-byte aligned:
+ *     [0, 256) codes of m   [256, 512) codes of v   [512] exponent E_m   [513] E_v   [514, 528) unused
+ * A code's low bits are the leading bits of an fp32 number (exponent and 3 mantissa bits) counted from the smallest
+ * exponent the block can hold: m is a sign bit and 7 bits (15 binary orders below E_m), v is 8 bits (31 orders below E_v;
+ * v is the square of what m averages, so both keep the same range of gradients).  Code 0 is 0.  All-zero bytes are zero
+ * moments.  The update is done in fp32 on the decoded moments; the new moments are rounded stochastically with 16 random
+ * bits each, so that their expected value is kept (at beta2 = 0.999 a moment moves by a thousandth per step, a hundredth of
+ * what rounding to nearest would need to move it at all): a moment below the block's range becomes 0, except that a
+ * positive v stays at the smallest code.  A moment that is not finite is stored as 0 (the master then holds a NaN or an
+ * infinity).  The random bits depend on seed, hp->step, the tenant id, the matrix and the element's index alone: the same
+ * call gives the same bits.
+ * state_A[i] / state_B[i]: the tenant's state for A [d_in][rank] and B [rank][d_out]; on a pool over several projections,
+ * the projections' states one after another, each of marlaas_adamw_compact_state_bytes of its own elements.
+ * ranks: HOST [n], the ranks that the buffers were made for, or NULL; a tenant whose adapter has another rank by now is
+ * refused (MARLAAS_ERR_INVALID_ARG).
+ * Everything else, the errors included, as marlaas_adapter_pool_adamw_commit. */
+size_t marlaas_adamw_compact_state_bytes(int64_t n);
+marlaas_status_t marlaas_adapter_pool_adamw_compact_commit(marlaas_pool_t* pool, int32_t n, const uint64_t* tenant_ids,
+                                                           const uint64_t* new_versions, const float* const* dA,
+                                                           const float* const* dB, float* const* A, float* const* B,
+                                                           void* const* state_A, void* const* state_B,
+                                                           const int32_t* ranks, const marlaas_adamw_t* hp,
+                                                           uint64_t seed, void* cuda_stream);
+/* The values that `blocks` consecutive blocks of such a state stand for: fp32 m and v of 256 * blocks elements, 16-byte
+ * aligned (for inspection, or to go on with marlaas_adapter_pool_adamw_commit); either may be NULL. */
+marlaas_status_t marlaas_adamw_compact_state_export(marlaas_pool_t* pool, int64_t blocks, const void* state, float* m,
+                                                    float* v, void* cuda_stream);
+/* Device addresses of the pool's bf16 rows inside its storage: At [parts][capacity * rank_stride][d_in] (row
+ * slot * rank_stride + j of block p is column j of A_t,p), Bs [capacity * rank_stride][d_out].  Read-only for the caller. */
+marlaas_status_t marlaas_adapter_pool_store(const marlaas_pool_t* pool, const void** At, const void** Bs);
 
 /* Synchronise `cuda_stream`, read and clear the pool's device status word: MARLAAS_OK, or the first
  * device-side finding since the last check (BAD_SEGMENT_TABLE, DEVICE_BAD_INDEX, DEVICE_TIMEOUT). */

@@ -33,6 +33,13 @@ MARLAAS_FLAG_VALIDATE_SYNC = 4
 MARLAAS_FLAG_CUDA_CORE_PATH = 8
 MARLAAS_FLAG_REUSE_PLAN = 16
 MARLAAS_FLAG_OVERLAP_PREVIOUS = 32
+MARLAAS_FLAG_TOKEN_MEAN = 64
+MARLAAS_FLAG_NO_STD = 128
+
+MARLAAS_DTYPE_BF16 = 0
+MARLAAS_DTYPE_F32 = 1
+MARLAAS_MAX_VOCABULARY = 262144
+MARLAAS_POLICY_STATS = 8
 
 EXPORTED_SYMBOLS = [
     "marlaas_adapter_pool_storage_bytes", "marlaas_adapter_pool_create", "marlaas_adapter_pool_destroy",
@@ -43,6 +50,9 @@ EXPORTED_SYMBOLS = [
     "marlaas_last_error", "marlaas_kernel_launch_count", "marlaas_kernel_timing_begin", "marlaas_kernel_timing_end",
     "marlaas_lora_static_workspace_limit", "marlaas_lora_forward_static_ws", "marlaas_adapter_pool_adamw_commit",
     "marlaas_lora_forward_workspace_min_bytes", "marlaas_adapter_pool_storage_bytes_segmented", "marlaas_adapter_pool_create_segmented", "marlaas_adapter_pool_parts",
+    "marlaas_policy_workspace_bytes", "marlaas_group_advantages", "marlaas_token_logprobs", "marlaas_policy_loss",
+    "marlaas_adamw_compact_state_bytes", "marlaas_adapter_pool_adamw_compact_commit", "marlaas_adamw_compact_state_export",
+    "marlaas_adapter_pool_store",
 ]
 
 
@@ -55,6 +65,11 @@ class MarlaasError(RuntimeError):
 class marlaas_adamw_t(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
                 ("weight_decay", ctypes.c_float), ("grad_scale", ctypes.c_float), ("step", ctypes.c_int64)]
+
+
+class marlaas_policy_loss_t(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("kl_coef", ctypes.c_float),
+                ("entropy_coef", ctypes.c_float), ("inv_temperature", ctypes.c_float), ("grad_scale", ctypes.c_float)]
 
 
 class marlaas_segments_t(ctypes.Structure):
@@ -127,6 +142,23 @@ def load_library() -> ctypes.CDLL:
     L.marlaas_kernel_timing_begin.argtypes = [vp]
     L.marlaas_kernel_timing_end.restype = i32
     L.marlaas_kernel_timing_end.argtypes = [vp, P(f32), P(i32)]
+    L.marlaas_policy_workspace_bytes.restype = sz
+    L.marlaas_policy_workspace_bytes.argtypes = [vp, i64, i32, i32]
+    L.marlaas_group_advantages.restype = i32
+    L.marlaas_group_advantages.argtypes = [vp, i64, P(marlaas_segments_t), vp, i32, vp, vp, f32, vp, vp, vp, vp, sz, u32, vp]
+    L.marlaas_token_logprobs.restype = i32
+    L.marlaas_token_logprobs.argtypes = [vp, i64, i64, vp, i64, i32, vp, f32, vp, vp, u32, vp]
+    L.marlaas_policy_loss.restype = i32
+    L.marlaas_policy_loss.argtypes = [vp, i64, i64, vp, i64, i32, vp, P(marlaas_segments_t), vp, vp, vp, vp,
+                                      P(marlaas_policy_loss_t), vp, i64, vp, vp, vp, sz, u32, vp]
+    L.marlaas_adamw_compact_state_bytes.restype = sz
+    L.marlaas_adamw_compact_state_bytes.argtypes = [i64]
+    L.marlaas_adapter_pool_adamw_compact_commit.restype = i32
+    L.marlaas_adapter_pool_adamw_compact_commit.argtypes = [vp, i32, P(u64), P(u64)] + [P(vp)] * 6 + [P(i32), P(marlaas_adamw_t), u64, vp]
+    L.marlaas_adamw_compact_state_export.restype = i32
+    L.marlaas_adamw_compact_state_export.argtypes = [vp, i64, vp, vp, vp, vp]
+    L.marlaas_adapter_pool_store.restype = i32
+    L.marlaas_adapter_pool_store.argtypes = [vp, P(vp), P(vp)]
     L.marlaas_last_error.restype = ctypes.c_char_p
     L.marlaas_last_error.argtypes = []
     L.marlaas_kernel_launch_count.restype = u64
@@ -219,6 +251,7 @@ class AdapterPool:
         self.handle = h
         self.rank_stride = int(L.marlaas_adapter_pool_rank_stride(h))
         self._workspaces = {}
+        self._policy_sizes = (None, 0)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -239,6 +272,32 @@ class AdapterPool:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             self._workspaces["ws"] = ws
         return ws
+
+    def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0) -> torch.Tensor:
+        """A cached workspace tensor for marlaas_group_advantages and marlaas_policy_loss (one per pool; not for
+        overlapping calls)."""
+        key = (T, num_segments, num_groups)
+        if self._policy_sizes[0] != key:
+            self._policy_sizes = (key, marlaas_policy_workspace_bytes(self, T, num_segments, num_groups))
+        need = max(self._policy_sizes[1], 256)
+        ws = self._workspaces.get("policy")
+        if ws is None or ws.numel() < need:
+            ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self._workspaces["policy"] = ws
+        return ws
+
+    def store(self):
+        """Views of the pool's bf16 rows: At [n_parts][capacity * rank_stride][d_in] and Bs [capacity * rank_stride][d_out]
+        (not to be written)."""
+        at, bs = ctypes.c_void_p(), ctypes.c_void_p()
+        _check(load_library().marlaas_adapter_pool_store(self.handle, ctypes.byref(at), ctypes.byref(bs)))
+        rows, base, flat = self.capacity * self.rank_stride, self.storage.data_ptr(), self.storage
+        def view(p, *shape):
+            n = 2
+            for d in shape:
+                n *= d
+            return flat[p.value - base:p.value - base + n].view(torch.bfloat16).view(*shape)
+        return view(at, self.n_parts, rows, self.d_in), view(bs, rows, self.d_out)
 
 
 def marlaas_adapter_pool_register(pool: AdapterPool, tenant_id: int, version: int, rank: int, alpha: float,
@@ -456,3 +515,164 @@ def marlaas_kernel_timing_end(pool: AdapterPool):
     ms, n = ctypes.c_float(), ctypes.c_int32()
     _check(load_library().marlaas_kernel_timing_end(pool.handle, ctypes.byref(ms), ctypes.byref(n)))
     return float(ms.value), int(n.value)
+
+
+# ---- the policy update around the layer ----
+
+def _f32(t: torch.Tensor, n: int, name: str) -> ctypes.c_void_p:
+    assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n and t.is_cuda, name
+    return t.data_ptr()
+
+
+def _i32(t: torch.Tensor, n: int, name: str) -> ctypes.c_void_p:
+    assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n, name
+    return t.data_ptr()
+
+
+_DTYPES = {torch.bfloat16: MARLAAS_DTYPE_BF16, torch.float32: MARLAAS_DTYPE_F32}
+
+
+def _rows(t: torch.Tensor, V: int, name: str) -> int:
+    assert t.dim() == 2 and t.shape[1] == V and (V == 1 or t.stride(1) == 1) and t.is_cuda, name
+    ld = t.stride(0)
+    # (torch is free with the stride of a single row)
+    return ld if t.shape[0] > 1 else max(ld, (V + 7) // 8 * 8)
+
+
+def marlaas_policy_workspace_bytes(pool: AdapterPool, T: int, num_segments: int, num_groups: int = 0) -> int:
+    return int(load_library().marlaas_policy_workspace_bytes(pool.handle, T, num_segments, num_groups))
+
+
+def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Tensor, group_offsets: torch.Tensor,
+                             targets: torch.Tensor, *, eps: float = 1e-6, seq_adv: Optional[torch.Tensor] = None,
+                             adv: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None):
+    """(seq_adv [S], adv [T], weight [T]) of a batch whose sequences are the segments of `seg`; group_offsets lives where
+    the segment table does.  Outputs that are not given are allocated."""
+    T, S, G = targets.numel(), seg.c.num_segments, group_offsets.numel() - 1
+    dev = pool.device
+    assert targets.is_cuda and group_offsets.is_cuda != seg.on_host, "group_offsets must be where the segment table is"
+    if seq_adv is None:
+        seq_adv = torch.empty(S, dtype=torch.float32, device=dev)
+    if adv is None:
+        adv = torch.empty(T, dtype=torch.float32, device=dev)
+    if weight is None:
+        weight = torch.empty(T, dtype=torch.float32, device=dev)
+    ws = workspace if workspace is not None else pool.policy_workspace(T, S, G)
+    _check(load_library().marlaas_group_advantages(
+        pool.handle, T, ctypes.byref(seg.c), _f32(rewards, S, "rewards"), G, _i32(group_offsets, G + 1, "group_offsets"),
+        _i32(targets, T, "targets"), eps, _f32(seq_adv, S, "seq_adv"), _f32(adv, T, "adv"), _f32(weight, T, "weight"),
+        ws.data_ptr(), ws.numel(), flags | seg.flags, _stream(stream)))
+    return seq_adv, adv, weight
+
+
+def marlaas_token_logprobs(pool: AdapterPool, logits: torch.Tensor, targets: torch.Tensor, *, inv_temperature: float = 1.0,
+                           logp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                           with_entropy: bool = False, flags: int = 0, stream=None):
+    """logp [T] of the targets (negative = ignored), and with `with_entropy` or `entropy` (logp, entropy)."""
+    T, V = logits.shape
+    if logp is None:
+        logp = torch.empty(T, dtype=torch.float32, device=logits.device)
+    if entropy is None and with_entropy:
+        entropy = torch.empty(T, dtype=torch.float32, device=logits.device)
+    assert logits.dtype in _DTYPES and targets.is_cuda, "logits"
+    _check(load_library().marlaas_token_logprobs(
+        pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES[logits.dtype], _i32(targets, T, "targets"),
+        inv_temperature, _f32(logp, T, "logp"), None if entropy is None else _f32(entropy, T, "entropy"), flags, _stream(stream)))
+    return logp if entropy is None else (logp, entropy)
+
+
+def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.Tensor, seg: Segments, old_logp: torch.Tensor,
+                        adv: torch.Tensor, weight: torch.Tensor, *, ref_logp: Optional[torch.Tensor] = None,
+                        dlogits: Optional[torch.Tensor] = None, logp: Optional[torch.Tensor] = None,
+                        stats: Optional[torch.Tensor] = None, clip_low: float = 0.2, clip_high: float = 0.2,
+                        kl_coef: float = 0.0, entropy_coef: float = 0.0, inv_temperature: float = 1.0, grad_scale: float = 1.0,
+                        workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> torch.Tensor:
+    """Clipped policy loss with KL and entropy terms: returns stats [capacity + 1][8] (see marlaas.h; column 0 is the loss
+    per slot) and writes its gradient by the logits to `dlogits` (which may be `logits` itself) if given."""
+    T, V = logits.shape
+    if stats is None:
+        assert not (flags & MARLAAS_FLAG_ACCUMULATE), "stats to add to"
+        stats = torch.empty((pool.capacity + 1, MARLAAS_POLICY_STATS), dtype=torch.float32, device=pool.device)
+    assert logits.dtype in _DTYPES and targets.is_cuda, "logits"
+    lddl = 0
+    if dlogits is not None:
+        assert dlogits.dtype == logits.dtype and dlogits.shape[0] == T, "dlogits"
+        lddl = _rows(dlogits, V, "dlogits")
+    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.c.num_segments)
+    hp = marlaas_policy_loss_t(clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale)
+    _check(load_library().marlaas_policy_loss(
+        pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES[logits.dtype], _i32(targets, T, "targets"),
+        ctypes.byref(seg.c), _f32(old_logp, T, "old_logp"), None if ref_logp is None else _f32(ref_logp, T, "ref_logp"),
+        _f32(adv, T, "adv"), _f32(weight, T, "weight"), ctypes.byref(hp), None if dlogits is None else dlogits.data_ptr(), lddl,
+        None if logp is None else _f32(logp, T, "logp"), _f32(stats, (pool.capacity + 1) * MARLAAS_POLICY_STATS, "stats"),
+        ws.data_ptr(), ws.numel(), flags | seg.flags, _stream(stream)))
+    return stats
+
+
+def marlaas_adamw_compact_state_bytes(n: int) -> int:
+    return int(load_library().marlaas_adamw_compact_state_bytes(n))
+
+
+def compact_state(pool: AdapterPool, rank: int):
+    """Zeroed 8-bit moments (state_A, state_B) of one tenant's adapter of the given rank."""
+    widths = pool.parts if pool.parts is not None else [pool.d_out]
+    a = pool.n_parts * marlaas_adamw_compact_state_bytes(pool.d_in * rank)
+    b = sum(marlaas_adamw_compact_state_bytes(rank * w) for w in widths)
+    return tuple(torch.zeros(n, dtype=torch.uint8, device=pool.device) for n in (a, b))
+
+
+class CompactAdamWTables:
+    """The tensors of marlaas_adapter_pool_adamw_compact_commit, one entry per listed tenant: gradients and masters
+    (contiguous fp32) and 8-bit states (contiguous uint8, see compact_state).  Made once for buffers that stay in place from
+    step to step; keeps them alive."""
+
+    def __init__(self, pool: AdapterPool, tenant_ids: Sequence[int], dA, dB, A, B, state_A, state_B):
+        n = self.n = len(tenant_ids)
+        self.tensors = (list(dA), list(dB), list(A), list(B), list(state_A), list(state_B))
+        widths = pool.parts if pool.parts is not None else [pool.d_out]
+        ranks = [marlaas_adapter_pool_lookup(pool, t)[1] for t in tenant_ids]
+        self.tables = []
+        for k, (name, lst) in enumerate(zip(("dA", "dB", "A", "B", "state_A", "state_B"), self.tensors)):
+            assert len(lst) == n, name
+            tab = (ctypes.c_void_p * max(n, 1))()
+            for i, t in enumerate(lst):
+                r = ranks[i]
+                if k < 4:
+                    need = pool.n_parts * pool.d_in * r if k % 2 == 0 else r * pool.d_out
+                    ok = t.dtype == torch.float32 and t.numel() == need
+                else:
+                    need = (pool.n_parts * marlaas_adamw_compact_state_bytes(pool.d_in * r) if k == 4 else
+                            sum(marlaas_adamw_compact_state_bytes(r * w) for w in widths))
+                    ok = t.dtype == torch.uint8 and t.numel() == need
+                assert ok and t.is_contiguous() and t.device == pool.device, f"{name}[{i}]"
+                tab[i] = t.data_ptr()
+            self.tables.append(tab)
+        self.ids = (ctypes.c_uint64 * max(n, 1))(*tenant_ids)
+        self.ranks = (ctypes.c_int32 * max(n, 1))(*ranks)
+
+
+def marlaas_adapter_pool_adamw_compact_commit(pool: AdapterPool, tables: CompactAdamWTables, *, lr: float, beta1: float = 0.9,
+                                              beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
+                                              grad_scale: float = 1.0, step: int = 1, seed: int = 0,
+                                              new_versions: Optional[Sequence[int]] = None, stream=None) -> None:
+    """AdamW with 8-bit moments on the masters of the listed tenants, and commit of their bf16 rounding into the pool.
+    A tenant whose rank has changed since the tables were made is refused."""
+    vers = None if new_versions is None else (ctypes.c_uint64 * max(tables.n, 1))(*new_versions)
+    hp = marlaas_adamw_t(lr, beta1, beta2, eps, weight_decay, grad_scale, step)
+    _check(load_library().marlaas_adapter_pool_adamw_compact_commit(pool.handle, tables.n, tables.ids, vers, *tables.tables,
+                                                                    tables.ranks, ctypes.byref(hp), seed, _stream(stream)))
+
+
+def marlaas_adamw_compact_state_export(pool: AdapterPool, state: torch.Tensor, m: Optional[torch.Tensor] = None,
+                                       v: Optional[torch.Tensor] = None, stream=None):
+    """fp32 (m, v) that the blocks of `state` stand for (256 elements per block, those past a matrix's end are 0)."""
+    assert state.dtype == torch.uint8 and state.is_contiguous() and state.numel() % 528 == 0 and state.device == pool.device
+    blocks = state.numel() // 528
+    if m is None:
+        m = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
+    if v is None:
+        v = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
+    _check(load_library().marlaas_adamw_compact_state_export(pool.handle, blocks, state.data_ptr(), _f32(m, 256 * blocks, "m"),
+                                                             _f32(v, 256 * blocks, "v"), _stream(stream)))
+    return m, v

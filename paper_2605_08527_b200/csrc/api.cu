@@ -67,9 +67,8 @@ static marlaas_status_t check_matrix(const char* fn, const char* name, const voi
 
 // Validates the table argument; for host tables also validates the contents and expands them into
 // host_tok_slot (so that nothing is launched for a malformed table).
-static marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_t T,
-                                       const marlaas_segments_t* seg, uint32_t flags,
-                                       std::vector<int32_t>* host_tok_slot) {
+marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
+                                uint32_t flags, std::vector<int32_t>* host_tok_slot) {
     if (!seg) return fail(MARLAAS_ERR_INVALID_ARG, "%s: segment table is NULL", fn);
     if (seg->num_segments < 0) return fail(MARLAAS_ERR_INVALID_ARG, "%s: negative segment count", fn);
     if (T > 0 && (seg->num_segments == 0 || !seg->seg_offsets || !seg->seg_slot))
@@ -98,9 +97,8 @@ static marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool,
     return MARLAAS_OK;
 }
 
-static marlaas_status_t make_tok_slot(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
-                                      uint32_t flags, const std::vector<int32_t>& host_tok_slot, int32_t* tok_slot,
-                                      cudaStream_t st) {
+marlaas_status_t make_tok_slot(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, uint32_t flags,
+                               const std::vector<int32_t>& host_tok_slot, int32_t* tok_slot, cudaStream_t st) {
     if (T <= 0) return MARLAAS_OK;
     if (flags & MARLAAS_FLAG_HOST_TABLE) {
         // pageable source: the runtime stages it before returning, so the vector may die after this call
@@ -150,7 +148,7 @@ static void set_parts(const marlaas_pool* pool, GemmOperands* o, bool all_parts)
 }
 
 // Host tables are copied from temporaries of the call: a stream capture would keep pointers into them for its replays.
-static marlaas_status_t reject_host_table_in_capture(const char* fn, uint32_t flags, cudaStream_t st) {
+marlaas_status_t reject_host_table_in_capture(const char* fn, uint32_t flags, cudaStream_t st) {
     if (!(flags & MARLAAS_FLAG_HOST_TABLE)) return MARLAAS_OK;
     cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
     MARLAAS_CUDA_TRY(cudaStreamIsCapturing(st, &cs));
@@ -159,7 +157,7 @@ static marlaas_status_t reject_host_table_in_capture(const char* fn, uint32_t fl
     return MARLAAS_OK;
 }
 
-static marlaas_status_t finish(marlaas_pool* pool, uint32_t flags, cudaStream_t st) {
+marlaas_status_t finish(marlaas_pool* pool, uint32_t flags, cudaStream_t st) {
     if (flags & MARLAAS_FLAG_VALIDATE_SYNC) return marlaas_check_status(pool, (void*)st);
     return MARLAAS_OK;
 }

@@ -143,6 +143,14 @@ struct Workspace {
 };
 Workspace carve_workspace(const marlaas_pool* pool, int64_t T, void* base);
 
+// ---- argument checks and table staging (api.cu), shared by the exported calls -------------------------
+marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
+                                uint32_t flags, std::vector<int32_t>* host_tok_slot);
+marlaas_status_t make_tok_slot(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, uint32_t flags,
+                               const std::vector<int32_t>& host_tok_slot, int32_t* tok_slot, cudaStream_t st);
+marlaas_status_t reject_host_table_in_capture(const char* fn, uint32_t flags, cudaStream_t st);
+marlaas_status_t finish(marlaas_pool* pool, uint32_t flags, cudaStream_t st);
+
 // ---- kernels launched by api.cu ---------------------------------------------------------------------
 // plan.cu
 marlaas_status_t launch_tok_slot(const marlaas_pool* pool, int64_t T, int32_t S, const int32_t* seg_offsets,
@@ -249,5 +257,26 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
                                    const float* hg, float* const* out_ptrs, float* const* host_ptrs, bool transpose_out,
                                    bool accumulate, const Workspace& ws, cudaStream_t st, bf16* hm, int phases = GRAD_PHASE_COPIES | GRAD_PHASE_REDUCE);
 // host_ptrs: the same table in host memory; pools of at most 64 slots pass it with the launch and never read out_ptrs
+
+// vocab_rows.cu: one pass over rows of logits (softmax statistics, the policy loss's per-token terms, the gradient)
+struct PolicyTerms {           // what a token adds to its tenant's stats
+    float loss, pg, kl, entropy, ratio, clipped, weight, count;
+};
+struct VocabRows {
+    int64_t T, V;
+    const void* logits; int64_t ld;
+    bool f32;                          // element type: fp32, else bf16
+    const int32_t* targets;
+    float inv_temperature;
+    float* logp;                       // [T] or NULL
+    float* entropy;                    // [T] or NULL
+    // policy loss (terms != NULL)
+    PolicyTerms* terms;                // [T]
+    const float* old_logp; const float* ref_logp; const float* adv; const float* weight;
+    float clip_low, clip_high, kl_coef, entropy_coef, grad_scale;
+    void* dlogits; int64_t lddl;       // NULL = no gradient
+    int32_t* status;
+};
+marlaas_status_t launch_vocab_rows(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st);
 
 }  // namespace marlaas

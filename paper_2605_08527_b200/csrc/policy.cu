@@ -1,0 +1,353 @@
+// The policy update's calls on whole batches (Algorithm 1, training branch; Experimental setup: GRPO): group-relative
+// advantages and token weights from rewards, token log-probabilities, the clipped policy loss.  The passes over the
+// logits are in vocab_rows.cu.
+#include <string.h>
+
+#include <cmath>
+
+#include "internal.cuh"
+
+namespace marlaas {
+
+constexpr int ADV_THREADS = 256;
+
+__device__ __forceinline__ void policy_report(int32_t* status, int code, int detail) {
+    if (atomicCAS(status, 0, code) == 0) status[1] = detail;
+}
+
+struct AdvArgs {
+    int T, S, G, cap;
+    const int32_t* off;
+    const int32_t* slot;
+    const int32_t* group_off;
+    const int32_t* targets;
+    const float* rewards;
+    float eps;
+    int token_mean, no_std;
+    float* seq_adv;     // [S] always written (the caller's or the workspace's)
+    float* adv;
+    float* weight;
+    int32_t* count;     // [S] active tokens
+    int32_t* total;     // [cap + 1] active tokens, or sequences that have any, per bucket
+    int32_t* status;
+};
+
+// First token and end of sequence s, inside [0, T] whatever the table holds.
+__device__ __forceinline__ void seq_range(const AdvArgs& a, int s, int* lo, int* hi) {
+    const int x = a.off[s], y = a.off[s + 1];
+    *lo = min(max(x, 0), a.T);
+    *hi = min(max(y, *lo), a.T);
+}
+
+// One warp per sequence: its active tokens.  Then one warp per group: its sequences' advantages.
+__global__ void __launch_bounds__(ADV_THREADS) k_adv_count(const AdvArgs a) {
+    const int lane = threadIdx.x & 31;
+    const int w = (int)((blockIdx.x * (unsigned)ADV_THREADS + threadIdx.x) >> 5), nw = (int)(gridDim.x * (ADV_THREADS / 32));
+    for (int s = w; s < a.S; s += nw) {
+        int lo, hi;
+        seq_range(a, s, &lo, &hi);
+        if (lane == 0) {
+            const int x = a.off[s], y = a.off[s + 1], t = a.slot[s];
+            if (y < x || x < 0 || y > a.T || (s == 0 && x != 0) || (s == a.S - 1 && y != a.T)) policy_report(a.status, DEV_BAD_TABLE, s);
+            if (t < -1 || t >= a.cap) policy_report(a.status, DEV_BAD_INDEX, s);
+        }
+        int n = 0;
+        for (int i = lo + lane; i < hi; i += 32) n += a.targets[i] >= 0;
+        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+        if (lane == 0) a.count[s] = n;
+    }
+    for (int g = w; g < a.G; g += nw) {
+        const int x = a.group_off[g], y = a.group_off[g + 1];
+        if (lane == 0 && (y < x || x < 0 || y > a.S || (g == 0 && x != 0) || (g == a.G - 1 && y != a.S)))
+            policy_report(a.status, DEV_BAD_TABLE, -10 - g);
+        const int lo = min(max(x, 0), a.S), hi = min(max(y, lo), a.S);
+        if (hi <= lo) continue;
+        // differences to the group's first reward: rewards that are all alike give exact zeros
+        const float r0 = a.rewards[lo], n = (float)(hi - lo);
+        float sum = 0.f;
+        for (int i = lo + lane; i < hi; i += 32) sum += a.rewards[i] - r0;
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float mean = sum / n;
+        float sq = 0.f;
+        if (!a.no_std) {
+            for (int i = lo + lane; i < hi; i += 32) {
+                const float d = (a.rewards[i] - r0) - mean;
+                sq += d * d;
+            }
+            for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+        }
+        const float sd = sqrtf(sq / n);
+        for (int i = lo + lane; i < hi; i += 32) {
+            const float d = (a.rewards[i] - r0) - mean;
+            a.seq_adv[i] = a.no_std ? d : (d == 0.f ? 0.f : d / (sd + a.eps));      // (eps may be 0)
+        }
+    }
+}
+
+// Totals per bucket: integer sums, so their order does not matter.
+__global__ void __launch_bounds__(1024) k_adv_totals(const AdvArgs a) {
+    for (int b = threadIdx.x; b <= a.cap; b += 1024) a.total[b] = 0;
+    __syncthreads();
+    for (int s = threadIdx.x; s < a.S; s += 1024) {
+        const int t = a.slot[s], n = a.count[s];
+        if (n) atomicAdd(a.total + (t < 0 || t >= a.cap ? a.cap : t), a.token_mean ? n : 1);
+    }
+}
+
+// One CTA per sequence in turn: its tokens' advantages and weights.
+__global__ void __launch_bounds__(ADV_THREADS) k_adv_expand(const AdvArgs a) {
+    for (int s = blockIdx.x; s < a.S; s += gridDim.x) {
+        int lo, hi;
+        seq_range(a, s, &lo, &hi);
+        const int t = a.slot[s], n = a.count[s];
+        const float total = (float)a.total[t < 0 || t >= a.cap ? a.cap : t];
+        const float w = n == 0 ? 0.f : 1.f / (a.token_mean ? total : total * (float)n), v = a.seq_adv[s];
+        for (int i = lo + threadIdx.x; i < hi; i += ADV_THREADS) {
+            const bool on = a.targets[i] >= 0;
+            if (a.adv) a.adv[i] = on ? v : 0.f;
+            if (a.weight) a.weight[i] = on ? w : 0.f;
+        }
+    }
+}
+
+// One CTA per bucket sums its tokens' terms, every thread its own tokens in ascending order, then a fixed tree.
+__global__ void __launch_bounds__(1024) k_policy_stats(int64_t T, int cap, const int32_t* __restrict__ tok_slot,
+                                                       const PolicyTerms* __restrict__ terms, float* __restrict__ stats,
+                                                       int accumulate) {
+    __shared__ float s_sum[32][MARLAAS_POLICY_STATS];
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    float v[MARLAAS_POLICY_STATS] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int64_t i = tid; i < T; i += 1024) {
+        const int t = tok_slot[i];
+        if ((t < 0 || t >= cap ? cap : t) != b) continue;
+        const float4 x = reinterpret_cast<const float4*>(terms + i)[0], y = reinterpret_cast<const float4*>(terms + i)[1];
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+    }
+#pragma unroll
+    for (int k = 0; k < MARLAAS_POLICY_STATS; ++k)
+        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    if (lane == 0)
+#pragma unroll
+        for (int k = 0; k < MARLAAS_POLICY_STATS; ++k) s_sum[warp][k] = v[k];
+    __syncthreads();
+    if (tid < MARLAAS_POLICY_STATS) {
+        float x = 0.f;
+        for (int w = 0; w < 32; ++w) x += s_sum[w][tid];
+        float* out = stats + (size_t)b * MARLAAS_POLICY_STATS + tid;
+        *out = accumulate ? *out + x : x;
+    }
+}
+
+// Workspace of the two calls that need one.
+struct PolicyWorkspace {
+    PolicyTerms* terms;     // [T]
+    int32_t* tok_slot;      // [T]
+    int32_t* off;           // [S + 1] host tables, staged
+    int32_t* slot;          // [S]
+    int32_t* group_off;     // [G + 1]
+    int32_t* count;         // [S]
+    int32_t* total;         // [cap + 1]
+    float* seq_adv;         // [S]
+    size_t total_bytes;
+};
+static PolicyWorkspace carve_policy(const marlaas_pool* pool, int64_t T, int32_t S, int32_t G, void* base) {
+    PolicyWorkspace w;
+    char* p = (char*)base;
+    size_t o = 0;
+    auto take = [&](size_t bytes) { char* q = p ? p + o : nullptr; o += align_up(bytes, 256); return q; };
+    w.terms = (PolicyTerms*)take(sizeof(PolicyTerms) * (size_t)T);
+    w.tok_slot = (int32_t*)take(sizeof(int32_t) * (size_t)T);
+    w.off = (int32_t*)take(sizeof(int32_t) * ((size_t)S + 1));
+    w.slot = (int32_t*)take(sizeof(int32_t) * (size_t)S);
+    w.group_off = (int32_t*)take(sizeof(int32_t) * ((size_t)G + 1));
+    w.count = (int32_t*)take(sizeof(int32_t) * (size_t)S);
+    w.total = (int32_t*)take(sizeof(int32_t) * ((size_t)pool->cap + 1));
+    w.seq_adv = (float*)take(sizeof(float) * (size_t)S);
+    w.total_bytes = o;
+    return w;
+}
+
+static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+
+static marlaas_status_t check_rows(const char* fn, const char* name, const void* p, int64_t ld, int64_t V, int32_t dtype) {
+    const int64_t per16 = dtype == MARLAAS_DTYPE_F32 ? 4 : 8;
+    if (!p || misaligned(p, 16)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: %s is NULL or not 16-byte aligned", fn, name);
+    if (ld < V || ld % per16 != 0 || ld >= (1ll << 31))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: leading dimension of %s (%lld) must be >= %lld and a multiple of %lld", fn, name,
+                    (long long)ld, (long long)V, (long long)per16);
+    return MARLAAS_OK;
+}
+
+// The arguments that token_logprobs and policy_loss have in common.
+static marlaas_status_t check_logits(const char* fn, const marlaas_pool* pool, int64_t T, int64_t V, const void* logits,
+                                     int64_t ld, int32_t dtype, const int32_t* targets, float inv_temperature) {
+    if (!pool) return fail(MARLAAS_ERR_INVALID_ARG, "%s: pool is NULL", fn);
+    if (T < 0 || T >= (1ll << 31)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: T out of range", fn);
+    if (V < 1 || V > MARLAAS_MAX_VOCABULARY)
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: V = %lld outside [1, %d]", fn, (long long)V, (int)MARLAAS_MAX_VOCABULARY);
+    if (dtype != MARLAAS_DTYPE_BF16 && dtype != MARLAAS_DTYPE_F32) return fail(MARLAAS_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, (int)dtype);
+    if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: inv_temperature must be positive and finite", fn);
+    if (T == 0) return MARLAAS_OK;
+    if (!targets || misaligned(targets, 4)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: targets is NULL or misaligned", fn);
+    return check_rows(fn, "logits", logits, ld, V, dtype);
+}
+
+}  // namespace marlaas
+
+using namespace marlaas;
+
+extern "C" {
+
+size_t marlaas_policy_workspace_bytes(const marlaas_pool_t* pool, int64_t T, int32_t num_segments, int32_t num_groups) {
+    if (!pool || T < 0 || T >= (1ll << 31) || num_segments < 0 || num_groups < 0) return 0;
+    return carve_policy(pool, T, num_segments, num_groups, nullptr).total_bytes;
+}
+
+marlaas_status_t marlaas_group_advantages(marlaas_pool_t* pool, int64_t T, const marlaas_segments_t* seg, const float* rewards,
+                                          int32_t num_groups, const int32_t* group_offsets, const int32_t* targets, float eps,
+                                          float* seq_adv, float* adv, float* weight, void* workspace, size_t workspace_bytes,
+                                          uint32_t flags, void* cuda_stream) try {
+    const char* fn = "group_advantages";
+    if (!pool) return fail(MARLAAS_ERR_INVALID_ARG, "%s: pool is NULL", fn);
+    if (T < 0 || T >= (1ll << 31)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: T out of range", fn);
+    if (flags & ~(uint32_t)(MARLAAS_FLAG_HOST_TABLE | MARLAAS_FLAG_VALIDATE_SYNC | MARLAAS_FLAG_TOKEN_MEAN | MARLAAS_FLAG_NO_STD))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: a flag does not apply to this call", fn);
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: eps must be finite and not negative", fn);
+    std::vector<int32_t> host_ts;
+    marlaas_status_t rc = check_segments(fn, pool, T, seg, flags, &host_ts);
+    if (rc != MARLAAS_OK) return rc;
+    const int32_t S = seg->num_segments;
+    if (num_groups < 0) return fail(MARLAAS_ERR_INVALID_ARG, "%s: negative group count", fn);
+    if (S > 0 && (num_groups == 0 || !group_offsets))
+        return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: empty group table for %d sequences", fn, S);
+    if (S > 0 && (!seg->seg_offsets || !seg->seg_slot)) return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: segment arrays are NULL", fn);
+    const bool host = (flags & MARLAAS_FLAG_HOST_TABLE) != 0;
+    if (host && S > 0) {
+        if (group_offsets[0] != 0 || group_offsets[num_groups] != S)
+            return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: group_offsets must run from 0 to %d", fn, S);
+        for (int32_t g = 0; g < num_groups; ++g)
+            if (group_offsets[g + 1] < group_offsets[g])
+                return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: group_offsets decreases at group %d", fn, g);
+    }
+    if (S > 0 && (!rewards || misaligned(rewards, 4))) return fail(MARLAAS_ERR_INVALID_ARG, "%s: rewards is NULL or misaligned", fn);
+    if (T > 0 && (!targets || misaligned(targets, 4))) return fail(MARLAAS_ERR_INVALID_ARG, "%s: targets is NULL or misaligned", fn);
+    if (misaligned(seq_adv, 4) || misaligned(adv, 4) || misaligned(weight, 4))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: an output is misaligned", fn);
+    if (S == 0) return MARLAAS_OK;
+    if (!workspace || misaligned(workspace, 256)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: workspace NULL or misaligned", fn);
+    const PolicyWorkspace ws = carve_policy(pool, T, S, num_groups, workspace);
+    if (workspace_bytes < ws.total_bytes)
+        return fail(MARLAAS_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < required %zu", fn, workspace_bytes, ws.total_bytes);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
+    if ((rc = reject_host_table_in_capture(fn, flags, st)) != MARLAAS_OK) return rc;
+    AdvArgs a;
+    a.T = (int)T; a.S = S; a.G = num_groups; a.cap = pool->cap;
+    a.off = seg->seg_offsets; a.slot = seg->seg_slot; a.group_off = group_offsets;
+    if (host) {
+        // pageable sources: the runtime stages them before returning
+        MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.off, seg->seg_offsets, sizeof(int32_t) * ((size_t)S + 1), cudaMemcpyHostToDevice, st));
+        MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.slot, seg->seg_slot, sizeof(int32_t) * (size_t)S, cudaMemcpyHostToDevice, st));
+        MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.group_off, group_offsets, sizeof(int32_t) * ((size_t)num_groups + 1),
+                                         cudaMemcpyHostToDevice, st));
+        a.off = ws.off; a.slot = ws.slot; a.group_off = ws.group_off;
+    }
+    a.targets = targets; a.rewards = rewards; a.eps = eps;
+    a.token_mean = (flags & MARLAAS_FLAG_TOKEN_MEAN) != 0; a.no_std = (flags & MARLAAS_FLAG_NO_STD) != 0;
+    a.seq_adv = seq_adv ? seq_adv : ws.seq_adv;
+    a.adv = adv; a.weight = weight; a.count = ws.count; a.total = ws.total; a.status = pool->d_status;
+    const int64_t warps = std::max(S, num_groups);
+    k_adv_count<<<(unsigned)std::min<int64_t>(cdiv(warps, ADV_THREADS / 32), (int64_t)pool->sm_count * 8), ADV_THREADS, 0, st>>>(a);
+    MARLAAS_LAUNCH_CHECK("k_adv_count");
+    if (adv || weight) {
+        k_adv_totals<<<1, 1024, 0, st>>>(a);
+        MARLAAS_LAUNCH_CHECK("k_adv_totals");
+        k_adv_expand<<<(unsigned)std::min<int64_t>(S, (int64_t)pool->sm_count * 8), ADV_THREADS, 0, st>>>(a);
+        MARLAAS_LAUNCH_CHECK("k_adv_expand");
+    }
+    return finish(pool, flags, st);
+} catch (const std::exception& e) {
+    return fail(MARLAAS_ERR_INVALID_ARG, "group_advantages: %s", e.what());
+}
+
+marlaas_status_t marlaas_token_logprobs(marlaas_pool_t* pool, int64_t T, int64_t V, const void* logits, int64_t ld, int32_t dtype,
+                                        const int32_t* targets, float inv_temperature, float* logp, float* entropy,
+                                        uint32_t flags, void* cuda_stream) {
+    const char* fn = "token_logprobs";
+    marlaas_status_t rc = check_logits(fn, pool, T, V, logits, ld, dtype, targets, inv_temperature);
+    if (rc != MARLAAS_OK) return rc;
+    if (flags & ~(uint32_t)MARLAAS_FLAG_VALIDATE_SYNC) return fail(MARLAAS_ERR_INVALID_ARG, "%s: a flag does not apply to this call", fn);
+    if (T == 0) return MARLAAS_OK;
+    if (!logp || misaligned(logp, 4) || misaligned(entropy, 4))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: logp is NULL or an output is misaligned", fn);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
+    VocabRows r;
+    memset(&r, 0, sizeof(r));
+    r.T = T; r.V = V; r.logits = logits; r.ld = ld; r.f32 = dtype == MARLAAS_DTYPE_F32;
+    r.targets = targets; r.inv_temperature = inv_temperature; r.logp = logp; r.entropy = entropy; r.status = pool->d_status;
+    if ((rc = launch_vocab_rows(pool, r, st)) != MARLAAS_OK) return rc;
+    return finish(pool, flags, st);
+}
+
+marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V, const void* logits, int64_t ld, int32_t dtype,
+                                     const int32_t* targets, const marlaas_segments_t* seg, const float* old_logp,
+                                     const float* ref_logp, const float* adv, const float* weight,
+                                     const marlaas_policy_loss_t* hp, void* dlogits, int64_t lddl, float* logp, float* stats,
+                                     void* workspace, size_t workspace_bytes, uint32_t flags, void* cuda_stream) try {
+    const char* fn = "policy_loss";
+    if (!hp) return fail(MARLAAS_ERR_INVALID_ARG, "%s: the loss's parameters are NULL", fn);
+    marlaas_status_t rc = check_logits(fn, pool, T, V, logits, ld, dtype, targets, hp->inv_temperature);
+    if (rc != MARLAAS_OK) return rc;
+    if (flags & ~(uint32_t)(MARLAAS_FLAG_HOST_TABLE | MARLAAS_FLAG_VALIDATE_SYNC | MARLAAS_FLAG_ACCUMULATE))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: a flag does not apply to this call", fn);
+    if (!(hp->clip_low >= 0.f) || !(hp->clip_high >= 0.f))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: clip_low and clip_high must not be negative", fn);
+    if (!std::isfinite(hp->kl_coef) || !std::isfinite(hp->entropy_coef) || !std::isfinite(hp->grad_scale))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: a coefficient is not finite", fn);
+    if (!stats || misaligned(stats, 4) || misaligned(logp, 4)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: stats is NULL or an output is misaligned", fn);
+    std::vector<int32_t> host_ts;
+    if ((rc = check_segments(fn, pool, T, seg, flags, &host_ts)) != MARLAAS_OK) return rc;
+    const bool accumulate = (flags & MARLAAS_FLAG_ACCUMULATE) != 0;
+    PolicyWorkspace ws;
+    memset(&ws, 0, sizeof(ws));
+    if (T > 0) {
+        if (!old_logp || !adv || !weight || misaligned(old_logp, 4) || misaligned(adv, 4) || misaligned(weight, 4) || misaligned(ref_logp, 4))
+            return fail(MARLAAS_ERR_INVALID_ARG, "%s: old_logp, adv or weight is NULL, or an input is misaligned", fn);
+        if (!ref_logp && hp->kl_coef != 0.f) return fail(MARLAAS_ERR_INVALID_ARG, "%s: ref_logp is NULL although kl_coef is not 0", fn);
+        if (dlogits) {
+            if ((rc = check_rows(fn, "dlogits", dlogits, lddl, V, dtype)) != MARLAAS_OK) return rc;
+            const size_t e = dtype == MARLAAS_DTYPE_F32 ? 4 : 2;
+            const uintptr_t z0 = (uintptr_t)logits, z1 = z0 + ((size_t)(T - 1) * ld + V) * e;
+            const uintptr_t d0 = (uintptr_t)dlogits, d1 = d0 + ((size_t)(T - 1) * lddl + V) * e;
+            if (d0 < z1 && z0 < d1 && !(d0 == z0 && lddl == ld))
+                return fail(MARLAAS_ERR_INVALID_ARG, "%s: dlogits overlaps logits without being the same matrix", fn);
+        }
+        if (!workspace || misaligned(workspace, 256)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: workspace NULL or misaligned", fn);
+        ws = carve_policy(pool, T, seg->num_segments, 0, workspace);
+        if (workspace_bytes < ws.total_bytes)
+            return fail(MARLAAS_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < required %zu", fn, workspace_bytes, ws.total_bytes);
+    }
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
+    if ((rc = reject_host_table_in_capture(fn, flags, st)) != MARLAAS_OK) return rc;
+    if (T > 0) {
+        if ((rc = make_tok_slot(pool, T, seg, flags, host_ts, ws.tok_slot, st)) != MARLAAS_OK) return rc;
+        VocabRows r;
+        memset(&r, 0, sizeof(r));
+        r.T = T; r.V = V; r.logits = logits; r.ld = ld; r.f32 = dtype == MARLAAS_DTYPE_F32;
+        r.targets = targets; r.inv_temperature = hp->inv_temperature; r.logp = logp; r.terms = ws.terms;
+        r.old_logp = old_logp; r.ref_logp = ref_logp; r.adv = adv; r.weight = weight;
+        r.clip_low = hp->clip_low; r.clip_high = hp->clip_high; r.kl_coef = hp->kl_coef; r.entropy_coef = hp->entropy_coef;
+        r.grad_scale = hp->grad_scale; r.dlogits = dlogits; r.lddl = lddl; r.status = pool->d_status;
+        if ((rc = launch_vocab_rows(pool, r, st)) != MARLAAS_OK) return rc;
+    }
+    k_policy_stats<<<(unsigned)(pool->cap + 1), 1024, 0, st>>>(T, pool->cap, ws.tok_slot, ws.terms, stats, accumulate);
+    MARLAAS_LAUNCH_CHECK("k_policy_stats");
+    return finish(pool, flags, st);
+} catch (const std::exception& e) {
+    return fail(MARLAAS_ERR_INVALID_ARG, "policy_loss: %s", e.what());
+}
+
+}  // extern "C"
