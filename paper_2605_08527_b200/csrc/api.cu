@@ -97,8 +97,9 @@ marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_
     return MARLAAS_OK;
 }
 
-marlaas_status_t make_tok_slot(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, uint32_t flags,
-                               const std::vector<int32_t>& host_tok_slot, int32_t* tok_slot, cudaStream_t st) {
+static marlaas_status_t make_tok_slot(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
+                                      uint32_t flags, const std::vector<int32_t>& host_tok_slot, int32_t* tok_slot,
+                                      cudaStream_t st) {
     if (T <= 0) return MARLAAS_OK;
     if (flags & MARLAAS_FLAG_HOST_TABLE) {
         // pageable source: the runtime stages it before returning, so the vector may die after this call

@@ -146,8 +146,6 @@ Workspace carve_workspace(const marlaas_pool* pool, int64_t T, void* base);
 // ---- argument checks and table staging (api.cu), shared by the exported calls -------------------------
 marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
                                 uint32_t flags, std::vector<int32_t>* host_tok_slot);
-marlaas_status_t make_tok_slot(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, uint32_t flags,
-                               const std::vector<int32_t>& host_tok_slot, int32_t* tok_slot, cudaStream_t st);
 marlaas_status_t reject_host_table_in_capture(const char* fn, uint32_t flags, cudaStream_t st);
 marlaas_status_t finish(marlaas_pool* pool, uint32_t flags, cudaStream_t st);
 

@@ -5,7 +5,7 @@
 
 #include <cmath>
 
-#include "internal.cuh"
+#include "sm100_cluster.cuh"
 
 namespace marlaas {
 
@@ -110,15 +110,36 @@ __global__ void __launch_bounds__(ADV_THREADS) k_adv_expand(const AdvArgs a) {
     }
 }
 
-// One CTA per bucket sums its tokens' terms, every thread its own tokens in ascending order, then a fixed tree.
-__global__ void __launch_bounds__(1024) k_policy_stats(int64_t T, int cap, const int32_t* __restrict__ tok_slot,
-                                                       const PolicyTerms* __restrict__ terms, float* __restrict__ stats,
-                                                       int accumulate) {
+// One CTA per bucket sums its tokens' terms, every thread its own tokens in ascending order, then a fixed tree.  A token's
+// segment is found by bisection, in a copy of the offsets in shared memory where they fit.
+constexpr int STATS_THREADS = 1024, STATS_OFFSETS = 4096;
+__global__ void __launch_bounds__(STATS_THREADS) k_policy_stats(int T, int S, int cap, const int32_t* __restrict__ seg_offsets,
+                                                                const int32_t* __restrict__ seg_slot, const PolicyTerms* __restrict__ terms,
+                                                                float* __restrict__ stats, int accumulate, int32_t* status) {
     __shared__ float s_sum[32][MARLAAS_POLICY_STATS];
+    __shared__ int32_t s_off[STATS_OFFSETS];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // launched while the rows kernel runs: the tables are there, the terms are not
+    const bool cached = S < STATS_OFFSETS;
+    for (int s = tid; s < S; s += STATS_THREADS) {
+        const int x = seg_offsets[s], y = seg_offsets[s + 1], t = seg_slot[s];
+        if (cached) s_off[s] = x;
+        if (b == 0) {
+            if (y < x || x < 0 || y > T || (s == 0 && x != 0) || (s == S - 1 && y != T)) policy_report(status, DEV_BAD_TABLE, s);
+            if (t < -1 || t >= cap) policy_report(status, DEV_BAD_INDEX, s);
+        }
+    }
+    __syncthreads();
+    sm100::dk_wait_prerequisites();
+    const int32_t* off = cached ? s_off : seg_offsets;
     float v[MARLAAS_POLICY_STATS] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int64_t i = tid; i < T; i += 1024) {
-        const int t = tok_slot[i];
+    for (int i = tid; i < T; i += STATS_THREADS) {
+        int lo = 0, hi = S;         // segments that begin at or before the token: the last of them holds it
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (off[mid] <= i) lo = mid + 1; else hi = mid;
+        }
+        const int t = lo > 0 ? seg_slot[lo - 1] : -1;
         if ((t < 0 || t >= cap ? cap : t) != b) continue;
         const float4 x = reinterpret_cast<const float4*>(terms + i)[0], y = reinterpret_cast<const float4*>(terms + i)[1];
         v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
@@ -141,7 +162,6 @@ __global__ void __launch_bounds__(1024) k_policy_stats(int64_t T, int cap, const
 // Workspace of the two calls that need one.
 struct PolicyWorkspace {
     PolicyTerms* terms;     // [T]
-    int32_t* tok_slot;      // [T]
     int32_t* off;           // [S + 1] host tables, staged
     int32_t* slot;          // [S]
     int32_t* group_off;     // [G + 1]
@@ -156,7 +176,6 @@ static PolicyWorkspace carve_policy(const marlaas_pool* pool, int64_t T, int32_t
     size_t o = 0;
     auto take = [&](size_t bytes) { char* q = p ? p + o : nullptr; o += align_up(bytes, 256); return q; };
     w.terms = (PolicyTerms*)take(sizeof(PolicyTerms) * (size_t)T);
-    w.tok_slot = (int32_t*)take(sizeof(int32_t) * (size_t)T);
     w.off = (int32_t*)take(sizeof(int32_t) * ((size_t)S + 1));
     w.slot = (int32_t*)take(sizeof(int32_t) * (size_t)S);
     w.group_off = (int32_t*)take(sizeof(int32_t) * ((size_t)G + 1));
@@ -165,6 +184,17 @@ static PolicyWorkspace carve_policy(const marlaas_pool* pool, int64_t T, int32_t
     w.seq_adv = (float*)take(sizeof(float) * (size_t)S);
     w.total_bytes = o;
     return w;
+}
+
+// Host tables into the workspace (pageable sources: the runtime stages them before it returns).
+static marlaas_status_t stage_segments(const marlaas_segments_t* seg, const PolicyWorkspace& ws, const int32_t** off,
+                                       const int32_t** slot, cudaStream_t st) {
+    const size_t S = (size_t)seg->num_segments;
+    MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.off, seg->seg_offsets, sizeof(int32_t) * (S + 1), cudaMemcpyHostToDevice, st));
+    MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.slot, seg->seg_slot, sizeof(int32_t) * S, cudaMemcpyHostToDevice, st));
+    *off = ws.off;
+    *slot = ws.slot;
+    return MARLAAS_OK;
 }
 
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
@@ -246,12 +276,10 @@ marlaas_status_t marlaas_group_advantages(marlaas_pool_t* pool, int64_t T, const
     a.T = (int)T; a.S = S; a.G = num_groups; a.cap = pool->cap;
     a.off = seg->seg_offsets; a.slot = seg->seg_slot; a.group_off = group_offsets;
     if (host) {
-        // pageable sources: the runtime stages them before returning
-        MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.off, seg->seg_offsets, sizeof(int32_t) * ((size_t)S + 1), cudaMemcpyHostToDevice, st));
-        MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.slot, seg->seg_slot, sizeof(int32_t) * (size_t)S, cudaMemcpyHostToDevice, st));
+        if ((rc = stage_segments(seg, ws, &a.off, &a.slot, st)) != MARLAAS_OK) return rc;
         MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.group_off, group_offsets, sizeof(int32_t) * ((size_t)num_groups + 1),
                                          cudaMemcpyHostToDevice, st));
-        a.off = ws.off; a.slot = ws.slot; a.group_off = ws.group_off;
+        a.group_off = ws.group_off;
     }
     a.targets = targets; a.rewards = rewards; a.eps = eps;
     a.token_mean = (flags & MARLAAS_FLAG_TOKEN_MEAN) != 0; a.no_std = (flags & MARLAAS_FLAG_NO_STD) != 0;
@@ -307,6 +335,8 @@ marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V,
     if (!std::isfinite(hp->kl_coef) || !std::isfinite(hp->entropy_coef) || !std::isfinite(hp->grad_scale))
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: a coefficient is not finite", fn);
     if (!stats || misaligned(stats, 4) || misaligned(logp, 4)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: stats is NULL or an output is misaligned", fn);
+    if (logp && (logp == old_logp || logp == ref_logp || logp == adv || logp == weight))
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: logp must not be one of the inputs", fn);
     std::vector<int32_t> host_ts;
     if ((rc = check_segments(fn, pool, T, seg, flags, &host_ts)) != MARLAAS_OK) return rc;
     const bool accumulate = (flags & MARLAAS_FLAG_ACCUMULATE) != 0;
@@ -332,8 +362,9 @@ marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V,
     cudaStream_t st = (cudaStream_t)cuda_stream;
     MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
     if ((rc = reject_host_table_in_capture(fn, flags, st)) != MARLAAS_OK) return rc;
+    const int32_t *off = seg->seg_offsets, *slot = seg->seg_slot;
     if (T > 0) {
-        if ((rc = make_tok_slot(pool, T, seg, flags, host_ts, ws.tok_slot, st)) != MARLAAS_OK) return rc;
+        if ((flags & MARLAAS_FLAG_HOST_TABLE) && (rc = stage_segments(seg, ws, &off, &slot, st)) != MARLAAS_OK) return rc;
         VocabRows r;
         memset(&r, 0, sizeof(r));
         r.T = T; r.V = V; r.logits = logits; r.ld = ld; r.f32 = dtype == MARLAAS_DTYPE_F32;
@@ -343,7 +374,18 @@ marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V,
         r.grad_scale = hp->grad_scale; r.dlogits = dlogits; r.lddl = lddl; r.status = pool->d_status;
         if ((rc = launch_vocab_rows(pool, r, st)) != MARLAAS_OK) return rc;
     }
-    k_policy_stats<<<(unsigned)(pool->cap + 1), 1024, 0, st>>>(T, pool->cap, ws.tok_slot, ws.terms, stats, accumulate);
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)(pool->cap + 1));
+    cfg.blockDim = dim3(STATS_THREADS);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_policy_stats, (int)T, T > 0 ? (int)seg->num_segments : 0, (int)pool->cap, off, slot,
+                                        (const PolicyTerms*)ws.terms, stats, (int)accumulate, pool->d_status));
     MARLAAS_LAUNCH_CHECK("k_policy_stats");
     return finish(pool, flags, st);
 } catch (const std::exception& e) {

@@ -2,13 +2,17 @@
 // (Algorithm 1: "PolicyUpdate"; Experimental setup: GRPO).  With z the row, k = inv_temperature:
 //     m = max z    s = sum exp((z - m) k)    logp = (z_a - m) k - log s    H = log s - sum p (z - m) k
 //     dz_j = g ( p_j (c_H (log p_j + H) - c) + [j = a] c ),   g = grad_scale w k,   c = d(pg + kl_coef kl) / d logp
-#include <math_constants.h>
+#include <math.h>
+#include <string.h>
 
-#include "sm100_ptx.cuh"
+#include <atomic>
+
+#include "sm100_cluster.cuh"
 
 namespace marlaas {
+using namespace sm100;
 
-constexpr int VR_THREADS = 512;
+constexpr int MAX_DEVICES = 16;
 constexpr float VR_LOG2E = 1.4426950408889634f, VR_LN2 = 0.6931471805599453f;
 
 // max that keeps a NaN (fmaxf drops it): a bad logit has to show in the row's outputs
@@ -23,44 +27,22 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 // The reference point of a running maximum: 0 while there is no finite logit, so that -inf - m stays -inf.
-__device__ __forceinline__ float ref_of(float m) { return m == -CUDART_INF_F ? 0.f : m; }
+__device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
 // (z - m) k in units of log 2, not below -200: 2^-200 is 0 in fp32, and a product with it stays 0 where (z - m) k itself is
 // -inf.  The difference comes first: z k alone may leave fp32's range where a mask is the type's lowest value.
 __device__ __forceinline__ float exponent(float z, float m, float k2) { return max_nan((z - m) * k2, -200.f); }
-
-struct RowStats {       // running statistics of a part of a row, relative to its own maximum
-    float m, s, u;      // u = sum 2^t t, t = exponent of each element
-};
-__device__ __forceinline__ RowStats merge(RowStats a, RowStats b, float k2) {
-    RowStats r;
-    r.m = max_nan(a.m, b.m);
-    const float mr = ref_of(r.m);
-    const float da = exponent(a.m, mr, k2), db = exponent(b.m, mr, k2);
-    const float fa = ex2(da), fb = ex2(db);
-    r.s = fa * a.s + fb * b.s;
-    r.u = fa * (a.u + a.s * da) + fb * (b.u + b.s * db);
-    return r;
-}
 
 template <bool F32>
 struct Vec;
 template <>
 struct Vec<false> {     // 8 bf16 in 16 bytes
     static constexpr int N = 8;
-    static __device__ __forceinline__ void unpack(uint4 q, float (&f)[8]) {
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    }
-    static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+    static __device__ __forceinline__ uint4 pack(const float2 (&f)[4]) {
         uint4 q;
         uint32_t* w = &q.x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+            __nv_bfloat162 p = __floats2bfloat162_rn(f[i].x, f[i].y);
             w[i] = *reinterpret_cast<uint32_t*>(&p);
         }
         return q;
@@ -71,11 +53,8 @@ struct Vec<false> {     // 8 bf16 in 16 bytes
 template <>
 struct Vec<true> {
     static constexpr int N = 4;
-    static __device__ __forceinline__ void unpack(uint4 q, float (&f)[4]) {
-        f[0] = __uint_as_float(q.x); f[1] = __uint_as_float(q.y); f[2] = __uint_as_float(q.z); f[3] = __uint_as_float(q.w);
-    }
-    static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
-        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    static __device__ __forceinline__ uint4 pack(const float2 (&f)[2]) {
+        return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
     }
     static __device__ __forceinline__ float load(const void* p, int64_t i) { return ((const float*)p)[i]; }
     static __device__ __forceinline__ void store(void* p, int64_t i, float v) { ((float*)p)[i] = v; }
@@ -86,10 +65,15 @@ struct RowGrad {
     float alpha, beta, gamma;
 };
 
+// A token's inputs of the loss, loaded while its row is on the way.
+struct TokenIn {
+    float old, ref, A, w;
+};
+
 // The token's loss terms from its log-probability and entropy; the coefficients of its gradient.
-__device__ __forceinline__ RowGrad token_terms(const VocabRows& a, int64_t i, float logp, float H, float log2s, PolicyTerms* out) {
-    const float w = a.weight[i], A = a.adv[i];
-    const float ratio = expf(logp - a.old_logp[i]);
+__device__ __forceinline__ RowGrad token_terms(const VocabRows& a, const TokenIn& in, float logp, float H, float log2s, PolicyTerms* out) {
+    const float w = in.w, A = in.A;
+    const float ratio = expf(logp - in.old);
     // 0 A is 0 whatever the ratio
     const float plain = A == 0.f ? 0.f : ratio * A;
     const float clipped = A == 0.f ? 0.f : fminf(fmaxf(ratio, 1.f - a.clip_low), 1.f + a.clip_high) * A;
@@ -97,7 +81,7 @@ __device__ __forceinline__ RowGrad token_terms(const VocabRows& a, int64_t i, fl
     const float pg = -(is_clipped ? clipped : plain);
     float c = is_clipped ? 0.f : -plain, kl = 0.f;
     if (a.kl_coef != 0.f) {
-        const float d = a.ref_logp[i] - logp, e1 = expm1f(d);     // exp(d) - d - 1 without its cancellation for small d
+        const float d = in.ref - logp, e1 = expm1f(d);     // exp(d) - d - 1 without its cancellation for small d
         kl = e1 - d;
         c -= a.kl_coef * e1;
     }
@@ -117,115 +101,363 @@ __device__ __forceinline__ RowGrad token_terms(const VocabRows& a, int64_t i, fl
     return r;
 }
 
-// One CTA per row, which is read twice: statistics, then the gradient.
+// Element i of a 16-byte vector, and the maximum of a vector's elements.
 template <bool F32>
-__global__ void __launch_bounds__(VR_THREADS) k_vocab_rows(const VocabRows a) {
+__device__ __forceinline__ float element(const uint4& q, int i) {
+    const uint32_t* w = &q.x;
+    if constexpr (F32) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+}
+template <bool F32>
+__device__ __forceinline__ float2 pair_of(const uint4& q, int i) { return make_float2(element<F32>(q, i), element<F32>(q, i + 1)); }
+template <bool F32>
+__device__ __forceinline__ float max_of(const uint4& q) {
+    float m = element<F32>(q, 0);
+#pragma unroll
+    for (int i = 1; i < (F32 ? 4 : 8); ++i) m = max_nan(m, element<F32>(q, i));
+    return m;
+}
+
+// ---- the kernel ----
+// A cluster of C CTAs (one CTA for most vocabularies) takes a row, a slice each, and keeps it in registers, as the 16-byte
+// vectors it was loaded in, between the statistics and the gradient: the row crosses HBM once in each direction and needs
+// neither shared memory nor a second read.  As the gradient's vectors leave their registers, the next row's are loaded into
+// them.  The warps of a row do not wait for one another except here: each publishes its statistics (to all CTAs of the
+// cluster), then every warp merges all of them.
+struct RowsLayout {
+    int32_t C;              // CTAs per row
+    int64_t slice;          // elements per CTA (whole vectors)
+};
+
+__device__ __forceinline__ void send_stats(uint32_t dst, uint32_t bar, float m, float s, float u, float z) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(dst),
+                 "r"(__float_as_uint(m)), "r"(__float_as_uint(s)), "r"(__float_as_uint(u)), "r"(__float_as_uint(z)), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return x;
+}
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// Whether a row's logits are needed: it has a valid target, and its loss (a token of weight 0 contributes nothing) or an
+// output of its own is wanted.
+__device__ __forceinline__ bool row_read(const VocabRows& a, int32_t target, float weight) {
+    return (target >= 0) & (target < a.V) & ((a.logp != nullptr) | (a.entropy != nullptr) | (weight != 0.f));
+}
+
+template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD, int NT, int VPT, bool CLUSTER>
+__global__ void __launch_bounds__(NT, 8192 / (NT * VPT) > 32 ? 32 : 8192 / (NT * VPT)) k_vocab_rows(const VocabRows a, const RowsLayout lay) {
     using X = Vec<F32>;
-    constexpr int E = F32 ? 4 : 2;
-    __shared__ RowStats s_part[VR_THREADS / 32];
-    __shared__ RowGrad s_grad;
-    __shared__ float s_log2s, s_m;
-    __shared__ int s_live;
+    constexpr int E = F32 ? 4 : 2, W = NT / 32, PARTS = CLUSTER ? 8 * W : W;
+    __shared__ __align__(16) float4 s_part[2][PARTS];       // statistics of all warps of a row
+    __shared__ __align__(8) uint64_t s_stat[2];
+    __shared__ int s_abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const float k2 = a.inv_temperature * VR_LOG2E;
-    const int64_t V = a.V, nv = V / X::N;
-    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
-        const char* z = (const char*)a.logits + (size_t)row * a.ld * E;
-        char* dz = a.dlogits ? (char*)a.dlogits + (size_t)row * a.lddl * E : nullptr;
-        const int32_t target = a.targets[row];
-        bool live = target >= 0 && target < V;
-        if (target >= V && tid == 0) {
-            if (atomicCAS(a.status, 0, DEV_BAD_INDEX) == 0) a.status[1] = (int)row;
-        }
-        const bool wanted = !a.terms || a.weight[row] != 0.f;      // else only logp / entropy
-        if (live && (wanted || a.logp || a.entropy)) {
-            RowStats st = {-CUDART_INF_F, 0.f, 0.f};
-            for (int64_t v = tid; v < nv; v += VR_THREADS) {
-                float f[X::N];
-                X::unpack(reinterpret_cast<const uint4*>(z)[v], f);
-                RowStats b = {f[0], 0.f, 0.f};
-#pragma unroll
-                for (int i = 1; i < X::N; ++i) b.m = max_nan(b.m, f[i]);
-                const float mr = ref_of(b.m);
-#pragma unroll
-                for (int i = 0; i < X::N; ++i) {
-                    const float t = exponent(f[i], mr, k2), e = ex2(t);
-                    b.s += e;
-                    b.u += e * t;
-                }
-                st = merge(st, b, k2);
-            }
-            for (int64_t i = nv * X::N + tid; i < V; i += VR_THREADS) {
-                const float f = X::load(z, i);
-                const float t = exponent(f, ref_of(f), k2), e = ex2(t);
-                st = merge(st, RowStats{f, e, e * t}, k2);
-            }
-            for (int o = 16; o > 0; o >>= 1) {
-                RowStats b;
-                b.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-                b.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-                b.u = __shfl_xor_sync(0xffffffffu, st.u, o);
-                st = merge(st, b, k2);
-            }
-            if (lane == 0) s_part[warp] = st;
-            __syncthreads();
-            if (tid == 0) {
-                for (int w = 1; w < VR_THREADS / 32; ++w) st = merge(st, s_part[w], k2);
-                const bool dist = !(st.s == 0.f);
-                const float log2s = dist ? log2f(st.s) : 0.f, mr = ref_of(st.m);
-                const float logp = dist ? ((X::load(z, target) - mr) * k2 - log2s) * VR_LN2 : 0.f;
-                const float H = dist ? (log2s - st.u / st.s) * VR_LN2 : 0.f;
-                if (a.logp) a.logp[row] = logp;
-                if (a.entropy) a.entropy[row] = H;
-                s_live = dist && wanted;
-                s_m = mr;
-                s_log2s = log2s;
-                if (a.terms && s_live) s_grad = token_terms(a, row, logp, H, log2s, a.terms + row);
-            }
-            __syncthreads();
-            live = s_live;
-        } else {
-            if (tid == 0) {
-                if (a.logp) a.logp[row] = 0.f;
-                if (a.entropy) a.entropy[row] = 0.f;
-            }
-            live = false;
-        }
-        if (a.terms && !live && tid == 0) a.terms[row] = PolicyTerms{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (dz) {
-            if (!live) {
-                for (int64_t v = tid; v < nv; v += VR_THREADS) reinterpret_cast<uint4*>(dz)[v] = make_uint4(0, 0, 0, 0);
-                for (int64_t i = nv * X::N + tid; i < V; i += VR_THREADS) X::store(dz, i, 0.f);
-            } else {
-                const RowGrad g = s_grad;
-                const float m = s_m, log2s = s_log2s;
-                for (int64_t v = tid; v < nv; v += VR_THREADS) {
-                    float f[X::N];
-                    X::unpack(reinterpret_cast<const uint4*>(z)[v], f);
-#pragma unroll
-                    for (int i = 0; i < X::N; ++i) {
-                        const float t = exponent(f[i], m, k2);
-                        f[i] = ex2(t - log2s) * (g.alpha * t + g.beta);
-                        if (v * X::N + i == target) f[i] += g.gamma;
-                    }
-                    reinterpret_cast<uint4*>(dz)[v] = X::pack(f);
-                }
-                for (int64_t i = nv * X::N + tid; i < V; i += VR_THREADS) {
-                    const float t = exponent(X::load(z, i), m, k2);
-                    X::store(dz, i, ex2(t - log2s) * (g.alpha * t + g.beta) + (i == target ? g.gamma : 0.f));
-                }
-            }
+    const uint32_t rank = CLUSTER ? dk_cluster_ctarank() : 0;
+    const int C = CLUSTER ? lay.C : 1;
+    const int64_t stride = gridDim.x / C;
+    const uint32_t bar_stat = smem_u32(s_stat);
+    if (CLUSTER) {
+        if (tid == 0) {
+            mbar_init(bar_stat, 1);
+            mbar_init(bar_stat + 8, 1);
+            s_abort = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
+        dk_cluster_sync();
+    }
+    if (a.terms) dk_launch_dependents();        // the kernel that sums the terms; it waits for this one's end
+    // this CTA's part of every row: whole vectors, and behind the last of the row up to 7 elements
+    const int64_t V = a.V, begin = min((int64_t)rank * lay.slice, V);
+    const int64_t end = (int)rank == C - 1 ? V : min(begin + lay.slice, V);
+    const int nvec = (int)((end - begin) / X::N), ntail = (int)(end - begin) - nvec * X::N;
+    const int64_t tail = begin + (int64_t)nvec * X::N;
+    const float k2 = a.inv_temperature * VR_LOG2E;
+
+    uint4 q[VPT];
+    float zt = -INFINITY;
+    // vector i of this thread; past the end a number that adds nothing to a row's statistics (-1e30: finite, so that its
+    // term of the entropy is 0 as well)
+    constexpr uint32_t NOTHING = F32 ? 0xf149f2cau : 0xf149f149u;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) q[i] = make_uint4(NOTHING, NOTHING, NOTHING, NOTHING);
+    auto load_row = [&](int64_t row, int i) {
+        if (tid + i * NT < nvec) q[i] = __ldcs(reinterpret_cast<const uint4*>((const char*)a.logits + ((size_t)row * a.ld + begin) * E) + tid + i * NT);
+    };
+    auto load_tail = [&](int64_t row) {
+        if (tid < ntail) zt = X::load((const char*)a.logits + (size_t)row * a.ld * E, tail + tid);
+    };
+    int64_t row = blockIdx.x / C;
+    int32_t target = row < a.T ? a.targets[row] : -1;
+    TokenIn in = {0.f, 0.f, 0.f, 1.f};
+    if (a.terms && row < a.T) in.w = a.weight[row];
+    bool read = row_read(a, target, in.w);
+    if (read) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) load_row(row, i);
+        load_tail(row);
+    }
+    // what the next rows are, two ahead: the row after the next is brought into L2 while this one is worked on
+    int32_t target_next = -1;
+    float w_next = 1.f;
+    if (row + stride < a.T) {
+        target_next = a.targets[row + stride];
+        if (a.terms) w_next = a.weight[row + stride];
+    }
+    for (int it = 0; row < a.T; row += stride) {
+        const int64_t next = row + stride, after = next + stride;
+        int32_t target_after = -1;
+        float w_after = 1.f;
+        if (after < a.T) {
+            target_after = a.targets[after];
+            if (a.terms) w_after = a.weight[after];
+        }
+        if (tid == 0 && nvec > 0 && row_read(a, target_next, w_next))
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"((const char*)a.logits + ((size_t)next * a.ld + begin) * E), "r"(nvec * 16));
+        if (a.terms) {
+            in.old = a.old_logp[row];
+            in.A = a.adv[row];
+            if (a.ref_logp) in.ref = a.ref_logp[row];
+        }
+        const bool first = rank == 0 && tid == 0;
+        bool live = read;
+        RowGrad g = {0.f, 0.f, 0.f};
+        float m = 0.f, log2s = 0.f, za = 0.f;      // za: the target's logit
+        if (read) {
+            if (rank == 0 && warp == 0) za = X::load((const char*)a.logits + (size_t)row * a.ld * E, target);
+            // The warp's sums, relative to a reference that any element near its maximum gives as well: the maximum of each
+            // thread's first vector.  Finding the true one first would take as many instructions as the sums.
+            float wm = warp_max(tid < nvec ? max_nan(zt, max_of<F32>(q[0])) : zt), s, u = 0.f;
+            {
+                const float mr = ref_of(wm), tt = exponent(zt, mr, k2);
+                float2 s2 = make_float2(ex2(tt), 0.f), u2 = make_float2(s2.x * tt, 0.f);
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+                    if (i * NT < nvec) {
+#pragma unroll
+                        for (int j = 0; j < X::N; j += 2) {
+                            const float2 t = __fmul2_rn(__fadd2_rn(pair_of<F32>(q[i], j), make_float2(-mr, -mr)), make_float2(k2, k2));
+                            const float2 e = make_float2(ex2(t.x), ex2(t.y));
+                            s2 = __fadd2_rn(s2, e);
+                            if (ENTROPY) u2 = __ffma2_rn(e, t, u2);
+                        }
+                    }
+                s = warp_sum(s2.x + s2.y);
+                if (ENTROPY) u = warp_sum(u2.x + u2.y);
+            }
+            // Again from the true maximum if the reference was too far off, or if there is no finite logit or a NaN; the
+            // entropy's sum again, with exponents that stay finite, if a logit of -inf has made 0 (-inf) of its term.
+            const bool far = !(s > 0x1p-30f && s < 0x1p40f);
+            if (far || u != u) {
+                if (far) {
+                    wm = zt;
+#pragma unroll
+                    for (int i = 0; i < VPT; ++i)
+                        if (tid + i * NT < nvec) wm = max_nan(wm, max_of<F32>(q[i]));
+                    wm = warp_max(wm);
+                }
+                const float mr = ref_of(wm), tt = exponent(zt, mr, k2);
+                float sx = ex2(tt), ux = sx * tt;
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+                    if (tid + i * NT < nvec) {
+#pragma unroll
+                        for (int j = 0; j < X::N; ++j) {
+                            const float t = exponent(element<F32>(q[i], j), mr, k2), e = ex2(t);
+                            sx += e;
+                            ux += e * t;
+                        }
+                    }
+                sx = warp_sum(sx);
+                if (far) s = sx;
+                if (ENTROPY) u = warp_sum(ux);
+            }
+            if (!GRAD && row_read(a, target_next, w_next)) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) load_row(next, i);
+            }
+            // Two buffers: a warp writes for row i + 2 only after all warps have written for row i + 1, which they do
+            // when they have read row i.
+            const int b = it & 1;
+            if (CLUSTER) {
+                if (tid == 0) mbar_expect_tx(bar_stat + 8 * b, (uint32_t)(C * W * 16));
+                if (lane < C)
+                    send_stats(dk_map_to_cta(smem_u32(&s_part[b][rank * W + warp]), lane), dk_map_to_cta(bar_stat + 8 * b, lane), wm, s, u, za);
+                if (!__all_sync(0xffffffffu, mbar_wait(bar_stat + 8 * b, (it >> 1) & 1, &s_abort, 3))) break;
+            } else {
+                if (lane == 0) s_part[b][warp] = make_float4(wm, s, u, za);
+                __syncthreads();
+            }
+            ++it;
+            // all warps' statistics, relative to the row's maximum; one to PARTS / 32 of them per lane
+            float rm = -INFINITY, rs = 0.f, ru = 0.f;
+            for (int i = lane; i < C * W; i += 32) rm = max_nan(rm, s_part[b][i].x);
+            rm = warp_max(rm);
+            m = ref_of(rm);
+            for (int i = lane; i < C * W; i += 32) {
+                const float4 x = s_part[b][i];
+                const float d = exponent(x.x, m, k2), f = ex2(d);
+                rs += f * x.y;
+                if (ENTROPY) ru += f * (x.z + x.y * d);
+            }
+            rs = warp_sum(rs);
+            if (ENTROPY) ru = warp_sum(ru);
+            const bool dist = !(rs == 0.f);        // else there is no finite logit
+            log2s = dist ? log2f(rs) : 0.f;
+            za = s_part[b][0].w;
+            const float logp = dist ? ((za - m) * k2 - log2s) * VR_LN2 : 0.f;
+            const float H = ENTROPY && dist ? (log2s - ru / rs) * VR_LN2 : 0.f;
+            if (first) {
+                if (a.logp) a.logp[row] = logp;
+                if (a.entropy) a.entropy[row] = H;
+            }
+            live = dist && in.w != 0.f;
+            if (a.terms && live) {
+                PolicyTerms t;
+                g = token_terms(a, in, logp, H, log2s, &t);
+                if (first) a.terms[row] = t;
+            }
+        } else if (first) {
+            if (target >= V) dk_report(a.status, DEV_BAD_INDEX, (int)row);
+            if (a.logp) a.logp[row] = 0.f;
+            if (a.entropy) a.entropy[row] = 0.f;
+        }
+        if (a.terms && !live && first) a.terms[row] = PolicyTerms{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const bool read_next = row_read(a, target_next, w_next);
+        if (GRAD) {
+            uint4* dz = reinterpret_cast<uint4*>((char*)a.dlogits + ((size_t)row * a.lddl + begin) * E);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                if (i * NT >= nvec) continue;
+                const int v = tid + i * NT;
+                uint4 o4 = make_uint4(0, 0, 0, 0);
+                if (live) {
+                    float2 f[X::N / 2];
+#pragma unroll
+                    for (int j = 0; j < X::N; j += 2) {
+                        const float2 d = __fadd2_rn(pair_of<F32>(q[i], j), make_float2(-m, -m));
+                        if (ENTROPY_GRAD) {
+                            float2 t = __fmul2_rn(d, make_float2(k2, k2));
+                            t = make_float2(max_nan(t.x, -200.f), max_nan(t.y, -200.f));
+                            const float2 w = __fadd2_rn(t, make_float2(-log2s, -log2s));
+                            f[j / 2] = __fmul2_rn(make_float2(ex2(w.x), ex2(w.y)), __ffma2_rn(make_float2(g.alpha, g.alpha), t, make_float2(g.beta, g.beta)));
+                        } else {
+                            const float2 w = __ffma2_rn(d, make_float2(k2, k2), make_float2(-log2s, -log2s));
+                            f[j / 2] = __fmul2_rn(make_float2(ex2(w.x), ex2(w.y)), make_float2(g.beta, g.beta));
+                        }
+                    }
+                    o4 = X::pack(f);
+                }
+                if (v < nvec) __stcs(dz + v, o4);
+                if (read_next) load_row(next, i);
+            }
+            // the target's element once more, by the thread that has just written its vector
+            const int64_t at = (int64_t)target - begin;
+            if (live && target >= begin && target < tail && tid == (int)(at / X::N) % NT) {
+                const float t = exponent(za, m, k2);
+                X::store(dz, at, ex2(t - log2s) * fmaf(g.alpha, t, g.beta) + g.gamma);
+            }
+            if (tid < ntail) {
+                float o = 0.f;
+                if (live) {
+                    const float t = exponent(zt, m, k2);
+                    o = ex2(t - log2s) * (g.alpha * t + g.beta) + (tail + tid == target ? g.gamma : 0.f);
+                }
+                X::store((char*)a.dlogits + (size_t)row * a.lddl * E, tail + tid, o);
+            }
+        }
+        if (read_next) {
+            if (!(GRAD || read)) {      // nothing has brought the next row's vectors yet
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) load_row(next, i);
+            }
+            load_tail(next);
+        }
+        target = target_next;
+        in.w = w_next;
+        read = read_next;
+        target_next = target_after;
+        w_next = w_after;
+    }
+    if (CLUSTER) {
+        if (tid == 0 && s_abort != 0) dk_report(a.status, DEV_TIMEOUT, s_abort * 1000000 + (int)blockIdx.x);
+        // no CTA of a cluster leaves while another may still write to its shared memory
+        __syncwarp();
+        dk_cluster_sync();
     }
 }
 
-marlaas_status_t launch_vocab_rows(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st) {
-    const int grid = (int)std::min<int64_t>(r.T, (int64_t)pool->sm_count * 4);
-    if (r.f32) k_vocab_rows<true><<<grid, VR_THREADS, 0, st>>>(r);
-    else k_vocab_rows<false><<<grid, VR_THREADS, 0, st>>>(r);
+template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD, int NT, int VPT, bool CLUSTER>
+static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r, int C, cudaStream_t st) {
+    constexpr int N = F32 ? 4 : 8;
+    auto kernel = k_vocab_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, NT, VPT, CLUSTER>;
+    RowsLayout lay;
+    lay.C = C;
+    lay.slice = cdiv(cdiv(r.V, C), N) * N;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = C; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = CLUSTER ? 1 : 0;
+    cfg.blockDim = dim3(NT);
+    cfg.stream = st;
+    cfg.gridDim = dim3(C);
+    // rows that the device holds at once (asked once per device and cluster size)
+    static std::atomic<int> resident[MAX_DEVICES][4];
+    std::atomic<int>* known = pool->device < MAX_DEVICES ? &resident[pool->device][C == 1 ? 0 : C == 2 ? 1 : C == 4 ? 2 : 3] : nullptr;
+    int rows = known ? known->load(std::memory_order_relaxed) : 0;
+    if (rows == 0) {
+        if (CLUSTER) {
+            MARLAAS_CUDA_TRY(cudaOccupancyMaxActiveClusters(&rows, kernel, &cfg));
+        } else {
+            MARLAAS_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&rows, kernel, NT, 0));
+            rows *= pool->sm_count;
+        }
+        if (rows < 1) return fail(MARLAAS_ERR_CUDA, "k_vocab_rows: no room for a cluster of %d", C);
+        if (known) known->store(rows, std::memory_order_relaxed);
+    }
+    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(rows, r.T) * C));
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, r, lay));
     MARLAAS_LAUNCH_CHECK("k_vocab_rows");
     return MARLAAS_OK;
+}
+
+// The shape of a launch, from the sizes alone (not from what is wanted of the rows, so that all calls on a batch sum in one
+// order: the log-probabilities of marlaas_token_logprobs and of the loss are the same bits, and the ratios of an update's
+// first pass exactly 1).
+template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD>
+static marlaas_status_t launch_shape(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st) {
+    const int64_t vecs = cdiv(r.V, F32 ? 4 : 8);
+    int C = 1;
+    while (C < 8 && vecs > (int64_t)C * 256 * 16) C *= 2;
+    // few rows: more CTAs for each, down to one vector per thread
+    while (C < 8 && r.T * C * 2 <= pool->sm_count && vecs > (int64_t)C * 256) C *= 2;
+    if (C > 1) {
+        if (F32 && vecs > 8 * 256 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, F32 ? 512 : 256, 16, true>(pool, r, C, st);
+        return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 256, 16, true>(pool, r, C, st);
+    }
+    if (vecs <= 32 * 8) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 32, 8, false>(pool, r, 1, st);
+    if (vecs <= 32 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 32, 16, false>(pool, r, 1, st);
+    if (vecs <= 64 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 64, 16, false>(pool, r, 1, st);
+    if (vecs <= 128 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 128, 16, false>(pool, r, 1, st);
+    return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 256, 16, false>(pool, r, 1, st);
+}
+
+marlaas_status_t launch_vocab_rows(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st) {
+    const bool entropy = r.entropy || r.terms, eg = r.dlogits && r.entropy_coef != 0.f;
+    if (r.f32) return !r.dlogits ? (entropy ? launch_shape<true, false, true, false>(pool, r, st) : launch_shape<true, false, false, false>(pool, r, st))
+                                 : eg ? launch_shape<true, true, true, true>(pool, r, st) : launch_shape<true, true, true, false>(pool, r, st);
+    return !r.dlogits ? (entropy ? launch_shape<false, false, true, false>(pool, r, st) : launch_shape<false, false, false, false>(pool, r, st))
+                      : eg ? launch_shape<false, true, true, true>(pool, r, st) : launch_shape<false, true, true, false>(pool, r, st);
 }
 
 }  // namespace marlaas

@@ -162,7 +162,7 @@ def _large(z, tgt, r):
 
 
 MASKS = {"plain": None, "minus infinity": _mask_inf, "lowest": _mask_lowest, "large": _large}
-SHAPES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (7, 255), (3, 1000), (6, 4099), (150, 515), (2, 33001), (3, 70001), (2, 131080)]
+SHAPES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (7, 255), (3, 1000), (6, 4099), (150, 515), (2, 33001), (3, 70001), (2, 131080), (700, 3001), (301, 40003)]
 
 
 def logp_close(got, ref, what):
@@ -267,6 +267,8 @@ def test_policy_loss(pool, T, V, mask, kl, ent, dtype):
     assert torch.equal(more, stats)
     B.marlaas_policy_loss(pool, z, *args, ref_logp=refs, stats=more, flags=B.MARLAAS_FLAG_ACCUMULATE, **hp)
     assert torch.equal(more, 2 * stats)
+    # the rollout's call on the same batch gives the same log-probabilities, bit for bit
+    assert torch.equal(B.marlaas_token_logprobs(pool, z, args[0], inv_temperature=1 / 0.8), logp)
     # in place of the logits
     B.marlaas_policy_loss(pool, z, *args, ref_logp=refs, dlogits=z, **hp)
     assert torch.equal(z, grad[:, :V]) and torch.all(buf[:, V:] == 777.0)
