@@ -26,6 +26,11 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+__device__ __forceinline__ float lg2(float x) {
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 // The reference point of a running maximum: 0 while there is no finite logit, so that -inf - m stays -inf.
 __device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
 // (z - m) k in units of log 2, not below -200: 2^-200 is 0 in fp32, and a product with it stays 0 where (z - m) k itself is
@@ -73,7 +78,7 @@ struct TokenIn {
 // The token's loss terms from its log-probability and entropy; the coefficients of its gradient.
 __device__ __forceinline__ RowGrad token_terms(const VocabRows& a, const TokenIn& in, float logp, float H, float log2s, PolicyTerms* out) {
     const float w = in.w, A = in.A;
-    const float ratio = expf(logp - in.old);
+    const float ratio = ex2((logp - in.old) * VR_LOG2E);
     // 0 A is 0 whatever the ratio
     const float plain = A == 0.f ? 0.f : ratio * A;
     const float clipped = A == 0.f ? 0.f : fminf(fmaxf(ratio, 1.f - a.clip_low), 1.f + a.clip_high) * A;
@@ -119,20 +124,34 @@ __device__ __forceinline__ float max_of(const uint4& q) {
 }
 
 // ---- the kernel ----
-// A cluster of C CTAs (one CTA for most vocabularies) takes a row, a slice each, and keeps it in registers, as the 16-byte
-// vectors it was loaded in, between the statistics and the gradient: the row crosses HBM once in each direction and needs
-// neither shared memory nor a second read.  As the gradient's vectors leave their registers, the next row's are loaded into
-// them.  The warps of a row do not wait for one another except here: each publishes its statistics (to all CTAs of the
-// cluster), then every warp merges all of them.
+// A cluster of C CTAs (one CTA for most vocabularies) takes a row, a slice each, and keeps it in shared memory between the
+// statistics and the gradient: the row crosses HBM once in each direction.  One bulk copy brings a slice, started by
+// whichever warp is the last to be done with the row before, so that no warp waits to start it.  Three CTAs share an SM: the
+// copy and the exchange of statistics of one run beside the arithmetic of the others.  The warps of a row wait for one
+// another only for that exchange: each publishes its statistics (to all CTAs of the cluster), then every warp merges all of
+// them.
+//
+// What bounds it: HBM, with the arithmetic close behind (per element of a bf16 row 12 issue slots and 2 special-function
+// operations, 45 % and 65 % of what the SMs have while the row streams).  Tried and not kept: the slice in registers
+// (2 CTAs per SM, 438 us for the loss over 4096 x 131072 against 400), chunks that are refilled one by one (441 us: the
+// waits cost more than the earlier copies gain), a share of the exponentials as polynomials on the FMA pipes (425 us).
 struct RowsLayout {
     int32_t C;              // CTAs per row
     int64_t slice;          // elements per CTA (whole vectors)
 };
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
 __device__ __forceinline__ void send_stats(uint32_t dst, uint32_t bar, float m, float s, float u, float z) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(dst),
                  "r"(__float_as_uint(m)), "r"(__float_as_uint(s)), "r"(__float_as_uint(u)), "r"(__float_as_uint(z)), "r"(bar)
                  : "memory");
+}
+__device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes));
 }
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
@@ -151,169 +170,223 @@ __device__ __forceinline__ bool row_read(const VocabRows& a, int32_t target, flo
     return (target >= 0) & (target < a.V) & ((a.logp != nullptr) | (a.entropy != nullptr) | (weight != 0.f));
 }
 
-template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD, int NT, int VPT, bool CLUSTER>
-__global__ void __launch_bounds__(NT, 8192 / (NT * VPT) > 32 ? 32 : 8192 / (NT * VPT)) k_vocab_rows(const VocabRows a, const RowsLayout lay) {
+// Statistics of a warp's part of a row.  `done` is called when the slice has been read once; `again`: where it is read a second
+// time if it has to be (without a gradient its place in shared memory has been given up by then: from L2).
+struct WarpStats {
+    float m, s, u;          // the reference, sum 2^t, sum t 2^t
+};
+template <bool F32, bool ENTROPY, int NT, typename Done>
+__device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const uint4* again, int nvec, float zt, int tid, float k2, Done done) {
+    constexpr int N = Vec<F32>::N;
+    WarpStats r;
+    // Sums relative to a reference that any element near the maximum gives as well: the maximum of each thread's first
+    // vector.  Finding the true one first would take as many instructions as the sums.
+    r.m = warp_max(tid < nvec ? max_nan(zt, max_of<F32>(slice[tid])) : zt);
+    {
+        const float mr = ref_of(r.m), tt = exponent(zt, mr, k2);
+        float2 s2 = make_float2(ex2(tt), 0.f), u2 = make_float2(s2.x * tt, 0.f);
+#pragma unroll 4
+        for (int v = tid; v < nvec; v += NT) {
+            const uint4 q = slice[v];
+#pragma unroll
+            for (int j = 0; j < N; j += 2) {
+                const float2 t = __fmul2_rn(__fadd2_rn(pair_of<F32>(q, j), make_float2(-mr, -mr)), make_float2(k2, k2));
+                const float2 e = make_float2(ex2(t.x), ex2(t.y));
+                s2 = __fadd2_rn(s2, e);
+                if (ENTROPY) u2 = __ffma2_rn(e, t, u2);
+            }
+        }
+        done();
+        r.s = warp_sum(s2.x + s2.y);
+        r.u = ENTROPY ? warp_sum(u2.x + u2.y) : 0.f;
+    }
+    // Again from the true maximum if the reference was too far off, or if there is no finite logit or a NaN; the entropy's
+    // sum again, with exponents that stay finite, if a logit of -inf has made 0 (-inf) of its term.
+    const bool far = !(r.s > 0x1p-30f && r.s < 0x1p40f);
+    if (far || r.u != r.u) {
+        if (far) {
+            r.m = zt;
+            for (int v = tid; v < nvec; v += NT) r.m = max_nan(r.m, max_of<F32>(again[v]));
+            r.m = warp_max(r.m);
+        }
+        const float mr = ref_of(r.m), tt = exponent(zt, mr, k2);
+        float s = ex2(tt), u = s * tt;
+        for (int v = tid; v < nvec; v += NT) {
+            const uint4 q = again[v];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float t = exponent(element<F32>(q, j), mr, k2), e = ex2(t);
+                s += e;
+                u += e * t;
+            }
+        }
+        s = warp_sum(s);
+        if (far) r.s = s;
+        if (ENTROPY) r.u = warp_sum(u);
+    }
+    return r;
+}
+
+template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD, int NT, bool CLUSTER>
+__global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, const RowsLayout lay) {
     using X = Vec<F32>;
     constexpr int E = F32 ? 4 : 2, W = NT / 32, PARTS = CLUSTER ? 8 * W : W;
+    extern __shared__ __align__(128) uint4 s_slice[];
     __shared__ __align__(16) float4 s_part[2][PARTS];       // statistics of all warps of a row
-    __shared__ __align__(8) uint64_t s_stat[2];
-    __shared__ int s_abort;
+    __shared__ __align__(8) uint64_t s_full, s_stat[2];
+    __shared__ int s_done, s_copies, s_abort;      // warps done with the slice; copies started; given up
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = CLUSTER ? dk_cluster_ctarank() : 0;
     const int C = CLUSTER ? lay.C : 1;
     const int64_t stride = gridDim.x / C;
-    const uint32_t bar_stat = smem_u32(s_stat);
-    if (CLUSTER) {
-        if (tid == 0) {
-            mbar_init(bar_stat, 1);
-            mbar_init(bar_stat + 8, 1);
-            s_abort = 0;
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        __syncthreads();
-        dk_cluster_sync();
+    const uint32_t bar_full = smem_u32(&s_full), bar_stat = smem_u32(s_stat);
+    if (tid == 0) {
+        mbar_init(bar_full, 1);
+        s_done = s_copies = 0;
+        mbar_init(bar_stat, 1);
+        mbar_init(bar_stat + 8, 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncthreads();
+    if (CLUSTER) dk_cluster_sync();
     if (a.terms) dk_launch_dependents();        // the kernel that sums the terms; it waits for this one's end
     // this CTA's part of every row: whole vectors, and behind the last of the row up to 7 elements
     const int64_t V = a.V, begin = min((int64_t)rank * lay.slice, V);
     const int64_t end = (int)rank == C - 1 ? V : min(begin + lay.slice, V);
     const int nvec = (int)((end - begin) / X::N), ntail = (int)(end - begin) - nvec * X::N;
     const int64_t tail = begin + (int64_t)nvec * X::N;
-    const float k2 = a.inv_temperature * VR_LOG2E;
-
-    uint4 q[VPT];
-    float zt = -INFINITY;
-    // vector i of this thread; past the end a number that adds nothing to a row's statistics (-1e30: finite, so that its
-    // term of the entropy is 0 as well)
-    constexpr uint32_t NOTHING = F32 ? 0xf149f2cau : 0xf149f149u;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) q[i] = make_uint4(NOTHING, NOTHING, NOTHING, NOTHING);
-    auto load_row = [&](int64_t row, int i) {
-        if (tid + i * NT < nvec) q[i] = __ldcs(reinterpret_cast<const uint4*>((const char*)a.logits + ((size_t)row * a.ld + begin) * E) + tid + i * NT);
+    // (through a shuffle: a value of each lane's own, which two-element instructions take as it is, not a uniform one)
+    const float k2 = __shfl_sync(0xffffffffu, a.inv_temperature * VR_LOG2E, 0);
+    // The rows of this cluster are base + n stride.  Lane l holds target and weight of the row n0 + l of a window of 32,
+    // and `window` which of them are read.
+    const int64_t base = blockIdx.x / C;
+    const int nrows = base < a.T ? (int)((a.T - 1 - base) / stride) + 1 : 0;
+    auto source = [&](int n) { return (const char*)a.logits + ((size_t)(base + (int64_t)n * stride) * a.ld + begin) * E; };
+    auto copy = [&](int n) {            // one thread; the slice's place is free
+        ++s_copies;
+        mbar_expect_tx(bar_full, (uint32_t)nvec * 16);
+        bulk_load(smem_u32(s_slice), source(n), (uint32_t)nvec * 16, bar_full);
     };
-    auto load_tail = [&](int64_t row) {
-        if (tid < ntail) zt = X::load((const char*)a.logits + (size_t)row * a.ld * E, tail + tid);
-    };
-    int64_t row = blockIdx.x / C;
-    int32_t target = row < a.T ? a.targets[row] : -1;
-    TokenIn in = {0.f, 0.f, 0.f, 1.f};
-    if (a.terms && row < a.T) in.w = a.weight[row];
-    bool read = row_read(a, target, in.w);
-    if (read) {
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) load_row(row, i);
-        load_tail(row);
-    }
-    // what the next rows are, two ahead: the row after the next is brought into L2 while this one is worked on
-    int32_t target_next = -1;
-    float w_next = 1.f;
-    if (row + stride < a.T) {
-        target_next = a.targets[row + stride];
-        if (a.terms) w_next = a.weight[row + stride];
-    }
-    for (int it = 0; row < a.T; row += stride) {
-        const int64_t next = row + stride, after = next + stride;
-        int32_t target_after = -1;
-        float w_after = 1.f;
-        if (after < a.T) {
-            target_after = a.targets[after];
-            if (a.terms) w_after = a.weight[after];
+    int32_t target_l = -1;
+    float w_l = 1.f;
+    auto look = [&](int n0) {
+        target_l = -1;
+        w_l = 1.f;
+        if (n0 + lane < nrows) {
+            target_l = a.targets[base + (int64_t)(n0 + lane) * stride];
+            if (a.terms) w_l = a.weight[base + (int64_t)(n0 + lane) * stride];
         }
-        if (tid == 0 && nvec > 0 && row_read(a, target_next, w_next))
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"((const char*)a.logits + ((size_t)next * a.ld + begin) * E), "r"(nvec * 16));
+        return __ballot_sync(0xffffffffu, row_read(a, target_l, w_l));
+    };
+    // the first row after n that is read, nrows if there is none
+    auto next_read = [&](int n, uint32_t window) {
+        const uint32_t later = (n & 31) == 31 ? 0u : window >> ((n & 31) + 1);
+        if (later) return n + __ffs(later);
+        const int32_t t = target_l;
+        const float w = w_l;
+        int found = nrows;
+        for (int n0 = (n | 31) + 1; n0 < nrows; n0 += 32) {
+            const uint32_t bits = look(n0);
+            if (bits) {
+                found = n0 + __ffs(bits) - 1;
+                break;
+            }
+        }
+        target_l = t;
+        w_l = w;
+        return found;
+    };
+    uint32_t window = look(0);
+    {
+        const int n = window & 1u ? 0 : next_read(0, window);
+        if (tid == 0 && nvec > 0 && n < nrows) copy(n);
+    }
+    TokenIn in = {0.f, 0.f, 0.f, 1.f};
+    int it = 0;                     // rows read so far
+    for (int n = 0; n < nrows; ++n) {
+        if (n > 0 && (n & 31) == 0) window = look(n);
+        const int64_t row = base + (int64_t)n * stride;
+        const bool first = rank == 0 && tid == 0, read = (window >> (n & 31)) & 1u;
+        const int32_t target = __shfl_sync(0xffffffffu, target_l, n & 31);
+        in.w = __shfl_sync(0xffffffffu, w_l, n & 31);
         if (a.terms) {
             in.old = a.old_logp[row];
             in.A = a.adv[row];
             if (a.ref_logp) in.ref = a.ref_logp[row];
         }
-        const bool first = rank == 0 && tid == 0;
+        const int next = read ? next_read(n, window) : nrows;
+        // a warp is done with the slice: the last one starts the copy of the next row's
+        auto release = [&]() {
+            __syncwarp();
+            if (lane == 0 && nvec > 0) {
+                __threadfence_block();
+                if (atomicAdd(&s_done, 1) == W - 1) {
+                    s_done = 0;
+                    __threadfence_block();
+                    if (next < nrows && s_abort == 0) copy(next);
+                }
+            }
+        };
         bool live = read;
         RowGrad g = {0.f, 0.f, 0.f};
-        float m = 0.f, log2s = 0.f, za = 0.f;      // za: the target's logit
+        float m = 0.f, log2s = 0.f, za = 0.f, zt = -INFINITY;      // za: the target's logit
         if (read) {
-            if (rank == 0 && warp == 0) za = X::load((const char*)a.logits + (size_t)row * a.ld * E, target);
-            // The warp's sums, relative to a reference that any element near its maximum gives as well: the maximum of each
-            // thread's first vector.  Finding the true one first would take as many instructions as the sums.
-            float wm = warp_max(tid < nvec ? max_nan(zt, max_of<F32>(q[0])) : zt), s, u = 0.f;
-            {
-                const float mr = ref_of(wm), tt = exponent(zt, mr, k2);
-                float2 s2 = make_float2(ex2(tt), 0.f), u2 = make_float2(s2.x * tt, 0.f);
-#pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    if (i * NT < nvec) {
-#pragma unroll
-                        for (int j = 0; j < X::N; j += 2) {
-                            const float2 t = __fmul2_rn(__fadd2_rn(pair_of<F32>(q[i], j), make_float2(-mr, -mr)), make_float2(k2, k2));
-                            const float2 e = make_float2(ex2(t.x), ex2(t.y));
-                            s2 = __fadd2_rn(s2, e);
-                            if (ENTROPY) u2 = __ffma2_rn(e, t, u2);
-                        }
-                    }
-                s = warp_sum(s2.x + s2.y);
-                if (ENTROPY) u = warp_sum(u2.x + u2.y);
-            }
-            // Again from the true maximum if the reference was too far off, or if there is no finite logit or a NaN; the
-            // entropy's sum again, with exponents that stay finite, if a logit of -inf has made 0 (-inf) of its term.
-            const bool far = !(s > 0x1p-30f && s < 0x1p40f);
-            if (far || u != u) {
-                if (far) {
-                    wm = zt;
-#pragma unroll
-                    for (int i = 0; i < VPT; ++i)
-                        if (tid + i * NT < nvec) wm = max_nan(wm, max_of<F32>(q[i]));
-                    wm = warp_max(wm);
-                }
-                const float mr = ref_of(wm), tt = exponent(zt, mr, k2);
-                float sx = ex2(tt), ux = sx * tt;
-#pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    if (tid + i * NT < nvec) {
-#pragma unroll
-                        for (int j = 0; j < X::N; ++j) {
-                            const float t = exponent(element<F32>(q[i], j), mr, k2), e = ex2(t);
-                            sx += e;
-                            ux += e * t;
-                        }
-                    }
-                sx = warp_sum(sx);
-                if (far) s = sx;
-                if (ENTROPY) u = warp_sum(ux);
-            }
-            if (!GRAD && row_read(a, target_next, w_next)) {
-#pragma unroll
-                for (int i = 0; i < VPT; ++i) load_row(next, i);
-            }
+            const char* z = (const char*)a.logits + (size_t)row * a.ld * E;
+            if (tid < ntail) zt = X::load(z, tail + tid);
+            if (rank == 0 && warp == 0) za = X::load(z, target);
+            if (nvec > 0 && !__all_sync(0xffffffffu, mbar_wait(bar_full, it & 1, &s_abort, 2))) break;
+            const WarpStats ws = warp_statistics<F32, ENTROPY, NT>(s_slice, GRAD ? s_slice : reinterpret_cast<const uint4*>(z + begin * E), nvec,
+                                                                   zt, tid, k2, [&]() {
+                                                                       if (!GRAD) release();
+                                                                   });
             // Two buffers: a warp writes for row i + 2 only after all warps have written for row i + 1, which they do
             // when they have read row i.
             const int b = it & 1;
             if (CLUSTER) {
                 if (tid == 0) mbar_expect_tx(bar_stat + 8 * b, (uint32_t)(C * W * 16));
                 if (lane < C)
-                    send_stats(dk_map_to_cta(smem_u32(&s_part[b][rank * W + warp]), lane), dk_map_to_cta(bar_stat + 8 * b, lane), wm, s, u, za);
+                    send_stats(dk_map_to_cta(smem_u32(&s_part[b][rank * W + warp]), lane), dk_map_to_cta(bar_stat + 8 * b, lane), ws.m,
+                               ws.s, ws.u, za);
                 if (!__all_sync(0xffffffffu, mbar_wait(bar_stat + 8 * b, (it >> 1) & 1, &s_abort, 3))) break;
-            } else {
-                if (lane == 0) s_part[b][warp] = make_float4(wm, s, u, za);
+            } else if (PARTS > 1) {
+                if (lane == 0) s_part[b][warp] = make_float4(ws.m, ws.s, ws.u, za);
                 __syncthreads();
             }
+            // the next row into L2 while this one's gradient leaves (not earlier: the rows in flight and what has been
+            // written of the gradient fill the part of L2 that would have to keep it)
+            if (GRAD && tid == 0 && nvec > 0 && next < nrows) bulk_prefetch(source(next), (uint32_t)nvec * 16);
             ++it;
-            // all warps' statistics, relative to the row's maximum; one to PARTS / 32 of them per lane
-            float rm = -INFINITY, rs = 0.f, ru = 0.f;
-            for (int i = lane; i < C * W; i += 32) rm = max_nan(rm, s_part[b][i].x);
-            rm = warp_max(rm);
-            m = ref_of(rm);
-            for (int i = lane; i < C * W; i += 32) {
-                const float4 x = s_part[b][i];
-                const float d = exponent(x.x, m, k2), f = ex2(d);
-                rs += f * x.y;
-                if (ENTROPY) ru += f * (x.z + x.y * d);
+            // all warps' statistics, relative to the row's maximum; up to PARTS / 32 of them per lane
+            float rs = 0.f, ru = 0.f;
+            if (PARTS == 1) {
+                m = ref_of(ws.m);
+                rs = ws.s;
+                ru = ws.u;
+            } else {
+                constexpr int PER = (PARTS + 31) / 32;
+                float4 x[PER];
+                float rm = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    x[i] = lane + 32 * i < C * W ? s_part[b][lane + 32 * i] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+                    rm = max_nan(rm, x[i].x);
+                }
+                m = ref_of(warp_max(rm));
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const float d = exponent(x[i].x, m, k2), f = ex2(d);
+                    rs += f * x[i].y;
+                    if (ENTROPY) ru += f * (x[i].z + x[i].y * d);
+                }
+                rs = warp_sum(rs);
+                if (ENTROPY) ru = warp_sum(ru);
+                za = s_part[b][0].w;
             }
-            rs = warp_sum(rs);
-            if (ENTROPY) ru = warp_sum(ru);
             const bool dist = !(rs == 0.f);        // else there is no finite logit
-            log2s = dist ? log2f(rs) : 0.f;
-            za = s_part[b][0].w;
+            log2s = dist ? lg2(rs) : 0.f;
             const float logp = dist ? ((za - m) * k2 - log2s) * VR_LN2 : 0.f;
-            const float H = ENTROPY && dist ? (log2s - ru / rs) * VR_LN2 : 0.f;
+            const float H = ENTROPY && dist ? (log2s - __fdividef(ru, rs)) * VR_LN2 : 0.f;
             if (first) {
                 if (a.logp) a.logp[row] = logp;
                 if (a.entropy) a.entropy[row] = H;
@@ -330,19 +403,17 @@ __global__ void __launch_bounds__(NT, 8192 / (NT * VPT) > 32 ? 32 : 8192 / (NT *
             if (a.entropy) a.entropy[row] = 0.f;
         }
         if (a.terms && !live && first) a.terms[row] = PolicyTerms{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        const bool read_next = row_read(a, target_next, w_next);
         if (GRAD) {
-            uint4* dz = reinterpret_cast<uint4*>((char*)a.dlogits + ((size_t)row * a.lddl + begin) * E);
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                if (i * NT >= nvec) continue;
-                const int v = tid + i * NT;
-                uint4 o4 = make_uint4(0, 0, 0, 0);
-                if (live) {
+            char* dzr = (char*)a.dlogits + (size_t)row * a.lddl * E;
+            uint4* dz = reinterpret_cast<uint4*>(dzr + begin * E);
+            if (live) {
+#pragma unroll 4
+                for (int v = tid; v < nvec; v += NT) {
+                    const uint4 q = s_slice[v];
                     float2 f[X::N / 2];
 #pragma unroll
                     for (int j = 0; j < X::N; j += 2) {
-                        const float2 d = __fadd2_rn(pair_of<F32>(q[i], j), make_float2(-m, -m));
+                        const float2 d = __fadd2_rn(pair_of<F32>(q, j), make_float2(-m, -m));
                         if (ENTROPY_GRAD) {
                             float2 t = __fmul2_rn(d, make_float2(k2, k2));
                             t = make_float2(max_nan(t.x, -200.f), max_nan(t.y, -200.f));
@@ -353,54 +424,51 @@ __global__ void __launch_bounds__(NT, 8192 / (NT * VPT) > 32 ? 32 : 8192 / (NT *
                             f[j / 2] = __fmul2_rn(make_float2(ex2(w.x), ex2(w.y)), make_float2(g.beta, g.beta));
                         }
                     }
-                    o4 = X::pack(f);
+                    __stcs(dz + v, X::pack(f));
                 }
-                if (v < nvec) __stcs(dz + v, o4);
-                if (read_next) load_row(next, i);
+                // the target's element once more, by the thread that has just written its vector
+                if (target >= begin && target < tail && tid == (int)((target - begin) / X::N) % NT) {
+                    const float t = exponent(za, m, k2);
+                    X::store(dzr, target, ex2(t - log2s) * fmaf(g.alpha, t, g.beta) + g.gamma);
+                }
+            } else {
+                for (int v = tid; v < nvec; v += NT) __stcs(dz + v, make_uint4(0, 0, 0, 0));
             }
-            // the target's element once more, by the thread that has just written its vector
-            const int64_t at = (int64_t)target - begin;
-            if (live && target >= begin && target < tail && tid == (int)(at / X::N) % NT) {
-                const float t = exponent(za, m, k2);
-                X::store(dz, at, ex2(t - log2s) * fmaf(g.alpha, t, g.beta) + g.gamma);
-            }
+            if (read) release();
             if (tid < ntail) {
                 float o = 0.f;
                 if (live) {
                     const float t = exponent(zt, m, k2);
-                    o = ex2(t - log2s) * (g.alpha * t + g.beta) + (tail + tid == target ? g.gamma : 0.f);
+                    o = ex2(t - log2s) * fmaf(g.alpha, t, g.beta) + (tail + tid == target ? g.gamma : 0.f);
                 }
-                X::store((char*)a.dlogits + (size_t)row * a.lddl * E, tail + tid, o);
+                X::store(dzr, tail + tid, o);
             }
         }
-        if (read_next) {
-            if (!(GRAD || read)) {      // nothing has brought the next row's vectors yet
-#pragma unroll
-                for (int i = 0; i < VPT; ++i) load_row(next, i);
-            }
-            load_tail(next);
-        }
-        target = target_next;
-        in.w = w_next;
-        read = read_next;
-        target_next = target_after;
-        w_next = w_after;
+    }
+    __syncthreads();
+    if (s_abort != 0 && tid == 0) {
+        // given up: the shared memory is left only when no copy into it is in flight
+        dk_report(a.status, DEV_TIMEOUT, s_abort * 1000000 + (int)blockIdx.x);
+        const unsigned long long t0 = global_ns();
+        while (s_copies > 0 && !mbar_try_wait(bar_full, (s_copies - 1) & 1) && global_ns() - t0 < WAIT_LIMIT_NS) {}
     }
     if (CLUSTER) {
-        if (tid == 0 && s_abort != 0) dk_report(a.status, DEV_TIMEOUT, s_abort * 1000000 + (int)blockIdx.x);
         // no CTA of a cluster leaves while another may still write to its shared memory
         __syncwarp();
         dk_cluster_sync();
     }
 }
 
-template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD, int NT, int VPT, bool CLUSTER>
+template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD, int NT, bool CLUSTER>
 static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r, int C, cudaStream_t st) {
     constexpr int N = F32 ? 4 : 8;
-    auto kernel = k_vocab_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, NT, VPT, CLUSTER>;
+    auto kernel = k_vocab_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, NT, CLUSTER>;
     RowsLayout lay;
     lay.C = C;
     lay.slice = cdiv(cdiv(r.V, C), N) * N;
+    // shared memory in eight sizes, so that the number of CTAs an SM holds is asked for once per device and size
+    const int size = (int)cdiv(lay.slice * (F32 ? 4 : 2), NT * 16 * 4);        // in quarters of 16 vectors per thread
+    const size_t smem = (size_t)size * NT * 16 * 4;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cudaLaunchAttribute at[1];
@@ -409,17 +477,19 @@ static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r
     cfg.attrs = at;
     cfg.numAttrs = CLUSTER ? 1 : 0;
     cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.gridDim = dim3(C);
-    // rows that the device holds at once (asked once per device and cluster size)
-    static std::atomic<int> resident[MAX_DEVICES][4];
-    std::atomic<int>* known = pool->device < MAX_DEVICES ? &resident[pool->device][C == 1 ? 0 : C == 2 ? 1 : C == 4 ? 2 : 3] : nullptr;
+    static std::atomic<int> resident[MAX_DEVICES][4][9];
+    const int log2c = C == 1 ? 0 : C == 2 ? 1 : C == 4 ? 2 : 3;
+    std::atomic<int>* known = pool->device < MAX_DEVICES && size <= 8 ? &resident[pool->device][log2c][size] : nullptr;
     int rows = known ? known->load(std::memory_order_relaxed) : 0;
     if (rows == 0) {
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NT * 16 * 4 * 8));
         if (CLUSTER) {
             MARLAAS_CUDA_TRY(cudaOccupancyMaxActiveClusters(&rows, kernel, &cfg));
         } else {
-            MARLAAS_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&rows, kernel, NT, 0));
+            MARLAAS_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&rows, kernel, NT, smem));
             rows *= pool->sm_count;
         }
         if (rows < 1) return fail(MARLAAS_ERR_CUDA, "k_vocab_rows: no room for a cluster of %d", C);
@@ -441,15 +511,11 @@ static marlaas_status_t launch_shape(const marlaas_pool* pool, const VocabRows& 
     while (C < 8 && vecs > (int64_t)C * 256 * 16) C *= 2;
     // few rows: more CTAs for each, down to one vector per thread
     while (C < 8 && r.T * C * 2 <= pool->sm_count && vecs > (int64_t)C * 256) C *= 2;
-    if (C > 1) {
-        if (F32 && vecs > 8 * 256 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, F32 ? 512 : 256, 16, true>(pool, r, C, st);
-        return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 256, 16, true>(pool, r, C, st);
-    }
-    if (vecs <= 32 * 8) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 32, 8, false>(pool, r, 1, st);
-    if (vecs <= 32 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 32, 16, false>(pool, r, 1, st);
-    if (vecs <= 64 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 64, 16, false>(pool, r, 1, st);
-    if (vecs <= 128 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 128, 16, false>(pool, r, 1, st);
-    return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 256, 16, false>(pool, r, 1, st);
+    if (C > 1) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 256, true>(pool, r, C, st);
+    if (vecs <= 32 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 32, false>(pool, r, 1, st);
+    if (vecs <= 64 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 64, false>(pool, r, 1, st);
+    if (vecs <= 128 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 128, false>(pool, r, 1, st);
+    return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 256, false>(pool, r, 1, st);
 }
 
 marlaas_status_t launch_vocab_rows(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st) {
