@@ -14,7 +14,8 @@ namespace marlaas {
 constexpr int OC_THREADS = 256;
 constexpr int OC_BLOCK = 256;               // elements that share their exponents: one warp, 8 per lane
 constexpr int OC_STATE_BYTES = 528;
-constexpr int OC_UNIT = 2048;               // elements of B (and at least, of A) per CTA
+constexpr int OC_UNIT = 2048;               // elements of B (and at least, of A) per CTA, or OC_LONG times as many
+constexpr int OC_LONG = 4;
 constexpr int OC_MAX_TENANTS = 256;         // tenants per launch
 constexpr uint32_t OC_M_ORDERS = 15, OC_V_ORDERS = 31;      // binary orders below the block's largest exponent
 
@@ -25,9 +26,13 @@ struct CompactTenant {
     float* B;
     uint8_t* sA;
     uint8_t* sB;
-    uint64_t id;
     int32_t slot;
     uint16_t rank, vec;     // vec: gradients and masters are 16-byte aligned
+    uint32_t key[2 * MARLAAS_MAX_PARTS];    // of the random bits: A and B of each projection
+};
+struct CompactHyper {
+    float b1, b2, one_b1, one_b2, gscale;
+    float sqrt_c2, eps, lr_c1, lr_wd;       // c1 = 1 / (1 - beta1^step), c2 = 1 / (1 - beta2^step)
 };
 // The table of a launch; three sizes, so that a few tenants do not pay for the parameters of 256.
 template <int N>
@@ -35,8 +40,8 @@ struct CompactArgs {
     int n, P, RP, cap;
     int64_t K, ldB;
     int64_t part_begin[MARLAAS_MAX_PARTS + 1];
-    float lr, b1, b2, one_b1, one_b2, eps, wd, gscale, c1, c2;
-    uint64_t seed, step;
+    CompactHyper h;
+    int unit;                       // elements of B per CTA
     bf16* At;
     bf16* Bs;
     int32_t first[2 * N + 1];       // first CTA of tenant t's A (2t) and B (2t + 1)
@@ -50,123 +55,152 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
     x = (x ^ (x >> 15)) * 0xB504F333u;
     return x ^ (x >> 16);
 }
-__device__ __forceinline__ uint32_t stream_key(uint64_t seed, uint64_t step, uint64_t tenant, uint32_t matrix) {
+static uint32_t stream_key(uint64_t seed, uint64_t step, uint64_t tenant, uint32_t matrix) {
     const uint32_t w[7] = {(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)step, (uint32_t)(step >> 32),
                            (uint32_t)tenant, (uint32_t)(tenant >> 32), matrix};
     uint32_t k = 0;
-#pragma unroll
     for (int i = 0; i < 7; ++i) k = mix32((k + 0x9E3779B9u) ^ w[i]);
     return k;
 }
 
 // Codes count in steps of 2^20 of the fp32 bit pattern (sign cut off): exponent and 3 mantissa bits.
 __device__ __forceinline__ uint32_t code_base(uint32_t E, uint32_t orders) { return E > orders ? (E - orders) * 8 : 0; }
-__device__ __forceinline__ float code_value(uint32_t c, uint32_t base) { return c ? __uint_as_float((c + base) << 20) : 0.f; }
-// The magnitude to store: not finite -> 0; never so large that rounding up leaves the finite numbers.
-__device__ __forceinline__ uint32_t magnitude(float x) {
-    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-    return b >= 0x7f800000u ? 0u : min(b, 0x7f700000u);
+__device__ __forceinline__ float code_value(uint32_t c, uint32_t base20) { return c ? __uint_as_float((c << 20) + base20) : 0.f; }
+__device__ __forceinline__ uint32_t byte_of(uint32_t w, int i) { return __byte_perm(w, 0, 0x4440 + i); }
+__device__ __forceinline__ uint32_t bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
+// The magnitude to store where a block holds numbers that are too large: not finite -> 0; never so large that rounding up
+// leaves the finite numbers.
+constexpr uint32_t OC_LARGEST = 0x7f700000u;
+__device__ __forceinline__ uint32_t magnitude(uint32_t b) { return b >= 0x7f800000u ? 0u : min(b, OC_LARGEST); }
 // The exponent that holds a block's largest magnitude also after rounding up.
 __device__ __forceinline__ uint32_t block_exponent(uint32_t largest) { return (largest + 0xfffffu) >> 23; }
 __device__ __forceinline__ int32_t code_of(uint32_t mag, uint32_t rnd16, uint32_t base) { return (int32_t)((mag + (rnd16 << 4)) >> 20) - (int32_t)base; }
+__device__ __forceinline__ float sqrt_approx(float x) {
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
-struct CompactHyper {
-    float lr, b1, b2, one_b1, one_b2, eps, wd, gscale, c1, c2;
+// What a lane holds of a block of 256 elements: elements 4 lane .. 4 lane + 3 and 128 further on.
+struct CompactLane {
+    float4 g[2], th[2];
+    uint32_t m[2], v[2], E;
 };
-
-// Elements [first, first + 256) of a matrix of n elements: lane's elements are 4 lane .. 4 lane + 3 and 128 further on.
-// Writes masters and state, leaves the new masters in th[8].
-__device__ __forceinline__ void compact_block(const CompactHyper& h, const float* __restrict__ grad, float* __restrict__ theta,
-                                              uint8_t* __restrict__ state, int64_t first, int64_t n, bool vec, uint32_t key,
-                                              int lane, float (&th)[8]) {
-    uint8_t* blk = state + (first / OC_BLOCK) * OC_STATE_BYTES;
-    float g[8];
-    uint32_t mc[2], vc[2];
-    bool in[2];
+__device__ __forceinline__ void compact_load(CompactLane& x, const float* __restrict__ grad, const float* __restrict__ theta,
+                                             const uint8_t* __restrict__ blk, int64_t first, int64_t n, bool vec, int lane) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         const int64_t e = first + 128 * q + 4 * lane;
-        in[q] = e < n;      // n is a multiple of 8
-        mc[q] = vc[q] = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g[4 * q + i] = th[4 * q + i] = 0.f;
-        if (in[q]) {
-            mc[q] = reinterpret_cast<const uint32_t*>(blk)[32 * q + lane];
-            vc[q] = reinterpret_cast<const uint32_t*>(blk + 256)[32 * q + lane];
+        x.m[q] = x.v[q] = 0;
+        x.g[q] = x.th[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (e < n) {        // n is a multiple of 8
+            x.m[q] = reinterpret_cast<const uint32_t*>(blk)[32 * q + lane];
+            x.v[q] = reinterpret_cast<const uint32_t*>(blk + 256)[32 * q + lane];
             if (vec) {
-                const float4 a = __ldcs(reinterpret_cast<const float4*>(grad + e)), b = *reinterpret_cast<const float4*>(theta + e);
-                g[4 * q] = a.x; g[4 * q + 1] = a.y; g[4 * q + 2] = a.z; g[4 * q + 3] = a.w;
-                th[4 * q] = b.x; th[4 * q + 1] = b.y; th[4 * q + 2] = b.z; th[4 * q + 3] = b.w;
+                x.g[q] = __ldcs(reinterpret_cast<const float4*>(grad + e));
+                x.th[q] = __ldcs(reinterpret_cast<const float4*>(theta + e));
             } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    g[4 * q + i] = grad[e + i];
-                    th[4 * q + i] = theta[e + i];
-                }
+                x.g[q] = make_float4(grad[e], grad[e + 1], grad[e + 2], grad[e + 3]);
+                x.th[q] = make_float4(theta[e], theta[e + 1], theta[e + 2], theta[e + 3]);
             }
         }
     }
-    const uint32_t E = *reinterpret_cast<const uint16_t*>(blk + 512);
-    const uint32_t bm = code_base(E & 255u, OC_M_ORDERS), bv = code_base(E >> 8, OC_V_ORDERS);
-    uint32_t am[8], av[8], neg = 0, top_m = 0, top_v = 0;
+    x.E = *reinterpret_cast<const uint16_t*>(blk + 512);
+}
+
+// The step of a block: writes masters and state, leaves the new masters in x.th.
+__device__ __forceinline__ void compact_step(CompactLane& x, const CompactHyper& h, float* __restrict__ theta, uint8_t* __restrict__ blk,
+                                             int64_t first, int64_t n, bool vec, uint32_t key, int lane) {
+    const uint32_t bm = code_base(x.E & 255u, OC_M_ORDERS) << 20, bv = code_base(x.E >> 8, OC_V_ORDERS) << 20;
+    uint32_t mb[8], vb[8], top_m = 0, top_v = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t cm = (mc[i >> 2] >> (8 * (i & 3))) & 255u, cv = (vc[i >> 2] >> (8 * (i & 3))) & 255u;
-        float m = code_value(cm & 127u, bm);
-        m = (cm & 128u) ? -m : m;
-        float v = code_value(cv, bv);
-        const float gr = __fmul_rn(h.gscale, g[i]);
-        // separate roundings of products and sums: the same bits wherever this is computed
-        m = __fadd_rn(__fmul_rn(h.b1, m), __fmul_rn(h.one_b1, gr));
-        v = __fadd_rn(__fmul_rn(h.b2, v), __fmul_rn(__fmul_rn(h.one_b2, gr), gr));
-        const float mh = m * h.c1, vh = v * h.c2;
-        th[i] -= h.lr * (mh / (sqrtf(vh) + h.eps) + h.wd * th[i]);
-        am[i] = magnitude(m);
-        av[i] = magnitude(v);
-        neg |= (uint32_t)(m < 0.f) << i;
-        top_m = max(top_m, am[i]);
-        top_v = max(top_v, av[i]);
+    for (int q = 0; q < 2; ++q) {
+        float2* th = reinterpret_cast<float2*>(&x.th[q]);
+        const float2* gp = reinterpret_cast<const float2*>(&x.g[q]);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            float mo[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t c = byte_of(x.m[q], 2 * p + i);
+                mo[i] = __uint_as_float(__float_as_uint(code_value(c & 127u, bm)) | ((c & 128u) << 24));
+            }
+            const float2 vo = make_float2(code_value(byte_of(x.v[q], 2 * p), bv), code_value(byte_of(x.v[q], 2 * p + 1), bv));
+            // products and sums rounded one by one: the same bits wherever this is computed
+            const float2 g = __fmul2_rn(make_float2(h.gscale, h.gscale), gp[p]);
+            const float2 m = __fadd2_rn(__fmul2_rn(make_float2(h.b1, h.b1), make_float2(mo[0], mo[1])), __fmul2_rn(make_float2(h.one_b1, h.one_b1), g));
+            const float2 v = __fadd2_rn(__fmul2_rn(make_float2(h.b2, h.b2), vo), __fmul2_rn(__fmul2_rn(make_float2(h.one_b2, h.one_b2), g), g));
+            // theta -= lr (c1 m / (sqrt(c2 v) + eps) + wd theta), root and reciprocal to about an ulp of the step
+            const float2 u = __fmul2_rn(m, make_float2(h.lr_c1, h.lr_c1));
+            th[p].x = fmaf(-h.lr_wd, th[p].x, th[p].x) - u.x * rcp_approx(fmaf(sqrt_approx(v.x), h.sqrt_c2, h.eps));
+            th[p].y = fmaf(-h.lr_wd, th[p].y, th[p].y) - u.y * rcp_approx(fmaf(sqrt_approx(v.y), h.sqrt_c2, h.eps));
+            const int k = 4 * q + 2 * p;
+            mb[k] = __float_as_uint(m.x);
+            mb[k + 1] = __float_as_uint(m.y);
+            vb[k] = __float_as_uint(v.x) & 0x7fffffffu;
+            vb[k + 1] = __float_as_uint(v.y) & 0x7fffffffu;
+            top_m = max(top_m, max(mb[k] & 0x7fffffffu, mb[k + 1] & 0x7fffffffu));
+            top_v = max(top_v, max(vb[k], vb[k + 1]));
+        }
+        const int64_t e = first + 128 * q + 4 * lane;
+        if (e < n) {
+            if (vec) {
+                __stcs(reinterpret_cast<float4*>(theta + e), x.th[q]);
+            } else {
+                theta[e] = x.th[q].x; theta[e + 1] = x.th[q].y; theta[e + 2] = x.th[q].z; theta[e + 3] = x.th[q].w;
+            }
+        }
     }
     top_m = __reduce_max_sync(0xffffffffu, top_m);
     top_v = __reduce_max_sync(0xffffffffu, top_v);
+    if (max(top_m, top_v) > OC_LARGEST) {
+        top_m = top_v = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t a = magnitude(mb[k] & 0x7fffffffu);
+            mb[k] = a | (__uint_as_float(mb[k]) < 0.f ? 0x80000000u : 0u);
+            vb[k] = magnitude(vb[k]);
+            top_m = max(top_m, a);
+            top_v = max(top_v, vb[k]);
+        }
+        top_m = __reduce_max_sync(0xffffffffu, top_m);
+        top_v = __reduce_max_sync(0xffffffffu, top_v);
+    }
     const uint32_t Em = block_exponent(top_m), Ev = block_exponent(top_v);
     const uint32_t nm = code_base(Em, OC_M_ORDERS), nv = code_base(Ev, OC_V_ORDERS);
-    mc[0] = mc[1] = vc[0] = vc[1] = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t r = mix32((uint32_t)first + (uint32_t)(128 * (i >> 2) + 4 * lane + (i & 3)) + key);
-        const uint32_t cm = (uint32_t)max(code_of(am[i], r & 0xffffu, nm), 0) | (((neg >> i) & 1u) << 7);
-        const uint32_t cv = av[i] ? (uint32_t)max(code_of(av[i], r >> 16, nv), 1) : 0u;
-        mc[i >> 2] |= cm << (8 * (i & 3));
-        vc[i >> 2] |= cv << (8 * (i & 3));
-    }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        reinterpret_cast<uint32_t*>(blk)[32 * q + lane] = mc[q];
-        reinterpret_cast<uint32_t*>(blk + 256)[32 * q + lane] = vc[q];
-        if (in[q]) {
-            const int64_t e = first + 128 * q + 4 * lane;
-            if (vec) {
-                *reinterpret_cast<float4*>(theta + e) = make_float4(th[4 * q], th[4 * q + 1], th[4 * q + 2], th[4 * q + 3]);
-            } else {
+        uint32_t cm[4], cv[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) theta[e + i] = th[4 * q + i];
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int k = 4 * q + i;
+            const uint32_t r = mix32((uint32_t)first + (uint32_t)(128 * q + 4 * lane + i) + key);
+            // (a sign without a magnitude, of a -0 or a moment that was cut off, is a zero too)
+            cm[i] = (uint32_t)max(code_of(mb[k] & 0x7fffffffu, r & 0xffffu, nm), 0) | (mb[k] > 0x80000000u ? 128u : 0u);
+            cv[i] = vb[k] ? (uint32_t)max(code_of(vb[k], r >> 16, nv), 1) : 0u;
         }
+        reinterpret_cast<uint32_t*>(blk)[32 * q + lane] = bytes(cm[0], cm[1], cm[2], cm[3]);
+        reinterpret_cast<uint32_t*>(blk + 256)[32 * q + lane] = bytes(cv[0], cv[1], cv[2], cv[3]);
     }
     if (lane == 0) *reinterpret_cast<uint16_t*>(blk + 512) = (uint16_t)(Em | (Ev << 8));
 }
 
-// Rows of A per CTA: whole state blocks, at least 64 rows (128-byte runs of the pool's At rows) and OC_UNIT elements.
-__host__ __device__ __forceinline__ int rows_per_cta(int r) {
+// Rows of A per CTA: whole state blocks, at least 64 rows (128-byte runs of the pool's At rows) and `unit` elements.
+__host__ __device__ __forceinline__ int rows_per_cta(int r, int unit) {
     int g = r, b = OC_BLOCK;        // 256 / gcd(256, r) rows are whole blocks
     while (b) {
         const int c = g % b;
         g = b;
         b = c;
     }
-    const int step = OC_BLOCK / g, want = max(64, (OC_UNIT + r - 1) / r);
+    const int step = OC_BLOCK / g, want = max(64, (unit + r - 1) / r);
     return (want + step - 1) / step * step;
 }
 __host__ __device__ __forceinline__ int tile_pitch(int r) { return r | 1; }     // odd: column reads spread over the banks
@@ -188,51 +222,66 @@ __global__ void __launch_bounds__(OC_THREADS) k_adamw_compact(const __grid_const
     const int r = t.rank;
     const bool is_b = lo & 1, vec = t.vec != 0;
     int u = (int)blockIdx.x - a.first[lo];
-    const CompactHyper h = {a.lr, a.b1, a.b2, a.one_b1, a.one_b2, a.eps, a.wd, a.gscale, a.c1, a.c2};
     if (is_b) {
         int p = 0;
         int64_t soff = 0;
         for (; p < a.P - 1; ++p) {
             const int64_t n = (int64_t)r * (a.part_begin[p + 1] - a.part_begin[p]);
-            const int units = (int)((n + OC_UNIT - 1) / OC_UNIT);
+            const int units = (int)((n + a.unit - 1) / a.unit);
             if (u < units) break;
             u -= units;
             soff += state_bytes(n);
         }
         const int64_t c0 = a.part_begin[p], Np = a.part_begin[p + 1] - c0, n = (int64_t)r * Np;
-        const uint32_t key = stream_key(a.seed, a.step, t.id, 2u * p + 1u);
-        const int64_t e0 = (int64_t)u * OC_UNIT + warp * OC_BLOCK;
-        if (e0 >= n) return;
-        float th[8];
-        compact_block(h, t.dB + (int64_t)r * c0, t.B + (int64_t)r * c0, t.sB + soff, e0, n, vec, key, lane, th);
+        const uint32_t key = t.key[2 * p + 1];
+        const float* grad = t.dB + (int64_t)r * c0;
+        float* theta = t.B + (int64_t)r * c0;
+        uint8_t* state = t.sB + soff;
         bf16* bs = a.Bs + (size_t)t.slot * a.RP * a.ldB + c0;
+        const int64_t end = min((int64_t)(u + 1) * a.unit, n);
+        // the unit's first element is in row j0 at column i0; what follows is found by 32-bit division
+        const int64_t u0 = (int64_t)u * a.unit, j0 = u0 / Np, i0 = u0 - j0 * Np;
+        for (int64_t e0 = u0 + warp * OC_BLOCK; e0 < end; e0 += OC_THREADS / 32 * OC_BLOCK) {
+            CompactLane x;
+            uint8_t* blk = state + (e0 / OC_BLOCK) * OC_STATE_BYTES;
+            compact_load(x, grad, theta, blk, e0, n, vec, lane);
+            compact_step(x, a.h, theta, blk, e0, n, vec, key, lane);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int64_t e = e0 + 128 * q + 4 * lane;
-            if (e >= n) continue;
-            const int64_t j = e / Np;       // four elements of one row: Np is a multiple of 8
-            __nv_bfloat162 x = __floats2bfloat162_rn(th[4 * q], th[4 * q + 1]), y = __floats2bfloat162_rn(th[4 * q + 2], th[4 * q + 3]);
-            *reinterpret_cast<uint2*>(bs + j * a.ldB + (e - j * Np)) = make_uint2(*reinterpret_cast<uint32_t*>(&x), *reinterpret_cast<uint32_t*>(&y));
+            for (int q = 0; q < 2; ++q) {
+                const int64_t e = e0 + 128 * q + 4 * lane;
+                if (e >= n) continue;
+                const uint32_t c = (uint32_t)(i0 + (e - u0)), dj = c / (uint32_t)Np;      // four elements of one row: Np is a multiple of 8
+                __nv_bfloat162 y = __floats2bfloat162_rn(x.th[q].x, x.th[q].y), z = __floats2bfloat162_rn(x.th[q].z, x.th[q].w);
+                *reinterpret_cast<uint2*>(bs + (j0 + dj) * a.ldB + (c - dj * (uint32_t)Np)) =
+                    make_uint2(*reinterpret_cast<uint32_t*>(&y), *reinterpret_cast<uint32_t*>(&z));
+            }
         }
         return;
     }
-    const int R = rows_per_cta(r), pitch = tile_pitch(r);
+    const int R = rows_per_cta(r, a.unit), pitch = tile_pitch(r);
     const int per_part = (int)((a.K + R - 1) / R);
     const int p = u / per_part;
     const int64_t k0 = (int64_t)(u - p * per_part) * R, n = a.K * r, poff = (int64_t)p * n;
-    const int rows = (int)min((int64_t)R, a.K - k0);
-    const uint32_t key = stream_key(a.seed, a.step, t.id, 2u * p);
-    for (int b = warp * OC_BLOCK; b < rows * r; b += OC_THREADS / 32 * OC_BLOCK) {
-        float th[8];
-        compact_block(h, t.dA + poff, t.A + poff, t.sA + p * state_bytes(n), k0 * r + b, n, vec, key, lane, th);
+    const int rows = (int)min((int64_t)R, a.K - k0), elems = rows * r;
+    const uint32_t key = t.key[2 * p], over_r = r > 1 ? 0xffffffffu / (uint32_t)r + 1u : 0u;      // e / r = high word of e over_r (e < 2^16)
+    const float* grad = t.dA + poff;
+    float* theta = t.A + poff;
+    uint8_t* state = t.sA + p * state_bytes(n);
+    for (int b = warp * OC_BLOCK; b < elems; b += OC_THREADS / 32 * OC_BLOCK) {
+        CompactLane x;
+        const int64_t e0 = k0 * r + b;
+        uint8_t* blk = state + (e0 / OC_BLOCK) * OC_STATE_BYTES;
+        compact_load(x, grad, theta, blk, e0, n, vec, lane);
+        compact_step(x, a.h, theta, blk, e0, n, vec, key, lane);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const int e = b + 128 * q + 4 * lane;
-            int kk = e / r, j = e - kk * r;
-            if (e >= rows * r) continue;
+            if (e >= elems) continue;
+            const float th[4] = {x.th[q].x, x.th[q].y, x.th[q].z, x.th[q].w};
+            int kk = r > 1 ? (int)__umulhi((uint32_t)e, over_r) : e, j = e - kk * r;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                tile[kk * pitch + j] = __float2bfloat16_rn(th[4 * q + i]);
+                tile[kk * pitch + j] = __float2bfloat16_rn(th[i]);
                 if (++j == r) {
                     j = 0;
                     ++kk;
@@ -266,7 +315,7 @@ __global__ void __launch_bounds__(OC_THREADS) k_compact_export(const uint8_t* __
     for (int64_t b = w; b < blocks; b += nw) {
         const uint8_t* blk = state + b * OC_STATE_BYTES;
         const uint32_t E = *reinterpret_cast<const uint16_t*>(blk + 512);
-        const uint32_t bm = code_base(E & 255u, OC_M_ORDERS), bv = code_base(E >> 8, OC_V_ORDERS);
+        const uint32_t bm = code_base(E & 255u, OC_M_ORDERS) << 20, bv = code_base(E >> 8, OC_V_ORDERS) << 20;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const uint32_t mc = reinterpret_cast<const uint32_t*>(blk)[32 * q + lane];
@@ -274,10 +323,9 @@ __global__ void __launch_bounds__(OC_THREADS) k_compact_export(const uint8_t* __
             float fm[4], fv[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t cm = (mc >> (8 * i)) & 255u;
-                fm[i] = code_value(cm & 127u, bm);
-                fm[i] = (cm & 128u) ? -fm[i] : fm[i];
-                fv[i] = code_value((vc >> (8 * i)) & 255u, bv);
+                const uint32_t c = byte_of(mc, i);
+                fm[i] = __uint_as_float(__float_as_uint(code_value(c & 127u, bm)) | ((c & 128u) << 24));
+                fv[i] = code_value(byte_of(vc, i), bv);
             }
             const int64_t e = b * OC_BLOCK + 128 * q + 4 * lane;
             if (m) *reinterpret_cast<float4*>(m + e) = make_float4(fm[0], fm[1], fm[2], fm[3]);
@@ -287,26 +335,27 @@ __global__ void __launch_bounds__(OC_THREADS) k_compact_export(const uint8_t* __
 }
 
 template <int N>
-static marlaas_status_t launch_compact(const marlaas_pool* pool, const CompactTenant* t, int n, const marlaas_adamw_t& hp,
-                                       uint64_t seed, cudaStream_t st) {
+static marlaas_status_t launch_compact(const marlaas_pool* pool, const CompactTenant* t, int n, const marlaas_adamw_t& hp, cudaStream_t st) {
     CompactArgs<N> a;
     a.n = n; a.P = pool->P; a.RP = pool->RP; a.cap = pool->cap; a.K = pool->K; a.ldB = pool->ldB;
     for (int p = 0; p <= MARLAAS_MAX_PARTS; ++p) a.part_begin[p] = pool->part_begin[p];
-    a.lr = hp.lr; a.b1 = hp.beta1; a.b2 = hp.beta2; a.one_b1 = 1.f - hp.beta1; a.one_b2 = 1.f - hp.beta2;
-    a.eps = hp.eps; a.wd = hp.weight_decay; a.gscale = hp.grad_scale;
-    a.c1 = (float)(1.0 / (1.0 - std::pow((double)hp.beta1, (double)hp.step)));
-    a.c2 = (float)(1.0 / (1.0 - std::pow((double)hp.beta2, (double)hp.step)));
-    a.seed = seed; a.step = (uint64_t)hp.step;
+    const double c1 = 1.0 / (1.0 - std::pow((double)hp.beta1, (double)hp.step)), c2 = 1.0 / (1.0 - std::pow((double)hp.beta2, (double)hp.step));
+    a.h.b1 = hp.beta1; a.h.b2 = hp.beta2; a.h.one_b1 = 1.f - hp.beta1; a.h.one_b2 = 1.f - hp.beta2; a.h.gscale = hp.grad_scale;
+    a.h.sqrt_c2 = (float)std::sqrt(c2); a.h.eps = hp.eps; a.h.lr_c1 = (float)(hp.lr * c1); a.h.lr_wd = hp.lr * hp.weight_decay;
+    // longer units spread a CTA's set-up over more elements, shorter ones a small update over more SMs
+    int64_t elems = 0;
+    for (int i = 0; i < n; ++i) elems += t[i].rank * (pool->P * pool->K + pool->N);
+    a.unit = elems >= (int64_t)pool->sm_count * 8 * OC_UNIT * OC_LONG ? OC_UNIT * OC_LONG : OC_UNIT;
     a.At = pool->d_At; a.Bs = pool->d_Bs;
     int64_t ctas = 0;
     size_t smem = 0;
     for (int i = 0; i < n; ++i) {
-        const int r = t[i].rank, R = rows_per_cta(r);
+        const int r = t[i].rank, R = rows_per_cta(r, a.unit);
         a.t[i] = t[i];
         a.first[2 * i] = (int32_t)ctas;
         ctas += (int64_t)pool->P * cdiv(pool->K, R);
         a.first[2 * i + 1] = (int32_t)ctas;
-        for (int p = 0; p < pool->P; ++p) ctas += cdiv((int64_t)r * (pool->part_begin[p + 1] - pool->part_begin[p]), OC_UNIT);
+        for (int p = 0; p < pool->P; ++p) ctas += cdiv((int64_t)r * (pool->part_begin[p + 1] - pool->part_begin[p]), (int64_t)a.unit);
         smem = std::max(smem, sizeof(bf16) * (size_t)R * tile_pitch(r));
         if (ctas >= (1ll << 31)) return fail(MARLAAS_ERR_INVALID_ARG, "pool_adamw_compact_commit: too many elements for one call");
     }
@@ -367,15 +416,16 @@ marlaas_status_t marlaas_adapter_pool_adamw_compact_commit(marlaas_pool_t* pool,
         }
         if (!state_A[i] || !state_B[i] || (((uintptr_t)state_A[i] | (uintptr_t)state_B[i]) & 15))
             return fail(MARLAAS_ERR_INVALID_ARG, "%s: tenant %llu: a state is NULL or not 16-byte aligned", fn, id);
-        t[i] = CompactTenant{dA[i], dB[i], A[i], B[i], (uint8_t*)state_A[i], (uint8_t*)state_B[i], tenant_ids[i], slot,
-                             (uint16_t)pool->slots[slot].rank, (uint16_t)((low & 15) == 0)};
+        t[i] = CompactTenant{dA[i], dB[i], A[i], B[i], (uint8_t*)state_A[i], (uint8_t*)state_B[i], slot,
+                             (uint16_t)pool->slots[slot].rank, (uint16_t)((low & 15) == 0), {}};
+        for (uint32_t k = 0; k < 2u * pool->P; ++k) t[i].key[k] = stream_key(seed, (uint64_t)hp->step, tenant_ids[i], k);
     }
     MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
     for (int i0 = 0; i0 < n; i0 += OC_MAX_TENANTS) {
         const int m = std::min(OC_MAX_TENANTS, n - i0);
-        marlaas_status_t rc = m <= 8    ? launch_compact<8>(pool, t.data() + i0, m, *hp, seed, (cudaStream_t)cuda_stream)
-                              : m <= 48 ? launch_compact<48>(pool, t.data() + i0, m, *hp, seed, (cudaStream_t)cuda_stream)
-                                        : launch_compact<OC_MAX_TENANTS>(pool, t.data() + i0, m, *hp, seed, (cudaStream_t)cuda_stream);
+        marlaas_status_t rc = m <= 8    ? launch_compact<8>(pool, t.data() + i0, m, *hp, (cudaStream_t)cuda_stream)
+                              : m <= 48 ? launch_compact<48>(pool, t.data() + i0, m, *hp, (cudaStream_t)cuda_stream)
+                                        : launch_compact<OC_MAX_TENANTS>(pool, t.data() + i0, m, *hp, (cudaStream_t)cuda_stream);
         if (rc != MARLAAS_OK) return rc;
     }
     for (int i = 0; i < n; ++i) {
