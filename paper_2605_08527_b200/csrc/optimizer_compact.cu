@@ -67,8 +67,20 @@ static uint32_t stream_key(uint64_t seed, uint64_t step, uint64_t tenant, uint32
 __device__ __forceinline__ uint32_t code_base(uint32_t E, uint32_t orders) { return E > orders ? (E - orders) * 8 : 0; }
 __device__ __forceinline__ float code_value(uint32_t c, uint32_t base20) { return c ? __uint_as_float((c << 20) + base20) : 0.f; }
 __device__ __forceinline__ uint32_t byte_of(uint32_t w, int i) { return __byte_perm(w, 0, 0x4440 + i); }
-__device__ __forceinline__ uint32_t bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+// Byte i of w in bits 16 to 23, so that one multiply-add by 16 makes a code's bit pattern of it.
+__device__ __forceinline__ uint32_t byte_at_16(uint32_t w, int i) { return __byte_perm(w, 0, 0x4044 + (i << 8)); }
+// Four numbers as unsigned bytes, cut off at 0 and 255.
+__device__ __forceinline__ uint32_t bytes(int32_t a, int32_t b, int32_t c, int32_t d) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 t;\n\t"
+        "cvt.pack.sat.u8.s32.b32 t, %4, %3, 0;\n\t"
+        "cvt.pack.sat.u8.s32.b32 %0, %2, %1, t;\n\t}"
+        : "=r"(r) : "r"(a), "r"(b), "r"(c), "r"(d));
+    return r;
+}
+// The top bits of four words as 0x80 in four bytes.
+__device__ __forceinline__ uint32_t signs(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410) & 0x80808080u;
 }
 // The magnitude to store where a block holds numbers that are too large: not finite -> 0; never so large that rounding up
 // leaves the finite numbers.
@@ -76,7 +88,8 @@ constexpr uint32_t OC_LARGEST = 0x7f700000u;
 __device__ __forceinline__ uint32_t magnitude(uint32_t b) { return b >= 0x7f800000u ? 0u : min(b, OC_LARGEST); }
 // The exponent that holds a block's largest magnitude also after rounding up.
 __device__ __forceinline__ uint32_t block_exponent(uint32_t largest) { return (largest + 0xfffffu) >> 23; }
-__device__ __forceinline__ int32_t code_of(uint32_t mag, uint32_t rnd16, uint32_t base) { return (int32_t)((mag + (rnd16 << 4)) >> 20) - (int32_t)base; }
+// (below the block's range: 0 or negative)
+__device__ __forceinline__ int32_t code_of(uint32_t mag, uint32_t rnd16, uint32_t base20) { return (int32_t)(rnd16 * 16u + mag - base20) >> 20; }
 __device__ __forceinline__ float sqrt_approx(float x) {
     float r;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -93,20 +106,26 @@ struct CompactLane {
     float4 g[2], th[2];
     uint32_t m[2], v[2], E;
 };
+// `left`: elements of the matrix from the block's first on (a multiple of 8); below 256 the rest of the block is zeros.
 __device__ __forceinline__ void compact_load(CompactLane& x, const float* __restrict__ grad, const float* __restrict__ theta,
-                                             const uint8_t* __restrict__ blk, int64_t first, int64_t n, bool vec, int lane) {
+                                             const uint8_t* __restrict__ blk, int left, bool vec, int lane) {
+    if (left >= OC_BLOCK && vec) {
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        const int64_t e = first + 128 * q + 4 * lane;
-        x.m[q] = x.v[q] = 0;
-        x.g[q] = x.th[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (e < n) {        // n is a multiple of 8
+        for (int q = 0; q < 2; ++q) {
             x.m[q] = reinterpret_cast<const uint32_t*>(blk)[32 * q + lane];
             x.v[q] = reinterpret_cast<const uint32_t*>(blk + 256)[32 * q + lane];
-            if (vec) {
-                x.g[q] = __ldcs(reinterpret_cast<const float4*>(grad + e));
-                x.th[q] = __ldcs(reinterpret_cast<const float4*>(theta + e));
-            } else {
+            x.g[q] = __ldcs(reinterpret_cast<const float4*>(grad) + 32 * q + lane);
+            x.th[q] = __ldcs(reinterpret_cast<const float4*>(theta) + 32 * q + lane);
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int e = 128 * q + 4 * lane;
+            x.m[q] = x.v[q] = 0;
+            x.g[q] = x.th[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (e < left) {
+                x.m[q] = reinterpret_cast<const uint32_t*>(blk)[32 * q + lane];
+                x.v[q] = reinterpret_cast<const uint32_t*>(blk + 256)[32 * q + lane];
                 x.g[q] = make_float4(grad[e], grad[e + 1], grad[e + 2], grad[e + 3]);
                 x.th[q] = make_float4(theta[e], theta[e + 1], theta[e + 2], theta[e + 3]);
             }
@@ -115,9 +134,9 @@ __device__ __forceinline__ void compact_load(CompactLane& x, const float* __rest
     x.E = *reinterpret_cast<const uint16_t*>(blk + 512);
 }
 
-// The step of a block: writes masters and state, leaves the new masters in x.th.
+// The step of a block: writes masters and state, leaves the new masters in x.th.  `rnd`: the block's first element + key.
 __device__ __forceinline__ void compact_step(CompactLane& x, const CompactHyper& h, float* __restrict__ theta, uint8_t* __restrict__ blk,
-                                             int64_t first, int64_t n, bool vec, uint32_t key, int lane) {
+                                             int left, bool vec, uint32_t rnd, int lane) {
     const uint32_t bm = code_base(x.E & 255u, OC_M_ORDERS) << 20, bv = code_base(x.E >> 8, OC_V_ORDERS) << 20;
     uint32_t mb[8], vb[8], top_m = 0, top_v = 0;
 #pragma unroll
@@ -126,17 +145,18 @@ __device__ __forceinline__ void compact_step(CompactLane& x, const CompactHyper&
         const float2* gp = reinterpret_cast<const float2*>(&x.g[q]);
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            float mo[2];
+            float mo[2], vo[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint32_t c = byte_of(x.m[q], 2 * p + i);
-                mo[i] = __uint_as_float(__float_as_uint(code_value(c & 127u, bm)) | ((c & 128u) << 24));
+                const uint32_t cm = byte_at_16(x.m[q] & 0x7f7f7f7fu, 2 * p + i), cv = byte_at_16(x.v[q], 2 * p + i);
+                const uint32_t sign = __byte_perm(x.m[q], 0, 0x0444 + ((2 * p + i) << 12)) & 0x80000000u;
+                mo[i] = __uint_as_float((cm ? cm * 16u + bm : 0u) | sign);
+                vo[i] = __uint_as_float(cv ? cv * 16u + bv : 0u);
             }
-            const float2 vo = make_float2(code_value(byte_of(x.v[q], 2 * p), bv), code_value(byte_of(x.v[q], 2 * p + 1), bv));
             // products and sums rounded one by one: the same bits wherever this is computed
             const float2 g = __fmul2_rn(make_float2(h.gscale, h.gscale), gp[p]);
             const float2 m = __fadd2_rn(__fmul2_rn(make_float2(h.b1, h.b1), make_float2(mo[0], mo[1])), __fmul2_rn(make_float2(h.one_b1, h.one_b1), g));
-            const float2 v = __fadd2_rn(__fmul2_rn(make_float2(h.b2, h.b2), vo), __fmul2_rn(__fmul2_rn(make_float2(h.one_b2, h.one_b2), g), g));
+            const float2 v = __fadd2_rn(__fmul2_rn(make_float2(h.b2, h.b2), make_float2(vo[0], vo[1])), __fmul2_rn(__fmul2_rn(make_float2(h.one_b2, h.one_b2), g), g));
             // theta -= lr (c1 m / (sqrt(c2 v) + eps) + wd theta), root and reciprocal to about an ulp of the step
             const float2 u = __fmul2_rn(m, make_float2(h.lr_c1, h.lr_c1));
             th[p].x = fmaf(-h.lr_wd, th[p].x, th[p].x) - u.x * rcp_approx(fmaf(sqrt_approx(v.x), h.sqrt_c2, h.eps));
@@ -149,8 +169,8 @@ __device__ __forceinline__ void compact_step(CompactLane& x, const CompactHyper&
             top_m = max(top_m, max(mb[k] & 0x7fffffffu, mb[k + 1] & 0x7fffffffu));
             top_v = max(top_v, max(vb[k], vb[k + 1]));
         }
-        const int64_t e = first + 128 * q + 4 * lane;
-        if (e < n) {
+        const int e = 128 * q + 4 * lane;
+        if (e < left) {
             if (vec) {
                 __stcs(reinterpret_cast<float4*>(theta + e), x.th[q]);
             } else {
@@ -174,19 +194,19 @@ __device__ __forceinline__ void compact_step(CompactLane& x, const CompactHyper&
         top_v = __reduce_max_sync(0xffffffffu, top_v);
     }
     const uint32_t Em = block_exponent(top_m), Ev = block_exponent(top_v);
-    const uint32_t nm = code_base(Em, OC_M_ORDERS), nv = code_base(Ev, OC_V_ORDERS);
+    const uint32_t nm = code_base(Em, OC_M_ORDERS) << 20, nv = code_base(Ev, OC_V_ORDERS) << 20;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        uint32_t cm[4], cv[4];
+        int32_t cm[4], cv[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int k = 4 * q + i;
-            const uint32_t r = mix32((uint32_t)first + (uint32_t)(128 * q + 4 * lane + i) + key);
-            // (a sign without a magnitude, of a -0 or a moment that was cut off, is a zero too)
-            cm[i] = (uint32_t)max(code_of(mb[k] & 0x7fffffffu, r & 0xffffu, nm), 0) | (mb[k] > 0x80000000u ? 128u : 0u);
-            cv[i] = vb[k] ? (uint32_t)max(code_of(vb[k], r >> 16, nv), 1) : 0u;
+            const uint32_t r = mix32(rnd + 4 * lane + (uint32_t)(128 * q + i));
+            cm[i] = code_of(mb[k] & 0x7fffffffu, r & 0xffffu, nm);
+            cv[i] = max(code_of(vb[k], r >> 16, nv), (int32_t)min(vb[k], 1u));       // a positive v keeps the smallest code
         }
-        reinterpret_cast<uint32_t*>(blk)[32 * q + lane] = bytes(cm[0], cm[1], cm[2], cm[3]);
+        // (a sign without a magnitude, of a -0 or a moment that was cut off, is a zero too)
+        reinterpret_cast<uint32_t*>(blk)[32 * q + lane] = bytes(cm[0], cm[1], cm[2], cm[3]) | signs(mb[4 * q], mb[4 * q + 1], mb[4 * q + 2], mb[4 * q + 3]);
         reinterpret_cast<uint32_t*>(blk + 256)[32 * q + lane] = bytes(cv[0], cv[1], cv[2], cv[3]);
     }
     if (lane == 0) *reinterpret_cast<uint16_t*>(blk + 512) = (uint16_t)(Em | (Ev << 8));
@@ -210,7 +230,7 @@ __device__ __forceinline__ int64_t state_bytes(int64_t n) { return (n + OC_BLOCK
 // One CTA per unit: a run of B, stored as the pool stores it, or a tile of rows of A, which goes through shared memory so
 // that both the reads of A [K][r] and the writes of the pool's At rows [r][K] are contiguous.
 template <int N>
-__global__ void __launch_bounds__(OC_THREADS) k_adamw_compact(const __grid_constant__ CompactArgs<N> a) {
+__global__ void __launch_bounds__(OC_THREADS, 4) k_adamw_compact(const __grid_constant__ CompactArgs<N> a) {
     extern __shared__ bf16 tile[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int lo = 0, hi = 2 * a.n;       // the last entry whose first CTA is not after this one
@@ -238,21 +258,30 @@ __global__ void __launch_bounds__(OC_THREADS) k_adamw_compact(const __grid_const
         float* theta = t.B + (int64_t)r * c0;
         uint8_t* state = t.sB + soff;
         bf16* bs = a.Bs + (size_t)t.slot * a.RP * a.ldB + c0;
-        const int64_t end = min((int64_t)(u + 1) * a.unit, n);
-        // the unit's first element is in row j0 at column i0; what follows is found by 32-bit division
-        const int64_t u0 = (int64_t)u * a.unit, j0 = u0 / Np, i0 = u0 - j0 * Np;
-        for (int64_t e0 = u0 + warp * OC_BLOCK; e0 < end; e0 += OC_THREADS / 32 * OC_BLOCK) {
+        const int64_t u0 = (int64_t)u * a.unit;
+        const int count = (int)min((int64_t)a.unit, n - u0);
+        grad += u0;
+        theta += u0;
+        state += u0 / OC_BLOCK * OC_STATE_BYTES;
+        // the unit begins in row j0 at column i0.  Rows longer than a unit: at most one ends in it; else e / Np is the high
+        // word of e over_n, both below 2^16
+        const int64_t j0 = u0 / Np;
+        const uint32_t i0 = (uint32_t)(u0 - j0 * Np), width = (uint32_t)Np;
+        const bool wide = Np >= a.unit;
+        const uint32_t over_n = wide ? 0u : 0xffffffffu / width + 1u;
+        bs += j0 * a.ldB;
+        for (int b = warp * OC_BLOCK; b < count; b += OC_THREADS / 32 * OC_BLOCK) {
             CompactLane x;
-            uint8_t* blk = state + (e0 / OC_BLOCK) * OC_STATE_BYTES;
-            compact_load(x, grad, theta, blk, e0, n, vec, lane);
-            compact_step(x, a.h, theta, blk, e0, n, vec, key, lane);
+            uint8_t* blk = state + b / OC_BLOCK * OC_STATE_BYTES;
+            compact_load(x, grad + b, theta + b, blk, count - b, vec, lane);
+            compact_step(x, a.h, theta + b, blk, count - b, vec, (uint32_t)u0 + (uint32_t)b + key, lane);
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const int64_t e = e0 + 128 * q + 4 * lane;
-                if (e >= n) continue;
-                const uint32_t c = (uint32_t)(i0 + (e - u0)), dj = c / (uint32_t)Np;      // four elements of one row: Np is a multiple of 8
+                const int e = b + 128 * q + 4 * lane;
+                if (e >= count) continue;
+                const uint32_t c = i0 + (uint32_t)e, dj = wide ? (uint32_t)(c >= width) : __umulhi(c, over_n);   // four elements of one row
                 __nv_bfloat162 y = __floats2bfloat162_rn(x.th[q].x, x.th[q].y), z = __floats2bfloat162_rn(x.th[q].z, x.th[q].w);
-                *reinterpret_cast<uint2*>(bs + (j0 + dj) * a.ldB + (c - dj * (uint32_t)Np)) =
+                *reinterpret_cast<uint2*>(bs + (int64_t)dj * a.ldB + (c - dj * width)) =
                     make_uint2(*reinterpret_cast<uint32_t*>(&y), *reinterpret_cast<uint32_t*>(&z));
             }
         }
@@ -264,46 +293,56 @@ __global__ void __launch_bounds__(OC_THREADS) k_adamw_compact(const __grid_const
     const int64_t k0 = (int64_t)(u - p * per_part) * R, n = a.K * r, poff = (int64_t)p * n;
     const int rows = (int)min((int64_t)R, a.K - k0), elems = rows * r;
     const uint32_t key = t.key[2 * p], over_r = r > 1 ? 0xffffffffu / (uint32_t)r + 1u : 0u;      // e / r = high word of e over_r (e < 2^16)
-    const float* grad = t.dA + poff;
-    float* theta = t.A + poff;
-    uint8_t* state = t.sA + p * state_bytes(n);
+    const float* grad = t.dA + poff + k0 * r;
+    float* theta = t.A + poff + k0 * r;
+    uint8_t* state = t.sA + p * state_bytes(n) + k0 * r / OC_BLOCK * OC_STATE_BYTES;
     for (int b = warp * OC_BLOCK; b < elems; b += OC_THREADS / 32 * OC_BLOCK) {
         CompactLane x;
-        const int64_t e0 = k0 * r + b;
-        uint8_t* blk = state + (e0 / OC_BLOCK) * OC_STATE_BYTES;
-        compact_load(x, grad, theta, blk, e0, n, vec, lane);
-        compact_step(x, a.h, theta, blk, e0, n, vec, key, lane);
+        uint8_t* blk = state + b / OC_BLOCK * OC_STATE_BYTES;
+        compact_load(x, grad + b, theta + b, blk, elems - b, vec, lane);
+        compact_step(x, a.h, theta + b, blk, elems - b, vec, (uint32_t)(k0 * r) + (uint32_t)b + key, lane);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const int e = b + 128 * q + 4 * lane;
             if (e >= elems) continue;
-            const float th[4] = {x.th[q].x, x.th[q].y, x.th[q].z, x.th[q].w};
             int kk = r > 1 ? (int)__umulhi((uint32_t)e, over_r) : e, j = e - kk * r;
+            bf16* to = tile + kk * pitch + j;
+            if ((r & 3) == 0) {         // four elements of one row
+                to[0] = __float2bfloat16_rn(x.th[q].x);
+                to[1] = __float2bfloat16_rn(x.th[q].y);
+                to[2] = __float2bfloat16_rn(x.th[q].z);
+                to[3] = __float2bfloat16_rn(x.th[q].w);
+            } else {
+                const float th[4] = {x.th[q].x, x.th[q].y, x.th[q].z, x.th[q].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                tile[kk * pitch + j] = __float2bfloat16_rn(th[i]);
-                if (++j == r) {
-                    j = 0;
-                    ++kk;
+                for (int i = 0; i < 4; ++i) {
+                    *to++ = __float2bfloat16_rn(th[i]);
+                    if (++j == r) {
+                        j = 0;
+                        to += pitch - r;
+                    }
                 }
             }
         }
     }
     __syncthreads();
+    // A thread takes 8 rows of a column; neighbours take neighbouring columns (conflict-free reads of the tile), so that a
+    // warp's 16-byte writes go to as many rows of At and the lines fill up in L2.  K and R are multiples of 8.
     bf16* at = a.At + ((size_t)p * a.cap + t.slot) * a.RP * (size_t)a.K + k0;
-    const int groups = rows / 8;        // K and R are multiples of 8
-    for (int x = tid; x < groups * r; x += OC_THREADS) {
-        const int j = x / groups, g8 = (x - j * groups) * 8;
+    const int work = rows / 8 * r;
+    for (int x = tid; x < work; x += OC_THREADS) {
+        const int g = r > 1 ? (int)__umulhi((uint32_t)x, over_r) : x, j = x - g * r;
+        const bf16* from = tile + 8 * g * pitch + j;
         uint4 o;
         uint32_t* w = &o.x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             __nv_bfloat162 y;
-            y.x = tile[(g8 + 2 * i) * pitch + j];
-            y.y = tile[(g8 + 2 * i + 1) * pitch + j];
+            y.x = from[2 * i * pitch];
+            y.y = from[(2 * i + 1) * pitch];
             w[i] = *reinterpret_cast<uint32_t*>(&y);
         }
-        *reinterpret_cast<uint4*>(at + (size_t)j * a.K + g8) = o;
+        *reinterpret_cast<uint4*>(at + (size_t)j * a.K + 8 * g) = o;
     }
 }
 
