@@ -174,7 +174,8 @@ def _check(rc: int) -> None:
 
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the current device's current stream, without the Stream object (a few microseconds) that torch.cuda makes for it
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -252,6 +253,7 @@ class AdapterPool:
         self.rank_stride = int(L.marlaas_adapter_pool_rank_stride(h))
         self._workspaces = {}
         self._policy_sizes = (None, 0)
+        self._store = None
 
     def close(self):
         if getattr(self, "handle", None):
@@ -289,6 +291,8 @@ class AdapterPool:
     def store(self):
         """Views of the pool's bf16 rows: At [n_parts][capacity * rank_stride][d_in] and Bs [capacity * rank_stride][d_out]
         (not to be written)."""
+        if self._store is not None:
+            return self._store
         at, bs = ctypes.c_void_p(), ctypes.c_void_p()
         _check(load_library().marlaas_adapter_pool_store(self.handle, ctypes.byref(at), ctypes.byref(bs)))
         rows, base, flat = self.capacity * self.rank_stride, self.storage.data_ptr(), self.storage
@@ -297,7 +301,8 @@ class AdapterPool:
             for d in shape:
                 n *= d
             return flat[p.value - base:p.value - base + n].view(torch.bfloat16).view(*shape)
-        return view(at, self.n_parts, rows, self.d_in), view(bs, rows, self.d_out)
+        self._store = view(at, self.n_parts, rows, self.d_in), view(bs, rows, self.d_out)
+        return self._store
 
 
 def marlaas_adapter_pool_register(pool: AdapterPool, tenant_id: int, version: int, rank: int, alpha: float,
@@ -550,14 +555,13 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
     """(seq_adv [S], adv [T], weight [T]) of a batch whose sequences are the segments of `seg`; group_offsets lives where
     the segment table does.  Outputs that are not given are allocated."""
     T, S, G = targets.numel(), seg.c.num_segments, group_offsets.numel() - 1
-    dev = pool.device
-    assert targets.is_cuda and group_offsets.is_cuda != seg.on_host, "group_offsets must be where the segment table is"
+    assert targets.is_cuda and rewards.is_cuda and group_offsets.is_cuda != seg.on_host, "group_offsets must be where the segment table is"
     if seq_adv is None:
-        seq_adv = torch.empty(S, dtype=torch.float32, device=dev)
+        seq_adv = rewards.new_empty(S)
     if adv is None:
-        adv = torch.empty(T, dtype=torch.float32, device=dev)
+        adv = rewards.new_empty(T)
     if weight is None:
-        weight = torch.empty(T, dtype=torch.float32, device=dev)
+        weight = rewards.new_empty(T)
     ws = workspace if workspace is not None else pool.policy_workspace(T, S, G)
     _check(load_library().marlaas_group_advantages(
         pool.handle, T, ctypes.byref(seg.c), _f32(rewards, S, "rewards"), G, _i32(group_offsets, G + 1, "group_offsets"),

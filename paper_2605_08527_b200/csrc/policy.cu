@@ -9,11 +9,17 @@
 
 namespace marlaas {
 
-constexpr int ADV_THREADS = 256;
-
 __device__ __forceinline__ void policy_report(int32_t* status, int code, int detail) {
     if (atomicCAS(status, 0, code) == 0) status[1] = detail;
 }
+
+// ---- group-relative advantages ----
+// Three steps: active tokens per sequence and advantages per group; totals per tenant (integer sums, so their order does not
+// matter); every token's advantage and weight.  They move 12 bytes per token: HBM for millions of tokens, launches for
+// ordinary batches.  A batch of at most ADV_SMALL_T tokens takes all three in one CTA (one launch); a larger one counts in
+// one kernel and expands in a second, each of whose CTAs forms the totals from the counts for itself; only for more than
+// ADV_SHARED_S sequences, whose counts would cost every CTA too much, a kernel between them does.
+constexpr int ADV_THREADS = 256, ADV_SMALL_THREADS = 1024, ADV_SMALL_T = 8192, ADV_SMALL_S = 1024, ADV_SHARED_S = 4096;
 
 struct AdvArgs {
     int T, S, G, cap;
@@ -28,7 +34,7 @@ struct AdvArgs {
     float* adv;
     float* weight;
     int32_t* count;     // [S] active tokens
-    int32_t* total;     // [cap + 1] active tokens, or sequences that have any, per bucket
+    int32_t* total;     // [cap + 1] active tokens, or sequences that have any, per bucket (of the kernel between)
     int32_t* status;
 };
 
@@ -38,76 +44,238 @@ __device__ __forceinline__ void seq_range(const AdvArgs& a, int s, int* lo, int*
     *lo = min(max(x, 0), a.T);
     *hi = min(max(y, *lo), a.T);
 }
-
-// One warp per sequence: its active tokens.  Then one warp per group: its sequences' advantages.
-__global__ void __launch_bounds__(ADV_THREADS) k_adv_count(const AdvArgs a) {
-    const int lane = threadIdx.x & 31;
-    const int w = (int)((blockIdx.x * (unsigned)ADV_THREADS + threadIdx.x) >> 5), nw = (int)(gridDim.x * (ADV_THREADS / 32));
-    for (int s = w; s < a.S; s += nw) {
-        int lo, hi;
-        seq_range(a, s, &lo, &hi);
-        if (lane == 0) {
-            const int x = a.off[s], y = a.off[s + 1], t = a.slot[s];
-            if (y < x || x < 0 || y > a.T || (s == 0 && x != 0) || (s == a.S - 1 && y != a.T)) policy_report(a.status, DEV_BAD_TABLE, s);
-            if (t < -1 || t >= a.cap) policy_report(a.status, DEV_BAD_INDEX, s);
-        }
-        int n = 0;
-        for (int i = lo + lane; i < hi; i += 32) n += a.targets[i] >= 0;
-        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        if (lane == 0) a.count[s] = n;
+__device__ __forceinline__ int bucket_of(const AdvArgs& a, int slot) { return slot < 0 || slot >= a.cap ? a.cap : slot; }
+__device__ __forceinline__ void check_sequence(const AdvArgs& a, int s) {
+    const int x = a.off[s], y = a.off[s + 1], t = a.slot[s];
+    if (y < x || x < 0 || y > a.T || (s == 0 && x != 0) || (s == a.S - 1 && y != a.T)) policy_report(a.status, DEV_BAD_TABLE, s);
+    if (t < -1 || t >= a.cap) policy_report(a.status, DEV_BAD_INDEX, s);
+}
+// Active tokens among [lo, hi) that lane `lane` of `lanes` looks at: whole 16-byte words in the middle, single tokens around.
+__device__ __forceinline__ int count_active(const int32_t* targets, int lo, int hi, int lane, int lanes) {
+    const int head = (int)(((16 - ((uintptr_t)(targets + lo) & 15)) & 15) >> 2), mid = min(lo + head, hi), words = (hi - mid) >> 2;
+    int n = 0;
+    if (lane < mid - lo) n += targets[lo + lane] >= 0;
+    const int4* w = reinterpret_cast<const int4*>(targets + mid);
+#pragma unroll 4
+    for (int i = lane; i < words; i += lanes) {
+        const int4 t = w[i];
+        n += (t.x >= 0) + (t.y >= 0) + (t.z >= 0) + (t.w >= 0);
     }
-    for (int g = w; g < a.G; g += nw) {
-        const int x = a.group_off[g], y = a.group_off[g + 1];
-        if (lane == 0 && (y < x || x < 0 || y > a.S || (g == 0 && x != 0) || (g == a.G - 1 && y != a.S)))
-            policy_report(a.status, DEV_BAD_TABLE, -10 - g);
-        const int lo = min(max(x, 0), a.S), hi = min(max(y, lo), a.S);
-        if (hi <= lo) continue;
-        // differences to the group's first reward: rewards that are all alike give exact zeros
-        const float r0 = a.rewards[lo], n = (float)(hi - lo);
-        float sum = 0.f;
-        for (int i = lo + lane; i < hi; i += 32) sum += a.rewards[i] - r0;
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const float mean = sum / n;
-        float sq = 0.f;
-        if (!a.no_std) {
-            for (int i = lo + lane; i < hi; i += 32) {
-                const float d = (a.rewards[i] - r0) - mean;
-                sq += d * d;
-            }
-            for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        }
-        const float sd = sqrtf(sq / n);
+    const int last = mid + 4 * words + lane;
+    if (last < hi) n += targets[last] >= 0;
+    return n;
+}
+__device__ __forceinline__ int warp_total(int n) { return __reduce_add_sync(0xffffffffu, n); }
+
+// One warp: the advantages of group g's sequences.
+__device__ __forceinline__ void group_advantages(const AdvArgs& a, int g, int lane, float* seq_adv) {
+    const int x = a.group_off[g], y = a.group_off[g + 1];
+    if (lane == 0 && (y < x || x < 0 || y > a.S || (g == 0 && x != 0) || (g == a.G - 1 && y != a.S)))
+        policy_report(a.status, DEV_BAD_TABLE, -10 - g);
+    const int lo = min(max(x, 0), a.S), hi = min(max(y, lo), a.S);
+    if (hi <= lo) return;
+    // differences to the group's first reward: rewards that are all alike give exact zeros
+    const float r0 = a.rewards[lo], n = (float)(hi - lo);
+    float sum = 0.f;
+    for (int i = lo + lane; i < hi; i += 32) sum += a.rewards[i] - r0;
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float mean = sum / n;
+    float sq = 0.f;
+    if (!a.no_std) {
         for (int i = lo + lane; i < hi; i += 32) {
             const float d = (a.rewards[i] - r0) - mean;
-            a.seq_adv[i] = a.no_std ? d : (d == 0.f ? 0.f : d / (sd + a.eps));      // (eps may be 0)
+            sq += d * d;
         }
+        for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+    }
+    const float sd = sqrtf(sq / n);
+    for (int i = lo + lane; i < hi; i += 32) {
+        const float d = (a.rewards[i] - r0) - mean, v = a.no_std ? d : (d == 0.f ? 0.f : d / (sd + a.eps));      // (eps may be 0)
+        seq_adv[i] = v;
+        if (seq_adv != a.seq_adv) a.seq_adv[i] = v;
+    }
+}
+__device__ __forceinline__ float token_weight(const AdvArgs& a, int count, int total) {
+    return count == 0 ? 0.f : 1.f / (a.token_mean ? (float)total : (float)total * (float)count);
+}
+
+__global__ void __launch_bounds__(ADV_SMALL_THREADS) k_adv_small(const AdvArgs a) {
+    extern __shared__ int32_t s_total[];                    // [cap + 1]
+    __shared__ float s_adv[ADV_SMALL_S], s_weight[ADV_SMALL_S];
+    __shared__ int32_t s_count[ADV_SMALL_S], s_off[ADV_SMALL_S];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    for (int b = tid; b <= a.cap; b += ADV_SMALL_THREADS) s_total[b] = 0;
+    if (tid < a.S) {
+        s_adv[tid] = 0.f;       // (a table that leaves a sequence out)
+        s_off[tid] = a.off[tid];
+    }
+    __syncthreads();
+    for (int s = warp; s < a.S; s += ADV_SMALL_THREADS / 32) {
+        int lo, hi;
+        seq_range(a, s, &lo, &hi);
+        const int n = warp_total(count_active(a.targets, lo, hi, lane, 32));
+        if (lane == 0) {
+            check_sequence(a, s);
+            s_count[s] = n;
+            if (n) atomicAdd(s_total + bucket_of(a, a.slot[s]), a.token_mean ? n : 1);
+        }
+    }
+    for (int g = warp; g < a.G; g += ADV_SMALL_THREADS / 32) group_advantages(a, g, lane, s_adv);
+    __syncthreads();
+    if (tid < a.S) s_weight[tid] = token_weight(a, s_count[tid], s_total[bucket_of(a, a.slot[tid])]);
+    __syncthreads();
+    for (int i = tid; i < a.T; i += ADV_SMALL_THREADS) {
+        int lo = 0, hi = a.S;           // sequences that begin at or before the token: the last of them holds it
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (s_off[mid] <= i) lo = mid + 1; else hi = mid;
+        }
+        const bool on = lo > 0 && a.targets[i] >= 0;
+        if (a.adv) a.adv[i] = on ? s_adv[lo - 1] : 0.f;
+        if (a.weight) a.weight[i] = on ? s_weight[lo - 1] : 0.f;
     }
 }
 
-// Totals per bucket: integer sums, so their order does not matter.
+// WPS warps per sequence count its active tokens; then one warp per group.
+template <int WPS>
+__global__ void __launch_bounds__(ADV_THREADS) k_adv_count(const AdvArgs a) {
+    __shared__ int s_n[ADV_THREADS / 32];
+    constexpr int TEAMS = ADV_THREADS / 32 / WPS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team = warp / WPS;
+    sm100::dk_launch_dependents();
+    for (int s0 = blockIdx.x * TEAMS; s0 < a.S; s0 += gridDim.x * TEAMS) {
+        const int s = s0 + team;
+        int n = 0;
+        if (s < a.S) {
+            int lo, hi;
+            seq_range(a, s, &lo, &hi);
+            n = warp_total(count_active(a.targets, lo, hi, threadIdx.x % (32 * WPS), 32 * WPS));
+        }
+        if (WPS > 1) {
+            if (lane == 0) s_n[warp] = n;
+            __syncthreads();
+            if (warp % WPS == 0)
+                for (int w = 1; w < WPS; ++w) n += s_n[warp + w];
+            __syncthreads();
+        }
+        if (s < a.S && warp % WPS == 0 && lane == 0) {
+            check_sequence(a, s);
+            a.count[s] = n;
+        }
+    }
+    for (int g = (int)gridDim.x - 1 - (int)blockIdx.x + (int)gridDim.x * warp; g < a.G; g += (int)gridDim.x * (ADV_THREADS / 32))
+        group_advantages(a, g, lane, a.seq_adv);
+}
+
 __global__ void __launch_bounds__(1024) k_adv_totals(const AdvArgs a) {
     for (int b = threadIdx.x; b <= a.cap; b += 1024) a.total[b] = 0;
     __syncthreads();
     for (int s = threadIdx.x; s < a.S; s += 1024) {
-        const int t = a.slot[s], n = a.count[s];
-        if (n) atomicAdd(a.total + (t < 0 || t >= a.cap ? a.cap : t), a.token_mean ? n : 1);
+        const int n = a.count[s];
+        if (n) atomicAdd(a.total + bucket_of(a, a.slot[s]), a.token_mean ? n : 1);
     }
 }
 
-// One CTA per sequence in turn: its tokens' advantages and weights.
+// Four tokens per thread; the sequence of the first by bisection, the others' from there on.
+template <bool SHARED>
 __global__ void __launch_bounds__(ADV_THREADS) k_adv_expand(const AdvArgs a) {
-    for (int s = blockIdx.x; s < a.S; s += gridDim.x) {
-        int lo, hi;
-        seq_range(a, s, &lo, &hi);
-        const int t = a.slot[s], n = a.count[s];
-        const float total = (float)a.total[t < 0 || t >= a.cap ? a.cap : t];
-        const float w = n == 0 ? 0.f : 1.f / (a.token_mean ? total : total * (float)n), v = a.seq_adv[s];
-        for (int i = lo + threadIdx.x; i < hi; i += ADV_THREADS) {
-            const bool on = a.targets[i] >= 0;
-            if (a.adv) a.adv[i] = on ? v : 0.f;
-            if (a.weight) a.weight[i] = on ? w : 0.f;
+    extern __shared__ int32_t s_mem[];      // SHARED: [cap + 1] totals, [S + 1] offsets
+    const int tid = threadIdx.x;
+    int32_t* s_total = s_mem;
+    int32_t* s_off = s_mem + a.cap + 1;
+    if (SHARED) {
+        for (int b = tid; b <= a.cap; b += ADV_THREADS) s_total[b] = 0;
+        for (int s = tid; s <= a.S; s += ADV_THREADS) s_off[s] = a.off[s];
+        __syncthreads();
+        sm100::dk_wait_prerequisites();
+        for (int s = tid; s < a.S; s += ADV_THREADS) {
+            const int n = a.count[s];
+            if (n) atomicAdd(s_total + bucket_of(a, a.slot[s]), a.token_mean ? n : 1);
+        }
+        __syncthreads();
+    }
+    const int32_t* off = SHARED ? s_off : a.off;
+    const int32_t* total = SHARED ? s_total : a.total;
+    const bool wide = ((((uintptr_t)a.targets | (uintptr_t)a.adv | (uintptr_t)a.weight)) & 15) == 0;
+    for (int64_t i0 = ((int64_t)blockIdx.x * ADV_THREADS + tid) * 4; i0 < a.T; i0 += (int64_t)gridDim.x * ADV_THREADS * 4) {
+        const int first = (int)i0, n = min(4, a.T - first);
+        int32_t t[4] = {-1, -1, -1, -1};
+        if (wide && n == 4) {
+            const int4 x = *reinterpret_cast<const int4*>(a.targets + first);
+            t[0] = x.x; t[1] = x.y; t[2] = x.z; t[3] = x.w;
+        } else {
+            for (int k = 0; k < n; ++k) t[k] = a.targets[first + k];
+        }
+        int lo = 0, hi = a.S;               // sequences that begin at or before the token: the last of them holds it
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (off[mid] <= first) lo = mid + 1; else hi = mid;
+        }
+        int s = lo - 1;
+        float v = 0.f, w = 0.f, va[4], wa[4];
+        bool have = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            while (k > 0 && s + 1 < a.S && off[s + 1] <= first + k) {       // (sequences may be empty)
+                ++s;
+                have = false;
+            }
+            if (!have && s >= 0) {
+                v = a.seq_adv[s];
+                w = token_weight(a, a.count[s], total[bucket_of(a, a.slot[s])]);
+                have = true;
+            }
+            va[k] = t[k] >= 0 ? v : 0.f;
+            wa[k] = t[k] >= 0 ? w : 0.f;
+        }
+        if (wide && n == 4) {
+            if (a.adv) *reinterpret_cast<float4*>(a.adv + first) = make_float4(va[0], va[1], va[2], va[3]);
+            if (a.weight) *reinterpret_cast<float4*>(a.weight + first) = make_float4(wa[0], wa[1], wa[2], wa[3]);
+        } else {
+            for (int k = 0; k < n; ++k) {
+                if (a.adv) a.adv[first + k] = va[k];
+                if (a.weight) a.weight[first + k] = wa[k];
+            }
         }
     }
+}
+
+static marlaas_status_t launch_advantages(const marlaas_pool* pool, const AdvArgs& a, cudaStream_t st) {
+    if (a.T <= ADV_SMALL_T && a.S <= ADV_SMALL_S) {
+        k_adv_small<<<1, ADV_SMALL_THREADS, sizeof(int32_t) * ((size_t)a.cap + 1), st>>>(a);
+        MARLAAS_LAUNCH_CHECK("k_adv_small");
+        return MARLAAS_OK;
+    }
+    const int64_t most = (int64_t)pool->sm_count * (2048 / ADV_THREADS);
+    // long sequences: four warps each
+    const bool long_ones = a.T / a.S > 256;
+    const int64_t teams = long_ones ? ADV_THREADS / 128 : ADV_THREADS / 32;
+    const int grid = (int)std::min<int64_t>(std::max<int64_t>(cdiv(a.S, teams), cdiv(a.G, ADV_THREADS / 32)), most);
+    if (long_ones) k_adv_count<4><<<grid, ADV_THREADS, 0, st>>>(a);
+    else k_adv_count<1><<<grid, ADV_THREADS, 0, st>>>(a);
+    MARLAAS_LAUNCH_CHECK("k_adv_count");
+    if (!a.adv && !a.weight) return MARLAAS_OK;
+    const int egrid = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(a.T, ADV_THREADS * 4), most));
+    if (a.S <= ADV_SHARED_S) {
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3((unsigned)egrid);
+        cfg.blockDim = dim3(ADV_THREADS);
+        cfg.dynamicSmemBytes = sizeof(int32_t) * ((size_t)a.cap + 1 + a.S + 1);
+        cfg.stream = st;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_adv_expand<true>, a));
+    } else {
+        k_adv_totals<<<1, 1024, 0, st>>>(a);
+        MARLAAS_LAUNCH_CHECK("k_adv_totals");
+        k_adv_expand<false><<<egrid, ADV_THREADS, 0, st>>>(a);
+    }
+    MARLAAS_LAUNCH_CHECK("k_adv_expand");
+    return MARLAAS_OK;
 }
 
 // One CTA per bucket sums its tokens' terms, every thread its own tokens in ascending order, then a fixed tree.  A token's
@@ -285,15 +453,7 @@ marlaas_status_t marlaas_group_advantages(marlaas_pool_t* pool, int64_t T, const
     a.token_mean = (flags & MARLAAS_FLAG_TOKEN_MEAN) != 0; a.no_std = (flags & MARLAAS_FLAG_NO_STD) != 0;
     a.seq_adv = seq_adv ? seq_adv : ws.seq_adv;
     a.adv = adv; a.weight = weight; a.count = ws.count; a.total = ws.total; a.status = pool->d_status;
-    const int64_t warps = std::max(S, num_groups);
-    k_adv_count<<<(unsigned)std::min<int64_t>(cdiv(warps, ADV_THREADS / 32), (int64_t)pool->sm_count * 8), ADV_THREADS, 0, st>>>(a);
-    MARLAAS_LAUNCH_CHECK("k_adv_count");
-    if (adv || weight) {
-        k_adv_totals<<<1, 1024, 0, st>>>(a);
-        MARLAAS_LAUNCH_CHECK("k_adv_totals");
-        k_adv_expand<<<(unsigned)std::min<int64_t>(S, (int64_t)pool->sm_count * 8), ADV_THREADS, 0, st>>>(a);
-        MARLAAS_LAUNCH_CHECK("k_adv_expand");
-    }
+    if ((rc = launch_advantages(pool, a, st)) != MARLAAS_OK) return rc;
     return finish(pool, flags, st);
 } catch (const std::exception& e) {
     return fail(MARLAAS_ERR_INVALID_ARG, "group_advantages: %s", e.what());
