@@ -88,10 +88,10 @@ __device__ __forceinline__ RowGrad token_terms(const VocabRows& a, const TokenIn
     if (a.kl_coef != 0.f) {
         const float d = in.ref - logp, e1 = expm1f(d);     // exp(d) - d - 1 without its cancellation for small d
         kl = e1 - d;
-        c -= a.kl_coef * e1;
+        c = fmaf(-a.kl_coef, e1, c);
     }
     PolicyTerms t;
-    t.loss = w * (pg + a.kl_coef * kl - a.entropy_coef * H);
+    t.loss = w * fmaf(-a.entropy_coef, H, fmaf(a.kl_coef, kl, pg));
     t.pg = w * pg; t.kl = w * kl; t.entropy = w * H; t.ratio = w * ratio;
     t.clipped = is_clipped ? w : 0.f;
     t.weight = w;
@@ -135,10 +135,17 @@ __device__ __forceinline__ float max_of(const uint4& q) {
 // operations, 45 % and 65 % of what the SMs have while the row streams).  Tried and not kept: the slice in registers
 // (2 CTAs per SM, 438 us for the loss over 4096 x 131072 against 400), chunks that are refilled one by one (441 us: the
 // waits cost more than the earlier copies gain), a share of the exponentials as polynomials on the FMA pipes (425 us).
+// Rows are dealt out in advance (no counter that calls would have to share): the k-th row that is read goes to cluster
+// k mod clusters, so that prompt tokens, which cost next to nothing, do not leave some clusters with more work than others.
+// Each CTA makes a bit mask of the rows that are read for that, if the batch is neither so small that every cluster has one
+// row nor larger than the mask; otherwise row i goes to cluster i mod clusters.
 struct RowsLayout {
     int32_t C;              // CTAs per row
+    int32_t stages;         // slices that shared memory holds: one is worked on, copies of later rows go to the others
+    int32_t mask_words;     // 32-row words of the mask, 0 = none
     int64_t slice;          // elements per CTA (whole vectors)
 };
+constexpr int VR_STAGES = 4, VR_RING = 8;       // most stages; row numbers known ahead (a power of two above VR_STAGES)
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
@@ -184,7 +191,7 @@ __device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const u
     r.m = warp_max(tid < nvec ? max_nan(zt, max_of<F32>(slice[tid])) : zt);
     {
         const float mr = ref_of(r.m), tt = exponent(zt, mr, k2);
-        float2 s2 = make_float2(ex2(tt), 0.f), u2 = make_float2(s2.x * tt, 0.f);
+        float2 s2 = make_float2(ex2(tt), 0.f), u2 = make_float2(__fmul_rn(s2.x, tt), 0.f);
 #pragma unroll 4
         for (int v = tid; v < nvec; v += NT) {
             const uint4 q = slice[v];
@@ -210,14 +217,14 @@ __device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const u
             r.m = warp_max(r.m);
         }
         const float mr = ref_of(r.m), tt = exponent(zt, mr, k2);
-        float s = ex2(tt), u = s * tt;
+        float s = ex2(tt), u = __fmul_rn(s, tt);
         for (int v = tid; v < nvec; v += NT) {
             const uint4 q = again[v];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const float t = exponent(element<F32>(q, j), mr, k2), e = ex2(t);
                 s += e;
-                u += e * t;
+                u = fmaf(e, t, u);
             }
         }
         s = warp_sum(s);
@@ -231,111 +238,183 @@ template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD, int NT, bool CLU
 __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, const RowsLayout lay) {
     using X = Vec<F32>;
     constexpr int E = F32 ? 4 : 2, W = NT / 32, PARTS = CLUSTER ? 8 * W : W;
-    extern __shared__ __align__(128) uint4 s_slice[];
+    extern __shared__ __align__(128) uint4 s_dynamic[];     // the slices, then the mask
     __shared__ __align__(16) float4 s_part[2][PARTS];       // statistics of all warps of a row
-    __shared__ __align__(8) uint64_t s_full, s_stat[2];
-    __shared__ int s_done, s_copies, s_abort;      // warps done with the slice; copies started; given up
+    __shared__ __align__(8) uint64_t s_full[VR_STAGES], s_stat[2];
+    __shared__ int64_t s_row[VR_RING];                      // the rows this cluster reads, in order; -1 = no more
+    __shared__ int s_done[VR_STAGES], s_copies[VR_STAGES], s_abort;     // warps done with a slice; copies started; given up
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = CLUSTER ? dk_cluster_ctarank() : 0;
-    const int C = CLUSTER ? lay.C : 1;
-    const int64_t stride = gridDim.x / C;
-    const uint32_t bar_full = smem_u32(&s_full), bar_stat = smem_u32(s_stat);
+    const int C = CLUSTER ? lay.C : 1, stages = lay.stages;
+    const int64_t clusters = gridDim.x / C, me = blockIdx.x / C;
+    const uint32_t bar_full = smem_u32(s_full), bar_stat = smem_u32(s_stat);
     if (tid == 0) {
-        mbar_init(bar_full, 1);
-        s_done = s_copies = 0;
+        for (int i = 0; i < stages; ++i) {
+            mbar_init(bar_full + 8 * i, 1);
+            s_done[i] = s_copies[i] = 0;
+        }
         mbar_init(bar_stat, 1);
         mbar_init(bar_stat + 8, 1);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncthreads();
-    if (CLUSTER) dk_cluster_sync();
-    if (a.terms) dk_launch_dependents();        // the kernel that sums the terms; it waits for this one's end
     // this CTA's part of every row: whole vectors, and behind the last of the row up to 7 elements
     const int64_t V = a.V, begin = min((int64_t)rank * lay.slice, V);
     const int64_t end = (int)rank == C - 1 ? V : min(begin + lay.slice, V);
     const int nvec = (int)((end - begin) / X::N), ntail = (int)(end - begin) - nvec * X::N;
     const int64_t tail = begin + (int64_t)nvec * X::N;
+    const int stage_vecs = (int)(lay.slice / X::N);
     // (through a shuffle: a value of each lane's own, which two-element instructions take as it is, not a uniform one)
     const float k2 = __shfl_sync(0xffffffffu, a.inv_temperature * VR_LOG2E, 0);
-    // The rows of this cluster are base + n stride.  Lane l holds target and weight of the row n0 + l of a window of 32,
-    // and `window` which of them are read.
-    const int64_t base = blockIdx.x / C;
-    const int nrows = base < a.T ? (int)((a.T - 1 - base) / stride) + 1 : 0;
-    auto source = [&](int n) { return (const char*)a.logits + ((size_t)(base + (int64_t)n * stride) * a.ld + begin) * E; };
-    auto copy = [&](int n) {            // one thread; the slice's place is free
-        ++s_copies;
-        mbar_expect_tx(bar_full, (uint32_t)nvec * 16);
-        bulk_load(smem_u32(s_slice), source(n), (uint32_t)nvec * 16, bar_full);
+    auto reads = [&](int64_t row) {
+        return row < a.T && row_read(a, a.targets[row], a.terms ? a.weight[row] : 1.f);
     };
-    int32_t target_l = -1;
-    float w_l = 1.f;
-    auto look = [&](int n0) {
-        target_l = -1;
-        w_l = 1.f;
-        if (n0 + lane < nrows) {
-            target_l = a.targets[base + (int64_t)(n0 + lane) * stride];
-            if (a.terms) w_l = a.weight[base + (int64_t)(n0 + lane) * stride];
+    uint32_t* s_mask = reinterpret_cast<uint32_t*>(s_dynamic + (size_t)stages * stage_vecs);
+    for (int w0 = warp * 8; w0 < lay.mask_words; w0 += W * 8) {         // eight words' loads at once
+        int32_t t[8];
+        float wt[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t r = (int64_t)(w0 + k) * 32 + lane;
+            t[k] = r < a.T ? a.targets[r] : -1;
+            wt[k] = a.terms && r < a.T ? a.weight[r] : 1.f;
         }
-        return __ballot_sync(0xffffffffu, row_read(a, target_l, w_l));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t word = __ballot_sync(0xffffffffu, row_read(a, t[k], wt[k]));
+            if (lane == 0 && w0 + k < lay.mask_words) s_mask[w0 + k] = word;
+        }
+    }
+    __syncthreads();
+    if (CLUSTER) dk_cluster_sync();
+    if (a.terms) dk_launch_dependents();        // the kernel that sums the terms; it waits for this one's end
+    auto source = [&](int64_t row) { return (const char*)a.logits + ((size_t)row * a.ld + begin) * E; };
+    auto copy = [&](int64_t row, int stage) {            // one thread; the stage is free
+        ++s_copies[stage];
+        mbar_expect_tx(bar_full + 8 * stage, (uint32_t)nvec * 16);
+        bulk_load(smem_u32(s_dynamic + (size_t)stage * stage_vecs), source(row), (uint32_t)nvec * 16, bar_full + 8 * stage);
     };
-    // the first row after n that is read, nrows if there is none
-    auto next_read = [&](int n, uint32_t window) {
-        const uint32_t later = (n & 31) == 31 ? 0u : window >> ((n & 31) + 1);
-        if (later) return n + __ffs(later);
-        const int32_t t = target_l;
-        const float w = w_l;
-        int found = nrows;
-        for (int n0 = (n | 31) + 1; n0 < nrows; n0 += 32) {
-            const uint32_t bits = look(n0);
-            if (bits) {
-                found = n0 + __ffs(bits) - 1;
-                break;
+    // Warp 0 finds the rows.  With a mask: `skip` rows that are read lie before the next one from word `at` on (in which
+    // `bits` are left); without: from row `at` on in steps of `clusters`.
+    int64_t at = lay.mask_words ? 0 : me, skip = me;
+    uint32_t bits = lay.mask_words ? s_mask[0] : 0u;
+    auto next_row = [&]() -> int64_t {
+        if (lay.mask_words) {
+            if (__popc(bits) <= skip) {
+                skip -= __popc(bits);
+                int64_t w0 = at + 1;
+                while (true) {      // 32 words at a time
+                    if (w0 >= lay.mask_words) {
+                        at = lay.mask_words;
+                        bits = 0;
+                        skip = 0;
+                        return -1;
+                    }
+                    const uint32_t word = w0 + lane < lay.mask_words ? s_mask[w0 + lane] : 0u;
+                    int upto = __popc(word);
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+                        if (lane >= o) upto += x;
+                    }
+                    const uint32_t reached = __ballot_sync(0xffffffffu, upto > skip);
+                    if (reached) {
+                        const int l = __ffs(reached) - 1;
+                        bits = __shfl_sync(0xffffffffu, word, l);
+                        skip -= __shfl_sync(0xffffffffu, upto, l) - __popc(bits);
+                        at = w0 + l;
+                        break;
+                    }
+                    skip -= __shfl_sync(0xffffffffu, upto, 31);
+                    w0 += 32;
+                }
+            }
+            for (; skip > 0; --skip) bits &= bits - 1;
+            const int64_t row = at * 32 + __ffs(bits) - 1;
+            bits &= bits - 1;
+            skip = clusters - 1;
+            return row;
+        }
+        while (at < a.T) {
+            const uint32_t found = __ballot_sync(0xffffffffu, reads(at + lane * clusters));
+            if (found) {
+                const int64_t row = at + (int64_t)(__ffs(found) - 1) * clusters;
+                at = row + clusters;
+                return row;
+            }
+            at += 32 * clusters;
+        }
+        return -1;
+    };
+    if (warp == 0) {
+        bool more = true;
+        for (int i = 0; i < stages; ++i) {
+            const int64_t row = more ? next_row() : -1;
+            more = row >= 0;
+            if (lane == 0) {
+                s_row[i] = row;
+                if (more && nvec > 0) copy(row, i);
             }
         }
-        target_l = t;
-        w_l = w;
-        return found;
-    };
-    uint32_t window = look(0);
-    {
-        const int n = window & 1u ? 0 : next_read(0, window);
-        if (tid == 0 && nvec > 0 && n < nrows) copy(n);
     }
+    // rows that are not read, row i by cluster i mod clusters, while the first copies are under way
+    for (int64_t r0 = me; r0 < a.T; r0 += 32 * clusters) {
+        uint32_t left = __ballot_sync(0xffffffffu, r0 + lane * clusters < a.T && !reads(r0 + lane * clusters));
+        for (; left; left &= left - 1) {
+            const int64_t row = r0 + (int64_t)(__ffs(left) - 1) * clusters;
+            if (rank == 0 && tid == 0) {
+                if (a.targets[row] >= V) dk_report(a.status, DEV_BAD_INDEX, (int)row);
+                if (a.logp) a.logp[row] = 0.f;
+                if (a.entropy) a.entropy[row] = 0.f;
+                if (a.terms) a.terms[row] = PolicyTerms{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            }
+            if (GRAD) {
+                char* dzr = (char*)a.dlogits + (size_t)row * a.lddl * E;
+                uint4* dz = reinterpret_cast<uint4*>(dzr + begin * E);
+                for (int v = tid; v < nvec; v += NT) __stcs(dz + v, make_uint4(0, 0, 0, 0));
+                if (tid < ntail) X::store(dzr, tail + tid, 0.f);
+            }
+        }
+    }
+    __syncthreads();        // s_row
     TokenIn in = {0.f, 0.f, 0.f, 1.f};
-    int it = 0;                     // rows read so far
-    for (int n = 0; n < nrows; ++n) {
-        if (n > 0 && (n & 31) == 0) window = look(n);
-        const int64_t row = base + (int64_t)n * stride;
-        const bool first = rank == 0 && tid == 0, read = (window >> (n & 31)) & 1u;
-        const int32_t target = __shfl_sync(0xffffffffu, target_l, n & 31);
-        in.w = __shfl_sync(0xffffffffu, w_l, n & 31);
+    uint32_t phase = 0;
+    for (int it = 0, stage = 0; s_row[it & (VR_RING - 1)] >= 0; ++it) {
+        const int64_t row = s_row[it & (VR_RING - 1)];
+        const bool first = rank == 0 && tid == 0;
+        const int32_t target = a.targets[row];
         if (a.terms) {
+            in.w = a.weight[row];
             in.old = a.old_logp[row];
             in.A = a.adv[row];
             if (a.ref_logp) in.ref = a.ref_logp[row];
         }
-        const int next = read ? next_read(n, window) : nrows;
-        // a warp is done with the slice: the last one starts the copy of the next row's
+        const char* z = (const char*)a.logits + (size_t)row * a.ld * E;
+        const uint4* s_slice = s_dynamic + (size_t)stage * stage_vecs;
+        if (warp == 0) {
+            const int64_t later = s_row[(it + stages - 1) & (VR_RING - 1)] >= 0 ? next_row() : -1;
+            if (lane == 0) s_row[(it + stages) & (VR_RING - 1)] = later;
+        }
+        // a warp is done with the slice: the last one starts the copy of a later row's
         auto release = [&]() {
             __syncwarp();
-            if (lane == 0 && nvec > 0) {
+            if (lane == 0) {
                 __threadfence_block();
-                if (atomicAdd(&s_done, 1) == W - 1) {
-                    s_done = 0;
+                if (atomicAdd(&s_done[stage], 1) == W - 1) {
+                    s_done[stage] = 0;
                     __threadfence_block();
-                    if (next < nrows && s_abort == 0) copy(next);
+                    const int64_t later = s_row[(it + stages) & (VR_RING - 1)];
+                    if (nvec > 0 && later >= 0 && s_abort == 0) copy(later, stage);
                 }
             }
         };
-        bool live = read;
         RowGrad g = {0.f, 0.f, 0.f};
         float m = 0.f, log2s = 0.f, za = 0.f, zt = -INFINITY;      // za: the target's logit
-        if (read) {
-            const char* z = (const char*)a.logits + (size_t)row * a.ld * E;
+        bool live;
+        {
             if (tid < ntail) zt = X::load(z, tail + tid);
             if (rank == 0 && warp == 0) za = X::load(z, target);
-            if (nvec > 0 && !__all_sync(0xffffffffu, mbar_wait(bar_full, it & 1, &s_abort, 2))) break;
+            if (nvec > 0 && !__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, &s_abort, 2))) break;
             const WarpStats ws = warp_statistics<F32, ENTROPY, NT>(s_slice, GRAD ? s_slice : reinterpret_cast<const uint4*>(z + begin * E), nvec,
                                                                    zt, tid, k2, [&]() {
                                                                        if (!GRAD) release();
@@ -355,8 +434,8 @@ __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, 
             }
             // the next row into L2 while this one's gradient leaves (not earlier: the rows in flight and what has been
             // written of the gradient fill the part of L2 that would have to keep it)
-            if (GRAD && tid == 0 && nvec > 0 && next < nrows) bulk_prefetch(source(next), (uint32_t)nvec * 16);
-            ++it;
+            if (GRAD && tid == 0 && nvec > 0 && stages == 1 && s_row[(it + 1) & (VR_RING - 1)] >= 0)
+                bulk_prefetch(source(s_row[(it + 1) & (VR_RING - 1)]), (uint32_t)nvec * 16);
             // all warps' statistics, relative to the row's maximum; up to PARTS / 32 of them per lane
             float rs = 0.f, ru = 0.f;
             if (PARTS == 1) {
@@ -376,8 +455,8 @@ __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, 
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
                     const float d = exponent(x[i].x, m, k2), f = ex2(d);
-                    rs += f * x[i].y;
-                    if (ENTROPY) ru += f * (x[i].z + x[i].y * d);
+                    rs = fmaf(f, x[i].y, rs);
+                    if (ENTROPY) ru = fmaf(f, fmaf(x[i].y, d, x[i].z), ru);
                 }
                 rs = warp_sum(rs);
                 if (ENTROPY) ru = warp_sum(ru);
@@ -385,7 +464,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, 
             }
             const bool dist = !(rs == 0.f);        // else there is no finite logit
             log2s = dist ? lg2(rs) : 0.f;
-            const float logp = dist ? ((za - m) * k2 - log2s) * VR_LN2 : 0.f;
+            const float logp = dist ? fmaf(za - m, k2, -log2s) * VR_LN2 : 0.f;
             const float H = ENTROPY && dist ? (log2s - __fdividef(ru, rs)) * VR_LN2 : 0.f;
             if (first) {
                 if (a.logp) a.logp[row] = logp;
@@ -397,10 +476,6 @@ __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, 
                 g = token_terms(a, in, logp, H, log2s, &t);
                 if (first) a.terms[row] = t;
             }
-        } else if (first) {
-            if (target >= V) dk_report(a.status, DEV_BAD_INDEX, (int)row);
-            if (a.logp) a.logp[row] = 0.f;
-            if (a.entropy) a.entropy[row] = 0.f;
         }
         if (a.terms && !live && first) a.terms[row] = PolicyTerms{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (GRAD) {
@@ -434,7 +509,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, 
             } else {
                 for (int v = tid; v < nvec; v += NT) __stcs(dz + v, make_uint4(0, 0, 0, 0));
             }
-            if (read) release();
+            release();
             if (tid < ntail) {
                 float o = 0.f;
                 if (live) {
@@ -444,13 +519,18 @@ __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, 
                 X::store(dzr, tail + tid, o);
             }
         }
+        if (++stage == stages) {
+            stage = 0;
+            phase ^= 1;
+        }
     }
     __syncthreads();
     if (s_abort != 0 && tid == 0) {
         // given up: the shared memory is left only when no copy into it is in flight
         dk_report(a.status, DEV_TIMEOUT, s_abort * 1000000 + (int)blockIdx.x);
         const unsigned long long t0 = global_ns();
-        while (s_copies > 0 && !mbar_try_wait(bar_full, (s_copies - 1) & 1) && global_ns() - t0 < WAIT_LIMIT_NS) {}
+        for (int i = 0; i < stages; ++i)
+            while (s_copies[i] > 0 && !mbar_try_wait(bar_full + 8 * i, (s_copies[i] - 1) & 1) && global_ns() - t0 < WAIT_LIMIT_NS) {}
     }
     if (CLUSTER) {
         // no CTA of a cluster leaves while another may still write to its shared memory
@@ -461,14 +541,21 @@ __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, 
 
 template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD, int NT, bool CLUSTER>
 static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r, int C, cudaStream_t st) {
-    constexpr int N = F32 ? 4 : 8;
+    constexpr int N = F32 ? 4 : 8, SIZES = 18;
     auto kernel = k_vocab_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, NT, CLUSTER>;
     RowsLayout lay;
     lay.C = C;
     lay.slice = cdiv(cdiv(r.V, C), N) * N;
-    // shared memory in eight sizes, so that the number of CTAs an SM holds is asked for once per device and size
-    const int size = (int)cdiv(lay.slice * (F32 ? 4 : 2), NT * 16 * 4);        // in quarters of 16 vectors per thread
-    const size_t smem = (size_t)size * NT * 16 * 4;
+    // as many stages as leave the SM room for 768 threads; the mask where a CTA's 8 warps make it in a few microseconds (with
+    // shorter rows there are more of them per CTA, which evens them out, and fewer warps to make it)
+    const int64_t slice_bytes = lay.slice * (F32 ? 4 : 2), words = cdiv(r.T, 32);
+    const int64_t mask_bytes = NT >= 256 && words <= 256 ? words * 4 : 0;
+    lay.stages = (int)std::max<int64_t>(1, std::min<int64_t>(VR_STAGES, (NT * 280 - mask_bytes) / slice_bytes));
+    // shared memory in sixteenths of the largest slice (128 KB for 256 threads), so that the number of rows the device holds
+    // is asked for once per device and size
+    const int64_t unit = (int64_t)NT * 32;
+    const int size = (int)cdiv(lay.stages * slice_bytes + mask_bytes, unit);
+    const size_t smem = (size_t)size * unit;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cudaLaunchAttribute at[1];
@@ -480,12 +567,12 @@ static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.gridDim = dim3(C);
-    static std::atomic<int> resident[MAX_DEVICES][4][9];
+    static std::atomic<int> resident[MAX_DEVICES][4][SIZES];
     const int log2c = C == 1 ? 0 : C == 2 ? 1 : C == 4 ? 2 : 3;
-    std::atomic<int>* known = pool->device < MAX_DEVICES && size <= 8 ? &resident[pool->device][log2c][size] : nullptr;
+    std::atomic<int>* known = pool->device < MAX_DEVICES && size < SIZES ? &resident[pool->device][log2c][size] : nullptr;
     int rows = known ? known->load(std::memory_order_relaxed) : 0;
     if (rows == 0) {
-        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NT * 16 * 4 * 8));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((SIZES - 1) * unit)));
         if (CLUSTER) {
             MARLAAS_CUDA_TRY(cudaOccupancyMaxActiveClusters(&rows, kernel, &cfg));
         } else {
@@ -495,6 +582,7 @@ static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r
         if (rows < 1) return fail(MARLAAS_ERR_CUDA, "k_vocab_rows: no room for a cluster of %d", C);
         if (known) known->store(rows, std::memory_order_relaxed);
     }
+    lay.mask_words = r.T > rows && mask_bytes ? (int)words : 0;
     cfg.gridDim = dim3((unsigned)(std::min<int64_t>(rows, r.T) * C));
     MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, r, lay));
     MARLAAS_LAUNCH_CHECK("k_vocab_rows");
@@ -502,7 +590,7 @@ static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r
 }
 
 // The shape of a launch, from the sizes alone (not from what is wanted of the rows, so that all calls on a batch sum in one
-// order: the log-probabilities of marlaas_token_logprobs and of the loss are the same bits, and the ratios of an update's
+// order, and products and sums are fused where the code says so, not as the compiler likes: the log-probabilities of marlaas_token_logprobs and of the loss are the same bits, and the ratios of an update's
 // first pass exactly 1).
 template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD>
 static marlaas_status_t launch_shape(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st) {
