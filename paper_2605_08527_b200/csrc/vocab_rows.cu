@@ -197,7 +197,8 @@ __device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const u
             const uint4 q = slice[v];
 #pragma unroll
             for (int j = 0; j < N; j += 2) {
-                const float2 t = __fmul2_rn(__fadd2_rn(pair_of<F32>(q, j), make_float2(-mr, -mr)), make_float2(k2, k2));
+                float2 t = __fmul2_rn(__fadd2_rn(pair_of<F32>(q, j), make_float2(-mr, -mr)), make_float2(k2, k2));
+                if (ENTROPY) t = make_float2(max_nan(t.x, -200.f), max_nan(t.y, -200.f));
                 const float2 e = make_float2(ex2(t.x), ex2(t.y));
                 s2 = __fadd2_rn(s2, e);
                 if (ENTROPY) u2 = __ffma2_rn(e, t, u2);
@@ -207,15 +208,11 @@ __device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const u
         r.s = warp_sum(s2.x + s2.y);
         r.u = ENTROPY ? warp_sum(u2.x + u2.y) : 0.f;
     }
-    // Again from the true maximum if the reference was too far off, or if there is no finite logit or a NaN; the entropy's
-    // sum again, with exponents that stay finite, if a logit of -inf has made 0 (-inf) of its term.
-    const bool far = !(r.s > 0x1p-30f && r.s < 0x1p40f);
-    if (far || r.u != r.u) {
-        if (far) {
-            r.m = zt;
-            for (int v = tid; v < nvec; v += NT) r.m = max_nan(r.m, max_of<F32>(again[v]));
-            r.m = warp_max(r.m);
-        }
+    // again from the true maximum if the reference was too far off, or if there is no finite logit or a NaN
+    if (!(r.s > 0x1p-30f && r.s < 0x1p40f)) {
+        r.m = zt;
+        for (int v = tid; v < nvec; v += NT) r.m = max_nan(r.m, max_of<F32>(again[v]));
+        r.m = warp_max(r.m);
         const float mr = ref_of(r.m), tt = exponent(zt, mr, k2);
         float s = ex2(tt), u = __fmul_rn(s, tt);
         for (int v = tid; v < nvec; v += NT) {
@@ -227,8 +224,7 @@ __device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const u
                 u = fmaf(e, t, u);
             }
         }
-        s = warp_sum(s);
-        if (far) r.s = s;
+        r.s = warp_sum(s);
         if (ENTROPY) r.u = warp_sum(u);
     }
     return r;
