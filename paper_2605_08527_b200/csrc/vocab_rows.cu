@@ -563,9 +563,8 @@ static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.gridDim = dim3(C);
-    static std::atomic<int> resident[MAX_DEVICES][4][SIZES];
-    const int log2c = C == 1 ? 0 : C == 2 ? 1 : C == 4 ? 2 : 3;
-    std::atomic<int>* known = pool->device < MAX_DEVICES && size < SIZES ? &resident[pool->device][log2c][size] : nullptr;
+    static std::atomic<int> resident[MAX_DEVICES][9][SIZES];
+    std::atomic<int>* known = pool->device < MAX_DEVICES && size < SIZES ? &resident[pool->device][C][size] : nullptr;
     int rows = known ? known->load(std::memory_order_relaxed) : 0;
     if (rows == 0) {
         MARLAAS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((SIZES - 1) * unit)));
@@ -591,15 +590,16 @@ static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r
 template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD>
 static marlaas_status_t launch_shape(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st) {
     const int64_t vecs = cdiv(r.V, F32 ? 4 : 8);
-    int C = 1;
-    while (C < 8 && vecs > (int64_t)C * 256 * 16) C *= 2;
+    // as few CTAs per row as their shared memory allows
+    constexpr int BIG = 256;
+    int C = (int)std::min<int64_t>(8, cdiv(vecs * 16, BIG * 280));
     // few rows: more CTAs for each, down to one vector per thread
-    while (C < 8 && r.T * C * 2 <= pool->sm_count && vecs > (int64_t)C * 256) C *= 2;
-    if (C > 1) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 256, true>(pool, r, C, st);
+    while (C < 8 && r.T * C * 2 <= pool->sm_count && vecs > (int64_t)C * BIG) C = std::min(8, 2 * C);
+    if (C > 1) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, BIG, true>(pool, r, C, st);
     if (vecs <= 32 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 32, false>(pool, r, 1, st);
     if (vecs <= 64 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 64, false>(pool, r, 1, st);
     if (vecs <= 128 * 16) return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 128, false>(pool, r, 1, st);
-    return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, 256, false>(pool, r, 1, st);
+    return launch_rows<F32, GRAD, ENTROPY, ENTROPY_GRAD, BIG, false>(pool, r, 1, st);
 }
 
 marlaas_status_t launch_vocab_rows(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st) {
