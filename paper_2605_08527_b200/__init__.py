@@ -8,7 +8,7 @@ from . import workloads  # noqa: F401
 
 def __getattr__(name):
     if name == "binding" or name.startswith("marlaas_") or name in ("AdapterPool", "Segments", "MarlaasError",
-                                                                    "load_library"):
+                                                                    "load_library", "CompactAdamWTables", "compact_state"):
         import importlib
         b = importlib.import_module(".binding", __name__)
         return b if name == "binding" else getattr(b, name)

@@ -179,6 +179,18 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
+def _used_on(stream, *tensors) -> None:
+    """Tells torch's allocator of the stream that a call was given to run on, for tensors that were allocated for the call
+    on the current stream."""
+    if stream is None:
+        return
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream))
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
 def _dptr(t: Optional[torch.Tensor]) -> ctypes.c_void_p:
     return ctypes.c_void_p(None if t is None else t.data_ptr())
 
@@ -275,17 +287,18 @@ class AdapterPool:
             self._workspaces["ws"] = ws
         return ws
 
-    def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0) -> torch.Tensor:
-        """A cached workspace tensor for marlaas_group_advantages and marlaas_policy_loss (one per pool; not for
-        overlapping calls)."""
+    def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0, stream=None) -> torch.Tensor:
+        """A cached workspace tensor for marlaas_group_advantages and marlaas_policy_loss, one per stream."""
         key = (T, num_segments, num_groups)
         if self._policy_sizes[0] != key:
             self._policy_sizes = (key, marlaas_policy_workspace_bytes(self, T, num_segments, num_groups))
         need = max(self._policy_sizes[1], 256)
-        ws = self._workspaces.get("policy")
+        where = ("policy", _stream(stream).value)
+        ws = self._workspaces.get(where)
         if ws is None or ws.numel() < need:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-            self._workspaces["policy"] = ws
+            _used_on(stream, ws)
+            self._workspaces[where] = ws
         return ws
 
     def store(self):
@@ -562,7 +575,8 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
         adv = rewards.new_empty(T)
     if weight is None:
         weight = rewards.new_empty(T)
-    ws = workspace if workspace is not None else pool.policy_workspace(T, S, G)
+    ws = workspace if workspace is not None else pool.policy_workspace(T, S, G, stream)
+    _used_on(stream, seq_adv, adv, weight)
     _check(load_library().marlaas_group_advantages(
         pool.handle, T, ctypes.byref(seg.c), _f32(rewards, S, "rewards"), G, _i32(group_offsets, G + 1, "group_offsets"),
         _i32(targets, T, "targets"), eps, _f32(seq_adv, S, "seq_adv"), _f32(adv, T, "adv"), _f32(weight, T, "weight"),
@@ -580,6 +594,7 @@ def marlaas_token_logprobs(pool: AdapterPool, logits: torch.Tensor, targets: tor
     if entropy is None and with_entropy:
         entropy = torch.empty(T, dtype=torch.float32, device=logits.device)
     assert logits.dtype in _DTYPES and targets.is_cuda, "logits"
+    _used_on(stream, logp, entropy)
     _check(load_library().marlaas_token_logprobs(
         pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES[logits.dtype], _i32(targets, T, "targets"),
         inv_temperature, _f32(logp, T, "logp"), None if entropy is None else _f32(entropy, T, "entropy"), flags, _stream(stream)))
@@ -603,7 +618,8 @@ def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.
     if dlogits is not None:
         assert dlogits.dtype == logits.dtype and dlogits.shape[0] == T, "dlogits"
         lddl = _rows(dlogits, V, "dlogits")
-    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.c.num_segments)
+    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.c.num_segments, 0, stream)
+    _used_on(stream, stats)
     hp = marlaas_policy_loss_t(clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale)
     _check(load_library().marlaas_policy_loss(
         pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES[logits.dtype], _i32(targets, T, "targets"),
@@ -677,6 +693,7 @@ def marlaas_adamw_compact_state_export(pool: AdapterPool, state: torch.Tensor, m
         m = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
     if v is None:
         v = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
+    _used_on(stream, m, v)
     _check(load_library().marlaas_adamw_compact_state_export(pool.handle, blocks, state.data_ptr(), _f32(m, 256 * blocks, "m"),
                                                              _f32(v, 256 * blocks, "v"), _stream(stream)))
     return m, v

@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(ADV_THREADS) k_adv_expand(const AdvArgs a) {
         bool have = false;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            while (k > 0 && s + 1 < a.S && off[s + 1] <= first + k) {       // (sequences may be empty)
+            while (k > 0 && k < n && s + 1 < a.S && off[s + 1] <= first + k) {       // (sequences may be empty)
                 ++s;
                 have = false;
             }
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(STATS_THREADS) k_policy_stats(int T, int S, in
     sm100::dk_wait_prerequisites();
     const int32_t* off = cached ? s_off : seg_offsets;
     float v[MARLAAS_POLICY_STATS] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int i = tid; i < T; i += STATS_THREADS) {
+    for (int64_t i = tid; i < T; i += STATS_THREADS) {
         int lo = 0, hi = S;         // segments that begin at or before the token: the last of them holds it
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;

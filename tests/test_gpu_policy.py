@@ -348,6 +348,65 @@ def test_offsets_past_two_to_the_31(pool):
     assert all((grad[i] == 0).all() for i in (1, 6, T // 2 + 1, T - 3)) and logp[1].item() == 0
 
 
+@pytest.mark.parametrize("T,V,dtype", [(8300, 34001, torch.bfloat16), (9001, 8193, torch.float32), (1500, 33000, torch.float32)])
+def test_more_rows_than_the_device_holds_at_once(pool, T, V, dtype):
+    # rows of a quarter ignored tokens, in runs; torch's float64 log-softmax is the reference, a part of the rows at a time
+    unit = 4 if dtype == torch.float32 else 8
+    z = torch.empty((T, -(-V // unit) * unit), dtype=dtype, device="cuda").normal_(0, 3)[:, :V]
+    tgt = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
+    tgt[(torch.arange(T, device="cuda") // 37) % 4 == 0] = -1
+    old = torch.full((T,), -9.0, device="cuda")
+    adv, w = torch.randn(T, device="cuda"), torch.rand(T, device="cuda")
+    grad = torch.empty_strided(z.shape, z.stride(), dtype=dtype, device="cuda")
+    logp = torch.empty(T, device="cuda")
+    stats = B.marlaas_policy_loss(pool, z, tgt, segments([0, T // 3, T], [2, 0]), old, adv, w, dlogits=grad, logp=logp, clip_low=1e9, clip_high=1e9)
+    B.marlaas_check_status(pool)
+    assert torch.equal(B.marlaas_token_logprobs(pool, z, tgt), logp)
+    total = torch.zeros(2, dtype=torch.float64, device="cuda")
+    for i in range(0, T, 500):
+        y = torch.log_softmax(z[i:i + 500].double(), 1)
+        live = tgt[i:i + 500] >= 0
+        a = tgt[i:i + 500].clamp(min=0).long()[:, None]
+        lp = torch.where(live, y.gather(1, a)[:, 0], 0.0)
+        assert torch.all((logp[i:i + 500].double() - lp).abs() <= 1e-5 + 1e-6 * lp.abs())
+        c = torch.exp(lp + 9.0) * adv[i:i + 500].double() * w[i:i + 500].double() * live
+        want = y.exp() * c[:, None]
+        want.scatter_add_(1, a, -c[:, None])
+        err, size = (grad[i:i + 500].double() - want).abs(), want.abs()
+        assert torch.all(err <= (2.0 ** -8 if dtype == torch.bfloat16 else 0) * size + 6e-5 * (size + 1e-3 * c.abs()[:, None]) + 1e-37)
+        rows = torch.arange(i, min(i + 500, T), device="cuda")
+        total += torch.stack([(-c * (rows < T // 3)).sum(), (-c * (rows >= T // 3)).sum()])
+    assert torch.allclose(stats[[2, 0], 1].double(), total, rtol=1e-4, atol=1e-4 * total.abs().max().item())
+    assert stats[[2, 0], 7].sum().item() == (tgt >= 0).sum().item()
+
+
+@pytest.mark.parametrize("T,V", [(500, 40003), (600, 100), (3, 100)])
+def test_batches_without_a_row_to_read(pool, T, V):
+    z = torch.full((T, -(-V // 8) * 8), math.nan, dtype=torch.bfloat16, device="cuda")[:, :V]
+    grad = torch.full((T, -(-V // 8) * 8), 3.0, dtype=torch.bfloat16, device="cuda")[:, :V]
+    f = torch.full((T,), math.nan, device="cuda")
+    logp = torch.full((T,), 7.0, device="cuda")
+    stats = B.marlaas_policy_loss(pool, z, dev(np.full(T, -1), torch.int32), segments([0, T], [1]), f, f, f, dlogits=grad, logp=logp)
+    assert torch.all(grad == 0) and torch.all(logp == 0) and torch.all(stats == 0)
+    B.marlaas_check_status(pool)
+
+
+def test_a_call_on_a_stream_of_its_own(pool):
+    # the stream is an argument, the outputs are allocated by the call while another stream is current
+    _, z, z64, tgt = make_logits(40, 3001, torch.bfloat16, 12)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for st in (side, side.cuda_stream):
+        logp, H = B.marlaas_token_logprobs(pool, z, dev(tgt, torch.int32), with_entropy=True, stream=st)
+        side.synchronize()
+        logp_close(logp, op.token_logprobs(z64, tgt, 1.0)[0], "logp")
+        one = torch.ones(40, device="cuda")
+        torch.cuda.synchronize()
+        stats = B.marlaas_policy_loss(pool, z, dev(tgt, torch.int32), segments([0, 40], [0]), one, one, one, stream=st)
+        side.synchronize()
+        assert stats[0, 7].item() == (tgt >= 0).sum()
+
+
 def test_calls_can_be_captured_and_run_on_another_stream(pool):
     _, z, _, tgt = make_logits(33, 5003, torch.bfloat16, 9)
     old, ref, adv, w = (torch.rand(33, device="cuda") - 3 for _ in range(4))
@@ -395,6 +454,7 @@ def test_row_calls_refuse(pool):
     refused(inv, B.marlaas_policy_loss, z, t, seg, f, f, f, clip_high=math.nan)
     refused(inv, B.marlaas_policy_loss, z, t, seg, f, f, f, entropy_coef=INF)
     refused(inv, B.marlaas_policy_loss, z, t, seg, f, f, f, dlogits=torch.zeros(5 * 64, dtype=torch.bfloat16, device="cuda")[1:257].view(4, 64))
+    refused(inv, B.marlaas_policy_loss, z, t, seg, f, f, f, logp=f)                 # an input
     both = torch.zeros((5, 64), dtype=torch.bfloat16, device="cuda")
     refused(inv, B.marlaas_policy_loss, both[:4], t, seg, f, f, f, dlogits=both[1:])
     refused(inv, B.marlaas_policy_loss, z, t, seg, f, f, f, flags=B.MARLAAS_FLAG_REUSE_PLAN)
