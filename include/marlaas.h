@@ -322,7 +322,9 @@ marlaas_status_t marlaas_group_advantages(marlaas_pool_t* pool, int64_t T, const
  *  - A row with a negative target is ignored: it is not read, logp and entropy are 0.
  *  - Logits of -inf have probability 0.  A row whose logits are all -inf has no distribution: logp and entropy are 0.
  *  - A row with a NaN or +inf gets NaN.
- *  - A target >= V is reported by marlaas_check_status (MARLAAS_ERR_DEVICE_BAD_INDEX) and its row is ignored. */
+ *  - A target >= V is reported by marlaas_check_status (MARLAAS_ERR_DEVICE_BAD_INDEX) and its row is ignored.
+ *  - Sums run in an order that depends on T, V and dtype alone: on the same logits this call and marlaas_policy_loss give
+ *    the same bits, so that the ratios of an update's first pass are exactly 1. */
 marlaas_status_t marlaas_token_logprobs(marlaas_pool_t* pool, int64_t T, int64_t V, const void* logits, int64_t ld,
                                         int32_t dtype, const int32_t* targets, float inv_temperature, float* logp,
                                         float* entropy, uint32_t flags, void* cuda_stream);

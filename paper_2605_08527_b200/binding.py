@@ -175,7 +175,7 @@ def _check(rc: int) -> None:
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
         # the current device's current stream, without the Stream object (a few microseconds) that torch.cuda makes for it
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -287,13 +287,14 @@ class AdapterPool:
             self._workspaces["ws"] = ws
         return ws
 
-    def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0, stream=None) -> torch.Tensor:
-        """A cached workspace tensor for marlaas_group_advantages and marlaas_policy_loss, one per stream."""
+    def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0, stream=None, handle=None) -> torch.Tensor:
+        """A cached workspace tensor for marlaas_group_advantages and marlaas_policy_loss, one per stream (`handle`: what
+        _stream(stream) gives, if it is known)."""
         key = (T, num_segments, num_groups)
         if self._policy_sizes[0] != key:
             self._policy_sizes = (key, marlaas_policy_workspace_bytes(self, T, num_segments, num_groups))
         need = max(self._policy_sizes[1], 256)
-        where = ("policy", _stream(stream).value)
+        where = ("policy", (handle or _stream(stream)).value)
         ws = self._workspaces.get(where)
         if ws is None or ws.numel() < need:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)
@@ -537,13 +538,13 @@ def marlaas_kernel_timing_end(pool: AdapterPool):
 
 # ---- the policy update around the layer ----
 
-def _f32(t: torch.Tensor, n: int, name: str) -> ctypes.c_void_p:
-    assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n and t.is_cuda, name
+def _f32(t: torch.Tensor, n: int, name: str) -> int:
+    assert t.dtype is torch.float32 and t.is_cuda and t.is_contiguous() and t.numel() == n, name
     return t.data_ptr()
 
 
-def _i32(t: torch.Tensor, n: int, name: str) -> ctypes.c_void_p:
-    assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n, name
+def _i32(t: torch.Tensor, n: int, name: str) -> int:
+    assert t.dtype is torch.int32 and t.is_contiguous() and t.numel() == n, name
     return t.data_ptr()
 
 
@@ -575,12 +576,13 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
         adv = rewards.new_empty(T)
     if weight is None:
         weight = rewards.new_empty(T)
-    ws = workspace if workspace is not None else pool.policy_workspace(T, S, G, stream)
+    handle = _stream(stream)
+    ws = workspace if workspace is not None else pool.policy_workspace(T, S, G, stream, handle)
     _used_on(stream, seq_adv, adv, weight)
     _check(load_library().marlaas_group_advantages(
         pool.handle, T, ctypes.byref(seg.c), _f32(rewards, S, "rewards"), G, _i32(group_offsets, G + 1, "group_offsets"),
         _i32(targets, T, "targets"), eps, _f32(seq_adv, S, "seq_adv"), _f32(adv, T, "adv"), _f32(weight, T, "weight"),
-        ws.data_ptr(), ws.numel(), flags | seg.flags, _stream(stream)))
+        ws.data_ptr(), ws.numel(), flags | seg.flags, handle))
     return seq_adv, adv, weight
 
 
@@ -618,7 +620,8 @@ def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.
     if dlogits is not None:
         assert dlogits.dtype == logits.dtype and dlogits.shape[0] == T, "dlogits"
         lddl = _rows(dlogits, V, "dlogits")
-    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.c.num_segments, 0, stream)
+    handle = _stream(stream)
+    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.c.num_segments, 0, stream, handle)
     _used_on(stream, stats)
     hp = marlaas_policy_loss_t(clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale)
     _check(load_library().marlaas_policy_loss(
@@ -626,7 +629,7 @@ def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.
         ctypes.byref(seg.c), _f32(old_logp, T, "old_logp"), None if ref_logp is None else _f32(ref_logp, T, "ref_logp"),
         _f32(adv, T, "adv"), _f32(weight, T, "weight"), ctypes.byref(hp), None if dlogits is None else dlogits.data_ptr(), lddl,
         None if logp is None else _f32(logp, T, "logp"), _f32(stats, (pool.capacity + 1) * MARLAAS_POLICY_STATS, "stats"),
-        ws.data_ptr(), ws.numel(), flags | seg.flags, _stream(stream)))
+        ws.data_ptr(), ws.numel(), flags | seg.flags, handle))
     return stats
 
 

@@ -104,6 +104,11 @@ __device__ __forceinline__ float rcp_approx(float x) {
     return r;
 }
 
+// Products and sums of two numbers, each rounded by itself.  (Two-element instructions are no use here: a product and the sum
+// that takes it become one multiply-add, also with their rounding written out, and that moves about one code in a million.)
+__device__ __forceinline__ float2 mul_rn(float2 a, float2 b) { return make_float2(__fmul_rn(a.x, b.x), __fmul_rn(a.y, b.y)); }
+__device__ __forceinline__ float2 add_rn(float2 a, float2 b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
+
 // What a lane holds of a block of 256 elements: elements 4 lane .. 4 lane + 3 and 128 further on.
 struct CompactLane {
     float4 g[2], th[2];
@@ -157,9 +162,9 @@ __device__ __forceinline__ void compact_step(CompactLane& x, const CompactHyper&
                 vo[i] = __uint_as_float(cv ? cv * 16u + bv : 0u);
             }
             // products and sums rounded one by one: the same bits wherever this is computed
-            const float2 g = __fmul2_rn(make_float2(h.gscale, h.gscale), gp[p]);
-            const float2 m = __fadd2_rn(__fmul2_rn(make_float2(h.b1, h.b1), make_float2(mo[0], mo[1])), __fmul2_rn(make_float2(h.one_b1, h.one_b1), g));
-            const float2 v = __fadd2_rn(__fmul2_rn(make_float2(h.b2, h.b2), make_float2(vo[0], vo[1])), __fmul2_rn(__fmul2_rn(make_float2(h.one_b2, h.one_b2), g), g));
+            const float2 g = mul_rn(make_float2(h.gscale, h.gscale), gp[p]);
+            const float2 m = add_rn(mul_rn(make_float2(h.b1, h.b1), make_float2(mo[0], mo[1])), mul_rn(make_float2(h.one_b1, h.one_b1), g));
+            const float2 v = add_rn(mul_rn(make_float2(h.b2, h.b2), make_float2(vo[0], vo[1])), mul_rn(mul_rn(make_float2(h.one_b2, h.one_b2), g), g));
             // theta -= lr (c1 m / (sqrt(c2 v) + eps) + wd theta), root and reciprocal to about an ulp of the step
             const float2 u = __fmul2_rn(m, make_float2(h.lr_c1, h.lr_c1));
             th[p].x = fmaf(-h.lr_wd, th[p].x, th[p].x) - u.x * rcp_approx(fmaf(sqrt_approx(v.x), h.sqrt_c2, h.eps));

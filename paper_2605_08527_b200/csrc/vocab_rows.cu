@@ -21,6 +21,8 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+// Powers and logarithms of 2 by the special-function unit: a relative error of 2^-22 for the powers, an absolute one of
+// 2^-22 for the logarithm of a row's sum, 2e-7 of a log-probability of order 10.
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -87,7 +89,7 @@ __device__ __forceinline__ RowGrad token_terms(const VocabRows& a, const TokenIn
     float c = is_clipped ? 0.f : -plain, kl = 0.f;
     if (a.kl_coef != 0.f) {
         const float d = in.ref - logp, e1 = expm1f(d);     // exp(d) - d - 1 without its cancellation for small d
-        kl = e1 - d;
+        kl = d > 80.f ? e1 : e1 - d;        // (both may be infinite)
         c = fmaf(-a.kl_coef, e1, c);
     }
     PolicyTerms t;

@@ -132,6 +132,48 @@ def test_compact_commit_matches_the_definition(name):
     assert not all(torch.equal(x, y) for x, y in zip(after[0], after[2]))
 
 
+def test_codes_are_those_of_separately_rounded_operations_over_millions_of_elements():
+    # a product and a sum fused into one rounding move about one code in a million: 16 million elements, two steps, all
+    # bytes equal to the same fp32 operations done one by one with torch
+    K, N, r, T = 4096, 4096, 64, 32
+    pool = B.AdapterPool(K, N, r, T)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for t in range(T):
+        B.marlaas_adapter_pool_register(pool, t, 0, r, 1.0, torch.zeros(K, r, dtype=torch.bfloat16, device="cuda"),
+                                        torch.zeros(r, N, dtype=torch.bfloat16, device="cuda"))
+    n = K * r
+    grad = torch.randn(2 * T, n, generator=g, device="cuda") * torch.exp(2 * torch.randn(2 * T, n, generator=g, device="cuda"))
+    theta, state = torch.zeros_like(grad), torch.zeros(2 * T, n // 256 * 528, dtype=torch.uint8, device="cuda")
+    part = lambda x, k: [x[2 * t + k] for t in range(T)]        # noqa: E731
+    tables = B.CompactAdamWTables(pool, range(T), part(grad, 0), part(grad, 1), part(theta, 0), part(theta, 1), part(state, 0), part(state, 1))
+    f = lambda x: float(np.float32(x))      # noqa: E731
+    ref = state.clone()
+    bits = [torch.from_numpy(op.random_bits(n, 6, s, t, 0, k).astype(np.int64)) for s in (1, 2) for t in range(T) for k in (0, 1)]
+    for step in (1, 2):
+        B.marlaas_adapter_pool_adamw_compact_commit(pool, tables, step=step, seed=6, **HP)
+        blk = ref.view(-1, 528)
+        rnd = torch.stack(bits[(step - 1) * 2 * T:step * 2 * T]).cuda().view(-1, 256)
+        new = {}
+        gr = (grad * f(HP["grad_scale"])).view(-1, 256)
+        for name, at, orders, beta in (("m", 0, 15, HP["beta1"]), ("v", 256, 31, HP["beta2"])):
+            code = blk[:, at:at + 256].int()
+            base = ((blk[:, 512 + at // 256].int() - orders) * 8).clamp(min=0)[:, None]
+            mag = code & 127 if name == "m" else code
+            old = torch.where(mag > 0, (mag + base) << 20, torch.zeros_like(mag)).view(torch.float32)
+            old = torch.where(code > 127, -old, old) if name == "m" else old
+            one = float(np.float32(1) - np.float32(beta))
+            new[name] = old * f(beta) + (gr * one if name == "m" else (gr * one) * gr)
+        for name, at, orders, half in (("m", 0, 15, rnd & 0xFFFF), ("v", 256, 31, rnd >> 16)):
+            x = new[name]
+            b = x.view(torch.int32) & 0x7FFFFFFF
+            E = (b.amax(1) + 0xFFFFF) >> 23
+            code = ((b + (half.int() << 4)) >> 20) - ((E - orders) * 8).clamp(min=0)[:, None]
+            code = code.clamp(min=0) + torch.where(x < 0, 128, 0) if name == "m" else torch.where(b > 0, code.clamp(min=1), torch.zeros_like(code))
+            blk[:, at:at + 256], blk[:, 512 + at // 256] = code.to(torch.uint8), E.to(torch.uint8)
+        got = state.view(-1, 528)[:, :514]
+        assert torch.equal(got, blk[:, :514]), f"step {step}: {(got != blk[:, :514]).sum().item()} bytes differ"
+
+
 def _small_pool(ranks=(8, 4)):
     pool = B.AdapterPool(64, 64, 8, 3)
     bufs = []

@@ -326,6 +326,17 @@ def test_extreme_ratios(pool):
     assert stats[1, 1].item() == 0 and stats[2, 1].item() == INF
 
 
+def test_a_target_without_probability_has_an_infinite_kl_and_leaves_the_other_rows_alone(pool):
+    z = torch.zeros((3, 16), device="cuda")
+    z[1, 4] = -INF
+    f = torch.full((3,), -2.5, device="cuda")
+    grad = torch.empty_like(z)
+    stats = B.marlaas_policy_loss(pool, z, dev(np.full(3, 4), torch.int32), segments([0, 1, 2, 3], [0, 1, 2]), f, torch.ones(3, device="cuda"),
+                                  torch.ones(3, device="cuda"), ref_logp=f, dlogits=grad, kl_coef=0.1)
+    assert stats[1, 2].item() == INF and stats[1, 0].item() == INF and stats[1, 4].item() == 0
+    assert torch.isfinite(stats[[0, 2]]).all() and torch.isfinite(grad[[0, 2]]).all()
+
+
 def test_offsets_past_two_to_the_31(pool):
     V = 131072
     T = (1 << 31) // V + 40
