@@ -222,6 +222,8 @@ class Segments:
         self.seg_offsets, self.seg_slot = seg_offsets, seg_slot
         self.on_host = seg_offsets.device.type == "cpu"
         self.c = marlaas_segments_t(seg_slot.numel(), seg_offsets.data_ptr(), seg_slot.data_ptr())
+        self.ref = ctypes.byref(self.c)
+        self.num_segments = seg_slot.numel()
 
     @property
     def flags(self) -> int:
@@ -264,7 +266,7 @@ class AdapterPool:
         self.handle = h
         self.rank_stride = int(L.marlaas_adapter_pool_rank_stride(h))
         self._workspaces = {}
-        self._policy_sizes = (None, 0)
+        self._policy_last = None
         self._store = None
 
     def close(self):
@@ -290,16 +292,18 @@ class AdapterPool:
     def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0, stream=None, handle=None) -> torch.Tensor:
         """A cached workspace tensor for marlaas_group_advantages and marlaas_policy_loss, one per stream (`handle`: what
         _stream(stream) gives, if it is known)."""
-        key = (T, num_segments, num_groups)
-        if self._policy_sizes[0] != key:
-            self._policy_sizes = (key, marlaas_policy_workspace_bytes(self, T, num_segments, num_groups))
-        need = max(self._policy_sizes[1], 256)
-        where = ("policy", (handle or _stream(stream)).value)
+        key = (T, num_segments, num_groups, (handle or _stream(stream)).value)
+        last = self._policy_last
+        if last is not None and last[0] == key:
+            return last[1]
+        need = max(marlaas_policy_workspace_bytes(self, T, num_segments, num_groups), 256)
+        where = ("policy", key[3])
         ws = self._workspaces.get(where)
         if ws is None or ws.numel() < need:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             _used_on(stream, ws)
             self._workspaces[where] = ws
+        self._policy_last = (key, ws)
         return ws
 
     def store(self):
@@ -568,7 +572,7 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
                              workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None):
     """(seq_adv [S], adv [T], weight [T]) of a batch whose sequences are the segments of `seg`; group_offsets lives where
     the segment table does.  Outputs that are not given are allocated."""
-    T, S, G = targets.numel(), seg.c.num_segments, group_offsets.numel() - 1
+    T, S, G = targets.numel(), seg.num_segments, group_offsets.numel() - 1
     assert targets.is_cuda and rewards.is_cuda and group_offsets.is_cuda != seg.on_host, "group_offsets must be where the segment table is"
     if seq_adv is None:
         seq_adv = rewards.new_empty(S)
@@ -580,7 +584,7 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
     ws = workspace if workspace is not None else pool.policy_workspace(T, S, G, stream, handle)
     _used_on(stream, seq_adv, adv, weight)
     _check(load_library().marlaas_group_advantages(
-        pool.handle, T, ctypes.byref(seg.c), _f32(rewards, S, "rewards"), G, _i32(group_offsets, G + 1, "group_offsets"),
+        pool.handle, T, seg.ref, _f32(rewards, S, "rewards"), G, _i32(group_offsets, G + 1, "group_offsets"),
         _i32(targets, T, "targets"), eps, _f32(seq_adv, S, "seq_adv"), _f32(adv, T, "adv"), _f32(weight, T, "weight"),
         ws.data_ptr(), ws.numel(), flags | seg.flags, handle))
     return seq_adv, adv, weight
@@ -614,19 +618,19 @@ def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.
     T, V = logits.shape
     if stats is None:
         assert not (flags & MARLAAS_FLAG_ACCUMULATE), "stats to add to"
-        stats = torch.empty((pool.capacity + 1, MARLAAS_POLICY_STATS), dtype=torch.float32, device=pool.device)
+        stats = adv.new_empty((pool.capacity + 1, MARLAAS_POLICY_STATS))
     assert logits.dtype in _DTYPES and targets.is_cuda, "logits"
     lddl = 0
     if dlogits is not None:
         assert dlogits.dtype == logits.dtype and dlogits.shape[0] == T, "dlogits"
         lddl = _rows(dlogits, V, "dlogits")
     handle = _stream(stream)
-    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.c.num_segments, 0, stream, handle)
+    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.num_segments, 0, stream, handle)
     _used_on(stream, stats)
     hp = marlaas_policy_loss_t(clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale)
     _check(load_library().marlaas_policy_loss(
         pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES[logits.dtype], _i32(targets, T, "targets"),
-        ctypes.byref(seg.c), _f32(old_logp, T, "old_logp"), None if ref_logp is None else _f32(ref_logp, T, "ref_logp"),
+        seg.ref, _f32(old_logp, T, "old_logp"), None if ref_logp is None else _f32(ref_logp, T, "ref_logp"),
         _f32(adv, T, "adv"), _f32(weight, T, "weight"), ctypes.byref(hp), None if dlogits is None else dlogits.data_ptr(), lddl,
         None if logp is None else _f32(logp, T, "logp"), _f32(stats, (pool.capacity + 1) * MARLAAS_POLICY_STATS, "stats"),
         ws.data_ptr(), ws.numel(), flags | seg.flags, handle))
