@@ -17,9 +17,10 @@ __device__ __forceinline__ void policy_report(int32_t* status, int code, int det
 // Three steps: active tokens per sequence and advantages per group; totals per tenant (integer sums, so their order does not
 // matter); every token's advantage and weight.  They move 12 bytes per token: HBM for millions of tokens, launches for
 // ordinary batches.  A batch of at most ADV_SMALL_T tokens takes all three in one CTA (one launch); a larger one counts in
-// one kernel and expands in a second, each of whose CTAs forms the totals from the counts for itself; only for more than
-// ADV_SHARED_S sequences, whose counts would cost every CTA too much, a kernel between them does.
-constexpr int ADV_THREADS = 256, ADV_SMALL_THREADS = 1024, ADV_SMALL_T = 8192, ADV_SMALL_S = 1024, ADV_SHARED_S = 4096;
+// one kernel and expands in a second, each of whose CTAs forms the totals from the counts, and then every sequence's
+// advantage and weight, for itself in shared memory; only for more than ADV_SHARED_S sequences, for which that would cost
+// every CTA too much, a kernel between them forms the totals.
+constexpr int ADV_THREADS = 256, ADV_EXPAND_THREADS = 512, ADV_SMALL_THREADS = 1024, ADV_SMALL_T = 8192, ADV_SMALL_S = 1024, ADV_SHARED_S = 2048, ADV_RUN = 512;
 
 struct AdvArgs {
     int T, S, G, cap;
@@ -176,65 +177,98 @@ __global__ void __launch_bounds__(1024) k_adv_totals(const AdvArgs a) {
     }
 }
 
-// Four tokens per thread; the sequence of the first by bisection, the others' from there on.
+// A warp takes a run of ADV_RUN tokens, four per lane at a time; the sequence of the run's first token by bisection, the
+// others' from there on.
 template <bool SHARED>
-__global__ void __launch_bounds__(ADV_THREADS) k_adv_expand(const AdvArgs a) {
-    extern __shared__ int32_t s_mem[];      // SHARED: [cap + 1] totals, [S + 1] offsets
+__global__ void __launch_bounds__(ADV_EXPAND_THREADS) k_adv_expand(const AdvArgs a) {
+    extern __shared__ float2 s_seq[];       // SHARED: [S] advantage and weight, then [cap + 1] totals, [S] offsets
     const int tid = threadIdx.x;
-    int32_t* s_total = s_mem;
-    int32_t* s_off = s_mem + a.cap + 1;
+    int32_t* s_total = reinterpret_cast<int32_t*>(s_seq + a.S);
+    int32_t* s_off = s_total + a.cap + 1;
     if (SHARED) {
-        for (int b = tid; b <= a.cap; b += ADV_THREADS) s_total[b] = 0;
-        for (int s = tid; s <= a.S; s += ADV_THREADS) s_off[s] = a.off[s];
+        for (int b = tid; b <= a.cap; b += ADV_EXPAND_THREADS) s_total[b] = 0;
+        for (int s = tid; s < a.S; s += ADV_EXPAND_THREADS) s_off[s] = a.off[s];
         __syncthreads();
         sm100::dk_wait_prerequisites();
-        for (int s = tid; s < a.S; s += ADV_THREADS) {
-            const int n = a.count[s];
-            if (n) atomicAdd(s_total + bucket_of(a, a.slot[s]), a.token_mean ? n : 1);
+        for (int s0 = 0; s0 < a.S; s0 += ADV_EXPAND_THREADS) {
+            const int s = s0 + tid, n = s < a.S ? a.count[s] : 0, b = s < a.S ? bucket_of(a, a.slot[s]) : a.cap;
+            const int add = n ? (a.token_mean ? n : 1) : 0;
+            if (__all_sync(0xffffffffu, b == __shfl_sync(0xffffffffu, b, 0))) {     // a tenant's sequences side by side
+                const int sum = warp_total(add);
+                if ((tid & 31) == 0 && sum) atomicAdd(s_total + b, sum);
+            } else if (add) {
+                atomicAdd(s_total + b, add);
+            }
         }
+        __syncthreads();
+        for (int s = tid; s < a.S; s += ADV_EXPAND_THREADS)
+            s_seq[s] = make_float2(a.seq_adv[s], token_weight(a, a.count[s], s_total[bucket_of(a, a.slot[s])]));
         __syncthreads();
     }
     const int32_t* off = SHARED ? s_off : a.off;
-    const int32_t* total = SHARED ? s_total : a.total;
     const bool wide = ((((uintptr_t)a.targets | (uintptr_t)a.adv | (uintptr_t)a.weight)) & 15) == 0;
-    for (int64_t i0 = ((int64_t)blockIdx.x * ADV_THREADS + tid) * 4; i0 < a.T; i0 += (int64_t)gridDim.x * ADV_THREADS * 4) {
-        const int first = (int)i0, n = min(4, a.T - first);
-        int32_t t[4] = {-1, -1, -1, -1};
-        if (wide && n == 4) {
-            const int4 x = *reinterpret_cast<const int4*>(a.targets + first);
-            t[0] = x.x; t[1] = x.y; t[2] = x.z; t[3] = x.w;
-        } else {
-            for (int k = 0; k < n; ++k) t[k] = a.targets[first + k];
+    const int lane = tid & 31;
+    const int64_t warps = (int64_t)gridDim.x * (ADV_EXPAND_THREADS / 32);
+    for (int64_t w = ((int64_t)blockIdx.x * ADV_EXPAND_THREADS + tid) >> 5; w * ADV_RUN < a.T; w += warps) {
+        const int begin = (int)(w * ADV_RUN), end = min(a.T - begin, ADV_RUN) + begin;
+        int4 t[ADV_RUN / 128];
+#pragma unroll
+        for (int j = 0; j < ADV_RUN / 128; ++j) {
+            const int i = 128 * j + 4 * lane, n = end - begin - i;         // tokens from this thread's first on
+            t[j] = make_int4(-1, -1, -1, -1);
+            if (wide && n >= 4) {
+                t[j] = *reinterpret_cast<const int4*>(a.targets + begin + i);
+            } else {
+                if (n > 0) t[j].x = a.targets[begin + i];
+                if (n > 1) t[j].y = a.targets[begin + i + 1];
+                if (n > 2) t[j].z = a.targets[begin + i + 2];
+                if (n > 3) t[j].w = a.targets[begin + i + 3];
+            }
         }
-        int lo = 0, hi = a.S;               // sequences that begin at or before the token: the last of them holds it
+        int lo = 0, hi = a.S;               // sequences that begin at or before the run: the last of them holds its first token
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
-            if (off[mid] <= first) lo = mid + 1; else hi = mid;
+            if (off[mid] <= begin) lo = mid + 1; else hi = mid;
         }
         int s = lo - 1;
-        float v = 0.f, w = 0.f, va[4], wa[4];
-        bool have = false;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            while (k > 0 && k < n && s + 1 < a.S && off[s + 1] <= first + k) {       // (sequences may be empty)
-                ++s;
-                have = false;
+        for (int j = 0; j < ADV_RUN / 128; ++j) {
+            const int step = 128 * j, i = step + 4 * lane, n = end - begin - i;
+            if (begin + step >= end) break;
+            while (s + 1 < a.S && off[s + 1] <= begin + step) ++s;
+            const bool on[4] = {t[j].x >= 0, t[j].y >= 0, t[j].z >= 0, t[j].w >= 0};
+            float va[4], wa[4];
+            auto values = [&](int q) {
+                if (q < 0) return make_float2(0.f, 0.f);
+                if (SHARED) return s_seq[q];
+                return make_float2(a.seq_adv[q], token_weight(a, a.count[q], a.total[bucket_of(a, a.slot[q])]));
+            };
+            if (s + 1 >= a.S || off[s + 1] - begin >= step + 128) {        // all 128 tokens are of one sequence
+                const float2 vw = values(s);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    va[k] = on[k] ? vw.x : 0.f;
+                    wa[k] = on[k] ? vw.y : 0.f;
+                }
+            } else {
+                int q = s;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    while (k < n && q + 1 < a.S && off[q + 1] <= begin + i + k) ++q;       // (sequences may be empty)
+                    const float2 vw = on[k] ? values(q) : make_float2(0.f, 0.f);
+                    va[k] = vw.x;
+                    wa[k] = vw.y;
+                }
             }
-            if (!have && s >= 0) {
-                v = a.seq_adv[s];
-                w = token_weight(a, a.count[s], total[bucket_of(a, a.slot[s])]);
-                have = true;
-            }
-            va[k] = t[k] >= 0 ? v : 0.f;
-            wa[k] = t[k] >= 0 ? w : 0.f;
-        }
-        if (wide && n == 4) {
-            if (a.adv) *reinterpret_cast<float4*>(a.adv + first) = make_float4(va[0], va[1], va[2], va[3]);
-            if (a.weight) *reinterpret_cast<float4*>(a.weight + first) = make_float4(wa[0], wa[1], wa[2], wa[3]);
-        } else {
-            for (int k = 0; k < n; ++k) {
-                if (a.adv) a.adv[first + k] = va[k];
-                if (a.weight) a.weight[first + k] = wa[k];
+            if (wide && n >= 4) {
+                if (a.adv) *reinterpret_cast<float4*>(a.adv + begin + i) = make_float4(va[0], va[1], va[2], va[3]);
+                if (a.weight) *reinterpret_cast<float4*>(a.weight + begin + i) = make_float4(wa[0], wa[1], wa[2], wa[3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k < n && a.adv) a.adv[begin + i + k] = va[k];
+                    if (k < n && a.weight) a.weight[begin + i + k] = wa[k];
+                }
             }
         }
     }
@@ -255,7 +289,7 @@ static marlaas_status_t launch_advantages(const marlaas_pool* pool, const AdvArg
     else k_adv_count<1><<<grid, ADV_THREADS, 0, st>>>(a);
     MARLAAS_LAUNCH_CHECK("k_adv_count");
     if (!a.adv && !a.weight) return MARLAAS_OK;
-    const int egrid = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(a.T, ADV_THREADS * 4), most));
+    const int egrid = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(a.T, (int64_t)ADV_EXPAND_THREADS / 32 * ADV_RUN), (int64_t)pool->sm_count * 4));
     if (a.S <= ADV_SHARED_S) {
         cudaLaunchConfig_t cfg;
         memset(&cfg, 0, sizeof(cfg));
@@ -263,8 +297,8 @@ static marlaas_status_t launch_advantages(const marlaas_pool* pool, const AdvArg
         at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.gridDim = dim3((unsigned)egrid);
-        cfg.blockDim = dim3(ADV_THREADS);
-        cfg.dynamicSmemBytes = sizeof(int32_t) * ((size_t)a.cap + 1 + a.S + 1);
+        cfg.blockDim = dim3(ADV_EXPAND_THREADS);
+        cfg.dynamicSmemBytes = sizeof(float2) * (size_t)a.S + sizeof(int32_t) * ((size_t)a.cap + 1 + a.S);
         cfg.stream = st;
         cfg.attrs = at;
         cfg.numAttrs = 1;
@@ -272,7 +306,7 @@ static marlaas_status_t launch_advantages(const marlaas_pool* pool, const AdvArg
     } else {
         k_adv_totals<<<1, 1024, 0, st>>>(a);
         MARLAAS_LAUNCH_CHECK("k_adv_totals");
-        k_adv_expand<false><<<egrid, ADV_THREADS, 0, st>>>(a);
+        k_adv_expand<false><<<egrid, ADV_EXPAND_THREADS, 0, st>>>(a);
     }
     MARLAAS_LAUNCH_CHECK("k_adv_expand");
     return MARLAAS_OK;

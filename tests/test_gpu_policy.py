@@ -56,6 +56,8 @@ def _ragged(seed, S, longest, slots):
 ADV_CASES["ragged"] = _ragged(1, 61, 40, 5)
 ADV_CASES["many short sequences"] = _ragged(2, 3001, 3, 5)
 ADV_CASES["few long sequences"] = _ragged(3, 3, 30000, 2)
+ADV_CASES["a thousand sequences"] = _ragged(4, 1500, 40, 5)
+ADV_CASES["more sequences than fit shared memory"] = _ragged(5, 2500, 90, 3)
 
 
 @pytest.mark.parametrize("name", ADV_CASES)
@@ -73,6 +75,30 @@ def test_group_advantages(pool, name, token_mean, no_std):
         # a few fp32 operations on values of order 1; groups all alike are exact zeros on both sides
         np.testing.assert_allclose(g.cpu().numpy(), r, rtol=1e-5, atol=2e-6 if what != "weight" else 0, err_msg=what)
         assert np.array_equal(g.cpu().numpy() == 0, r == 0) or what != "weight"
+
+
+@pytest.mark.parametrize("name", ["ragged", "a thousand sequences", "more sequences than fit shared memory"])
+def test_group_advantages_of_unaligned_and_absent_outputs(pool, name):
+    off, slot, rewards, groups, tgt = ADV_CASES[name]
+    T, S = len(tgt), len(slot)
+    r, g = dev(np.array(rewards), torch.float32), dev(groups, torch.int32)
+    want = B.marlaas_group_advantages(pool, segments(off, slot), r, g, dev(np.array(tgt), torch.int32))
+    t = torch.zeros(T + 1, dtype=torch.int32, device="cuda")
+    t[1:] = torch.tensor(tgt)
+    out = [torch.full((n + 3,), 9.0, device="cuda") for n in (S, T, T)]
+    B.marlaas_group_advantages(pool, segments(off, slot), r, g, t[1:], seq_adv=out[0][1:S + 1], adv=out[1][1:T + 1], weight=out[2][2:T + 2])
+    assert torch.equal(out[0][1:S + 1], want[0]) and torch.equal(out[1][1:T + 1], want[1]) and torch.equal(out[2][2:T + 2], want[2])
+    assert all((o[[0, -1]] == 9.0).all() for o in out)
+    # an output that is not wanted is NULL at the C boundary
+    ws = torch.empty(B.marlaas_policy_workspace_bytes(pool, T, S, len(groups) - 1), dtype=torch.uint8, device="cuda")
+    seg = segments(off, slot)
+    for keep in range(3):
+        got = [torch.full((n,), 7.0, device="cuda") for n in (S, T, T)]
+        ptr = [o.data_ptr() if k == keep else None for k, o in enumerate(got)]
+        rc = B.load_library().marlaas_group_advantages(pool.handle, T, seg.ref, r.data_ptr(), len(groups) - 1, g.data_ptr(),
+                                                       t[1:].data_ptr(), 1e-6, *ptr, ws.data_ptr(), ws.numel(), 0, B._stream(None))
+        assert rc == B.MARLAAS_OK and torch.equal(got[keep], want[keep])
+        assert all((o == 7.0).all() for k, o in enumerate(got) if k != keep)
 
 
 def test_group_advantages_alike_rewards_host_tables_and_streams(pool):
