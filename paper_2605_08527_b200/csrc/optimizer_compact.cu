@@ -53,9 +53,12 @@ struct CompactArgs {
 
 // Random bits of an element: two rounds of xor-shift and multiplication by odd constants (2^32 divided by the golden ratio,
 // and by the square root of 2), a bijection of the 32-bit numbers.
-__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
+__host__ __device__ __forceinline__ uint32_t mix32_open(uint32_t x) {      // without the last step
     x = (x ^ (x >> 16)) * 0x9E3779B9u;
-    x = (x ^ (x >> 15)) * 0xB504F333u;
+    return (x ^ (x >> 15)) * 0xB504F333u;
+}
+static uint32_t mix32(uint32_t x) {
+    x = mix32_open(x);
     return x ^ (x >> 16);
 }
 static uint32_t stream_key(uint64_t seed, uint64_t step, uint64_t tenant, uint32_t matrix) {
@@ -209,9 +212,10 @@ __device__ __forceinline__ void compact_step(CompactLane& x, const CompactHyper&
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int k = 4 * q + i;
-            const uint32_t r = mix32(rnd + 4 * lane + (uint32_t)(128 * q + i));
-            cm[i] = code_of(mb[k] & 0x7fffffffu, r & 0xffffu, nm);
-            cv[i] = max(code_of(vb[k], r >> 16, nv), (int32_t)min(vb[k], 1u));       // a positive v keeps the smallest code
+            // mix32's last step leaves the high half as it is and adds it to the low half
+            const uint32_t r = mix32_open(rnd + 4 * lane + (uint32_t)(128 * q + i)), high = r >> 16;
+            cm[i] = code_of(mb[k] & 0x7fffffffu, (r ^ high) & 0xffffu, nm);
+            cv[i] = max(code_of(vb[k], high, nv), (int32_t)min(vb[k], 1u));       // a positive v keeps the smallest code
         }
         // (a sign without a magnitude, of a -0 or a moment that was cut off, is a zero too)
         reinterpret_cast<uint32_t*>(blk)[32 * q + lane] = bytes(cm[0], cm[1], cm[2], cm[3]) | signs(mb[4 * q], mb[4 * q + 1], mb[4 * q + 2], mb[4 * q + 3]);
