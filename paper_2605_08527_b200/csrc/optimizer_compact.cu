@@ -1,9 +1,9 @@
 // AdamW and commit with both moments in 8 bits (Algorithm 1: "PolicyUpdate" and the commit of the new adapter version;
 // Methods, Multi-Task Manager: per-task optimizer state, which at 8 bytes per element is four times the bf16 adapter
 // itself).  The state's format is in marlaas.h.  Per element: gradient 4 B read, master 4 + 4, moments 2.06 + 2.06, the
-// pool's bf16 2 written = 18.1 bytes and no reuse: bound by HBM, with the arithmetic not far behind (81 instructions per
+// pool's bf16 2 written = 18.1 bytes and no reuse: bound by HBM, with the arithmetic not far behind (90 instructions per
 // element, most of them integer work on codes and random bits: the ALU pipes are two thirds busy at the rate reached).
-// Measured: 89 us for 32 tenants of rank 32 over a 4096 x (3 x 4096) pool (25.2 M elements, 456 MB, 0.79 of the copy rate;
+// Measured: 91 us for 32 tenants of rank 32 over a 4096 x (3 x 4096) pool (25.2 M elements, 456 MB, 0.78 of the copy rate;
 // 155 us with one element at a time and IEEE division and root), 115 us for rank 128 over 4096 x 4096 (0.82).
 #include <string.h>
 
@@ -402,7 +402,8 @@ static marlaas_status_t launch_compact(const marlaas_pool* pool, const CompactTe
     const double c1 = 1.0 / (1.0 - std::pow((double)hp.beta1, (double)hp.step)), c2 = 1.0 / (1.0 - std::pow((double)hp.beta2, (double)hp.step));
     a.h.b1 = hp.beta1; a.h.b2 = hp.beta2; a.h.one_b1 = 1.f - hp.beta1; a.h.one_b2 = 1.f - hp.beta2; a.h.gscale = hp.grad_scale;
     a.h.sqrt_c2 = (float)std::sqrt(c2); a.h.eps = hp.eps; a.h.lr_c1 = (float)(hp.lr * c1); a.h.lr_wd = hp.lr * hp.weight_decay;
-    // longer units spread a CTA's set-up over more elements, shorter ones a small update over more SMs
+    // longer units spread a CTA's set-up over more elements (32 tenants of rank 32 over 4096 x 3 4096: 91 us against 120),
+    // shorter ones a small update over more SMs (4 tenants of rank 16 over 1024 x 1024: 9.2 us against 13.1)
     int64_t elems = 0;
     for (int i = 0; i < n; ++i) elems += t[i].rank * (pool->P * pool->K + pool->N);
     a.unit = elems >= (int64_t)pool->sm_count * 8 * OC_UNIT * OC_LONG ? OC_UNIT * OC_LONG : OC_UNIT;
