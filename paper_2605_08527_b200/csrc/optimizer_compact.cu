@@ -8,7 +8,6 @@
 #include <string.h>
 
 #include <cmath>
-#include <numeric>
 
 #include "internal.cuh"
 

@@ -133,9 +133,10 @@ __device__ __forceinline__ float max_of(const uint4& q) {
 // another only for that exchange: each publishes its statistics (to all CTAs of the cluster), then every warp merges all of
 // them.
 //
-// What bounds it: HBM, with the arithmetic close behind (per element of a bf16 row 12 issue slots and 2 special-function
-// operations, 45 % and 65 % of what the SMs have while the row streams).  Tried and not kept: the slice in registers
-// (2 CTAs per SM, 438 us for the loss over 4096 x 131072 against 400), chunks that are refilled one by one (441 us: the
+// What bounds it: HBM, with the arithmetic close behind (per element of a bf16 row 13 issue slots and 2 special-function
+// operations, 56 % and 69 % of what the SMs have while the row streams): loss and gradient over 16384 x 32768 bf16 in 381 us,
+// 0.87 of the copy rate; over 8192 x 131072, four CTAs per row, 764 us, 0.87.  Tried and not kept: the slice in registers
+// (2 CTAs per SM, 438 us for the loss over 4096 x 131072 against 398), chunks that are refilled one by one (441 us: the
 // waits cost more than the earlier copies gain), a share of the exponentials as polynomials on the FMA pipes (425 us).
 // Rows are dealt out in advance (no counter that calls would have to share): the k-th row that is read goes to cluster
 // k mod clusters, so that prompt tokens, which cost next to nothing, do not leave some clusters with more work than others.
@@ -409,72 +410,69 @@ __global__ void __launch_bounds__(NT, 768 / NT) k_vocab_rows(const VocabRows a, 
         };
         RowGrad g = {0.f, 0.f, 0.f};
         float m = 0.f, log2s = 0.f, za = 0.f, zt = -INFINITY;      // za: the target's logit
-        bool live;
-        {
-            if (tid < ntail) zt = X::load(z, tail + tid);
-            if (rank == 0 && warp == 0) za = X::load(z, target);
-            if (nvec > 0 && !__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, &s_abort, 2))) break;
-            const WarpStats ws = warp_statistics<F32, ENTROPY, NT>(s_slice, GRAD ? s_slice : reinterpret_cast<const uint4*>(z + begin * E), nvec,
-                                                                   zt, tid, k2, [&]() {
-                                                                       if (!GRAD) release();
-                                                                   });
-            // Two buffers: a warp writes for row i + 2 only after all warps have written for row i + 1, which they do
-            // when they have read row i.
-            const int b = it & 1;
-            if (CLUSTER) {
-                if (tid == 0) mbar_expect_tx(bar_stat + 8 * b, (uint32_t)(C * W * 16));
-                if (lane < C)
-                    send_stats(dk_map_to_cta(smem_u32(&s_part[b][rank * W + warp]), lane), dk_map_to_cta(bar_stat + 8 * b, lane), ws.m,
-                               ws.s, ws.u, za);
-                if (!__all_sync(0xffffffffu, mbar_wait(bar_stat + 8 * b, (it >> 1) & 1, &s_abort, 3))) break;
-            } else if (PARTS > 1) {
-                if (lane == 0) s_part[b][warp] = make_float4(ws.m, ws.s, ws.u, za);
-                __syncthreads();
-            }
-            // the next row into L2 while this one's gradient leaves (not earlier: the rows in flight and what has been
-            // written of the gradient fill the part of L2 that would have to keep it)
-            if (GRAD && tid == 0 && nvec > 0 && stages == 1 && s_row[(it + 1) & (VR_RING - 1)] >= 0)
-                bulk_prefetch(source(s_row[(it + 1) & (VR_RING - 1)]), (uint32_t)nvec * 16);
-            // all warps' statistics, relative to the row's maximum; up to PARTS / 32 of them per lane
-            float rs = 0.f, ru = 0.f;
-            if (PARTS == 1) {
-                m = ref_of(ws.m);
-                rs = ws.s;
-                ru = ws.u;
-            } else {
-                constexpr int PER = (PARTS + 31) / 32;
-                float4 x[PER];
-                float rm = -INFINITY;
+        if (tid < ntail) zt = X::load(z, tail + tid);
+        if (rank == 0 && warp == 0) za = X::load(z, target);
+        if (nvec > 0 && !__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * stage, phase, &s_abort, 2))) break;
+        const uint4* again = GRAD ? s_slice : reinterpret_cast<const uint4*>(z + begin * E);
+        const WarpStats ws = warp_statistics<F32, ENTROPY, NT>(s_slice, again, nvec, zt, tid, k2, [&]() {
+            if (!GRAD) release();
+        });
+        // Two buffers: a warp writes for row i + 2 only after all warps have written for row i + 1, which they do
+        // when they have read row i.
+        const int b = it & 1;
+        if (CLUSTER) {
+            if (tid == 0) mbar_expect_tx(bar_stat + 8 * b, (uint32_t)(C * W * 16));
+            if (lane < C)
+                send_stats(dk_map_to_cta(smem_u32(&s_part[b][rank * W + warp]), lane), dk_map_to_cta(bar_stat + 8 * b, lane), ws.m,
+                           ws.s, ws.u, za);
+            if (!__all_sync(0xffffffffu, mbar_wait(bar_stat + 8 * b, (it >> 1) & 1, &s_abort, 3))) break;
+        } else if (PARTS > 1) {
+            if (lane == 0) s_part[b][warp] = make_float4(ws.m, ws.s, ws.u, za);
+            __syncthreads();
+        }
+        // the next row into L2 while this one's gradient leaves (not earlier: the rows in flight and what has been
+        // written of the gradient fill the part of L2 that would have to keep it)
+        if (GRAD && tid == 0 && nvec > 0 && stages == 1 && s_row[(it + 1) & (VR_RING - 1)] >= 0)
+            bulk_prefetch(source(s_row[(it + 1) & (VR_RING - 1)]), (uint32_t)nvec * 16);
+        // all warps' statistics, relative to the row's maximum; up to PARTS / 32 of them per lane
+        float rs = 0.f, ru = 0.f;
+        if (PARTS == 1) {
+            m = ref_of(ws.m);
+            rs = ws.s;
+            ru = ws.u;
+        } else {
+            constexpr int PER = (PARTS + 31) / 32;
+            float4 x[PER];
+            float rm = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    x[i] = lane + 32 * i < C * W ? s_part[b][lane + 32 * i] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-                    rm = max_nan(rm, x[i].x);
-                }
-                m = ref_of(warp_max(rm));
+            for (int i = 0; i < PER; ++i) {
+                x[i] = lane + 32 * i < C * W ? s_part[b][lane + 32 * i] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+                rm = max_nan(rm, x[i].x);
+            }
+            m = ref_of(warp_max(rm));
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const float d = exponent(x[i].x, m, k2), f = ex2(d);
-                    rs = fmaf(f, x[i].y, rs);
-                    if (ENTROPY) ru = fmaf(f, fmaf(x[i].y, d, x[i].z), ru);
-                }
-                rs = warp_sum(rs);
-                if (ENTROPY) ru = warp_sum(ru);
-                za = s_part[b][0].w;
+            for (int i = 0; i < PER; ++i) {
+                const float d = exponent(x[i].x, m, k2), f = ex2(d);
+                rs = fmaf(f, x[i].y, rs);
+                if (ENTROPY) ru = fmaf(f, fmaf(x[i].y, d, x[i].z), ru);
             }
-            const bool dist = !(rs == 0.f);        // else there is no finite logit
-            log2s = dist ? lg2(rs) : 0.f;
-            const float logp = dist ? fmaf(za - m, k2, -log2s) * VR_LN2 : 0.f;
-            const float H = ENTROPY && dist ? (log2s - __fdividef(ru, rs)) * VR_LN2 : 0.f;
-            if (first) {
-                if (a.logp) a.logp[row] = logp;
-                if (a.entropy) a.entropy[row] = H;
-            }
-            live = dist && in.w != 0.f;
-            if (a.terms && live) {
-                PolicyTerms t;
-                g = token_terms(a, in, logp, H, log2s, &t);
-                if (first) a.terms[row] = t;
-            }
+            rs = warp_sum(rs);
+            if (ENTROPY) ru = warp_sum(ru);
+            za = s_part[b][0].w;
+        }
+        const bool dist = !(rs == 0.f);        // else there is no finite logit
+        log2s = dist ? lg2(rs) : 0.f;
+        const float logp = dist ? fmaf(za - m, k2, -log2s) * VR_LN2 : 0.f;
+        const float H = ENTROPY && dist ? (log2s - __fdividef(ru, rs)) * VR_LN2 : 0.f;
+        if (first) {
+            if (a.logp) a.logp[row] = logp;
+            if (a.entropy) a.entropy[row] = H;
+        }
+        const bool live = dist && in.w != 0.f;
+        if (a.terms && live) {
+            PolicyTerms t;
+            g = token_terms(a, in, logp, H, log2s, &t);
+            if (first) a.terms[row] = t;
         }
         if (a.terms && !live && first) a.terms[row] = PolicyTerms{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (GRAD) {
