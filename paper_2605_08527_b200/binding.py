@@ -254,6 +254,7 @@ class AdapterPool:
             nbytes = L.marlaas_adapter_pool_storage_bytes_segmented(d_in, len(self.parts), widths, max_rank, capacity)
         if nbytes == 0:
             raise MarlaasError(MARLAAS_ERR_INVALID_ARG, "invalid pool dimensions")
+        self.index = idx
         with torch.cuda.device(idx):
             self.storage = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
             h = ctypes.c_void_p()
@@ -542,24 +543,24 @@ def marlaas_kernel_timing_end(pool: AdapterPool):
 
 # ---- the policy update around the layer ----
 
-def _f32(t: torch.Tensor, n: int, name: str) -> int:
-    assert t.dtype is torch.float32 and t.is_cuda and t.is_contiguous() and t.numel() == n, name
+def _f32(t: torch.Tensor, n: int, name: str, device: int) -> int:
+    assert t.dtype is torch.float32 and t.get_device() == device and t.is_contiguous() and t.numel() == n, name
     return t.data_ptr()
 
 
-def _i32(t: torch.Tensor, n: int, name: str) -> int:
-    assert t.dtype is torch.int32 and t.is_contiguous() and t.numel() == n, name
+def _i32(t: torch.Tensor, n: int, name: str, device: int) -> int:
+    assert t.dtype is torch.int32 and t.get_device() == device and t.is_contiguous() and t.numel() == n, name
     return t.data_ptr()
 
 
 _DTYPES = {torch.bfloat16: MARLAAS_DTYPE_BF16, torch.float32: MARLAAS_DTYPE_F32}
 
 
-def _rows(t: torch.Tensor, V: int, name: str) -> int:
-    assert t.dim() == 2 and t.shape[1] == V and (V == 1 or t.stride(1) == 1) and t.is_cuda, name
-    ld = t.stride(0)
+def _rows(t: torch.Tensor, V: int, name: str, device: int) -> int:
+    """Leading dimension of a [T][V] matrix of logits or of their gradient."""
+    assert t.dim() == 2 and t.shape[1] == V and (V == 1 or t.stride(1) == 1) and t.get_device() == device, name
     # (torch is free with the stride of a single row)
-    return ld if t.shape[0] > 1 else max(ld, (V + 7) // 8 * 8)
+    return t.stride(0) if t.shape[0] > 1 else (V + 7) // 8 * 8
 
 
 def marlaas_policy_workspace_bytes(pool: AdapterPool, T: int, num_segments: int, num_groups: int = 0) -> int:
@@ -572,8 +573,7 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
                              workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None):
     """(seq_adv [S], adv [T], weight [T]) of a batch whose sequences are the segments of `seg`; group_offsets lives where
     the segment table does.  Outputs that are not given are allocated."""
-    T, S, G = targets.numel(), seg.num_segments, group_offsets.numel() - 1
-    assert targets.is_cuda and rewards.is_cuda and group_offsets.is_cuda != seg.on_host, "group_offsets must be where the segment table is"
+    T, S, G, dev = targets.numel(), seg.num_segments, group_offsets.numel() - 1, pool.index
     if seq_adv is None:
         seq_adv = rewards.new_empty(S)
     if adv is None:
@@ -584,8 +584,8 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
     ws = workspace if workspace is not None else pool.policy_workspace(T, S, G, stream, handle)
     _used_on(stream, seq_adv, adv, weight)
     _check(load_library().marlaas_group_advantages(
-        pool.handle, T, seg.ref, _f32(rewards, S, "rewards"), G, _i32(group_offsets, G + 1, "group_offsets"),
-        _i32(targets, T, "targets"), eps, _f32(seq_adv, S, "seq_adv"), _f32(adv, T, "adv"), _f32(weight, T, "weight"),
+        pool.handle, T, seg.ref, _f32(rewards, S, "rewards", dev), G, _i32(group_offsets, G + 1, "group_offsets (where the segment table is)", -1 if seg.on_host else dev),
+        _i32(targets, T, "targets", dev), eps, _f32(seq_adv, S, "seq_adv", dev), _f32(adv, T, "adv", dev), _f32(weight, T, "weight", dev),
         ws.data_ptr(), ws.numel(), flags | seg.flags, handle))
     return seq_adv, adv, weight
 
@@ -594,16 +594,16 @@ def marlaas_token_logprobs(pool: AdapterPool, logits: torch.Tensor, targets: tor
                            logp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
                            with_entropy: bool = False, flags: int = 0, stream=None):
     """logp [T] of the targets (negative = ignored), and with `with_entropy` or `entropy` (logp, entropy)."""
-    T, V = logits.shape
+    (T, V), dev = logits.shape, pool.index
     if logp is None:
         logp = torch.empty(T, dtype=torch.float32, device=logits.device)
     if entropy is None and with_entropy:
         entropy = torch.empty(T, dtype=torch.float32, device=logits.device)
-    assert logits.dtype in _DTYPES and targets.is_cuda, "logits"
+    assert logits.dtype in _DTYPES, "logits"
     _used_on(stream, logp, entropy)
     _check(load_library().marlaas_token_logprobs(
-        pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES[logits.dtype], _i32(targets, T, "targets"),
-        inv_temperature, _f32(logp, T, "logp"), None if entropy is None else _f32(entropy, T, "entropy"), flags, _stream(stream)))
+        pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits", dev), _DTYPES[logits.dtype], _i32(targets, T, "targets", dev),
+        inv_temperature, _f32(logp, T, "logp", dev), None if entropy is None else _f32(entropy, T, "entropy", dev), flags, _stream(stream)))
     return logp if entropy is None else (logp, entropy)
 
 
@@ -615,24 +615,24 @@ def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.
                         workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> torch.Tensor:
     """Clipped policy loss with KL and entropy terms: returns stats [capacity + 1][8] (see marlaas.h; column 0 is the loss
     per slot) and writes its gradient by the logits to `dlogits` (which may be `logits` itself) if given."""
-    T, V = logits.shape
+    (T, V), dev = logits.shape, pool.index
     if stats is None:
         assert not (flags & MARLAAS_FLAG_ACCUMULATE), "stats to add to"
         stats = adv.new_empty((pool.capacity + 1, MARLAAS_POLICY_STATS))
-    assert logits.dtype in _DTYPES and targets.is_cuda, "logits"
+    assert logits.dtype in _DTYPES, "logits"
     lddl = 0
     if dlogits is not None:
         assert dlogits.dtype == logits.dtype and dlogits.shape[0] == T, "dlogits"
-        lddl = _rows(dlogits, V, "dlogits")
+        lddl = _rows(dlogits, V, "dlogits", dev)
     handle = _stream(stream)
     ws = workspace if workspace is not None else pool.policy_workspace(T, seg.num_segments, 0, stream, handle)
     _used_on(stream, stats)
     hp = marlaas_policy_loss_t(clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale)
     _check(load_library().marlaas_policy_loss(
-        pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES[logits.dtype], _i32(targets, T, "targets"),
-        seg.ref, _f32(old_logp, T, "old_logp"), None if ref_logp is None else _f32(ref_logp, T, "ref_logp"),
-        _f32(adv, T, "adv"), _f32(weight, T, "weight"), ctypes.byref(hp), None if dlogits is None else dlogits.data_ptr(), lddl,
-        None if logp is None else _f32(logp, T, "logp"), _f32(stats, (pool.capacity + 1) * MARLAAS_POLICY_STATS, "stats"),
+        pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits", dev), _DTYPES[logits.dtype], _i32(targets, T, "targets", dev),
+        seg.ref, _f32(old_logp, T, "old_logp", dev), None if ref_logp is None else _f32(ref_logp, T, "ref_logp", dev),
+        _f32(adv, T, "adv", dev), _f32(weight, T, "weight", dev), ctypes.byref(hp), None if dlogits is None else dlogits.data_ptr(), lddl,
+        None if logp is None else _f32(logp, T, "logp", dev), _f32(stats, (pool.capacity + 1) * MARLAAS_POLICY_STATS, "stats", dev),
         ws.data_ptr(), ws.numel(), flags | seg.flags, handle))
     return stats
 
@@ -695,12 +695,12 @@ def marlaas_adamw_compact_state_export(pool: AdapterPool, state: torch.Tensor, m
                                        v: Optional[torch.Tensor] = None, stream=None):
     """fp32 (m, v) that the blocks of `state` stand for (256 elements per block, those past a matrix's end are 0)."""
     assert state.dtype == torch.uint8 and state.is_contiguous() and state.numel() % 528 == 0 and state.device == pool.device
-    blocks = state.numel() // 528
+    blocks, dev = state.numel() // 528, pool.index
     if m is None:
         m = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
     if v is None:
         v = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
     _used_on(stream, m, v)
-    _check(load_library().marlaas_adamw_compact_state_export(pool.handle, blocks, state.data_ptr(), _f32(m, 256 * blocks, "m"),
-                                                             _f32(v, 256 * blocks, "v"), _stream(stream)))
+    _check(load_library().marlaas_adamw_compact_state_export(pool.handle, blocks, state.data_ptr(), _f32(m, 256 * blocks, "m", dev),
+                                                             _f32(v, 256 * blocks, "v", dev), _stream(stream)))
     return m, v

@@ -324,16 +324,22 @@ __global__ void __launch_bounds__(STATS_THREADS) k_policy_stats(int T, int S, in
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // launched while the rows kernel runs: the tables are there, the terms are not
     const bool cached = S < STATS_OFFSETS;
+    bool mine = b == cap;           // (tokens that an ill-formed table leaves out count there)
     for (int s = tid; s < S; s += STATS_THREADS) {
         const int x = seg_offsets[s], y = seg_offsets[s + 1], t = seg_slot[s];
         if (cached) s_off[s] = x;
+        mine |= t == b;
         if (b == 0) {
             if (y < x || x < 0 || y > T || (s == 0 && x != 0) || (s == S - 1 && y != T)) policy_report(status, DEV_BAD_TABLE, s);
             if (t < -1 || t >= cap) policy_report(status, DEV_BAD_INDEX, s);
         }
     }
-    __syncthreads();
+    const bool any = __syncthreads_or(mine) != 0;
     sm100::dk_wait_prerequisites();
+    if (!any) {
+        if (tid < MARLAAS_POLICY_STATS && !accumulate) stats[(size_t)b * MARLAAS_POLICY_STATS + tid] = 0.f;
+        return;
+    }
     const int32_t* off = cached ? s_off : seg_offsets;
     float v[MARLAAS_POLICY_STATS] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int64_t i = tid; i < T; i += STATS_THREADS) {
@@ -419,8 +425,8 @@ static marlaas_status_t check_logits(const char* fn, const marlaas_pool* pool, i
     if (V < 1 || V > MARLAAS_MAX_VOCABULARY)
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: V = %lld outside [1, %d]", fn, (long long)V, (int)MARLAAS_MAX_VOCABULARY);
     if (dtype != MARLAAS_DTYPE_BF16 && dtype != MARLAAS_DTYPE_F32) return fail(MARLAAS_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, (int)dtype);
-    if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature))
-        return fail(MARLAAS_ERR_INVALID_ARG, "%s: inv_temperature must be positive and finite", fn);
+    if (!(inv_temperature > 0.f) || !std::isfinite(2.f * inv_temperature))       // (it is scaled by 1 / ln 2)
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: inv_temperature must be positive, finite and below 1.7e38", fn);
     if (T == 0) return MARLAAS_OK;
     if (!targets || misaligned(targets, 4)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: targets is NULL or misaligned", fn);
     return check_rows(fn, "logits", logits, ld, V, dtype);

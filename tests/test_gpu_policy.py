@@ -417,6 +417,25 @@ def test_more_rows_than_the_device_holds_at_once(pool, T, V, dtype):
     assert stats[[2, 0], 7].sum().item() == (tgt >= 0).sum().item()
 
 
+def test_stats_of_many_tenants_and_a_single_row_of_any_stride(pool):
+    many = B.AdapterPool(64, 64, 1, 700)
+    T, V = 200, 72
+    z = torch.randn(T, V, device="cuda")
+    slot = torch.randint(-1, 700, (T,)).tolist()
+    one = torch.ones(T, device="cuda")
+    stats = torch.full((701, 8), 5.0, device="cuda")
+    B.marlaas_policy_loss(many, z, dev(np.zeros(T), torch.int32), segments(list(range(T + 1)), slot), one * -4, one, one, stats=stats)
+    want = np.bincount([s if s >= 0 else 700 for s in slot], minlength=701)
+    assert np.array_equal(stats[:, 7].cpu().numpy(), want) and torch.all(stats[torch.from_numpy(want == 0)] == 0)
+    more = stats.clone()
+    B.marlaas_policy_loss(many, z, dev(np.zeros(T), torch.int32), segments(list(range(T + 1)), slot), one * -4, one, one, stats=more,
+                          flags=B.MARLAAS_FLAG_ACCUMULATE)
+    assert torch.equal(more, 2 * stats)
+    row = torch.randn(3 * 85, device="cuda").as_strided((1, V), (85, 1))
+    logp = B.marlaas_token_logprobs(pool, row, dev(np.full(1, 7), torch.int32))
+    logp_close(logp, torch.log_softmax(row.double(), 1)[:, 7].cpu().numpy(), "logp")
+
+
 @pytest.mark.parametrize("T,V", [(500, 40003), (600, 100), (3, 100)])
 def test_batches_without_a_row_to_read(pool, T, V):
     z = torch.full((T, -(-V // 8) * 8), math.nan, dtype=torch.bfloat16, device="cuda")[:, :V]
@@ -480,7 +499,7 @@ def test_row_calls_refuse(pool):
         assert e.value.status == status, e.value
 
     inv = B.MARLAAS_ERR_INVALID_ARG
-    for bad in (0.0, -1.0, INF, math.nan):
+    for bad in (0.0, -1.0, INF, math.nan, 3e38):
         refused(inv, B.marlaas_token_logprobs, z, t, inv_temperature=bad)
         refused(inv, B.marlaas_policy_loss, z, t, seg, f, f, f, inv_temperature=bad)
     refused(inv, B.marlaas_token_logprobs, z[:, 1:], t)                             # rows off their 16-byte boundary
@@ -500,8 +519,12 @@ def test_row_calls_refuse(pool):
     for bad in (t.long(), t[:3], t[::2]):
         with pytest.raises(AssertionError):
             B.marlaas_token_logprobs(pool, z, bad)
-    with pytest.raises(AssertionError):
-        B.marlaas_token_logprobs(pool, z.half(), t)
+    for args in ((z.half(), t), (z.cpu(), t), (z, t.cpu())):
+        with pytest.raises(AssertionError):
+            B.marlaas_token_logprobs(pool, *args)
+    for k in range(3):
+        with pytest.raises(AssertionError):
+            B.marlaas_policy_loss(pool, z, t, seg, *[f.cpu() if i == k else f for i in range(3)])
     assert B.marlaas_kernel_launch_count() == n0
     # a target past the vocabulary: reported, its row ignored
     t[2] = 64
