@@ -364,8 +364,11 @@ marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V,
  * moments.  The update is done in fp32 on the decoded moments; the new moments are rounded stochastically with 16 random
  * bits each, so that their expected value is kept (at beta2 = 0.999 a moment moves by a thousandth per step, a hundredth of
  * what rounding to nearest would need to move it at all): a moment below the block's range becomes 0, except that a
- * positive v stays at the smallest code.  A moment that is not finite is stored as 0 (the master then holds a NaN or an
- * infinity).  The random bits depend on seed, hp->step, the tenant id, the matrix and the element's index alone: the same
+ * positive v stays at the smallest code.  A moment that is not finite is stored as 0.  If the gradient itself was not finite,
+ * the master then holds a NaN or an infinity.  If only its square left fp32's range (from about 6e20 at beta2 = 0.999), the
+ * step leaves the master as it is but for the weight decay, and the next one starts both moments of the element anew from 0:
+ * a step reads the m of an element whose v is 0 as 0 in blocks with E_m >= 127, where nothing else leaves the two like that
+ * (the export gives the codes' values as they are).  The random bits depend on seed, hp->step, the tenant id, the matrix and the element's index alone: the same
  * call gives the same bits.
  * state_A[i] / state_B[i]: the tenant's state for A [d_in][rank] and B [rank][d_out]; on a pool over several projections,
  * the projections' states one after another, each of marlaas_adamw_compact_state_bytes of its own elements.

@@ -132,6 +132,14 @@ def decode_state(state, n):
     return m[:n], v[:n]
 
 
+def held_moments(state, n):
+    """(m, v) that a step starts from.  A v of 0 in a block with an m of 1 or more stands for a square that has left fp32's
+    range (a positive v never becomes 0): both start anew from 0."""
+    m, v = decode_state(state, n)
+    large = np.repeat(np.asarray(state, dtype=np.uint8).reshape(-1, STATE_BLOCK)[:, 512] >= 127, BLOCK)[:n]
+    return np.where((v == 0) & large, 0.0, m), v
+
+
 def encode_state(m, v, bits):
     """The state that stands for the moments rounded with the given random bits."""
     n = len(m)
@@ -169,7 +177,7 @@ def adamw_compact_step(theta, grad, state, bits, lr, beta1, beta2, eps, weight_d
     """(theta, m, v, state) after a step; m, v are the new moments before they are rounded into the state."""
     n = len(theta)
     f = lambda x: float(np.float32(x))      # noqa: E731 - the call's fp32 hyper-parameters
-    m, v = decode_state(state, n)
+    m, v = held_moments(state, n)
     g = f(grad_scale) * np.asarray(grad, dtype=np.float64)
     m = f(beta1) * m + (1 - f(beta1)) * g
     v = f(beta2) * v + (1 - f(beta2)) * g * g
