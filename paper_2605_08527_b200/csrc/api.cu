@@ -1,6 +1,7 @@
 // The exported layer calls: argument validation on the host, then the kernel sequence on the caller's stream.
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "internal.cuh"
@@ -82,7 +83,6 @@ marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_
     if (S > 0 && seg->seg_offsets[S] != T)
         return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: seg_offsets[S] = %d, expected T = %lld", fn,
                     seg->seg_offsets[S], (long long)T);
-    host_tok_slot->assign((size_t)T, -1);
     for (int32_t s = 0; s < S; ++s) {
         const int32_t a = seg->seg_offsets[s], b = seg->seg_offsets[s + 1];
         if (b < a) return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: seg_offsets decreases at segment %d", fn, s);
@@ -92,8 +92,11 @@ marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_
                         pool->cap);
         if (t >= 0 && !pool->slots[t].used)
             return fail(MARLAAS_ERR_UNKNOWN_TENANT, "%s: segment %d names slot %d, which holds no adapter", fn, s, t);
-        for (int32_t i = a; i < b; ++i) (*host_tok_slot)[i] = t;
     }
+    // the offsets run from 0 to T without a decrease: all inside [0, T]
+    host_tok_slot->assign((size_t)T, -1);
+    for (int32_t s = 0; s < S; ++s)
+        std::fill(host_tok_slot->begin() + seg->seg_offsets[s], host_tok_slot->begin() + seg->seg_offsets[s + 1], seg->seg_slot[s]);
     return MARLAAS_OK;
 }
 
