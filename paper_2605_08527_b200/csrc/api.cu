@@ -66,8 +66,8 @@ static marlaas_status_t check_matrix(const char* fn, const char* name, const voi
     return MARLAAS_OK;
 }
 
-// Validates the table argument; for host tables also validates the contents and expands them into
-// host_tok_slot (so that nothing is launched for a malformed table).
+// Validates the table argument; for host tables also validates the contents and, if host_tok_slot is not NULL, expands them
+// into it (so that nothing is launched for a malformed table).
 marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
                                 uint32_t flags, std::vector<int32_t>* host_tok_slot) {
     if (!seg) return fail(MARLAAS_ERR_INVALID_ARG, "%s: segment table is NULL", fn);
@@ -93,6 +93,7 @@ marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_
         if (t >= 0 && !pool->slots[t].used)
             return fail(MARLAAS_ERR_UNKNOWN_TENANT, "%s: segment %d names slot %d, which holds no adapter", fn, s, t);
     }
+    if (!host_tok_slot) return MARLAAS_OK;
     // the offsets run from 0 to T without a decrease: all inside [0, T]
     host_tok_slot->assign((size_t)T, -1);
     for (int32_t s = 0; s < S; ++s)

@@ -3,7 +3,9 @@
 // logits are in vocab_rows.cu.
 #include <string.h>
 
+#include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "sm100_cluster.cuh"
 
@@ -368,10 +370,17 @@ __global__ void __launch_bounds__(STATS_THREADS) k_policy_stats(int T, int S, in
     }
 }
 
+// Segment and group tables on the device.
+struct PolicyTables {
+    const int32_t* off;
+    const int32_t* slot;
+    const int32_t* group_off;
+};
+
 // Workspace of the two calls that need one.
 struct PolicyWorkspace {
     PolicyTerms* terms;     // [T]
-    int32_t* off;           // [S + 1] host tables, staged
+    int32_t* off;           // [S + 1] host tables, staged by one copy
     int32_t* slot;          // [S]
     int32_t* group_off;     // [G + 1]
     int32_t* count;         // [S]
@@ -395,14 +404,19 @@ static PolicyWorkspace carve_policy(const marlaas_pool* pool, int64_t T, int32_t
     return w;
 }
 
-// Host tables into the workspace (pageable sources: the runtime stages them before it returns).
-static marlaas_status_t stage_segments(const marlaas_segments_t* seg, const PolicyWorkspace& ws, const int32_t** off,
-                                       const int32_t** slot, cudaStream_t st) {
+// Host tables into the workspace, whose arrays for them lie one after another, by one copy.  Its source is a vector of the
+// call's own: pageable, so the runtime has staged it when the copy returns, and the caller's tables may be page-locked memory that
+// is written again after the call.
+static marlaas_status_t stage_tables(const marlaas_segments_t* seg, int32_t num_groups, const int32_t* group_offsets,
+                                     const PolicyWorkspace& ws, PolicyTables* t, cudaStream_t st) {
     const size_t S = (size_t)seg->num_segments;
-    MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.off, seg->seg_offsets, sizeof(int32_t) * (S + 1), cudaMemcpyHostToDevice, st));
-    MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.slot, seg->seg_slot, sizeof(int32_t) * S, cudaMemcpyHostToDevice, st));
-    *off = ws.off;
-    *slot = ws.slot;
+    const int32_t* end = group_offsets ? ws.group_off + num_groups + 1 : ws.slot + S;
+    std::vector<int32_t> copy((size_t)(end - ws.off));
+    std::copy(seg->seg_offsets, seg->seg_offsets + S + 1, copy.begin());
+    std::copy(seg->seg_slot, seg->seg_slot + S, copy.begin() + (ws.slot - ws.off));
+    if (group_offsets) std::copy(group_offsets, group_offsets + num_groups + 1, copy.begin() + (ws.group_off - ws.off));
+    MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.off, copy.data(), sizeof(int32_t) * copy.size(), cudaMemcpyHostToDevice, st));
+    *t = PolicyTables{ws.off, ws.slot, ws.group_off};
     return MARLAAS_OK;
 }
 
@@ -453,8 +467,7 @@ marlaas_status_t marlaas_group_advantages(marlaas_pool_t* pool, int64_t T, const
     if (flags & ~(uint32_t)(MARLAAS_FLAG_HOST_TABLE | MARLAAS_FLAG_VALIDATE_SYNC | MARLAAS_FLAG_TOKEN_MEAN | MARLAAS_FLAG_NO_STD))
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: a flag does not apply to this call", fn);
     if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: eps must be finite and not negative", fn);
-    std::vector<int32_t> host_ts;
-    marlaas_status_t rc = check_segments(fn, pool, T, seg, flags, &host_ts);
+    marlaas_status_t rc = check_segments(fn, pool, T, seg, flags, nullptr);
     if (rc != MARLAAS_OK) return rc;
     const int32_t S = seg->num_segments;
     if (num_groups < 0) return fail(MARLAAS_ERR_INVALID_ARG, "%s: negative group count", fn);
@@ -483,13 +496,9 @@ marlaas_status_t marlaas_group_advantages(marlaas_pool_t* pool, int64_t T, const
     if ((rc = reject_host_table_in_capture(fn, flags, st)) != MARLAAS_OK) return rc;
     AdvArgs a;
     a.T = (int)T; a.S = S; a.G = num_groups; a.cap = pool->cap;
-    a.off = seg->seg_offsets; a.slot = seg->seg_slot; a.group_off = group_offsets;
-    if (host) {
-        if ((rc = stage_segments(seg, ws, &a.off, &a.slot, st)) != MARLAAS_OK) return rc;
-        MARLAAS_CUDA_TRY(cudaMemcpyAsync(ws.group_off, group_offsets, sizeof(int32_t) * ((size_t)num_groups + 1),
-                                         cudaMemcpyHostToDevice, st));
-        a.group_off = ws.group_off;
-    }
+    PolicyTables t = {seg->seg_offsets, seg->seg_slot, group_offsets};
+    if (host && (rc = stage_tables(seg, num_groups, group_offsets, ws, &t, st)) != MARLAAS_OK) return rc;
+    a.off = t.off; a.slot = t.slot; a.group_off = t.group_off;
     a.targets = targets; a.rewards = rewards; a.eps = eps;
     a.token_mean = (flags & MARLAAS_FLAG_TOKEN_MEAN) != 0; a.no_std = (flags & MARLAAS_FLAG_NO_STD) != 0;
     a.seq_adv = seq_adv ? seq_adv : ws.seq_adv;
@@ -538,8 +547,7 @@ marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V,
     if (!stats || misaligned(stats, 4) || misaligned(logp, 4)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: stats is NULL or an output is misaligned", fn);
     if (logp && (logp == old_logp || logp == ref_logp || logp == adv || logp == weight))
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: logp must not be one of the inputs", fn);
-    std::vector<int32_t> host_ts;
-    if ((rc = check_segments(fn, pool, T, seg, flags, &host_ts)) != MARLAAS_OK) return rc;
+    if ((rc = check_segments(fn, pool, T, seg, flags, nullptr)) != MARLAAS_OK) return rc;
     const bool accumulate = (flags & MARLAAS_FLAG_ACCUMULATE) != 0;
     PolicyWorkspace ws;
     memset(&ws, 0, sizeof(ws));
@@ -563,9 +571,9 @@ marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V,
     cudaStream_t st = (cudaStream_t)cuda_stream;
     MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
     if ((rc = reject_host_table_in_capture(fn, flags, st)) != MARLAAS_OK) return rc;
-    const int32_t *off = seg->seg_offsets, *slot = seg->seg_slot;
+    PolicyTables t = {seg->seg_offsets, seg->seg_slot, nullptr};
     if (T > 0) {
-        if ((flags & MARLAAS_FLAG_HOST_TABLE) && (rc = stage_segments(seg, ws, &off, &slot, st)) != MARLAAS_OK) return rc;
+        if ((flags & MARLAAS_FLAG_HOST_TABLE) && (rc = stage_tables(seg, 0, nullptr, ws, &t, st)) != MARLAAS_OK) return rc;
         VocabRows r;
         memset(&r, 0, sizeof(r));
         r.T = T; r.V = V; r.logits = logits; r.ld = ld; r.f32 = dtype == MARLAAS_DTYPE_F32;
@@ -585,7 +593,7 @@ marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V,
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_policy_stats, (int)T, T > 0 ? (int)seg->num_segments : 0, (int)pool->cap, off, slot,
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_policy_stats, (int)T, T > 0 ? (int)seg->num_segments : 0, (int)pool->cap, t.off, t.slot,
                                         (const PolicyTerms*)ws.terms, stats, (int)accumulate, pool->d_status));
     MARLAAS_LAUNCH_CHECK("k_policy_stats");
     return finish(pool, flags, st);
