@@ -179,6 +179,12 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
+def _is_capturing(stream) -> bool:
+    """Whether the stream that a call was given to run on is being captured into a graph."""
+    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _used_on(stream, *tensors) -> None:
     """Tells torch's allocator of the stream that a call was given to run on, for tensors that were allocated for the call
     on the current stream."""
@@ -267,6 +273,7 @@ class AdapterPool:
         self.handle = h
         self.rank_stride = int(L.marlaas_adapter_pool_rank_stride(h))
         self._workspaces = {}
+        self._captured_workspaces = []
         self._policy_last = None
         self._store = None
 
@@ -281,18 +288,27 @@ class AdapterPool:
         except Exception:
             pass
 
-    def workspace(self, T: int) -> torch.Tensor:
-        """A cached workspace tensor large enough for T tokens (one per pool; not for overlapping calls)."""
+    def workspace(self, T: int, stream=None) -> torch.Tensor:
+        """A cached workspace tensor large enough for T tokens (one per pool; not for overlapping calls, and so not for graphs
+        that run at the same time).  A buffer that a captured call was given stays as long as the pool, since its graph goes on
+        using it when a larger batch has replaced it here."""
         need = marlaas_lora_workspace_bytes(self, T)
         ws = self._workspaces.get("ws")
         if ws is None or ws.numel() < need:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             self._workspaces["ws"] = ws
+        if (torch._C._cuda_isCurrentStreamCapturing() if stream is None else _is_capturing(stream)) and not any(ws is w for w in self._captured_workspaces):
+            self._captured_workspaces.append(ws)
         return ws
 
     def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0, stream=None, handle=None) -> torch.Tensor:
-        """A cached workspace tensor for marlaas_group_advantages and marlaas_policy_loss, one per stream (`handle`: what
-        _stream(stream) gives, if it is known)."""
+        """A workspace tensor for marlaas_group_advantages and marlaas_policy_loss, cached per stream (`handle`: what
+        _stream(stream) gives, if it is known).  A call that is being captured gets one of its own from the graph's memory, as
+        torch's own operations get theirs; a capture that torch.cuda.graph does not make has to pass a workspace."""
+        if torch._C._cuda_isCurrentStreamCapturing() if stream is None else _is_capturing(stream):
+            ws = torch.empty(max(marlaas_policy_workspace_bytes(self, T, num_segments, num_groups), 256), dtype=torch.uint8, device=self.device)
+            _used_on(stream, ws)
+            return ws
         key = (T, num_segments, num_groups, (handle or _stream(stream)).value)
         last = self._policy_last
         if last is not None and last[0] == key:
@@ -417,7 +433,7 @@ def marlaas_lora_forward(pool: AdapterPool, x: torch.Tensor, W: torch.Tensor, se
     T = x.shape[0]
     if y is None:
         y = torch.empty((T, pool.d_out), dtype=torch.bfloat16, device=x.device)
-    ws = workspace if workspace is not None else pool.workspace(T)
+    ws = workspace if workspace is not None else pool.workspace(T, stream)
     ldx, ldw, ldy = _mat(x, pool.d_in, "x"), _mat(W, pool.d_out, "W"), _mat(y, pool.d_out, "y")
     assert W.shape[0] == pool.d_in
     if h_save is not None:
@@ -497,7 +513,7 @@ def marlaas_lora_backward(pool: AdapterPool, x: torch.Tensor, W: torch.Tensor, d
                           h_saved: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                           flags: int = 0, stream=None) -> None:
     T = dy.shape[0]
-    ws = workspace if workspace is not None else pool.workspace(T)
+    ws = workspace if workspace is not None else pool.workspace(T, stream)
     ldx = _mat(x, pool.d_in, "x") if x is not None else 0
     ldw, lddy = _mat(W, pool.d_out, "W"), _mat(dy, pool.d_out, "dy")
     lddx = _mat(dx, pool.d_in, "dx") if dx is not None else 0
@@ -514,7 +530,7 @@ def marlaas_lora_build_index(pool: AdapterPool, T: int, seg: Segments, workspace
     slot_count = torch.empty(pool.capacity + 1, dtype=torch.int32, device=dev)
     slot_offset = torch.empty(pool.capacity + 2, dtype=torch.int32, device=dev)
     perm = torch.empty(max(T, 1), dtype=torch.int32, device=dev)
-    ws = workspace if workspace is not None else pool.workspace(T)
+    ws = workspace if workspace is not None else pool.workspace(T, stream)
     _check(load_library().marlaas_lora_build_index(pool.handle, T, ctypes.byref(seg.c), _dptr(tok_slot),
                                                    _dptr(slot_count), _dptr(slot_offset), _dptr(perm), _dptr(ws),
                                                    ws.numel(), flags | seg.flags, _stream(stream)))
@@ -684,7 +700,8 @@ def marlaas_adapter_pool_adamw_compact_commit(pool: AdapterPool, tables: Compact
                                               grad_scale: float = 1.0, step: int = 1, seed: int = 0,
                                               new_versions: Optional[Sequence[int]] = None, stream=None) -> None:
     """AdamW with 8-bit moments on the masters of the listed tenants, and commit of their bf16 rounding into the pool.
-    A tenant whose rank has changed since the tables were made is refused."""
+    A tenant whose rank has changed since the tables were made is refused.  A captured commit repeats its step number, rates and
+    random bits at every replay, and raises the version once, when it is captured."""
     vers = None if new_versions is None else (ctypes.c_uint64 * max(tables.n, 1))(*new_versions)
     hp = marlaas_adamw_t(lr, beta1, beta2, eps, weight_decay, grad_scale, step)
     _check(load_library().marlaas_adapter_pool_adamw_compact_commit(pool.handle, tables.n, tables.ids, vers, *tables.tables,
