@@ -342,8 +342,8 @@ marlaas_status_t marlaas_token_logprobs(marlaas_pool_t* pool, int64_t T, int64_t
  * gradient is 0.  ref_logp may be NULL if kl_coef is 0.
  * stats: fp32 [capacity + 1][MARLAAS_POLICY_STATS], per slot (last row: slot -1) the sums over its tokens of
  *     w (pg + kl_coef kl - entropy_coef H), w pg, w kl, w H, w ratio, w [clipped], w, 1
- * (with weights that sum to 1, the first six are the tenant's means); written, or added to with MARLAAS_FLAG_ACCUMULATE,
- * in a fixed order of the sums.  A token of an ill-formed device table counts as slot -1 and is reported. */
+ * (with weights that sum to 1, the first six are the tenant's means; w kl is 0 without ref_logp, and filled with it also if
+ * kl_coef is 0); written, or added to with MARLAAS_FLAG_ACCUMULATE, in a fixed order of the sums.  A token of an ill-formed device table counts as slot -1 and is reported. */
 typedef struct marlaas_policy_loss {
     float clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale;
 } marlaas_policy_loss_t;

@@ -86,14 +86,17 @@ __device__ __forceinline__ RowGrad token_terms(const VocabRows& a, const TokenIn
     const float clipped = A == 0.f ? 0.f : fminf(fmaxf(ratio, 1.f - a.clip_low), 1.f + a.clip_high) * A;
     const bool is_clipped = plain > clipped;      // (a NaN counts as not clipped and shows in the loss)
     const float pg = -(is_clipped ? clipped : plain);
-    float c = is_clipped ? 0.f : -plain, kl = 0.f;
-    if (a.kl_coef != 0.f) {
+    float c = is_clipped ? 0.f : -plain, kl = 0.f, reg = pg;
+    if (a.ref_logp) {       // the column is filled also where the loss has no such term
         const float d = in.ref - logp, e1 = expm1f(d);     // exp(d) - d - 1 without its cancellation for small d
         kl = d > 80.f ? e1 : e1 - d;        // (both may be infinite)
-        c = fmaf(-a.kl_coef, e1, c);
+        if (a.kl_coef != 0.f) {
+            c = fmaf(-a.kl_coef, e1, c);
+            reg = fmaf(a.kl_coef, kl, pg);
+        }
     }
     PolicyTerms t;
-    t.loss = w * fmaf(-a.entropy_coef, H, fmaf(a.kl_coef, kl, pg));
+    t.loss = w * fmaf(-a.entropy_coef, H, reg);
     t.pg = w * pg; t.kl = w * kl; t.entropy = w * H; t.ratio = w * ratio;
     t.clipped = is_clipped ? w : 0.f;
     t.weight = w;
