@@ -96,7 +96,7 @@ enum {
  * recur in any number of non-adjacent segments.  An unsorted decode batch is T segments of one token.
  * The arrays are device memory unless MARLAAS_FLAG_HOST_TABLE is set. */
 typedef struct {
-    int32_t num_segments;       /* S >= 0 */
+    int32_t num_segments;       /* 0 <= S <= 2^30 */
     const int32_t* seg_offsets; /* [S+1] */
     const int32_t* seg_slot;    /* [S]   */
 } marlaas_segments_t;

@@ -71,7 +71,8 @@ static marlaas_status_t check_matrix(const char* fn, const char* name, const voi
 marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
                                 uint32_t flags, std::vector<int32_t>* host_tok_slot) {
     if (!seg) return fail(MARLAAS_ERR_INVALID_ARG, "%s: segment table is NULL", fn);
-    if (seg->num_segments < 0) return fail(MARLAAS_ERR_INVALID_ARG, "%s: negative segment count", fn);
+    if (seg->num_segments < 0 || seg->num_segments > MAX_SEGMENTS)
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: segment count outside [0, %d]", fn, (int)MAX_SEGMENTS);
     if (T > 0 && (seg->num_segments == 0 || !seg->seg_offsets || !seg->seg_slot))
         return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: empty segment table for %lld tokens", fn, (long long)T);
     if (!(flags & MARLAAS_FLAG_HOST_TABLE)) return MARLAAS_OK;

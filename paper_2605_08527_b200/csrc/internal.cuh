@@ -144,6 +144,7 @@ struct Workspace {
 Workspace carve_workspace(const marlaas_pool* pool, int64_t T, void* base);
 
 // ---- argument checks and table staging (api.cu), shared by the exported calls -------------------------
+constexpr int32_t MAX_SEGMENTS = 1 << 30;      // of a batch, and groups: the kernels' 32-bit steps and bisections over them stay in range
 marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
                                 uint32_t flags, std::vector<int32_t>* host_tok_slot);
 marlaas_status_t reject_host_table_in_capture(const char* fn, uint32_t flags, cudaStream_t st);

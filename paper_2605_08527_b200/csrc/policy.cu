@@ -65,8 +65,8 @@ __device__ __forceinline__ int count_active(const int32_t* targets, int lo, int 
         const int4 t = w[i];
         n += (t.x >= 0) + (t.y >= 0) + (t.z >= 0) + (t.w >= 0);
     }
-    const int last = mid + 4 * words + lane;
-    if (last < hi) n += targets[last] >= 0;
+    const int tail = mid + 4 * words;       // (compared with what is left: tail + lane may pass 2^31)
+    if (lane < hi - tail) n += targets[tail + lane] >= 0;
     return n;
 }
 __device__ __forceinline__ int warp_total(int n) { return __reduce_add_sync(0xffffffffu, n); }
@@ -453,7 +453,8 @@ using namespace marlaas;
 extern "C" {
 
 size_t marlaas_policy_workspace_bytes(const marlaas_pool_t* pool, int64_t T, int32_t num_segments, int32_t num_groups) {
-    if (!pool || T < 0 || T >= (1ll << 31) || num_segments < 0 || num_groups < 0) return 0;
+    if (!pool || T < 0 || T >= (1ll << 31) || num_segments < 0 || num_segments > MAX_SEGMENTS || num_groups < 0 || num_groups > MAX_SEGMENTS)
+        return 0;
     return carve_policy(pool, T, num_segments, num_groups, nullptr).total_bytes;
 }
 
@@ -467,10 +468,11 @@ marlaas_status_t marlaas_group_advantages(marlaas_pool_t* pool, int64_t T, const
     if (flags & ~(uint32_t)(MARLAAS_FLAG_HOST_TABLE | MARLAAS_FLAG_VALIDATE_SYNC | MARLAAS_FLAG_TOKEN_MEAN | MARLAAS_FLAG_NO_STD))
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: a flag does not apply to this call", fn);
     if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: eps must be finite and not negative", fn);
+    if (num_groups < 0 || num_groups > MAX_SEGMENTS)
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: group count outside [0, %d]", fn, (int)MAX_SEGMENTS);
     marlaas_status_t rc = check_segments(fn, pool, T, seg, flags, nullptr);
     if (rc != MARLAAS_OK) return rc;
     const int32_t S = seg->num_segments;
-    if (num_groups < 0) return fail(MARLAAS_ERR_INVALID_ARG, "%s: negative group count", fn);
     if (S > 0 && (num_groups == 0 || !group_offsets))
         return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: empty group table for %d sequences", fn, S);
     if (S > 0 && (!seg->seg_offsets || !seg->seg_slot)) return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "%s: segment arrays are NULL", fn);
