@@ -179,22 +179,23 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
-def _is_capturing(stream) -> bool:
-    """Whether the stream that a call was given to run on is being captured into a graph."""
-    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
-        return torch.cuda.is_current_stream_capturing()
-
-
-def _used_on(stream, *tensors) -> None:
-    """Tells torch's allocator of the stream that a call was given to run on, for tensors that were allocated for the call
-    on the current stream."""
-    if stream is None:
-        return
+def _on_stream(stream, call, *args, **kwargs):
+    """`call` with `stream` made the current one, so that what it allocates is memory of that stream: a block of the stream that
+    is current now may still be in use by work there.  What the call returns may be used, and let go, on either."""
+    before = torch.cuda.current_stream()
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream))
-    for t in tensors:
-        if t is not None:
+    with torch.cuda.stream(stream):
+        out = call(*args, **kwargs)
+    todo = [out]
+    while todo:
+        t = todo.pop()
+        if isinstance(t, (tuple, list)):
+            todo += t
+        elif t is not None:
             t.record_stream(stream)
+            t.record_stream(before)
+    return out
 
 
 def _dptr(t: Optional[torch.Tensor]) -> ctypes.c_void_p:
@@ -288,7 +289,7 @@ class AdapterPool:
         except Exception:
             pass
 
-    def workspace(self, T: int, stream=None) -> torch.Tensor:
+    def workspace(self, T: int) -> torch.Tensor:
         """A cached workspace tensor large enough for T tokens (one per pool; not for overlapping calls, and so not for graphs
         that run at the same time).  A buffer that a captured call was given stays as long as the pool, since its graph goes on
         using it when a larger batch has replaced it here."""
@@ -296,20 +297,22 @@ class AdapterPool:
         ws = self._workspaces.get("ws")
         if ws is None or ws.numel() < need:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-            self._workspaces["ws"] = ws
-        if (torch._C._cuda_isCurrentStreamCapturing() if stream is None else _is_capturing(stream)) and not any(ws is w for w in self._captured_workspaces):
+            self._workspaces["ws"], self._workspace_stream = ws, torch._C._cuda_getCurrentRawStream(self.index)
+        elif torch._C._cuda_getCurrentRawStream(self.index) != self._workspace_stream:
+            ws.record_stream(torch.cuda.current_stream(self.index))
+        if torch._C._cuda_isCurrentStreamCapturing() and not any(ws is w for w in self._captured_workspaces):
             self._captured_workspaces.append(ws)
         return ws
 
     def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0, stream=None, handle=None) -> torch.Tensor:
         """A workspace tensor for marlaas_group_advantages and marlaas_policy_loss, cached per stream (`handle`: what
-        _stream(stream) gives, if it is known).  A call that is being captured gets one of its own from the graph's memory, as
+        _stream(None) gives, if it is known).  A call that is being captured gets one of its own from the graph's memory, as
         torch's own operations get theirs; a capture that torch.cuda.graph does not make has to pass a workspace."""
-        if torch._C._cuda_isCurrentStreamCapturing() if stream is None else _is_capturing(stream):
-            ws = torch.empty(max(marlaas_policy_workspace_bytes(self, T, num_segments, num_groups), 256), dtype=torch.uint8, device=self.device)
-            _used_on(stream, ws)
-            return ws
-        key = (T, num_segments, num_groups, (handle or _stream(stream)).value)
+        if stream is not None:
+            return _on_stream(stream, self.policy_workspace, T, num_segments, num_groups)
+        if torch._C._cuda_isCurrentStreamCapturing():
+            return torch.empty(max(marlaas_policy_workspace_bytes(self, T, num_segments, num_groups), 256), dtype=torch.uint8, device=self.device)
+        key = (T, num_segments, num_groups, (handle or _stream(None)).value)
         last = self._policy_last
         if last is not None and last[0] == key:
             return last[1]
@@ -318,7 +321,6 @@ class AdapterPool:
         ws = self._workspaces.get(where)
         if ws is None or ws.numel() < need:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-            _used_on(stream, ws)
             self._workspaces[where] = ws
         self._policy_last = (key, ws)
         return ws
@@ -397,6 +399,8 @@ def marlaas_adapter_pool_lookup(pool: AdapterPool, tenant_id: int):
 def marlaas_adapter_pool_export(pool: AdapterPool, slot: int, rank: int, stream=None):
     """The slot's adapter in the caller's layout; for a pool over several projections, two lists (one A and one B per
     projection)."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_adapter_pool_export, pool, slot, rank)
     A = torch.empty((pool.n_parts * pool.d_in, rank), dtype=torch.bfloat16, device=pool.device)
     B = torch.empty(rank * pool.d_out, dtype=torch.bfloat16, device=pool.device)
     _check(load_library().marlaas_adapter_pool_export(pool.handle, slot, _dptr(A), _dptr(B), _stream(stream)))
@@ -430,10 +434,12 @@ def _mat(t: torch.Tensor, cols: int, name: str):
 def marlaas_lora_forward(pool: AdapterPool, x: torch.Tensor, W: torch.Tensor, seg: Segments,
                          y: Optional[torch.Tensor] = None, h_save: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> torch.Tensor:
+    if stream is not None:
+        return _on_stream(stream, marlaas_lora_forward, pool, x, W, seg, y, h_save, workspace, flags)
     T = x.shape[0]
     if y is None:
         y = torch.empty((T, pool.d_out), dtype=torch.bfloat16, device=x.device)
-    ws = workspace if workspace is not None else pool.workspace(T, stream)
+    ws = workspace if workspace is not None else pool.workspace(T)
     ldx, ldw, ldy = _mat(x, pool.d_in, "x"), _mat(W, pool.d_out, "W"), _mat(y, pool.d_out, "y")
     assert W.shape[0] == pool.d_in
     if h_save is not None:
@@ -448,6 +454,8 @@ def marlaas_lora_forward_multi(calls, flags: int = 0, stream=None):
     """Independent forward calls as one (see marlaas.h): `calls` is a list of dicts with the keyword arguments of
     marlaas_lora_forward (pool, x, W, seg, and y / h_save / workspace, which must be distinct per call; missing y and
     workspace are allocated).  Returns the list of outputs."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_lora_forward_multi, calls, flags)
     n = len(calls)
     arr = (marlaas_forward_call_t * max(n, 1))()
     keep, ys = [], []
@@ -512,8 +520,10 @@ def marlaas_lora_backward(pool: AdapterPool, x: torch.Tensor, W: torch.Tensor, d
                           dB: Optional[Sequence[Optional[torch.Tensor]]] = None,
                           h_saved: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                           flags: int = 0, stream=None) -> None:
+    if stream is not None:
+        return _on_stream(stream, marlaas_lora_backward, pool, x, W, dy, seg, dx, dA, dB, h_saved, workspace, flags)
     T = dy.shape[0]
-    ws = workspace if workspace is not None else pool.workspace(T, stream)
+    ws = workspace if workspace is not None else pool.workspace(T)
     ldx = _mat(x, pool.d_in, "x") if x is not None else 0
     ldw, lddy = _mat(W, pool.d_out, "W"), _mat(dy, pool.d_out, "dy")
     lddx = _mat(dx, pool.d_in, "dx") if dx is not None else 0
@@ -525,12 +535,14 @@ def marlaas_lora_backward(pool: AdapterPool, x: torch.Tensor, W: torch.Tensor, d
 
 def marlaas_lora_build_index(pool: AdapterPool, T: int, seg: Segments, workspace: Optional[torch.Tensor] = None,
                              flags: int = 0, stream=None):
+    if stream is not None:
+        return _on_stream(stream, marlaas_lora_build_index, pool, T, seg, workspace, flags)
     dev = pool.device
     tok_slot = torch.empty(max(T, 1), dtype=torch.int32, device=dev)
     slot_count = torch.empty(pool.capacity + 1, dtype=torch.int32, device=dev)
     slot_offset = torch.empty(pool.capacity + 2, dtype=torch.int32, device=dev)
     perm = torch.empty(max(T, 1), dtype=torch.int32, device=dev)
-    ws = workspace if workspace is not None else pool.workspace(T, stream)
+    ws = workspace if workspace is not None else pool.workspace(T)
     _check(load_library().marlaas_lora_build_index(pool.handle, T, ctypes.byref(seg.c), _dptr(tok_slot),
                                                    _dptr(slot_count), _dptr(slot_offset), _dptr(perm), _dptr(ws),
                                                    ws.numel(), flags | seg.flags, _stream(stream)))
@@ -589,6 +601,9 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
                              workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None):
     """(seq_adv [S], adv [T], weight [T]) of a batch whose sequences are the segments of `seg`; group_offsets lives where
     the segment table does.  Outputs that are not given are allocated."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_group_advantages, pool, seg, rewards, group_offsets, targets, eps=eps, seq_adv=seq_adv, adv=adv,
+                          weight=weight, workspace=workspace, flags=flags)
     T, S, G, dev = targets.numel(), seg.num_segments, group_offsets.numel() - 1, pool.index
     if seq_adv is None:
         seq_adv = rewards.new_empty(S)
@@ -596,9 +611,8 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
         adv = rewards.new_empty(T)
     if weight is None:
         weight = rewards.new_empty(T)
-    handle = _stream(stream)
-    ws = workspace if workspace is not None else pool.policy_workspace(T, S, G, stream, handle)
-    _used_on(stream, seq_adv, adv, weight)
+    handle = _stream(None)
+    ws = workspace if workspace is not None else pool.policy_workspace(T, S, G, None, handle)
     _check(load_library().marlaas_group_advantages(
         pool.handle, T, seg.ref, _f32(rewards, S, "rewards", dev), G, _i32(group_offsets, G + 1, "group_offsets (where the segment table is)", -1 if seg.on_host else dev),
         _i32(targets, T, "targets", dev), eps, _f32(seq_adv, S, "seq_adv", dev), _f32(adv, T, "adv", dev), _f32(weight, T, "weight", dev),
@@ -610,16 +624,18 @@ def marlaas_token_logprobs(pool: AdapterPool, logits: torch.Tensor, targets: tor
                            logp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
                            with_entropy: bool = False, flags: int = 0, stream=None):
     """logp [T] of the targets (negative = ignored), and with `with_entropy` or `entropy` (logp, entropy)."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_token_logprobs, pool, logits, targets, inv_temperature=inv_temperature, logp=logp, entropy=entropy,
+                          with_entropy=with_entropy, flags=flags)
     (T, V), dev = logits.shape, pool.index
     if logp is None:
         logp = torch.empty(T, dtype=torch.float32, device=logits.device)
     if entropy is None and with_entropy:
         entropy = torch.empty(T, dtype=torch.float32, device=logits.device)
     assert logits.dtype in _DTYPES, "logits"
-    _used_on(stream, logp, entropy)
     _check(load_library().marlaas_token_logprobs(
         pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits", dev), _DTYPES[logits.dtype], _i32(targets, T, "targets", dev),
-        inv_temperature, _f32(logp, T, "logp", dev), None if entropy is None else _f32(entropy, T, "entropy", dev), flags, _stream(stream)))
+        inv_temperature, _f32(logp, T, "logp", dev), None if entropy is None else _f32(entropy, T, "entropy", dev), flags, _stream(None)))
     return logp if entropy is None else (logp, entropy)
 
 
@@ -631,6 +647,10 @@ def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.
                         workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> torch.Tensor:
     """Clipped policy loss with KL and entropy terms: returns stats [capacity + 1][8] (see marlaas.h; column 0 is the loss
     per slot) and writes its gradient by the logits to `dlogits` (which may be `logits` itself) if given."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_policy_loss, pool, logits, targets, seg, old_logp, adv, weight, ref_logp=ref_logp, dlogits=dlogits,
+                          logp=logp, stats=stats, clip_low=clip_low, clip_high=clip_high, kl_coef=kl_coef, entropy_coef=entropy_coef,
+                          inv_temperature=inv_temperature, grad_scale=grad_scale, workspace=workspace, flags=flags)
     (T, V), dev = logits.shape, pool.index
     if stats is None:
         assert not (flags & MARLAAS_FLAG_ACCUMULATE), "stats to add to"
@@ -640,9 +660,8 @@ def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.
     if dlogits is not None:
         assert dlogits.dtype == logits.dtype and dlogits.shape[0] == T, "dlogits"
         lddl = _rows(dlogits, V, "dlogits", dev)
-    handle = _stream(stream)
-    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.num_segments, 0, stream, handle)
-    _used_on(stream, stats)
+    handle = _stream(None)
+    ws = workspace if workspace is not None else pool.policy_workspace(T, seg.num_segments, 0, None, handle)
     hp = marlaas_policy_loss_t(clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale)
     _check(load_library().marlaas_policy_loss(
         pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits", dev), _DTYPES[logits.dtype], _i32(targets, T, "targets", dev),
@@ -711,13 +730,14 @@ def marlaas_adapter_pool_adamw_compact_commit(pool: AdapterPool, tables: Compact
 def marlaas_adamw_compact_state_export(pool: AdapterPool, state: torch.Tensor, m: Optional[torch.Tensor] = None,
                                        v: Optional[torch.Tensor] = None, stream=None):
     """fp32 (m, v) that the blocks of `state` stand for (256 elements per block, those past a matrix's end are 0)."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_adamw_compact_state_export, pool, state, m, v)
     assert state.dtype == torch.uint8 and state.is_contiguous() and state.numel() % 528 == 0 and state.device == pool.device
     blocks, dev = state.numel() // 528, pool.index
     if m is None:
         m = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
     if v is None:
         v = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
-    _used_on(stream, m, v)
     _check(load_library().marlaas_adamw_compact_state_export(pool.handle, blocks, state.data_ptr(), _f32(m, 256 * blocks, "m", dev),
-                                                             _f32(v, 256 * blocks, "v", dev), _stream(stream)))
+                                                             _f32(v, 256 * blocks, "v", dev), _stream(None)))
     return m, v
