@@ -408,11 +408,13 @@ static marlaas_status_t launch_compact(const marlaas_pool* pool, const CompactTe
     const double c1 = 1.0 / (1.0 - std::pow((double)hp.beta1, (double)hp.step)), c2 = 1.0 / (1.0 - std::pow((double)hp.beta2, (double)hp.step));
     a.h.b1 = hp.beta1; a.h.b2 = hp.beta2; a.h.one_b1 = 1.f - hp.beta1; a.h.one_b2 = 1.f - hp.beta2; a.h.gscale = hp.grad_scale;
     a.h.sqrt_c2 = (float)std::sqrt(c2); a.h.eps = hp.eps; a.h.lr_c1 = (float)(hp.lr * c1); a.h.lr_wd = hp.lr * hp.weight_decay;
-    // longer units spread a CTA's set-up over more elements (32 tenants of rank 32 over 4096 x 3 4096: 91 us against 120),
-    // shorter ones a small update over more SMs (4 tenants of rank 16 over 1024 x 1024: 9.2 us against 13.1)
+    // Longer units spread a CTA's set-up over more elements and overlap more loads with steps, shorter ones spread a small update
+    // over more SMs.  32 tenants of ranks 8 to 64, 32 and 16, us with short / long units: 0.5 M elements 6.3-8.3 / 10.1-10.3,
+    // 1 M 10.4-11.4 / 10.4-12.4, 2 M 14.5-14.9 / 13.1-16.5, 3 M 18.6-19.0 / 16.5-17.4, 5 M 26.8 / 24.6-24.9, 10 M 47-48 / 39-40,
+    // 25 M 107-113 / 84-85.  The change is at two long units per SM, 2.4 M elements.
     int64_t elems = 0;
     for (int i = 0; i < n; ++i) elems += t[i].rank * (pool->P * pool->K + pool->N);
-    a.unit = elems >= (int64_t)pool->sm_count * 8 * OC_UNIT * OC_LONG ? OC_UNIT * OC_LONG : OC_UNIT;
+    a.unit = elems >= (int64_t)pool->sm_count * 2 * OC_UNIT * OC_LONG ? OC_UNIT * OC_LONG : OC_UNIT;
     a.At = pool->d_At; a.Bs = pool->d_Bs;
     int64_t ctas = 0;
     size_t smem = 0;
