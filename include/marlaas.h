@@ -53,7 +53,8 @@ enum {
     MARLAAS_ERR_CUDA = -7,               /* a CUDA runtime / driver call failed */
     MARLAAS_ERR_DEVICE_TIMEOUT = -8,     /* a bounded wait inside a kernel ran out; results of that call are invalid */
     MARLAAS_ERR_DEVICE_BAD_INDEX = -9,   /* a device-side check met a slot outside [-1, capacity): that token was
-                                            computed with the base weight only */
+                                            computed with the base weight only; or, in a policy call, a target outside the
+                                            vocabulary: that row was ignored */
     MARLAAS_ERR_WORKSPACE_TOO_SMALL = -10
 };
 
@@ -343,7 +344,8 @@ marlaas_status_t marlaas_token_logprobs(marlaas_pool_t* pool, int64_t T, int64_t
  * stats: fp32 [capacity + 1][MARLAAS_POLICY_STATS], per slot (last row: slot -1) the sums over its tokens of
  *     w (pg + kl_coef kl - entropy_coef H), w pg, w kl, w H, w ratio, w [clipped], w, 1
  * (with weights that sum to 1, the first six are the tenant's means; w kl is 0 without ref_logp, and filled with it also if
- * kl_coef is 0); written, or added to with MARLAAS_FLAG_ACCUMULATE, in a fixed order of the sums.  A token of an ill-formed device table counts as slot -1 and is reported. */
+ * kl_coef is 0); written, or added to with MARLAAS_FLAG_ACCUMULATE, in a fixed order of the sums.  A token of an ill-formed
+ * device table counts as slot -1 and is reported. */
 typedef struct marlaas_policy_loss {
     float clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale;
 } marlaas_policy_loss_t;
@@ -368,8 +370,8 @@ marlaas_status_t marlaas_policy_loss(marlaas_pool_t* pool, int64_t T, int64_t V,
  * the master then holds a NaN or an infinity.  If only its square left fp32's range (from about 6e20 at beta2 = 0.999), the
  * step leaves the master as it is but for the weight decay, and the next one starts both moments of the element anew from 0:
  * a step reads the m of an element whose v is 0 as 0 in blocks with E_m >= 127, where nothing else leaves the two like that
- * (the export gives the codes' values as they are).  The random bits depend on seed, hp->step, the tenant id, the matrix and the element's index alone: the same
- * call gives the same bits.
+ * (the export gives the codes' values as they are).  The random bits depend on seed, hp->step, the tenant id, the matrix and
+ * the element's index alone: the same call gives the same bits.
  * state_A[i] / state_B[i]: the tenant's state for A [d_in][rank] and B [rank][d_out]; on a pool over several projections,
  * the projections' states one after another, each of marlaas_adamw_compact_state_bytes of its own elements.
  * ranks: HOST [n], the ranks that the buffers were made for, or NULL; a tenant whose adapter has another rank by now is

@@ -403,7 +403,7 @@ marlaas_status_t marlaas_check_status(marlaas_pool_t* pool, void* cuda_stream) {
         case DEV_BAD_TABLE:
             return fail(MARLAAS_ERR_BAD_SEGMENT_TABLE, "device check: malformed segment table (detail %d)", w[1]);
         case DEV_BAD_INDEX:
-            return fail(MARLAAS_ERR_DEVICE_BAD_INDEX, "device check: slot outside [-1, capacity) at token %d", w[1]);
+            return fail(MARLAAS_ERR_DEVICE_BAD_INDEX, "device check: slot outside [-1, capacity), or target outside the vocabulary, at token or segment %d", w[1]);
         case DEV_TIMEOUT:
             return fail(MARLAAS_ERR_DEVICE_TIMEOUT, "device check: a bounded wait ran out (site %d)", w[1]);
         default:

@@ -61,3 +61,11 @@ def test_more_segments_or_groups_than_can_be_counted_are_refused():
                                    B._stream(None))
         assert rc == B.MARLAAS_ERR_INVALID_ARG
     assert B.marlaas_kernel_launch_count() == n0
+
+
+def test_a_target_outside_the_vocabulary_is_named_as_that():
+    pool = B.AdapterPool(64, 64, 8, 2)
+    B.marlaas_token_logprobs(pool, torch.zeros((4, 8), device="cuda"), dev([0, 1, 8, 2], torch.int32))
+    with pytest.raises(B.MarlaasError, match="vocabulary.*2$") as e:
+        B.marlaas_check_status(pool)
+    assert e.value.status == B.MARLAAS_ERR_DEVICE_BAD_INDEX
