@@ -11,9 +11,7 @@
 
 namespace marlaas {
 
-__device__ __forceinline__ void policy_report(int32_t* status, int code, int detail) {
-    if (atomicCAS(status, 0, code) == 0) status[1] = detail;
-}
+using sm100::dk_report;
 
 // ---- group-relative advantages ----
 // Three steps: active tokens per sequence and advantages per group; totals per tenant (integer sums, so their order does not
@@ -23,7 +21,8 @@ __device__ __forceinline__ void policy_report(int32_t* status, int code, int det
 // kernel and expands in a second, each of whose CTAs forms the totals from the counts, and then every sequence's advantage
 // and weight, for itself in shared memory; for more sequences than fit that way a kernel between them forms the totals (with
 // 2000 sequences of 1000 tokens 15.1 us against 12.3).
-constexpr int ADV_THREADS = 256, ADV_EXPAND_THREADS = 512, ADV_SMALL_THREADS = 1024, ADV_SMALL_T = 4096, ADV_SMALL_S = 128, ADV_SHARED_S = 2048, ADV_RUN = 512;
+constexpr int ADV_THREADS = 256, ADV_EXPAND_THREADS = 512, ADV_SMALL_THREADS = 1024;
+constexpr int ADV_SMALL_T = 4096, ADV_SMALL_S = 128, ADV_SHARED_S = 2048, ADV_RUN = 512;
 
 struct AdvArgs {
     int T, S, G, cap;
@@ -51,8 +50,8 @@ __device__ __forceinline__ void seq_range(const AdvArgs& a, int s, int* lo, int*
 __device__ __forceinline__ int bucket_of(const AdvArgs& a, int slot) { return slot < 0 || slot >= a.cap ? a.cap : slot; }
 __device__ __forceinline__ void check_sequence(const AdvArgs& a, int s) {
     const int x = a.off[s], y = a.off[s + 1], t = a.slot[s];
-    if (y < x || x < 0 || y > a.T || (s == 0 && x != 0) || (s == a.S - 1 && y != a.T)) policy_report(a.status, DEV_BAD_TABLE, s);
-    if (t < -1 || t >= a.cap) policy_report(a.status, DEV_BAD_INDEX, s);
+    if (y < x || x < 0 || y > a.T || (s == 0 && x != 0) || (s == a.S - 1 && y != a.T)) dk_report(a.status, DEV_BAD_TABLE, s);
+    if (t < -1 || t >= a.cap) dk_report(a.status, DEV_BAD_INDEX, s);
 }
 // Active tokens among [lo, hi) that lane `lane` of `lanes` looks at: whole 16-byte words in the middle, single tokens around.
 __device__ __forceinline__ int count_active(const int32_t* targets, int lo, int hi, int lane, int lanes) {
@@ -75,7 +74,7 @@ __device__ __forceinline__ int warp_total(int n) { return __reduce_add_sync(0xff
 __device__ __forceinline__ void group_advantages(const AdvArgs& a, int g, int lane, float* seq_adv) {
     const int x = a.group_off[g], y = a.group_off[g + 1];
     if (lane == 0 && (y < x || x < 0 || y > a.S || (g == 0 && x != 0) || (g == a.G - 1 && y != a.S)))
-        policy_report(a.status, DEV_BAD_TABLE, -10 - g);
+        dk_report(a.status, DEV_BAD_TABLE, -10 - g);
     const int lo = min(max(x, 0), a.S), hi = min(max(y, lo), a.S);
     if (hi <= lo) return;
     // differences to the group's first reward: rewards that are all alike give exact zeros
@@ -332,8 +331,8 @@ __global__ void __launch_bounds__(STATS_THREADS) k_policy_stats(int T, int S, in
         if (cached) s_off[s] = x;
         mine |= t == b;
         if (b == 0) {
-            if (y < x || x < 0 || y > T || (s == 0 && x != 0) || (s == S - 1 && y != T)) policy_report(status, DEV_BAD_TABLE, s);
-            if (t < -1 || t >= cap) policy_report(status, DEV_BAD_INDEX, s);
+            if (y < x || x < 0 || y > T || (s == 0 && x != 0) || (s == S - 1 && y != T)) dk_report(status, DEV_BAD_TABLE, s);
+            if (t < -1 || t >= cap) dk_report(status, DEV_BAD_INDEX, s);
         }
     }
     const bool any = __syncthreads_or(mine) != 0;

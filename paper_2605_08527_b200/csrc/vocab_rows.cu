@@ -187,7 +187,7 @@ __device__ __forceinline__ bool row_read(const VocabRows& a, int32_t target, flo
 // Statistics of a warp's part of a row.  `done` is called when the slice has been read once; `again`: where it is read a second
 // time if it has to be (without a gradient its place in shared memory has been given up by then: from L2).
 struct WarpStats {
-    float m, s, u;          // the reference that the sums are relative to (-inf: no finite logit, and sums of 0), sum 2^t, sum t 2^t
+    float m, s, u;          // the reference that the sums are relative to (-inf: no finite logit, sums of 0), sum 2^t, sum t 2^t
 };
 template <bool F32, bool ENTROPY, int NT, typename Done>
 __device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const uint4* again, int nvec, float zt, int tid, float k2, Done done) {
@@ -601,8 +601,8 @@ static marlaas_status_t launch_rows(const marlaas_pool* pool, const VocabRows& r
 }
 
 // The shape of a launch, from the sizes alone (not from what is wanted of the rows, so that all calls on a batch sum in one
-// order, and products and sums are fused where the code says so, not as the compiler likes: the log-probabilities of marlaas_token_logprobs and of the loss are the same bits, and the ratios of an update's
-// first pass exactly 1).
+// order; and products and sums are fused where the code says so, not as the compiler likes): the log-probabilities of
+// marlaas_token_logprobs and of the loss are the same bits, and the ratios of an update's first pass exactly 1.
 template <bool F32, bool GRAD, bool ENTROPY, bool ENTROPY_GRAD>
 static marlaas_status_t launch_shape(const marlaas_pool* pool, const VocabRows& r, cudaStream_t st) {
     const int64_t vecs = cdiv(r.V, F32 ? 4 : 8);
