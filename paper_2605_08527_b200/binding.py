@@ -172,10 +172,14 @@ def _check(rc: int) -> None:
         raise MarlaasError(rc, load_library().marlaas_last_error().decode())
 
 
+def _current() -> int:
+    """The current device's current stream, without the Stream object (a few microseconds) that torch.cuda makes for it."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
-        # the current device's current stream, without the Stream object (a few microseconds) that torch.cuda makes for it
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+        return ctypes.c_void_p(_current())
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -306,13 +310,13 @@ class AdapterPool:
 
     def policy_workspace(self, T: int, num_segments: int, num_groups: int = 0, stream=None, handle=None) -> torch.Tensor:
         """A workspace tensor for marlaas_group_advantages and marlaas_policy_loss, cached per stream (`handle`: what
-        _stream(None) gives, if it is known).  A call that is being captured gets one of its own from the graph's memory, as
+        _current() gives, if it is known).  A call that is being captured gets one of its own from the graph's memory, as
         torch's own operations get theirs; a capture that torch.cuda.graph does not make has to pass a workspace."""
         if stream is not None:
             return _on_stream(stream, self.policy_workspace, T, num_segments, num_groups)
         if torch._C._cuda_isCurrentStreamCapturing():
             return torch.empty(max(marlaas_policy_workspace_bytes(self, T, num_segments, num_groups), 256), dtype=torch.uint8, device=self.device)
-        key = (T, num_segments, num_groups, (handle or _stream(None)).value)
+        key = (T, num_segments, num_groups, _current() if handle is None else handle)
         last = self._policy_last
         if last is not None and last[0] == key:
             return last[1]
@@ -611,7 +615,7 @@ def marlaas_group_advantages(pool: AdapterPool, seg: Segments, rewards: torch.Te
         adv = rewards.new_empty(T)
     if weight is None:
         weight = rewards.new_empty(T)
-    handle = _stream(None)
+    handle = _current()
     ws = workspace if workspace is not None else pool.policy_workspace(T, S, G, None, handle)
     _check(load_library().marlaas_group_advantages(
         pool.handle, T, seg.ref, _f32(rewards, S, "rewards", dev), G, _i32(group_offsets, G + 1, "group_offsets (where the segment table is)", -1 if seg.on_host else dev),
@@ -635,7 +639,7 @@ def marlaas_token_logprobs(pool: AdapterPool, logits: torch.Tensor, targets: tor
     assert logits.dtype in _DTYPES, "logits"
     _check(load_library().marlaas_token_logprobs(
         pool.handle, T, V, logits.data_ptr(), _rows(logits, V, "logits", dev), _DTYPES[logits.dtype], _i32(targets, T, "targets", dev),
-        inv_temperature, _f32(logp, T, "logp", dev), None if entropy is None else _f32(entropy, T, "entropy", dev), flags, _stream(None)))
+        inv_temperature, _f32(logp, T, "logp", dev), None if entropy is None else _f32(entropy, T, "entropy", dev), flags, _current()))
     return logp if entropy is None else (logp, entropy)
 
 
@@ -660,7 +664,7 @@ def marlaas_policy_loss(pool: AdapterPool, logits: torch.Tensor, targets: torch.
     if dlogits is not None:
         assert dlogits.dtype == logits.dtype and dlogits.shape[0] == T, "dlogits"
         lddl = _rows(dlogits, V, "dlogits", dev)
-    handle = _stream(None)
+    handle = _current()
     ws = workspace if workspace is not None else pool.policy_workspace(T, seg.num_segments, 0, None, handle)
     hp = marlaas_policy_loss_t(clip_low, clip_high, kl_coef, entropy_coef, inv_temperature, grad_scale)
     _check(load_library().marlaas_policy_loss(
@@ -739,5 +743,5 @@ def marlaas_adamw_compact_state_export(pool: AdapterPool, state: torch.Tensor, m
     if v is None:
         v = torch.empty(256 * blocks, dtype=torch.float32, device=pool.device)
     _check(load_library().marlaas_adamw_compact_state_export(pool.handle, blocks, state.data_ptr(), _f32(m, 256 * blocks, "m", dev),
-                                                             _f32(v, 256 * blocks, "v", dev), _stream(None)))
+                                                             _f32(v, 256 * blocks, "v", dev), _current()))
     return m, v
