@@ -197,15 +197,13 @@ __device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const u
     // vector.  Finding the true one first would take as many instructions as the sums.
     r.m = warp_max(tid < nvec ? max_nan(zt, max_of<F32>(slice[tid])) : zt);
     // All masked there (-inf): the next vectors in which any lane finds something else; a warp that finds nothing has sums of 0.
-    // (4096 x 131072 with all but the 50 largest masked: log-probabilities 254 us, 203 without a mask.)
-    bool any = true;
-    if (__builtin_expect(r.m == -INFINITY, 0)) {
-        any = false;
+    // (4096 x 131072 with all but the 50 largest masked: log-probabilities 246 us, 436 if such warps go through a second time,
+    // 203 without a mask.)  The one warp of a short row goes through a second time instead: the look costs it 4 % of a row.
+    if (NT > 32 && __builtin_expect(r.m == -INFINITY, 0)) {
 #pragma unroll 1
-        for (int v = tid + NT; !any && v - (tid & 31) < nvec; v += NT) {
+        for (int v = tid + NT; r.m == -INFINITY && v - (tid & 31) < nvec; v += NT) {
             const float x = v < nvec ? max_of<F32>(slice[v]) : -INFINITY;
-            any = __any_sync(0xffffffffu, x != -INFINITY);
-            if (any) r.m = warp_max(x);
+            if (__any_sync(0xffffffffu, x != -INFINITY)) r.m = warp_max(x);
         }
     }
     {
@@ -227,8 +225,9 @@ __device__ __forceinline__ WarpStats warp_statistics(const uint4* slice, const u
         r.s = warp_sum(s2.x + s2.y);
         r.u = ENTROPY ? warp_sum(u2.x + u2.y) : 0.f;
     }
-    // again from the true maximum if the reference was too far below it (or there is a NaN)
-    if (any && !(r.s > 0x1p-30f && r.s < 0x1p40f)) {
+    // again from the true maximum if the reference was too far below it, or if there is a NaN (a sum with a reference among its
+    // elements is 1 at least: 0 means that nothing was found)
+    if (NT == 32 ? r.m == -INFINITY || !(r.s > 0x1p-30f && r.s < 0x1p40f) : !(r.s == 0.f || (r.s > 0x1p-30f && r.s < 0x1p40f))) {
         r.m = zt;
         for (int v = tid; v < nvec; v += NT) r.m = max_nan(r.m, max_of<F32>(again[v]));
         r.m = warp_max(r.m);
