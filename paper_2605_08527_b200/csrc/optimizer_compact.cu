@@ -3,8 +3,9 @@
 // itself).  The state's format is in marlaas.h.  Per element: gradient 4 B read, master 4 + 4, moments 2.06 + 2.06, the
 // pool's bf16 2 written = 18.1 bytes and no reuse: bound by HBM, with the arithmetic not far behind (90 instructions per
 // element, most of them integer work on codes and random bits: the ALU pipes are two thirds busy at the rate reached).
-// Measured: 91 us for 32 tenants of rank 32 over a 4096 x (3 x 4096) pool (25.2 M elements, 456 MB, 0.78 of the copy rate;
-// 155 us with one element at a time and IEEE division and root), 115 us for rank 128 over 4096 x 4096 (0.82).
+// Measured: 87 us for 32 tenants of rank 32 over a 4096 x (3 x 4096) pool (25.2 M elements, 456 MB, 0.81 of the copy rate;
+// 155 us with one element at a time and IEEE division and root), 113 us for rank 128 over 4096 x 4096 (0.83), 39.1 us for ranks
+// 8 to 64 over 5120 x 5120 (9.8 M elements, 0.71: 2.7 rounds of units over the places for CTAs).
 #include <string.h>
 
 #include <cmath>

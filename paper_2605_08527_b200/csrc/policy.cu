@@ -315,7 +315,9 @@ static marlaas_status_t launch_advantages(const marlaas_pool* pool, const AdvArg
 }
 
 // One CTA per bucket sums its tokens' terms, every thread its own tokens in ascending order, then a fixed tree.  A token's
-// segment is found by bisection, in a copy of the offsets in shared memory where they fit.
+// segment is found by bisection, in a copy of the offsets in shared memory where they fit.  Every bucket with a segment looks at
+// all tokens: beside wide rows that does not show, for hundreds of tenants over short rows it does (the loss over 4096 x 1000
+// takes 20 us for up to 128 tenants, 33 for 512; over 65536 x 1000 175 to 190, and 341).
 constexpr int STATS_THREADS = 1024, STATS_OFFSETS = 4096;
 __global__ void __launch_bounds__(STATS_THREADS) k_policy_stats(int T, int S, int cap, const int32_t* __restrict__ seg_offsets,
                                                                 const int32_t* __restrict__ seg_slot, const PolicyTerms* __restrict__ terms,

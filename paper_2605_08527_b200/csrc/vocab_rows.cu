@@ -137,8 +137,8 @@ __device__ __forceinline__ float max_of(const uint4& q) {
 // them.
 //
 // What bounds it: HBM, with the arithmetic close behind (per element of a bf16 row 13 issue slots and 2 special-function
-// operations, 56 % and 69 % of what the SMs have while the row streams): loss and gradient over 16384 x 32768 bf16 in 381 us,
-// 0.87 of the copy rate; over 8192 x 131072, four CTAs per row, 764 us, 0.87.  Tried and not kept: the slice in registers
+// operations, 57 % and 69 % of what the SMs have while the row streams): loss and gradient over 16384 x 32768 bf16 in 376 to
+// 388 us, 0.86 to 0.88 of the copy rate; over 8192 x 131072, four CTAs per row, 763 us, 0.87.  Tried and not kept: the slice in registers
 // (2 CTAs per SM, 438 us for the loss over 4096 x 131072 against 398), chunks that are refilled one by one (441 us: the
 // waits cost more than the earlier copies gain), a share of the exponentials as polynomials on the FMA pipes (425 us).
 // Rows are dealt out in advance (no counter that calls would have to share): the k-th row that is read goes to cluster
