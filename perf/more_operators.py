@@ -23,27 +23,27 @@ EPS = 1e-5
 def listed():
     return [
         # log-probabilities of the tokens that one decode step of a small model sampled
-        dict(name="head logp, decode", op="head", T=32, d=1024, V=32768, grad=False, ignored=0.0, tenants=8),
+        dict(name="head logp decode", op="head", T=32, d=1024, V=32768, grad=False, ignored=0.0, tenants=8),
         # reference-policy pass over a training batch, an odd vocabulary
-        dict(name="head logp, odd", op="head", T=1021, d=2048, V=50001, grad=False, ignored=0.25, tenants=8),
+        dict(name="head logp odd", op="head", T=1021, d=2048, V=50001, grad=False, ignored=0.25, tenants=8),
         # loss and gradient of a small batch: launches count
-        dict(name="head loss, small", op="head", T=64, d=512, V=8000, grad=True, ignored=0.1, tenants=4),
+        dict(name="head loss small", op="head", T=64, d=512, V=8000, grad=True, ignored=0.1, tenants=4),
         # a training batch over a large vocabulary, a quarter prompt tokens
-        dict(name="head loss, large", op="head", T=4096, d=4096, V=131072, grad=True, ignored=0.25, tenants=10),
+        dict(name="head loss large", op="head", T=4096, d=4096, V=131072, grad=True, ignored=0.25, tenants=10),
         # one tenant's few tokens through a small projection
-        dict(name="dropout forward, small", op="dropout", back=False, T=100, K=512, N=512, tenants=1, rank=8),
+        dict(name="dropout forward small", op="dropout", back=False, T=100, K=512, N=512, tenants=1, rank=8),
         # 32 tenants' training batch through a square projection of a 7B-shaped model
-        dict(name="dropout forward, large", op="dropout", back=False, T=8192, K=4096, N=4096, tenants=32, rank=16),
+        dict(name="dropout forward large", op="dropout", back=False, T=8192, K=4096, N=4096, tenants=32, rank=16),
         # mixed ranks, sizes that end inside a tile
-        dict(name="dropout backward, odd", op="dropout", back=True, T=1000, K=1544, N=1032, tenants=5, rank=0),
-        dict(name="dropout backward, large", op="dropout", back=True, T=8192, K=4096, N=4096, tenants=32, rank=16),
+        dict(name="dropout backward odd", op="dropout", back=True, T=1000, K=1544, N=1032, tenants=5, rank=0),
+        dict(name="dropout backward large", op="dropout", back=True, T=8192, K=4096, N=4096, tenants=32, rank=16),
         # the norm of a decode step
-        dict(name="norm forward, decode", op="norm", back=False, T=64, d=1024, tenants=8, rms=True),
+        dict(name="norm forward decode", op="norm", back=False, T=64, d=1024, tenants=8, rms=True),
         # every position of a long training batch
-        dict(name="norm forward, large", op="norm", back=False, T=65536, d=4096, tenants=32, rms=False),
+        dict(name="norm forward large", op="norm", back=False, T=65536, d=4096, tenants=32, rms=False),
         # an odd batch, RMS norm
-        dict(name="norm backward, odd", op="norm", back=True, T=1021, d=1000, tenants=5, rms=True),
-        dict(name="norm backward, large", op="norm", back=True, T=32768, d=5120, tenants=32, rms=False),
+        dict(name="norm backward odd", op="norm", back=True, T=1021, d=1000, tenants=5, rms=True),
+        dict(name="norm backward large", op="norm", back=True, T=32768, d=5120, tenants=32, rms=False),
     ]
 
 
