@@ -74,6 +74,7 @@ enum {
                                          flag (their plan is built inside the first kernel anyway). */
     MARLAAS_FLAG_TOKEN_MEAN = 64u,    /* marlaas_group_advantages: every active token of a tenant weighs the same */
     MARLAAS_FLAG_NO_STD = 128u,       /* marlaas_group_advantages: rewards are centred, not divided by their deviation */
+    MARLAAS_FLAG_RMS_NORM = 256u,     /* marlaas_layer_norm, _backward: the mean is not subtracted (RMS norm) */
     MARLAAS_FLAG_OVERLAP_PREVIOUS = 32u /* forward, decode-shaped batches (at most 1024 tokens): the caller states that the
                                          work submitted to the stream immediately before this call -- typically the same
                                          layer's call for another micro-batch of a serving loop that interleaves two --
@@ -391,6 +392,32 @@ marlaas_status_t marlaas_adamw_compact_state_export(marlaas_pool_t* pool, int64_
 /* Device addresses of the pool's bf16 rows inside its storage: At [parts][capacity * rank_stride][d_in] (row
  * slot * rank_stride + j of block p is column j of A_t,p), Bs [capacity * rank_stride][d_out].  Read-only for the caller. */
 marlaas_status_t marlaas_adapter_pool_store(const marlaas_pool_t* pool, const void** At, const void** Bs);
+
+/* ---- around the adapted projections of a training step ---- */
+
+enum { MARLAAS_MAX_NORM_WIDTH = 16384 };
+
+/* Layer norm whose gain and bias are each tenant's own, over rows of d elements (d a multiple of 8 up to
+ * MARLAAS_MAX_NORM_WIDTH; x and y are bf16 with leading dimensions ldx, ldy).  With t the slot of token i,
+ *     y_i = (x_i - mean_i) rstd_i gain_t + bias_t,     rstd_i = 1 / sqrt(var_i + eps)
+ * var the population variance; with MARLAAS_FLAG_RMS_NORM mean_i = 0.  gain and bias (NULL = none) are fp32
+ * [capacity + 1][d], 16-byte aligned; row `capacity` serves slot -1, and the tokens that an ill-formed device table leaves out
+ * (reported by marlaas_check_status).  mean and rstd: fp32 [T] for the backward pass, each may be NULL.  y may be x itself.
+ * A row of infinities or NaN gives NaN and touches no other row.  `pool` supplies the device, the slots and the status word.
+ * The workspace is used with MARLAAS_FLAG_HOST_TABLE alone (marlaas_layer_norm_workspace_bytes with backward = 0). */
+size_t marlaas_layer_norm_workspace_bytes(const marlaas_pool_t* pool, int64_t T, int64_t d, int32_t num_segments, int32_t backward);
+marlaas_status_t marlaas_layer_norm(marlaas_pool_t* pool, int64_t T, int64_t d, const void* x, int64_t ldx,
+                                    const marlaas_segments_t* seg, const float* gain, const float* bias, float eps, void* y,
+                                    int64_t ldy, float* mean, float* rstd, void* workspace, size_t workspace_bytes,
+                                    uint32_t flags, void* cuda_stream);
+/* Its gradients: dx bf16 [T][d] (NULL = skip; may be dy or x itself), dgain and dbias fp32 [capacity + 1][d], 16-byte aligned
+ * (each may be NULL), the sums over each tenant's tokens: exact zeros for a tenant without tokens, added to with
+ * MARLAAS_FLAG_ACCUMULATE, in an order that depends on the sizes and the segment table alone.  mean (not read with
+ * MARLAAS_FLAG_RMS_NORM) and rstd as the forward pass wrote them. */
+marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, int64_t d, const void* x, int64_t ldx, const void* dy,
+                                             int64_t lddy, const marlaas_segments_t* seg, const float* gain, const float* mean,
+                                             const float* rstd, void* dx, int64_t lddx, float* dgain, float* dbias, void* workspace,
+                                             size_t workspace_bytes, uint32_t flags, void* cuda_stream);
 
 /* Synchronise `cuda_stream`, read and clear the pool's device status word: MARLAAS_OK, or the first
  * device-side finding since the last check (BAD_SEGMENT_TABLE, DEVICE_BAD_INDEX, DEVICE_TIMEOUT). */

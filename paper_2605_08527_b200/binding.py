@@ -35,11 +35,13 @@ MARLAAS_FLAG_REUSE_PLAN = 16
 MARLAAS_FLAG_OVERLAP_PREVIOUS = 32
 MARLAAS_FLAG_TOKEN_MEAN = 64
 MARLAAS_FLAG_NO_STD = 128
+MARLAAS_FLAG_RMS_NORM = 256
 
 MARLAAS_DTYPE_BF16 = 0
 MARLAAS_DTYPE_F32 = 1
 MARLAAS_MAX_VOCABULARY = 262144
 MARLAAS_POLICY_STATS = 8
+MARLAAS_MAX_NORM_WIDTH = 16384
 
 EXPORTED_SYMBOLS = [
     "marlaas_adapter_pool_storage_bytes", "marlaas_adapter_pool_create", "marlaas_adapter_pool_destroy",
@@ -52,7 +54,7 @@ EXPORTED_SYMBOLS = [
     "marlaas_lora_forward_workspace_min_bytes", "marlaas_adapter_pool_storage_bytes_segmented", "marlaas_adapter_pool_create_segmented", "marlaas_adapter_pool_parts",
     "marlaas_policy_workspace_bytes", "marlaas_group_advantages", "marlaas_token_logprobs", "marlaas_policy_loss",
     "marlaas_adamw_compact_state_bytes", "marlaas_adapter_pool_adamw_compact_commit", "marlaas_adamw_compact_state_export",
-    "marlaas_adapter_pool_store",
+    "marlaas_adapter_pool_store", "marlaas_layer_norm_workspace_bytes", "marlaas_layer_norm", "marlaas_layer_norm_backward",
 ]
 
 
@@ -159,6 +161,12 @@ def load_library() -> ctypes.CDLL:
     L.marlaas_adamw_compact_state_export.argtypes = [vp, i64, vp, vp, vp, vp]
     L.marlaas_adapter_pool_store.restype = i32
     L.marlaas_adapter_pool_store.argtypes = [vp, P(vp), P(vp)]
+    L.marlaas_layer_norm_workspace_bytes.restype = sz
+    L.marlaas_layer_norm_workspace_bytes.argtypes = [vp, i64, i64, i32, i32]
+    L.marlaas_layer_norm.restype = i32
+    L.marlaas_layer_norm.argtypes = [vp, i64, i64, vp, i64, P(marlaas_segments_t), vp, vp, f32, vp, i64, vp, vp, vp, sz, u32, vp]
+    L.marlaas_layer_norm_backward.restype = i32
+    L.marlaas_layer_norm_backward.argtypes = [vp, i64, i64, vp, i64, vp, i64, P(marlaas_segments_t), vp, vp, vp, vp, i64, vp, vp, vp, sz, u32, vp]
     L.marlaas_last_error.restype = ctypes.c_char_p
     L.marlaas_last_error.argtypes = []
     L.marlaas_kernel_launch_count.restype = u64
@@ -327,6 +335,16 @@ class AdapterPool:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             self._workspaces[where] = ws
         self._policy_last = (key, ws)
+        return ws
+
+    def step_workspace(self, need: int, handle: int) -> torch.Tensor:
+        """At least `need` bytes of scratch for the calls around a training step's layers, cached per stream (`handle`: the pool's
+        device's current one).  A call that is being captured gets one of its own from the graph's memory."""
+        if torch._C._cuda_isCurrentStreamCapturing():
+            return torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+        ws = self._workspaces.get(("step", handle))
+        if ws is None or ws.numel() < need:
+            ws = self._workspaces[("step", handle)] = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
         return ws
 
     def store(self):
@@ -745,3 +763,62 @@ def marlaas_adamw_compact_state_export(pool: AdapterPool, state: torch.Tensor, m
     _check(load_library().marlaas_adamw_compact_state_export(pool.handle, blocks, state.data_ptr(), _f32(m, 256 * blocks, "m", dev),
                                                              _f32(v, 256 * blocks, "v", dev), _current()))
     return m, v
+
+
+# ---- around the adapted projections of a training step ----
+
+def _bf16_rows(t: torch.Tensor, T: int, cols: int, name: str, device: int) -> int:
+    """Leading dimension of a bf16 [T][cols] matrix."""
+    assert t.dtype is torch.bfloat16 and t.dim() == 2 and t.shape[0] == T and t.shape[1] == cols and t.get_device() == device, name
+    assert cols == 1 or t.stride(1) == 1, name
+    return t.stride(0) if T > 1 else -(-cols // 8) * 8
+
+
+def marlaas_layer_norm_workspace_bytes(pool: AdapterPool, T: int, d: int, num_segments: int, backward: bool) -> int:
+    return int(load_library().marlaas_layer_norm_workspace_bytes(pool.handle, T, d, num_segments, int(backward)))
+
+
+def marlaas_layer_norm(pool: AdapterPool, x: torch.Tensor, seg: Segments, gain: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
+                       eps: float = 1e-5, y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                       rstd: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None):
+    """(y, mean [T], rstd [T]) of the rows of x with the gain and bias [capacity + 1][d] of their tenants (the last row: slot
+    -1).  Outputs that are not given are allocated."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_layer_norm, pool, x, seg, gain, bias, eps=eps, y=y, mean=mean, rstd=rstd, workspace=workspace,
+                          flags=flags)
+    (T, d), dev = x.shape, pool.index
+    y = torch.empty_like(x, memory_format=torch.contiguous_format) if y is None else y
+    mean = torch.empty(T, dtype=torch.float32, device=x.device) if mean is None else mean
+    rstd = torch.empty(T, dtype=torch.float32, device=x.device) if rstd is None else rstd
+    handle = torch._C._cuda_getCurrentRawStream(dev)
+    ws = workspace
+    if ws is None and seg.on_host:
+        ws = pool.step_workspace(marlaas_layer_norm_workspace_bytes(pool, T, d, seg.num_segments, False), handle)
+    params = (pool.capacity + 1) * d
+    _check(load_library().marlaas_layer_norm(
+        pool.handle, T, d, x.data_ptr(), _bf16_rows(x, T, d, "x", dev), seg.ref, _f32(gain, params, "gain", dev),
+        None if bias is None else _f32(bias, params, "bias", dev), eps, y.data_ptr(), _bf16_rows(y, T, d, "y", dev), _f32(mean, T, "mean", dev),
+        _f32(rstd, T, "rstd", dev), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), flags | seg.flags, handle))
+    return y, mean, rstd
+
+
+def marlaas_layer_norm_backward(pool: AdapterPool, x: torch.Tensor, dy: torch.Tensor, seg: Segments, gain: torch.Tensor,
+                                mean: Optional[torch.Tensor], rstd: torch.Tensor, *, dx: Optional[torch.Tensor] = None,
+                                dgain: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                                workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> None:
+    """Writes those of dx, dgain, dbias ([capacity + 1][d]) that are given."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_layer_norm_backward, pool, x, dy, seg, gain, mean, rstd, dx=dx, dgain=dgain, dbias=dbias,
+                          workspace=workspace, flags=flags)
+    (T, d), dev = x.shape, pool.index
+    params = (pool.capacity + 1) * d
+    handle = torch._C._cuda_getCurrentRawStream(dev)
+    ws = workspace
+    if ws is None:
+        ws = pool.step_workspace(marlaas_layer_norm_workspace_bytes(pool, T, d, seg.num_segments, True), handle)
+    _check(load_library().marlaas_layer_norm_backward(
+        pool.handle, T, d, x.data_ptr(), _bf16_rows(x, T, d, "x", dev), dy.data_ptr(), _bf16_rows(dy, T, d, "dy", dev), seg.ref,
+        _f32(gain, params, "gain", dev), None if mean is None else _f32(mean, T, "mean", dev), _f32(rstd, T, "rstd", dev),
+        None if dx is None else dx.data_ptr(), 0 if dx is None else _bf16_rows(dx, T, d, "dx", dev),
+        None if dgain is None else _f32(dgain, params, "dgain", dev), None if dbias is None else _f32(dbias, params, "dbias", dev),
+        ws.data_ptr(), ws.numel(), flags | seg.flags, handle))

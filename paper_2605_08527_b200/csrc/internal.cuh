@@ -164,6 +164,28 @@ marlaas_status_t launch_slot_sort(const marlaas_pool* pool, int64_t T, const int
 marlaas_status_t launch_plan_tiles(const marlaas_pool* pool, int64_t T, int32_t S, const int32_t* seg_offsets,
                                    const int32_t* seg_slot, const Workspace& ws, cudaStream_t st);
 
+// order.cu: a stable order of a batch's tokens by a small key
+struct OrderArgs {
+    int64_t T;
+    // keys by tenant: the segment table (slot -1 is key cap, nkeys = cap + 1)
+    int S;
+    const int32_t* off;
+    const int32_t* slot;
+    int cap;
+    // or, with targets, the tokens that count (key 0: a target in [0, V), a weight that is not 0) before the others (nkeys = 2)
+    const int32_t* targets;
+    const float* weight;               // or NULL
+    int64_t V;
+    int nkeys;
+    int32_t* perm;                     // [T]  out: the tokens in order
+    int32_t* key_off;                  // [nkeys + 1]  out: where each key's tokens begin
+    int32_t* keyrank;                  // scratch
+    int32_t* hist;
+    int32_t* status;
+};
+size_t order_scratch_ints(int64_t T, int nkeys);
+marlaas_status_t launch_order(const marlaas_pool* pool, OrderArgs a, int32_t* scratch, cudaStream_t st);
+
 // gemm_sm100.cu
 struct GemmOperands {
     int64_t M, Nout, Kc;
