@@ -395,7 +395,8 @@ marlaas_status_t marlaas_adapter_pool_store(const marlaas_pool_t* pool, const vo
 
 /* ---- around the adapted projections of a training step ---- */
 
-enum { MARLAAS_MAX_NORM_WIDTH = 16384 };
+enum { MARLAAS_MAX_NORM_WIDTH = 16384, MARLAAS_MAX_HEAD_WIDTH = 65536 };
+enum { MARLAAS_HEAD_STATS = 4 };                           /* columns of marlaas_head_cross_entropy's stats */
 
 /* Layer norm whose gain and bias are each tenant's own, over rows of d elements (d a multiple of 8 up to
  * MARLAAS_MAX_NORM_WIDTH; x and y are bf16 with leading dimensions ldx, ldy).  With t the slot of token i,
@@ -418,6 +419,32 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
                                              int64_t lddy, const marlaas_segments_t* seg, const float* gain, const float* mean,
                                              const float* rstd, void* dx, int64_t lddx, float* dgain, float* dbias, void* workspace,
                                              size_t workspace_bytes, uint32_t flags, void* cuda_stream);
+
+/* Cross entropy of the vocabulary head from the last hidden states, and its gradient by them, without the logits: what
+ * marlaas_token_logprobs gives for logits = x W, and weighted sums of it, with x [T][d] and the frozen W [d][V] bf16 (ldx, ldw
+ * multiples of 8; d a multiple of 8 up to MARLAAS_MAX_HEAD_WIDTH, V any number from 1 to MARLAAS_MAX_VOCABULARY).  With
+ * z_i = inv_temperature x_i W in fp32, y_i = targets[i], w_i = weight[i] (NULL: 1):
+ *     logp_i = z_i[y_i] - log sum exp z_i          loss = sum_i w_i (-logp_i)
+ *     dx_i = grad_scale d loss / d x_i = grad_scale inv_temperature w_i (softmax(z_i) - e_y) W^T
+ * Weights may have either sign: with w_i = weight_i adv_i of marlaas_group_advantages, dx is the gradient of
+ * marlaas_policy_loss where all ratios are 1 (the first pass over a batch, without KL and entropy terms).
+ *  - A token with a negative target or a weight of 0 is ignored whatever its row holds: logp 0, dx 0, nothing in the sums,
+ *    and its part of the products is not computed.
+ *  - A target >= V is reported by marlaas_check_status (MARLAAS_ERR_DEVICE_BAD_INDEX) and its token is ignored.
+ *  - A row with a NaN or +inf logit gets NaN, and touches no other row; a logit of -inf has probability 0; a row whose logits
+ *    are all -inf has no distribution: logp and dx are 0.
+ * dx: bf16 [T][d] or NULL (no gradient: half the work and a smaller workspace); it may be x itself.  logp: fp32 [T] or NULL.
+ * stats (or NULL; then seg is not read): fp32 [capacity + 1][MARLAAS_HEAD_STATS], per slot (last row: slot -1) the sums over its
+ * tokens of  w (-logp), w, -logp, 1;  written, or added to with MARLAAS_FLAG_ACCUMULATE, in a fixed order.
+ * The exponentials in the workspace are those of a piece of the batch (512 MB, or 256 rows where those are more).  The probabilities
+ * in the gradient's product are bf16, rounded twice on their way there (2^-8 relative each time); all sums are fp32. */
+size_t marlaas_head_cross_entropy_workspace_bytes(const marlaas_pool_t* pool, int64_t T, int64_t d, int64_t V, int32_t num_segments,
+                                                  int32_t with_gradient);
+marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int64_t d, int64_t V, const void* x, int64_t ldx,
+                                            const void* W, int64_t ldw, const int32_t* targets, const marlaas_segments_t* seg,
+                                            const float* weight, float inv_temperature, float grad_scale, void* dx, int64_t lddx,
+                                            float* logp, float* stats, void* workspace, size_t workspace_bytes, uint32_t flags,
+                                            void* cuda_stream);
 
 /* Synchronise `cuda_stream`, read and clear the pool's device status word: MARLAAS_OK, or the first
  * device-side finding since the last check (BAD_SEGMENT_TABLE, DEVICE_BAD_INDEX, DEVICE_TIMEOUT). */

@@ -42,6 +42,8 @@ MARLAAS_DTYPE_F32 = 1
 MARLAAS_MAX_VOCABULARY = 262144
 MARLAAS_POLICY_STATS = 8
 MARLAAS_MAX_NORM_WIDTH = 16384
+MARLAAS_MAX_HEAD_WIDTH = 65536
+MARLAAS_HEAD_STATS = 4
 
 EXPORTED_SYMBOLS = [
     "marlaas_adapter_pool_storage_bytes", "marlaas_adapter_pool_create", "marlaas_adapter_pool_destroy",
@@ -55,6 +57,7 @@ EXPORTED_SYMBOLS = [
     "marlaas_policy_workspace_bytes", "marlaas_group_advantages", "marlaas_token_logprobs", "marlaas_policy_loss",
     "marlaas_adamw_compact_state_bytes", "marlaas_adapter_pool_adamw_compact_commit", "marlaas_adamw_compact_state_export",
     "marlaas_adapter_pool_store", "marlaas_layer_norm_workspace_bytes", "marlaas_layer_norm", "marlaas_layer_norm_backward",
+    "marlaas_head_cross_entropy_workspace_bytes", "marlaas_head_cross_entropy",
 ]
 
 
@@ -167,6 +170,11 @@ def load_library() -> ctypes.CDLL:
     L.marlaas_layer_norm.argtypes = [vp, i64, i64, vp, i64, P(marlaas_segments_t), vp, vp, f32, vp, i64, vp, vp, vp, sz, u32, vp]
     L.marlaas_layer_norm_backward.restype = i32
     L.marlaas_layer_norm_backward.argtypes = [vp, i64, i64, vp, i64, vp, i64, P(marlaas_segments_t), vp, vp, vp, vp, i64, vp, vp, vp, sz, u32, vp]
+    L.marlaas_head_cross_entropy_workspace_bytes.restype = sz
+    L.marlaas_head_cross_entropy_workspace_bytes.argtypes = [vp, i64, i64, i64, i32, i32]
+    L.marlaas_head_cross_entropy.restype = i32
+    L.marlaas_head_cross_entropy.argtypes = [vp, i64, i64, i64, vp, i64, vp, i64, vp, P(marlaas_segments_t), vp, f32, f32, vp, i64, vp, vp,
+                                             vp, sz, u32, vp]
     L.marlaas_last_error.restype = ctypes.c_char_p
     L.marlaas_last_error.argtypes = []
     L.marlaas_kernel_launch_count.restype = u64
@@ -822,3 +830,38 @@ def marlaas_layer_norm_backward(pool: AdapterPool, x: torch.Tensor, dy: torch.Te
         None if dx is None else dx.data_ptr(), 0 if dx is None else _bf16_rows(dx, T, d, "dx", dev),
         None if dgain is None else _f32(dgain, params, "dgain", dev), None if dbias is None else _f32(dbias, params, "dbias", dev),
         ws.data_ptr(), ws.numel(), flags | seg.flags, handle))
+
+
+def marlaas_head_cross_entropy_workspace_bytes(pool: AdapterPool, T: int, d: int, V: int, num_segments: int, with_gradient: bool) -> int:
+    return int(load_library().marlaas_head_cross_entropy_workspace_bytes(pool.handle, T, d, V, num_segments, int(with_gradient)))
+
+
+def marlaas_head_cross_entropy(pool: AdapterPool, x: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, seg: Optional[Segments] = None, *,
+                               weight: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, logp: Optional[torch.Tensor] = None,
+                               stats: Optional[torch.Tensor] = None, inv_temperature: float = 1.0, grad_scale: float = 1.0,
+                               workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None):
+    """(logp [T], stats [capacity + 1][4]) of the targets under softmax(inv_temperature x W), and the weighted loss's gradient by x
+    in `dx` (which may be `x` itself) if given.  Without `seg` there are no stats: (logp, None)."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_head_cross_entropy, pool, x, W, targets, seg, weight=weight, dx=dx, logp=logp, stats=stats,
+                          inv_temperature=inv_temperature, grad_scale=grad_scale, workspace=workspace, flags=flags)
+    (T, d), V, dev = x.shape, W.shape[1], pool.index
+    if logp is None:
+        logp = torch.empty(T, dtype=torch.float32, device=x.device)
+    if seg is None:
+        assert stats is None, "stats need the segment table"
+    elif stats is None:
+        assert not (flags & MARLAAS_FLAG_ACCUMULATE), "stats to add to"
+        stats = torch.empty((pool.capacity + 1, MARLAAS_HEAD_STATS), dtype=torch.float32, device=x.device)
+    S = 0 if seg is None else seg.num_segments
+    handle = torch._C._cuda_getCurrentRawStream(dev)
+    ws = workspace
+    if ws is None:
+        ws = pool.step_workspace(marlaas_head_cross_entropy_workspace_bytes(pool, T, d, V, S, dx is not None), handle)
+    _check(load_library().marlaas_head_cross_entropy(
+        pool.handle, T, d, V, x.data_ptr(), _bf16_rows(x, T, d, "x", dev), W.data_ptr(), _bf16_rows(W, d, V, "W", dev),
+        _i32(targets, T, "targets", dev), None if seg is None else seg.ref, None if weight is None else _f32(weight, T, "weight", dev),
+        inv_temperature, grad_scale, None if dx is None else dx.data_ptr(), 0 if dx is None else _bf16_rows(dx, T, d, "dx", dev),
+        _f32(logp, T, "logp", dev), None if stats is None else _f32(stats, (pool.capacity + 1) * MARLAAS_HEAD_STATS, "stats", dev),
+        ws.data_ptr(), ws.numel(), flags | (0 if seg is None else seg.flags), handle))
+    return logp, stats

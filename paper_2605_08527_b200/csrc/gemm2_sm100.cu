@@ -12,6 +12,15 @@
 //   empty[s]  one per CTA; the leader's tcgen05.commit (multicast to both CTAs) releases the stage in both
 //   tfull[b]  one per CTA, same multicast commit after the tile's last MMA
 //   tempty[b] leader's barrier, 8 arrivals: the four epilogue warps of each CTA (the peer's arrive remotely)
+//
+// The vocabulary head's cross entropy (head.cu) runs the same main loop with epilogues of its own and a number of rows that
+// only the device knows:
+//   EPI_SOFTMAX  a tile of logits leaves the SM as its rows' largest logit and sum of exponentials, the target's logit, and
+//                (for a gradient) the exponentials in bf16; the logits themselves are never written
+//   EPI_GRAD     the product over the vocabulary is cut along it into `splits` ranges, so that few row tiles still fill the
+//                SMs; each (range, tile) leaves an fp32 tile, or the output itself when there is one range
+#include <string.h>
+
 #include "sm100_ptx.cuh"
 
 namespace marlaas {
@@ -40,7 +49,10 @@ struct Gemm2Args {
     bf16* C;
     int64_t ldc;
     int32_t* status;
+    HeadEpilogue head;                      // EPI_SOFTMAX, EPI_GRAD
 };
+
+enum { EPI_LAYER = 0, EPI_SOFTMAX = 1, EPI_GRAD = 2 };
 
 // the parts whose low-rank term enters output columns n0 ...
 __device__ __forceinline__ void tile_parts(const Gemm2Args& g, int n0, int& p_lo, int& p_hi) {
@@ -101,12 +113,12 @@ __host__ __device__ constexpr uint32_t make_idesc_pair(int b_mn) {
            ((uint32_t)(256 >> 4) << 24);
 }
 
-__device__ __forceinline__ void decode_tile2(const Gemm2Args& g, int tile, int& m_idx, int& n_idx) {
+__device__ __forceinline__ void decode_tile2(const Gemm2Args& g, int num_m_tiles, int tile, int& m_idx, int& n_idx) {
     const int per_band = g.group_m * g.num_n_tiles;
     const int band = tile / per_band;
     const int rem = tile - band * per_band;
     const int m_first = band * g.group_m;
-    const int gm = min(g.group_m, g.num_m_tiles - m_first);
+    const int gm = min(g.group_m, num_m_tiles - m_first);
     n_idx = rem / gm;
     m_idx = m_first + (rem - n_idx * gm);
 }
@@ -115,8 +127,8 @@ __device__ __forceinline__ void decode_tile2(const Gemm2Args& g, int tile, int& 
 __device__ __forceinline__ int half_chunks(const Gemm2Args& g, int n0, int r) {
     return max(0, min(2, (g.Nout - (n0 + r * 128) + 63) / 64));
 }
-__device__ __forceinline__ uint32_t main_bytes(const Gemm2Args& g, int m0, int n0, int r, uint32_t kp) {
-    const uint32_t a = (m0 + r * 128 < g.M) ? A_STAGE_BYTES : 0u;
+__device__ __forceinline__ uint32_t main_bytes(const Gemm2Args& g, int M, int m0, int n0, int r, uint32_t kp) {
+    const uint32_t a = (m0 + r * 128 < M) ? A_STAGE_BYTES : 0u;
     const uint32_t b = g.b_mn ? (uint32_t)half_chunks(g, n0, r) * CHUNK_BYTES
                               : ((n0 + r * 128 < g.Nout) ? G2_B_STAGE_BYTES : 0u);
     return kp * (a + b);      // kp 64-deep panels per pipeline step
@@ -133,10 +145,109 @@ __device__ __forceinline__ uint32_t extra_bytes(const Gemm2Args& g, int m0, int 
     return a + (uint32_t)(nv * half_chunks(g, n0, r)) * UNIT_BYTES;
 }
 
+// Rows the device says there are, of at most `most`.
+__device__ __forceinline__ int head_rows(const HeadEpilogue& h, int most) {
+    return min(most, max(0, *h.active - h.row0));
+}
+
+// A row's 256 logits of one tile (the thread's lane of tensor memory at trow), in units of log 2 and of 1 / inv_temperature:
+// the largest, then the sum of exponentials relative to it.  Two passes over tensor memory, whose reads cost less than keeping
+// 256 values.  The reference is rounded once and used as rounded everywhere, so its rounding cancels.
+__device__ __forceinline__ void head_softmax_tile(const HeadEpilogue& h, uint32_t trow, int row, bool on, int n0, int V, int n_idx, bf16* E,
+                                                  int64_t lde) {
+    const int cols = min(G2_BN, V - n0);        // columns of the tile inside the vocabulary
+    float m = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < cols; c += 32) {
+        uint32_t v[32];
+        __syncwarp();
+        tc_ld_32x32(trow + c, v);
+        tc_wait_ld();
+        if (c + 32 <= cols) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) m = fmaxf(m, __uint_as_float(v[e]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) m = c + e < cols ? fmaxf(m, __uint_as_float(v[e])) : m;
+        }
+    }
+    const float ref = m == -INFINITY ? 0.f : m * h.k2;
+    const int t = on ? h.targets[h.row0 + row] - n0 : -1;       // the target's column in this tile
+    float sum0 = 0.f, sum1 = 0.f;
+    bf16* erow = E + (size_t)row * lde + n0;
+#pragma unroll 1
+    for (int c = 0; c < cols; c += 32) {
+        uint32_t v[32];
+        __syncwarp();
+        tc_ld_32x32(trow + c, v);
+        tc_wait_ld();
+        if (t >= c && t < c + 32) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+                if (t == c + e) h.target_logit[row] = __uint_as_float(v[e]) * h.k2;
+        }
+        uint32_t o[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            float x, y;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(fmaf(__uint_as_float(v[2 * e]), h.k2, -ref)));
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaf(__uint_as_float(v[2 * e + 1]), h.k2, -ref)));
+            if (c + 32 > cols) {
+                x = c + 2 * e < cols ? x : 0.f;
+                y = c + 2 * e + 1 < cols ? y : 0.f;
+            }
+            sum0 += x;
+            sum1 += y;
+            __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
+            o[e] = *reinterpret_cast<uint32_t*>(&p);
+        }
+        if (h.keep && on) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e * 8 < cols) *reinterpret_cast<uint4*>(erow + c + e * 8) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        }
+    }
+    if (on) h.part[(size_t)row * h.part_ld + n_idx] = make_float2(ref, sum0 + sum1);
+}
+
+// The tile's rows of the gradient by x: fp32 for a later sum over the ranges of the vocabulary, or scaled and rounded.
+__device__ __forceinline__ void head_grad_tile(const HeadEpilogue& h, uint32_t trow, int row, bool on, int n0, int d, int splits, size_t at,
+                                               bf16* dx, int64_t lddx) {
+    const float f = on && splits == 1 ? h.coef[row] : 0.f;
+    bf16* out = on && splits == 1 ? dx + (size_t)h.perm[h.row0 + row] * lddx + n0 : nullptr;
+    float* part = h.partial + at + (size_t)(row & 255) * 256;
+#pragma unroll 1
+    for (int c = 0; c < G2_BN; c += 32) {
+        if (n0 + c >= d) break;
+        uint32_t v[32];
+        __syncwarp();
+        tc_ld_32x32(trow + c, v);
+        tc_wait_ld();
+        if (on && splits > 1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<uint4*>(part + c + e * 4) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+        } else if (on) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (n0 + c + e * 8 < d) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        __nv_bfloat162 p = __floats2bfloat162_rn(f * __uint_as_float(v[e * 8 + 2 * i]), f * __uint_as_float(v[e * 8 + 2 * i + 1]));
+                        o[i] = *reinterpret_cast<uint32_t*>(&p);
+                    }
+                    *reinterpret_cast<uint4*>(out + c + e * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+                }
+            }
+        }
+    }
+}
+
 // KP = 64-deep panels per pipeline step.  KP = 2 (contraction depth a multiple of 64): x / dy and a K-major W are viewed as
 // 3-D tensors so that ONE TMA instruction brings both panels, and the barrier wait / expect / commit of the two issuing
 // threads is paid once per 128 of depth; KP = 1 is the plain 2-D form for any depth.
-template <int KP>
+template <int KP, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G2_THREADS, 1)
 k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
               const __grid_constant__ CUtensorMap tmXA, const __grid_constant__ CUtensorMap tmXB, const Gemm2Args g) {
@@ -159,7 +270,23 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();      // 0 = leader
     const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
-    const int num_tiles = g.num_m_tiles * g.num_n_tiles;
+    const int M = EPI == EPI_LAYER ? g.M : head_rows(g.head, g.M);
+    const int num_m_tiles = EPI == EPI_LAYER ? g.num_m_tiles : (M + 255) / 256;
+    const int plane_tiles = num_m_tiles * g.num_n_tiles;
+    const int splits = EPI == EPI_GRAD ? head_splits(g.head, plane_tiles, (int)g.num_kb * KP) : 1;
+    const int num_tiles = plane_tiles * splits;       // work items: the tiles of the first range of k, then of the next
+    // the k-steps of a work item, and its tile
+    auto item = [&](int tile, int& m_idx, int& n_idx, int& kb0, int& kb1) {
+        kb0 = 0;
+        kb1 = g.num_kb;
+        if (EPI == EPI_GRAD) {
+            const int sp = tile / plane_tiles;
+            tile -= sp * plane_tiles;
+            kb0 = (int)((int64_t)g.num_kb * sp / splits);
+            kb1 = (int)((int64_t)g.num_kb * (sp + 1) / splits);
+        }
+        decode_tile2(g, num_m_tiles, tile, m_idx, n_idx);
+    };
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -200,14 +327,14 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             bool ok = true, waited = false;
             const uint32_t full0 = map_to_cta(bar_full, 0);      // the leader's full barriers (8 bytes apart)
             for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
-                int m_idx, n_idx;
-                decode_tile2(g, tile, m_idx, n_idx);
+                int m_idx, n_idx, kb0, kb1;
+                item(tile, m_idx, n_idx, kb0, kb1);
                 const int m0 = m_idx * 256, n0 = n_idx * G2_BN;
                 const int my_m = m0 + (int)rank * 128, my_n = n0 + (int)rank * 128;
-                const bool have_rows = my_m < g.M;
+                const bool have_rows = my_m < M;
                 const int nchunk = half_chunks(g, n0, (int)rank);
-                const uint32_t stage_tx = main_bytes(g, m0, n0, 0, KP) + main_bytes(g, m0, n0, 1, KP);
-                for (int kb = 0; kb < g.num_kb && ok; ++kb, ++it) {
+                const uint32_t stage_tx = main_bytes(g, M, m0, n0, 0, KP) + main_bytes(g, M, m0, n0, 1, KP);
+                for (int kb = kb0; kb < kb1 && ok; ++kb, ++it) {
                     if (!(ok = mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_word, 31))) break;
                     const uint32_t full = full0 + 8 * s;
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, stage_tx);
@@ -228,7 +355,7 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     asm volatile("griddepcontrol.wait;" ::: "memory");
                     waited = true;
                 }
-                const int nun = g.tile_nunits ? g.tile_nunits[m_idx] : 0;
+                const int nun = EPI == EPI_LAYER && g.tile_nunits ? g.tile_nunits[m_idx] : 0;
                 int p_lo, p_hi;
                 tile_parts(g, n0, p_lo, p_hi);
                 for (int p = p_lo; p < p_hi; ++p)
@@ -274,14 +401,14 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             const uint64_t db_base = g.b_mn ? desc_mn_major(sB, KP * CHUNK_BYTES) : desc_k_major(sB);
             const uint64_t db_step = g.b_mn ? (uint64_t)(UNIT_BYTES >> 4) : 2ull;
             for (int tile = pair; tile < num_tiles && ok; tile += num_pairs, ++lt) {
-                int m_idx, n_idx;
-                decode_tile2(g, tile, m_idx, n_idx);
+                int m_idx, n_idx, kb0, kb1;
+                item(tile, m_idx, n_idx, kb0, kb1);
                 const uint32_t b = lt & 1, aph = (lt >> 1) & 1;
                 if (!(ok = mbar_wait(bar_tempty + 8 * b, aph ^ 1, abort_word, 33))) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + b * G2_BN;
                 uint32_t acc = 0;
-                for (int kb = 0; kb < g.num_kb && ok; ++kb) {
+                for (int kb = kb0; kb < kb1 && ok; ++kb) {
                     if (!(ok = mbar_wait(bar_full + 8 * s, ph, abort_word, 34))) break;
                     const uint64_t da = da_base + (uint64_t)(s * (A_ST >> 4));
                     const uint64_t db = db_base + (uint64_t)(s * (B_ST >> 4));
@@ -303,7 +430,7 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     asm volatile("griddepcontrol.wait;" ::: "memory");
                     waited = true;
                 }
-                const int nun = g.tile_nunits ? g.tile_nunits[m_idx] : 0;
+                const int nun = EPI == EPI_LAYER && g.tile_nunits ? g.tile_nunits[m_idx] : 0;
                 int p_lo, p_hi;
                 tile_parts(g, n_idx * G2_BN, p_lo, p_hi);
                 for (int p = p_lo; p < p_hi; ++p)
@@ -338,8 +465,8 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         uint32_t lt = 0;
         bool ok = true;
         for (int tile = pair; tile < num_tiles && ok; tile += num_pairs, ++lt) {
-            int m_idx, n_idx;
-            decode_tile2(g, tile, m_idx, n_idx);
+            int m_idx, n_idx, kb0, kb1;
+            item(tile, m_idx, n_idx, kb0, kb1);
             const int m0 = m_idx * 256 + (int)rank * 128, n0 = n_idx * G2_BN;
             const uint32_t b = lt & 1, aph = (lt >> 1) & 1;
             ok = mbar_wait(bar_tfull + 8 * b, aph, abort_word, 36);
@@ -347,6 +474,13 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             if (!ok) break;
             tc_fence_after();
             const int row = m0 + q * 32 + lane;
+            const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16) + b * G2_BN;
+            if constexpr (EPI == EPI_SOFTMAX) {
+                head_softmax_tile(g.head, trow, row, row < M, n0, g.Nout, n_idx, g.C, g.ldc);
+            } else if constexpr (EPI == EPI_GRAD) {
+                head_grad_tile(g.head, trow, row, row < M, n0, g.Nout, splits,
+                               ((size_t)(tile / plane_tiles) * plane_tiles + (size_t)m_idx * g.num_n_tiles + n_idx) * 65536, g.C, g.ldc);
+            } else {
             bf16* crow = g.C + (size_t)row * g.ldc + n0;
 #pragma unroll 1
             for (int c = 0; c < G2_BN / 32; ++c) {
@@ -372,6 +506,7 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     }
                 }
             }
+            }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(tempty_leader0 + 8 * b);
@@ -395,8 +530,8 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 
 bool gemm2_sm100_eligible(const marlaas_pool* pool, int64_t M) { return M >= 1024 && pool->sm_count >= 2; }
 
-template <int KP>
-static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st) {
+template <int KP, int EPI>
+static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st, const HeadEpilogue* head = nullptr) {
     using namespace sm100;
     Gemm2Args g;
     g.M = (int)o.M;
@@ -420,6 +555,8 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     g.C = o.C;
     g.ldc = o.ldc;
     g.status = pool->d_status;
+    if (head) g.head = *head;
+    else memset(&g.head, 0, sizeof(g.head));
 
     alignas(64) CUtensorMap tmA, tmB, tmXA, tmXB;
     marlaas_status_t rc;
@@ -441,7 +578,7 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     static int max_clusters[64] = {};
     int& mc = max_clusters[pool->device < 64 ? pool->device : 63];
     if (mc == 0 || pool->device >= 64) {
-        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_gemm2_sm100<KP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_gemm2_sm100<KP, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes));
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(2 * (unsigned)(pool->sm_count / 2));
         cfg.blockDim = dim3(G2_THREADS);
@@ -454,12 +591,13 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
         cfg.attrs = &at;
         cfg.numAttrs = 1;
         int n = 0;
-        MARLAAS_CUDA_TRY(cudaOccupancyMaxActiveClusters(&n, k_gemm2_sm100<KP>, &cfg));
+        MARLAAS_CUDA_TRY(cudaOccupancyMaxActiveClusters(&n, k_gemm2_sm100<KP, EPI>, &cfg));
         if (n < 1) return fail(MARLAAS_ERR_CUDA, "no 2-CTA cluster of the GEMM kernel fits on this device");
         mc = n;
     }
     const int tiles = g.num_m_tiles * g.num_n_tiles;
-    const int pairs = tiles < mc ? tiles : mc;
+    // (with ranges of k the number of work items is the device's to choose)
+    const int pairs = EPI == EPI_GRAD || tiles > mc ? mc : tiles;
     // launched as a programmatic dependent: its main loop (x and W only) may start while the shrink's last CTAs run
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (unsigned)pairs);
@@ -469,8 +607,9 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at; cfg.numAttrs = 1;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_gemm2_sm100<KP>, tmA, tmB, tmXA, tmXB, g));
+    // (the head's kernels read what the kernel before them wrote from their first step on)
+    cfg.attrs = at; cfg.numAttrs = EPI == EPI_LAYER ? 1 : 0;
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_gemm2_sm100<KP, EPI>, tmA, tmB, tmXA, tmXB, g));
     count_launch();
     return MARLAAS_OK;
 }
@@ -478,7 +617,17 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
 marlaas_status_t launch_gemm2_sm100(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st) {
     if (o.M <= 0) return MARLAAS_OK;
     // two panels per step need the contraction depth in whole 64-deep panels (3-D views of the row-major operands)
-    return (o.Kc % 64) == 0 ? launch_gemm2_t<2>(pool, o, st) : launch_gemm2_t<1>(pool, o, st);
+    return (o.Kc % 64) == 0 ? launch_gemm2_t<2, sm100::EPI_LAYER>(pool, o, st) : launch_gemm2_t<1, sm100::EPI_LAYER>(pool, o, st);
+}
+
+int head_pairs(const marlaas_pool* pool) { return pool->sm_count / 2; }
+
+marlaas_status_t launch_head_softmax(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st) {
+    return (o.Kc % 64) == 0 ? launch_gemm2_t<2, sm100::EPI_SOFTMAX>(pool, o, st, &h) : launch_gemm2_t<1, sm100::EPI_SOFTMAX>(pool, o, st, &h);
+}
+
+marlaas_status_t launch_head_grad(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st) {
+    return (o.Kc % 64) == 0 ? launch_gemm2_t<2, sm100::EPI_GRAD>(pool, o, st, &h) : launch_gemm2_t<1, sm100::EPI_GRAD>(pool, o, st, &h);
 }
 
 }  // namespace marlaas

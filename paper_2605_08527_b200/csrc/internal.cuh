@@ -209,6 +209,41 @@ marlaas_status_t launch_gemm_sm100(const marlaas_pool* pool, const GemmOperands&
 bool gemm2_sm100_eligible(const marlaas_pool* pool, int64_t M);
 marlaas_status_t launch_gemm2_sm100(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st);
 
+// The vocabulary head's cross entropy (head.cu), whose products run gemm2_sm100.cu's main loop: the rows are the batch's tokens
+// that count, in order, of which this launch takes those from row0 on.
+struct HeadEpilogue {
+    const int32_t* active;             // [1] tokens that count
+    int row0;
+    const int32_t* targets;            // [all rows]
+    const int32_t* perm;               // [all rows] the rows' tokens
+    float k2;                          // inv_temperature / ln 2
+    int keep;                          // the exponentials are wanted
+    float2* part;                      // [rows][part_ld] (reference, sum of exponentials) of every 256-column tile
+    int part_ld;
+    float* target_logit;               // [rows] in units of log 2
+    const float* coef;                 // [rows] factor of a row's gradient
+    float* partial;                    // [max_items][256][256]
+    int max_items;
+    int pairs;                         // CTA pairs of the device
+};
+// Ranges of the vocabulary that the gradient's product is cut into: the fewest k-steps of the busiest pair, where a further
+// range costs its tiles' way through memory (512 KB at a pair's share of the bandwidth is about 22 steps; a third of it shows
+// beside the main loop), and no range is shorter than 16 steps of 64.
+__host__ __device__ inline int head_splits(const HeadEpilogue& h, int tiles, int steps) {
+    int best = 1;
+    int64_t least = -1;
+    for (int s = 1; s <= 32; ++s) {
+        if (s > 1 && (tiles * s > h.max_items || steps < 16 * s)) break;
+        const int64_t cost = (int64_t)((tiles * s + h.pairs - 1) / h.pairs) * ((steps + s - 1) / s + 4) + (s > 1 ? (int64_t)s * tiles * 8 / h.pairs : 0);
+        if (least < 0 || cost < least) { least = cost; best = s; }
+    }
+    return best;
+}
+int head_pairs(const marlaas_pool* pool);
+// E = exponentials of (x W) (o.C, when kept); dx = E W^T over the ranges
+marlaas_status_t launch_head_softmax(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st);
+marlaas_status_t launch_head_grad(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st);
+
 // decode_sm100.cu: the whole forward for batches of at most 1024 tokens (two overlapping kernels).
 // S < 0: ws.tok_slot already holds the per-token slots.
 bool decode_sm100_eligible(const marlaas_pool* pool, int64_t T);
