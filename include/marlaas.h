@@ -398,6 +398,37 @@ marlaas_status_t marlaas_adapter_pool_store(const marlaas_pool_t* pool, const vo
 enum { MARLAAS_MAX_NORM_WIDTH = 16384, MARLAAS_MAX_HEAD_WIDTH = 65536 };
 enum { MARLAAS_HEAD_STATS = 4 };                           /* columns of marlaas_head_cross_entropy's stats */
 
+/* The layer with dropout in its adapters, for training.  With m_i the mask of token i (a truth value per element of x_i),
+ * t its slot, p_t the tenant's rate and s'_t = s_t / (1 - p_t):
+ *     y_i  = x_i W + s'_t ((m_i o x_i) A_t) B_t
+ *     dx_i = dy_i W^T + s'_t m_i o ((dy_i B_t^T) A_t^T)
+ *     dA_t = s'_t sum (m_i o x_i)^T (dy_i B_t^T)           dB_t = s'_t sum ((m_i o x_i) A_t)^T dy_i
+ * Masks are never stored: every pass computes them from the generator.  Philox-4x32 of seven rounds (Salmon, Moraes, Dror and
+ * Shaw, 2011) with the key (low, high word of seed) and the counter (c, i, low, high word of offset) gives four words, whose
+ * low and high halves in turn are the 16-bit numbers of the elements 8 c to 8 c + 7 of token i; an element is dropped if its
+ * number is below round(65536 p_t), and p_t in the formulas is that number over 65536.  The backward pass takes the seed, the
+ * offset and the rates of its forward pass; another step or another projection takes another offset.  A pool over several
+ * projections drops the same elements for all of them.
+ * rates: fp32 [capacity] on the device, per slot; a rate that is not above 0 (or a NaN) drops nothing, one of 1 or more drops
+ * everything (the adapter then gives nothing and gets zero gradients).  What a dropped element holds does not matter to the
+ * adapters.  With rates of 0 the results are marlaas_lora_forward's and marlaas_lora_backward's up to the order of sums.
+ * Otherwise as those two calls, with h_save = (m_i o x_i) A_t; of the flags, HOST_TABLE, VALIDATE_SYNC and (backward)
+ * ACCUMULATE apply.  Workspace: marlaas_lora_dropout_workspace_bytes, for both.  Adapter gradients of pools of more than 64
+ * slots cannot be captured. */
+typedef struct marlaas_dropout {
+    const float* rates;
+    uint64_t seed, offset;
+} marlaas_dropout_t;
+size_t marlaas_lora_dropout_workspace_bytes(const marlaas_pool_t* pool, int64_t T);
+marlaas_status_t marlaas_lora_forward_dropout(marlaas_pool_t* pool, int64_t T, const void* x, int64_t ldx, const void* W, int64_t ldw, void* y,
+                                              int64_t ldy, const marlaas_segments_t* seg, const marlaas_dropout_t* drop, float* h_save,
+                                              void* workspace, size_t workspace_bytes, uint32_t flags, void* cuda_stream);
+marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, const void* x, int64_t ldx, const void* W, int64_t ldw,
+                                               const void* dy, int64_t lddy, void* dx, int64_t lddx, float* const* dA_slots,
+                                               float* const* dB_slots, const marlaas_segments_t* seg, const marlaas_dropout_t* drop,
+                                               const float* h_saved, void* workspace, size_t workspace_bytes, uint32_t flags,
+                                               void* cuda_stream);
+
 /* Layer norm whose gain and bias are each tenant's own, over rows of d elements (d a multiple of 8 up to
  * MARLAAS_MAX_NORM_WIDTH; x and y are bf16 with leading dimensions ldx, ldy).  With t the slot of token i,
  *     y_i = (x_i - mean_i) rstd_i gain_t + bias_t,     rstd_i = 1 / sqrt(var_i + eps)

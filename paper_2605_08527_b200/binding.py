@@ -57,7 +57,8 @@ EXPORTED_SYMBOLS = [
     "marlaas_policy_workspace_bytes", "marlaas_group_advantages", "marlaas_token_logprobs", "marlaas_policy_loss",
     "marlaas_adamw_compact_state_bytes", "marlaas_adapter_pool_adamw_compact_commit", "marlaas_adamw_compact_state_export",
     "marlaas_adapter_pool_store", "marlaas_layer_norm_workspace_bytes", "marlaas_layer_norm", "marlaas_layer_norm_backward",
-    "marlaas_head_cross_entropy_workspace_bytes", "marlaas_head_cross_entropy",
+    "marlaas_head_cross_entropy_workspace_bytes", "marlaas_head_cross_entropy", "marlaas_lora_dropout_workspace_bytes",
+    "marlaas_lora_forward_dropout", "marlaas_lora_backward_dropout",
 ]
 
 
@@ -75,6 +76,10 @@ class marlaas_adamw_t(ctypes.Structure):
 class marlaas_policy_loss_t(ctypes.Structure):
     _fields_ = [("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("kl_coef", ctypes.c_float),
                 ("entropy_coef", ctypes.c_float), ("inv_temperature", ctypes.c_float), ("grad_scale", ctypes.c_float)]
+
+
+class marlaas_dropout_t(ctypes.Structure):
+    _fields_ = [("rates", ctypes.c_void_p), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64)]
 
 
 class marlaas_segments_t(ctypes.Structure):
@@ -175,6 +180,13 @@ def load_library() -> ctypes.CDLL:
     L.marlaas_head_cross_entropy.restype = i32
     L.marlaas_head_cross_entropy.argtypes = [vp, i64, i64, i64, vp, i64, vp, i64, vp, P(marlaas_segments_t), vp, f32, f32, vp, i64, vp, vp,
                                              vp, sz, u32, vp]
+    L.marlaas_lora_dropout_workspace_bytes.restype = sz
+    L.marlaas_lora_dropout_workspace_bytes.argtypes = [vp, i64]
+    L.marlaas_lora_forward_dropout.restype = i32
+    L.marlaas_lora_forward_dropout.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, P(marlaas_segments_t), P(marlaas_dropout_t), vp, vp, sz, u32, vp]
+    L.marlaas_lora_backward_dropout.restype = i32
+    L.marlaas_lora_backward_dropout.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, P(marlaas_segments_t), P(marlaas_dropout_t),
+                                                vp, vp, sz, u32, vp]
     L.marlaas_last_error.restype = ctypes.c_char_p
     L.marlaas_last_error.argtypes = []
     L.marlaas_kernel_launch_count.restype = u64
@@ -780,6 +792,55 @@ def _bf16_rows(t: torch.Tensor, T: int, cols: int, name: str, device: int) -> in
     assert t.dtype is torch.bfloat16 and t.dim() == 2 and t.shape[0] == T and t.shape[1] == cols and t.get_device() == device, name
     assert cols == 1 or t.stride(1) == 1, name
     return t.stride(0) if T > 1 else -(-cols // 8) * 8
+
+
+def marlaas_lora_dropout_workspace_bytes(pool: AdapterPool, T: int) -> int:
+    return int(load_library().marlaas_lora_dropout_workspace_bytes(pool.handle, T))
+
+
+def _drop(pool: AdapterPool, rates: torch.Tensor, seed: int, offset: int) -> marlaas_dropout_t:
+    assert 0 <= seed < 1 << 64 and 0 <= offset < 1 << 64, "seed and offset are 64-bit numbers"
+    return marlaas_dropout_t(_f32(rates, pool.capacity, "rates", pool.index), seed, offset)
+
+
+def marlaas_lora_forward_dropout(pool: AdapterPool, x: torch.Tensor, W: torch.Tensor, seg: Segments, rates: torch.Tensor, seed: int,
+                                 offset: int = 0, y: Optional[torch.Tensor] = None, h_save: Optional[torch.Tensor] = None,
+                                 workspace: Optional[torch.Tensor] = None, flags: int = 0, stream=None) -> torch.Tensor:
+    """marlaas_lora_forward with dropout in the adapters: `rates` fp32 [capacity] per slot, masks from (seed, offset)."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_lora_forward_dropout, pool, x, W, seg, rates, seed, offset, y, h_save, workspace, flags)
+    T, dev = x.shape[0], pool.index
+    y = torch.empty((T, pool.d_out), dtype=torch.bfloat16, device=x.device) if y is None else y
+    handle = torch._C._cuda_getCurrentRawStream(dev)
+    ws = pool.step_workspace(marlaas_lora_dropout_workspace_bytes(pool, T), handle) if workspace is None else workspace
+    drop = _drop(pool, rates, seed, offset)
+    _check(load_library().marlaas_lora_forward_dropout(
+        pool.handle, T, x.data_ptr(), _bf16_rows(x, T, pool.d_in, "x", dev), W.data_ptr(), _bf16_rows(W, pool.d_in, pool.d_out, "W", dev),
+        y.data_ptr(), _bf16_rows(y, T, pool.d_out, "y", dev), seg.ref, ctypes.byref(drop),
+        None if h_save is None else _f32(h_save, pool.n_parts * T * pool.rank_stride, "h_save", dev), ws.data_ptr(), ws.numel(),
+        flags | seg.flags, handle))
+    return y
+
+
+def marlaas_lora_backward_dropout(pool: AdapterPool, x: Optional[torch.Tensor], W: torch.Tensor, dy: torch.Tensor, seg: Segments,
+                                  rates: torch.Tensor, seed: int, offset: int = 0, dx: Optional[torch.Tensor] = None,
+                                  dA: Optional[Sequence[Optional[torch.Tensor]]] = None, dB: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                                  h_saved: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, flags: int = 0,
+                                  stream=None) -> None:
+    """marlaas_lora_backward with the masks of the forward call (the same rates, seed and offset)."""
+    if stream is not None:
+        return _on_stream(stream, marlaas_lora_backward_dropout, pool, x, W, dy, seg, rates, seed, offset, dx, dA, dB, h_saved, workspace, flags)
+    T, dev = dy.shape[0], pool.index
+    handle = torch._C._cuda_getCurrentRawStream(dev)
+    ws = pool.step_workspace(marlaas_lora_dropout_workspace_bytes(pool, T), handle) if workspace is None else workspace
+    drop = _drop(pool, rates, seed, offset)
+    _check(load_library().marlaas_lora_backward_dropout(
+        pool.handle, T, None if x is None else x.data_ptr(), 0 if x is None else _bf16_rows(x, T, pool.d_in, "x", dev), W.data_ptr(),
+        _bf16_rows(W, pool.d_in, pool.d_out, "W", dev), dy.data_ptr(), _bf16_rows(dy, T, pool.d_out, "dy", dev),
+        None if dx is None else dx.data_ptr(), 0 if dx is None else _bf16_rows(dx, T, pool.d_in, "dx", dev),
+        _ptr_table(dA, pool.capacity), _ptr_table(dB, pool.capacity), seg.ref, ctypes.byref(drop),
+        None if h_saved is None else _f32(h_saved, pool.n_parts * T * pool.rank_stride, "h_saved", dev), ws.data_ptr(), ws.numel(),
+        flags | seg.flags, handle))
 
 
 def marlaas_layer_norm_workspace_bytes(pool: AdapterPool, T: int, d: int, num_segments: int, backward: bool) -> int:

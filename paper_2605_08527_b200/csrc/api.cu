@@ -57,7 +57,7 @@ Workspace carve_workspace(const marlaas_pool* pool, int64_t T, void* base) {
 
 static bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
 
-static marlaas_status_t check_matrix(const char* fn, const char* name, const void* p, int64_t ld, int64_t cols) {
+marlaas_status_t check_matrix(const char* fn, const char* name, const void* p, int64_t ld, int64_t cols) {
     if (!p) return fail(MARLAAS_ERR_INVALID_ARG, "%s: %s is NULL", fn, name);
     if (!aligned16(p)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: %s is not 16-byte aligned", fn, name);
     if (ld < cols || (ld % 8) != 0)
@@ -115,7 +115,7 @@ static marlaas_status_t make_tok_slot(const marlaas_pool* pool, int64_t T, const
     return launch_tok_slot(pool, T, seg->num_segments, seg->seg_offsets, seg->seg_slot, tok_slot, st);
 }
 
-static marlaas_status_t make_plan(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, uint32_t flags,
+marlaas_status_t make_plan(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, uint32_t flags,
                                   const std::vector<int32_t>& host_tok_slot, const Workspace& ws, cudaStream_t st) {
     if (T <= 0) return MARLAAS_OK;
     if (flags & MARLAAS_FLAG_HOST_TABLE) {
@@ -128,9 +128,8 @@ static marlaas_status_t make_plan(const marlaas_pool* pool, int64_t T, const mar
 
 // Shrink for the tensor-core path: batches with several 128-token tiles go through the tcgen05 kernel, small
 // (decode-shaped) batches through the per-token gather kernel, which spreads over more SMs.
-static marlaas_status_t shrink(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D,
-                               const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st,
-                               bool out_is_zero = false) {
+marlaas_status_t shrink(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D, const bf16* store, int64_t sld,
+                        const Workspace& ws, float* out, cudaStream_t st, bool out_is_zero) {
     if (T >= 512 && shrink_split_sm100_eligible(pool, T, D))
         return launch_shrink_split_sm100(pool, T, src, ld, D, store, sld, ws, out, st, out_is_zero);
     if (T >= 512) return launch_shrink_sm100(pool, T, src, ld, D, store, sld, ws, out, st);
@@ -139,7 +138,7 @@ static marlaas_status_t shrink(const marlaas_pool* pool, int64_t T, const bf16* 
 
 // Projection p of a pool over several: the plan (per-token slots, unit lists, gradient block lists) is shared, h, g and hd
 // are planes of T rows each.
-static Workspace part_workspace(const marlaas_pool* pool, const Workspace& ws, int p, int64_t T) {
+Workspace part_workspace(const marlaas_pool* pool, const Workspace& ws, int p, int64_t T) {
     Workspace w = ws;
     w.h = ws.h + (size_t)p * T * pool->RP;
     w.g = ws.g + (size_t)p * T * pool->RP;
@@ -151,6 +150,80 @@ static void set_parts(const marlaas_pool* pool, GemmOperands* o, bool all_parts)
     o->parts = pool->P;
     o->all_parts = all_parts;
     for (int p = 0; p < pool->P; ++p) o->part_end[p] = pool->part_begin[p + 1];
+}
+
+// The product of the forward pass with its low-rank term (plan and hd in the workspace), and of dx.
+void forward_operands(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* W, int64_t ldw, bf16* y, int64_t ldy,
+                      const Workspace& ws, GemmOperands* o) {
+    o->M = T; o->Nout = pool->N; o->Kc = pool->K;
+    o->A = x; o->lda = ldx;
+    o->B = W; o->ldb = ldw; o->b_mn = true;
+    o->C = y; o->ldc = ldy;
+    o->XA = ws.hd; o->xa_cols = (int64_t)ws.umax * 16;
+    o->XB = pool->d_Bs; o->xb_rows = (int64_t)pool->cap * pool->RP; o->xb_ld = pool->ldB;
+    o->tile_nunits = ws.tile_nunits; o->tile_units = ws.tile_units; o->umax = ws.umax;
+    set_parts(pool, o, false);
+}
+void backward_operands(const marlaas_pool* pool, int64_t T, const bf16* W, int64_t ldw, const bf16* dy, int64_t lddy, bf16* dx, int64_t lddx,
+                       const Workspace& ws, GemmOperands* o) {
+    o->M = T; o->Nout = pool->K; o->Kc = pool->N;
+    o->A = dy; o->lda = lddy;
+    o->B = W; o->ldb = ldw; o->b_mn = false;
+    o->C = dx; o->ldc = lddx;
+    o->XA = ws.hd; o->xa_cols = (int64_t)ws.umax * 16;
+    o->XB = pool->d_At; o->xb_rows = (int64_t)pool->P * pool->cap * pool->RP; o->xb_ld = pool->K;
+    o->tile_nunits = ws.tile_nunits; o->tile_units = ws.tile_units; o->umax = ws.umax;
+    set_parts(pool, o, true);      // the low-rank term of dx sums over every projection
+}
+
+// Pools of more than 64 slots copy the gradients' pointer tables by memcpy nodes, whose sources do not outlive the call.
+marlaas_status_t reject_captured_tables(const char* fn, const marlaas_pool* pool, cudaStream_t st) {
+    if (pool->cap <= 64) return MARLAAS_OK;
+    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+    MARLAAS_CUDA_TRY(cudaStreamIsCapturing(st, &cs));
+    if (cs != cudaStreamCaptureStatusNone)
+        return fail(MARLAAS_ERR_INVALID_ARG, "%s: adapter gradients of a pool of more than 64 slots cannot be captured", fn);
+    return MARLAAS_OK;
+}
+
+// dA and dB of all slots on one stream, for the plan, g and (T > 0) h in the workspace or as saved: what marlaas_lora_backward
+// does when it does not run them beside the dx product.
+marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
+                                   float* const* dA_slots, float* const* dB_slots, const marlaas_segments_t* seg, const float* h,
+                                   const Workspace& ws, bool acc, cudaStream_t st) {
+    marlaas_status_t rc;
+    const int NP = pool->P;
+    const size_t plane = (size_t)T * pool->RP;
+    const bool tc_grad = grad_sm100_eligible(pool, T);
+    // as in marlaas_lora_backward: the copies fit for certain, and with 64 slots at most the tables travel with the launches
+    const bool fits = tc_grad && cdiv(T, 64) + (int64_t)seg->num_segments <= (int64_t)ws.max_copies;
+    const bool inline_tables = fits && pool->cap <= 64;
+    const int32_t* run_flag = tc_grad ? ws.gflag : nullptr;
+    if (tc_grad && (rc = launch_grad_plan(pool, T, ws, st)) != MARLAAS_OK) return rc;
+    if (!fits && (rc = launch_slot_sort(pool, T, ws.tok_slot, ws.slot_count, ws.slot_offset, ws.perm, st, run_flag)) != MARLAAS_OK) return rc;
+    std::vector<float*> part((size_t)pool->cap, nullptr);
+    for (int p = 0; p < NP; ++p) {
+        if (tc_grad && p > 0) MARLAAS_CUDA_TRY(cudaMemsetAsync(ws.gflag + 2, 0, 2 * sizeof(int32_t), st));
+        const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
+        for (int which = 0; which < 2; ++which) {       // dB, then dA
+            float* const* all = which == 0 ? dB_slots : dA_slots;
+            if (!all) continue;
+            for (int s = 0; s < pool->cap; ++s) {       // block p of dA_t is [K][r_t], block p of dB_t is [r_t][N_p]
+                const size_t r = (size_t)pool->slots[s].rank;
+                part[s] = all[s] ? all[s] + (which == 0 ? r * (size_t)c0 : (size_t)p * pool->K * r) : nullptr;
+            }
+            float** dev = which == 0 ? ws.dB_ptrs : ws.dA_ptrs;
+            const bf16* src = which == 0 ? dy + c0 : x;
+            const int64_t ld = which == 0 ? lddy : ldx, C = which == 0 ? Np : pool->K;
+            const float* r = which == 0 ? h + p * plane : ws.g + p * plane;
+            if (!inline_tables)
+                MARLAAS_CUDA_TRY(cudaMemcpyAsync(dev, part.data(), sizeof(float*) * (size_t)pool->cap, cudaMemcpyHostToDevice, st));
+            if (tc_grad && (rc = launch_grad_sm100(pool, T, C, src, ld, r, dev, part.data(), which == 1, acc, ws, st, ws.hm)) != MARLAAS_OK) return rc;
+            if (!fits && (rc = launch_grad_reduce(pool, C, src, ld, r, ws.perm, ws.slot_offset, dev, which == 1, acc, st, run_flag)) != MARLAAS_OK)
+                return rc;
+        }
+    }
+    return MARLAAS_OK;
 }
 
 // Host tables are copied from temporaries of the call: a stream capture would keep pointers into them for its replays.
@@ -287,14 +360,7 @@ static marlaas_status_t forward_impl(marlaas_pool_t* pool, int64_t T, const void
             }
         }
         GemmOperands o;
-        o.M = T; o.Nout = pool->N; o.Kc = pool->K;
-        o.A = (const bf16*)x; o.lda = ldx;
-        o.B = (const bf16*)W; o.ldb = ldw; o.b_mn = true;
-        o.C = (bf16*)y; o.ldc = ldy;
-        o.XA = ws.hd; o.xa_cols = (int64_t)ws.umax * 16;
-        o.XB = pool->d_Bs; o.xb_rows = (int64_t)pool->cap * pool->RP; o.xb_ld = pool->ldB;
-        o.tile_nunits = ws.tile_nunits; o.tile_units = ws.tile_units; o.umax = ws.umax;
-        set_parts(pool, &o, false);
+        forward_operands(pool, T, (const bf16*)x, ldx, (const bf16*)W, ldw, (bf16*)y, ldy, ws, &o);
         {
             TimedLaunch timed(pool, st);
             rc = (NP > 1 || gemm2_sm100_eligible(pool, T)) ? launch_gemm2_sm100(pool, o, st) : launch_gemm_sm100(pool, o, st);
@@ -484,14 +550,7 @@ marlaas_status_t marlaas_lora_backward(marlaas_pool_t* pool, int64_t T, const vo
     }
     if (T > 0 && dx && tc_path) {
         GemmOperands o;
-        o.M = T; o.Nout = pool->K; o.Kc = pool->N;
-        o.A = (const bf16*)dy; o.lda = lddy;
-        o.B = (const bf16*)W; o.ldb = ldw; o.b_mn = false;
-        o.C = (bf16*)dx; o.ldc = lddx;
-        o.XA = ws.hd; o.xa_cols = (int64_t)ws.umax * 16;
-        o.XB = pool->d_At; o.xb_rows = (int64_t)NP * pool->cap * pool->RP; o.xb_ld = pool->K;
-        o.tile_nunits = ws.tile_nunits; o.tile_units = ws.tile_units; o.umax = ws.umax;
-        set_parts(pool, &o, true);      // the low-rank term of dx sums over every projection
+        backward_operands(pool, T, (const bf16*)W, ldw, (const bf16*)dy, lddy, (bf16*)dx, lddx, ws, &o);
         TimedLaunch timed(pool, st);
         rc = gemm2 ? launch_gemm2_sm100(pool, o, st) : launch_gemm_sm100(pool, o, st);
         if (rc != MARLAAS_OK) return rc;

@@ -1,0 +1,38 @@
+// Masks of the adapters' dropout: 16 random bits per element from a counter-based generator, so that every kernel that needs an
+// element's mask computes it anew and none is stored.  Philox-4x32 of seven rounds (Salmon, Moraes, Dror and Shaw, "Parallel
+// random numbers: as easy as 1, 2, 3", 2011, who name seven as the fewest that pass their tests) on the counter
+// (column / 8, token, offset) under the seed gives 128 bits: eight columns of a token.
+#pragma once
+
+#include "internal.cuh"
+
+namespace marlaas {
+
+__device__ __forceinline__ uint4 drop_bits(const DropKey& k, uint32_t vec, uint32_t token) {
+    uint32_t c0 = vec, c1 = token, c2 = k.o0, c3 = k.o1, k0 = k.k0, k1 = k.k1;
+#pragma unroll
+    for (int r = 0; r < 7; ++r) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+
+// Eight bf16 elements with the dropped ones (16 bits below `limit`) set to 0, whatever they hold.
+__device__ __forceinline__ uint4 drop_apply(uint4 x, const uint4& bits, uint32_t limit) {
+    uint32_t* v = &x.x;
+    const uint32_t* b = &bits.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = (b[i] & 0xffffu) >= limit ? 0x0000ffffu : 0u, hi = (b[i] >> 16) >= limit ? 0xffff0000u : 0u;
+        v[i] &= lo | hi;
+    }
+    return x;
+}
+
+}  // namespace marlaas

@@ -268,14 +268,6 @@ static HeadWorkspace carve_head(int64_t T, int64_t d, int64_t V, int32_t S, bool
 
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
-static marlaas_status_t check_matrix(const char* fn, const char* name, const void* p, int64_t ld, int64_t cols) {
-    if (!p || misaligned(p, 16)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: %s is NULL or not 16-byte aligned", fn, name);
-    if (ld < cols || ld % 8 != 0 || ld >= (1ll << 31))
-        return fail(MARLAAS_ERR_INVALID_ARG, "%s: leading dimension of %s (%lld) must be >= %lld and a multiple of 8", fn, name,
-                    (long long)ld, (long long)cols);
-    return MARLAAS_OK;
-}
-
 static bool head_sizes_ok(int64_t T, int64_t d, int64_t V) {
     return T >= 0 && T < (1ll << 31) && d >= 8 && d <= MARLAAS_MAX_HEAD_WIDTH && d % 8 == 0 && V >= 1 && V <= MARLAAS_MAX_VOCABULARY;
 }

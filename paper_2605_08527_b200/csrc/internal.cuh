@@ -314,6 +314,29 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
                                    bool accumulate, const Workspace& ws, cudaStream_t st, bf16* hm, int phases = GRAD_PHASE_COPIES | GRAD_PHASE_REDUCE);
 // host_ptrs: the same table in host memory; pools of at most 64 slots pass it with the launch and never read out_ptrs
 
+// api.cu: the layer's steps, shared with its form with dropout (dropout.cu)
+marlaas_status_t check_matrix(const char* fn, const char* name, const void* p, int64_t ld, int64_t cols);
+marlaas_status_t make_plan(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, uint32_t flags,
+                           const std::vector<int32_t>& host_tok_slot, const Workspace& ws, cudaStream_t st);
+marlaas_status_t shrink(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D, const bf16* store, int64_t sld,
+                        const Workspace& ws, float* out, cudaStream_t st, bool out_is_zero = false);
+Workspace part_workspace(const marlaas_pool* pool, const Workspace& ws, int p, int64_t T);
+void forward_operands(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* W, int64_t ldw, bf16* y, int64_t ldy,
+                      const Workspace& ws, GemmOperands* o);
+void backward_operands(const marlaas_pool* pool, int64_t T, const bf16* W, int64_t ldw, const bf16* dy, int64_t lddy, bf16* dx, int64_t lddx,
+                       const Workspace& ws, GemmOperands* o);
+marlaas_status_t reject_captured_tables(const char* fn, const marlaas_pool* pool, cudaStream_t st);
+marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
+                                   float* const* dA_slots, float* const* dB_slots, const marlaas_segments_t* seg, const float* h,
+                                   const Workspace& ws, bool acc, cudaStream_t st);
+// pool.cu: the pool with other scales of its slots, for the kernel launchers alone (no streams)
+void scaled_view(const marlaas_pool* pool, const float* d_scale, marlaas_pool* view);
+
+// The counter-based generator's key and the counter's fixed half (dropout.cuh).
+struct DropKey {
+    uint32_t k0, k1, o0, o1;
+};
+
 // vocab_rows.cu: one pass over rows of logits (softmax statistics, the policy loss's per-token terms, the gradient)
 struct PolicyTerms {           // what a token adds to its tenant's stats
     float loss, pg, kl, entropy, ratio, clipped, weight, count;

@@ -407,14 +407,6 @@ static marlaas_status_t launch_norm_backward_t(const marlaas_pool* pool, const N
 
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
-static marlaas_status_t check_matrix(const char* fn, const char* name, const void* p, int64_t ld, int64_t d) {
-    if (!p || misaligned(p, 16)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: %s is NULL or not 16-byte aligned", fn, name);
-    if (ld < d || ld % 8 != 0 || ld >= (1ll << 31))
-        return fail(MARLAAS_ERR_INVALID_ARG, "%s: leading dimension of %s (%lld) must be >= %lld and a multiple of 8", fn, name,
-                    (long long)ld, (long long)d);
-    return MARLAAS_OK;
-}
-
 // An output matrix may be an input matrix itself, with the same leading dimension; any other overlap is refused.
 static marlaas_status_t check_overlap(const char* fn, const char* name, const void* out, int64_t ldo, const void* in, int64_t ldi,
                                       int64_t T, int64_t d) {

@@ -75,6 +75,14 @@ void part_view(const marlaas_pool* pool, int p, marlaas_pool* v) {
     v->slots = pool->slots;
 }
 
+void scaled_view(const marlaas_pool* pool, const float* d_scale, marlaas_pool* v) {
+    *v = *pool;
+    v->d_scale = const_cast<float*>(d_scale);
+    v->timing = false;
+    v->side = nullptr;
+    v->ev_fork = v->ev_join = nullptr;
+}
+
 StorageLayout storage_layout(int64_t K, int64_t N, int32_t RP, int32_t cap, int32_t parts) {
     StorageLayout L;
     size_t o = 0;
