@@ -15,8 +15,8 @@
 //
 // The vocabulary head's cross entropy (head.cu) runs the same main loop with epilogues of its own and a number of rows that
 // only the device knows:
-//   EPI_SOFTMAX  a tile of logits leaves the SM as its rows' largest logit and sum of exponentials, the target's logit, and
-//                (for a gradient) the exponentials in bf16; the logits themselves are never written
+//   EPI_SOFTMAX  a tile of logits leaves the SM as its rows' largest logit, sum of exponentials and target's logit, and (for a
+//                gradient) the exponentials in bf16; the logits themselves are never written
 //   EPI_GRAD     the product over the vocabulary is cut along it into `splits` ranges, so that few row tiles still fill the
 //                SMs; each (range, tile) leaves an fp32 tile, or the output itself when there is one range
 #include <string.h>
@@ -150,8 +150,8 @@ __device__ __forceinline__ int head_rows(const HeadEpilogue& h, int most) {
     return min(most, max(0, *h.active - h.row0));
 }
 
-// A row's 256 logits of one tile (the thread's lane of tensor memory at trow), in units of log 2 and of 1 / inv_temperature:
-// the largest, then the sum of exponentials relative to it.  Two passes over tensor memory, whose reads cost less than keeping
+// A row's 256 logits of one tile (the thread's lane of tensor memory at trow), in units of log 2: the largest, then the sum of
+// the exponentials relative to it but for the target's.  Two passes over tensor memory, whose reads cost less than keeping
 // 256 values.  The reference is rounded once and used as rounded everywhere, so its rounding cancels.
 __device__ __forceinline__ void head_softmax_tile(const HeadEpilogue& h, uint32_t trow, int row, bool on, int n0, int V, int n_idx, bf16* E,
                                                   int64_t lde) {
@@ -183,8 +183,12 @@ __device__ __forceinline__ void head_softmax_tile(const HeadEpilogue& h, uint32_
         tc_wait_ld();
         if (t >= c && t < c + 32) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-                if (t == c + e) h.target_logit[row] = __uint_as_float(v[e]) * h.k2;
+            for (int e = 0; e < 32; ++e) {
+                if (t == c + e) {
+                    h.target_logit[row] = __uint_as_float(v[e]) * h.k2;
+                    v[e] = 0xff800000u;
+                }
+            }
         }
         uint32_t o[16];
 #pragma unroll

@@ -8,7 +8,8 @@
 //   2. x W tile by tile in tensor memory; a tile leaves it as a pair (reference, sum of exponentials) per row, and for the
 //      gradient as exponentials in bf16, relative to the row's reference in the tile: their error is 2^-8 of each probability,
 //      where rounding the logits would make it 2^-8 of a logit
-//   3. a row's pairs give its log-sum-exp; the exponentials become p - e_y in place (p_y - 1 from the fp32 logit: it cancels)
+//   3. a row's pairs give the sum R of the exponentials of all entries but the target, and logp = -log(1 + R / exp z_y), which
+//      keeps its digits however sure the model is; the exponentials become p - e_y in place
 //   4. times W^T, cut along the vocabulary so that few rows fill the SMs too; the row's factor enters in fp32
 // The exponentials of at most HEAD_PIECE_BYTES are held at a time: larger batches go through steps 2 to 4 in pieces of rows.
 #include <math.h>
@@ -43,7 +44,7 @@ struct HeadArgs {
     float* row_coef;                        // [T]
     bf16* E; int64_t lde;
     float2* part;
-    float* target_logit;
+    float* target_logit;                    // [piece] in units of log 2
     float4* terms;                          // [T] or NULL
     float* logp;                            // [T] or NULL
     bf16* dx; int64_t lddx;                 // or NULL
@@ -106,8 +107,12 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_rows(const HeadArgs a, in
         s += q.y != 0.f ? q.y * exp2f(q.x - m) : 0.f;
     }
     s = all(s, false);
-    const bool none = s == 0.f;                 // no logit above -inf: no distribution
-    const float logp = none ? 0.f : ((a.target_logit[row] - m) - log2f(s)) * HEAD_LN2;
+    // m, s: reference and sum of the others' exponentials; zy, the target's logit, may be anything beside them
+    const float zy = a.target_logit[row], top = s == 0.f ? zy : fmaxf(m, zy), gap = m - zy;
+    const bool none = s == 0.f && zy == -INFINITY;      // no logit above -inf: no distribution
+    float logp = s == 0.f ? zy - zy : gap < 30.f ? -log1pf(s * exp2f(gap)) : -(gap * HEAD_LN2 + logf(s + exp2f(-gap)));
+    if (!(zy < INFINITY)) logp = NAN;
+    if (none) logp = 0.f;
     if (tid == 0) {
         const int64_t i = a.perm[row0 + row];
         const float w = a.weight ? a.weight[i] : 1.f;
@@ -115,10 +120,10 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_rows(const HeadArgs a, in
         if (a.terms) a.terms[i] = make_float4(-w * logp, w, -logp, 1.f);
     }
     if (!GRAD) return;
-    const float inv = none ? 0.f : 1.f / s;
+    const float inv = none ? 0.f : 1.f / (s * exp2f(s == 0.f ? 0.f : m - top) + exp2f(zy - top));
     for (int j = tid; j < a.NT; j += HEAD_THREADS) {
         const float2 q = part[j];
-        s_f[j] = q.y != 0.f ? exp2f(q.x - m) * inv : 0.f;
+        s_f[j] = q.y != 0.f ? exp2f(q.x - top) * inv : 0.f;
     }
     __syncthreads();
     const int y = a.row_target[row0 + row], nvec = (a.V + 7) / 8;

@@ -218,7 +218,7 @@ struct HeadEpilogue {
     const int32_t* perm;               // [all rows] the rows' tokens
     float k2;                          // inv_temperature / ln 2
     int keep;                          // the exponentials are wanted
-    float2* part;                      // [rows][part_ld] (reference, sum of exponentials) of every 256-column tile
+    float2* part;                      // [rows][part_ld] (reference, sum of exponentials but the target's) of every 256-column tile
     int part_ld;
     float* target_logit;               // [rows] in units of log 2
     const float* coef;                 // [rows] factor of a row's gradient
