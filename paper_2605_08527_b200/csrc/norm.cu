@@ -63,149 +63,218 @@ __device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
     f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
-__device__ __forceinline__ float warp_sum(float v) {
+// ---- both passes ----
+// A group of W warps takes a run of rows, B at a time; a thread keeps the same NV x 8 columns throughout, so that its tenant's
+// parameters (and the sums for their gradients) stay in registers until the tenant changes: read per row, they were twice the
+// bytes of the row itself.  The next batches of rows are on their way as asynchronous copies into shared memory that only the
+// copying thread reads, so that the only barriers are those of the rows' sums, of four values at a time.
+constexpr int NORM_MAX_GROUPS = 8;
+struct GroupSums {
+    float v[2][NORM_MAX_GROUPS][4][32];
+};
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Four sums over a group's threads.  In the warp, lanes hand over half of their values in each of the first two steps: six
+// shuffles instead of twenty; eight lanes then hold one value each.  The same tree in every call.
+__device__ __forceinline__ void group_sum4(float (&v)[4], GroupSums& s, int& par, int W, int g, int wg, int lane) {
+    const bool hi = lane & 16, mid = lane & 8;
+    float a0 = hi ? v[2] : v[0], a1 = hi ? v[3] : v[1];
+    a0 += __shfl_xor_sync(0xffffffffu, hi ? v[0] : v[2], 16);
+    a1 += __shfl_xor_sync(0xffffffffu, hi ? v[1] : v[3], 16);
+    float x = (mid ? a1 : a0) + __shfl_xor_sync(0xffffffffu, mid ? a0 : a1, 8);
+    x += __shfl_xor_sync(0xffffffffu, x, 4);
+    x += __shfl_xor_sync(0xffffffffu, x, 2);
+    x += __shfl_xor_sync(0xffffffffu, x, 1);
+    const int k = lane >> 3;                    // the value that this lane holds
+    if (W > 1) {
+        if ((lane & 7) == 0) s.v[par][g][k][wg] = x;
+        asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "r"(32 * W) : "memory");
+        x = 0.f;
+        for (int w = lane & 7; w < W; w += 8) x += s.v[par][g][k][w];
+        x += __shfl_xor_sync(0xffffffffu, x, 4);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+        par ^= 1;
+    }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+    for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xffffffffu, x, 8 * i);
 }
 
 // ---- forward ----
-// W warps per row, NV vectors of 8 elements per lane, the row in registers between its statistics and the output.
-constexpr int NORM_THREADS = 256;
-template <int W, int NV, bool RMS>
-__global__ void __launch_bounds__(NORM_THREADS) k_norm_forward(const NormArgs a) {
-    constexpr int ROWS = NORM_THREADS / 32 / W;
-    __shared__ float s_part[2][ROWS][W];
+template <int NV, int B, int STAGES, int THREADS, bool RMS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const NormArgs a, int W, int G) {
+    extern __shared__ uint4 s_ring[];           // [STAGES][B][NV][threads]
+    __shared__ GroupSums s_sums;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = warp / W, wg = warp % W, l = wg * 32 + lane;
-    const int nvec = a.d / 8;
+    const int nvec = a.d / 8, threads = blockDim.x;
     const float inv_d = 1.f / (float)a.d;
-    for (int64_t s = (int64_t)blockIdx.x * NORM_THREADS + threadIdx.x; s < a.S; s += (int64_t)gridDim.x * NORM_THREADS) {
+    for (int64_t s = (int64_t)blockIdx.x * threads + threadIdx.x; s < a.S; s += (int64_t)gridDim.x * threads) {
         const int p = a.off[s], q = a.off[s + 1], t = a.slot[s];
         if (q < p || p < 0 || q > a.T || (s == 0 && p != 0) || (s == a.S - 1 && q != a.T)) dk_report(a.status, DEV_BAD_TABLE, (int)s);
         if (t < -1 || t >= a.cap) dk_report(a.status, DEV_BAD_INDEX, (int)s);
     }
-    // sum over the row's lanes; all threads of the CTA take the same steps
-    auto row_sum = [&](float v, int which) {
-        v = warp_sum(v);
-        if (W == 1) return v;
-        if (lane == 0) s_part[which][g][wg] = v;
-        __syncthreads();
-        v = 0.f;
+    const int64_t first = ((int64_t)blockIdx.x * G + g) * a.rows_per_group;
+    if (first >= a.T) return;                   // (a group synchronises with itself alone)
+    const int n = (int)min(a.rows_per_group, a.T - first);      // rows of the group
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
+    const bf16* x0 = a.x + first * a.ldx + l * 8;
+    bf16* y0 = a.y + first * a.ldy + l * 8;
+    auto fetch = [&](int r, int st) {           // starts the copies of the batch at the group's row r
 #pragma unroll
-        for (int w = 0; w < W; ++w) v += s_part[which][g][w];
-        return v;
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (r + b < n && l + j * 32 * W < nvec)
+                    copy16(ring + (uint32_t)(((st * B + b) * NV + j) * threads * 16), x0 + (int64_t)(r + b) * a.ldx + j * 256 * W);
+        copy_commit();
     };
-    for (int64_t i0 = (int64_t)blockIdx.x * ROWS; i0 < a.T; i0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t i = i0 + g;
-        const bool on = i < a.T;
-        uint4 q[NV];
+    auto element = [&](int st, int b, int j) { return s_ring[((st * B + b) * NV + j) * threads + threadIdx.x]; };
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int v = l + j * 32 * W;
-            q[j] = on && v < nvec ? reinterpret_cast<const uint4*>(a.x + i * a.ldx)[v] : make_uint4(0u, 0u, 0u, 0u);
+    for (int u = 0; u < STAGES - 1; ++u) fetch(u * B, u);
+    // the tenant of the next row: of the last one's segment, of the one after it, or else looked for
+    int seg = -1, seg_begin = 0, seg_end = 0, cur = -1, par = 0, st = 0;
+    auto slot_of = [&](int i) {
+        if (i < seg_begin || i >= seg_end) {
+            int lo = seg + 1;
+            if (seg < 0 || lo >= a.S || a.off[lo] > i || a.off[lo + 1] <= i) {
+                lo = 0;
+                int hi = a.S;
+                while (lo < hi) {
+                    const int m = (lo + hi) >> 1;
+                    if (a.off[m + 1] > i) hi = m; else lo = m + 1;
+                }
+            }
+            if (lo >= a.S) return a.cap;
+            seg = lo;
+            seg_begin = a.off[lo];
+            seg_end = a.off[lo + 1];
         }
-        int lo = 0, hi = on ? a.S : 0;          // the token's segment, while the row is on its way
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (__ldg(a.off + mid + 1) > i) hi = mid; else lo = mid + 1;
-        }
-        int t = on && lo < a.S ? a.slot[lo] : -1;
-        if (t < 0 || t >= a.cap) t = a.cap;
-        const float* gain = a.gain + (size_t)t * a.d;
-        const float* bias = a.bias ? a.bias + (size_t)t * a.d : nullptr;
-        float mean = 0.f, f[8];
+        const int t = a.slot[seg];
+        return t < 0 || t >= a.cap ? a.cap : t;
+    };
+    float gain[NV][8], bias[NV][8], f[8];
+    for (int r = 0; r < n; r += B) {
+        fetch(r + (STAGES - 1) * B, st == 0 ? STAGES - 1 : st - 1);
+        copy_wait<STAGES - 1>();
+        float v[4] = {0.f, 0.f, 0.f, 0.f}, mean[4] = {0.f, 0.f, 0.f, 0.f};
         if (!RMS) {
-            float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                unpack8(q[j], f);
+            for (int b = 0; b < B; ++b)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += f[e];
+                for (int j = 0; j < NV; ++j)
+                    if (r + b < n && l + j * 32 * W < nvec) {
+                        unpack8(element(st, b, j), f);
+                        v[b] += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+                    }
+            group_sum4(v, s_sums, par, W, g, wg, lane);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                mean[b] = v[b] * inv_d;
+                v[b] = 0.f;
             }
-            mean = row_sum(sum, 0) * inv_d;
         }
-        float sq = 0.f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (l + j * 32 * W < nvec) {
-                unpack8(q[j], f);
+        for (int b = 0; b < B; ++b)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float c = f[e] - mean;
-                    sq = fmaf(c, c, sq);
+            for (int j = 0; j < NV; ++j)
+                if (r + b < n && l + j * 32 * W < nvec) {
+                    unpack8(element(st, b, j), f);
+                    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float c0 = f[e] - mean[b], c1 = f[e + 1] - mean[b];
+                        s0 = fmaf(c0, c0, s0);
+                        s1 = fmaf(c1, c1, s1);
+                    }
+                    v[b] += s0 + s1;
+                }
+        group_sum4(v, s_sums, par, W, g, wg, lane);
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            if (r + b < n) {
+                const int64_t i = first + r + b;
+                const int t = slot_of((int)i);
+                if (t != cur) {
+                    cur = t;
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) {
+                        const int c = l + j * 32 * W;
+                        if (c < nvec) {
+                            load8(a.gain + (size_t)t * a.d + c * 8, gain[j]);
+                            if (a.bias) load8(a.bias + (size_t)t * a.d + c * 8, bias[j]);
+                            else
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) bias[j][e] = 0.f;
+                        }
+                    }
+                }
+                const float rstd = 1.f / sqrtf(fmaf(v[b], inv_d, a.eps)), m = mean[b];
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (l + j * 32 * W < nvec) {
+                        unpack8(element(st, b, j), f);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] = fmaf((f[e] - m) * rstd, gain[j][e], bias[j][e]);
+                        *reinterpret_cast<uint4*>(y0 + (int64_t)(r + b) * a.ldy + j * 256 * W) = pack8(f);
+                    }
+                if (l == 0) {
+                    if (a.mean) a.mean[i] = m;
+                    if (a.rstd) a.rstd[i] = rstd;
                 }
             }
         }
-        const float rstd = 1.f / sqrtf(fmaf(row_sum(sq, 1), inv_d, a.eps));
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int v = l + j * 32 * W;
-            if (on && v < nvec) {
-                float w[8];
-                unpack8(q[j], f);
-                load8(gain + v * 8, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = (f[e] - mean) * rstd * w[e];
-                if (bias) {
-                    load8(bias + v * 8, w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] += w[e];
-                }
-                reinterpret_cast<uint4*>(a.y + i * a.ldy)[v] = pack8(f);
-            }
-        }
-        if (on && l == 0) {
-            if (a.mean) a.mean[i] = mean;
-            if (a.rstd) a.rstd[i] = rstd;
-        }
-        if (W > 1) __syncthreads();
+        st = st == STAGES - 1 ? 0 : st + 1;
     }
 }
 
 // ---- backward ----
-// A group of W warps takes a run of the ordered tokens, one row after another; a thread keeps the same NV x 8 columns
-// throughout, so that the tenant's gain and the sums for dgain and dbias stay in its registers until the tenant changes.  Rows
-// are fetched DEPTH - 1 ahead by asynchronous copies into shared memory that only the fetching thread reads: no barrier but the one
-// for a row's two sums.  The sums of a (group, tenant) pair go to partial[group + tenant]: both only rise along the ordered
-// tokens, so no two pairs share a place, and the order of all additions depends on the sizes and the tables alone.
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-constexpr int NORM_BACK_THREADS = 512;
-
-template <int NV, int NORM_DEPTH, bool RMS>
-__global__ void __launch_bounds__(NORM_BACK_THREADS) k_norm_backward(const NormArgs a, int W, int G) {
-    extern __shared__ uint4 s_ring[];       // [DEPTH][2][NV][threads]
-    __shared__ float2 s_part[2][32];
+// The rows are taken in the order of their tenants.  The sums of a (group, tenant) pair go to partial[group + tenant]: both only
+// rise along the ordered tokens, so no two pairs share a place, and the order of all additions depends on the sizes and the
+// table alone.
+template <int NV, int B, int STAGES, int THREADS, bool RMS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const NormArgs a, int W, int G) {
+    extern __shared__ uint4 s_ring[];           // [STAGES][B][x, dy][NV][threads]
+    __shared__ GroupSums s_sums;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = warp / W, wg = warp % W, l = wg * 32 + lane;
     const int nvec = a.d / 8, threads = blockDim.x;
     const float inv_d = 1.f / (float)a.d;
-    const int64_t q = (int64_t)blockIdx.x * G + g;
-    const int64_t p0 = q * a.rows_per_group, p1 = p0 + a.rows_per_group < a.T ? p0 + a.rows_per_group : a.T;
-    if (p0 >= a.T) return;                  // (a group synchronises with itself alone)
+    const int64_t q = (int64_t)blockIdx.x * G + g, first = q * a.rows_per_group;
+    if (first >= a.T) return;
+    const int n = (int)min(a.rows_per_group, a.T - first);
+    const int32_t* perm = a.perm + first;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
-    auto fetch = [&](int64_t p) -> int64_t {        // starts row p's copies; its token
-        int64_t i = -1;
-        if (p < p1) {
-            i = a.perm[p];
-            const int st = (int)((p - p0) % NORM_DEPTH);
+    auto fetch = [&](const int (&tok)[B], int r, int st) {
+#pragma unroll
+        for (int b = 0; b < B; ++b)
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int v = l + j * 32 * W;
-                if (v < nvec) {
-                    copy16(ring + ((st * 2 + 0) * NV + j) * threads * 16, a.x + i * a.ldx + v * 8);
-                    copy16(ring + ((st * 2 + 1) * NV + j) * threads * 16, a.dy + i * a.lddy + v * 8);
+                if (r + b < n && v < nvec) {
+                    const uint32_t to = ring + (uint32_t)((((st * B + b) * 2) * NV + j) * threads * 16);
+                    copy16(to, a.x + (int64_t)tok[b] * a.ldx + v * 8);
+                    copy16(to + (uint32_t)(NV * threads * 16), a.dy + (int64_t)tok[b] * a.lddy + v * 8);
                 }
             }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        return i;
+        copy_commit();
     };
-    int64_t tok[NORM_DEPTH];
+    auto element = [&](int st, int b, int which, int j) { return s_ring[(((st * B + b) * 2 + which) * NV + j) * threads + threadIdx.x]; };
+    // tok[u]: the tokens of the batch u steps ahead
+    int tok[STAGES][B];
+    auto tokens = [&](int (&t)[B], int r) {
 #pragma unroll
-    for (int u = 0; u < NORM_DEPTH - 1; ++u) tok[u] = fetch(p0 + u);
-    int key = -1;
-    int64_t key_end = p0;
+        for (int b = 0; b < B; ++b) t[b] = r + b < n ? perm[r + b] : 0;
+    };
+#pragma unroll
+    for (int u = 0; u < STAGES; ++u) tokens(tok[u], u * B);
+#pragma unroll
+    for (int u = 0; u < STAGES - 1; ++u) fetch(tok[u], u * B, u);
+    int key = -1, par = 0, st = 0, key_end = 0;     // key_end: the group's first row of a later tenant
     float gain[NV][8], sg[NV][8], sb[NV][8];
     auto flush = [&]() {
         float* out = a.partial + (size_t)(q + key) * 2 * a.d;
@@ -224,74 +293,88 @@ __global__ void __launch_bounds__(NORM_BACK_THREADS) k_norm_backward(const NormA
             }
         }
     };
-    int par = 0;
-    for (int64_t pb = p0; pb < p1; pb += NORM_DEPTH) {
+    auto next_tenant = [&](int r) {             // the next tenant that has tokens; its gain, and sums of 0
+        do key_end = (int)min((int64_t)n, a.key_off[++key + 1] - first); while (key_end <= r);
 #pragma unroll
-        for (int u = 0; u < NORM_DEPTH; ++u) {
-            const int64_t p = pb + u;
-            if (p >= p1) break;
-            tok[(u + NORM_DEPTH - 1) % NORM_DEPTH] = fetch(p + NORM_DEPTH - 1);
-            const int64_t i = tok[u];
-            const float mean = RMS ? 0.f : a.mean_in[i], rstd = a.rstd_in[i];
-            if (p >= key_end) {             // the next tenant that has tokens
-                if (key >= 0) flush();
-                do key_end = a.key_off[++key + 1]; while (key_end <= p);
+        for (int j = 0; j < NV; ++j) {
+            const int v = l + j * 32 * W;
+            if (v < nvec) load8(a.gain + (size_t)key * a.d + v * 8, gain[j]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sg[j][e] = sb[j][e] = 0.f;
+        }
+    };
+    for (int r = 0; r < n; r += B) {
+        fetch(tok[STAGES - 1], r + (STAGES - 1) * B, st == 0 ? STAGES - 1 : st - 1);
+        float mean[B], rstd[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            mean[b] = RMS || r + b >= n ? 0.f : a.mean_in[tok[0][b]];
+            rstd[b] = r + b >= n ? 0.f : a.rstd_in[tok[0][b]];
+        }
+        if (r >= key_end) {
+            if (key >= 0 && a.partial) flush();
+            next_tenant(r);
+        }
+        const int key0 = key;                   // (the batch's second row may be the next tenant's)
+        copy_wait<STAGES - 1>();
+        float v[4] = {0.f, 0.f, 0.f, 0.f}, x[8], dy[8];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            if (r + b < n) {
+                if (b == 1 && r + 1 >= key_end) {
+                    if (a.partial) flush();
+                    next_tenant(r + 1);
+                }
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
-                    const int v = l + j * 32 * W;
-                    if (v < nvec) load8(a.gain + (size_t)key * a.d + v * 8, gain[j]);
+                    if (l + j * 32 * W < nvec) {
+                        unpack8(element(st, b, 0, j), x);
+                        unpack8(element(st, b, 1, j), dy);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sg[j][e] = sb[j][e] = 0.f;
-                }
-            }
-            asm volatile("cp.async.wait_group %0;" ::"n"(NORM_DEPTH - 1) : "memory");
-            const int st = u;
-            float2 sum = make_float2(0.f, 0.f);
-            float xh[NV][8], av[NV][8];
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                if (l + j * 32 * W < nvec) {
-                    float dy[8];
-                    unpack8(s_ring[((st * 2 + 0) * NV + j) * threads + threadIdx.x], xh[j]);
-                    unpack8(s_ring[((st * 2 + 1) * NV + j) * threads + threadIdx.x], dy);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        xh[j][e] = (xh[j][e] - mean) * rstd;
-                        av[j][e] = dy[e] * gain[j][e];
-                        sg[j][e] = fmaf(dy[e], xh[j][e], sg[j][e]);
-                        sb[j][e] += dy[e];
-                        if (!RMS) sum.x += av[j][e];
-                        sum.y = fmaf(av[j][e], xh[j][e], sum.y);
-                    }
-                }
-            }
-            if (a.y) {
-                if (!RMS) sum.x = warp_sum(sum.x);
-                sum.y = warp_sum(sum.y);
-                if (W > 1) {
-                    if (lane == 0) s_part[par][warp] = sum;
-                    asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "r"(32 * W) : "memory");
-                    sum = make_float2(0.f, 0.f);
-                    for (int w = 0; w < W; ++w) {
-                        const float2 o = s_part[par][g * W + w];
-                        sum.x += o.x;
-                        sum.y += o.y;
-                    }
-                    par ^= 1;
-                }
-                const float ma = sum.x * inv_d, mx = sum.y * inv_d;
-#pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    const int v = l + j * 32 * W;
-                    if (v < nvec) {
-                        float o[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) o[e] = rstd * (av[j][e] - ma - xh[j][e] * mx);
-                        reinterpret_cast<uint4*>(a.y + i * a.ldy)[v] = pack8(o);
+                        for (int e = 0; e < 8; ++e) {
+                            const float xh = (x[e] - mean[b]) * rstd[b], av = dy[e] * gain[j][e];
+                            sg[j][e] = fmaf(dy[e], xh, sg[j][e]);
+                            sb[j][e] += dy[e];
+                            if (!RMS) v[2 * b] += av;
+                            v[2 * b + 1] = fmaf(av, xh, v[2 * b + 1]);
+                        }
                     }
                 }
             }
         }
+        if (a.y) {
+            group_sum4(v, s_sums, par, W, g, wg, lane);
+#pragma unroll
+            for (int b = B - 1; b >= 0; --b) {
+                const float ma = v[2 * b] * inv_d, mx = v[2 * b + 1] * inv_d;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    const int c = l + j * 32 * W;
+                    if (r + b < n && c < nvec) {
+                        unpack8(element(st, b, 0, j), x);
+                        unpack8(element(st, b, 1, j), dy);
+                        if (b == 0 && key0 != key) {
+                            float w[8];
+                            load8(a.gain + (size_t)key0 * a.d + c * 8, w);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) dy[e] *= w[e];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) dy[e] *= gain[j][e];
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = rstd[b] * (dy[e] - ma - (x[e] - mean[b]) * rstd[b] * mx);
+                        *reinterpret_cast<uint4*>(a.y + (int64_t)tok[0][b] * a.ldy + c * 8) = pack8(x);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < STAGES - 1; ++u)
+#pragma unroll
+            for (int b = 0; b < B; ++b) tok[u][b] = tok[u + 1][b];
+        tokens(tok[STAGES - 1], r + STAGES * B);
+        st = st == STAGES - 1 ? 0 : st + 1;
     }
     if (a.partial) flush();
 }
@@ -324,7 +407,7 @@ __global__ void __launch_bounds__(256) k_norm_reduce(const NormArgs a) {
     *out = a.accumulate ? *out + v : v;
 }
 
-// How the backward pass cuts a batch: warps per row and rows of a CTA at a time, groups in all.
+// How a pass cuts a batch: warps per row and rows of a CTA at a time, groups in all and their rows.
 struct NormPlan {
     int NV, W, G;
     int64_t groups, rows;
@@ -332,11 +415,10 @@ struct NormPlan {
 static NormPlan norm_plan(const marlaas_pool* pool, int64_t T, int d) {
     NormPlan p;
     const int nvec = d / 8;
-    p.NV = 1;
-    while (p.NV * NORM_BACK_THREADS < nvec) p.NV *= 2;           // one vector per lane while 16 warps hold a row
+    p.NV = nvec <= 1024 ? 1 : 2;
     p.W = (int)cdiv(nvec, 32 * p.NV);
-    p.G = std::min(8, NORM_BACK_THREADS / 32 / p.W);
-    const int64_t most = (int64_t)pool->sm_count * 2 * p.G;      // two CTAs per SM
+    p.G = std::max(1, std::min(NORM_MAX_GROUPS, 16 / p.W));
+    const int64_t most = (int64_t)pool->sm_count * std::max(1, 1024 / (32 * p.W * p.G)) * p.G;      // 1024 threads per SM
     p.rows = std::max<int64_t>(cdiv(T, most), 1);
     p.groups = cdiv(cdiv(T, p.rows), p.G) * p.G;
     return p;
@@ -370,39 +452,30 @@ static NormWorkspace carve_norm(const marlaas_pool* pool, int64_t T, int32_t S, 
     return w;
 }
 
-static marlaas_status_t launch_norm_forward(const marlaas_pool* pool, const NormArgs& a, bool rms, cudaStream_t st) {
-    const int nvec = a.d / 8;
-    // One warp per row while its registers hold it and there are rows enough for two CTAs per SM; else four.
-    const int W = nvec <= 16 * 32 && cdiv(a.T, 8) >= 2 * (int64_t)pool->sm_count ? 1 : 4;
-    int NV = 1;
-    while (NV * 32 * W < nvec) NV *= 2;
-    const int rows = NORM_THREADS / 32 / W;
-    const unsigned grid = (unsigned)std::min<int64_t>(cdiv(a.T, rows), (int64_t)pool->sm_count * 8);
-#define NORM_GO(w, n)                                                                   \
-    if (W == w && NV == n) {                                                            \
-        if (rms) k_norm_forward<w, n, true><<<grid, NORM_THREADS, 0, st>>>(a);          \
-        else k_norm_forward<w, n, false><<<grid, NORM_THREADS, 0, st>>>(a);             \
-    }
-    NORM_GO(1, 1) NORM_GO(1, 2) NORM_GO(1, 4) NORM_GO(1, 8) NORM_GO(1, 16)
-    NORM_GO(4, 1) NORM_GO(4, 2) NORM_GO(4, 4) NORM_GO(4, 8) NORM_GO(4, 16)
-#undef NORM_GO
-    MARLAAS_LAUNCH_CHECK("k_norm_forward");
-    return MARLAAS_OK;
-}
-
-template <int NV, bool RMS>
-static marlaas_status_t launch_norm_backward_t(const marlaas_pool* pool, const NormArgs& a, const NormPlan& n, cudaStream_t st) {
-    constexpr int DEPTH = NV == 4 ? 2 : 4;          // as deep as shared memory allows for the widest rows
-    constexpr size_t most = (size_t)DEPTH * 2 * NV * NORM_BACK_THREADS * 16;
+// Instances by the width of a row and of a CTA: a CTA of up to 512 threads shares its SM with others.
+template <int NV, int THREADS, bool RMS>
+static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& a, const NormPlan& n, bool backward, cudaStream_t st) {
+    constexpr int FB = NV == 1 ? 4 : 2, FS = NV == 1 && THREADS == 512 ? 3 : 2, BB = NV == 1 ? 2 : 1, BS = NV == 1 ? 3 : 2;
     const int threads = 32 * n.W * n.G;
+    const size_t fwd = (size_t)FS * FB * NV * 16, bwd = (size_t)BS * BB * 2 * NV * 16;       // bytes of the ring per thread
     static bool attr_set[64] = {};
     if (pool->device >= 64 || !attr_set[pool->device]) {
-        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_norm_backward<NV, DEPTH, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_norm_forward<NV, FB, FS, THREADS, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fwd * THREADS)));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_norm_backward<NV, BB, BS, THREADS, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(bwd * THREADS)));
         if (pool->device < 64) attr_set[pool->device] = true;
     }
-    k_norm_backward<NV, DEPTH, RMS><<<(unsigned)(n.groups / n.G), threads, (size_t)DEPTH * 2 * NV * threads * 16, st>>>(a, n.W, n.G);
-    MARLAAS_LAUNCH_CHECK("k_norm_backward");
+    const unsigned grid = (unsigned)(n.groups / n.G);
+    if (backward) k_norm_backward<NV, BB, BS, THREADS, RMS><<<grid, threads, bwd * threads, st>>>(a, n.W, n.G);
+    else k_norm_forward<NV, FB, FS, THREADS, RMS><<<grid, threads, fwd * threads, st>>>(a, n.W, n.G);
+    MARLAAS_LAUNCH_CHECK(backward ? "k_norm_backward" : "k_norm_forward");
     return MARLAAS_OK;
+}
+static marlaas_status_t launch_norm(const marlaas_pool* pool, NormArgs a, bool rms, bool backward, cudaStream_t st) {
+    const NormPlan n = norm_plan(pool, a.T, a.d);
+    a.rows_per_group = n.rows;
+    if (n.NV == 2) return rms ? launch_norm_t<2, 1024, true>(pool, a, n, backward, st) : launch_norm_t<2, 1024, false>(pool, a, n, backward, st);
+    if (n.W > 16) return rms ? launch_norm_t<1, 1024, true>(pool, a, n, backward, st) : launch_norm_t<1, 1024, false>(pool, a, n, backward, st);
+    return rms ? launch_norm_t<1, 512, true>(pool, a, n, backward, st) : launch_norm_t<1, 512, false>(pool, a, n, backward, st);
 }
 
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
@@ -482,7 +555,7 @@ marlaas_status_t marlaas_layer_norm(marlaas_pool_t* pool, int64_t T, int64_t d, 
     a.x = (const bf16*)x; a.ldx = ldx; a.y = (bf16*)y; a.ldy = ldy;
     a.gain = gain; a.bias = bias; a.eps = eps; a.mean = mean; a.rstd = rstd; a.status = pool->d_status;
     if (host && (rc = stage_table(seg, ws, &a, st)) != MARLAAS_OK) return rc;
-    if ((rc = launch_norm_forward(pool, a, (flags & MARLAAS_FLAG_RMS_NORM) != 0, st)) != MARLAAS_OK) return rc;
+    if ((rc = launch_norm(pool, a, (flags & MARLAAS_FLAG_RMS_NORM) != 0, false, st)) != MARLAAS_OK) return rc;
     return finish(pool, flags, st);
 } catch (const std::exception& e) {
     return fail(MARLAAS_ERR_INVALID_ARG, "layer_norm: %s", e.what());
@@ -539,9 +612,7 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
     o.T = T; o.S = a.S; o.off = a.off; o.slot = a.slot; o.cap = pool->cap; o.nkeys = pool->cap + 1;
     o.perm = ws.perm; o.key_off = ws.key_off;
     if ((rc = launch_order(pool, o, ws.scratch, st)) != MARLAAS_OK) return rc;
-    if (n.NV == 1) rc = rms ? launch_norm_backward_t<1, true>(pool, a, n, st) : launch_norm_backward_t<1, false>(pool, a, n, st);
-    else if (n.NV == 2) rc = rms ? launch_norm_backward_t<2, true>(pool, a, n, st) : launch_norm_backward_t<2, false>(pool, a, n, st);
-    else rc = rms ? launch_norm_backward_t<4, true>(pool, a, n, st) : launch_norm_backward_t<4, false>(pool, a, n, st);
+    rc = launch_norm(pool, a, rms, true, st);
     if (rc != MARLAAS_OK) return rc;
     if (a.partial) {
         k_norm_reduce<<<dim3((unsigned)cdiv(d, 32), (unsigned)(pool->cap + 1)), 256, 0, st>>>(a);
