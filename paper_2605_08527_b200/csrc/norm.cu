@@ -40,29 +40,29 @@ struct NormArgs {
     int32_t* status;
 };
 
-__device__ __forceinline__ void unpack8(const uint4& q, float (&f)[8]) {
+// Eight elements as four pairs, for the two-element fp32 instructions: both passes are short of issue slots before anything else.
+__device__ __forceinline__ void unpack8(const uint4& q, float2 (&f)[4]) {
     const uint32_t* w = &q.x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+__device__ __forceinline__ uint4 pack8(const float2 (&f)[4]) {
     uint4 q;
     uint32_t* w = &q.x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        __nv_bfloat162 p = __floats2bfloat162_rn(f[i].x, f[i].y);
         w[i] = *reinterpret_cast<uint32_t*>(&p);
     }
     return q;
 }
-__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
+__device__ __forceinline__ void load8(const float* p, float2 (&f)[4]) {
     const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    f[0] = make_float2(a.x, a.y); f[1] = make_float2(a.z, a.w);
+    f[2] = make_float2(b.x, b.y); f[3] = make_float2(b.z, b.w);
 }
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
 // ---- both passes ----
 // A group of W warps takes a run of rows, B at a time; a thread keeps the same NV x 8 columns throughout, so that its tenant's
 // parameters (and the sums for their gradients) stay in registers until the tenant changes: read per row, they were twice the
@@ -138,27 +138,26 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
 #pragma unroll
     for (int u = 0; u < STAGES - 1; ++u) fetch(u * B, u);
     // the tenant of the next row: of the last one's segment, of the one after it, or else looked for
-    int seg = -1, seg_begin = 0, seg_end = 0, cur = -1, par = 0, st = 0;
+    int seg = -1, seg_begin = 0, seg_end = 0, slot = a.cap, cur = -1, par = 0, st = 0;
     auto slot_of = [&](int i) {
-        if (i < seg_begin || i >= seg_end) {
-            int lo = seg + 1;
-            if (seg < 0 || lo >= a.S || a.off[lo] > i || a.off[lo + 1] <= i) {
-                lo = 0;
-                int hi = a.S;
-                while (lo < hi) {
-                    const int m = (lo + hi) >> 1;
-                    if (a.off[m + 1] > i) hi = m; else lo = m + 1;
-                }
+        if (i >= seg_begin && i < seg_end) return slot;
+        int lo = seg + 1;
+        if (seg < 0 || lo >= a.S || a.off[lo] > i || a.off[lo + 1] <= i) {
+            lo = 0;
+            int hi = a.S;
+            while (lo < hi) {
+                const int m = (lo + hi) >> 1;
+                if (a.off[m + 1] > i) hi = m; else lo = m + 1;
             }
-            if (lo >= a.S) return a.cap;
-            seg = lo;
-            seg_begin = a.off[lo];
-            seg_end = a.off[lo + 1];
         }
-        const int t = a.slot[seg];
-        return t < 0 || t >= a.cap ? a.cap : t;
+        if (lo >= a.S) return a.cap;
+        seg = lo;
+        seg_begin = a.off[lo];
+        seg_end = a.off[lo + 1];
+        const int t = a.slot[lo];
+        return slot = t < 0 || t >= a.cap ? a.cap : t;
     };
-    float gain[NV][8], bias[NV][8], f[8];
+    float2 gain[NV][4], bias[NV][4], f[4];
     for (int r = 0; r < n; r += B) {
         fetch(r + (STAGES - 1) * B, st == 0 ? STAGES - 1 : st - 1);
         copy_wait<STAGES - 1>();
@@ -170,7 +169,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
                 for (int j = 0; j < NV; ++j)
                     if (r + b < n && l + j * 32 * W < nvec) {
                         unpack8(element(st, b, j), f);
-                        v[b] += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+                        const float2 s = __fadd2_rn(__fadd2_rn(f[0], f[1]), __fadd2_rn(f[2], f[3]));
+                        v[b] += s.x + s.y;
                     }
             group_sum4(v, s_sums, par, W, g, wg, lane);
 #pragma unroll
@@ -185,14 +185,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
             for (int j = 0; j < NV; ++j)
                 if (r + b < n && l + j * 32 * W < nvec) {
                     unpack8(element(st, b, j), f);
-                    float s0 = 0.f, s1 = 0.f;
+                    float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float c0 = f[e] - mean[b], c1 = f[e + 1] - mean[b];
-                        s0 = fmaf(c0, c0, s0);
-                        s1 = fmaf(c1, c1, s1);
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 c = RMS ? f[e] : __fadd2_rn(f[e], both(-mean[b]));
+                        s = __ffma2_rn(c, c, s);
                     }
-                    v[b] += s0 + s1;
+                    v[b] += s.x + s.y;
                 }
         group_sum4(v, s_sums, par, W, g, wg, lane);
 #pragma unroll
@@ -210,17 +209,20 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
                             if (a.bias) load8(a.bias + (size_t)t * a.d + c * 8, bias[j]);
                             else
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) bias[j][e] = 0.f;
+                                for (int e = 0; e < 4; ++e) bias[j][e] = make_float2(0.f, 0.f);
                         }
                     }
                 }
-                const float rstd = 1.f / sqrtf(fmaf(v[b], inv_d, a.eps)), m = mean[b];
+                const float rstd = rsqrtf(fmaf(v[b], inv_d, a.eps)), m = mean[b];
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
                     if (l + j * 32 * W < nvec) {
                         unpack8(element(st, b, j), f);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) f[e] = fmaf((f[e] - m) * rstd, gain[j][e], bias[j][e]);
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 c = RMS ? f[e] : __fadd2_rn(f[e], both(-m));
+                            f[e] = __ffma2_rn(__fmul2_rn(c, both(rstd)), gain[j][e], bias[j][e]);
+                        }
                         *reinterpret_cast<uint4*>(y0 + (int64_t)(r + b) * a.ldy + j * 256 * W) = pack8(f);
                     }
                 if (l == 0) {
@@ -275,7 +277,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
 #pragma unroll
     for (int u = 0; u < STAGES - 1; ++u) fetch(tok[u], u * B, u);
     int key = -1, par = 0, st = 0, key_end = 0;     // key_end: the group's first row of a later tenant
-    float gain[NV][8], sg[NV][8], sb[NV][8];
+    float2 gain[NV][4], sg[NV][4], sb[NV][4];
     auto flush = [&]() {
         float* out = a.partial + (size_t)(q + key) * 2 * a.d;
 #pragma unroll
@@ -283,12 +285,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
             const int v = l + j * 32 * W;
             if (v < nvec) {
                 float4* o = reinterpret_cast<float4*>(out + v * 8);
-                o[0] = make_float4(sg[j][0], sg[j][1], sg[j][2], sg[j][3]);
-                o[1] = make_float4(sg[j][4], sg[j][5], sg[j][6], sg[j][7]);
+                o[0] = make_float4(sg[j][0].x, sg[j][0].y, sg[j][1].x, sg[j][1].y);
+                o[1] = make_float4(sg[j][2].x, sg[j][2].y, sg[j][3].x, sg[j][3].y);
                 if (a.dbias) {
                     o = reinterpret_cast<float4*>(out + a.d + v * 8);
-                    o[0] = make_float4(sb[j][0], sb[j][1], sb[j][2], sb[j][3]);
-                    o[1] = make_float4(sb[j][4], sb[j][5], sb[j][6], sb[j][7]);
+                    o[0] = make_float4(sb[j][0].x, sb[j][0].y, sb[j][1].x, sb[j][1].y);
+                    o[1] = make_float4(sb[j][2].x, sb[j][2].y, sb[j][3].x, sb[j][3].y);
                 }
             }
         }
@@ -300,7 +302,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
             const int v = l + j * 32 * W;
             if (v < nvec) load8(a.gain + (size_t)key * a.d + v * 8, gain[j]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sg[j][e] = sb[j][e] = 0.f;
+            for (int e = 0; e < 4; ++e) sg[j][e] = sb[j][e] = make_float2(0.f, 0.f);
         }
     };
     for (int r = 0; r < n; r += B) {
@@ -317,7 +319,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
         }
         const int key0 = key;                   // (the batch's second row may be the next tenant's)
         copy_wait<STAGES - 1>();
-        float v[4] = {0.f, 0.f, 0.f, 0.f}, x[8], dy[8];
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float2 x[4], dy[4];
 #pragma unroll
         for (int b = 0; b < B; ++b) {
             if (r + b < n) {
@@ -330,14 +333,18 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
                     if (l + j * 32 * W < nvec) {
                         unpack8(element(st, b, 0, j), x);
                         unpack8(element(st, b, 1, j), dy);
+                        float2 s = make_float2(0.f, 0.f), u = s;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float xh = (x[e] - mean[b]) * rstd[b], av = dy[e] * gain[j][e];
-                            sg[j][e] = fmaf(dy[e], xh, sg[j][e]);
-                            sb[j][e] += dy[e];
-                            if (!RMS) v[2 * b] += av;
-                            v[2 * b + 1] = fmaf(av, xh, v[2 * b + 1]);
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 xh = __fmul2_rn(RMS ? x[e] : __fadd2_rn(x[e], both(-mean[b])), both(rstd[b]));
+                            const float2 av = __fmul2_rn(dy[e], gain[j][e]);
+                            sg[j][e] = __ffma2_rn(dy[e], xh, sg[j][e]);
+                            sb[j][e] = __fadd2_rn(dy[e], sb[j][e]);
+                            if (!RMS) s = __fadd2_rn(av, s);
+                            u = __ffma2_rn(av, xh, u);
                         }
+                        v[2 * b] += s.x + s.y;
+                        v[2 * b + 1] += u.x + u.y;
                     }
                 }
             }
@@ -354,16 +361,23 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
                         unpack8(element(st, b, 0, j), x);
                         unpack8(element(st, b, 1, j), dy);
                         if (b == 0 && key0 != key) {
-                            float w[8];
+                            float2 w[4];
                             load8(a.gain + (size_t)key0 * a.d + c * 8, w);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) dy[e] *= w[e];
+                            for (int e = 0; e < 4; ++e) dy[e] = __fmul2_rn(dy[e], w[e]);
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) dy[e] *= gain[j][e];
+                            for (int e = 0; e < 4; ++e) dy[e] = __fmul2_rn(dy[e], gain[j][e]);
                         }
+                        const float k = rstd[b] * mx;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = rstd[b] * (dy[e] - ma - (x[e] - mean[b]) * rstd[b] * mx);
+                        for (int e = 0; e < 4; ++e) {
+                            if (!RMS) {
+                                x[e] = __fadd2_rn(x[e], both(-mean[b]));
+                                dy[e] = __fadd2_rn(dy[e], both(-ma));
+                            }
+                            x[e] = __fmul2_rn(__ffma2_rn(x[e], both(-k), dy[e]), both(rstd[b]));
+                        }
                         *reinterpret_cast<uint4*>(a.y + (int64_t)tok[0][b] * a.ldy + c * 8) = pack8(x);
                     }
                 }
