@@ -73,8 +73,9 @@ struct GroupSums {
     float v[2][NORM_MAX_GROUPS][4][32];
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// 16 bytes, or as many zeros where there is nothing to read: what follows needs no branches for ends of rows and batches
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -95,8 +96,13 @@ __device__ __forceinline__ void group_sum4(float (&v)[4], GroupSums& s, int& par
     if (W > 1) {
         if ((lane & 7) == 0) s.v[par][g][k][wg] = x;
         asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "r"(32 * W) : "memory");
-        x = 0.f;
-        for (int w = lane & 7; w < W; w += 8) x += s.v[par][g][k][w];
+        const float* part = s.v[par][g][k] + (lane & 7);
+        x = (lane & 7) < W ? part[0] : 0.f;
+        if (W > 8) x += (lane & 7) + 8 < W ? part[8] : 0.f;
+        if (W > 16) {
+            x += (lane & 7) + 16 < W ? part[16] : 0.f;
+            x += (lane & 7) + 24 < W ? part[24] : 0.f;
+        }
         x += __shfl_xor_sync(0xffffffffu, x, 4);
         x += __shfl_xor_sync(0xffffffffu, x, 2);
         x += __shfl_xor_sync(0xffffffffu, x, 1);
@@ -123,15 +129,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
     if (first >= a.T) return;                   // (a group synchronises with itself alone)
     const int n = (int)min(a.rows_per_group, a.T - first);      // rows of the group
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
-    const bf16* x0 = a.x + first * a.ldx + l * 8;
+    const bf16* x0 = a.x + first * a.ldx;
     bf16* y0 = a.y + first * a.ldy + l * 8;
+    bool mine[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) mine[j] = l + j * 32 * W < nvec;
     auto fetch = [&](int r, int st) {           // starts the copies of the batch at the group's row r
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (r + b < n && l + j * 32 * W < nvec)
-                    copy16(ring + (uint32_t)(((st * B + b) * NV + j) * threads * 16), x0 + (int64_t)(r + b) * a.ldx + j * 256 * W);
+            for (int j = 0; j < NV; ++j) {
+                const bool on = r + b < n && mine[j];
+                copy16(ring + (uint32_t)(((st * B + b) * NV + j) * threads * 16), on ? x0 + (int64_t)(r + b) * a.ldx + (l + j * 32 * W) * 8 : a.x, on);
+            }
         copy_commit();
     };
     auto element = [&](int st, int b, int j) { return s_ring[((st * B + b) * NV + j) * threads + threadIdx.x]; };
@@ -166,12 +176,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
 #pragma unroll
             for (int b = 0; b < B; ++b)
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (r + b < n && l + j * 32 * W < nvec) {
-                        unpack8(element(st, b, j), f);
-                        const float2 s = __fadd2_rn(__fadd2_rn(f[0], f[1]), __fadd2_rn(f[2], f[3]));
-                        v[b] += s.x + s.y;
-                    }
+                for (int j = 0; j < NV; ++j) {
+                    unpack8(element(st, b, j), f);
+                    const float2 s = __fadd2_rn(__fadd2_rn(f[0], f[1]), __fadd2_rn(f[2], f[3]));
+                    v[b] += s.x + s.y;
+                }
             group_sum4(v, s_sums, par, W, g, wg, lane);
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -182,17 +191,16 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (r + b < n && l + j * 32 * W < nvec) {
-                    unpack8(element(st, b, j), f);
-                    float2 s = make_float2(0.f, 0.f);
+            for (int j = 0; j < NV; ++j) {
+                unpack8(element(st, b, j), f);
+                float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 c = RMS ? f[e] : __fadd2_rn(f[e], both(-mean[b]));
-                        s = __ffma2_rn(c, c, s);
-                    }
-                    v[b] += s.x + s.y;
+                for (int e = 0; e < 4; ++e) {
+                    const float2 c = RMS ? f[e] : __fadd2_rn(f[e], both(-mean[b]));
+                    s = __ffma2_rn(c, c, s);
                 }
+                v[b] += RMS || mine[j] ? s.x + s.y : 0.f;
+            }
         group_sum4(v, s_sums, par, W, g, wg, lane);
 #pragma unroll
         for (int b = 0; b < B; ++b) {
@@ -204,7 +212,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
 #pragma unroll
                     for (int j = 0; j < NV; ++j) {
                         const int c = l + j * 32 * W;
-                        if (c < nvec) {
+                        if (mine[j]) {
                             load8(a.gain + (size_t)t * a.d + c * 8, gain[j]);
                             if (a.bias) load8(a.bias + (size_t)t * a.d + c * 8, bias[j]);
                             else
@@ -215,16 +223,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
                 }
                 const float rstd = rsqrtf(fmaf(v[b], inv_d, a.eps)), m = mean[b];
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (l + j * 32 * W < nvec) {
-                        unpack8(element(st, b, j), f);
+                for (int j = 0; j < NV; ++j) {
+                    unpack8(element(st, b, j), f);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 c = RMS ? f[e] : __fadd2_rn(f[e], both(-m));
-                            f[e] = __ffma2_rn(__fmul2_rn(c, both(rstd)), gain[j][e], bias[j][e]);
-                        }
-                        *reinterpret_cast<uint4*>(y0 + (int64_t)(r + b) * a.ldy + j * 256 * W) = pack8(f);
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 c = RMS ? f[e] : __fadd2_rn(f[e], both(-m));
+                        f[e] = __ffma2_rn(__fmul2_rn(c, both(rstd)), gain[j][e], bias[j][e]);
                     }
+                    if (mine[j]) *reinterpret_cast<uint4*>(y0 + (int64_t)(r + b) * a.ldy + j * 256 * W) = pack8(f);
+                }
                 if (l == 0) {
                     if (a.mean) a.mean[i] = m;
                     if (a.rstd) a.rstd[i] = rstd;
@@ -251,17 +258,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
     const int n = (int)min(a.rows_per_group, a.T - first);
     const int32_t* perm = a.perm + first;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
+    bool mine[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) mine[j] = l + j * 32 * W < nvec;
     auto fetch = [&](const int (&tok)[B], int r, int st) {
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const int v = l + j * 32 * W;
-                if (r + b < n && v < nvec) {
-                    const uint32_t to = ring + (uint32_t)((((st * B + b) * 2) * NV + j) * threads * 16);
-                    copy16(to, a.x + (int64_t)tok[b] * a.ldx + v * 8);
-                    copy16(to + (uint32_t)(NV * threads * 16), a.dy + (int64_t)tok[b] * a.lddy + v * 8);
-                }
+                const int c = (l + j * 32 * W) * 8;
+                const bool on = r + b < n && mine[j];
+                const uint32_t to = ring + (uint32_t)((((st * B + b) * 2) * NV + j) * threads * 16);
+                copy16(to, on ? a.x + (int64_t)tok[b] * a.ldx + c : a.x, on);
+                copy16(to + (uint32_t)(NV * threads * 16), on ? a.dy + (int64_t)tok[b] * a.lddy + c : a.dy, on);
             }
         copy_commit();
     };
@@ -278,12 +287,16 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
     for (int u = 0; u < STAGES - 1; ++u) fetch(tok[u], u * B, u);
     int key = -1, par = 0, st = 0, key_end = 0;     // key_end: the group's first row of a later tenant
     float2 gain[NV][4], sg[NV][4], sb[NV][4];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) gain[j][e] = make_float2(0.f, 0.f);
     auto flush = [&]() {
         float* out = a.partial + (size_t)(q + key) * 2 * a.d;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int v = l + j * 32 * W;
-            if (v < nvec) {
+            if (mine[j]) {
                 float4* o = reinterpret_cast<float4*>(out + v * 8);
                 o[0] = make_float4(sg[j][0].x, sg[j][0].y, sg[j][1].x, sg[j][1].y);
                 o[1] = make_float4(sg[j][2].x, sg[j][2].y, sg[j][3].x, sg[j][3].y);
@@ -299,8 +312,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
         do key_end = (int)min((int64_t)n, a.key_off[++key + 1] - first); while (key_end <= r);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int v = l + j * 32 * W;
-            if (v < nvec) load8(a.gain + (size_t)key * a.d + v * 8, gain[j]);
+            if (mine[j]) load8(a.gain + (size_t)key * a.d + (l + j * 32 * W) * 8, gain[j]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sg[j][e] = sb[j][e] = make_float2(0.f, 0.f);
         }
@@ -323,30 +335,26 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
         float2 x[4], dy[4];
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-            if (r + b < n) {
-                if (b == 1 && r + 1 >= key_end) {
-                    if (a.partial) flush();
-                    next_tenant(r + 1);
-                }
+            if (b == 1 && r + 1 >= key_end && r + 1 < n) {
+                if (a.partial) flush();
+                next_tenant(r + 1);
+            }
 #pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    if (l + j * 32 * W < nvec) {
-                        unpack8(element(st, b, 0, j), x);
-                        unpack8(element(st, b, 1, j), dy);
-                        float2 s = make_float2(0.f, 0.f), u = s;
+            for (int j = 0; j < NV; ++j) {      // (zeros past the row's and the batch's end add nothing)
+                unpack8(element(st, b, 0, j), x);
+                unpack8(element(st, b, 1, j), dy);
+                float2 s = make_float2(0.f, 0.f), u = s;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 xh = __fmul2_rn(RMS ? x[e] : __fadd2_rn(x[e], both(-mean[b])), both(rstd[b]));
-                            const float2 av = __fmul2_rn(dy[e], gain[j][e]);
-                            sg[j][e] = __ffma2_rn(dy[e], xh, sg[j][e]);
-                            sb[j][e] = __fadd2_rn(dy[e], sb[j][e]);
-                            if (!RMS) s = __fadd2_rn(av, s);
-                            u = __ffma2_rn(av, xh, u);
-                        }
-                        v[2 * b] += s.x + s.y;
-                        v[2 * b + 1] += u.x + u.y;
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const float2 xh = __fmul2_rn(RMS ? x[e] : __fadd2_rn(x[e], both(-mean[b])), both(rstd[b]));
+                    const float2 av = __fmul2_rn(dy[e], gain[j][e]);
+                    sg[j][e] = __ffma2_rn(dy[e], xh, sg[j][e]);
+                    sb[j][e] = __fadd2_rn(dy[e], sb[j][e]);
+                    if (!RMS) s = __fadd2_rn(av, s);
+                    u = __ffma2_rn(av, xh, u);
                 }
+                v[2 * b] += s.x + s.y;
+                v[2 * b + 1] += u.x + u.y;
             }
         }
         if (a.y) {
@@ -357,7 +365,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     const int c = l + j * 32 * W;
-                    if (r + b < n && c < nvec) {
+                    if (r + b < n && mine[j]) {
                         unpack8(element(st, b, 0, j), x);
                         unpack8(element(st, b, 1, j), dy);
                         if (b == 0 && key0 != key) {
