@@ -55,48 +55,6 @@ __global__ void __launch_bounds__(256) k_drop_rows(int64_t T, int nvec, const bf
     }
 }
 
-// dx += s'_t m o (g A_t^T): eight columns of a token per thread.
-__global__ void __launch_bounds__(256) k_drop_expand(int64_t T, int nvec, bf16* __restrict__ dx, int64_t lddx, const float* __restrict__ g, int64_t g_plane,
-                                                     const bf16* __restrict__ At, int64_t at_plane, int K, int RP, int parts,
-                                                     const int32_t* __restrict__ tok_slot, const int32_t* __restrict__ d_rank,
-                                                     const float* __restrict__ scale, const uint32_t* __restrict__ limit, DropKey key) {
-    const int64_t n = T * nvec;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
-        const int64_t i = e / nvec;
-        const int v = (int)(e - i * nvec), t = tok_slot[i], r = t >= 0 ? d_rank[t] : 0;
-        if (r == 0) continue;
-        float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < parts; ++p) {
-            const float* gi = g + p * g_plane + i * RP;
-            const bf16* a = At + p * at_plane + (size_t)t * RP * K + v * 8;
-            for (int j = 0; j < r; ++j) {
-                const uint4 q = *reinterpret_cast<const uint4*>(a + (size_t)j * K);
-                const uint32_t* w = &q.x;
-                const float c = gi[j];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    acc[2 * k] = fmaf(c, __uint_as_float(w[k] << 16), acc[2 * k]);
-                    acc[2 * k + 1] = fmaf(c, __uint_as_float(w[k] & 0xffff0000u), acc[2 * k + 1]);
-                }
-            }
-        }
-        const uint32_t l = limit[t];
-        const uint4 bits = drop_bits(key, (uint32_t)v, (uint32_t)i);
-        const uint32_t* b = &bits.x;
-        const float s = scale[t];
-        uint4 q = *reinterpret_cast<uint4*>(dx + i * lddx + v * 8);
-        uint32_t* w = &q.x;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float lo = __uint_as_float(w[k] << 16) + ((b[k] & 0xffffu) >= l ? s * acc[2 * k] : 0.f);
-            const float hi = __uint_as_float(w[k] & 0xffff0000u) + ((b[k] >> 16) >= l ? s * acc[2 * k + 1] : 0.f);
-            __nv_bfloat162 o = __floats2bfloat162_rn(lo, hi);
-            w[k] = *reinterpret_cast<uint32_t*>(&o);
-        }
-        *reinterpret_cast<uint4*>(dx + i * lddx + v * 8) = q;
-    }
-}
-
 static unsigned stream_grid(const marlaas_pool* pool, int64_t n) { return (unsigned)std::min<int64_t>(cdiv(n, 256), (int64_t)pool->sm_count * 16); }
 
 static marlaas_status_t launch_drop_rows(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const Workspace& ws, const DropTables& d,
@@ -227,14 +185,7 @@ marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, 
         if (dx) {
             GemmOperands o;
             backward_operands(pool, T, (const bf16*)W, ldw, (const bf16*)dy, lddy, (bf16*)dx, lddx, ws, &o);
-            o.tile_nunits = nullptr;            // the product alone; the masked term follows
-            rc = (NP > 1 || gemm2_sm100_eligible(pool, T)) ? launch_gemm2_sm100(&v, o, st) : launch_gemm_sm100(&v, o, st);
-            if (rc != MARLAAS_OK) return rc;
-            const int nvec = (int)(pool->K / 8);
-            k_drop_expand<<<stream_grid(pool, T * nvec), 256, 0, st>>>(T, nvec, (bf16*)dx, lddx, ws.g, (int64_t)plane, pool->d_At,
-                                                                       (int64_t)pool->cap * pool->RP * pool->K, (int)pool->K, pool->RP, NP,
-                                                                       ws.tok_slot, pool->d_rank, d.scale, d.limit, key);
-            MARLAAS_LAUNCH_CHECK("k_drop_expand");
+            if ((rc = launch_gemm2_dropped(&v, o, DropMask{ws.tok_slot, d.limit, key}, st)) != MARLAAS_OK) return rc;
         }
         if (want_dB && !h_saved)
             for (int p = 0; p < NP; ++p)

@@ -19,8 +19,17 @@
 //                gradient) the exponentials in bf16; the logits themselves are never written
 //   EPI_GRAD     the product over the vocabulary is cut along it into `splits` ranges, so that few row tiles still fill the
 //                SMs; each (range, tile) leaves an fp32 tile, or the output itself when there is one range
+//
+// EPI_DROP is the dx product of the layer with dropout in its adapters (dropout.cu), whose low-rank term is masked element by
+// element before it joins the sum.  The term of a tile is multiplied first, in the middle of the tile before; the epilogue warps
+// read it from tensor memory, zero what the mask drops and write it back as the value that the tile's main loop starts from:
+// the masks (about 3000 cycles of the generator per tile) are made while the other buffer's main loop runs, and the sum is
+// rounded once.
+//   lfull[b]  one per CTA: the low-rank term of the buffer's next tile is there
+//   minit[b]  leader's barrier, 8 arrivals: it is masked in both CTAs
 #include <string.h>
 
+#include "dropout.cuh"
 #include "sm100_ptx.cuh"
 
 namespace marlaas {
@@ -50,9 +59,10 @@ struct Gemm2Args {
     int64_t ldc;
     int32_t* status;
     HeadEpilogue head;                      // EPI_SOFTMAX, EPI_GRAD
+    DropMask drop;                          // EPI_DROP
 };
 
-enum { EPI_LAYER = 0, EPI_SOFTMAX = 1, EPI_GRAD = 2 };
+enum { EPI_LAYER = 0, EPI_SOFTMAX = 1, EPI_GRAD = 2, EPI_DROP = 3 };
 
 // the parts whose low-rank term enters output columns n0 ...
 __device__ __forceinline__ void tile_parts(const Gemm2Args& g, int n0, int& p_lo, int& p_hi) {
@@ -248,6 +258,49 @@ __device__ __forceinline__ void head_grad_tile(const HeadEpilogue& h, uint32_t t
     }
 }
 
+__device__ __forceinline__ void tc_st_32x32(uint32_t taddr, const uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+          "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]),
+          "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]),
+          "r"(v[31]), "r"(taddr)
+        : "memory");
+}
+
+// A row's part of a tile's low-rank term with the dropped elements zeroed, in tensor memory.
+__device__ __forceinline__ void drop_tile(const DropMask& d, uint32_t trow, int row, bool on, int n0, int Nout) {
+    uint32_t limit = 0;
+    if (on) {
+        const int t = d.tok_slot[row];
+        if (t >= 0) limit = d.limit[t];
+    }
+    if (__all_sync(0xffffffffu, limit == 0)) return;
+    const int cols = min(G2_BN, Nout - n0);
+#pragma unroll 1
+    for (int c = 0; c < cols; c += 32) {
+        uint32_t v[32];
+        __syncwarp();
+        tc_ld_32x32(trow + c, v);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint4 bits = drop_bits(d.key, (uint32_t)((n0 + c) / 8 + e), (uint32_t)row);
+            const uint32_t* w = &bits.x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[8 * e + 2 * i] = (w[i] & 0xffffu) >= limit ? v[8 * e + 2 * i] : 0u;
+                v[8 * e + 2 * i + 1] = (w[i] >> 16) >= limit ? v[8 * e + 2 * i + 1] : 0u;
+            }
+        }
+        __syncwarp();
+        tc_st_32x32(trow + c, v);
+    }
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 // KP = 64-deep panels per pipeline step.  KP = 2 (contraction depth a multiple of 64): x / dy and a K-major W are viewed as
 // 3-D tensors so that ONE TMA instruction brings both panels, and the barrier wait / expect / commit of the two issuing
 // threads is paid once per 128 of depth; KP = 1 is the plain 2-D form for any depth.
@@ -268,14 +321,16 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     const uint32_t bar_tfull = bar_empty + 8 * STAGES;
     const uint32_t bar_tempty = bar_tfull + 16;
     const uint32_t bar_drain = bar_tempty + 16;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
+    const uint32_t bar_lfull = bar_drain + 8, bar_minit = bar_lfull + 16;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 9);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();      // 0 = leader
     const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
-    const int M = EPI == EPI_LAYER ? g.M : head_rows(g.head, g.M);
-    const int num_m_tiles = EPI == EPI_LAYER ? g.num_m_tiles : (M + 255) / 256;
+    constexpr bool HEAD = EPI == EPI_SOFTMAX || EPI == EPI_GRAD;
+    const int M = HEAD ? head_rows(g.head, g.M) : g.M;
+    const int num_m_tiles = HEAD ? (M + 255) / 256 : g.num_m_tiles;
     const int plane_tiles = num_m_tiles * g.num_n_tiles;
     const int splits = EPI == EPI_GRAD ? head_splits(g.head, plane_tiles, (int)g.num_kb * KP) : 1;
     const int num_tiles = plane_tiles * splits;       // work items: the tiles of the first range of k, then of the next
@@ -300,6 +355,8 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar_tfull + 8 * b, 1);
             mbar_init(bar_tempty + 8 * b, 8);
+            mbar_init(bar_lfull + 8 * b, 1);
+            mbar_init(bar_minit + 8 * b, 8);
         }
         mbar_init(bar_drain, 1);
         *abort_word = 0;
@@ -330,6 +387,37 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             uint32_t it = 0, s = 0, ph = 0;     // blocks issued; stage and phase bit of the next block
             bool ok = true, waited = false;
             const uint32_t full0 = map_to_cta(bar_full, 0);      // the leader's full barriers (8 bytes apart)
+            // the low-rank steps of a tile: four 16-deep units each
+            auto low_rank = [&](int m_idx, int n_idx) {
+                const int m0 = m_idx * 256, n0 = n_idx * G2_BN;
+                const int my_m = m0 + (int)rank * 128, my_n = n0 + (int)rank * 128;
+                const bool have_rows = my_m < M;
+                const int nchunk = half_chunks(g, n0, (int)rank);
+                const int nun = !HEAD && g.tile_nunits ? g.tile_nunits[m_idx] : 0;
+                int p_lo, p_hi;
+                tile_parts(g, n0, p_lo, p_hi);
+                for (int p = p_lo; p < p_hi; ++p)
+                for (int x0 = 0; x0 < nun && ok; x0 += 4, ++it) {
+                    if (!(ok = mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_word, 32))) break;
+                    const uint32_t full = full0 + 8 * s;
+                    const int nv = min(4, nun - x0);
+                    if (rank == 0)
+                        mbar_expect_tx(bar_full + 8 * s, extra_bytes(g, m0, n0, 0, nv) + extra_bytes(g, m0, n0, 1, nv));
+                    if (have_rows) tma_load_2d_pair(sA + s * A_ST, &tmXA, full, x0 * 16, my_m + p * g.M);
+                    for (int u = 0; u < nv; ++u) {
+                        const int row = g.tile_units[(size_t)m_idx * g.umax + x0 + u] + (g.all_parts ? p * g.xb_part_rows : 0);
+                        for (int c = 0; c < nchunk; ++c)
+                            tma_load_2d_pair(sB + s * B_ST + c * CHUNK_BYTES + u * UNIT_BYTES, &tmXB, full,
+                                             my_n + c * 64, row);
+                    }
+                    if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
+                }
+            };
+            if (EPI == EPI_DROP && pair < num_tiles) {
+                int m_idx, n_idx;
+                decode_tile2(g, num_m_tiles, pair, m_idx, n_idx);
+                low_rank(m_idx, n_idx);
+            }
             for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
                 int m_idx, n_idx, kb0, kb1;
                 item(tile, m_idx, n_idx, kb0, kb1);
@@ -339,6 +427,12 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 const int nchunk = half_chunks(g, n0, (int)rank);
                 const uint32_t stage_tx = main_bytes(g, M, m0, n0, 0, KP) + main_bytes(g, M, m0, n0, 1, KP);
                 for (int kb = kb0; kb < kb1 && ok; ++kb, ++it) {
+                    if (EPI == EPI_DROP && kb == g.num_kb / 2 && tile + num_pairs < num_tiles) {
+                        int m_next, n_next;
+                        decode_tile2(g, num_m_tiles, tile + num_pairs, m_next, n_next);
+                        low_rank(m_next, n_next);
+                        if (!ok) break;
+                    }
                     if (!(ok = mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_word, 31))) break;
                     const uint32_t full = full0 + 8 * s;
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, stage_tx);
@@ -359,25 +453,7 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     asm volatile("griddepcontrol.wait;" ::: "memory");
                     waited = true;
                 }
-                const int nun = EPI == EPI_LAYER && g.tile_nunits ? g.tile_nunits[m_idx] : 0;
-                int p_lo, p_hi;
-                tile_parts(g, n0, p_lo, p_hi);
-                for (int p = p_lo; p < p_hi; ++p)
-                for (int x0 = 0; x0 < nun && ok; x0 += 4, ++it) {
-                    if (!(ok = mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_word, 32))) break;
-                    const uint32_t full = full0 + 8 * s;
-                    const int nv = min(4, nun - x0);
-                    if (rank == 0)
-                        mbar_expect_tx(bar_full + 8 * s, extra_bytes(g, m0, n0, 0, nv) + extra_bytes(g, m0, n0, 1, nv));
-                    if (have_rows) tma_load_2d_pair(sA + s * A_ST, &tmXA, full, x0 * 16, my_m + p * g.M);
-                    for (int u = 0; u < nv; ++u) {
-                        const int row = g.tile_units[(size_t)m_idx * g.umax + x0 + u] + (g.all_parts ? p * g.xb_part_rows : 0);
-                        for (int c = 0; c < nchunk; ++c)
-                            tma_load_2d_pair(sB + s * B_ST + c * CHUNK_BYTES + u * UNIT_BYTES, &tmXB, full,
-                                             my_n + c * 64, row);
-                    }
-                    if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
-                }
+                if (EPI == EPI_LAYER) low_rank(m_idx, n_idx);
             }
             if (!ok && rank == 0) {
                 // let the copies already issued land (bounded) before shared memory is released
@@ -404,15 +480,62 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             const uint64_t da_base = desc_k_major(sA);
             const uint64_t db_base = g.b_mn ? desc_mn_major(sB, KP * CHUNK_BYTES) : desc_k_major(sB);
             const uint64_t db_step = g.b_mn ? (uint64_t)(UNIT_BYTES >> 4) : 2ull;
+            // the low-rank steps of a tile, into the accumulator at d_tmem; true if there were any
+            auto low_rank = [&](int m_idx, int n_idx, uint32_t d_tmem, uint32_t& acc) -> bool {
+                const int nun = !HEAD && g.tile_nunits ? g.tile_nunits[m_idx] : 0;
+                int p_lo, p_hi;
+                tile_parts(g, n_idx * G2_BN, p_lo, p_hi);
+                for (int p = p_lo; p < p_hi; ++p)
+                for (int x0 = 0; x0 < nun && ok; x0 += 4) {
+                    if (!(ok = mbar_wait(bar_full + 8 * s, ph, abort_word, 35))) break;
+                    tc_fence_after();
+                    const uint32_t a0 = sA + s * A_ST, b0 = sB + s * B_ST;
+                    const int nv = min(4, nun - x0);
+                    for (int u = 0; u < nv; ++u) {
+                        tc_mma_bf16_pair(d_tmem, desc_k_major(a0 + u * 32),
+                                         desc_mn_major(b0 + u * UNIT_BYTES, CHUNK_BYTES), idesc_mn, acc);
+                        acc = 1;
+                    }
+                    tc_commit_pair(bar_empty + 8 * s);
+                    if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
+                }
+                return nun > 0;
+            };
+            // EPI_DROP: the low-rank term of tile number j of this pair, into its buffer
+            uint32_t masked[2] = {0, 0};        // terms handed to the epilogue per buffer
+            bool starts[2] = {false, false};    // the buffer's next main loop starts from such a term
+            auto next_term = [&](int tile, uint32_t j) {
+                const uint32_t b = j & 1, aph = (j >> 1) & 1;
+                if (!(ok = mbar_wait(bar_tempty + 8 * b, aph ^ 1, abort_word, 33))) return;
+                tc_fence_after();
+                int m_idx, n_idx;
+                decode_tile2(g, num_m_tiles, tile, m_idx, n_idx);
+                uint32_t acc = 0;
+                starts[b] = low_rank(m_idx, n_idx, tmem_base + b * G2_BN, acc);
+                if (ok && starts[b]) tc_commit_pair(bar_lfull + 8 * b);
+            };
+            if (EPI == EPI_DROP && pair < num_tiles) next_term(pair, 0);
             for (int tile = pair; tile < num_tiles && ok; tile += num_pairs, ++lt) {
                 int m_idx, n_idx, kb0, kb1;
                 item(tile, m_idx, n_idx, kb0, kb1);
                 const uint32_t b = lt & 1, aph = (lt >> 1) & 1;
-                if (!(ok = mbar_wait(bar_tempty + 8 * b, aph ^ 1, abort_word, 33))) break;
+                uint32_t acc = 0;
+                if (EPI == EPI_DROP) {
+                    if (starts[b]) {
+                        if (!(ok = mbar_wait(bar_minit + 8 * b, masked[b] & 1, abort_word, 37))) break;
+                        ++masked[b];
+                        acc = 1;
+                    }
+                } else {
+                    if (!(ok = mbar_wait(bar_tempty + 8 * b, aph ^ 1, abort_word, 33))) break;
+                }
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + b * G2_BN;
-                uint32_t acc = 0;
                 for (int kb = kb0; kb < kb1 && ok; ++kb) {
+                    if (EPI == EPI_DROP && kb == g.num_kb / 2 && tile + num_pairs < num_tiles) {
+                        next_term(tile + num_pairs, lt + 1);
+                        if (!ok) break;
+                    }
                     if (!(ok = mbar_wait(bar_full + 8 * s, ph, abort_word, 34))) break;
                     const uint64_t da = da_base + (uint64_t)(s * (A_ST >> 4));
                     const uint64_t db = db_base + (uint64_t)(s * (B_ST >> 4));
@@ -434,23 +557,7 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     asm volatile("griddepcontrol.wait;" ::: "memory");
                     waited = true;
                 }
-                const int nun = EPI == EPI_LAYER && g.tile_nunits ? g.tile_nunits[m_idx] : 0;
-                int p_lo, p_hi;
-                tile_parts(g, n_idx * G2_BN, p_lo, p_hi);
-                for (int p = p_lo; p < p_hi; ++p)
-                for (int x0 = 0; x0 < nun && ok; x0 += 4) {
-                    if (!(ok = mbar_wait(bar_full + 8 * s, ph, abort_word, 35))) break;
-                    tc_fence_after();
-                    const uint32_t a0 = sA + s * A_ST, b0 = sB + s * B_ST;
-                    const int nv = min(4, nun - x0);
-                    for (int u = 0; u < nv; ++u) {
-                        tc_mma_bf16_pair(d_tmem, desc_k_major(a0 + u * 32),
-                                         desc_mn_major(b0 + u * UNIT_BYTES, CHUNK_BYTES), idesc_mn, acc);
-                        acc = 1;
-                    }
-                    tc_commit_pair(bar_empty + 8 * s);
-                    if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
-                }
+                if (EPI == EPI_LAYER) low_rank(m_idx, n_idx, d_tmem, acc);
                 if (ok) tc_commit_pair(bar_tfull + 8 * b);
             }
             if (!ok) {
@@ -468,7 +575,31 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const uint32_t tempty_leader0 = map_to_cta(bar_tempty, 0);
         uint32_t lt = 0;
         bool ok = true;
+        // EPI_DROP: masks the low-rank term of tile number j of this pair once it is there
+        const uint32_t minit_leader0 = map_to_cta(bar_minit, 0);
+        uint32_t masked[2] = {0, 0};
+        auto mask_term = [&](int tile, uint32_t j) {
+            int m_idx, n_idx;
+            decode_tile2(g, num_m_tiles, tile, m_idx, n_idx);
+            if (g.tile_nunits[m_idx] == 0) return;
+            const uint32_t b = j & 1;
+            ok = mbar_wait(bar_lfull + 8 * b, masked[b] & 1, abort_word, 38);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
+            ++masked[b];
+            tc_fence_after();
+            const int row = m_idx * 256 + (int)rank * 128 + q * 32 + lane;
+            drop_tile(g.drop, tmem_base + ((uint32_t)(q * 32) << 16) + b * G2_BN, row, row < M, n_idx * G2_BN, g.Nout);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(minit_leader0 + 8 * b);
+        };
+        if (EPI == EPI_DROP && pair < num_tiles) mask_term(pair, 0);
         for (int tile = pair; tile < num_tiles && ok; tile += num_pairs, ++lt) {
+            if (EPI == EPI_DROP && tile + num_pairs < num_tiles) {
+                mask_term(tile + num_pairs, lt + 1);
+                if (!ok) break;
+            }
             int m_idx, n_idx, kb0, kb1;
             item(tile, m_idx, n_idx, kb0, kb1);
             const int m0 = m_idx * 256 + (int)rank * 128, n0 = n_idx * G2_BN;
@@ -535,7 +666,8 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 bool gemm2_sm100_eligible(const marlaas_pool* pool, int64_t M) { return M >= 1024 && pool->sm_count >= 2; }
 
 template <int KP, int EPI>
-static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st, const HeadEpilogue* head = nullptr) {
+static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st, const HeadEpilogue* head = nullptr,
+                                       const DropMask* drop = nullptr) {
     using namespace sm100;
     Gemm2Args g;
     g.M = (int)o.M;
@@ -561,6 +693,8 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     g.status = pool->d_status;
     if (head) g.head = *head;
     else memset(&g.head, 0, sizeof(g.head));
+    if (drop) g.drop = *drop;
+    else memset(&g.drop, 0, sizeof(g.drop));
 
     alignas(64) CUtensorMap tmA, tmB, tmXA, tmXB;
     marlaas_status_t rc;
@@ -611,7 +745,7 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    // (the head's kernels read what the kernel before them wrote from their first step on)
+    // (the other forms read what the kernel before them wrote from their first step on)
     cfg.attrs = at; cfg.numAttrs = EPI == EPI_LAYER ? 1 : 0;
     MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_gemm2_sm100<KP, EPI>, tmA, tmB, tmXA, tmXB, g));
     count_launch();
@@ -622,6 +756,10 @@ marlaas_status_t launch_gemm2_sm100(const marlaas_pool* pool, const GemmOperands
     if (o.M <= 0) return MARLAAS_OK;
     // two panels per step need the contraction depth in whole 64-deep panels (3-D views of the row-major operands)
     return (o.Kc % 64) == 0 ? launch_gemm2_t<2, sm100::EPI_LAYER>(pool, o, st) : launch_gemm2_t<1, sm100::EPI_LAYER>(pool, o, st);
+}
+
+marlaas_status_t launch_gemm2_dropped(const marlaas_pool* pool, const GemmOperands& o, const DropMask& d, cudaStream_t st) {
+    return (o.Kc % 64) == 0 ? launch_gemm2_t<2, sm100::EPI_DROP>(pool, o, st, nullptr, &d) : launch_gemm2_t<1, sm100::EPI_DROP>(pool, o, st, nullptr, &d);
 }
 
 int head_pairs(const marlaas_pool* pool) { return pool->sm_count / 2; }

@@ -209,6 +209,20 @@ marlaas_status_t launch_gemm_sm100(const marlaas_pool* pool, const GemmOperands&
 bool gemm2_sm100_eligible(const marlaas_pool* pool, int64_t M);
 marlaas_status_t launch_gemm2_sm100(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st);
 
+// The counter-based generator's key and the counter's fixed half (dropout.cuh).
+struct DropKey {
+    uint32_t k0, k1, o0, o1;
+};
+
+// The masks of a dx product with dropout (dropout.cu): the share of 65536 that a tenant's elements are dropped by, per slot.
+struct DropMask {
+    const int32_t* tok_slot;           // [M]
+    const uint32_t* limit;             // [cap]
+    DropKey key;
+};
+// dx = dy W^T + m o (XA XB): launch_gemm2_sm100 with the low-rank term masked, for any number of rows
+marlaas_status_t launch_gemm2_dropped(const marlaas_pool* pool, const GemmOperands& o, const DropMask& d, cudaStream_t st);
+
 // The vocabulary head's cross entropy (head.cu), whose products run gemm2_sm100.cu's main loop: the rows are the batch's tokens
 // that count, in order, of which this launch takes those from row0 on.
 struct HeadEpilogue {
@@ -331,11 +345,6 @@ marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf
                                    const Workspace& ws, bool acc, cudaStream_t st);
 // pool.cu: the pool with other scales of its slots, for the kernel launchers alone (no streams)
 void scaled_view(const marlaas_pool* pool, const float* d_scale, marlaas_pool* view);
-
-// The counter-based generator's key and the counter's fixed half (dropout.cuh).
-struct DropKey {
-    uint32_t k0, k1, o0, o1;
-};
 
 // vocab_rows.cu: one pass over rows of logits (softmax statistics, the policy loss's per-token terms, the gradient)
 struct PolicyTerms {           // what a token adds to its tenant's stats

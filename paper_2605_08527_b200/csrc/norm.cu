@@ -401,31 +401,34 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
     if (a.partial) flush();
 }
 
-// dgain and dbias of one tenant, 32 columns per CTA: eight warps share the tenant's partial sums, then a fixed tree.
-__global__ void __launch_bounds__(256) k_norm_reduce(const NormArgs a) {
-    __shared__ float s_sum[8][2][32];
-    const int key = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+// dgain and dbias of one tenant, 32 columns per CTA: the warps share the tenant's partial sums, four at a time on their way, then
+// add up in their order.
+__global__ void __launch_bounds__(1024) k_norm_reduce(const NormArgs a) {
+    __shared__ float s_sum[2][32][33];
+    const int key = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, c = blockIdx.x * 32 + lane;
     const int64_t b = a.key_off[key], e = a.key_off[key + 1];
-    const bool on = c < a.d;
     float g = 0.f, h = 0.f;
-    if (e > b && on) {
-        const int64_t q1 = (e - 1) / a.rows_per_group;
-        for (int64_t q = b / a.rows_per_group + warp; q <= q1; q += 8) {
-            const float* in = a.partial + (size_t)(q + key) * 2 * a.d + c;
-            g += in[0];
-            if (a.dbias) h += in[a.d];
+    if (e > b) {
+        if (c < a.d) {
+            const int q0 = (int)(b / a.rows_per_group), q1 = (int)((e - 1) / a.rows_per_group);
+            const float* in = a.partial + (size_t)key * 2 * a.d + c;
+#pragma unroll 4
+            for (int q = q0 + warp; q <= q1; q += warps) {
+                g += in[(size_t)q * 2 * a.d];
+                if (a.dbias) h += in[(size_t)q * 2 * a.d + a.d];
+            }
         }
+        s_sum[0][warp][lane] = g;
+        s_sum[1][warp][lane] = h;
+        __syncthreads();
     }
-    s_sum[warp][0][lane] = g;
-    s_sum[warp][1][lane] = h;
-    __syncthreads();
-    if (warp >= 2 || !on) return;
+    if (warp >= 2 || c >= a.d) return;
     float* out = warp == 0 ? a.dgain : a.dbias;
     if (!out) return;
     out += (size_t)key * a.d + c;
     float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) v += s_sum[w][warp][lane];
+    if (e > b)
+        for (int w = 0; w < warps; ++w) v += s_sum[warp][w][lane];
     *out = a.accumulate ? *out + v : v;
 }
 
@@ -434,14 +437,15 @@ struct NormPlan {
     int NV, W, G;
     int64_t groups, rows;
 };
-static NormPlan norm_plan(const marlaas_pool* pool, int64_t T, int d) {
+static NormPlan norm_plan(const marlaas_pool* pool, int64_t T, int d, bool backward) {
     NormPlan p;
     const int nvec = d / 8;
     p.NV = nvec <= 1024 ? 1 : 2;
     p.W = (int)cdiv(nvec, 32 * p.NV);
     p.G = std::max(1, std::min(NORM_MAX_GROUPS, 16 / p.W));
     const int64_t most = (int64_t)pool->sm_count * std::max(1, 1024 / (32 * p.W * p.G)) * p.G;      // 1024 threads per SM
-    p.rows = std::max<int64_t>(cdiv(T, most), 1);
+    // (a group's partial sums cost as much as four of its rows: backward, no group takes fewer)
+    p.rows = std::max<int64_t>(cdiv(T, most), backward ? 4 : 1);
     p.groups = cdiv(cdiv(T, p.rows), p.G) * p.G;
     return p;
 }
@@ -464,7 +468,7 @@ static NormWorkspace carve_norm(const marlaas_pool* pool, int64_t T, int32_t S, 
     w.off = (int32_t*)take(sizeof(int32_t) * ((size_t)S + 1));
     w.slot = (int32_t*)take(sizeof(int32_t) * (size_t)S);
     if (backward) {
-        const NormPlan n = norm_plan(pool, T, (int)d);
+        const NormPlan n = norm_plan(pool, T, (int)d, true);
         w.perm = (int32_t*)take(sizeof(int32_t) * (size_t)T);
         w.key_off = (int32_t*)take(sizeof(int32_t) * ((size_t)pool->cap + 2));
         w.scratch = (int32_t*)take(sizeof(int32_t) * order_scratch_ints(T, pool->cap + 1));
@@ -493,7 +497,7 @@ static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& 
     return MARLAAS_OK;
 }
 static marlaas_status_t launch_norm(const marlaas_pool* pool, NormArgs a, bool rms, bool backward, cudaStream_t st) {
-    const NormPlan n = norm_plan(pool, a.T, a.d);
+    const NormPlan n = norm_plan(pool, a.T, a.d, backward);
     a.rows_per_group = n.rows;
     if (n.NV == 2) return rms ? launch_norm_t<2, 1024, true>(pool, a, n, backward, st) : launch_norm_t<2, 1024, false>(pool, a, n, backward, st);
     if (n.W > 16) return rms ? launch_norm_t<1, 1024, true>(pool, a, n, backward, st) : launch_norm_t<1, 1024, false>(pool, a, n, backward, st);
@@ -618,7 +622,7 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
         return fail(MARLAAS_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < required %zu", fn, workspace_bytes, ws.total_bytes);
     MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
     if ((rc = reject_host_table_in_capture(fn, flags, st)) != MARLAAS_OK) return rc;
-    const NormPlan n = norm_plan(pool, T, (int)d);
+    const NormPlan n = norm_plan(pool, T, (int)d, true);
     NormArgs a;
     memset(&a, 0, sizeof(a));
     a.T = T; a.d = (int)d; a.S = seg->num_segments; a.cap = pool->cap;
@@ -637,7 +641,9 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
     rc = launch_norm(pool, a, rms, true, st);
     if (rc != MARLAAS_OK) return rc;
     if (a.partial) {
-        k_norm_reduce<<<dim3((unsigned)cdiv(d, 32), (unsigned)(pool->cap + 1)), 256, 0, st>>>(a);
+        int warps = 4;              // one per 32 groups
+        while (warps < 32 && warps * 32 < n.groups) warps *= 2;
+        k_norm_reduce<<<dim3((unsigned)cdiv(d, 32), (unsigned)(pool->cap + 1)), warps * 32, 0, st>>>(a);
         MARLAAS_LAUNCH_CHECK("k_norm_reduce");
     }
     return finish(pool, flags, st);
