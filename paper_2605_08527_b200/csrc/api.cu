@@ -186,6 +186,17 @@ marlaas_status_t reject_captured_tables(const char* fn, const marlaas_pool* pool
     return MARLAAS_OK;
 }
 
+// The pool's side stream and its events, on first use.
+marlaas_status_t make_side_stream(marlaas_pool* pool) {
+    if (pool->side) return MARLAAS_OK;
+    int lo = 0, hi = 0;
+    MARLAAS_CUDA_TRY(cudaDeviceGetStreamPriorityRange(&lo, &hi));
+    MARLAAS_CUDA_TRY(cudaStreamCreateWithPriority(&pool->side, cudaStreamNonBlocking, lo));   // lowest priority
+    MARLAAS_CUDA_TRY(cudaEventCreateWithFlags(&pool->ev_fork, cudaEventDisableTiming));
+    MARLAAS_CUDA_TRY(cudaEventCreateWithFlags(&pool->ev_join, cudaEventDisableTiming));
+    return MARLAAS_OK;
+}
+
 // dA and dB of all slots on one stream, for the plan, g and (T > 0) h in the workspace or as saved: what marlaas_lora_backward
 // does when it does not run them beside the dx product.
 marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
@@ -539,13 +550,7 @@ marlaas_status_t marlaas_lora_backward(marlaas_pool_t* pool, int64_t T, const vo
     const bool gemm2 = NP > 1 || gemm2_sm100_eligible(pool, T);
     const bool overlap = fits0 && T > 0 && dx && (!want_dB || h_saved) && gemm2_sm100_eligible(pool, T) && pool->cap <= 64;
     if (overlap) {
-        if (!pool->side) {
-            int lo = 0, hi = 0;
-            MARLAAS_CUDA_TRY(cudaDeviceGetStreamPriorityRange(&lo, &hi));
-            MARLAAS_CUDA_TRY(cudaStreamCreateWithPriority(&pool->side, cudaStreamNonBlocking, lo));   // lowest priority
-            MARLAAS_CUDA_TRY(cudaEventCreateWithFlags(&pool->ev_fork, cudaEventDisableTiming));
-            MARLAAS_CUDA_TRY(cudaEventCreateWithFlags(&pool->ev_join, cudaEventDisableTiming));
-        }
+        if ((rc = make_side_stream(pool)) != MARLAAS_OK) return rc;
         MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_fork, st));
     }
     if (T > 0 && dx && tc_path) {

@@ -172,21 +172,60 @@ marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, 
     const int NP = pool->P;
     const size_t plane = (size_t)T * pool->RP;
     if ((rc = launch_drop_tables(pool, drop, d, st)) != MARLAAS_OK) return rc;
-    if (T > 0) {
-        if ((rc = make_plan(&v, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
-        if (want_dA || (want_dB && !h_saved))
-            if ((rc = launch_drop_rows(pool, T, (const bf16*)x, ldx, ws, d, key, st)) != MARLAAS_OK) return rc;
-        if (dx || want_dA)
-            for (int p = 0; p < NP; ++p) {
-                const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
-                const Workspace wp = part_workspace(pool, ws, p, T);
-                if ((rc = shrink(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st)) != MARLAAS_OK) return rc;
-            }
-        if (dx) {
-            GemmOperands o;
-            backward_operands(pool, T, (const bf16*)W, ldw, (const bf16*)dy, lddy, (bf16*)dx, lddx, ws, &o);
-            if ((rc = launch_gemm2_dropped(&v, o, DropMask{ws.tok_slot, d.limit, key}, st)) != MARLAAS_OK) return rc;
+    if (T > 0 && (rc = make_plan(&v, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
+    auto masked_rows = [&](cudaStream_t s) { return launch_drop_rows(pool, T, (const bf16*)x, ldx, ws, d, key, s); };
+    auto g_of_dy = [&]() -> marlaas_status_t {
+        for (int p = 0; p < NP; ++p) {
+            const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
+            const Workspace wp = part_workspace(pool, ws, p, T);
+            const marlaas_status_t r = shrink(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st);
+            if (r != MARLAAS_OK) return r;
         }
+        return MARLAAS_OK;
+    };
+    auto product = [&]() {
+        GemmOperands o;
+        backward_operands(pool, T, (const bf16*)W, ldw, (const bf16*)dy, lddy, (bf16*)dx, lddx, ws, &o);
+        return launch_gemm2_dropped(&v, o, DropMask{ws.tok_slot, d.limit, key}, st);
+    };
+    // As in marlaas_lora_backward: where the reductions are certain to fit, all that the adapters' gradients need besides g is made
+    // on the pool's side stream beside the dx product, and the reductions take the SMs that the product leaves (8192 x 4096 x 4096,
+    // 32 tenants of rank 16: 364 us one after another, 321 so).
+    const bool fits = grad_sm100_eligible(pool, T) && cdiv(T, 64) + (int64_t)seg->num_segments <= (int64_t)ws.max_copies;
+    if (T >= 1024 && NP == 1 && fits && dx && (want_dA || want_dB) && (!want_dB || h_saved) && pool->cap <= 64) {
+        if ((rc = make_side_stream(pool)) != MARLAAS_OK) return rc;
+        cudaStream_t gs = pool->side;
+        MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_fork, st));
+        MARLAAS_CUDA_TRY(cudaStreamWaitEvent(gs, pool->ev_fork, 0));
+        // whatever happens from here on, the side stream is joined again before the call returns
+        auto work = [&]() -> marlaas_status_t {
+            marlaas_status_t r;
+            if ((r = launch_grad_plan(&v, T, ws, gs)) != MARLAAS_OK) return r;
+            if (want_dB && (r = launch_grad_sm100(&v, T, pool->N, (const bf16*)dy, lddy, h_saved, nullptr, dB_slots, false, acc, ws, gs, ws.hm,
+                                                  GRAD_PHASE_COPIES)) != MARLAAS_OK) return r;
+            if ((r = g_of_dy()) != MARLAAS_OK) return r;
+            MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_fork, st));
+            if ((r = product()) != MARLAAS_OK) return r;
+            if (want_dA && (r = masked_rows(gs)) != MARLAAS_OK) return r;
+            MARLAAS_CUDA_TRY(cudaStreamWaitEvent(gs, pool->ev_fork, 0));
+            if (want_dA && (r = launch_grad_sm100(&v, T, pool->K, d.xd, pool->K, ws.g, nullptr, dA_slots, true, acc, ws, gs, ws.hm2,
+                                                  GRAD_PHASE_COPIES)) != MARLAAS_OK) return r;
+            if (want_dB && (r = launch_grad_sm100(&v, T, pool->N, (const bf16*)dy, lddy, h_saved, nullptr, dB_slots, false, acc, ws, gs, ws.hm,
+                                                  GRAD_PHASE_REDUCE)) != MARLAAS_OK) return r;
+            if (want_dA && (r = launch_grad_sm100(&v, T, pool->K, d.xd, pool->K, ws.g, nullptr, dA_slots, true, acc, ws, gs, ws.hm2,
+                                                  GRAD_PHASE_REDUCE | (want_dB ? GRAD_PHASE_EARLY : 0))) != MARLAAS_OK) return r;
+            return MARLAAS_OK;
+        };
+        rc = work();
+        MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_join, gs));
+        MARLAAS_CUDA_TRY(cudaStreamWaitEvent(st, pool->ev_join, 0));
+        if (rc != MARLAAS_OK) return rc;
+        return finish(pool, flags, st);
+    }
+    if (T > 0) {
+        if ((want_dA || (want_dB && !h_saved)) && (rc = masked_rows(st)) != MARLAAS_OK) return rc;
+        if ((dx || want_dA) && (rc = g_of_dy()) != MARLAAS_OK) return rc;
+        if (dx && (rc = product()) != MARLAAS_OK) return rc;
         if (want_dB && !h_saved)
             for (int p = 0; p < NP; ++p)
                 if ((rc = shrink(&v, T, d.xd, pool->K, pool->K, pool->d_At + (size_t)p * pool->cap * pool->RP * pool->K, pool->K,

@@ -339,6 +339,7 @@ void forward_operands(const marlaas_pool* pool, int64_t T, const bf16* x, int64_
                       const Workspace& ws, GemmOperands* o);
 void backward_operands(const marlaas_pool* pool, int64_t T, const bf16* W, int64_t ldw, const bf16* dy, int64_t lddy, bf16* dx, int64_t lddx,
                        const Workspace& ws, GemmOperands* o);
+marlaas_status_t make_side_stream(marlaas_pool* pool);
 marlaas_status_t reject_captured_tables(const char* fn, const marlaas_pool* pool, cudaStream_t st);
 marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
                                    float* const* dA_slots, float* const* dB_slots, const marlaas_segments_t* seg, const float* h,
