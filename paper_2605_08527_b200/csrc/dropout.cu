@@ -30,12 +30,13 @@ static DropTables carve_drop(const marlaas_pool* pool, int64_t T, char* base, si
     return t;
 }
 
+// s'_t and the limits of all tenants.
+__device__ __forceinline__ uint32_t drop_limit(float p) { return p > 0.f ? (uint32_t)rintf(fminf(p, 1.f) * 65536.f) : 0u; }
 __global__ void k_drop_tables(int cap, const float* __restrict__ rates, const float* __restrict__ d_scale, uint32_t* __restrict__ limit,
                               float* __restrict__ scale) {
     const int t = blockIdx.x * blockDim.x + threadIdx.x;
     if (t >= cap) return;
-    const float p = rates[t];
-    const uint32_t l = p > 0.f ? (uint32_t)rintf(fminf(p, 1.f) * 65536.f) : 0u;
+    const uint32_t l = drop_limit(rates[t]);
     limit[t] = l;
     scale[t] = l < 65536u ? d_scale[t] * (65536.f / (float)(65536u - l)) : 0.f;
 }
@@ -68,6 +69,28 @@ static marlaas_status_t launch_drop_rows(const marlaas_pool* pool, int64_t T, co
 static marlaas_status_t launch_drop_tables(const marlaas_pool* pool, const marlaas_dropout_t* drop, const DropTables& d, cudaStream_t st) {
     k_drop_tables<<<(unsigned)cdiv(pool->cap, 256), 256, 0, st>>>(pool->cap, drop->rates, pool->d_scale, d.limit, d.scale);
     MARLAAS_LAUNCH_CHECK("k_drop_tables");
+    return MARLAAS_OK;
+}
+
+// h = (m o x) A of all projections.  From 512 tokens on the shrink kernels mask the rows themselves; for fewer, whose shrink reads a
+// row once per rank, they are masked first.
+static marlaas_status_t masked_shrink(const marlaas_pool* v, int64_t T, const bf16* x, int64_t ldx, const Workspace& ws, const DropTables& d,
+                                      const DropKey& key, float* h, bool h_is_zero, bool rows_masked, cudaStream_t st) {
+    marlaas_status_t rc;
+    const int NP = v->P;
+    const DropMask mask = {ws.tok_slot, d.limit, key};
+    if (T < 512 && !rows_masked && (rc = launch_drop_rows(v, T, x, ldx, ws, d, key, st)) != MARLAAS_OK) return rc;
+    if (NP > 1 && T >= 512 && shrink_split_sm100_parts_eligible(v, T, v->K, NP))
+        return launch_shrink_split_sm100(v, T, x, ldx, v->K, v->d_At, v->K, ws, h, st, h_is_zero, NP, &mask);
+    for (int p = 0; p < NP; ++p) {
+        const bf16* At = v->d_At + (size_t)p * v->cap * v->RP * v->K;
+        const Workspace wp = part_workspace(v, ws, p, T);
+        float* hp = h + (size_t)p * T * v->RP;
+        if (T < 512) rc = launch_shrink_hd(v, T, d.xd, v->K, v->K, At, v->K, wp, hp, st);
+        else if (shrink_split_sm100_eligible(v, T, v->K)) rc = launch_shrink_split_sm100(v, T, x, ldx, v->K, At, v->K, wp, hp, st, h_is_zero, 1, &mask);
+        else rc = launch_shrink_sm100(v, T, x, ldx, v->K, At, v->K, wp, hp, st, &mask);
+        if (rc != MARLAAS_OK) return rc;
+    }
     return MARLAAS_OK;
 }
 
@@ -122,16 +145,14 @@ marlaas_status_t marlaas_lora_forward_dropout(marlaas_pool_t* pool, int64_t T, c
     marlaas_pool v;
     scaled_view(pool, d.scale, &v);
     float* h = h_save ? h_save : ws.h;
-    const int NP = pool->P;
+    const bool pre_zero = T >= 512 && shrink_split_sm100_eligible(pool, T, pool->K);       // (before the plan: see lora_forward)
+    if (pre_zero) MARLAAS_CUDA_TRY(cudaMemsetAsync(h, 0, sizeof(float) * (size_t)pool->P * T * pool->RP, st));
     if ((rc = launch_drop_tables(pool, drop, d, st)) != MARLAAS_OK) return rc;
     if ((rc = make_plan(&v, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
-    if ((rc = launch_drop_rows(pool, T, (const bf16*)x, ldx, ws, d, drop_key(drop), st)) != MARLAAS_OK) return rc;
-    for (int p = 0; p < NP; ++p)
-        if ((rc = shrink(&v, T, d.xd, pool->K, pool->K, pool->d_At + (size_t)p * pool->cap * pool->RP * pool->K, pool->K,
-                         part_workspace(pool, ws, p, T), h + (size_t)p * T * pool->RP, st)) != MARLAAS_OK) return rc;
+    if ((rc = masked_shrink(&v, T, (const bf16*)x, ldx, ws, d, drop_key(drop), h, pre_zero, false, st)) != MARLAAS_OK) return rc;
     GemmOperands o;
     forward_operands(pool, T, (const bf16*)x, ldx, (const bf16*)W, ldw, (bf16*)y, ldy, ws, &o);
-    rc = (NP > 1 || gemm2_sm100_eligible(pool, T)) ? launch_gemm2_sm100(&v, o, st) : launch_gemm_sm100(&v, o, st);
+    rc = (pool->P > 1 || gemm2_sm100_eligible(pool, T)) ? launch_gemm2_sm100(&v, o, st) : launch_gemm_sm100(&v, o, st);
     if (rc != MARLAAS_OK) return rc;
     return finish(pool, flags, st);
 } catch (const std::exception& e) {
@@ -170,66 +191,25 @@ marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, 
     marlaas_pool v;
     scaled_view(pool, d.scale, &v);
     const int NP = pool->P;
-    const size_t plane = (size_t)T * pool->RP;
+    // One kernel after another on the caller's stream.
+    const bool pre_zero = T >= 512 && NP == 1 && (dx || want_dA) && shrink_split_sm100_eligible(pool, T, pool->N);
+    if (pre_zero) MARLAAS_CUDA_TRY(cudaMemsetAsync(ws.g, 0, sizeof(float) * (size_t)T * pool->RP, st));
     if ((rc = launch_drop_tables(pool, drop, d, st)) != MARLAAS_OK) return rc;
-    if (T > 0 && (rc = make_plan(&v, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
-    auto masked_rows = [&](cudaStream_t s) { return launch_drop_rows(pool, T, (const bf16*)x, ldx, ws, d, key, s); };
-    auto g_of_dy = [&]() -> marlaas_status_t {
-        for (int p = 0; p < NP; ++p) {
-            const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
-            const Workspace wp = part_workspace(pool, ws, p, T);
-            const marlaas_status_t r = shrink(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st);
-            if (r != MARLAAS_OK) return r;
-        }
-        return MARLAAS_OK;
-    };
-    auto product = [&]() {
-        GemmOperands o;
-        backward_operands(pool, T, (const bf16*)W, ldw, (const bf16*)dy, lddy, (bf16*)dx, lddx, ws, &o);
-        return launch_gemm2_dropped(&v, o, DropMask{ws.tok_slot, d.limit, key}, st);
-    };
-    // As in marlaas_lora_backward: where the reductions are certain to fit, all that the adapters' gradients need besides g is made
-    // on the pool's side stream beside the dx product, and the reductions take the SMs that the product leaves (8192 x 4096 x 4096,
-    // 32 tenants of rank 16: 364 us one after another, 321 so).
-    const bool fits = grad_sm100_eligible(pool, T) && cdiv(T, 64) + (int64_t)seg->num_segments <= (int64_t)ws.max_copies;
-    if (T >= 1024 && NP == 1 && fits && dx && (want_dA || want_dB) && (!want_dB || h_saved) && pool->cap <= 64) {
-        if ((rc = make_side_stream(pool)) != MARLAAS_OK) return rc;
-        cudaStream_t gs = pool->side;
-        MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_fork, st));
-        MARLAAS_CUDA_TRY(cudaStreamWaitEvent(gs, pool->ev_fork, 0));
-        // whatever happens from here on, the side stream is joined again before the call returns
-        auto work = [&]() -> marlaas_status_t {
-            marlaas_status_t r;
-            if ((r = launch_grad_plan(&v, T, ws, gs)) != MARLAAS_OK) return r;
-            if (want_dB && (r = launch_grad_sm100(&v, T, pool->N, (const bf16*)dy, lddy, h_saved, nullptr, dB_slots, false, acc, ws, gs, ws.hm,
-                                                  GRAD_PHASE_COPIES)) != MARLAAS_OK) return r;
-            if ((r = g_of_dy()) != MARLAAS_OK) return r;
-            MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_fork, st));
-            if ((r = product()) != MARLAAS_OK) return r;
-            if (want_dA && (r = masked_rows(gs)) != MARLAAS_OK) return r;
-            MARLAAS_CUDA_TRY(cudaStreamWaitEvent(gs, pool->ev_fork, 0));
-            if (want_dA && (r = launch_grad_sm100(&v, T, pool->K, d.xd, pool->K, ws.g, nullptr, dA_slots, true, acc, ws, gs, ws.hm2,
-                                                  GRAD_PHASE_COPIES)) != MARLAAS_OK) return r;
-            if (want_dB && (r = launch_grad_sm100(&v, T, pool->N, (const bf16*)dy, lddy, h_saved, nullptr, dB_slots, false, acc, ws, gs, ws.hm,
-                                                  GRAD_PHASE_REDUCE)) != MARLAAS_OK) return r;
-            if (want_dA && (r = launch_grad_sm100(&v, T, pool->K, d.xd, pool->K, ws.g, nullptr, dA_slots, true, acc, ws, gs, ws.hm2,
-                                                  GRAD_PHASE_REDUCE | (want_dB ? GRAD_PHASE_EARLY : 0))) != MARLAAS_OK) return r;
-            return MARLAAS_OK;
-        };
-        rc = work();
-        MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_join, gs));
-        MARLAAS_CUDA_TRY(cudaStreamWaitEvent(st, pool->ev_join, 0));
-        if (rc != MARLAAS_OK) return rc;
-        return finish(pool, flags, st);
-    }
     if (T > 0) {
-        if ((want_dA || (want_dB && !h_saved)) && (rc = masked_rows(st)) != MARLAAS_OK) return rc;
-        if ((dx || want_dA) && (rc = g_of_dy()) != MARLAAS_OK) return rc;
-        if (dx && (rc = product()) != MARLAAS_OK) return rc;
-        if (want_dB && !h_saved)
-            for (int p = 0; p < NP; ++p)
-                if ((rc = shrink(&v, T, d.xd, pool->K, pool->K, pool->d_At + (size_t)p * pool->cap * pool->RP * pool->K, pool->K,
-                                 part_workspace(pool, ws, p, T), ws.h + p * plane, st)) != MARLAAS_OK) return rc;
+        if ((rc = make_plan(&v, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
+        if (dx || want_dA)
+            for (int p = 0; p < NP; ++p) {
+                const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
+                const Workspace wp = part_workspace(pool, ws, p, T);
+                if ((rc = shrink(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st, pre_zero)) != MARLAAS_OK) return rc;
+            }
+        if (dx) {
+            GemmOperands o;
+            backward_operands(pool, T, (const bf16*)W, ldw, (const bf16*)dy, lddy, (bf16*)dx, lddx, ws, &o);
+            if ((rc = launch_gemm2_dropped(&v, o, DropMask{ws.tok_slot, d.limit, key}, st)) != MARLAAS_OK) return rc;
+        }
+        if (want_dA && (rc = launch_drop_rows(pool, T, (const bf16*)x, ldx, ws, d, key, st)) != MARLAAS_OK) return rc;
+        if (want_dB && !h_saved && (rc = masked_shrink(&v, T, (const bf16*)x, ldx, ws, d, key, ws.h, false, want_dA, st)) != MARLAAS_OK) return rc;
     }
     if ((want_dA || want_dB) &&
         (rc = adapter_gradients(&v, T, d.xd, pool->K, (const bf16*)dy, lddy, dA_slots, dB_slots, seg, h_saved ? h_saved : ws.h, ws, acc, st)) != MARLAAS_OK)

@@ -150,6 +150,17 @@ marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_
 marlaas_status_t reject_host_table_in_capture(const char* fn, uint32_t flags, cudaStream_t st);
 marlaas_status_t finish(marlaas_pool* pool, uint32_t flags, cudaStream_t st);
 
+// The counter-based generator's key and the counter's fixed half (dropout.cuh).
+struct DropKey {
+    uint32_t k0, k1, o0, o1;
+};
+
+// The masks of a kernel with dropout (dropout.cu): the share of 65536 that a tenant's elements are dropped by, per slot.
+struct DropMask {
+    const int32_t* tok_slot;           // [M]
+    const uint32_t* limit;             // [cap]
+    DropKey key;
+};
 // ---- kernels launched by api.cu ---------------------------------------------------------------------
 // plan.cu
 marlaas_status_t launch_tok_slot(const marlaas_pool* pool, int64_t T, int32_t S, const int32_t* seg_offsets,
@@ -209,17 +220,6 @@ marlaas_status_t launch_gemm_sm100(const marlaas_pool* pool, const GemmOperands&
 bool gemm2_sm100_eligible(const marlaas_pool* pool, int64_t M);
 marlaas_status_t launch_gemm2_sm100(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st);
 
-// The counter-based generator's key and the counter's fixed half (dropout.cuh).
-struct DropKey {
-    uint32_t k0, k1, o0, o1;
-};
-
-// The masks of a dx product with dropout (dropout.cu): the share of 65536 that a tenant's elements are dropped by, per slot.
-struct DropMask {
-    const int32_t* tok_slot;           // [M]
-    const uint32_t* limit;             // [cap]
-    DropKey key;
-};
 // dx = dy W^T + m o (XA XB): launch_gemm2_sm100 with the low-rank term masked, for any number of rows
 marlaas_status_t launch_gemm2_dropped(const marlaas_pool* pool, const GemmOperands& o, const DropMask& d, cudaStream_t st);
 
@@ -287,14 +287,15 @@ marlaas_status_t launch_decode_sm100(const marlaas_pool* pool, int64_t T, const 
 // shrink_sm100.cu: the same outputs as launch_shrink_hd, computed on the tensor cores tile by tile
 // store: the rows of the pooled store to contract with ([cap*RP] rows of D elements, sld elements apart)
 marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D,
-                                     const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st);
+                                     const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st,
+                                     const DropMask* drop = nullptr);
 
 // shrink_split_sm100.cu: the same outputs with one tile per cluster and the contraction split over the cluster's
 // CTAs; applies when all tiles fit one wave
 bool shrink_split_sm100_eligible(const marlaas_pool* pool, int64_t T, int64_t D);
 marlaas_status_t launch_shrink_split_sm100(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D,
                                            const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st,
-                                           bool out_is_zero = false, int P = 1);
+                                           bool out_is_zero = false, int P = 1, const DropMask* drop = nullptr);
 // whether ONE launch can serve all P blocks of adapter rows of a pool over several projections (planes of out and hd)
 bool shrink_split_sm100_parts_eligible(const marlaas_pool* pool, int64_t T, int64_t D, int P);
 

@@ -6,7 +6,11 @@
 // tcgen05.mma of N = 16 * units multiplies them, and the epilogue keeps, for every token, only the columns of its
 // own tenant: fp32 into out[T][RP] (the h / g the gradient reductions and h_save need) and bf16(s_t * value)
 // into the block-diagonal operand hd the base GEMM's extra k-steps consume (zeros in the other tenants' columns).
-// Same warp roles, pipeline and bounded waits as the base GEMM.
+// Same warp roles, pipeline and bounded waits as the base GEMM.  For the layer with dropout (DROP) the epilogue warps zero the
+// dropped elements of every stage in shared memory before the MMA warp may use it, as in shrink_split_sm100.cu.
+#include <string.h>
+
+#include "dropout.cuh"
 #include "sm100_ptx.cuh"
 
 namespace marlaas {
@@ -32,6 +36,7 @@ struct ShrinkArgs {
     bf16* hd;         // [T][hd_cols]
     int hd_cols;
     int32_t* status;
+    DropMask drop;    // DROP
 };
 
 __device__ __forceinline__ void tc_ld_32x16(uint32_t taddr, uint32_t (&v)[16]) {
@@ -44,6 +49,7 @@ __device__ __forceinline__ void tc_ld_32x16(uint32_t taddr, uint32_t (&v)[16]) {
         : "memory");
 }
 
+template <bool DROP>
 __global__ void __launch_bounds__(SHRINK_THREADS, 1)
 k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ CUtensorMap tmStore,
                const ShrinkArgs g) {
@@ -59,7 +65,8 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
     const uint32_t bar_tfull = bar_empty + 8 * STAGES;
     const uint32_t bar_tempty = bar_tfull + 16;
     const uint32_t bar_drain = bar_tempty + 16;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
+    const uint32_t bar_ready = bar_drain + 8;       // DROP: the stage is masked (the four epilogue warps)
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * STAGES + 5);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -68,6 +75,7 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(bar_full + 8 * s, 1);
             mbar_init(bar_empty + 8 * s, 1);
+            mbar_init(bar_ready + 8 * s, 4);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar_tfull + 8 * b, 1);
@@ -139,7 +147,7 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
                     uint32_t acc = 0;
                     for (int kb = 0; kb < g.num_kb && ok; ++kb, ++it) {
                         const uint32_t s = it % STAGES, ph = (it / STAGES) & 1;
-                        if (!(ok = mbar_wait(bar_full + 8 * s, ph, abort_word, 14))) break;
+                        if (!(ok = mbar_wait((DROP ? bar_ready : bar_full) + 8 * s, ph, abort_word, 14))) break;
                         tc_fence_after();
                         const uint32_t a0 = sA + s * A_STAGE_BYTES, b0 = sB + s * SB_STAGE_BYTES;
 #pragma unroll
@@ -163,13 +171,14 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
     } else {
         // ---- epilogue: keep each token's own tenant columns
         const int q = warp & 3;
-        uint32_t lt = 0;
+        uint32_t lt = 0, it = 0;
         bool ok = true;
         for (int m = blockIdx.x; m < g.num_m_tiles && ok; m += gridDim.x) {
             const int nun = g.tile_nunits[m >> 1];
             const int row = m * BM + q * 32 + lane;
             int uo = -1, nu = 0;
             float sc = 0.f;
+            uint32_t limit = 0;
             if (row < g.T && nun > 0) {
                 const int t = g.tok_slot[row];
                 const int r = (t >= 0 && t < g.cap) ? g.d_rank[t] : 0;
@@ -177,11 +186,34 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
                     uo = g.tok_uoff[row];
                     nu = (r + 15) >> 4;
                     sc = g.d_scale[t];
+                    if (DROP) limit = g.drop.limit[t];
                 }
             }
             for (int g0 = 0; g0 < nun && ok; g0 += GROUP_UNITS, ++lt) {
                 const int nug = min(GROUP_UNITS, nun - g0);
                 const uint32_t b = lt & 1, aph = (lt >> 1) & 1;
+                if (DROP) {
+                    const bool none = __all_sync(0xffffffffu, limit == 0);
+                    const int rl = q * 32 + lane;
+                    for (int kb = 0; kb < g.num_kb; ++kb, ++it) {
+                        const uint32_t s = it % STAGES, ph = (it / STAGES) & 1;
+                        ok = mbar_wait(bar_full + 8 * s, ph, abort_word, 17);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        if (!none) {
+                            uint8_t* rows = smem + s * A_STAGE_BYTES + rl * 128;
+#pragma unroll 4
+                            for (int c = 0; c < 8; ++c) {
+                                uint4* at = reinterpret_cast<uint4*>(rows + ((c ^ (rl & 7)) << 4));
+                                *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)(kb * 8 + c), (uint32_t)row), limit);
+                            }
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar_ready + 8 * s);
+                    }
+                    if (!ok) break;
+                }
                 ok = mbar_wait(bar_tfull + 8 * b, aph, abort_word, 16);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
@@ -235,7 +267,8 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
 }  // namespace sm100
 
 marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D,
-                                     const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st) {
+                                     const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st,
+                                     const DropMask* drop) {
     using namespace sm100;
     if (T <= 0) return MARLAAS_OK;
     ShrinkArgs g;
@@ -264,11 +297,15 @@ marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const 
     constexpr size_t smem_bytes = 1024 + (size_t)SHRINK_STAGES * (A_STAGE_BYTES + SB_STAGE_BYTES) + 256;
     static bool attr_set[64] = {};
     if (pool->device >= 64 || !attr_set[pool->device]) {
-        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_shrink_sm100, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_shrink_sm100<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_shrink_sm100<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes));
         if (pool->device < 64) attr_set[pool->device] = true;
     }
     const int grid = g.num_m_tiles < pool->sm_count ? g.num_m_tiles : pool->sm_count;
-    k_shrink_sm100<<<grid, SHRINK_THREADS, smem_bytes, st>>>(tmSrc, tmStore, g);
+    if (drop) g.drop = *drop;
+    else memset(&g.drop, 0, sizeof(g.drop));
+    if (drop) k_shrink_sm100<true><<<grid, SHRINK_THREADS, smem_bytes, st>>>(tmSrc, tmStore, g);
+    else k_shrink_sm100<false><<<grid, SHRINK_THREADS, smem_bytes, st>>>(tmSrc, tmStore, g);
     MARLAAS_LAUNCH_CHECK("k_shrink_sm100");
     return MARLAAS_OK;
 }

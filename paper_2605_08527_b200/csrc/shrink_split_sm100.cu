@@ -9,6 +9,13 @@
 // by ONE pass over the activations: an item's slab holds its units' rows of every block (virtual unit p * n + u = unit u
 // of block p, so items take 8 / P units), the accumulator one group of 16 columns per virtual unit, and the results go
 // to plane p of the outputs.
+//
+// For the layer with dropout (DROP) the tokens' rows are masked on their way: the four epilogue warps, idle until the accumulator is
+// there, zero the dropped elements of every stage in shared memory (a thread its own row: 16 bytes are one call of the generator)
+// before the MMA warp may use it.
+#include <string.h>
+
+#include "dropout.cuh"
 #include "sm100_ptx.cuh"
 
 namespace marlaas {
@@ -43,6 +50,7 @@ struct ShrinkSplitArgs {
     int part_rows;    // store rows from one block to the next
     long long out_plane, hd_plane;   // elements from one plane of out / hd to the next
     int32_t* status;
+    DropMask drop;    // DROP
 };
 
 __device__ __forceinline__ void ss_tc_ld_32x16(uint32_t taddr, uint32_t (&v)[16]) {
@@ -113,6 +121,7 @@ __device__ __forceinline__ int ss_plan_runs(const int32_t* units, int nug, UnitR
 //    pipeline is drained between items anyway), and each role keeps the phase of every stage barrier in a bit mask;
 //  - the gather buffer (C x 128 rows x RP floats, in the cluster's first CTA) lies over the stages: once every CTA of the
 //    cluster has seen its last MMA complete (one more cluster barrier per item) nothing touches them until the next item.
+template <bool DROP>
 __global__ void __launch_bounds__(SS_THREADS, 1)
 k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ StoreMaps tmStore,
                      const ShrinkSplitArgs g) {
@@ -134,13 +143,15 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
     const uint32_t bar_empty = bar_full + 8 * SS_MAX_STAGES;
     const uint32_t bar_tfull = bar_empty + 8 * SS_MAX_STAGES;
     const uint32_t bar_drain = bar_tfull + 8;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * SS_MAX_STAGES + 2);
+    const uint32_t bar_ready = bar_drain + 8;       // DROP: the stage is masked (the four epilogue warps)
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * SS_MAX_STAGES + 2);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < SS_MAX_STAGES; ++s) {
             mbar_init(bar_full + 8 * s, 1);
             mbar_init(bar_empty + 8 * s, 1);
+            mbar_init(bar_ready + 8 * s, 4);
         }
         mbar_init(bar_tfull, 1);
         mbar_init(bar_drain, 1);
@@ -190,6 +201,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
     // role-local pipeline state lives across items
     uint32_t p_mask = 0, p_issued = 0, p_stages = 1;     // producer: phase bit of every stage's next use; loads of this item
     uint32_t m_mask = 0;                                 // MMA issuer: likewise
+    uint32_t e_mask = 0;                                 // masking warps: likewise
     uint32_t done = 0;                        // items finished by this cluster (parity of bar_tfull)
     bool ok = true;
 
@@ -215,6 +227,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
         const int row = m * BM + rl;
         int uo = -1, nu = 0;
         float sc = 0.f;
+        uint32_t limit = 0;
         if (warp >= 2 && row < g.T) {
             const int t = g.tok_slot[row];
             const int r = (t >= 0 && t < g.cap) ? g.d_rank[t] : 0;
@@ -222,6 +235,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
                 uo = g.tok_uoff[row];
                 nu = (r + 15) >> 4;
                 sc = g.d_scale[t];
+                if (DROP) limit = g.drop.limit[t];
             }
         }
 
@@ -255,7 +269,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
                 const uint32_t idesc = make_idesc(nvu * 16, 0);
                 uint32_t acc = 0, m_s = 0;
                 for (int ks = ks0; ks < ks1 && ok; ++ks) {
-                    if (!(ok = mbar_wait(bar_full + 8 * m_s, (m_mask >> m_s) & 1u, abort_word, 54))) break;
+                    if (!(ok = mbar_wait((DROP ? bar_ready : bar_full) + 8 * m_s, (m_mask >> m_s) & 1u, abort_word, 54))) break;
                     tc_fence_after();
                     const uint32_t a0 = sS + m_s * stage_bytes, b0 = a0 + A_STEP;
 #pragma unroll
@@ -275,6 +289,29 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
             }
             __syncwarp();
         } else {
+            if (DROP) {
+                const bool none = __all_sync(0xffffffffu, limit == 0);
+                uint32_t e_s = 0;
+                for (int ks = ks0; ks < ks1; ++ks) {
+                    bool fok = mbar_wait(bar_full + 8 * e_s, (e_mask >> e_s) & 1u, abort_word, 57);
+                    if (!__all_sync(0xffffffffu, fok)) break;
+                    if (!none) {
+                        uint8_t* rows = smem + e_s * stage_bytes + rl * 128;
+#pragma unroll
+                        for (int p = 0; p < KP; ++p)
+#pragma unroll 4
+                            for (int c = 0; c < 8; ++c) {
+                                uint4* at = reinterpret_cast<uint4*>(rows + p * A_STAGE_BYTES + ((c ^ (rl & 7)) << 4));
+                                *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((ks * KP + p) * 8 + c), (uint32_t)row), limit);
+                            }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_ready + 8 * e_s);
+                    e_mask ^= 1u << e_s;
+                    if (++e_s == nst) e_s = 0;
+                }
+            }
             // ---- epilogue warps: wait for this CTA's accumulator
             bool eok = mbar_wait(bar_tfull, done & 1, abort_word, 56);
             eok = __all_sync(0xffffffffu, eok);
@@ -401,7 +438,7 @@ static int split_width(const marlaas_pool* pool, int64_t tiles, int64_t num_kb, 
         const size_t smem = 1024 + area + 256;
         int mc = pool->device < 64 ? max_active[pool->device][C] : 0;
         if (mc == 0) {
-            if (cudaFuncSetAttribute(k_shrink_split_sm100, cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024) != cudaSuccess) return 0;
+            if (cudaFuncSetAttribute(k_shrink_split_sm100<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024) != cudaSuccess) return 0;
             cudaLaunchConfig_t qc = {};
             qc.gridDim = dim3((unsigned)(C * 64));
             qc.blockDim = dim3(SS_THREADS);
@@ -410,7 +447,7 @@ static int split_width(const marlaas_pool* pool, int64_t tiles, int64_t num_kb, 
             qa.id = cudaLaunchAttributeClusterDimension;
             qa.val.clusterDim.x = (unsigned)C; qa.val.clusterDim.y = 1; qa.val.clusterDim.z = 1;
             qc.attrs = &qa; qc.numAttrs = 1;
-            if (cudaOccupancyMaxActiveClusters(&mc, k_shrink_split_sm100, &qc) != cudaSuccess || mc < 1) mc = -1;
+            if (cudaOccupancyMaxActiveClusters(&mc, k_shrink_split_sm100<false>, &qc) != cudaSuccess || mc < 1) mc = -1;
             cudaGetLastError();
             if (pool->device < 64) max_active[pool->device][C] = mc;
         }
@@ -438,7 +475,7 @@ bool shrink_split_sm100_parts_eligible(const marlaas_pool* pool, int64_t T, int6
 
 marlaas_status_t launch_shrink_split_sm100(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D,
                                            const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st,
-                                           bool out_is_zero, int P) {
+                                           bool out_is_zero, int P, const DropMask* drop) {
     using namespace sm100;
     if (T <= 0) return MARLAAS_OK;
     const int64_t tiles = cdiv(T, BM);
@@ -477,7 +514,18 @@ marlaas_status_t launch_shrink_split_sm100(const marlaas_pool* pool, int64_t T, 
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 2;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_shrink_split_sm100, tmSrc, maps, g));
+    if (drop) {
+        g.drop = *drop;
+        static bool attr_set[64] = {};
+        if (pool->device >= 64 || !attr_set[pool->device]) {
+            MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_shrink_split_sm100<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024));
+            if (pool->device < 64) attr_set[pool->device] = true;
+        }
+        MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_shrink_split_sm100<true>, tmSrc, maps, g));
+    } else {
+        memset(&g.drop, 0, sizeof(g.drop));
+        MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_shrink_split_sm100<false>, tmSrc, maps, g));
+    }
     count_launch();
     return MARLAAS_OK;
 }
