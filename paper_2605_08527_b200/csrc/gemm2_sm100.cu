@@ -30,7 +30,7 @@
 #include <string.h>
 
 #include "dropout.cuh"
-#include "sm100_ptx.cuh"
+#include "sm100_cluster.cuh"
 
 namespace marlaas {
 namespace sm100 {
@@ -328,25 +328,6 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();      // 0 = leader
     const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
-    constexpr bool HEAD = EPI == EPI_SOFTMAX || EPI == EPI_GRAD;
-    const int M = HEAD ? head_rows(g.head, g.M) : g.M;
-    const int num_m_tiles = HEAD ? (M + 255) / 256 : g.num_m_tiles;
-    const int plane_tiles = num_m_tiles * g.num_n_tiles;
-    const int splits = EPI == EPI_GRAD ? head_splits(g.head, plane_tiles, (int)g.num_kb * KP) : 1;
-    const int num_tiles = plane_tiles * splits;       // work items: the tiles of the first range of k, then of the next
-    // the k-steps of a work item, and its tile
-    auto item = [&](int tile, int& m_idx, int& n_idx, int& kb0, int& kb1) {
-        kb0 = 0;
-        kb1 = g.num_kb;
-        if (EPI == EPI_GRAD) {
-            const int sp = tile / plane_tiles;
-            tile -= sp * plane_tiles;
-            kb0 = (int)((int64_t)g.num_kb * sp / splits);
-            kb1 = (int)((int64_t)g.num_kb * (sp + 1) / splits);
-        }
-        decode_tile2(g, num_m_tiles, tile, m_idx, n_idx);
-    };
-
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(bar_full + 8 * s, 1);
@@ -380,6 +361,29 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     cluster_sync_all();     // both CTAs' barriers are initialised before any remote arrive or TMA completion
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+
+    constexpr bool HEAD = EPI == EPI_SOFTMAX || EPI == EPI_GRAD;
+    if (HEAD) {     // launched behind the kernel that makes this one's inputs: everything above overlapped its end
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
+    const int M = HEAD ? head_rows(g.head, g.M) : g.M;
+    const int num_m_tiles = HEAD ? (M + 255) / 256 : g.num_m_tiles;
+    const int plane_tiles = num_m_tiles * g.num_n_tiles;
+    const int splits = EPI == EPI_GRAD ? head_splits(g.head, plane_tiles, (int)g.num_kb * KP, lane) : 1;
+    const int num_tiles = plane_tiles * splits;       // work items: the tiles of the first range of k, then of the next
+    // the k-steps of a work item, and its tile
+    auto item = [&](int tile, int& m_idx, int& n_idx, int& kb0, int& kb1) {
+        kb0 = 0;
+        kb1 = g.num_kb;
+        if (EPI == EPI_GRAD) {
+            const int sp = tile / plane_tiles;
+            tile -= sp * plane_tiles;
+            kb0 = (int)((int64_t)g.num_kb * sp / splits);
+            kb1 = (int)((int64_t)g.num_kb * (sp + 1) / splits);
+        }
+        decode_tile2(g, num_m_tiles, tile, m_idx, n_idx);
+    };
 
     if (warp == 0) {
         // ================= TMA producer (both CTAs) =================
@@ -745,8 +749,8 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    // (the other forms read what the kernel before them wrote from their first step on)
-    cfg.attrs = at; cfg.numAttrs = EPI == EPI_LAYER ? 1 : 0;
+    // (EPI_DROP reads what the kernel before it wrote from its first step on)
+    cfg.attrs = at; cfg.numAttrs = EPI == EPI_DROP ? 0 : 1;
     MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_gemm2_sm100<KP, EPI>, tmA, tmB, tmXA, tmXB, g));
     count_launch();
     return MARLAAS_OK;

@@ -50,14 +50,47 @@ struct HeadArgs {
     bf16* dx; int64_t lddx;                 // or NULL
 };
 
-// A warp per place in the order: a token that counts is copied to its row, of another one the outputs are cleared.
-__global__ void __launch_bounds__(HEAD_THREADS) k_head_gather(const HeadArgs a) {
-    const int lane = threadIdx.x & 31;
-    const int64_t p = (int64_t)blockIdx.x * (HEAD_THREADS / 32) + (threadIdx.x >> 5);
-    if (p >= a.T) return;
-    const int64_t i = a.perm[p];
+// A token that counts is copied to its row, of another one the outputs are cleared; a warp per place in the order.  Batches of at
+// most HEAD_SMALL_T tokens need no order made before (SMALL): a warp takes a token, and each CTA counts the tokens before its own.
+constexpr int HEAD_SMALL_T = 4096;
+template <bool SMALL>
+__global__ void __launch_bounds__(HEAD_THREADS) k_head_gather(const HeadArgs a, int32_t* perm, int32_t* active, int32_t* status) {
+    __shared__ int s_cnt[HEAD_THREADS / 32], s_on[HEAD_THREADS / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    sm100::dk_launch_dependents();
+    int64_t p = (int64_t)blockIdx.x * (HEAD_THREADS / 32) + warp, i = p;
+    bool on;
+    if (SMALL) {
+        auto counts = [&](int64_t j) {
+            const int y = a.targets[j];
+            return y >= 0 && y < a.V && !(a.weight && a.weight[j] == 0.f);
+        };
+        const int64_t first = (int64_t)blockIdx.x * (HEAD_THREADS / 32);
+        int n = 0;
+        for (int64_t j = threadIdx.x; j < first; j += HEAD_THREADS) n += counts(j);
+        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+        on = i < a.T && counts(i);
+        if (lane == 0) {
+            s_cnt[warp] = n;
+            s_on[warp] = on;
+            if (i < a.T && a.targets[i] >= a.V) dk_report(status, DEV_BAD_INDEX, (int)i);
+        }
+        __syncthreads();
+        int before = 0, all = 0;
+        for (int w = 0; w < HEAD_THREADS / 32; ++w) {
+            before += s_cnt[w] + (w < warp ? s_on[w] : 0);
+            all += s_cnt[w] + s_on[w];
+        }
+        if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *active = all;
+        if (on && lane == 0) perm[before] = (int)i;
+        p = before;
+    } else {
+        on = p < *active;
+        if (p < a.T) i = perm[p];
+    }
+    if (i >= a.T) return;
     const int nvec = a.d / 8;
-    if (p < *a.active) {
+    if (on) {
         const uint4* src = reinterpret_cast<const uint4*>(a.x + i * a.ldx);
         uint4* dst = reinterpret_cast<uint4*>(a.rows + p * a.d);
         for (int v = lane; v < nvec; v += 32) dst[v] = src[v];
@@ -84,6 +117,8 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_rows(const HeadArgs a, in
     __shared__ float s_f[GRAD ? MARLAAS_MAX_VOCABULARY / 256 : 1];
     __shared__ float s_red[HEAD_THREADS / 32];
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    sm100::dk_wait_prerequisites();
+    sm100::dk_launch_dependents();
     if (row0 + row >= *a.active) return;
     const float2* part = a.part + (size_t)row * a.NT;
     auto all = [&](float v, bool is_max) {      // the same tree in every call
@@ -145,11 +180,74 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_rows(const HeadArgs a, in
     }
 }
 
-// The ranges' partial gradients of a row, summed in their order, scaled and rounded.
-__global__ void __launch_bounds__(HEAD_THREADS) k_head_dx(const HeadArgs a, const HeadEpilogue h, int most, int steps) {
+// A bucket (slot, then slot -1) sums its tokens' terms, every thread its own tokens in ascending order, then a tree.
+struct HeadStats {
+    int64_t T;
+    int S, cap;
+    const int32_t* off;
+    const int32_t* slot;
+    const float4* terms;
+    float* stats;           // or NULL
+    int accumulate;
+    int32_t* status;
+};
+__device__ __forceinline__ void head_bucket(const HeadStats& a, int b) {
+    __shared__ float4 s_sum[HEAD_THREADS / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    bool mine = b == a.cap;                 // (tokens that an ill-formed table leaves out count there)
+    for (int s = tid; s < a.S; s += HEAD_THREADS) {
+        const int t = a.slot[s];
+        mine |= t == b;
+        if (b == 0) {
+            const int x = a.off[s], y = a.off[s + 1];
+            if (y < x || x < 0 || y > a.T || (s == 0 && x != 0) || (s == a.S - 1 && y != a.T)) dk_report(a.status, DEV_BAD_TABLE, s);
+            if (t < -1 || t >= a.cap) dk_report(a.status, DEV_BAD_INDEX, s);
+        }
+    }
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (__syncthreads_or(mine)) {
+        for (int64_t i = tid; i < a.T; i += HEAD_THREADS) {
+            int lo = 0, hi = a.S;           // segments that begin at or before the token: the last of them holds it
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (a.off[mid] <= i) lo = mid + 1; else hi = mid;
+            }
+            const int t = lo > 0 ? a.slot[lo - 1] : -1;
+            if ((t < 0 || t >= a.cap ? a.cap : t) != b) continue;
+            const float4 q = a.terms[i];
+            v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
+        }
+    }
+    for (int o = 16; o > 0; o >>= 1) {
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+        v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
+        v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
+    }
+    if (lane == 0) s_sum[warp] = v;
+    __syncthreads();
+    if (tid < MARLAAS_HEAD_STATS) {
+        float x = 0.f;
+        for (int w = 0; w < HEAD_THREADS / 32; ++w) x += (&s_sum[w].x)[tid];
+        float* out = a.stats + (size_t)b * MARLAAS_HEAD_STATS + tid;
+        *out = a.accumulate ? *out + x : x;
+    }
+}
+__global__ void __launch_bounds__(HEAD_THREADS) k_head_stats(const HeadStats a) {
+    sm100::dk_wait_prerequisites();
+    head_bucket(a, blockIdx.x);
+}
+
+// The ranges' partial gradients of a row, summed in their order, scaled and rounded; CTAs behind the rows sum the stats.
+__global__ void __launch_bounds__(HEAD_THREADS) k_head_dx(const HeadArgs a, const HeadEpilogue h, int most, int steps, const HeadStats st) {
+    sm100::dk_wait_prerequisites();
+    if ((int)blockIdx.x >= most) {
+        head_bucket(st, (int)blockIdx.x - most);
+        return;
+    }
     const int rows = min(most, max(0, *h.active - h.row0)), row = blockIdx.x;
     if (row >= rows) return;
-    const int nt = (a.d + 255) / 256, tiles = (rows + 255) / 256 * nt, splits = head_splits(h, tiles, steps);
+    const int nt = (a.d + 255) / 256, tiles = (rows + 255) / 256 * nt, splits = sm100::head_splits(h, tiles, steps, threadIdx.x & 31);
     if (splits == 1) return;
     const float f = h.coef[row];
     bf16* out = a.dx + (int64_t)h.perm[h.row0 + row] * a.lddx;
@@ -174,51 +272,22 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_dx(const HeadArgs a, cons
     }
 }
 
-// One CTA per bucket (slot, then slot -1) sums its tokens' terms, every thread its own tokens in ascending order, then a tree.
-constexpr int HEAD_STATS_THREADS = 1024;
-__global__ void __launch_bounds__(HEAD_STATS_THREADS) k_head_stats(int64_t T, int S, int cap, const int32_t* __restrict__ off,
-                                                                   const int32_t* __restrict__ slot, const float4* __restrict__ terms,
-                                                                   float* __restrict__ stats, int accumulate, int32_t* status) {
-    __shared__ float4 s_sum[32];
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    bool mine = b == cap;                   // (tokens that an ill-formed table leaves out count there)
-    for (int s = tid; s < S; s += HEAD_STATS_THREADS) {
-        const int t = slot[s];
-        mine |= t == b;
-        if (b == 0) {
-            const int x = off[s], y = off[s + 1];
-            if (y < x || x < 0 || y > T || (s == 0 && x != 0) || (s == S - 1 && y != T)) dk_report(status, DEV_BAD_TABLE, s);
-            if (t < -1 || t >= cap) dk_report(status, DEV_BAD_INDEX, s);
-        }
-    }
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (__syncthreads_or(mine)) {
-        for (int64_t i = tid; i < T; i += HEAD_STATS_THREADS) {
-            int lo = 0, hi = S;             // segments that begin at or before the token: the last of them holds it
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (off[mid] <= i) lo = mid + 1; else hi = mid;
-            }
-            const int t = lo > 0 ? slot[lo - 1] : -1;
-            if ((t < 0 || t >= cap ? cap : t) != b) continue;
-            const float4 q = terms[i];
-            v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
-        }
-    }
-    for (int o = 16; o > 0; o >>= 1) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-        v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
-        v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
-    }
-    if (lane == 0) s_sum[warp] = v;
-    __syncthreads();
-    if (tid < MARLAAS_HEAD_STATS) {
-        float x = 0.f;
-        for (int w = 0; w < 32; ++w) x += (&s_sum[w].x)[tid];
-        float* out = stats + (size_t)b * MARLAAS_HEAD_STATS + tid;
-        *out = accumulate ? *out + x : x;
-    }
+// A launch behind the kernel before it, which it waits for itself.
+template <class... P, class... A>
+static marlaas_status_t launch_behind(const char* name, void (*kernel)(P...), unsigned grid, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(HEAD_THREADS);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
+    MARLAAS_LAUNCH_CHECK(name);
+    return MARLAAS_OK;
 }
 
 struct HeadWorkspace {
@@ -335,6 +404,10 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
     }
     MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
     if ((rc = reject_host_table_in_capture(fn, flags, st)) != MARLAAS_OK) return rc;
+    HeadStats sums;
+    memset(&sums, 0, sizeof(sums));
+    sums.T = T; sums.S = S; sums.cap = pool->cap; sums.terms = ws.terms; sums.stats = stats; sums.accumulate = accumulate;
+    sums.status = pool->d_status;
     if (T > 0) {
         if (host) {     // the copy's source is the call's own and pageable: staged when the copy returns
             std::vector<int32_t> copy((size_t)(ws.slot - ws.off) + (size_t)S);
@@ -344,11 +417,6 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
             off = ws.off;
             slot = ws.slot;
         }
-        OrderArgs o;
-        memset(&o, 0, sizeof(o));
-        o.T = T; o.targets = targets; o.weight = weight; o.V = V; o.nkeys = 2;
-        o.perm = ws.perm; o.key_off = ws.key_off;
-        if ((rc = launch_order(pool, o, ws.scratch, st)) != MARLAAS_OK) return rc;
         HeadArgs a;
         memset(&a, 0, sizeof(a));
         a.T = T; a.d = (int)d; a.V = (int)V; a.NT = (int)ws.NT;
@@ -356,13 +424,24 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
         a.perm = ws.perm; a.active = ws.key_off + 1; a.rows = ws.rows; a.row_target = ws.row_target; a.row_coef = ws.row_coef;
         a.E = ws.E; a.lde = ws.lde; a.part = ws.part; a.target_logit = ws.target_logit;
         a.terms = stats ? ws.terms : nullptr; a.logp = logp; a.dx = (bf16*)dx; a.lddx = lddx;
-        k_head_gather<<<(unsigned)cdiv(T, HEAD_THREADS / 32), HEAD_THREADS, 0, st>>>(a);
+        const unsigned gather = (unsigned)cdiv(T, HEAD_THREADS / 32);
+        if (T <= HEAD_SMALL_T) {
+            k_head_gather<true><<<gather, HEAD_THREADS, 0, st>>>(a, ws.perm, ws.key_off + 1, pool->d_status);
+        } else {
+            OrderArgs o;
+            memset(&o, 0, sizeof(o));
+            o.T = T; o.targets = targets; o.weight = weight; o.V = V; o.nkeys = 2;
+            o.perm = ws.perm; o.key_off = ws.key_off;
+            if ((rc = launch_order(pool, o, ws.scratch, st)) != MARLAAS_OK) return rc;
+            k_head_gather<false><<<gather, HEAD_THREADS, 0, st>>>(a, ws.perm, ws.key_off + 1, pool->d_status);
+        }
         MARLAAS_LAUNCH_CHECK("k_head_gather");
         HeadEpilogue h;
         memset(&h, 0, sizeof(h));
         h.active = a.active; h.targets = ws.row_target; h.perm = ws.perm; h.k2 = inv_temperature * HEAD_LOG2E; h.keep = dx != nullptr;
         h.part = ws.part; h.part_ld = (int)ws.NT; h.target_logit = ws.target_logit; h.partial = ws.partial; h.max_items = HEAD_ITEMS;
         h.pairs = head_pairs(pool);
+        sums.off = off; sums.slot = slot;
         for (int64_t r0 = 0; r0 < T; r0 += ws.piece) {
             const int64_t rows = std::min<int64_t>(ws.piece, T - r0);
             h.row0 = (int)r0;
@@ -376,27 +455,22 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
             g.tile_nunits = g.tile_units = nullptr; g.umax = 0;
             if ((rc = launch_head_softmax(pool, g, h, st)) != MARLAAS_OK) return rc;
             if (!dx) {
-                k_head_rows<false><<<(unsigned)rows, HEAD_THREADS, 0, st>>>(a, (int)r0);
-                MARLAAS_LAUNCH_CHECK("k_head_rows");
+                if ((rc = launch_behind("k_head_rows", k_head_rows<false>, (unsigned)rows, st, a, (int)r0)) != MARLAAS_OK) return rc;
                 continue;
             }
-            k_head_rows<true><<<(unsigned)rows, HEAD_THREADS, 0, st>>>(a, (int)r0);
-            MARLAAS_LAUNCH_CHECK("k_head_rows");
+            if ((rc = launch_behind("k_head_rows", k_head_rows<true>, (unsigned)rows, st, a, (int)r0)) != MARLAAS_OK) return rc;
             g.Nout = d; g.Kc = V;
             g.A = ws.E; g.lda = ws.lde;
             g.b_mn = false;
             g.C = (bf16*)dx; g.ldc = lddx;
             if ((rc = launch_head_grad(pool, g, h, st)) != MARLAAS_OK) return rc;
             const int kp = V % 64 == 0 ? 2 : 1;         // 64-deep panels per step of that product
-            k_head_dx<<<(unsigned)rows, HEAD_THREADS, 0, st>>>(a, h, (int)rows, (int)cdiv(V, 64 * kp) * kp);
-            MARLAAS_LAUNCH_CHECK("k_head_dx");
+            const bool with_stats = stats && r0 + rows >= T;
+            if ((rc = launch_behind("k_head_dx", k_head_dx, (unsigned)(rows + (with_stats ? pool->cap + 1 : 0)), st, a, h, (int)rows,
+                                    (int)cdiv(V, 64 * kp) * kp, sums)) != MARLAAS_OK) return rc;
         }
     }
-    if (stats) {
-        k_head_stats<<<(unsigned)(pool->cap + 1), HEAD_STATS_THREADS, 0, st>>>(T, (int)S, (int)pool->cap, off, slot, ws.terms, stats,
-                                                                               (int)accumulate, pool->d_status);
-        MARLAAS_LAUNCH_CHECK("k_head_stats");
-    }
+    if (stats && (T == 0 || !dx) && (rc = launch_behind("k_head_stats", k_head_stats, (unsigned)(pool->cap + 1), st, sums)) != MARLAAS_OK) return rc;
     return finish(pool, flags, st);
 } catch (const std::exception& e) {
     return fail(MARLAAS_ERR_INVALID_ARG, "head_cross_entropy: %s", e.what());

@@ -240,19 +240,6 @@ struct HeadEpilogue {
     int max_items;
     int pairs;                         // CTA pairs of the device
 };
-// Ranges of the vocabulary that the gradient's product is cut into: the fewest k-steps of the busiest pair, where a further
-// range costs its tiles' way through memory (512 KB at a pair's share of the bandwidth is about 22 steps; a third of it shows
-// beside the main loop), and no range is shorter than 16 steps of 64.
-__host__ __device__ inline int head_splits(const HeadEpilogue& h, int tiles, int steps) {
-    int best = 1;
-    int64_t least = -1;
-    for (int s = 1; s <= 32; ++s) {
-        if (s > 1 && (tiles * s > h.max_items || steps < 16 * s)) break;
-        const int64_t cost = (int64_t)((tiles * s + h.pairs - 1) / h.pairs) * ((steps + s - 1) / s + 4) + (s > 1 ? (int64_t)s * tiles * 8 / h.pairs : 0);
-        if (least < 0 || cost < least) { least = cost; best = s; }
-    }
-    return best;
-}
 int head_pairs(const marlaas_pool* pool);
 // E = exponentials of (x W) (o.C, when kept); dx = E W^T over the ranges
 marlaas_status_t launch_head_softmax(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st);

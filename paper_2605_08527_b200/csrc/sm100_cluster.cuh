@@ -38,6 +38,23 @@ __device__ __forceinline__ void dk_report(int32_t* status, int code, int detail)
     if (atomicCAS(status, 0, code) == 0) status[1] = detail;
 }
 
+// Ranges of the vocabulary that the head's gradient product is cut into (head.cu): the fewest k-steps of the busiest pair, where
+// a further range costs its tiles' way through memory (512 KB at a pair's share of the bandwidth is about 22 steps of 64; a
+// third of it shows beside the main loop), and no range is shorter than 16 steps.  A lane per number of ranges; the fewest win.
+__device__ __forceinline__ int head_splits(const HeadEpilogue& h, int tiles, int steps, int lane) {
+    const int s = lane + 1;
+    int cost = 0x7fffffff;
+    if (s == 1 || (tiles * s <= h.max_items && steps >= 16 * s))
+        cost = (tiles * s + h.pairs - 1) / h.pairs * ((steps + s - 1) / s + 4) + (s > 1 ? s * tiles * 8 / h.pairs : 0);
+    int best = cost, at = s;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const int c = __shfl_xor_sync(0xffffffffu, best, o), t = __shfl_xor_sync(0xffffffffu, at, o);
+        if (c < best || (c == best && t < at)) { best = c; at = t; }
+    }
+    return at;
+}
+
 // ---- CTA pair (cta_group::2): loads that complete on the leader's barrier, MMA and commit for both CTAs ----
 __device__ __forceinline__ void dg_tma_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar_cluster_addr, int c0, int c1) {
     asm volatile(
