@@ -23,6 +23,11 @@ __device__ __forceinline__ uint4 drop_bits(const DropKey& k, uint32_t vec, uint3
     return make_uint4(c0, c1, c2, c3);
 }
 
+// Of 65536 numbers, how many drop an element at rate p: none for a rate that is not above 0, or a NaN.
+__device__ __forceinline__ uint32_t drop_limit(float p) { return p > 0.f ? (uint32_t)rintf(fminf(p, 1.f) * 65536.f) : 0u; }
+// s / (1 - p), of the rate as it is rounded; 0 where everything is dropped.
+__device__ __forceinline__ float drop_scale(float s, uint32_t limit) { return limit < 65536u ? s * (65536.f / (float)(65536u - limit)) : 0.f; }
+
 // Eight bf16 elements with the dropped ones (16 bits below `limit`) set to 0, whatever they hold.
 __device__ __forceinline__ uint4 drop_apply(uint4 x, const uint4& bits, uint32_t limit) {
     uint32_t* v = &x.x;

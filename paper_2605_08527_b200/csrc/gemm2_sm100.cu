@@ -275,7 +275,7 @@ __device__ __forceinline__ void drop_tile(const DropMask& d, uint32_t trow, int 
     uint32_t limit = 0;
     if (on) {
         const int t = d.tok_slot[row];
-        if (t >= 0) limit = d.limit[t];
+        if (t >= 0) limit = drop_limit(d.rates[t]);
     }
     if (__all_sync(0xffffffffu, limit == 0)) return;
     const int cols = min(G2_BN, Nout - n0);

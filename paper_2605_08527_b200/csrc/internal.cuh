@@ -155,10 +155,10 @@ struct DropKey {
     uint32_t k0, k1, o0, o1;
 };
 
-// The masks of a kernel with dropout (dropout.cu): the share of 65536 that a tenant's elements are dropped by, per slot.
+// The masks of a kernel with dropout (dropout.cu).
 struct DropMask {
     const int32_t* tok_slot;           // [M]
-    const uint32_t* limit;             // [cap]
+    const float* rates;                // [cap]
     DropKey key;
 };
 // ---- kernels launched by api.cu ---------------------------------------------------------------------

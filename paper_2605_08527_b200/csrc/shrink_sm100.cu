@@ -186,7 +186,7 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
                     uo = g.tok_uoff[row];
                     nu = (r + 15) >> 4;
                     sc = g.d_scale[t];
-                    if (DROP) limit = g.drop.limit[t];
+                    if (DROP) limit = drop_limit(g.drop.rates[t]);
                 }
             }
             for (int g0 = 0; g0 < nun && ok; g0 += GROUP_UNITS, ++lt) {

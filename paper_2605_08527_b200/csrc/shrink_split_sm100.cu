@@ -235,7 +235,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
                 uo = g.tok_uoff[row];
                 nu = (r + 15) >> 4;
                 sc = g.d_scale[t];
-                if (DROP) limit = g.drop.limit[t];
+                if (DROP) limit = drop_limit(g.drop.rates[t]);
             }
         }
 
