@@ -789,9 +789,9 @@ def marlaas_adamw_compact_state_export(pool: AdapterPool, state: torch.Tensor, m
 
 def _bf16_rows(t: torch.Tensor, T: int, cols: int, name: str, device: int) -> int:
     """Leading dimension of a bf16 [T][cols] matrix."""
-    assert t.dtype is torch.bfloat16 and t.dim() == 2 and t.shape[0] == T and t.shape[1] == cols and t.get_device() == device, name
-    assert cols == 1 or t.stride(1) == 1, name
-    return t.stride(0) if T > 1 else -(-cols // 8) * 8
+    strides = t.stride()
+    assert t.dtype is torch.bfloat16 and t.shape == (T, cols) and t.get_device() == device and (cols == 1 or strides[1] == 1), name
+    return strides[0] if T > 1 else -(-cols // 8) * 8
 
 
 def marlaas_lora_dropout_workspace_bytes(pool: AdapterPool, T: int) -> int:

@@ -332,8 +332,8 @@ static HeadWorkspace carve_head(int64_t T, int64_t d, int64_t V, int32_t S, bool
     if (grad) {
         w.E = (bf16*)take(sizeof(bf16) * (size_t)w.piece * (size_t)w.lde);
         const int64_t tiles = cdiv(w.piece, 256) * cdiv(d, 256), steps = cdiv(V, 64) + 1;
-        // (one range needs no partial gradients, a range is at least 16 steps, and there are at most 32)
-        const int64_t items = std::min<int64_t>(HEAD_ITEMS, tiles * std::min<int64_t>(32, steps / 16));
+        // (one range needs no partial gradients, a range is at least 4 steps, and there are at most 32)
+        const int64_t items = std::min<int64_t>(HEAD_ITEMS, tiles * std::min<int64_t>(32, steps / 4));
         w.partial = (float*)take(sizeof(float) * 65536 * (size_t)std::max<int64_t>(items, 0));
     }
     w.total_bytes = o;

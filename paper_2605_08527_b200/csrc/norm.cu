@@ -113,8 +113,8 @@ __device__ __forceinline__ void group_sum4(float (&v)[4], GroupSums& s, int& par
 }
 
 // ---- forward ----
-template <int NV, int B, int STAGES, int THREADS, bool RMS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const NormArgs a, int W, int G) {
+template <int NV, int B, int STAGES, int THREADS, int PER_SM, bool RMS>
+__global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs a, int W, int G) {
     extern __shared__ uint4 s_ring[];           // [STAGES][B][NV][threads]
     __shared__ GroupSums s_sums;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = warp / W, wg = warp % W, l = wg * 32 + lane;
@@ -246,14 +246,16 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_forward(const 
 // The rows are taken in the order of their tenants.  The sums of a (group, tenant) pair go to partial[group + tenant]: both only
 // rise along the ordered tokens, so no two pairs share a place, and the order of all additions depends on the sizes and the
 // table alone.
-template <int NV, int B, int STAGES, int THREADS, bool RMS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const NormArgs a, int W, int G) {
+template <int NV, int B, int STAGES, int THREADS, int PER_SM, bool RMS>
+__global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArgs a, int W, int G) {
     extern __shared__ uint4 s_ring[];           // [STAGES][B][x, dy][NV][threads]
     __shared__ GroupSums s_sums;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = warp / W, wg = warp % W, l = wg * 32 + lane;
     const int nvec = a.d / 8, threads = blockDim.x;
     const float inv_d = 1.f / (float)a.d;
     const int64_t q = (int64_t)blockIdx.x * G + g, first = q * a.rows_per_group;
+    sm100::dk_wait_prerequisites();
+    sm100::dk_launch_dependents();
     if (first >= a.T) return;
     const int n = (int)min(a.rows_per_group, a.T - first);
     const int32_t* perm = a.perm + first;
@@ -401,21 +403,26 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm_backward(const
     if (a.partial) flush();
 }
 
-// dgain and dbias of one tenant, 32 columns per CTA: the warps share the tenant's partial sums, four at a time on their way, then
-// add up in their order.
+// dgain and dbias of one tenant, 128 columns per CTA, four per lane: the warps share the tenant's partial sums, four at a time on
+// their way, then add up in their order.
 __global__ void __launch_bounds__(1024) k_norm_reduce(const NormArgs a) {
-    __shared__ float s_sum[2][32][33];
-    const int key = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, c = blockIdx.x * 32 + lane;
+    __shared__ float4 s_sum[2][32][32];
+    const int key = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, c = blockIdx.x * 128 + lane * 4;
+    sm100::dk_wait_prerequisites();
     const int64_t b = a.key_off[key], e = a.key_off[key + 1];
-    float g = 0.f, h = 0.f;
+    float4 g = make_float4(0.f, 0.f, 0.f, 0.f), h = g;
     if (e > b) {
         if (c < a.d) {
             const int q0 = (int)(b / a.rows_per_group), q1 = (int)((e - 1) / a.rows_per_group);
             const float* in = a.partial + (size_t)key * 2 * a.d + c;
 #pragma unroll 4
             for (int q = q0 + warp; q <= q1; q += warps) {
-                g += in[(size_t)q * 2 * a.d];
-                if (a.dbias) h += in[(size_t)q * 2 * a.d + a.d];
+                const float4 x = *reinterpret_cast<const float4*>(in + (size_t)q * 2 * a.d);
+                g.x += x.x; g.y += x.y; g.z += x.z; g.w += x.w;
+                if (a.dbias) {
+                    const float4 y = *reinterpret_cast<const float4*>(in + (size_t)q * 2 * a.d + a.d);
+                    h.x += y.x; h.y += y.y; h.z += y.z; h.w += y.w;
+                }
             }
         }
         s_sum[0][warp][lane] = g;
@@ -425,14 +432,22 @@ __global__ void __launch_bounds__(1024) k_norm_reduce(const NormArgs a) {
     if (warp >= 2 || c >= a.d) return;
     float* out = warp == 0 ? a.dgain : a.dbias;
     if (!out) return;
-    out += (size_t)key * a.d + c;
-    float v = 0.f;
+    float4* to = reinterpret_cast<float4*>(out + (size_t)key * a.d + c);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (e > b)
-        for (int w = 0; w < warps; ++w) v += s_sum[warp][w][lane];
-    *out = a.accumulate ? *out + v : v;
+        for (int w = 0; w < warps; ++w) {
+            const float4 x = s_sum[warp][w][lane];
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+    if (a.accumulate) {
+        const float4 x = *to;
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    *to = v;
 }
 
-// How a pass cuts a batch: warps per row and rows of a CTA at a time, groups in all and their rows.
+// How a pass cuts a batch: vectors per lane, warps per row and rows of a CTA at a time, groups in all and their rows.
+// Two vectors per lane where a row has them: half of a row's instructions do not depend on how many elements a lane has.
 struct NormPlan {
     int NV, W, G;
     int64_t groups, rows;
@@ -440,10 +455,11 @@ struct NormPlan {
 static NormPlan norm_plan(const marlaas_pool* pool, int64_t T, int d, bool backward) {
     NormPlan p;
     const int nvec = d / 8;
-    p.NV = nvec <= 1024 ? 1 : 2;
+    p.NV = nvec >= 64 ? 2 : 1;
     p.W = (int)cdiv(nvec, 32 * p.NV);
-    p.G = std::max(1, std::min(NORM_MAX_GROUPS, 16 / p.W));
-    const int64_t most = (int64_t)pool->sm_count * std::max(1, 1024 / (32 * p.W * p.G)) * p.G;      // 1024 threads per SM
+    p.G = std::max(1, std::min(NORM_MAX_GROUPS, 8 / p.W));
+    const int threads = 32 * p.W * p.G;
+    const int64_t most = (int64_t)pool->sm_count * std::max(1, (threads <= 256 ? 768 : 640) / threads) * p.G;
     // (a group's partial sums cost as much as four of its rows: backward, no group takes fewer)
     p.rows = std::max<int64_t>(cdiv(T, most), backward ? 4 : 1);
     p.groups = cdiv(cdiv(T, p.rows), p.G) * p.G;
@@ -478,30 +494,44 @@ static NormWorkspace carve_norm(const marlaas_pool* pool, int64_t T, int32_t S, 
     return w;
 }
 
-// Instances by the width of a row and of a CTA: a CTA of up to 512 threads shares its SM with others.
-template <int NV, int THREADS, bool RMS>
+// Instances by the width of a row and of a CTA: rows of up to 4096 elements share an SM three CTAs at a time, up to 5120 two,
+// wider ones one; shared memory holds the rows on their way.
+template <int NV, int THREADS, int PER_SM, bool RMS>
 static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& a, const NormPlan& n, bool backward, cudaStream_t st) {
-    constexpr int FB = NV == 1 ? 4 : 2, FS = NV == 1 && THREADS == 512 ? 3 : 2, BB = NV == 1 ? 2 : 1, BS = NV == 1 ? 3 : 2;
+    constexpr int STAGES = NV == 1 ? 3 : 2, FB = 4, BB = THREADS == 1024 ? 1 : 2;
     const int threads = 32 * n.W * n.G;
-    const size_t fwd = (size_t)FS * FB * NV * 16, bwd = (size_t)BS * BB * 2 * NV * 16;       // bytes of the ring per thread
+    const size_t fwd = (size_t)STAGES * FB * NV * 16, bwd = (size_t)STAGES * BB * 2 * NV * 16;       // bytes of the ring per thread
+    auto* kf = k_norm_forward<NV, THREADS == 1024 ? 2 : FB, STAGES, THREADS, PER_SM, RMS>;
+    auto* kb = k_norm_backward<NV, BB, STAGES, THREADS, PER_SM, RMS>;
     static bool attr_set[64] = {};
     if (pool->device >= 64 || !attr_set[pool->device]) {
-        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_norm_forward<NV, FB, FS, THREADS, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fwd * THREADS)));
-        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_norm_backward<NV, BB, BS, THREADS, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(bwd * THREADS)));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(kf, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::min<size_t>(fwd * THREADS, 200 * 1024)));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(kb, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::min<size_t>(bwd * THREADS, 200 * 1024)));
         if (pool->device < 64) attr_set[pool->device] = true;
     }
-    const unsigned grid = (unsigned)(n.groups / n.G);
-    if (backward) k_norm_backward<NV, BB, BS, THREADS, RMS><<<grid, threads, bwd * threads, st>>>(a, n.W, n.G);
-    else k_norm_forward<NV, FB, FS, THREADS, RMS><<<grid, threads, fwd * threads, st>>>(a, n.W, n.G);
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // backward: behind the order's kernels
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)(n.groups / n.G));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (backward ? bwd : THREADS == 1024 ? fwd / 2 : fwd) * threads;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = backward ? 1 : 0;
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, backward ? kb : kf, a, n.W, n.G));
     MARLAAS_LAUNCH_CHECK(backward ? "k_norm_backward" : "k_norm_forward");
     return MARLAAS_OK;
 }
 static marlaas_status_t launch_norm(const marlaas_pool* pool, NormArgs a, bool rms, bool backward, cudaStream_t st) {
     const NormPlan n = norm_plan(pool, a.T, a.d, backward);
     a.rows_per_group = n.rows;
-    if (n.NV == 2) return rms ? launch_norm_t<2, 1024, true>(pool, a, n, backward, st) : launch_norm_t<2, 1024, false>(pool, a, n, backward, st);
-    if (n.W > 16) return rms ? launch_norm_t<1, 1024, true>(pool, a, n, backward, st) : launch_norm_t<1, 1024, false>(pool, a, n, backward, st);
-    return rms ? launch_norm_t<1, 512, true>(pool, a, n, backward, st) : launch_norm_t<1, 512, false>(pool, a, n, backward, st);
+#define NORM_GO(nv, threads, per) (rms ? launch_norm_t<nv, threads, per, true>(pool, a, n, backward, st) : launch_norm_t<nv, threads, per, false>(pool, a, n, backward, st))
+    if (n.NV == 1) return NORM_GO(1, 256, 3);
+    if (n.W <= 8) return NORM_GO(2, 256, 3);
+    return n.W <= 10 ? NORM_GO(2, 320, 2) : n.W <= 16 ? NORM_GO(2, 512, 1) : NORM_GO(2, 1024, 1);
+#undef NORM_GO
 }
 
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
@@ -643,7 +673,17 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
     if (a.partial) {
         int warps = 4;              // one per 32 groups
         while (warps < 32 && warps * 32 < n.groups) warps *= 2;
-        k_norm_reduce<<<dim3((unsigned)cdiv(d, 32), (unsigned)(pool->cap + 1)), warps * 32, 0, st>>>(a);
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3((unsigned)cdiv(d, 128), (unsigned)(pool->cap + 1));
+        cfg.blockDim = dim3((unsigned)(warps * 32));
+        cfg.stream = st;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_norm_reduce, a));
         MARLAAS_LAUNCH_CHECK("k_norm_reduce");
     }
     return finish(pool, flags, st);

@@ -2,6 +2,8 @@
 // or the tokens that a loss counts before those that it ignores.  A counting sort: each block of tokens counts its keys and
 // ranks its tokens, one CTA turns the blocks' counts into positions, a third kernel places the tokens.  Integer work of 12
 // bytes per token; a batch of one block takes all of it in one launch.
+#include <string.h>
+
 #include "sm100_cluster.cuh"
 
 namespace marlaas {
@@ -54,6 +56,7 @@ __global__ void k_order_count(OrderArgs a) {
     extern __shared__ int s_cnt[];          // [warps][nkeys], then [nkeys + 1]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5, n = a.nkeys;
     int* s_tot = s_cnt + warps * n;
+    sm100::dk_launch_dependents();          // (what follows waits before it reads the order)
     check_table(a);
     for (int k = tid; k < warps * n; k += blockDim.x) s_cnt[k] = 0;
     __syncthreads();
@@ -89,6 +92,8 @@ __global__ void k_order_count(OrderArgs a) {
 __global__ void __launch_bounds__(1024) k_order_scan(OrderArgs a, int nblk) {
     extern __shared__ int s_tot[];          // [nkeys + 1]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = a.nkeys;
+    sm100::dk_wait_prerequisites();
+    sm100::dk_launch_dependents();
     for (int k = warp; k < n; k += 32) {
         int run = 0;
         for (int b0 = 0; b0 < nblk; b0 += 32) {
@@ -112,6 +117,8 @@ __global__ void __launch_bounds__(1024) k_order_scan(OrderArgs a, int nblk) {
 
 __global__ void k_order_place(OrderArgs a) {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    sm100::dk_wait_prerequisites();
+    sm100::dk_launch_dependents();
     if (i >= a.T) return;
     const int kr = a.keyrank[i], key = kr / ORDER_LARGE, rank = kr % ORDER_LARGE;
     a.perm[a.key_off[key] + a.hist[(size_t)blockIdx.x * a.nkeys + key] + rank] = (int)i;
@@ -131,9 +138,23 @@ marlaas_status_t launch_order(const marlaas_pool* pool, OrderArgs a, int32_t* sc
     k_order_count<<<nblk, B, smem, st>>>(a);
     MARLAAS_LAUNCH_CHECK("k_order_count");
     if (nblk == 1) return MARLAAS_OK;
-    k_order_scan<<<1, 1024, sizeof(int) * ((size_t)a.nkeys + 1), st>>>(a, nblk);
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(1);
+    cfg.blockDim = dim3(1024);
+    cfg.dynamicSmemBytes = sizeof(int) * ((size_t)a.nkeys + 1);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_order_scan, a, nblk));
     MARLAAS_LAUNCH_CHECK("k_order_scan");
-    k_order_place<<<nblk, B, 0, st>>>(a);
+    cfg.gridDim = dim3((unsigned)nblk);
+    cfg.blockDim = dim3((unsigned)B);
+    cfg.dynamicSmemBytes = 0;
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_order_place, a));
     MARLAAS_LAUNCH_CHECK("k_order_place");
     return MARLAAS_OK;
 }

@@ -40,11 +40,11 @@ __device__ __forceinline__ void dk_report(int32_t* status, int code, int detail)
 
 // Ranges of the vocabulary that the head's gradient product is cut into (head.cu): the fewest k-steps of the busiest pair, where
 // a further range costs its tiles' way through memory (512 KB at a pair's share of the bandwidth is about 22 steps of 64; a
-// third of it shows beside the main loop), and no range is shorter than 16 steps.  A lane per number of ranges; the fewest win.
+// third of it shows beside the main loop), and no range is shorter than 4 steps.  A lane per number of ranges; the fewest win.
 __device__ __forceinline__ int head_splits(const HeadEpilogue& h, int tiles, int steps, int lane) {
     const int s = lane + 1;
     int cost = 0x7fffffff;
-    if (s == 1 || (tiles * s <= h.max_items && steps >= 16 * s))
+    if (s == 1 || (tiles * s <= h.max_items && steps >= 4 * s))
         cost = (tiles * s + h.pairs - 1) / h.pairs * ((steps + s - 1) / s + 4) + (s > 1 ? s * tiles * 8 / h.pairs : 0);
     int best = cost, at = s;
 #pragma unroll
