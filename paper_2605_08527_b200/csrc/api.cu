@@ -197,17 +197,22 @@ marlaas_status_t make_side_stream(marlaas_pool* pool) {
     return MARLAAS_OK;
 }
 
+// Whether the tensor-core reductions' copies fit the workspace for certain, whatever the tokens' tenants.
+bool adapter_gradients_fit(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, const Workspace& ws) {
+    return grad_sm100_eligible(pool, T) && cdiv(T, 64) + (int64_t)seg->num_segments <= (int64_t)ws.max_copies;
+}
+
 // dA and dB of all slots on one stream, for the plan, g and (T > 0) h in the workspace or as saved: what marlaas_lora_backward
-// does when it does not run them beside the dx product.
+// does when it does not run them beside the dx product.  drop (only where adapter_gradients_fit): x is masked on its way.
 marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
                                    float* const* dA_slots, float* const* dB_slots, const marlaas_segments_t* seg, const float* h,
-                                   const Workspace& ws, bool acc, cudaStream_t st) {
+                                   const Workspace& ws, bool acc, cudaStream_t st, const DropMask* drop) {
     marlaas_status_t rc;
     const int NP = pool->P;
     const size_t plane = (size_t)T * pool->RP;
     const bool tc_grad = grad_sm100_eligible(pool, T);
     // as in marlaas_lora_backward: the copies fit for certain, and with 64 slots at most the tables travel with the launches
-    const bool fits = tc_grad && cdiv(T, 64) + (int64_t)seg->num_segments <= (int64_t)ws.max_copies;
+    const bool fits = adapter_gradients_fit(pool, T, seg, ws);
     const bool inline_tables = fits && pool->cap <= 64;
     const int32_t* run_flag = tc_grad ? ws.gflag : nullptr;
     if (tc_grad && (rc = launch_grad_plan(pool, T, ws, st)) != MARLAAS_OK) return rc;
@@ -229,7 +234,8 @@ marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf
             const float* r = which == 0 ? h + p * plane : ws.g + p * plane;
             if (!inline_tables)
                 MARLAAS_CUDA_TRY(cudaMemcpyAsync(dev, part.data(), sizeof(float*) * (size_t)pool->cap, cudaMemcpyHostToDevice, st));
-            if (tc_grad && (rc = launch_grad_sm100(pool, T, C, src, ld, r, dev, part.data(), which == 1, acc, ws, st, ws.hm)) != MARLAAS_OK) return rc;
+            if (tc_grad && (rc = launch_grad_sm100(pool, T, C, src, ld, r, dev, part.data(), which == 1, acc, ws, st, ws.hm,
+                                                   GRAD_PHASE_COPIES | GRAD_PHASE_REDUCE, which == 1 ? drop : nullptr)) != MARLAAS_OK) return rc;
             if (!fits && (rc = launch_grad_reduce(pool, C, src, ld, r, ws.perm, ws.slot_offset, dev, which == 1, acc, st, run_flag)) != MARLAAS_OK)
                 return rc;
         }

@@ -428,10 +428,13 @@ marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, 
             if ((rc = shrink(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st, pre_zero)) != MARLAAS_OK) return rc;
         }
     if ((rc = product()) != MARLAAS_OK) return rc;
-    if (want_dA && (rc = launch_drop_rows(pool, T, (const bf16*)x, ldx, mask, d.xd, st)) != MARLAAS_OK) return rc;
+    // the reduction for dA masks the rows itself, but for batches whose tenants may mix too finely for it
+    const bool fits = adapter_gradients_fit(pool, T, seg, ws);
+    if (want_dA && !fits && (rc = launch_drop_rows(pool, T, (const bf16*)x, ldx, mask, d.xd, st)) != MARLAAS_OK) return rc;
     if (want_dB && !h_saved && (rc = masked_shrink(&v, T, (const bf16*)x, ldx, ws, mask, ws.h, false, st)) != MARLAAS_OK) return rc;
     if ((want_dA || want_dB) &&
-        (rc = adapter_gradients(&v, T, d.xd, pool->K, (const bf16*)dy, lddy, dA_slots, dB_slots, seg, h, ws, acc, st)) != MARLAAS_OK)
+        (rc = adapter_gradients(&v, T, fits ? (const bf16*)x : d.xd, fits ? ldx : pool->K, (const bf16*)dy, lddy, dA_slots, dB_slots, seg, h, ws, acc,
+                                st, fits ? &mask : nullptr)) != MARLAAS_OK)
         return rc;
     return finish(pool, flags, st);
 } catch (const std::exception& e) {

@@ -28,16 +28,22 @@ __device__ __forceinline__ uint32_t drop_limit(float p) { return p > 0.f ? (uint
 // s / (1 - p), of the rate as it is rounded; 0 where everything is dropped.
 __device__ __forceinline__ float drop_scale(float s, uint32_t limit) { return limit < 65536u ? s * (65536.f / (float)(65536u - limit)) : 0.f; }
 
-// Eight bf16 elements with the dropped ones (16 bits below `limit`) set to 0, whatever they hold.
+// Eight bf16 elements with the dropped ones (16 bits below `limit`) set to 0, whatever they hold.  The comparisons are made in the
+// upper halves of 32-bit words, where the lower halves' bits cannot matter.
 __device__ __forceinline__ uint4 drop_apply(uint4 x, const uint4& bits, uint32_t limit) {
+    if (limit >= 65536u) return make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t l = limit << 16;
     uint32_t* v = &x.x;
     const uint32_t* b = &bits.x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = (b[i] & 0xffffu) >= limit ? 0x0000ffffu : 0u, hi = (b[i] >> 16) >= limit ? 0xffff0000u : 0u;
-        v[i] &= lo | hi;
+        if ((b[i] << 16) < l) v[i] &= 0xffff0000u;
+        if (b[i] < l) v[i] &= 0x0000ffffu;
     }
     return x;
 }
+
+// Threads of a kernel whose streamed rows are masked in shared memory: four warps beside the four that also write its results.
+constexpr int DROP_EXTRA_THREADS = 128;
 
 }  // namespace marlaas

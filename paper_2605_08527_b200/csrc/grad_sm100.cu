@@ -12,6 +12,12 @@
 // One work item = (tenant, 128 output columns); a CTA walks the tenant's copy list accumulating in tensor memory
 // and writes the slot's gradient once.  If the batch interleaves tenants so finely that the copies would not
 // fit the workspace, a device flag routes the call to the CUDA-core reduction instead.
+//
+// For dA of the layer with dropout (DROP) the streamed rows of x are masked on their way: the four epilogue warps, idle until an
+// item's accumulator is there, and four more zero the dropped elements of every stage in shared memory before the MMA warp may use it.
+#include <string.h>
+
+#include "dropout.cuh"
 #include "sm100_ptx.cuh"
 
 namespace marlaas {
@@ -140,8 +146,11 @@ __global__ void __launch_bounds__(256) k_pad_split(int T, int cap, int RP, int H
     const int blk = blockIdx.x, tid = threadIdx.x;
     const int base = blk_base[blk];
     const int chunks_per_row = HW / 8;
+    __shared__ int s_rk[256];               // (one load's latency for all tenants, of whom few are present)
+    for (int t = tid; t < cap; t += 256) s_rk[t] = blk_rank[(size_t)blk * cap + t];
+    __syncthreads();
     for (int t = 0; t < cap; ++t) {
-        const int rk = blk_rank[(size_t)blk * cap + t];
+        const int rk = s_rk[t];
         if (rk < 0) continue;
         bf16* dst = hm + (size_t)(base + rk) * 64 * HW;
         for (int e = tid; e < 64 * chunks_per_row; e += 256) {
@@ -184,10 +193,13 @@ struct GradArgs {
     int transpose_out, accumulate;
     int stages;            // pipeline steps in flight
     int32_t* status;
+    int T;
+    DropMask drop;         // DROP
     float* inl[GRAD_INLINE_SLOTS];   // small pools: the pointer table travels with the launch (no host-to-device copy)
 };
 
-__global__ void __launch_bounds__(GRAD_THREADS, 1)
+template <bool DROP>
+__global__ void __launch_bounds__(GRAD_THREADS + (DROP ? DROP_EXTRA_THREADS : 0), 1)
 k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ CUtensorMap tmHm, const GradArgs g) {
     constexpr int MAX_STAGES = GRAD_STAGES;
     const int STAGES = g.stages;
@@ -211,7 +223,8 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
     const uint32_t bar_tempty = bar_tfull + 16;
     const uint32_t bar_drain = bar_tempty + 16;
     const uint32_t bar_qfull = bar_drain + 8, bar_qempty = bar_qfull + 8 * GRAD_QN;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 5 + 2 * GRAD_QN);
+    const uint32_t bar_ready = bar_qempty + 8 * GRAD_QN;        // DROP: the stage is masked (eight warps)
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * MAX_STAGES + 5 + 2 * GRAD_QN);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
     __shared__ int s_cnt[256], s_order[256];
     __shared__ volatile int s_q[GRAD_QN];
@@ -223,6 +236,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(bar_full + 8 * s, 1);
             mbar_init(bar_empty + 8 * s, 1);
+            mbar_init(bar_ready + 8 * s, 8);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar_tfull + 8 * b, 1);
@@ -231,7 +245,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
         mbar_init(bar_drain, 1);
         for (int i = 0; i < GRAD_QN; ++i) {
             mbar_init(bar_qfull + 8 * i, 1);
-            mbar_init(bar_qempty + 8 * i, 5);     // the MMA thread and the four epilogue warps
+            mbar_init(bar_qempty + 8 * i, DROP ? 9 : 5);     // the MMA thread and the epilogue (and masking) warps
         }
         *abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -247,10 +261,10 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
     }
     // Work items are handed out dynamically, heaviest tenants first (an item's cost is its tenant's copy count), so that
     // skewed batches still finish together; which CTA computes an item does not change its value.
-    for (int t = threadIdx.x; t < g.cap; t += GRAD_THREADS) s_cnt[t] = ((g.out_ptrs ? g.out_ptrs[t] : g.inl[t]) != nullptr && g.d_rank[t] > 0) ? g.ten_nblk[t] : -1;
+    for (int t = threadIdx.x; t < g.cap; t += blockDim.x) s_cnt[t] = ((g.out_ptrs ? g.out_ptrs[t] : g.inl[t]) != nullptr && g.d_rank[t] > 0) ? g.ten_nblk[t] : -1;
     tc_fence_before();
     __syncthreads();
-    for (int t = threadIdx.x; t < g.cap; t += GRAD_THREADS) {
+    for (int t = threadIdx.x; t < g.cap; t += blockDim.x) {
         const int c = s_cnt[t];
         int rk = 0;
         for (int u = 0; u < g.cap; ++u) rk += (s_cnt[u] > c) || (s_cnt[u] == c && u < t);
@@ -336,7 +350,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
                 uint32_t acc = 0;
                 for (int k = 0; k < nb && ok; k += GRAD_BPS, ++it) {
                     const uint32_t s = ms, ph = mph;
-                    if (!(ok = mbar_wait(bar_full + 8 * s, ph, abort_word, 24))) break;
+                    if (!(ok = mbar_wait((DROP ? bar_ready : bar_full) + 8 * s, ph, abort_word, 24))) break;
                     if (++ms == (uint32_t)STAGES) { ms = 0; mph ^= 1; }
                     tc_fence_after();
                     const int nj = min(GRAD_BPS, nb - k);
@@ -368,7 +382,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
         const int q = warp & 3;
         uint32_t lt = 0;
         bool ok = true;
-        uint32_t qi = 0;
+        uint32_t qi = 0, es = 0, eph = 0;     // DROP: stage and phase of the next step to mask
         while (ok) {
             const uint32_t qs = qi % GRAD_QN, qph = (qi / GRAD_QN) & 1;
             ok = mbar_wait(bar_qfull + 8 * qs, qph, abort_word, 29);
@@ -386,12 +400,42 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
             const int r = g.d_rank[t];
             const int c = c0 + q * 32 + lane;
             if (nb == 0) {   // tenant without tokens: exact zeros unless accumulating
-                if (!g.accumulate && c < g.C)
+                if (!g.accumulate && c < g.C && (!DROP || warp < 6))
                     for (int j = 0; j < r; ++j) {
                         if (g.transpose_out) out[(size_t)c * r + j] = 0.f;
                         else out[(size_t)j * g.C + c] = 0.f;
                     }
                 continue;
+            }
+            if (DROP) {
+                // thread: token row tl of each block, columns of chunk tc
+                const int tl = (q * 32 + lane) & 63, tc = (q * 32 + lane) >> 6;
+                for (int k = 0; k < nb; k += GRAD_BPS) {
+                    ok = mbar_wait(bar_full + 8 * es, eph, abort_word, 30);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    const int nj = min(GRAD_BPS, nb - k);
+                    for (int j = 0; j < nj; ++j) {
+                        const int i = g.ten_blks[(size_t)t * g.nblk + k + j] * 64 + tl;
+                        const int slot = i < g.T ? g.drop.tok_slot[i] : -1;
+                        const uint32_t limit = slot >= 0 ? drop_limit(g.drop.rates[slot]) : 0u;
+                        if (__any_sync(0xffffffffu, limit != 0) && c0 + tc * 64 < g.C) {
+                            uint8_t* rows = smem + es * A_STEP + j * A_STAGE_BYTES + tc * CHUNK_BYTES + tl * 128;
+#pragma unroll
+                            for (int v4 = 0; v4 < 4; ++v4) {
+                                const int v = v4 + (warp >= 6 ? 4 : 0);
+                                uint4* at = reinterpret_cast<uint4*>(rows + ((v ^ (tl & 7)) << 4));
+                                *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((c0 + tc * 64) / 8 + v), (uint32_t)i), limit);
+                            }
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_ready + 8 * es);
+                    if (++es == (uint32_t)STAGES) { es = 0; eph ^= 1; }
+                }
+                if (!ok) break;
+                if (warp >= 6) continue;
             }
             const float sc = g.d_scale[t];
             const uint32_t b = lt & 1, aph = (lt >> 1) & 1;
@@ -473,7 +517,7 @@ marlaas_status_t launch_grad_plan(const marlaas_pool* pool, int64_t T, const Wor
 marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t C, const bf16* src, int64_t ld,
                                    const float* hg, float* const* out_ptrs, float* const* host_ptrs, bool transpose_out,
                                    bool accumulate,
-                                   const Workspace& ws, cudaStream_t st, bf16* hm, int phases) {
+                                   const Workspace& ws, cudaStream_t st, bf16* hm, int phases, const DropMask* drop) {
     using namespace sm100;
     const int nblk = (int)cdiv(T, 64);
     if (phases & GRAD_PHASE_COPIES) {
@@ -504,6 +548,9 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
     g.transpose_out = transpose_out ? 1 : 0;
     g.accumulate = accumulate ? 1 : 0;
     g.status = pool->d_status;
+    g.T = (int)T;
+    if (drop) g.drop = *drop;
+    else memset(&g.drop, 0, sizeof(g.drop));
     alignas(64) CUtensorMap tmSrc, tmHm;
     marlaas_status_t rc;
     if ((rc = make_map(&tmSrc, src, T, C, ld, 64, 64)) != MARLAAS_OK) return rc;
@@ -514,7 +561,8 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
     g.stages = (int)std::min<size_t>(GRAD_STAGES, (smem_bytes - 1024 - 256) / step_bytes);
     static bool attr_set[64] = {};
     if (pool->device >= 64 || !attr_set[pool->device]) {
-        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_grad_sm100, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_grad_sm100<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes));
+        MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_grad_sm100<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes));
         if (pool->device < 64) attr_set[pool->device] = true;
     }
     const int items = g.num_c_tiles * g.cap;
@@ -531,9 +579,11 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
         at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = at; cfg.numAttrs = 1;
-        MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_grad_sm100, tmSrc, tmHm, g));
+        MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_grad_sm100<false>, tmSrc, tmHm, g));
+    } else if (drop) {
+        k_grad_sm100<true><<<grid, GRAD_THREADS + DROP_EXTRA_THREADS, smem_bytes, st>>>(tmSrc, tmHm, g);
     } else {
-        k_grad_sm100<<<grid, GRAD_THREADS, smem_bytes, st>>>(tmSrc, tmHm, g);
+        k_grad_sm100<false><<<grid, GRAD_THREADS, smem_bytes, st>>>(tmSrc, tmHm, g);
     }
     MARLAAS_LAUNCH_CHECK("k_grad_sm100");
     return MARLAAS_OK;

@@ -313,7 +313,8 @@ marlaas_status_t launch_grad_plan(const marlaas_pool* pool, int64_t T, const Wor
 enum { GRAD_PHASE_COPIES = 1, GRAD_PHASE_REDUCE = 2, GRAD_PHASE_EARLY = 4 };
 marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t C, const bf16* src, int64_t ld,
                                    const float* hg, float* const* out_ptrs, float* const* host_ptrs, bool transpose_out,
-                                   bool accumulate, const Workspace& ws, cudaStream_t st, bf16* hm, int phases = GRAD_PHASE_COPIES | GRAD_PHASE_REDUCE);
+                                   bool accumulate, const Workspace& ws, cudaStream_t st, bf16* hm, int phases = GRAD_PHASE_COPIES | GRAD_PHASE_REDUCE,
+                                   const DropMask* drop = nullptr);      // rows of src masked on their way
 // host_ptrs: the same table in host memory; pools of at most 64 slots pass it with the launch and never read out_ptrs
 
 // api.cu: the layer's steps, shared with its form with dropout (dropout.cu)
@@ -331,7 +332,8 @@ marlaas_status_t make_side_stream(marlaas_pool* pool);
 marlaas_status_t reject_captured_tables(const char* fn, const marlaas_pool* pool, cudaStream_t st);
 marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
                                    float* const* dA_slots, float* const* dB_slots, const marlaas_segments_t* seg, const float* h,
-                                   const Workspace& ws, bool acc, cudaStream_t st);
+                                   const Workspace& ws, bool acc, cudaStream_t st, const DropMask* drop = nullptr);
+bool adapter_gradients_fit(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, const Workspace& ws);
 // pool.cu: the pool with other scales of its slots, for the kernel launchers alone (no streams)
 void scaled_view(const marlaas_pool* pool, const float* d_scale, marlaas_pool* view);
 

@@ -6,8 +6,8 @@
 // tcgen05.mma of N = 16 * units multiplies them, and the epilogue keeps, for every token, only the columns of its
 // own tenant: fp32 into out[T][RP] (the h / g the gradient reductions and h_save need) and bf16(s_t * value)
 // into the block-diagonal operand hd the base GEMM's extra k-steps consume (zeros in the other tenants' columns).
-// Same warp roles, pipeline and bounded waits as the base GEMM.  For the layer with dropout (DROP) the epilogue warps zero the
-// dropped elements of every stage in shared memory before the MMA warp may use it, as in shrink_split_sm100.cu.
+// Same warp roles, pipeline and bounded waits as the base GEMM.  For the layer with dropout (DROP) the epilogue warps and
+// four more zero the dropped elements of every stage in shared memory before the MMA warp may use it, as in shrink_split_sm100.cu.
 #include <string.h>
 
 #include "dropout.cuh"
@@ -50,7 +50,7 @@ __device__ __forceinline__ void tc_ld_32x16(uint32_t taddr, uint32_t (&v)[16]) {
 }
 
 template <bool DROP>
-__global__ void __launch_bounds__(SHRINK_THREADS, 1)
+__global__ void __launch_bounds__(SHRINK_THREADS + (DROP ? DROP_EXTRA_THREADS : 0), 1)
 k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ CUtensorMap tmStore,
                const ShrinkArgs g) {
     constexpr int STAGES = SHRINK_STAGES;
@@ -65,7 +65,7 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
     const uint32_t bar_tfull = bar_empty + 8 * STAGES;
     const uint32_t bar_tempty = bar_tfull + 16;
     const uint32_t bar_drain = bar_tempty + 16;
-    const uint32_t bar_ready = bar_drain + 8;       // DROP: the stage is masked (the four epilogue warps)
+    const uint32_t bar_ready = bar_drain + 8;       // DROP: the stage is masked (eight warps)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * STAGES + 5);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -75,7 +75,7 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(bar_full + 8 * s, 1);
             mbar_init(bar_empty + 8 * s, 1);
-            mbar_init(bar_ready + 8 * s, 4);
+            mbar_init(bar_ready + 8 * s, 8);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar_tfull + 8 * b, 1);
@@ -202,8 +202,9 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
                         if (!ok) break;
                         if (!none) {
                             uint8_t* rows = smem + s * A_STAGE_BYTES + rl * 128;
-#pragma unroll 4
-                            for (int c = 0; c < 8; ++c) {
+#pragma unroll
+                            for (int c4 = 0; c4 < 4; ++c4) {
+                                const int c = c4 + (warp >= 6 ? 4 : 0);
                                 uint4* at = reinterpret_cast<uint4*>(rows + ((c ^ (rl & 7)) << 4));
                                 *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)(kb * 8 + c), (uint32_t)row), limit);
                             }
@@ -213,6 +214,7 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
                         if (lane == 0) mbar_arrive(bar_ready + 8 * s);
                     }
                     if (!ok) break;
+                    if (warp >= 6) continue;
                 }
                 ok = mbar_wait(bar_tfull + 8 * b, aph, abort_word, 16);
                 ok = __all_sync(0xffffffffu, ok);
@@ -304,7 +306,7 @@ marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const 
     const int grid = g.num_m_tiles < pool->sm_count ? g.num_m_tiles : pool->sm_count;
     if (drop) g.drop = *drop;
     else memset(&g.drop, 0, sizeof(g.drop));
-    if (drop) k_shrink_sm100<true><<<grid, SHRINK_THREADS, smem_bytes, st>>>(tmSrc, tmStore, g);
+    if (drop) k_shrink_sm100<true><<<grid, SHRINK_THREADS + DROP_EXTRA_THREADS, smem_bytes, st>>>(tmSrc, tmStore, g);
     else k_shrink_sm100<false><<<grid, SHRINK_THREADS, smem_bytes, st>>>(tmSrc, tmStore, g);
     MARLAAS_LAUNCH_CHECK("k_shrink_sm100");
     return MARLAAS_OK;

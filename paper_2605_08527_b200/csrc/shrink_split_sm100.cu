@@ -11,8 +11,8 @@
 // to plane p of the outputs.
 //
 // For the layer with dropout (DROP) the tokens' rows are masked on their way: the four epilogue warps, idle until the accumulator is
-// there, zero the dropped elements of every stage in shared memory (a thread its own row: 16 bytes are one call of the generator)
-// before the MMA warp may use it.
+// there, and four more zero the dropped elements of every stage in shared memory (a thread half of its row: 16 bytes are one call
+// of the generator) before the MMA warp may use it.
 #include <string.h>
 
 #include "dropout.cuh"
@@ -122,7 +122,7 @@ __device__ __forceinline__ int ss_plan_runs(const int32_t* units, int nug, UnitR
 //  - the gather buffer (C x 128 rows x RP floats, in the cluster's first CTA) lies over the stages: once every CTA of the
 //    cluster has seen its last MMA complete (one more cluster barrier per item) nothing touches them until the next item.
 template <bool DROP>
-__global__ void __launch_bounds__(SS_THREADS, 1)
+__global__ void __launch_bounds__(SS_THREADS + (DROP ? DROP_EXTRA_THREADS : 0), 1)
 k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ StoreMaps tmStore,
                      const ShrinkSplitArgs g) {
     constexpr uint32_t TMEM_COLS = 128;
@@ -143,7 +143,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
     const uint32_t bar_empty = bar_full + 8 * SS_MAX_STAGES;
     const uint32_t bar_tfull = bar_empty + 8 * SS_MAX_STAGES;
     const uint32_t bar_drain = bar_tfull + 8;
-    const uint32_t bar_ready = bar_drain + 8;       // DROP: the stage is masked (the four epilogue warps)
+    const uint32_t bar_ready = bar_drain + 8;       // DROP: the stage is masked (eight warps)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * SS_MAX_STAGES + 2);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -151,7 +151,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
         for (int s = 0; s < SS_MAX_STAGES; ++s) {
             mbar_init(bar_full + 8 * s, 1);
             mbar_init(bar_empty + 8 * s, 1);
-            mbar_init(bar_ready + 8 * s, 4);
+            mbar_init(bar_ready + 8 * s, 8);
         }
         mbar_init(bar_tfull, 1);
         mbar_init(bar_drain, 1);
@@ -166,7 +166,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // items per tile, then their exclusive scan (one warp, five tiles per lane)
-    for (int m = threadIdx.x; m < SS_MAX_TILES; m += SS_THREADS)
+    for (int m = threadIdx.x; m < SS_MAX_TILES; m += blockDim.x)
         s_first[m] = m < g.num_m_tiles ? (g.tile_nunits[m >> 1] + g.sub - 1) / g.sub : 0;
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
@@ -299,8 +299,9 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
                         uint8_t* rows = smem + e_s * stage_bytes + rl * 128;
 #pragma unroll
                         for (int p = 0; p < KP; ++p)
-#pragma unroll 4
-                            for (int c = 0; c < 8; ++c) {
+#pragma unroll
+                            for (int c4 = 0; c4 < 4; ++c4) {
+                                const int c = c4 + (warp >= 6 ? 4 : 0);
                                 uint4* at = reinterpret_cast<uint4*>(rows + p * A_STAGE_BYTES + ((c ^ (rl & 7)) << 4));
                                 *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((ks * KP + p) * 8 + c), (uint32_t)row), limit);
                             }
@@ -313,16 +314,18 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
                 }
             }
             // ---- epilogue warps: wait for this CTA's accumulator
-            bool eok = mbar_wait(bar_tfull, done & 1, abort_word, 56);
-            eok = __all_sync(0xffffffffu, eok);
-            ok = eok;
+            if (!DROP || warp < 6) {
+                bool eok = mbar_wait(bar_tfull, done & 1, abort_word, 56);
+                eok = __all_sync(0xffffffffu, eok);
+                ok = eok;
+            }
         }
         // every CTA's MMAs have completed: the stages of the first CTA may now take the partial vectors
         tc_fence_before();
         __syncthreads();
         ss_cluster_sync();
         tc_fence_after();
-        if (warp >= 2) {
+        if (warp >= 2 && (!DROP || warp < 6)) {
             // ---- this CTA's partial values of the row's own tenant columns -> gather buffer of CTA 0
             if (ok) {
                 const uint32_t gdst = ss_map_to_cta(sG, 0) + ((crank * 128u + (uint32_t)rl) * (uint32_t)(g.P * g.RP)) * 4u;
@@ -350,7 +353,7 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
         __syncthreads();
         ss_cluster_sync();
         tc_fence_after();
-        if (crank == 0 && warp >= 2 && row < g.T && ok) {
+        if (crank == 0 && warp >= 2 && (!DROP || warp < 6) && row < g.T && ok) {
             const float* gbuf = reinterpret_cast<const float*>(smem);
             const int prp = g.P * g.RP;
             for (int vu = 0; vu < nvu; ++vu) {
@@ -521,6 +524,7 @@ marlaas_status_t launch_shrink_split_sm100(const marlaas_pool* pool, int64_t T, 
             MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_shrink_split_sm100<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024));
             if (pool->device < 64) attr_set[pool->device] = true;
         }
+        cfg.blockDim = dim3(SS_THREADS + DROP_EXTRA_THREADS);
         MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_shrink_split_sm100<true>, tmSrc, maps, g));
     } else {
         memset(&g.drop, 0, sizeof(g.drop));
