@@ -30,9 +30,12 @@ static DropTables carve_drop(const marlaas_pool* pool, int64_t T, char* base, si
     return t;
 }
 
-__global__ void k_drop_scales(int cap, const float* __restrict__ rates, const float* __restrict__ d_scale, float* __restrict__ scale) {
-    const int t = blockIdx.x * blockDim.x + threadIdx.x;
-    if (t < cap) scale[t] = drop_scale(d_scale[t], drop_limit(rates[t]));
+// What the kernels of a batch of many tokens need before them: s'_t, and zeros in the n16 16-byte words that the split shrink adds to.
+__global__ void __launch_bounds__(256) k_drop_begin(int cap, const float* __restrict__ rates, const float* __restrict__ d_scale, float* __restrict__ scale,
+                                                    uint4* __restrict__ zero, int64_t n16) {
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at < cap) scale[at] = drop_scale(d_scale[at], drop_limit(rates[at]));
+    for (int64_t i = at; i < n16; i += (int64_t)gridDim.x * 256) zero[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // m o x, eight elements per thread and step.
@@ -289,9 +292,13 @@ static marlaas_status_t masked_shrink(const marlaas_pool* v, int64_t T, const bf
     return MARLAAS_OK;
 }
 
-static marlaas_status_t launch_drop_scales(const marlaas_pool* pool, const marlaas_dropout_t* drop, const DropTables& d, cudaStream_t st) {
-    k_drop_scales<<<(unsigned)cdiv(pool->cap, 256), 256, 0, st>>>(pool->cap, drop->rates, pool->d_scale, d.scale);
-    MARLAAS_LAUNCH_CHECK("k_drop_scales");
+// zero: rank vectors of n floats (a multiple of 16) to clear, or NULL
+static marlaas_status_t launch_drop_begin(const marlaas_pool* pool, const marlaas_dropout_t* drop, const DropTables& d, float* zero, size_t n,
+                                          cudaStream_t st) {
+    const int64_t n16 = zero ? (int64_t)(n / 4) : 0;
+    const unsigned grid = (unsigned)std::max<int64_t>(cdiv(pool->cap, 256), std::min<int64_t>(cdiv(n16, 256), (int64_t)pool->sm_count * 8));
+    k_drop_begin<<<grid, 256, 0, st>>>(pool->cap, drop->rates, pool->d_scale, d.scale, (uint4*)zero, n16);
+    MARLAAS_LAUNCH_CHECK("k_drop_begin");
     return MARLAAS_OK;
 }
 
@@ -352,8 +359,7 @@ marlaas_status_t marlaas_lora_forward_dropout(marlaas_pool_t* pool, int64_t T, c
         marlaas_pool v;
         scaled_view(pool, d.scale, &v);
         const bool pre_zero = shrink_split_sm100_eligible(pool, T, pool->K);       // (before the plan: see lora_forward)
-        if (pre_zero) MARLAAS_CUDA_TRY(cudaMemsetAsync(h, 0, sizeof(float) * (size_t)pool->P * T * pool->RP, st));
-        if ((rc = launch_drop_scales(pool, drop, d, st)) != MARLAAS_OK) return rc;
+        if ((rc = launch_drop_begin(pool, drop, d, pre_zero ? h : nullptr, (size_t)pool->P * T * pool->RP, st)) != MARLAAS_OK) return rc;
         if ((rc = make_plan(pool, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
         if ((rc = masked_shrink(&v, T, (const bf16*)x, ldx, ws, mask, h, pre_zero, st)) != MARLAAS_OK) return rc;
     }
@@ -418,8 +424,7 @@ marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, 
     marlaas_pool v;
     scaled_view(pool, d.scale, &v);
     const bool pre_zero = NP == 1 && (dx || want_dA) && shrink_split_sm100_eligible(pool, T, pool->N);
-    if (pre_zero) MARLAAS_CUDA_TRY(cudaMemsetAsync(ws.g, 0, sizeof(float) * (size_t)T * pool->RP, st));
-    if ((rc = launch_drop_scales(pool, drop, d, st)) != MARLAAS_OK) return rc;
+    if ((rc = launch_drop_begin(pool, drop, d, pre_zero ? ws.g : nullptr, (size_t)T * pool->RP, st)) != MARLAAS_OK) return rc;
     if ((rc = make_plan(pool, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
     if (dx || want_dA)
         for (int p = 0; p < NP; ++p) {

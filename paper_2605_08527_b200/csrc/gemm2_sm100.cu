@@ -363,9 +363,9 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     const uint32_t tmem_base = *tmem_slot;
 
     constexpr bool HEAD = EPI == EPI_SOFTMAX || EPI == EPI_GRAD;
-    if (HEAD) {     // launched behind the kernel that makes this one's inputs: everything above overlapped its end
+    if (EPI != EPI_LAYER) {     // launched behind the kernel that makes this one's inputs: everything above overlapped its end
         asm volatile("griddepcontrol.wait;" ::: "memory");
-        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        if (HEAD) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     }
     const int M = HEAD ? head_rows(g.head, g.M) : g.M;
     const int num_m_tiles = HEAD ? (M + 255) / 256 : g.num_m_tiles;
@@ -749,8 +749,7 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    // (EPI_DROP reads what the kernel before it wrote from its first step on)
-    cfg.attrs = at; cfg.numAttrs = EPI == EPI_DROP ? 0 : 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
     MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_gemm2_sm100<KP, EPI>, tmA, tmB, tmXA, tmXB, g));
     count_launch();
     return MARLAAS_OK;
