@@ -49,6 +49,7 @@ struct ShrinkSplitArgs {
     int sub;          // units per work item: SS_SUB_UNITS / P
     int part_rows;    // store rows from one block to the next
     long long out_plane, hd_plane;   // elements from one plane of out / hd to the next
+    int flat_src;     // the contraction is no multiple of 64: a plain map of the source, one copy per panel
     int32_t* status;
     DropMask drop;    // DROP
 };
@@ -253,7 +254,11 @@ k_shrink_split_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_con
                     const uint32_t full = bar_full + 8 * p_s;
                     const uint32_t a0 = sS + p_s * stage_bytes, b0 = a0 + A_STEP;
                     mbar_expect_tx(full, A_STEP + KP * b_panel);
-                    tma_load_3d(a0, &tmSrc, full, 0, m * BM, ks * KP);
+                    if (g.flat_src) {
+                        for (int p = 0; p < KP; ++p) tma_load_2d(a0 + p * A_STAGE_BYTES, &tmSrc, full, (ks * KP + p) * BK, m * BM);
+                    } else {
+                        tma_load_3d(a0, &tmSrc, full, 0, m * BM, ks * KP);
+                    }
                     for (int p = 0; p < KP; ++p)
                         for (int i = 0; i < nruns; ++i)
                             tma_load_2d(b0 + p * b_panel + s_runs[i].pos * UNIT_BYTES, &tmStore.m[s_runs[i].lg],
@@ -463,9 +468,9 @@ static int split_width(const marlaas_pool* pool, int64_t tiles, int64_t num_kb, 
     return 0;
 }
 
-bool shrink_split_sm100_eligible(const marlaas_pool* pool, int64_t T, int64_t D) {
+bool shrink_split_sm100_eligible(const marlaas_pool* pool, int64_t T, int64_t D, bool any_width) {
     size_t smem; int stages, clusters;
-    return T > 0 && (D % 64) == 0 && split_width(pool, cdiv(T, sm100::BM), cdiv(D, sm100::BK), &smem, &stages, &clusters) > 0;
+    return T > 0 && ((D % 64) == 0 || (any_width && D >= 2048)) && split_width(pool, cdiv(T, sm100::BM), cdiv(D, sm100::BK), &smem, &stages, &clusters) > 0;
 }
 
 // All P blocks of adapter rows of a pool over several projections in one pass over the activations (the blocks lie one
@@ -502,7 +507,9 @@ marlaas_status_t launch_shrink_split_sm100(const marlaas_pool* pool, int64_t T, 
     alignas(64) CUtensorMap tmSrc;
     alignas(64) StoreMaps maps;
     marlaas_status_t rc;
-    if ((rc = make_panel_map(&tmSrc, src, T, D, ld, SS_KP)) != MARLAAS_OK) return rc;
+    g.flat_src = D % 64 != 0;
+    rc = g.flat_src ? make_map(&tmSrc, src, T, D, ld, BK, BM) : make_panel_map(&tmSrc, src, T, D, ld, SS_KP);
+    if (rc != MARLAAS_OK) return rc;
     for (int i = 0; i < 4; ++i)
         if ((rc = make_map(&maps.m[i], store, (int64_t)P * pool->cap * pool->RP, D, sld, BK, 16u << i)) != MARLAAS_OK) return rc;
     if (!out_is_zero) MARLAAS_CUDA_TRY(cudaMemsetAsync(out, 0, sizeof(float) * (size_t)P * T * pool->RP, st));
