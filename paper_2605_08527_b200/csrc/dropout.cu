@@ -123,8 +123,11 @@ __global__ void __launch_bounds__(128) k_drop_shrink(int D, const bf16* __restri
     }
 }
 
-// dB and dA of one tenant, 256 columns and 16 ranks per CTA: it lists the tenant's tokens and adds up their products in ascending
-// order in fp32, a thread eight columns of four ranks.  The first CTAs along x do dB (columns of dy), the others dA (of x, masked).
+// dB and dA of one tenant, 256 columns and 16 ranks per CTA: it lists the tenant's tokens and adds up their products in fp32, a
+// thread eight columns of four ranks; DROP_PARTS parts of the CTA take the tokens in turn, and their sums are added in order.
+// Bound by the latency of a token's row: four rows of each part are on their way at a time.  The first CTAs along x do dB
+// (columns of dy), the others dA (of x, masked).
+constexpr int DROP_PARTS = 4;
 constexpr int DROP_INLINE_SLOTS = 64;
 struct DropGrads {
     int T, cap, RP, K, N, tiles_b;
@@ -141,29 +144,29 @@ struct DropGrads {
     float* dA[DROP_INLINE_SLOTS];
     float* dB[DROP_INLINE_SLOTS];
 };
-__global__ void __launch_bounds__(128) k_drop_grads(const __grid_constant__ DropGrads a) {
-    __shared__ int s_tok[DROP_SMALL_T], s_warp[4], s_n;
+__global__ void __launch_bounds__(128 * DROP_PARTS) k_drop_grads(const __grid_constant__ DropGrads a) {
+    constexpr int WARPS = 4 * DROP_PARTS;
+    __shared__ int s_tok[DROP_SMALL_T], s_warp[WARPS];
+    __shared__ float s_acc[32][128];
     const int t = blockIdx.y, j0 = blockIdx.z * 16, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const bool is_b = (int)blockIdx.x < a.tiles_b;
     float* out = is_b ? (a.dB_ptrs ? a.dB_ptrs[t] : a.dB[t]) : (a.dA_ptrs ? a.dA_ptrs[t] : a.dA[t]);
     const int r = a.d_rank[t];
     if (!out || j0 >= r) return;
-    if (tid == 0) s_n = 0;
-    for (int i0 = 0; i0 < a.T; i0 += 128) {
-        const int i = i0 + tid;
-        const bool mine = i < a.T && a.m.tok_slot[i] == t;
-        const unsigned b = __ballot_sync(0xffffffffu, mine);
-        if (lane == 0) s_warp[warp] = __popc(b);
-        __syncthreads();
-        int at = s_n + __popc(b & ((1u << lane) - 1u));
-        for (int w = 0; w < warp; ++w) at += s_warp[w];
-        if (mine) s_tok[at] = i;
-        __syncthreads();
-        if (tid == 0) s_n += s_warp[0] + s_warp[1] + s_warp[2] + s_warp[3];
-    }
+    static_assert(128 * DROP_PARTS == DROP_SMALL_T, "a thread per token");
+    const bool mine = tid < a.T && a.m.tok_slot[tid] == t;
+    const unsigned bal = __ballot_sync(0xffffffffu, mine);
+    if (lane == 0) s_warp[warp] = __popc(bal);
     __syncthreads();
-    const int n = s_n, C = is_b ? a.N : a.K, c = ((int)blockIdx.x - (is_b ? 0 : a.tiles_b)) * 256 + lane * 8, j = j0 + warp * 4;
-    if (c >= C || j >= r) return;
+    int n = 0, at = __popc(bal & ((1u << lane) - 1u));
+    for (int w = 0; w < WARPS; ++w) {
+        at += w < warp ? s_warp[w] : 0;
+        n += s_warp[w];
+    }
+    if (mine) s_tok[at] = tid;
+    __syncthreads();
+    const int C = is_b ? a.N : a.K, c = ((int)blockIdx.x - (is_b ? 0 : a.tiles_b)) * 256 + lane * 8, part = warp >> 2, j = j0 + (warp & 3) * 4;
+    const bool on = c < C && j < r;
     const uint32_t limit = drop_limit(a.m.rates[t]);
     const float s = drop_scale(a.d_scale[t], limit);
     const bf16* src = (is_b ? a.dy : a.x) + c;
@@ -175,32 +178,59 @@ __global__ void __launch_bounds__(128) k_drop_grads(const __grid_constant__ Drop
     for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[k][e] = 0.f;
-#pragma unroll 2
-    for (int q = 0; q < n; ++q) {
-        const int i = s_tok[q];
-        uint4 x = *reinterpret_cast<const uint4*>(src + i * ld);
-        const float4 f = *reinterpret_cast<const float4*>(v + (int64_t)i * a.RP);
-        if (masked) x = drop_apply(x, drop_bits(a.m.key, (uint32_t)(c / 8), (uint32_t)i), limit);
-        const uint32_t* w = &x.x;
+    constexpr int U = 4;
+    if (on) {
+        for (int q0 = part; q0 < n; q0 += DROP_PARTS * U) {
+            uint4 x[U];
+            float4 f[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float z = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
-            acc[0][e] = fmaf(f.x, z, acc[0][e]);
-            acc[1][e] = fmaf(f.y, z, acc[1][e]);
-            acc[2][e] = fmaf(f.z, z, acc[2][e]);
-            acc[3][e] = fmaf(f.w, z, acc[3][e]);
+            for (int u = 0; u < U; ++u) {
+                const int q = q0 + u * DROP_PARTS;
+                if (q < n) {
+                    const int i = s_tok[q];
+                    x[u] = *reinterpret_cast<const uint4*>(src + i * ld);
+                    f[u] = *reinterpret_cast<const float4*>(v + (int64_t)i * a.RP);
+                } else {
+                    x[u] = make_uint4(0u, 0u, 0u, 0u);
+                    f[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int q = q0 + u * DROP_PARTS;
+                if (masked && q < n) x[u] = drop_apply(x[u], drop_bits(a.m.key, (uint32_t)(c / 8), (uint32_t)s_tok[q]), limit);
+                const uint32_t* w = &x[u].x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float z = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+                    acc[0][e] = fmaf(f[u].x, z, acc[0][e]);
+                    acc[1][e] = fmaf(f[u].y, z, acc[1][e]);
+                    acc[2][e] = fmaf(f[u].z, z, acc[2][e]);
+                    acc[3][e] = fmaf(f[u].w, z, acc[3][e]);
+                }
+            }
         }
     }
-    if (n == 0 && a.accumulate) return;
+    for (int p = 0; p < DROP_PARTS; ++p) {      // the parts' sums in their order
+        if (part == p) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (j + k >= r) break;
+            for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float* to = is_b ? out + (size_t)(j + k) * C + c + e : out + (size_t)(c + e) * r + j + k;
-            const float z = s * acc[k][e];
-            *to = a.accumulate ? *to + z : z;
+                for (int e = 0; e < 8; ++e) {
+                    float* to = &s_acc[k * 8 + e][tid & 127];
+                    *to = p == 0 ? acc[k][e] : *to + acc[k][e];
+                }
         }
+        __syncthreads();
+    }
+    if (!on || (n == 0 && a.accumulate)) return;
+    // part k writes rank j + k: eight columns of dB's row, or one rank of eight of dA's
+    if (j + part >= r) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float* to = is_b ? out + (size_t)(j + part) * C + c + e : out + (size_t)(c + e) * r + j + part;
+        const float z = s * s_acc[part * 8 + e][tid & 127];
+        *to = a.accumulate ? *to + z : z;
     }
 }
 
@@ -267,7 +297,7 @@ static marlaas_status_t small_gradients(const marlaas_pool* pool, int64_t T, con
             a.dA_ptrs = ws.dA_ptrs;
             a.dB_ptrs = ws.dB_ptrs;
         }
-        k_drop_grads<<<dim3((unsigned)(a.tiles_b + tiles_a), (unsigned)pool->cap, (unsigned)(pool->RP / 16)), 128, 0, st>>>(a);
+        k_drop_grads<<<dim3((unsigned)(a.tiles_b + tiles_a), (unsigned)pool->cap, (unsigned)(pool->RP / 16)), 128 * DROP_PARTS, 0, st>>>(a);
         MARLAAS_LAUNCH_CHECK("k_drop_grads");
     }
     return MARLAAS_OK;

@@ -46,6 +46,7 @@ struct Gemm2Args {
     int num_m_tiles, num_n_tiles, num_kb;   // 256 x 256 tiles
     int group_m;
     int b_mn;
+    int b_flat;                             // K-major B by one copy per 64-deep panel: a contraction that ends inside a panel
     const int32_t* tile_nunits;             // per 256-row tile
     const int32_t* tile_units;
     int umax;
@@ -449,7 +450,10 @@ k_gemm2_sm100(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                             tma_load_2d_pair(sB + s * B_ST + c * (KP * CHUNK_BYTES), &tmB, full, my_n + c * 64, kb * KP * BK);
                     } else if (my_n < g.Nout) {
                         if (KP == 1) tma_load_2d_pair(sB + s * B_ST, &tmB, full, kb * BK, my_n);
-                        else tma_load_3d_pair(sB + s * B_ST, &tmB, full, 0, my_n, kb * KP);
+                        else if (EPI == EPI_GRAD && g.b_flat) {
+                            for (int p = 0; p < KP; ++p)
+                                tma_load_2d_pair(sB + s * B_ST + p * G2_B_STAGE_BYTES, &tmB, full, (kb * KP + p) * BK, my_n);
+                        } else tma_load_3d_pair(sB + s * B_ST, &tmB, full, 0, my_n, kb * KP);
                     }
                     if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
                 }
@@ -685,6 +689,7 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     // launch: 11008) sixteen row tiles are 90 MB and are read again by every wave of the band; eight are 45 MB.
     while (g.group_m > 4 && (int64_t)g.group_m * 256 * o.Kc * 2 > (int64_t)48 << 20) g.group_m >>= 1;
     g.b_mn = o.b_mn ? 1 : 0;
+    g.b_flat = o.b_cols > 0 && o.b_cols < o.Kc ? 1 : 0;
     g.tile_nunits = o.tile_nunits;
     g.tile_units = o.tile_units;
     g.umax = o.umax;
@@ -705,7 +710,9 @@ static marlaas_status_t launch_gemm2_t(const marlaas_pool* pool, const GemmOpera
     if (KP == 1) rc = make_map(&tmA, o.A, o.M, o.Kc, o.lda, BK, BM);
     else rc = make_panel_map(&tmA, o.A, o.M, o.Kc, o.lda, KP);
     if (rc != MARLAAS_OK) return rc;
-    if (o.b_mn) rc = make_map(&tmB, o.B, o.Kc, o.Nout, o.ldb, 64, BK * KP);
+    // (rows of an MN-major B, or columns of a K-major one, beyond those that there are read as zeros)
+    if (o.b_mn) rc = make_map(&tmB, o.B, o.b_cols > 0 ? o.b_cols : o.Kc, o.Nout, o.ldb, 64, BK * KP);
+    else if (g.b_flat) rc = make_map(&tmB, o.B, o.Nout, o.b_cols, o.ldb, BK, 128);
     else if (KP == 1) rc = make_map(&tmB, o.B, o.Nout, o.Kc, o.ldb, BK, 128);
     else rc = make_panel_map(&tmB, o.B, o.Nout, o.Kc, o.ldb, KP);
     if (rc != MARLAAS_OK) return rc;
@@ -767,12 +774,13 @@ marlaas_status_t launch_gemm2_dropped(const marlaas_pool* pool, const GemmOperan
 
 int head_pairs(const marlaas_pool* pool) { return pool->sm_count / 2; }
 
+// (the head's depths are padded to whole panels)
 marlaas_status_t launch_head_softmax(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st) {
-    return (o.Kc % 64) == 0 ? launch_gemm2_t<2, sm100::EPI_SOFTMAX>(pool, o, st, &h) : launch_gemm2_t<1, sm100::EPI_SOFTMAX>(pool, o, st, &h);
+    return launch_gemm2_t<2, sm100::EPI_SOFTMAX>(pool, o, st, &h);
 }
 
 marlaas_status_t launch_head_grad(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st) {
-    return (o.Kc % 64) == 0 ? launch_gemm2_t<2, sm100::EPI_GRAD>(pool, o, st, &h) : launch_gemm2_t<1, sm100::EPI_GRAD>(pool, o, st, &h);
+    return launch_gemm2_t<2, sm100::EPI_GRAD>(pool, o, st, &h);
 }
 
 }  // namespace marlaas

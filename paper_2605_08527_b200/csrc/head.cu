@@ -33,13 +33,14 @@ constexpr float HEAD_LOG2E = 1.4426950408889634f, HEAD_LN2 = 0.6931471805599453f
 struct HeadArgs {
     int64_t T;
     int d, V, NT;                           // NT: 256-column tiles of the vocabulary
+    int dp;                                 // d in whole 64-element panels: the pitch of the rows
     const bf16* x; int64_t ldx;
     const int32_t* targets;
     const float* weight;                    // or NULL
     float factor;                           // grad_scale * inv_temperature
     const int32_t* perm;
     const int32_t* active;
-    bf16* rows;                             // [T][d] the tokens that count
+    bf16* rows;                             // [T][dp] the tokens that count, zeros behind each
     int32_t* row_target;                    // [T]
     float* row_coef;                        // [T]
     bf16* E; int64_t lde;
@@ -92,8 +93,8 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_gather(const HeadArgs a, 
     const int nvec = a.d / 8;
     if (on) {
         const uint4* src = reinterpret_cast<const uint4*>(a.x + i * a.ldx);
-        uint4* dst = reinterpret_cast<uint4*>(a.rows + p * a.d);
-        for (int v = lane; v < nvec; v += 32) dst[v] = src[v];
+        uint4* dst = reinterpret_cast<uint4*>(a.rows + p * a.dp);
+        for (int v = lane; v < a.dp / 8; v += 32) dst[v] = v < nvec ? src[v] : make_uint4(0u, 0u, 0u, 0u);
         if (lane == 0) {
             a.row_target[p] = a.targets[i];
             a.row_coef[p] = a.factor * (a.weight ? a.weight[i] : 1.f);
@@ -164,20 +165,33 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_rows(const HeadArgs a, in
     const int y = a.row_target[row0 + row], nvec = (a.V + 7) / 8;
     const float py = none ? 0.f : expm1f(logp);
     uint4* e = reinterpret_cast<uint4*>(a.E + (size_t)row * a.lde);
-    for (int v = tid; v < nvec; v += HEAD_THREADS) {
-        uint4 q = e[v];
-        uint32_t* w = &q.x;
-        const float f = s_f[v >> 5];
+    constexpr int U = 4;                        // vectors on their way per thread
+    for (int v0 = tid; v0 < nvec; v0 += HEAD_THREADS * U) {
+        uint4 q[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float lo = __uint_as_float(w[i] << 16) * f, hi = __uint_as_float(w[i] & 0xffff0000u) * f;
-            if (v * 8 + 2 * i == y) lo = py;
-            if (v * 8 + 2 * i + 1 == y) hi = py;
-            __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
-            w[i] = *reinterpret_cast<uint32_t*>(&p);
+        for (int u = 0; u < U; ++u) {
+            const int v = v0 + u * HEAD_THREADS;
+            if (v < nvec) q[u] = e[v];
         }
-        e[v] = q;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int v = v0 + u * HEAD_THREADS;
+            if (v >= nvec) break;
+            uint32_t* w = &q[u].x;
+            const float f = s_f[v >> 5];
+            const int at = y - v * 8;           // the target's place in the vector, if it is there
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float lo = __uint_as_float(w[i] << 16) * f, hi = __uint_as_float(w[i] & 0xffff0000u) * f;
+                if (at == 2 * i) lo = py;
+                if (at == 2 * i + 1) hi = py;
+                __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+                w[i] = *reinterpret_cast<uint32_t*>(&p);
+            }
+            e[v] = q[u];
+        }
     }
+    for (int v = nvec + tid; v < a.lde / 8; v += HEAD_THREADS) e[v] = make_uint4(0u, 0u, 0u, 0u);      // to the end of the last panel
 }
 
 // A bucket (slot, then slot -1) sums its tokens' terms, every thread its own tokens in ascending order, then a tree.
@@ -296,7 +310,7 @@ struct HeadWorkspace {
     int32_t* perm;          // [T]
     int32_t* key_off;       // [3]
     int32_t* scratch;
-    bf16* rows;             // [T][d]
+    bf16* rows;             // [T][dp]
     int32_t* row_target;    // [T]
     float* row_coef;        // [T]
     float4* terms;          // [T]
@@ -304,7 +318,7 @@ struct HeadWorkspace {
     float* target_logit;    // [piece]
     bf16* E;                // [piece][lde]
     float* partial;         // [HEAD_ITEMS][256][256]
-    int64_t piece, lde, NT;
+    int64_t piece, lde, dp, NT;
     size_t total_bytes;
 };
 static HeadWorkspace carve_head(int64_t T, int64_t d, int64_t V, int32_t S, bool grad, void* base) {
@@ -315,6 +329,7 @@ static HeadWorkspace carve_head(int64_t T, int64_t d, int64_t V, int32_t S, bool
     auto take = [&](size_t bytes) { char* q = p ? p + o : nullptr; o += align_up(bytes, 256); return q; };
     w.NT = cdiv(V, 256);
     w.lde = (int64_t)align_up((size_t)V, 64);
+    w.dp = (int64_t)align_up((size_t)d, 64);
     // rows of a piece, a multiple of the row tile: by the exponentials' bytes, or without them by the tiles' pairs
     const size_t row_bytes = grad ? (size_t)w.lde * 2 : (size_t)w.NT * 8;
     w.piece = std::min<int64_t>(T, std::max<int64_t>(HEAD_PIECE_BYTES / row_bytes / 256, 1) * 256);
@@ -323,7 +338,7 @@ static HeadWorkspace carve_head(int64_t T, int64_t d, int64_t V, int32_t S, bool
     w.perm = (int32_t*)take(sizeof(int32_t) * (size_t)T);
     w.key_off = (int32_t*)take(sizeof(int32_t) * 3);
     w.scratch = (int32_t*)take(sizeof(int32_t) * order_scratch_ints(T, 2));
-    w.rows = (bf16*)take(sizeof(bf16) * (size_t)T * (size_t)d);
+    w.rows = (bf16*)take(sizeof(bf16) * (size_t)T * (size_t)w.dp);
     w.row_target = (int32_t*)take(sizeof(int32_t) * (size_t)T);
     w.row_coef = (float*)take(sizeof(float) * (size_t)T);
     w.terms = (float4*)take(sizeof(float4) * (size_t)T);
@@ -419,7 +434,7 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
         }
         HeadArgs a;
         memset(&a, 0, sizeof(a));
-        a.T = T; a.d = (int)d; a.V = (int)V; a.NT = (int)ws.NT;
+        a.T = T; a.d = (int)d; a.V = (int)V; a.NT = (int)ws.NT; a.dp = (int)ws.dp;
         a.x = (const bf16*)x; a.ldx = ldx; a.targets = targets; a.weight = weight; a.factor = grad_scale * inv_temperature;
         a.perm = ws.perm; a.active = ws.key_off + 1; a.rows = ws.rows; a.row_target = ws.row_target; a.row_coef = ws.row_coef;
         a.E = ws.E; a.lde = ws.lde; a.part = ws.part; a.target_logit = ws.target_logit;
@@ -447,8 +462,8 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
             h.row0 = (int)r0;
             h.coef = ws.row_coef + r0;
             GemmOperands g;
-            g.M = rows; g.Nout = V; g.Kc = d;
-            g.A = ws.rows + (size_t)r0 * d; g.lda = d;
+            g.M = rows; g.Nout = V; g.Kc = ws.dp; g.b_cols = d;
+            g.A = ws.rows + (size_t)r0 * ws.dp; g.lda = ws.dp;
             g.B = (const bf16*)W; g.ldb = ldw; g.b_mn = true;
             g.C = ws.E; g.ldc = ws.lde;
             g.XA = g.XB = nullptr; g.xa_cols = g.xb_rows = g.xb_ld = 0;
@@ -459,15 +474,14 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
                 continue;
             }
             if ((rc = launch_behind("k_head_rows", k_head_rows<true>, (unsigned)rows, st, a, (int)r0)) != MARLAAS_OK) return rc;
-            g.Nout = d; g.Kc = V;
+            g.Nout = d; g.Kc = ws.lde; g.b_cols = V;
             g.A = ws.E; g.lda = ws.lde;
             g.b_mn = false;
             g.C = (bf16*)dx; g.ldc = lddx;
             if ((rc = launch_head_grad(pool, g, h, st)) != MARLAAS_OK) return rc;
-            const int kp = V % 64 == 0 ? 2 : 1;         // 64-deep panels per step of that product
             const bool with_stats = stats && r0 + rows >= T;
             if ((rc = launch_behind("k_head_dx", k_head_dx, (unsigned)(rows + (with_stats ? pool->cap + 1 : 0)), st, a, h, (int)rows,
-                                    (int)cdiv(V, 64 * kp) * kp, sums)) != MARLAAS_OK) return rc;
+                                    (int)cdiv(V, 128) * 2, sums)) != MARLAAS_OK) return rc;
         }
     }
     if (stats && (T == 0 || !dx) && (rc = launch_behind("k_head_stats", k_head_stats, (unsigned)(pool->cap + 1), st, sums)) != MARLAAS_OK) return rc;

@@ -214,6 +214,7 @@ struct GemmOperands {
     int32_t parts = 1;
     bool all_parts = false;
     int64_t part_end[4] = {0, 0, 0, 0};
+    int64_t b_cols = 0;                // B's own depth where Kc is A's, padded with zeros to whole 64-deep panels (the head's products)
 };
 marlaas_status_t launch_gemm_sm100(const marlaas_pool* pool, const GemmOperands& o, cudaStream_t st);
 // gemm2_sm100.cu: the same product with 2-CTA clusters (256 x 256 tiles), for batches of at least 1024 rows
@@ -279,8 +280,9 @@ marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const 
 
 // shrink_split_sm100.cu: the same outputs with one tile per cluster and the contraction split over the cluster's
 // CTAs; applies when all tiles fit one wave
-// any_width (the layer with dropout): also where D is no multiple of 64, if it is long enough to be split: 3000 x 2600 masked rows
-// with 16 tenants 110 -> 67 us in all, while at 1032 the cluster's barriers cost 2 us and gain nothing
+// any_width (the layer with dropout): also where D is no multiple of 64, if it is long enough to be split (3000 x 2600 masked
+// rows with 16 tenants: 110 -> 67 us in all) or there are many tiles of a middling one (3000 x 1544: 142 -> 135); at 1000 x 1032 and
+// 6000 x 520 the cluster's barriers cost 2 us and gain nothing
 bool shrink_split_sm100_eligible(const marlaas_pool* pool, int64_t T, int64_t D, bool any_width = false);
 marlaas_status_t launch_shrink_split_sm100(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D,
                                            const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st,

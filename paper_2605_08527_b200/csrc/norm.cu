@@ -285,6 +285,16 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
     };
 #pragma unroll
     for (int u = 0; u < STAGES; ++u) tokens(tok[u], u * B);
+    // the moments of the next batch are asked for a batch ahead, too
+    float mean_next[B], rstd_next[B];
+    auto moments = [&](const int (&t)[B], int r) {
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            mean_next[b] = RMS || r + b >= n ? 0.f : a.mean_in[t[b]];
+            rstd_next[b] = r + b >= n ? 0.f : a.rstd_in[t[b]];
+        }
+    };
+    moments(tok[0], 0);
 #pragma unroll
     for (int u = 0; u < STAGES - 1; ++u) fetch(tok[u], u * B, u);
     int key = -1, par = 0, st = 0, key_end = 0;     // key_end: the group's first row of a later tenant
@@ -324,9 +334,10 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
         float mean[B], rstd[B];
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-            mean[b] = RMS || r + b >= n ? 0.f : a.mean_in[tok[0][b]];
-            rstd[b] = r + b >= n ? 0.f : a.rstd_in[tok[0][b]];
+            mean[b] = mean_next[b];
+            rstd[b] = rstd_next[b];
         }
+        moments(tok[1], r + B);
         if (r >= key_end) {
             if (key >= 0 && a.partial) flush();
             next_tenant(r);

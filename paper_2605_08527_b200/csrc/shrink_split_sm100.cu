@@ -470,7 +470,7 @@ static int split_width(const marlaas_pool* pool, int64_t tiles, int64_t num_kb, 
 
 bool shrink_split_sm100_eligible(const marlaas_pool* pool, int64_t T, int64_t D, bool any_width) {
     size_t smem; int stages, clusters;
-    return T > 0 && ((D % 64) == 0 || (any_width && D >= 2048)) && split_width(pool, cdiv(T, sm100::BM), cdiv(D, sm100::BK), &smem, &stages, &clusters) > 0;
+    return T > 0 && ((D % 64) == 0 || (any_width && (D >= 2048 || (D >= 1024 && T >= 2048)))) && split_width(pool, cdiv(T, sm100::BM), cdiv(D, sm100::BK), &smem, &stages, &clusters) > 0;
 }
 
 // All P blocks of adapter rows of a pool over several projections in one pass over the activations (the blocks lie one
