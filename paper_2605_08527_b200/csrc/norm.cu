@@ -73,9 +73,9 @@ struct GroupSums {
     float v[2][NORM_MAX_GROUPS][4][32];
 };
 
-// 16 bytes, or as many zeros where there is nothing to read: what follows needs no branches for ends of rows and batches
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+// 16 bytes, or (bytes = 0) as many zeros: what follows needs no branches for ends of rows and batches
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -115,12 +115,12 @@ __device__ __forceinline__ void group_sum4(float (&v)[4], GroupSums& s, int& par
 // ---- forward ----
 template <int NV, int B, int STAGES, int THREADS, int PER_SM, bool RMS>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs a, int W, int G) {
-    extern __shared__ uint4 s_ring[];           // [STAGES][B][NV][threads]
+    extern __shared__ uint4 s_ring[];           // [STAGES][B][NV][THREADS]
     __shared__ GroupSums s_sums;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = warp / W, wg = warp % W, l = wg * 32 + lane;
-    const int nvec = a.d / 8, threads = blockDim.x;
+    const int nvec = a.d / 8;
     const float inv_d = 1.f / (float)a.d;
-    for (int64_t s = (int64_t)blockIdx.x * threads + threadIdx.x; s < a.S; s += (int64_t)gridDim.x * threads) {
+    for (int64_t s = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; s < a.S; s += (int64_t)gridDim.x * blockDim.x) {
         const int p = a.off[s], q = a.off[s + 1], t = a.slot[s];
         if (q < p || p < 0 || q > a.T || (s == 0 && p != 0) || (s == a.S - 1 && q != a.T)) dk_report(a.status, DEV_BAD_TABLE, (int)s);
         if (t < -1 || t >= a.cap) dk_report(a.status, DEV_BAD_INDEX, (int)s);
@@ -129,28 +129,36 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
     if (first >= a.T) return;                   // (a group synchronises with itself alone)
     const int n = (int)min(a.rows_per_group, a.T - first);      // rows of the group
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
-    const bf16* x0 = a.x + first * a.ldx;
-    bf16* y0 = a.y + first * a.ldy + l * 8;
     bool mine[NV];
+    uint32_t bytes[NV], at[NV];                 // what a lane copies of a vector's 16 bytes, and from where in the row
 #pragma unroll
-    for (int j = 0; j < NV; ++j) mine[j] = l + j * 32 * W < nvec;
-    auto fetch = [&](int r, int st) {           // starts the copies of the batch at the group's row r
+    for (int j = 0; j < NV; ++j) {
+        const int c = l + j * 32 * W;
+        mine[j] = c < nvec;
+        bytes[j] = mine[j] ? 16 : 0;
+        at[j] = mine[j] ? (uint32_t)c * 16 : 0;
+    }
+    // the next row that is fetched; behind the group's last row it is read again, and dropped
+    const char* px = reinterpret_cast<const char*>(a.x + first * a.ldx);
+    char* py = reinterpret_cast<char*>(a.y + first * a.ldy);
+    const int64_t step_x = a.ldx * 2, step_y = a.ldy * 2;
+    int left = n - 1;                           // rows behind px
+    auto fetch = [&](int st) {
 #pragma unroll
-        for (int b = 0; b < B; ++b)
+        for (int b = 0; b < B; ++b) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const bool on = r + b < n && mine[j];
-                copy16(ring + (uint32_t)(((st * B + b) * NV + j) * threads * 16), on ? x0 + (int64_t)(r + b) * a.ldx + (l + j * 32 * W) * 8 : a.x, on);
-            }
+            for (int j = 0; j < NV; ++j) copy16(ring + (uint32_t)(((st * B + b) * NV + j) * THREADS * 16), px + at[j], bytes[j]);
+            if (left-- > 0) px += step_x;
+        }
         copy_commit();
     };
-    auto element = [&](int st, int b, int j) { return s_ring[((st * B + b) * NV + j) * threads + threadIdx.x]; };
+    auto element = [&](int st, int b, int j) { return s_ring[((st * B + b) * NV + j) * THREADS + threadIdx.x]; };
 #pragma unroll
-    for (int u = 0; u < STAGES - 1; ++u) fetch(u * B, u);
-    // the tenant of the next row: of the last one's segment, of the one after it, or else looked for
-    int seg = -1, seg_begin = 0, seg_end = 0, slot = a.cap, cur = -1, par = 0, st = 0;
-    auto slot_of = [&](int i) {
-        if (i >= seg_begin && i < seg_end) return slot;
+    for (int u = 0; u < STAGES - 1; ++u) fetch(u);
+    int par = 0, st = 0, seg = -1, seg_end = 0; // seg_end: the group's first row of a later segment
+    float2 gain[NV][4], bias[NV][4], f[4];
+    auto next_tenant = [&](int r) {             // the segment of the group's row r: the next one, or else looked for; its parameters
+        const int i = (int)first + r;
         int lo = seg + 1;
         if (seg < 0 || lo >= a.S || a.off[lo] > i || a.off[lo + 1] <= i) {
             lo = 0;
@@ -160,16 +168,26 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
                 if (a.off[m + 1] > i) hi = m; else lo = m + 1;
             }
         }
-        if (lo >= a.S) return a.cap;
-        seg = lo;
-        seg_begin = a.off[lo];
-        seg_end = a.off[lo + 1];
-        const int t = a.slot[lo];
-        return slot = t < 0 || t >= a.cap ? a.cap : t;
+        int t = a.cap;
+        seg_end = r + 1;
+        if (lo < a.S) {
+            seg = lo;
+            seg_end = (int)min((int64_t)n, (int64_t)a.off[lo + 1] - first);
+            t = a.slot[lo];
+            if (t < 0 || t >= a.cap) t = a.cap;
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const size_t c = (size_t)t * a.d + at[j] / 2;
+            load8(a.gain + c, gain[j]);
+            if (a.bias) load8(a.bias + c, bias[j]);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bias[j][e] = make_float2(0.f, 0.f);
+        }
     };
-    float2 gain[NV][4], bias[NV][4], f[4];
     for (int r = 0; r < n; r += B) {
-        fetch(r + (STAGES - 1) * B, st == 0 ? STAGES - 1 : st - 1);
+        fetch(st == 0 ? STAGES - 1 : st - 1);
         copy_wait<STAGES - 1>();
         float v[4] = {0.f, 0.f, 0.f, 0.f}, mean[4] = {0.f, 0.f, 0.f, 0.f};
         if (!RMS) {
@@ -204,39 +222,28 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
         group_sum4(v, s_sums, par, W, g, wg, lane);
 #pragma unroll
         for (int b = 0; b < B; ++b) {
+            v[b] = rsqrtf(fmaf(v[b], inv_d, a.eps));
             if (r + b < n) {
-                const int64_t i = first + r + b;
-                const int t = slot_of((int)i);
-                if (t != cur) {
-                    cur = t;
-#pragma unroll
-                    for (int j = 0; j < NV; ++j) {
-                        const int c = l + j * 32 * W;
-                        if (mine[j]) {
-                            load8(a.gain + (size_t)t * a.d + c * 8, gain[j]);
-                            if (a.bias) load8(a.bias + (size_t)t * a.d + c * 8, bias[j]);
-                            else
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) bias[j][e] = make_float2(0.f, 0.f);
-                        }
-                    }
-                }
-                const float rstd = rsqrtf(fmaf(v[b], inv_d, a.eps)), m = mean[b];
+                if (r + b >= seg_end) next_tenant(r + b);
+                const float2 scale = both(v[b]), shift = both(-mean[b]);
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     unpack8(element(st, b, j), f);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 c = RMS ? f[e] : __fadd2_rn(f[e], both(-m));
-                        f[e] = __ffma2_rn(__fmul2_rn(c, both(rstd)), gain[j][e], bias[j][e]);
-                    }
-                    if (mine[j]) *reinterpret_cast<uint4*>(y0 + (int64_t)(r + b) * a.ldy + j * 256 * W) = pack8(f);
+                    for (int e = 0; e < 4; ++e)         // (x - mean, so that a constant row is its bias)
+                        f[e] = __ffma2_rn(__fmul2_rn(RMS ? f[e] : __fadd2_rn(f[e], shift), scale), gain[j][e], bias[j][e]);
+                    if (mine[j]) *reinterpret_cast<uint4*>(py + at[j]) = pack8(f);
                 }
-                if (l == 0) {
-                    if (a.mean) a.mean[i] = m;
-                    if (a.rstd) a.rstd[i] = rstd;
-                }
+                py += step_y;
             }
+        }
+        if (l == 0) {
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                if (r + b < n) {
+                    if (a.mean) a.mean[first + r + b] = mean[b];
+                    if (a.rstd) a.rstd[first + r + b] = v[b];
+                }
         }
         st = st == STAGES - 1 ? 0 : st + 1;
     }
@@ -248,10 +255,13 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
 // table alone.
 template <int NV, int B, int STAGES, int THREADS, int PER_SM, bool RMS>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArgs a, int W, int G) {
-    extern __shared__ uint4 s_ring[];           // [STAGES][B][x, dy][NV][threads]
+    // CTAs of 1024 threads have no registers left for the gains: each thread keeps its own behind the ring
+    constexpr bool GAIN_SHARED = THREADS == 1024;
+    extern __shared__ uint4 s_ring[];           // [STAGES][B][x, dy][NV][THREADS]
+    float4* const s_gain = reinterpret_cast<float4*>(s_ring + STAGES * B * 2 * NV * THREADS) + threadIdx.x;     // [NV][2][THREADS]
     __shared__ GroupSums s_sums;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = warp / W, wg = warp % W, l = wg * 32 + lane;
-    const int nvec = a.d / 8, threads = blockDim.x;
+    const int nvec = a.d / 8;
     const float inv_d = 1.f / (float)a.d;
     const int64_t q = (int64_t)blockIdx.x * G + g, first = q * a.rows_per_group;
     sm100::dk_wait_prerequisites();
@@ -261,48 +271,54 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
     const int32_t* perm = a.perm + first;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
     bool mine[NV];
+    uint32_t at[NV];                            // a lane's bytes of a row
 #pragma unroll
-    for (int j = 0; j < NV; ++j) mine[j] = l + j * 32 * W < nvec;
-    auto fetch = [&](const int (&tok)[B], int r, int st) {
+    for (int j = 0; j < NV; ++j) {
+        const int c = l + j * 32 * W;
+        mine[j] = c < nvec;
+        at[j] = mine[j] ? (uint32_t)c * 16 : 0;
+    }
+    const char* const px = reinterpret_cast<const char*>(a.x);
+    const char* const pdy = reinterpret_cast<const char*>(a.dy);
+    char* const py = reinterpret_cast<char*>(a.y);
+    const int64_t step_x = a.ldx * 2, step_dy = a.lddy * 2, step_y = a.ldy * 2;
+    auto fetch = [&](const int (&tok)[B], int r, int st) {      // (rows past the end are zeros)
 #pragma unroll
-        for (int b = 0; b < B; ++b)
+        for (int b = 0; b < B; ++b) {
+            const char* x = px + tok[b] * step_x;
+            const char* dy = pdy + tok[b] * step_dy;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const int c = (l + j * 32 * W) * 8;
-                const bool on = r + b < n && mine[j];
-                const uint32_t to = ring + (uint32_t)((((st * B + b) * 2) * NV + j) * threads * 16);
-                copy16(to, on ? a.x + (int64_t)tok[b] * a.ldx + c : a.x, on);
-                copy16(to + (uint32_t)(NV * threads * 16), on ? a.dy + (int64_t)tok[b] * a.lddy + c : a.dy, on);
+                const uint32_t to = ring + (uint32_t)((((st * B + b) * 2) * NV + j) * THREADS * 16), bytes = r + b < n && mine[j] ? 16 : 0;
+                copy16(to, x + at[j], bytes);
+                copy16(to + (uint32_t)(NV * THREADS * 16), dy + at[j], bytes);
             }
+        }
         copy_commit();
     };
-    auto element = [&](int st, int b, int which, int j) { return s_ring[(((st * B + b) * 2 + which) * NV + j) * threads + threadIdx.x]; };
-    // tok[u]: the tokens of the batch u steps ahead
+    auto element = [&](int st, int b, int which, int j) { return s_ring[(((st * B + b) * 2 + which) * NV + j) * THREADS + threadIdx.x]; };
+    // tok[u]: the tokens of the batch u steps ahead; behind the group's last row, that row's
     int tok[STAGES][B];
     auto tokens = [&](int (&t)[B], int r) {
 #pragma unroll
-        for (int b = 0; b < B; ++b) t[b] = r + b < n ? perm[r + b] : 0;
+        for (int b = 0; b < B; ++b) t[b] = perm[min(r + b, n - 1)];
     };
 #pragma unroll
     for (int u = 0; u < STAGES; ++u) tokens(tok[u], u * B);
     // the moments of the next batch are asked for a batch ahead, too
     float mean_next[B], rstd_next[B];
-    auto moments = [&](const int (&t)[B], int r) {
+    auto moments = [&](const int (&t)[B]) {
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-            mean_next[b] = RMS || r + b >= n ? 0.f : a.mean_in[t[b]];
-            rstd_next[b] = r + b >= n ? 0.f : a.rstd_in[t[b]];
+            mean_next[b] = RMS ? 0.f : a.mean_in[t[b]];
+            rstd_next[b] = a.rstd_in[t[b]];
         }
     };
-    moments(tok[0], 0);
+    moments(tok[0]);
 #pragma unroll
     for (int u = 0; u < STAGES - 1; ++u) fetch(tok[u], u * B, u);
     int key = -1, par = 0, st = 0, key_end = 0;     // key_end: the group's first row of a later tenant
-    float2 gain[NV][4], sg[NV][4], sb[NV][4];
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) gain[j][e] = make_float2(0.f, 0.f);
+    float2 gain_kept[GAIN_SHARED ? 1 : NV][4], sg[NV][4], sb[NV][4];
     auto flush = [&]() {
         float* out = a.partial + (size_t)(q + key) * 2 * a.d;
 #pragma unroll
@@ -320,11 +336,35 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
             }
         }
     };
-    auto next_tenant = [&](int r) {             // the next tenant that has tokens; its gain, and sums of 0
-        do key_end = (int)min((int64_t)n, a.key_off[++key + 1] - first); while (key_end <= r);
+    auto load_gain = [&](int t) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            if (mine[j]) load8(a.gain + (size_t)key * a.d + (l + j * 32 * W) * 8, gain[j]);
+            float2 w[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
+            if (mine[j]) load8(a.gain + (size_t)t * a.d + at[j] / 2, w);
+            if (GAIN_SHARED) {
+                s_gain[2 * j * THREADS] = make_float4(w[0].x, w[0].y, w[1].x, w[1].y);
+                s_gain[(2 * j + 1) * THREADS] = make_float4(w[2].x, w[2].y, w[3].x, w[3].y);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) gain_kept[j][e] = w[e];
+            }
+        }
+    };
+    auto gains = [&](int j, float2 (&w)[4]) {
+        if (GAIN_SHARED) {
+            const float4 p = s_gain[2 * j * THREADS], q = s_gain[(2 * j + 1) * THREADS];
+            w[0] = make_float2(p.x, p.y); w[1] = make_float2(p.z, p.w);
+            w[2] = make_float2(q.x, q.y); w[3] = make_float2(q.z, q.w);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = gain_kept[j][e];
+        }
+    };
+    auto next_tenant = [&](int r) {             // the next tenant that has tokens; its gain, and sums of 0
+        do key_end = (int)min((int64_t)n, a.key_off[++key + 1] - first); while (key_end <= r);
+        load_gain(key);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) sg[j][e] = sb[j][e] = make_float2(0.f, 0.f);
         }
@@ -337,7 +377,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
             mean[b] = mean_next[b];
             rstd[b] = rstd_next[b];
         }
-        moments(tok[1], r + B);
+        moments(tok[1]);
         if (r >= key_end) {
             if (key >= 0 && a.partial) flush();
             next_tenant(r);
@@ -345,61 +385,51 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
         const int key0 = key;                   // (the batch's second row may be the next tenant's)
         copy_wait<STAGES - 1>();
         float v[4] = {0.f, 0.f, 0.f, 0.f};
-        float2 x[4], dy[4];
+        float2 x[4], dy[4], gain[4];
 #pragma unroll
         for (int b = 0; b < B; ++b) {
             if (b == 1 && r + 1 >= key_end && r + 1 < n) {
                 if (a.partial) flush();
                 next_tenant(r + 1);
             }
+            float2 s = make_float2(0.f, 0.f), u = s;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {      // (zeros past the row's and the batch's end add nothing)
+            for (int j = 0; j < NV; ++j) {      // (dy is zero past the row's and the batch's end and adds nothing)
                 unpack8(element(st, b, 0, j), x);
                 unpack8(element(st, b, 1, j), dy);
-                float2 s = make_float2(0.f, 0.f), u = s;
+                gains(j, gain);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+                    // (x - mean, so that a sum of one token keeps its digits where x is near the mean)
                     const float2 xh = __fmul2_rn(RMS ? x[e] : __fadd2_rn(x[e], both(-mean[b])), both(rstd[b]));
-                    const float2 av = __fmul2_rn(dy[e], gain[j][e]);
+                    const float2 av = __fmul2_rn(dy[e], gain[e]);
                     sg[j][e] = __ffma2_rn(dy[e], xh, sg[j][e]);
                     sb[j][e] = __fadd2_rn(dy[e], sb[j][e]);
                     if (!RMS) s = __fadd2_rn(av, s);
                     u = __ffma2_rn(av, xh, u);
                 }
-                v[2 * b] += s.x + s.y;
-                v[2 * b + 1] += u.x + u.y;
             }
+            v[2 * b] = s.x + s.y;
+            v[2 * b + 1] = u.x + u.y;
         }
         if (a.y) {
             group_sum4(v, s_sums, par, W, g, wg, lane);
 #pragma unroll
             for (int b = B - 1; b >= 0; --b) {
-                const float ma = v[2 * b] * inv_d, mx = v[2 * b + 1] * inv_d;
+                if (r + b < n) {
+                    // dx = a rstd + (x - mean) k + c
+                    const float mx = v[2 * b + 1] * inv_d, k = -rstd[b] * rstd[b] * mx, c = -rstd[b] * (v[2 * b] * inv_d);
+                    char* const to = py + tok[0][b] * step_y;
+                    if (b == 0 && key0 != key) load_gain(key0);
 #pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    const int c = l + j * 32 * W;
-                    if (r + b < n && mine[j]) {
+                    for (int j = 0; j < NV; ++j) {
                         unpack8(element(st, b, 0, j), x);
                         unpack8(element(st, b, 1, j), dy);
-                        if (b == 0 && key0 != key) {
-                            float2 w[4];
-                            load8(a.gain + (size_t)key0 * a.d + c * 8, w);
+                gains(j, gain);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) dy[e] = __fmul2_rn(dy[e], w[e]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) dy[e] = __fmul2_rn(dy[e], gain[j][e]);
-                        }
-                        const float k = rstd[b] * mx;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (!RMS) {
-                                x[e] = __fadd2_rn(x[e], both(-mean[b]));
-                                dy[e] = __fadd2_rn(dy[e], both(-ma));
-                            }
-                            x[e] = __fmul2_rn(__ffma2_rn(x[e], both(-k), dy[e]), both(rstd[b]));
-                        }
-                        *reinterpret_cast<uint4*>(a.y + (int64_t)tok[0][b] * a.ldy + c * 8) = pack8(x);
+                        for (int e = 0; e < 4; ++e)
+                            x[e] = __ffma2_rn(__fmul2_rn(dy[e], gain[e]), both(rstd[b]), RMS ? __fmul2_rn(x[e], both(k)) : __ffma2_rn(__fadd2_rn(x[e], both(-mean[b])), both(k), both(c)));
+                        if (mine[j]) *reinterpret_cast<uint4*>(to + at[j]) = pack8(x);
                     }
                 }
             }
@@ -410,6 +440,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
             for (int b = 0; b < B; ++b) tok[u][b] = tok[u + 1][b];
         tokens(tok[STAGES - 1], r + STAGES * B);
         st = st == STAGES - 1 ? 0 : st + 1;
+        if (a.y && key0 != key) load_gain(key);
     }
     if (a.partial) flush();
 }
@@ -470,7 +501,7 @@ static NormPlan norm_plan(const marlaas_pool* pool, int64_t T, int d, bool backw
     p.W = (int)cdiv(nvec, 32 * p.NV);
     p.G = std::max(1, std::min(NORM_MAX_GROUPS, 8 / p.W));
     const int threads = 32 * p.W * p.G;
-    const int64_t most = (int64_t)pool->sm_count * std::max(1, (threads <= 256 ? 768 : 640) / threads) * p.G;
+    const int64_t most = (int64_t)pool->sm_count * std::max(1, (threads <= 256 ? backward && p.NV == 2 ? 512 : 768 : 640) / threads) * p.G;
     // (a group's partial sums cost as much as four of its rows: backward, no group takes fewer)
     p.rows = std::max<int64_t>(cdiv(T, most), backward ? 4 : 1);
     p.groups = cdiv(cdiv(T, p.rows), p.G) * p.G;
@@ -511,9 +542,9 @@ template <int NV, int THREADS, int PER_SM, bool RMS>
 static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& a, const NormPlan& n, bool backward, cudaStream_t st) {
     constexpr int STAGES = NV == 1 ? 3 : 2, FB = 4, BB = THREADS == 1024 ? 1 : 2;
     const int threads = 32 * n.W * n.G;
-    const size_t fwd = (size_t)STAGES * FB * NV * 16, bwd = (size_t)STAGES * BB * 2 * NV * 16;       // bytes of the ring per thread
+    const size_t fwd = (size_t)STAGES * FB * NV * 16, bwd = (size_t)STAGES * BB * 2 * NV * 16 + (THREADS == 1024 ? NV * 32 : 0);      // shared bytes per thread
     auto* kf = k_norm_forward<NV, THREADS == 1024 ? 2 : FB, STAGES, THREADS, PER_SM, RMS>;
-    auto* kb = k_norm_backward<NV, BB, STAGES, THREADS, PER_SM, RMS>;
+    auto* kb = k_norm_backward<NV, BB, STAGES, THREADS, NV == 2 && PER_SM == 3 ? 2 : PER_SM, RMS>;
     static bool attr_set[64] = {};
     if (pool->device >= 64 || !attr_set[pool->device]) {
         MARLAAS_CUDA_TRY(cudaFuncSetAttribute(kf, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::min<size_t>(fwd * THREADS, 200 * 1024)));
@@ -527,7 +558,7 @@ static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& 
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3((unsigned)(n.groups / n.G));
     cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (backward ? bwd : THREADS == 1024 ? fwd / 2 : fwd) * threads;
+    cfg.dynamicSmemBytes = (backward ? bwd : THREADS == 1024 ? fwd / 2 : fwd) * THREADS;
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = backward ? 1 : 0;
