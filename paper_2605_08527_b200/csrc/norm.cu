@@ -70,7 +70,7 @@ __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 // copying thread reads, so that the only barriers are those of the rows' sums, of four values at a time.
 constexpr int NORM_MAX_GROUPS = 8;
 struct GroupSums {
-    float v[2][NORM_MAX_GROUPS][4][32];
+    float v[2][NORM_MAX_GROUPS][4][16];
 };
 
 // 16 bytes, or (bytes = 0) as many zeros: what follows needs no branches for ends of rows and batches
@@ -99,10 +99,6 @@ __device__ __forceinline__ void group_sum4(float (&v)[4], GroupSums& s, int& par
         const float* part = s.v[par][g][k] + (lane & 7);
         x = (lane & 7) < W ? part[0] : 0.f;
         if (W > 8) x += (lane & 7) + 8 < W ? part[8] : 0.f;
-        if (W > 16) {
-            x += (lane & 7) + 16 < W ? part[16] : 0.f;
-            x += (lane & 7) + 24 < W ? part[24] : 0.f;
-        }
         x += __shfl_xor_sync(0xffffffffu, x, 4);
         x += __shfl_xor_sync(0xffffffffu, x, 2);
         x += __shfl_xor_sync(0xffffffffu, x, 1);
@@ -255,8 +251,8 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
 // table alone.
 template <int NV, int B, int STAGES, int THREADS, int PER_SM, bool RMS>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArgs a, int W, int G) {
-    // CTAs of 1024 threads have no registers left for the gains: each thread keeps its own behind the ring
-    constexpr bool GAIN_SHARED = THREADS == 1024;
+    // four vectors per lane leave no registers for the gains: each thread keeps its own behind the ring
+    constexpr bool GAIN_SHARED = NV == 4;
     extern __shared__ uint4 s_ring[];           // [STAGES][B][x, dy][NV][THREADS]
     float4* const s_gain = reinterpret_cast<float4*>(s_ring + STAGES * B * 2 * NV * THREADS) + threadIdx.x;     // [NV][2][THREADS]
     __shared__ GroupSums s_sums;
@@ -489,7 +485,9 @@ __global__ void __launch_bounds__(1024) k_norm_reduce(const NormArgs a) {
 }
 
 // How a pass cuts a batch: vectors per lane, warps per row and rows of a CTA at a time, groups in all and their rows.
-// Two vectors per lane where a row has them: half of a row's instructions do not depend on how many elements a lane has.
+// As many vectors per lane as registers allow: half of a row's instructions do not depend on how many elements a lane has.
+// Backward 16384 x 5120: four per lane 92 us, two 105; 2000 x 16384: 54 us, with two (and 1024 threads, whose registers spill) 114;
+// below 2048 elements four leave too few warps per row's sum or idle lanes (2048: 41 us against 40).
 struct NormPlan {
     int NV, W, G;
     int64_t groups, rows;
@@ -497,11 +495,11 @@ struct NormPlan {
 static NormPlan norm_plan(const marlaas_pool* pool, int64_t T, int d, bool backward) {
     NormPlan p;
     const int nvec = d / 8;
-    p.NV = nvec >= 64 ? 2 : 1;
+    p.NV = nvec >= 256 ? 4 : nvec >= 64 ? 2 : 1;
     p.W = (int)cdiv(nvec, 32 * p.NV);
-    p.G = std::max(1, std::min(NORM_MAX_GROUPS, 8 / p.W));
+    p.G = (int)std::max<int64_t>(1, std::min<int64_t>({NORM_MAX_GROUPS, (p.NV == 4 ? 16 : 8) / p.W, cdiv(T, pool->sm_count)}));
     const int threads = 32 * p.W * p.G;
-    const int64_t most = (int64_t)pool->sm_count * std::max(1, (threads <= 256 ? backward && p.NV == 2 ? 512 : 768 : 640) / threads) * p.G;
+    const int64_t most = (int64_t)pool->sm_count * std::max(1, (p.NV == 4 || (backward && p.NV == 2) ? 512 : 768) / threads) * p.G;
     // (a group's partial sums cost as much as four of its rows: backward, no group takes fewer)
     p.rows = std::max<int64_t>(cdiv(T, most), backward ? 4 : 1);
     p.groups = cdiv(cdiv(T, p.rows), p.G) * p.G;
@@ -536,14 +534,15 @@ static NormWorkspace carve_norm(const marlaas_pool* pool, int64_t T, int32_t S, 
     return w;
 }
 
-// Instances by the width of a row and of a CTA: rows of up to 4096 elements share an SM three CTAs at a time, up to 5120 two,
-// wider ones one; shared memory holds the rows on their way.
+// Instances by the vectors per lane.  CTAs share an SM so that no instance spills: what is left of L1 beside the rows on their way
+// does not hold spilled registers (backward 16384 x 4096 with 80 registers per thread, RMS: 183 us, with 114 and two CTAs instead
+// of three: 74).
 template <int NV, int THREADS, int PER_SM, bool RMS>
 static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& a, const NormPlan& n, bool backward, cudaStream_t st) {
-    constexpr int STAGES = NV == 1 ? 3 : 2, FB = 4, BB = THREADS == 1024 ? 1 : 2;
+    constexpr int STAGES = NV == 1 ? 3 : 2, FB = NV == 4 ? 2 : 4, BB = NV == 4 ? 1 : 2;
     const int threads = 32 * n.W * n.G;
-    const size_t fwd = (size_t)STAGES * FB * NV * 16, bwd = (size_t)STAGES * BB * 2 * NV * 16 + (THREADS == 1024 ? NV * 32 : 0);      // shared bytes per thread
-    auto* kf = k_norm_forward<NV, THREADS == 1024 ? 2 : FB, STAGES, THREADS, PER_SM, RMS>;
+    const size_t fwd = (size_t)STAGES * FB * NV * 16, bwd = (size_t)STAGES * BB * 2 * NV * 16 + (NV == 4 ? NV * 32 : 0);      // shared bytes per thread
+    auto* kf = k_norm_forward<NV, FB, STAGES, THREADS, PER_SM, RMS>;
     auto* kb = k_norm_backward<NV, BB, STAGES, THREADS, NV == 2 && PER_SM == 3 ? 2 : PER_SM, RMS>;
     static bool attr_set[64] = {};
     if (pool->device >= 64 || !attr_set[pool->device]) {
@@ -558,7 +557,7 @@ static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& 
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3((unsigned)(n.groups / n.G));
     cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (backward ? bwd : THREADS == 1024 ? fwd / 2 : fwd) * THREADS;
+    cfg.dynamicSmemBytes = (backward ? bwd : fwd) * THREADS;
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = backward ? 1 : 0;
@@ -571,8 +570,7 @@ static marlaas_status_t launch_norm(const marlaas_pool* pool, NormArgs a, bool r
     a.rows_per_group = n.rows;
 #define NORM_GO(nv, threads, per) (rms ? launch_norm_t<nv, threads, per, true>(pool, a, n, backward, st) : launch_norm_t<nv, threads, per, false>(pool, a, n, backward, st))
     if (n.NV == 1) return NORM_GO(1, 256, 3);
-    if (n.W <= 8) return NORM_GO(2, 256, 3);
-    return n.W <= 10 ? NORM_GO(2, 320, 2) : n.W <= 16 ? NORM_GO(2, 512, 1) : NORM_GO(2, 1024, 1);
+    return n.NV == 2 ? NORM_GO(2, 256, 3) : NORM_GO(4, 512, 1);
 #undef NORM_GO
 }
 
