@@ -215,12 +215,16 @@ marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf
     const bool fits = adapter_gradients_fit(pool, T, seg, ws);
     const bool inline_tables = fits && pool->cap <= 64;
     const int32_t* run_flag = tc_grad ? ws.gflag : nullptr;
-    if (tc_grad && (rc = launch_grad_plan(pool, T, ws, st)) != MARLAAS_OK) return rc;
+    // (behind a copy or a clear nothing is launched ahead of time)
+    if (tc_grad && (rc = launch_grad_plan(pool, T, ws, st, true)) != MARLAAS_OK) return rc;
     if (!fits && (rc = launch_slot_sort(pool, T, ws.tok_slot, ws.slot_count, ws.slot_offset, ws.perm, st, run_flag)) != MARLAAS_OK) return rc;
     std::vector<float*> part((size_t)pool->cap, nullptr);
     for (int p = 0; p < NP; ++p) {
         if (tc_grad && p > 0) MARLAAS_CUDA_TRY(cudaMemsetAsync(ws.gflag + 2, 0, 2 * sizeof(int32_t), st));
         const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
+        const float *rB = h + p * plane, *rA = ws.g + p * plane;
+        if (tc_grad && (rc = launch_grad_copies(pool, T, ws, dB_slots ? rB : rA, dB_slots ? ws.hm : ws.hm2, dA_slots && dB_slots ? rA : nullptr, ws.hm2,
+                                                p == 0 && fits, st)) != MARLAAS_OK) return rc;
         for (int which = 0; which < 2; ++which) {       // dB, then dA
             float* const* all = which == 0 ? dB_slots : dA_slots;
             if (!all) continue;
@@ -231,11 +235,11 @@ marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf
             float** dev = which == 0 ? ws.dB_ptrs : ws.dA_ptrs;
             const bf16* src = which == 0 ? dy + c0 : x;
             const int64_t ld = which == 0 ? lddy : ldx, C = which == 0 ? Np : pool->K;
-            const float* r = which == 0 ? h + p * plane : ws.g + p * plane;
+            const float* r = which == 0 ? rB : rA;
             if (!inline_tables)
                 MARLAAS_CUDA_TRY(cudaMemcpyAsync(dev, part.data(), sizeof(float*) * (size_t)pool->cap, cudaMemcpyHostToDevice, st));
-            if (tc_grad && (rc = launch_grad_sm100(pool, T, C, src, ld, r, dev, part.data(), which == 1, acc, ws, st, ws.hm,
-                                                   GRAD_PHASE_COPIES | GRAD_PHASE_REDUCE, which == 1 ? drop : nullptr)) != MARLAAS_OK) return rc;
+            if (tc_grad && (rc = launch_grad_sm100(pool, T, C, src, ld, r, dev, part.data(), which == 1, acc, ws, st, which == 0 ? ws.hm : ws.hm2,
+                                                   GRAD_PHASE_REDUCE | (inline_tables ? GRAD_PHASE_CHAINED : 0), which == 1 ? drop : nullptr)) != MARLAAS_OK) return rc;
             if (!fits && (rc = launch_grad_reduce(pool, C, src, ld, r, ws.perm, ws.slot_offset, dev, which == 1, acc, st, run_flag)) != MARLAAS_OK)
                 return rc;
         }

@@ -40,11 +40,19 @@ __device__ __forceinline__ void tc_ld_32x16g(uint32_t taddr, uint32_t (&v)[16]) 
         : "memory");
 }
 
+// A kernel of a chained sequence: launched while the one before it still runs, it waits for that one's end, and lets the next one
+// be launched.  (Its inputs are not declared __restrict__: loads of what the kernel itself never writes could be moved before the wait.)
+__device__ __forceinline__ void chain_link() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // ---- plan: which tenants are present in each 64-token block ----------------------------------------------------
-__global__ void __launch_bounds__(64) k_grad_presence(int T, int cap, const int32_t* __restrict__ tok_slot,
-                                                      const int32_t* __restrict__ d_rank,
-                                                      int32_t* __restrict__ blk_np, int32_t* __restrict__ blk_rank) {
+__global__ void __launch_bounds__(64) k_grad_presence(int T, int cap, const int32_t* tok_slot,
+                                                      const int32_t* d_rank,
+                                                      int32_t* __restrict__ blk_np, int32_t* __restrict__ blk_rank, int chained) {
     __shared__ int pres[256];
+    if (chained) chain_link();
     const int blk = blockIdx.x, tid = threadIdx.x;
     for (int t = tid; t < cap; t += 64) pres[t] = 0;
     __syncthreads();
@@ -67,11 +75,12 @@ __global__ void __launch_bounds__(64) k_grad_presence(int T, int cap, const int3
 // One CTA per tenant: position of every copy (exclusive scan of the per-block counts) and the tenant's copy list in
 // ascending block order.  CTA 0 also publishes the scan and decides whether the copies fit.
 __global__ void __launch_bounds__(256) k_grad_lists(int nblk, int cap, int max_copies,
-                                                    const int32_t* __restrict__ blk_np,
-                                                    const int32_t* __restrict__ blk_rank,
+                                                    const int32_t* blk_np,
+                                                    const int32_t* blk_rank,
                                                     int32_t* __restrict__ blk_base, int32_t* __restrict__ ten_nblk,
                                                     int32_t* __restrict__ ten_blks, int32_t* __restrict__ ten_pos,
-                                                    int32_t* __restrict__ gflag) {
+                                                    int32_t* __restrict__ gflag, int chained) {
+    if (chained) chain_link();
     __shared__ int base[4096 + 1];
     __shared__ int s_warp[8];
     __shared__ int s_run;
@@ -136,13 +145,17 @@ __global__ void __launch_bounds__(256) k_grad_lists(int nblk, int cap, int max_c
 }
 
 // One CTA per 64-token block: writes the block's copies, hm[(copy*64 + row)][HW] = [ hi(v) | lo(v) | 0 ] for rows of
-// the copy's tenant and zero rows for the other tokens of the block.
-__global__ void __launch_bounds__(256) k_pad_split(int T, int cap, int RP, int HW, const float* __restrict__ src,
-                                                   const int32_t* __restrict__ tok_slot,
-                                                   const int32_t* __restrict__ blk_base,
-                                                   const int32_t* __restrict__ blk_rank,
-                                                   const int32_t* __restrict__ gflag, bf16* __restrict__ hm) {
+// the copy's tenant and zero rows for the other tokens of the block.  A grid of two rows does so for both r-vectors.
+__global__ void __launch_bounds__(256) k_pad_split(int T, int cap, int RP, int HW, const float* src0,
+                                                   const int32_t* tok_slot,
+                                                   const int32_t* blk_base,
+                                                   const int32_t* blk_rank,
+                                                   const int32_t* gflag, bf16* __restrict__ hm0,
+                                                   const float* src1, bf16* __restrict__ hm1, int chained) {
+    if (chained) chain_link();
     if (gflag[0] != 0) return;
+    const float* const src = blockIdx.y == 0 ? src0 : src1;
+    bf16* const hm = blockIdx.y == 0 ? hm0 : hm1;
     const int blk = blockIdx.x, tid = threadIdx.x;
     const int base = blk_base[blk];
     const int chunks_per_row = HW / 8;
@@ -194,6 +207,7 @@ struct GradArgs {
     int stages;            // pipeline steps in flight
     int32_t* status;
     int T;
+    int chained;           // launched while the kernel before it still runs: waits for its end
     DropMask drop;         // DROP
     float* inl[GRAD_INLINE_SLOTS];   // small pools: the pointer table travels with the launch (no host-to-device copy)
 };
@@ -207,6 +221,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
     // A second reduction launched behind this one as a programmatic dependent (it reads nothing this one writes) may
     // take over every SM a CTA of this grid leaves.
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (g.chained) asm volatile("griddepcontrol.wait;" ::: "memory");
     if (g.gflag[0] != 0) return;   // copies did not fit: the CUDA-core reduction handles this call
 
     extern __shared__ uint8_t smem_raw[];
@@ -503,15 +518,38 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
 
 bool grad_sm100_eligible(const marlaas_pool* pool, int64_t T) { return pool->cap <= 256 && T > 0 && cdiv(T, 64) <= 4096; }
 
-marlaas_status_t launch_grad_plan(const marlaas_pool* pool, int64_t T, const Workspace& ws, cudaStream_t st) {
-    using namespace sm100;
-    const int nblk = (int)cdiv(T, 64);
-    k_grad_presence<<<nblk, 64, 0, st>>>((int)T, pool->cap, ws.tok_slot, pool->d_rank, ws.blk_np, ws.blk_rank);
-    MARLAAS_LAUNCH_CHECK("k_grad_presence");
-    k_grad_lists<<<pool->cap, 256, 0, st>>>(nblk, pool->cap, ws.max_copies, ws.blk_np, ws.blk_rank, ws.blk_base,
-                                            ws.ten_nblk, ws.ten_blks, ws.ten_pos, ws.gflag);
-    MARLAAS_LAUNCH_CHECK("k_grad_lists");
+template <typename... P, typename... A>
+static marlaas_status_t launch_link(const char* name, void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, bool chained, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = chained ? 1 : 0;
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
+    MARLAAS_LAUNCH_CHECK(name);
     return MARLAAS_OK;
+}
+
+marlaas_status_t launch_grad_plan(const marlaas_pool* pool, int64_t T, const Workspace& ws, cudaStream_t st, bool chained) {
+    using namespace sm100;
+    const int nblk = (int)cdiv(T, 64), c = chained ? 1 : 0;
+    const marlaas_status_t rc = launch_link("k_grad_presence", k_grad_presence, dim3((unsigned)nblk), 64, 0, chained, st, (int)T, pool->cap, ws.tok_slot,
+                                            pool->d_rank, ws.blk_np, ws.blk_rank, c);
+    if (rc != MARLAAS_OK) return rc;
+    return launch_link("k_grad_lists", k_grad_lists, dim3((unsigned)pool->cap), 256, 0, chained, st, nblk, pool->cap, ws.max_copies, ws.blk_np, ws.blk_rank,
+                       ws.blk_base, ws.ten_nblk, ws.ten_blks, ws.ten_pos, ws.gflag, c);
+}
+
+marlaas_status_t launch_grad_copies(const marlaas_pool* pool, int64_t T, const Workspace& ws, const float* r0, bf16* hm0, const float* r1, bf16* hm1,
+                                    bool chained, cudaStream_t st) {
+    return launch_link("k_pad_split", sm100::k_pad_split, dim3((unsigned)cdiv(T, 64), r1 ? 2 : 1), 256, 0, chained, st, (int)T, pool->cap, pool->RP, ws.HW, r0,
+                       ws.tok_slot, ws.blk_base, ws.blk_rank, ws.gflag, hm0, r1, hm1, chained ? 1 : 0);
 }
 
 marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t C, const bf16* src, int64_t ld,
@@ -520,11 +558,8 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
                                    const Workspace& ws, cudaStream_t st, bf16* hm, int phases, const DropMask* drop) {
     using namespace sm100;
     const int nblk = (int)cdiv(T, 64);
-    if (phases & GRAD_PHASE_COPIES) {
-        k_pad_split<<<nblk, 256, 0, st>>>((int)T, pool->cap, pool->RP, ws.HW, hg, ws.tok_slot, ws.blk_base, ws.blk_rank,
-                                          ws.gflag, hm);
-        MARLAAS_LAUNCH_CHECK("k_pad_split");
-    }
+    marlaas_status_t rc;
+    if ((phases & GRAD_PHASE_COPIES) && (rc = launch_grad_copies(pool, T, ws, hg, hm, nullptr, nullptr, false, st)) != MARLAAS_OK) return rc;
     if (!(phases & GRAD_PHASE_REDUCE)) return MARLAAS_OK;
     GradArgs g;
     g.C = (int)C;
@@ -549,10 +584,11 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
     g.accumulate = accumulate ? 1 : 0;
     g.status = pool->d_status;
     g.T = (int)T;
+    const bool chained = (phases & GRAD_PHASE_CHAINED) != 0;
+    g.chained = chained ? 1 : 0;
     if (drop) g.drop = *drop;
     else memset(&g.drop, 0, sizeof(g.drop));
     alignas(64) CUtensorMap tmSrc, tmHm;
-    marlaas_status_t rc;
     if ((rc = make_map(&tmSrc, src, T, C, ld, 64, 64)) != MARLAAS_OK) return rc;
     if ((rc = make_map(&tmHm, hm, (int64_t)ws.max_copies * 64, ws.HW, ws.HW, 64, 64)) != MARLAAS_OK) return rc;
     // as many steps of GRAD_BPS blocks as fit what four single-block steps of the widest r-vectors take
@@ -580,13 +616,11 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
         at[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = at; cfg.numAttrs = 1;
         MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_grad_sm100<false>, tmSrc, tmHm, g));
-    } else if (drop) {
-        k_grad_sm100<true><<<grid, GRAD_THREADS + DROP_EXTRA_THREADS, smem_bytes, st>>>(tmSrc, tmHm, g);
-    } else {
-        k_grad_sm100<false><<<grid, GRAD_THREADS, smem_bytes, st>>>(tmSrc, tmHm, g);
+        MARLAAS_LAUNCH_CHECK("k_grad_sm100");
+        return MARLAAS_OK;
     }
-    MARLAAS_LAUNCH_CHECK("k_grad_sm100");
-    return MARLAAS_OK;
+    return drop ? launch_link("k_grad_sm100", k_grad_sm100<true>, dim3((unsigned)grid), GRAD_THREADS + DROP_EXTRA_THREADS, smem_bytes, chained, st, tmSrc, tmHm, g)
+                : launch_link("k_grad_sm100", k_grad_sm100<false>, dim3((unsigned)grid), GRAD_THREADS, smem_bytes, chained, st, tmSrc, tmHm, g);
 }
 
 }  // namespace marlaas

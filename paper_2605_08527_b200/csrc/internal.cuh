@@ -311,10 +311,14 @@ marlaas_status_t launch_grad_reduce(const marlaas_pool* pool, int64_t C, const b
 
 // grad_sm100.cu: the same reductions on the tensor cores
 bool grad_sm100_eligible(const marlaas_pool* pool, int64_t T);
-marlaas_status_t launch_grad_plan(const marlaas_pool* pool, int64_t T, const Workspace& ws, cudaStream_t st);
+// chained (here and below): launched while the kernel before it in the stream still runs, it waits for that one's end
+marlaas_status_t launch_grad_plan(const marlaas_pool* pool, int64_t T, const Workspace& ws, cudaStream_t st, bool chained = false);
 // phases: build the masked hi/lo copies of the r-vectors into hm, reduce from hm, or both
 // GRAD_PHASE_EARLY: the reduction reads nothing the kernel before it in the stream writes and may start while that one ends
-enum { GRAD_PHASE_COPIES = 1, GRAD_PHASE_REDUCE = 2, GRAD_PHASE_EARLY = 4 };
+enum { GRAD_PHASE_COPIES = 1, GRAD_PHASE_REDUCE = 2, GRAD_PHASE_EARLY = 4, GRAD_PHASE_CHAINED = 8 };
+// the copies of one r-vector, or of two (r1 may be NULL)
+marlaas_status_t launch_grad_copies(const marlaas_pool* pool, int64_t T, const Workspace& ws, const float* r0, bf16* hm0, const float* r1, bf16* hm1,
+                                    bool chained, cudaStream_t st);
 marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t C, const bf16* src, int64_t ld,
                                    const float* hg, float* const* out_ptrs, float* const* host_ptrs, bool transpose_out,
                                    bool accumulate, const Workspace& ws, cudaStream_t st, bf16* hm, int phases = GRAD_PHASE_COPIES | GRAD_PHASE_REDUCE,
