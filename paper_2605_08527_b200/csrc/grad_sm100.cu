@@ -13,8 +13,8 @@
 // and writes the slot's gradient once.  If the batch interleaves tenants so finely that the copies would not
 // fit the workspace, a device flag routes the call to the CUDA-core reduction instead.
 //
-// For dA of the layer with dropout (DROP) the streamed rows of x are masked on their way: the four epilogue warps, idle until an
-// item's accumulator is there, and four more zero the dropped elements of every stage in shared memory before the MMA warp may use it.
+// For dA of the layer with dropout (DROP) the streamed rows of x are masked on their way: eight warps more zero the dropped elements
+// of every stage in shared memory before the MMA warp may use it.
 #include <string.h>
 
 #include "dropout.cuh"
@@ -27,6 +27,7 @@ constexpr int GRAD_THREADS = 192;
 constexpr int GRAD_STAGES = 4;          // at most: as many steps as fit the shared-memory budget (see the launch)
 constexpr int GRAD_BPS = 2;              // 64-token blocks per pipeline step: one barrier round trip and one commit for both
 constexpr int GRAD_INLINE_SLOTS = 64;
+constexpr int GRAD_MASK_THREADS = 256;   // DROP: warps that mask
 constexpr int GRAD_QN = 4;               // depth of the CTA's work-item queue
 constexpr uint32_t GB_STAGE_BYTES = 4 * CHUNK_BYTES;   // up to 256 columns of split r-vectors
 
@@ -213,7 +214,7 @@ struct GradArgs {
 };
 
 template <bool DROP>
-__global__ void __launch_bounds__(GRAD_THREADS + (DROP ? DROP_EXTRA_THREADS : 0), 1)
+__global__ void __launch_bounds__(GRAD_THREADS + (DROP ? GRAD_MASK_THREADS : 0), 1)
 k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ CUtensorMap tmHm, const GradArgs g) {
     constexpr int MAX_STAGES = GRAD_STAGES;
     const int STAGES = g.stages;
@@ -242,6 +243,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * MAX_STAGES + 5 + 2 * GRAD_QN);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
     __shared__ int s_cnt[256], s_order[256];
+    __shared__ uint32_t s_limit[DROP ? 256 : 1];
     __shared__ volatile int s_q[GRAD_QN];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -260,7 +262,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
         mbar_init(bar_drain, 1);
         for (int i = 0; i < GRAD_QN; ++i) {
             mbar_init(bar_qfull + 8 * i, 1);
-            mbar_init(bar_qempty + 8 * i, DROP ? 9 : 5);     // the MMA thread and the epilogue (and masking) warps
+            mbar_init(bar_qempty + 8 * i, DROP ? 13 : 5);     // the MMA thread and the epilogue (and masking) warps
         }
         *abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -277,6 +279,8 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
     // Work items are handed out dynamically, heaviest tenants first (an item's cost is its tenant's copy count), so that
     // skewed batches still finish together; which CTA computes an item does not change its value.
     for (int t = threadIdx.x; t < g.cap; t += blockDim.x) s_cnt[t] = ((g.out_ptrs ? g.out_ptrs[t] : g.inl[t]) != nullptr && g.d_rank[t] > 0) ? g.ten_nblk[t] : -1;
+    if (DROP)
+        for (int t = threadIdx.x; t < g.cap; t += blockDim.x) s_limit[t] = drop_limit(g.drop.rates[t]);
     tc_fence_before();
     __syncthreads();
     for (int t = threadIdx.x; t < g.cap; t += blockDim.x) {
@@ -392,12 +396,59 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
             }
         }
         __syncwarp();
+    } else if (DROP && warp >= 6) {
+        // ---- masks.  The rows of a block's other tenants are masked as the copy's own: their r-vectors are zeros there.
+        const int mw = warp - 6, tl = (mw & 1) * 32 + lane, tc = (mw >> 1) & 1, v0 = (mw >> 2) * 4;    // token row, column chunk, first vector of four
+        bool ok = true;
+        uint32_t qi = 0, es = 0, eph = 0;     // stage and phase of the next step
+        while (ok) {
+            const uint32_t qs = qi % GRAD_QN, qph = (qi / GRAD_QN) & 1;
+            ok = mbar_wait(bar_qfull + 8 * qs, qph, abort_word, 29);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const int item = s_q[qs];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_qempty + 8 * qs);
+            ++qi;
+            if (item < 0) break;
+            int t, c0;
+            const int nb = item_blocks(item, t, c0);
+            const uint32_t limit = nb > 0 ? s_limit[t] : 0u;
+            const bool on = limit != 0 && c0 + tc * 64 < g.C;
+            const int32_t* blks = g.ten_blks + (size_t)t * g.nblk;
+            for (int k = 0; k < nb; k += GRAD_BPS) {
+                const int nj = min(GRAD_BPS, nb - k);
+                int blk[GRAD_BPS];
+#pragma unroll
+                for (int j = 0; j < GRAD_BPS; ++j) blk[j] = on && j < nj ? blks[k + j] : 0;
+                ok = mbar_wait(bar_full + 8 * es, eph, abort_word, 30);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (on) {
+#pragma unroll
+                    for (int j = 0; j < GRAD_BPS; ++j) {
+                        if (j >= nj) break;
+                        uint8_t* rows = smem + es * A_STEP + j * A_STAGE_BYTES + tc * CHUNK_BYTES + tl * 128;
+#pragma unroll
+                        for (int v4 = 0; v4 < 4; ++v4) {
+                            const int v = v0 + v4;
+                            uint4* at = reinterpret_cast<uint4*>(rows + ((v ^ (tl & 7)) << 4));
+                            *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((c0 + tc * 64) / 8 + v), (uint32_t)(blk[j] * 64 + tl)), limit);
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_ready + 8 * es);
+                if (++es == (uint32_t)STAGES) { es = 0; eph ^= 1; }
+            }
+        }
     } else {
         // ---- epilogue: out = s_t * (hi part + lo part)
         const int q = warp & 3;
         uint32_t lt = 0;
         bool ok = true;
-        uint32_t qi = 0, es = 0, eph = 0;     // DROP: stage and phase of the next step to mask
+        uint32_t qi = 0;
         while (ok) {
             const uint32_t qs = qi % GRAD_QN, qph = (qi / GRAD_QN) & 1;
             ok = mbar_wait(bar_qfull + 8 * qs, qph, abort_word, 29);
@@ -415,42 +466,12 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
             const int r = g.d_rank[t];
             const int c = c0 + q * 32 + lane;
             if (nb == 0) {   // tenant without tokens: exact zeros unless accumulating
-                if (!g.accumulate && c < g.C && (!DROP || warp < 6))
+                if (!g.accumulate && c < g.C)
                     for (int j = 0; j < r; ++j) {
                         if (g.transpose_out) out[(size_t)c * r + j] = 0.f;
                         else out[(size_t)j * g.C + c] = 0.f;
                     }
                 continue;
-            }
-            if (DROP) {
-                // thread: token row tl of each block, columns of chunk tc
-                const int tl = (q * 32 + lane) & 63, tc = (q * 32 + lane) >> 6;
-                for (int k = 0; k < nb; k += GRAD_BPS) {
-                    ok = mbar_wait(bar_full + 8 * es, eph, abort_word, 30);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    const int nj = min(GRAD_BPS, nb - k);
-                    for (int j = 0; j < nj; ++j) {
-                        const int i = g.ten_blks[(size_t)t * g.nblk + k + j] * 64 + tl;
-                        const int slot = i < g.T ? g.drop.tok_slot[i] : -1;
-                        const uint32_t limit = slot >= 0 ? drop_limit(g.drop.rates[slot]) : 0u;
-                        if (__any_sync(0xffffffffu, limit != 0) && c0 + tc * 64 < g.C) {
-                            uint8_t* rows = smem + es * A_STEP + j * A_STAGE_BYTES + tc * CHUNK_BYTES + tl * 128;
-#pragma unroll
-                            for (int v4 = 0; v4 < 4; ++v4) {
-                                const int v = v4 + (warp >= 6 ? 4 : 0);
-                                uint4* at = reinterpret_cast<uint4*>(rows + ((v ^ (tl & 7)) << 4));
-                                *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((c0 + tc * 64) / 8 + v), (uint32_t)i), limit);
-                            }
-                        }
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar_ready + 8 * es);
-                    if (++es == (uint32_t)STAGES) { es = 0; eph ^= 1; }
-                }
-                if (!ok) break;
-                if (warp >= 6) continue;
             }
             const float sc = g.d_scale[t];
             const uint32_t b = lt & 1, aph = (lt >> 1) & 1;
@@ -619,7 +640,7 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
         MARLAAS_LAUNCH_CHECK("k_grad_sm100");
         return MARLAAS_OK;
     }
-    return drop ? launch_link("k_grad_sm100", k_grad_sm100<true>, dim3((unsigned)grid), GRAD_THREADS + DROP_EXTRA_THREADS, smem_bytes, chained, st, tmSrc, tmHm, g)
+    return drop ? launch_link("k_grad_sm100", k_grad_sm100<true>, dim3((unsigned)grid), GRAD_THREADS + GRAD_MASK_THREADS, smem_bytes, chained, st, tmSrc, tmHm, g)
                 : launch_link("k_grad_sm100", k_grad_sm100<false>, dim3((unsigned)grid), GRAD_THREADS, smem_bytes, chained, st, tmSrc, tmHm, g);
 }
 
