@@ -397,7 +397,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
         }
         __syncwarp();
     } else if (DROP && warp >= 6) {
-        // ---- masks.  The rows of a block's other tenants are masked as the copy's own: their r-vectors are zeros there.
+        // ---- masks.  A block's rows of other tenants become zeros: what they hold does not reach this tenant's sums.
         const int mw = warp - 6, tl = (mw & 1) * 32 + lane, tc = (mw >> 1) & 1, v0 = (mw >> 2) * 4;    // token row, column chunk, first vector of four
         bool ok = true;
         uint32_t qi = 0, es = 0, eph = 0;     // stage and phase of the next step
@@ -414,26 +414,28 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
             int t, c0;
             const int nb = item_blocks(item, t, c0);
             const uint32_t limit = nb > 0 ? s_limit[t] : 0u;
-            const bool on = limit != 0 && c0 + tc * 64 < g.C;
             const int32_t* blks = g.ten_blks + (size_t)t * g.nblk;
             for (int k = 0; k < nb; k += GRAD_BPS) {
                 const int nj = min(GRAD_BPS, nb - k);
-                int blk[GRAD_BPS];
+                uint32_t row[GRAD_BPS], lim[GRAD_BPS];
 #pragma unroll
-                for (int j = 0; j < GRAD_BPS; ++j) blk[j] = on && j < nj ? blks[k + j] : 0;
+                for (int j = 0; j < GRAD_BPS; ++j) {        // (on their way while the stage's copies are)
+                    row[j] = j < nj ? (uint32_t)blks[k + j] * 64 + tl : 0u;
+                    lim[j] = j < nj && row[j] < (uint32_t)g.T && g.drop.tok_slot[row[j]] == t ? limit : 65536u;
+                }
                 ok = mbar_wait(bar_full + 8 * es, eph, abort_word, 30);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (on) {
+                if (c0 + tc * 64 < g.C) {
 #pragma unroll
                     for (int j = 0; j < GRAD_BPS; ++j) {
-                        if (j >= nj) break;
+                        if (j >= nj || !__any_sync(0xffffffffu, lim[j] != 0)) continue;
                         uint8_t* rows = smem + es * A_STEP + j * A_STAGE_BYTES + tc * CHUNK_BYTES + tl * 128;
 #pragma unroll
                         for (int v4 = 0; v4 < 4; ++v4) {
                             const int v = v0 + v4;
                             uint4* at = reinterpret_cast<uint4*>(rows + ((v ^ (tl & 7)) << 4));
-                            *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((c0 + tc * 64) / 8 + v), (uint32_t)(blk[j] * 64 + tl)), limit);
+                            *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((c0 + tc * 64) / 8 + v), row[j]), lim[j]);
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
