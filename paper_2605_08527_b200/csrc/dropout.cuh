@@ -43,7 +43,8 @@ __device__ __forceinline__ uint4 drop_apply(uint4 x, const uint4& bits, uint32_t
     return x;
 }
 
-// Threads of a kernel whose streamed rows are masked in shared memory: four warps beside the four that also write its results.
+// Threads more in a shrink kernel whose streamed rows are masked in shared memory: four warps, beside the four that also write its
+// results.
 constexpr int DROP_EXTRA_THREADS = 128;
 
 }  // namespace marlaas

@@ -14,7 +14,8 @@
 // fit the workspace, a device flag routes the call to the CUDA-core reduction instead.
 //
 // For dA of the layer with dropout (DROP) the streamed rows of x are masked on their way: eight warps more zero the dropped elements
-// of every stage in shared memory before the MMA warp may use it.
+// of every stage in shared memory before the MMA warp may use it, and the rows of the block's other tenants (8192 x 4096, 32 tenants
+// of rank 16: 37 us against 30 without masks; with the epilogue's warps doing half of it 48).
 #include <string.h>
 
 #include "dropout.cuh"
@@ -397,7 +398,8 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
         }
         __syncwarp();
     } else if (DROP && warp >= 6) {
-        // ---- masks.  A block's rows of other tenants become zeros: what they hold does not reach this tenant's sums.
+        // ---- masks.  Rows whose r-vector is zeros, those of the block's other tenants, become zeros: what they hold does not reach
+        // this tenant's sums.
         const int mw = warp - 6, tl = (mw & 1) * 32 + lane, tc = (mw >> 1) & 1, v0 = (mw >> 2) * 4;    // token row, column chunk, first vector of four
         bool ok = true;
         uint32_t qi = 0, es = 0, eph = 0;     // stage and phase of the next step
@@ -417,25 +419,37 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
             const int32_t* blks = g.ten_blks + (size_t)t * g.nblk;
             for (int k = 0; k < nb; k += GRAD_BPS) {
                 const int nj = min(GRAD_BPS, nb - k);
-                uint32_t row[GRAD_BPS], lim[GRAD_BPS];
+                int blk[GRAD_BPS];
 #pragma unroll
-                for (int j = 0; j < GRAD_BPS; ++j) {        // (on their way while the stage's copies are)
-                    row[j] = j < nj ? (uint32_t)blks[k + j] * 64 + tl : 0u;
-                    lim[j] = j < nj && row[j] < (uint32_t)g.T && g.drop.tok_slot[row[j]] == t ? limit : 65536u;
-                }
+                for (int j = 0; j < GRAD_BPS; ++j) blk[j] = j < nj ? blks[k + j] : 0;       // (on its way while the stage's copies are)
                 ok = mbar_wait(bar_full + 8 * es, eph, abort_word, 30);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (c0 + tc * 64 < g.C) {
 #pragma unroll
                     for (int j = 0; j < GRAD_BPS; ++j) {
-                        if (j >= nj || !__any_sync(0xffffffffu, lim[j] != 0)) continue;
-                        uint8_t* rows = smem + es * A_STEP + j * A_STAGE_BYTES + tc * CHUNK_BYTES + tl * 128;
+                        if (j >= nj) break;
+                        const uint8_t* r_row = smem + (sB - sA) + es * B_STEP + j * B_BLOCK + tl * 128;
+                        uint32_t bits = 0;
+                        for (int v = 0; v < g.RP / 8; v += 2) {
 #pragma unroll
-                        for (int v4 = 0; v4 < 4; ++v4) {
-                            const int v = v0 + v4;
-                            uint4* at = reinterpret_cast<uint4*>(rows + ((v ^ (tl & 7)) << 4));
-                            *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((c0 + tc * 64) / 8 + v), row[j]), lim[j]);
+                            for (int e = 0; e < 2; ++e) {
+                                const uint4 h = *reinterpret_cast<const uint4*>(r_row + (v >> 3) * CHUNK_BYTES + ((((v + e) & 7) ^ (tl & 7)) << 4));
+                                bits |= h.x | h.y | h.z | h.w;
+                            }
+                        }
+                        const uint32_t lim = bits == 0 ? 65536u : limit;
+                        uint8_t* rows = smem + es * A_STEP + j * A_STAGE_BYTES + tc * CHUNK_BYTES + tl * 128;
+                        if (limit != 0) {
+#pragma unroll
+                            for (int v4 = 0; v4 < 4; ++v4) {
+                                const int v = v0 + v4;
+                                uint4* at = reinterpret_cast<uint4*>(rows + ((v ^ (tl & 7)) << 4));
+                                *at = drop_apply(*at, drop_bits(g.drop.key, (uint32_t)((c0 + tc * 64) / 8 + v), (uint32_t)(blk[j] * 64 + tl)), lim);
+                            }
+                        } else if (lim != 0) {
+#pragma unroll
+                            for (int v4 = 0; v4 < 4; ++v4) *reinterpret_cast<uint4*>(rows + (((v0 + v4) ^ (tl & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
