@@ -162,3 +162,42 @@ def test_everything_at_once_on_two_streams(pool):
     assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
     B.marlaas_check_status(pool)
     B.marlaas_check_status(c.pool)
+
+
+@pytest.mark.parametrize("T,d,V", [(33, 65536, 264), (2, 64, B.MARLAAS_MAX_VOCABULARY), (260, 8, 9)])
+def test_head_at_its_largest(T, d, V):
+    pool = B.AdapterPool(64, 64, 8, head.CAP)
+    head.test_loss_and_gradient(pool, T, d, V)
+
+
+@pytest.mark.parametrize("T,K,N,ranks,S,cap", [(5, 98312, 64, [8, 16], 3, None), (600, 128, 256, [8, 16], 9, 300), (300, 128, 256, [8, 16], 9, 300),
+                                               (515, 8, 8, [128], 4, None), (2, 4096, 16, [128, 1], 2, None)])
+def test_dropout_at_its_largest(T, K, N, ranks, S, cap):
+    c = drop.Case(T, K, N, ranks, S, T + K + N, cap=cap)
+    drop.check_case(c, c.keep())
+
+
+@pytest.mark.parametrize("T", [40, 700])
+def test_dropout_without_any_adapter(T):
+    """Slots of rank 0, and a batch of the base model alone: the plain layer's products, each a sum in its own order
+    (2^-23 (n / 16 + 2) of the magnitudes) rounded once (2^-8)."""
+    def near(a, b, x, W):
+        size = x.double().abs() @ W.double().abs()
+        assert torch.all((a.double() - b.double()).abs() <= 2 * (2.0 ** -23 * (x.shape[1] / 16 + 2) * size + 2.0 ** -8 * 1.01 * b.double().abs()))
+
+    for ranks, on in (([0, 0], True), ([8, 16], False)):
+        c = drop.Case(T, 128, 256, ranks, 4, 41)
+        if not on:
+            c.slot = [-1] * 4
+            c.tok = [-1] * T
+            c.seg = drop.segments(c.off, c.slot)
+        y, h = c.forward()
+        assert not h.any()
+        plain = torch.empty_like(y)
+        B.marlaas_lora_forward(c.pool, c.x, c.W, c.seg, y=plain)
+        near(y, plain, c.x, c.W)
+        dx, dA, dB = c.backward(h)
+        back = torch.empty_like(dx)
+        B.marlaas_lora_backward(c.pool, c.x, c.W, c.dy, c.seg, dx=back)
+        near(dx, back, c.dy, c.W.T)
+        assert all(g is None or not g.any() for g in dA + dB)
