@@ -308,6 +308,7 @@ class AdapterPool:
         self._workspaces = {}
         self._captured_workspaces = []
         self._policy_last = None
+        self._step_bytes = {}               # workspace sizes of calls around the layer, by their sizes
         self._store = None
 
     def close(self):
@@ -357,14 +358,19 @@ class AdapterPool:
         self._policy_last = (key, ws)
         return ws
 
-    def step_workspace(self, need: int, handle: int) -> torch.Tensor:
-        """At least `need` bytes of scratch for the calls around a training step's layers, cached per stream (`handle`: the pool's
-        device's current one).  A call that is being captured gets one of its own from the graph's memory."""
+    def step_workspace(self, handle: int, workspace_bytes, *sizes) -> torch.Tensor:
+        """Scratch for the calls around a training step's layers, at least workspace_bytes(self, *sizes), cached per stream (`handle`:
+        the pool's device's current one).  A call that is being captured gets one of its own from the graph's memory."""
+        need = self._step_bytes.get((workspace_bytes, sizes))
+        if need is None:
+            if len(self._step_bytes) >= 4096:
+                self._step_bytes.clear()
+            need = self._step_bytes[workspace_bytes, sizes] = max(workspace_bytes(self, *sizes), 256)
         if torch._C._cuda_isCurrentStreamCapturing():
-            return torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            return torch.empty(need, dtype=torch.uint8, device=self.device)
         ws = self._workspaces.get(("step", handle))
         if ws is None or ws.numel() < need:
-            ws = self._workspaces[("step", handle)] = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            ws = self._workspaces[("step", handle)] = torch.empty(need, dtype=torch.uint8, device=self.device)
         return ws
 
     def store(self):
@@ -812,7 +818,7 @@ def marlaas_lora_forward_dropout(pool: AdapterPool, x: torch.Tensor, W: torch.Te
     T, dev = x.shape[0], pool.index
     y = torch.empty((T, pool.d_out), dtype=torch.bfloat16, device=x.device) if y is None else y
     handle = torch._C._cuda_getCurrentRawStream(dev)
-    ws = pool.step_workspace(marlaas_lora_dropout_workspace_bytes(pool, T), handle) if workspace is None else workspace
+    ws = pool.step_workspace(handle, marlaas_lora_dropout_workspace_bytes, T) if workspace is None else workspace
     drop = _drop(pool, rates, seed, offset)
     _check(load_library().marlaas_lora_forward_dropout(
         pool.handle, T, x.data_ptr(), _bf16_rows(x, T, pool.d_in, "x", dev), W.data_ptr(), _bf16_rows(W, pool.d_in, pool.d_out, "W", dev),
@@ -832,7 +838,7 @@ def marlaas_lora_backward_dropout(pool: AdapterPool, x: Optional[torch.Tensor], 
         return _on_stream(stream, marlaas_lora_backward_dropout, pool, x, W, dy, seg, rates, seed, offset, dx, dA, dB, h_saved, workspace, flags)
     T, dev = dy.shape[0], pool.index
     handle = torch._C._cuda_getCurrentRawStream(dev)
-    ws = pool.step_workspace(marlaas_lora_dropout_workspace_bytes(pool, T), handle) if workspace is None else workspace
+    ws = pool.step_workspace(handle, marlaas_lora_dropout_workspace_bytes, T) if workspace is None else workspace
     drop = _drop(pool, rates, seed, offset)
     _check(load_library().marlaas_lora_backward_dropout(
         pool.handle, T, None if x is None else x.data_ptr(), 0 if x is None else _bf16_rows(x, T, pool.d_in, "x", dev), W.data_ptr(),
@@ -862,7 +868,7 @@ def marlaas_layer_norm(pool: AdapterPool, x: torch.Tensor, seg: Segments, gain: 
     handle = torch._C._cuda_getCurrentRawStream(dev)
     ws = workspace
     if ws is None and seg.on_host:
-        ws = pool.step_workspace(marlaas_layer_norm_workspace_bytes(pool, T, d, seg.num_segments, False), handle)
+        ws = pool.step_workspace(handle, marlaas_layer_norm_workspace_bytes, T, d, seg.num_segments, False)
     params = (pool.capacity + 1) * d
     _check(load_library().marlaas_layer_norm(
         pool.handle, T, d, x.data_ptr(), _bf16_rows(x, T, d, "x", dev), seg.ref, _f32(gain, params, "gain", dev),
@@ -884,7 +890,7 @@ def marlaas_layer_norm_backward(pool: AdapterPool, x: torch.Tensor, dy: torch.Te
     handle = torch._C._cuda_getCurrentRawStream(dev)
     ws = workspace
     if ws is None:
-        ws = pool.step_workspace(marlaas_layer_norm_workspace_bytes(pool, T, d, seg.num_segments, True), handle)
+        ws = pool.step_workspace(handle, marlaas_layer_norm_workspace_bytes, T, d, seg.num_segments, True)
     _check(load_library().marlaas_layer_norm_backward(
         pool.handle, T, d, x.data_ptr(), _bf16_rows(x, T, d, "x", dev), dy.data_ptr(), _bf16_rows(dy, T, d, "dy", dev), seg.ref,
         _f32(gain, params, "gain", dev), None if mean is None else _f32(mean, T, "mean", dev), _f32(rstd, T, "rstd", dev),
@@ -918,7 +924,7 @@ def marlaas_head_cross_entropy(pool: AdapterPool, x: torch.Tensor, W: torch.Tens
     handle = torch._C._cuda_getCurrentRawStream(dev)
     ws = workspace
     if ws is None:
-        ws = pool.step_workspace(marlaas_head_cross_entropy_workspace_bytes(pool, T, d, V, S, dx is not None), handle)
+        ws = pool.step_workspace(handle, marlaas_head_cross_entropy_workspace_bytes, T, d, V, S, dx is not None)
     _check(load_library().marlaas_head_cross_entropy(
         pool.handle, T, d, V, x.data_ptr(), _bf16_rows(x, T, d, "x", dev), W.data_ptr(), _bf16_rows(W, d, V, "W", dev),
         _i32(targets, T, "targets", dev), None if seg is None else seg.ref, None if weight is None else _f32(weight, T, "weight", dev),

@@ -111,6 +111,27 @@ __device__ __forceinline__ void group_sum4(float (&v)[4], GroupSums& s, int& par
     for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xffffffffu, x, 8 * i);
 }
 
+// The segment of token i, a.S for a token that an ill-formed table leaves out.
+__device__ __forceinline__ int segment_of(const NormArgs& a, int i) {
+    int lo = 0, hi = a.S;
+    while (lo < hi) {
+        const int m = (lo + hi) >> 1;
+        if (a.off[m + 1] > i) hi = m; else lo = m + 1;
+    }
+    return lo;
+}
+__device__ __forceinline__ int norm_slot(const NormArgs& a, int seg) {
+    const int t = seg < a.S ? a.slot[seg] : -1;
+    return t < 0 || t >= a.cap ? a.cap : t;
+}
+__device__ __forceinline__ void check_table(const NormArgs& a) {
+    for (int64_t s = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; s < a.S; s += (int64_t)gridDim.x * blockDim.x) {
+        const int p = a.off[s], q = a.off[s + 1], t = a.slot[s];
+        if (q < p || p < 0 || q > a.T || (s == 0 && p != 0) || (s == a.S - 1 && q != a.T)) dk_report(a.status, DEV_BAD_TABLE, (int)s);
+        if (t < -1 || t >= a.cap) dk_report(a.status, DEV_BAD_INDEX, (int)s);
+    }
+}
+
 // ---- forward ----
 template <int NV, int B, int STAGES, int THREADS, int PER_SM, bool RMS>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs a, int W, int G) {
@@ -119,11 +140,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = warp / W, wg = warp % W, l = wg * 32 + lane;
     const int nvec = a.d / 8;
     const float inv_d = 1.f / (float)a.d;
-    for (int64_t s = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; s < a.S; s += (int64_t)gridDim.x * blockDim.x) {
-        const int p = a.off[s], q = a.off[s + 1], t = a.slot[s];
-        if (q < p || p < 0 || q > a.T || (s == 0 && p != 0) || (s == a.S - 1 && q != a.T)) dk_report(a.status, DEV_BAD_TABLE, (int)s);
-        if (t < -1 || t >= a.cap) dk_report(a.status, DEV_BAD_INDEX, (int)s);
-    }
+    check_table(a);
     const int64_t first = ((int64_t)blockIdx.x * G + g) * a.rows_per_group;
     if (first >= a.T) return;                   // (a group synchronises with itself alone)
     const int n = (int)min(a.rows_per_group, a.T - first);      // rows of the group
@@ -159,22 +176,13 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
     auto next_tenant = [&](int r) {             // the segment of the group's row r: the next one, or else looked for; its parameters
         const int i = (int)first + r;
         int lo = seg + 1;
-        if (seg < 0 || lo >= a.S || a.off[lo] > i || a.off[lo + 1] <= i) {
-            lo = 0;
-            int hi = a.S;
-            while (lo < hi) {
-                const int m = (lo + hi) >> 1;
-                if (a.off[m + 1] > i) hi = m; else lo = m + 1;
-            }
-        }
-        int t = a.cap;
+        if (seg < 0 || lo >= a.S || a.off[lo] > i || a.off[lo + 1] <= i) lo = segment_of(a, i);
         seg_end = r + 1;
         if (lo < a.S) {
             seg = lo;
             seg_end = (int)min((int64_t)n, (int64_t)a.off[lo + 1] - first);
-            t = a.slot[lo];
-            if (t < 0 || t >= a.cap) t = a.cap;
         }
+        const int t = norm_slot(a, lo);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const size_t c = (size_t)t * a.d + at[j] / 2;
@@ -251,7 +259,8 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
 // ---- backward ----
 // The rows are taken in the order of their tenants.  The sums of a (group, tenant) pair go to partial[group + tenant]: both only
 // rise along the ordered tokens, so no two pairs share a place, and the order of all additions depends on the sizes and the
-// table alone.
+// table alone.  A batch of few segments is taken as it comes (perm = NULL), without the launches that order it: the sums of a
+// (group, segment) pair go to partial[group + segment], for the same reason.
 template <int NV, int B, int STAGES, int THREADS, int PER_SM, bool RMS>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArgs a, int W, int G) {
     // four vectors per lane leave no registers for the gains: each thread keeps its own behind the ring
@@ -265,9 +274,10 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
     const int64_t q = (int64_t)blockIdx.x * G + g, first = q * a.rows_per_group;
     sm100::dk_wait_prerequisites();
     sm100::dk_launch_dependents();
+    const bool ordered = a.perm != nullptr;
+    if (!ordered) check_table(a);
     if (first >= a.T) return;
     const int n = (int)min(a.rows_per_group, a.T - first);
-    const int32_t* perm = a.perm + first;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
     bool mine[NV];
     uint32_t at[NV];                            // a lane's bytes of a row
@@ -300,7 +310,10 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
     int tok[STAGES][B];
     auto tokens = [&](int (&t)[B], int r) {
 #pragma unroll
-        for (int b = 0; b < B; ++b) t[b] = perm[min(r + b, n - 1)];
+        for (int b = 0; b < B; ++b) {
+            t[b] = (int)first + min(r + b, n - 1);
+            if (ordered) t[b] = a.perm[t[b]];
+        }
     };
 #pragma unroll
     for (int u = 0; u < STAGES; ++u) tokens(tok[u], u * B);
@@ -316,7 +329,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
     moments(tok[0]);
 #pragma unroll
     for (int u = 0; u < STAGES - 1; ++u) fetch(tok[u], u * B, u);
-    int key = -1, par = 0, st = 0, key_end = 0;     // key_end: the group's first row of a later tenant
+    int key = -1, par = 0, st = 0, key_end = 0;     // the tenant, or the segment; key_end: the group's first row of a later one
     float2 gain_kept[GAIN_SHARED ? 1 : NV][4], sg[NV][4], sb[NV][4];
     auto flush = [&]() {
         float* out = a.partial + (size_t)(q + key) * 2 * a.d;
@@ -335,7 +348,8 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
             }
         }
     };
-    auto load_gain = [&](int t) {
+    auto load_gain = [&](int k) {
+        const int t = ordered ? k : norm_slot(a, k);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float2 w[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
@@ -360,7 +374,13 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
         }
     };
     auto next_tenant = [&](int r) {             // the next tenant that has tokens; its gain, and sums of 0
-        do key_end = (int)min((int64_t)n, a.key_off[++key + 1] - first); while (key_end <= r);
+        if (ordered) {
+            do key_end = (int)min((int64_t)n, a.key_off[++key + 1] - first); while (key_end <= r);
+        } else {
+            // (tokens that an ill-formed table leaves out are a segment behind the last one)
+            key = segment_of(a, (int)first + r);
+            key_end = key < a.S ? (int)min((int64_t)n, a.off[key + 1] - first) : n;
+        }
         load_gain(key);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -381,7 +401,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
             if (key >= 0 && a.partial) flush();
             next_tenant(r);
         }
-        const int key0 = key;                   // (the batch's second row may be the next tenant's)
+        const int key0 = key;                   // (the batch's second row may be the next one's)
         copy_wait<STAGES - 1>();
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         float2 x[4], dy[4], gain[4];
@@ -444,47 +464,78 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
     if (a.partial) flush();
 }
 
-// dgain and dbias of one tenant, 128 columns per CTA, four per lane: the warps share the tenant's partial sums, four at a time on
-// their way, then add up in their order.
+// dgain and dbias of one tenant, 128 columns per CTA, four per lane: the warps share the tenant's partial sums, then add up in their
+// order.
 __global__ void __launch_bounds__(1024) k_norm_reduce(const NormArgs a) {
-    __shared__ float4 s_sum[2][32][32];
-    const int key = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, c = blockIdx.x * 128 + lane * 4;
-    sm100::dk_wait_prerequisites();
-    const int64_t b = a.key_off[key], e = a.key_off[key + 1];
+    extern __shared__ float4 s_sum[];           // [2][warps][32], then a range per thread
+    __shared__ int s_warp[32];
+    int2* const s_range = reinterpret_cast<int2*>(s_sum + 2 * blockDim.x);
+    const int key = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5, c = blockIdx.x * 128 + lane * 4;
+    const int rows = (int)a.rows_per_group;
     float4 g = make_float4(0.f, 0.f, 0.f, 0.f), h = g;
-    if (e > b) {
+    int seen = 0;                               // places before the present range
+    auto add = [&](int from, int to) {
         if (c < a.d) {
-            const int q0 = (int)(b / a.rows_per_group), q1 = (int)((e - 1) / a.rows_per_group);
-            const float* in = a.partial + (size_t)key * 2 * a.d + c;
 #pragma unroll 4
-            for (int q = q0 + warp; q <= q1; q += warps) {
-                const float4 x = *reinterpret_cast<const float4*>(in + (size_t)q * 2 * a.d);
+            for (int q = from + (warp + seen) % warps; q < to; q += warps) {
+                const float* in = a.partial + (size_t)q * 2 * a.d + c;
+                const float4 x = *reinterpret_cast<const float4*>(in);
                 g.x += x.x; g.y += x.y; g.z += x.z; g.w += x.w;
                 if (a.dbias) {
-                    const float4 y = *reinterpret_cast<const float4*>(in + (size_t)q * 2 * a.d + a.d);
+                    const float4 y = *reinterpret_cast<const float4*>(in + a.d);
                     h.x += y.x; h.y += y.y; h.z += y.z; h.w += y.w;
                 }
             }
         }
-        s_sum[0][warp][lane] = g;
-        s_sum[1][warp][lane] = h;
+        seen += to - from;
+    };
+    if (a.perm) {
+        sm100::dk_wait_prerequisites();
+        const int b = a.key_off[key], e = a.key_off[key + 1];
+        if (e > b) add(b / rows + key, (e - 1) / rows + key + 1);
+    } else {
+        // the tenant's segments, and what lies behind the last one
+        for (int s0 = 0; s0 <= a.S; s0 += blockDim.x) {
+            const int s = s0 + tid;
+            int b = 0, e = 0;
+            if (s <= a.S && norm_slot(a, s) == key) {
+                b = s == 0 ? 0 : max(0, a.off[s]);
+                e = s < a.S ? min((int)a.T, a.off[s + 1]) : (int)a.T;
+            }
+            const unsigned bal = __ballot_sync(0xffffffffu, e > b);
+            if (lane == 0) s_warp[warp] = __popc(bal);
+            __syncthreads();
+            int at = __popc(bal & ((1u << lane) - 1u)), n = 0;
+            for (int w = 0; w < warps; ++w) {
+                at += w < warp ? s_warp[w] : 0;
+                n += s_warp[w];
+            }
+            if (e > b) s_range[at] = make_int2(b / rows + s, (e - 1) / rows + s + 1);
+            __syncthreads();
+            sm100::dk_wait_prerequisites();
+            for (int k = 0; k < n; ++k) add(s_range[k].x, s_range[k].y);
+        }
+    }
+    if (seen > 0) {
+        s_sum[tid] = g;
+        s_sum[blockDim.x + tid] = h;
         __syncthreads();
     }
     if (warp >= 2 || c >= a.d) return;
     float* out = warp == 0 ? a.dgain : a.dbias;
     if (!out) return;
-    float4* to = reinterpret_cast<float4*>(out + (size_t)key * a.d + c);
+    float4* dst = reinterpret_cast<float4*>(out + (size_t)key * a.d + c);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (e > b)
+    if (seen > 0)
         for (int w = 0; w < warps; ++w) {
-            const float4 x = s_sum[warp][w][lane];
+            const float4 x = s_sum[(warp * warps + w) * 32 + lane];
             v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
         }
     if (a.accumulate) {
-        const float4 x = *to;
+        const float4 x = *dst;
         v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
     }
-    *to = v;
+    *dst = v;
 }
 
 // How a pass cuts a batch: vectors per lane, warps per row and rows of a CTA at a time, groups in all and their rows.
@@ -509,10 +560,14 @@ static NormPlan norm_plan(const marlaas_pool* pool, int64_t T, int d, bool backw
     return p;
 }
 
+// Whether backward takes a batch as it comes.  Each segment then costs sums of its own, 8 bytes per column to write and to read
+// again, where the order costs three launches in a row, about 12 us or 60 MB (8000 x 1600 in 62 segments: 34 us as it comes, 41 ordered).
+static bool norm_as_it_comes(int64_t d, int32_t S) { return S <= 8192 && 16 * d * S <= 60000000; }
+
 struct NormWorkspace {
     int32_t* off;           // [S + 1] host tables
     int32_t* slot;          // [S]
-    int32_t* perm;          // [T]
+    int32_t* perm;          // [T]; these three for batches that are ordered
     int32_t* key_off;       // [cap + 2]
     int32_t* scratch;
     float* partial;
@@ -528,10 +583,13 @@ static NormWorkspace carve_norm(const marlaas_pool* pool, int64_t T, int32_t S, 
     w.slot = (int32_t*)take(sizeof(int32_t) * (size_t)S);
     if (backward) {
         const NormPlan n = norm_plan(pool, T, (int)d, true);
-        w.perm = (int32_t*)take(sizeof(int32_t) * (size_t)T);
-        w.key_off = (int32_t*)take(sizeof(int32_t) * ((size_t)pool->cap + 2));
-        w.scratch = (int32_t*)take(sizeof(int32_t) * order_scratch_ints(T, pool->cap + 1));
-        w.partial = (float*)take(sizeof(float) * (size_t)(n.groups + pool->cap + 1) * 2 * (size_t)d);
+        const bool ordered = !norm_as_it_comes(d, S);
+        if (ordered) {
+            w.perm = (int32_t*)take(sizeof(int32_t) * (size_t)T);
+            w.key_off = (int32_t*)take(sizeof(int32_t) * ((size_t)pool->cap + 2));
+            w.scratch = (int32_t*)take(sizeof(int32_t) * order_scratch_ints(T, pool->cap + 1));
+        }
+        w.partial = (float*)take(sizeof(float) * (size_t)(n.groups + (ordered ? pool->cap : S) + 1) * 2 * (size_t)d);
     }
     w.total_bytes = o;
     return w;
@@ -563,7 +621,7 @@ static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& 
     cfg.dynamicSmemBytes = (backward ? bwd : fwd) * THREADS;
     cfg.stream = st;
     cfg.attrs = at;
-    cfg.numAttrs = backward ? 1 : 0;
+    cfg.numAttrs = a.perm ? 1 : 0;
     MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, backward ? kb : kf, a, n.W, n.G));
     MARLAAS_LAUNCH_CHECK(backward ? "k_norm_backward" : "k_norm_forward");
     return MARLAAS_OK;
@@ -706,16 +764,20 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
     a.partial = dgain || dbias ? ws.partial : nullptr;
     a.dgain = dgain; a.dbias = dbias; a.accumulate = accumulate ? 1 : 0;
     if (host && (rc = stage_table(seg, ws, &a, st)) != MARLAAS_OK) return rc;
-    OrderArgs o;
-    memset(&o, 0, sizeof(o));
-    o.T = T; o.S = a.S; o.off = a.off; o.slot = a.slot; o.cap = pool->cap; o.nkeys = pool->cap + 1;
-    o.perm = ws.perm; o.key_off = ws.key_off;
-    if ((rc = launch_order(pool, o, ws.scratch, st)) != MARLAAS_OK) return rc;
+    if (a.perm) {
+        OrderArgs o;
+        memset(&o, 0, sizeof(o));
+        o.T = T; o.S = a.S; o.off = a.off; o.slot = a.slot; o.cap = pool->cap; o.nkeys = pool->cap + 1;
+        o.perm = ws.perm; o.key_off = ws.key_off;
+        if ((rc = launch_order(pool, o, ws.scratch, st)) != MARLAAS_OK) return rc;
+    }
     rc = launch_norm(pool, a, rms, true, st);
     if (rc != MARLAAS_OK) return rc;
     if (a.partial) {
-        int warps = 4;              // one per 32 groups
-        while (warps < 32 && warps * 32 < n.groups) warps *= 2;
+        // as many warps as let all CTAs run at once
+        const int64_t ctas = cdiv(d, 128) * (pool->cap + 1);
+        int warps = 8;
+        while (warps < 32 && warps * 32 < n.groups && ctas * warps * 2 <= (int64_t)pool->sm_count * 64) warps *= 2;
         cudaLaunchConfig_t cfg;
         memset(&cfg, 0, sizeof(cfg));
         cudaLaunchAttribute at[1];
@@ -723,6 +785,7 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
         at[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.gridDim = dim3((unsigned)cdiv(d, 128), (unsigned)(pool->cap + 1));
         cfg.blockDim = dim3((unsigned)(warps * 32));
+        cfg.dynamicSmemBytes = (size_t)warps * 32 * (2 * sizeof(float4) + sizeof(int2));
         cfg.stream = st;
         cfg.attrs = at;
         cfg.numAttrs = 1;

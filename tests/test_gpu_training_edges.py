@@ -23,7 +23,7 @@ def pool():
 
 @pytest.mark.parametrize("rms", [False, True])
 @pytest.mark.parametrize("T,d,S", [(148, 504, 4), (149, 512, 9), (593, 2040, 20), (592, 2048, 3), (1185, 2304, 50), (597, 3592, 60), (741, 6152, 11),
-                                   (300, 16376, 25)])
+                                   (300, 16376, 25), (3000, 4096, 1000), (9000, 64, 8300), (9000, 72, 3000), (5000, 1600, 40), (4000, 520, 1)])
 def test_norms_on_both_sides_of_each_change(pool, T, d, S, rms):
     norm.test_both_passes(pool, T, d, S, rms)
 
