@@ -5,7 +5,7 @@
 //     dx_i = grad_scale k w_i (p - e_y) W^T,   p = softmax(z)
 // W is frozen, there is no dW.  Two products of 2 T d V operations, one without the gradient:
 //   1. the tokens that count are gathered, in their order, so that ignored ones (prompts, padding) cost nothing
-//   2. x W tile by tile in tensor memory; a tile leaves it as a pair (reference, sum of exponentials) per row, and for the
+//   2. x W tile by tile in tensor memory (a few tokens: head_few.cu); a tile leaves it as a pair (reference, sum of exponentials) per row, and for the
 //      gradient as exponentials in bf16, relative to the row's reference in the tile: their error is 2^-8 of each probability,
 //      where rounding the logits would make it 2^-8 of a logit
 //   3. a row's pairs give the sum R of the exponentials of all entries but the target, and logp = -log(1 + R / exp z_y), which
@@ -13,8 +13,8 @@
 //   4. times W^T, cut along the vocabulary so that few rows fill the SMs too; the row's factor enters in fp32
 // The exponentials of at most HEAD_PIECE_BYTES are held at a time: larger batches go through steps 2 to 4 in pieces of rows.
 // The tensor cores bound it: at 2048 counted rows x 131072 x 4096 steps 2 and 4 take 1.67 and 1.66 ms, 1.32 PFLOP/s each, and step
-// 3 0.19 ms, which is the exponentials once from HBM and back.  Few rows are bound by latency: 32 x 1024 x 32768 without gradient
-// 33 us, of which the weights' 67 MB are 10 and the two rounds of 256 x 256 tiles 22.
+// 3 0.19 ms, which is the exponentials once from HBM and back.  Few rows are bound by W's bytes and by latency: 32 x 1024 x 32768
+// without gradient 27 us in four dependent kernels, of which W's 67 MB are 10.
 #include <math.h>
 #include <string.h>
 
@@ -35,7 +35,8 @@ constexpr float HEAD_LOG2E = 1.4426950408889634f, HEAD_LN2 = 0.6931471805599453f
 
 struct HeadArgs {
     int64_t T;
-    int d, V, NT;                           // NT: 256-column tiles of the vocabulary
+    int d, V, NT;                           // NT: tiles of the vocabulary, of 256 columns, or 128 for a few tokens
+    int tile_shift;                         // log2 of a tile's vectors of eight columns
     int dp;                                 // d in whole 64-element panels: the pitch of the rows
     const bf16* x; int64_t ldx;
     const int32_t* targets;
@@ -97,7 +98,15 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_gather(const HeadArgs a, 
     if (on) {
         const uint4* src = reinterpret_cast<const uint4*>(a.x + i * a.ldx);
         uint4* dst = reinterpret_cast<uint4*>(a.rows + p * a.dp);
-        for (int v = lane; v < a.dp / 8; v += 32) dst[v] = v < nvec ? src[v] : make_uint4(0u, 0u, 0u, 0u);
+        constexpr int U = 4;                    // vectors on their way per lane
+        for (int v0 = lane; v0 < a.dp / 8; v0 += 32 * U) {
+            uint4 q[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) q[u] = v0 + 32 * u < nvec ? src[v0 + 32 * u] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v0 + 32 * u < a.dp / 8) dst[v0 + 32 * u] = q[u];
+        }
         if (lane == 0) {
             a.row_target[p] = a.targets[i];
             a.row_coef[p] = a.factor * (a.weight ? a.weight[i] : 1.f);
@@ -118,7 +127,7 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_gather(const HeadArgs a, 
 // Streams 4 bytes per element: HBM.
 template <bool GRAD>
 __global__ void __launch_bounds__(HEAD_THREADS) k_head_rows(const HeadArgs a, int row0) {
-    __shared__ float s_f[GRAD ? MARLAAS_MAX_VOCABULARY / 256 : 1];
+    __shared__ float s_f[GRAD ? MARLAAS_MAX_VOCABULARY / 128 : 1];
     __shared__ float s_red[HEAD_THREADS / 32];
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     sm100::dk_wait_prerequisites();
@@ -181,7 +190,7 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_rows(const HeadArgs a, in
             const int v = v0 + u * HEAD_THREADS;
             if (v >= nvec) break;
             uint32_t* w = &q[u].x;
-            const float f = s_f[v >> 5];
+            const float f = s_f[v >> a.tile_shift];
             const int at = y - v * 8;           // the target's place in the vector, if it is there
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -330,7 +339,7 @@ static HeadWorkspace carve_head(int64_t T, int64_t d, int64_t V, int32_t S, bool
     char* p = (char*)base;
     size_t o = 0;
     auto take = [&](size_t bytes) { char* q = p ? p + o : nullptr; o += align_up(bytes, 256); return q; };
-    w.NT = cdiv(V, 256);
+    w.NT = cdiv(V, T <= HEAD_FEW_T ? 128 : 256);
     w.lde = (int64_t)align_up((size_t)V, 64);
     w.dp = (int64_t)align_up((size_t)d, 64);
     // rows of a piece, a multiple of the row tile: by the exponentials' bytes, or without them by the tiles' pairs
@@ -437,7 +446,7 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
         }
         HeadArgs a;
         memset(&a, 0, sizeof(a));
-        a.T = T; a.d = (int)d; a.V = (int)V; a.NT = (int)ws.NT; a.dp = (int)ws.dp;
+        a.T = T; a.d = (int)d; a.V = (int)V; a.NT = (int)ws.NT; a.tile_shift = T <= HEAD_FEW_T ? 4 : 5; a.dp = (int)ws.dp;
         a.x = (const bf16*)x; a.ldx = ldx; a.targets = targets; a.weight = weight; a.factor = grad_scale * inv_temperature;
         a.perm = ws.perm; a.active = ws.key_off + 1; a.rows = ws.rows; a.row_target = ws.row_target; a.row_coef = ws.row_coef;
         a.E = ws.E; a.lde = ws.lde; a.part = ws.part; a.target_logit = ws.target_logit;
@@ -471,7 +480,8 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
             g.C = ws.E; g.ldc = ws.lde;
             g.XA = g.XB = nullptr; g.xa_cols = g.xb_rows = g.xb_ld = 0;
             g.tile_nunits = g.tile_units = nullptr; g.umax = 0;
-            if ((rc = launch_head_softmax(pool, g, h, st)) != MARLAAS_OK) return rc;
+            rc = T <= HEAD_FEW_T ? launch_head_few(pool, T, d, V, ws.rows, ws.dp, (const bf16*)W, ldw, ws.E, ws.lde, h, st) : launch_head_softmax(pool, g, h, st);
+            if (rc != MARLAAS_OK) return rc;
             if (!dx) {
                 if ((rc = launch_behind("k_head_rows", k_head_rows<false>, (unsigned)rows, st, a, (int)r0)) != MARLAAS_OK) return rc;
                 continue;

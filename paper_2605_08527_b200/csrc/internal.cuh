@@ -233,7 +233,7 @@ struct HeadEpilogue {
     const int32_t* perm;               // [all rows] the rows' tokens
     float k2;                          // inv_temperature / ln 2
     int keep;                          // the exponentials are wanted
-    float2* part;                      // [rows][part_ld] (reference, sum of exponentials but the target's) of every 256-column tile
+    float2* part;                      // [rows][part_ld] (reference, sum of exponentials but the target's) of every tile
     int part_ld;
     float* target_logit;               // [rows] in units of log 2
     const float* coef;                 // [rows] factor of a row's gradient
@@ -245,6 +245,10 @@ int head_pairs(const marlaas_pool* pool);
 // E = exponentials of (x W) (o.C, when kept); dx = E W^T over the ranges
 marlaas_status_t launch_head_softmax(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st);
 marlaas_status_t launch_head_grad(const marlaas_pool* pool, const GemmOperands& o, const HeadEpilogue& h, cudaStream_t st);
+// head_few.cu: the first product for at most HEAD_FEW_T tokens, in tiles of 128 columns
+constexpr int HEAD_FEW_T = 64;
+marlaas_status_t launch_head_few(const marlaas_pool* pool, int64_t T, int64_t d, int64_t V, const bf16* rows, int64_t dp, const bf16* W, int64_t ldw,
+                                 bf16* E, int64_t lde, const HeadEpilogue& h, cudaStream_t st);
 
 // decode_sm100.cu: the whole forward for batches of at most 1024 tokens (two overlapping kernels).
 // S < 0: ws.tok_slot already holds the per-token slots.

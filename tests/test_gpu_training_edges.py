@@ -164,6 +164,12 @@ def test_everything_at_once_on_two_streams(pool):
     B.marlaas_check_status(c.pool)
 
 
+@pytest.mark.parametrize("T,d,V", [(16, 200, 127), (17, 64, 128), (32, 72, 129), (33, 520, 20000), (63, 448, 191), (64, 456, 40000), (65, 456, 40000)])
+def test_head_of_a_few_tokens(T, d, V):
+    pool = B.AdapterPool(64, 64, 8, head.CAP)
+    head.test_loss_and_gradient(pool, T, d, V)
+
+
 @pytest.mark.parametrize("T,d,V", [(33, 65536, 264), (2, 64, B.MARLAAS_MAX_VOCABULARY), (260, 8, 9)])
 def test_head_at_its_largest(T, d, V):
     pool = B.AdapterPool(64, 64, 8, head.CAP)
