@@ -5,7 +5,7 @@
 //     dgain_t = sum over its tokens of dy xh                      dbias_t = sum of dy
 // (RMS norm: mean = 0 and no avg(a).)  Statistics and sums are fp32; x, y, dy, dx are bf16, rounded once when they are written.
 // HBM bounds both passes, 4 bytes per element forward and 6 backward, and the issue of instructions nearly as much: unpacking bf16
-// and the arithmetic on pairs take 58 % of the issue slots forward and 51 % backward (16384 x 4096, k_norm_forward 52 us, 5.2 TB/s;
+// and the arithmetic on pairs take 58 % of the issue slots in either pass (16384 x 4096, k_norm_forward 52 us, 5.2 TB/s;
 // k_norm_backward 75 us, 5.4 TB/s).  So elements are handled in pairs, sums four at a time, addresses as running pointers, and what
 // does not depend on a row (the tenant's parameters, the sums for their gradients) stays where it is from row to row.
 #include <string.h>
