@@ -322,7 +322,7 @@ static marlaas_status_t masked_shrink(const marlaas_pool* v, int64_t T, const bf
         float* hp = h + (size_t)p * T * v->RP;
         const marlaas_status_t rc = shrink_split_sm100_eligible(v, T, v->K, true)
                                         ? launch_shrink_split_sm100(v, T, x, ldx, v->K, At, v->K, wp, hp, st, h_is_zero, 1, &m)
-                                        : launch_shrink_sm100(v, T, x, ldx, v->K, At, v->K, wp, hp, st, &m);
+                                        : launch_shrink_sm100(v, T, x, ldx, v->K, At, v->K, wp, hp, st, h_is_zero, &m);
         if (rc != MARLAAS_OK) return rc;
     }
     return MARLAAS_OK;
@@ -394,10 +394,9 @@ marlaas_status_t marlaas_lora_forward_dropout(marlaas_pool_t* pool, int64_t T, c
     } else {
         marlaas_pool v;
         scaled_view(pool, d.scale, &v);
-        const bool pre_zero = shrink_split_sm100_eligible(pool, T, pool->K, true);       // (before the plan: see lora_forward)
-        if ((rc = launch_drop_begin(pool, drop, d, pre_zero ? h : nullptr, (size_t)pool->P * T * pool->RP, st)) != MARLAAS_OK) return rc;
+        if ((rc = launch_drop_begin(pool, drop, d, h, (size_t)pool->P * T * pool->RP, st)) != MARLAAS_OK) return rc;
         if ((rc = make_plan(pool, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
-        if ((rc = masked_shrink(&v, T, (const bf16*)x, ldx, ws, mask, h, pre_zero, st)) != MARLAAS_OK) return rc;
+        if ((rc = masked_shrink(&v, T, (const bf16*)x, ldx, ws, mask, h, true, st)) != MARLAAS_OK) return rc;
     }
     GemmOperands o;
     forward_operands(pool, T, (const bf16*)x, ldx, (const bf16*)W, ldw, (bf16*)y, ldy, ws, &o);
@@ -459,16 +458,15 @@ marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, 
     }
     marlaas_pool v;
     scaled_view(pool, d.scale, &v);
-    const bool pre_zero = NP == 1 && (dx || want_dA) && shrink_split_sm100_eligible(pool, T, pool->N, true);
-    if ((rc = launch_drop_begin(pool, drop, d, pre_zero ? ws.g : nullptr, (size_t)T * pool->RP, st)) != MARLAAS_OK) return rc;
+    if ((rc = launch_drop_begin(pool, drop, d, dx || want_dA ? ws.g : nullptr, (size_t)NP * T * pool->RP, st)) != MARLAAS_OK) return rc;
     if ((rc = make_plan(pool, T, seg, flags, host_ts, ws, st)) != MARLAAS_OK) return rc;
     if (dx || want_dA)
         for (int p = 0; p < NP; ++p) {
             const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
             const Workspace wp = part_workspace(pool, ws, p, T);
             rc = shrink_split_sm100_eligible(pool, T, Np, true)
-                     ? launch_shrink_split_sm100(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st, pre_zero)
-                     : launch_shrink_sm100(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st);
+                     ? launch_shrink_split_sm100(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st, true)
+                     : launch_shrink_sm100(&v, T, (const bf16*)dy + c0, lddy, Np, pool->d_Bs + c0, pool->ldB, wp, wp.g, st, true);
             if (rc != MARLAAS_OK) return rc;
         }
     if ((rc = product()) != MARLAAS_OK) return rc;

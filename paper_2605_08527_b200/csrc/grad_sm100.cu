@@ -555,24 +555,6 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
 
 bool grad_sm100_eligible(const marlaas_pool* pool, int64_t T) { return pool->cap <= 256 && T > 0 && cdiv(T, 64) <= 4096; }
 
-template <typename... P, typename... A>
-static marlaas_status_t launch_link(const char* name, void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, bool chained, cudaStream_t st, A... args) {
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = chained ? 1 : 0;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
-    MARLAAS_LAUNCH_CHECK(name);
-    return MARLAAS_OK;
-}
-
 marlaas_status_t launch_grad_plan(const marlaas_pool* pool, int64_t T, const Workspace& ws, cudaStream_t st, bool chained) {
     using namespace sm100;
     const int nblk = (int)cdiv(T, 64), c = chained ? 1 : 0;

@@ -298,24 +298,6 @@ __global__ void __launch_bounds__(HEAD_THREADS) k_head_dx(const HeadArgs a, cons
     }
 }
 
-// A launch behind the kernel before it, which it waits for itself.
-template <class... P, class... A>
-static marlaas_status_t launch_behind(const char* name, void (*kernel)(P...), unsigned grid, cudaStream_t st, A... args) {
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(HEAD_THREADS);
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
-    MARLAAS_LAUNCH_CHECK(name);
-    return MARLAAS_OK;
-}
-
 struct HeadWorkspace {
     int32_t* off;           // [S + 1] host tables
     int32_t* slot;          // [S]
@@ -483,21 +465,21 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
             rc = T <= HEAD_FEW_T ? launch_head_few(pool, T, d, V, ws.rows, ws.dp, (const bf16*)W, ldw, ws.E, ws.lde, h, st) : launch_head_softmax(pool, g, h, st);
             if (rc != MARLAAS_OK) return rc;
             if (!dx) {
-                if ((rc = launch_behind("k_head_rows", k_head_rows<false>, (unsigned)rows, st, a, (int)r0)) != MARLAAS_OK) return rc;
+                if ((rc = launch_link("k_head_rows", k_head_rows<false>, dim3((unsigned)rows), HEAD_THREADS, 0, true, st, a, (int)r0)) != MARLAAS_OK) return rc;
                 continue;
             }
-            if ((rc = launch_behind("k_head_rows", k_head_rows<true>, (unsigned)rows, st, a, (int)r0)) != MARLAAS_OK) return rc;
+            if ((rc = launch_link("k_head_rows", k_head_rows<true>, dim3((unsigned)rows), HEAD_THREADS, 0, true, st, a, (int)r0)) != MARLAAS_OK) return rc;
             g.Nout = d; g.Kc = ws.lde; g.b_cols = V;
             g.A = ws.E; g.lda = ws.lde;
             g.b_mn = false;
             g.C = (bf16*)dx; g.ldc = lddx;
             if ((rc = launch_head_grad(pool, g, h, st)) != MARLAAS_OK) return rc;
             const bool with_stats = stats && r0 + rows >= T;
-            if ((rc = launch_behind("k_head_dx", k_head_dx, (unsigned)(rows + (with_stats ? pool->cap + 1 : 0)), st, a, h, (int)rows,
+            if ((rc = launch_link("k_head_dx", k_head_dx, dim3((unsigned)(rows + (with_stats ? pool->cap + 1 : 0))), HEAD_THREADS, 0, true, st, a, h, (int)rows,
                                     (int)cdiv(V, 128) * 2, sums)) != MARLAAS_OK) return rc;
         }
     }
-    if (stats && (T == 0 || !dx) && (rc = launch_behind("k_head_stats", k_head_stats, (unsigned)(pool->cap + 1), st, sums)) != MARLAAS_OK) return rc;
+    if (stats && (T == 0 || !dx) && (rc = launch_link("k_head_stats", k_head_stats, dim3((unsigned)(pool->cap + 1)), HEAD_THREADS, 0, true, st, sums)) != MARLAAS_OK) return rc;
     return finish(pool, flags, st);
 } catch (const std::exception& e) {
     return fail(MARLAAS_ERR_INVALID_ARG, "head_cross_entropy: %s", e.what());

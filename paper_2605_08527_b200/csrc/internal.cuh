@@ -280,6 +280,7 @@ marlaas_status_t launch_decode_sm100(const marlaas_pool* pool, int64_t T, const 
 // store: the rows of the pooled store to contract with ([cap*RP] rows of D elements, sld elements apart)
 marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D,
                                      const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st,
+                                     bool chained = false,      // behind a kernel that cleared out, or one behind that
                                      const DropMask* drop = nullptr);
 
 // shrink_split_sm100.cu: the same outputs with one tile per cluster and the contraction split over the cluster's
@@ -348,6 +349,25 @@ marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf
 bool adapter_gradients_fit(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, const Workspace& ws);
 // pool.cu: the pool with other scales of its slots, for the kernel launchers alone (no streams)
 void scaled_view(const marlaas_pool* pool, const float* d_scale, marlaas_pool* view);
+
+// A launch on a stream; chained: while the kernel before it still runs, whose end the kernel waits for itself before it reads.
+template <typename... P, typename... A>
+inline marlaas_status_t launch_link(const char* name, void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, bool chained, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = chained ? 1 : 0;
+    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
+    MARLAAS_LAUNCH_CHECK(name);
+    return MARLAAS_OK;
+}
 
 // vocab_rows.cu: one pass over rows of logits (softmax statistics, the policy loss's per-token terms, the gradient)
 struct PolicyTerms {           // what a token adds to its tenant's stats

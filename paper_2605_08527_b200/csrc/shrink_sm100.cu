@@ -36,6 +36,7 @@ struct ShrinkArgs {
     bf16* hd;         // [T][hd_cols]
     int hd_cols;
     int32_t* status;
+    int chained;      // launched while the kernel before it still runs: waits for its end
     DropMask drop;    // DROP
 };
 
@@ -68,6 +69,10 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
     const uint32_t bar_ready = bar_drain + 8;       // DROP: the stage is masked (eight warps)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * STAGES + 5);
     volatile int* abort_word = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    if (g.chained) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -270,7 +275,7 @@ k_shrink_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant_
 
 marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D,
                                      const bf16* store, int64_t sld, const Workspace& ws, float* out, cudaStream_t st,
-                                     const DropMask* drop) {
+                                     bool chained, const DropMask* drop) {
     using namespace sm100;
     if (T <= 0) return MARLAAS_OK;
     ShrinkArgs g;
@@ -295,7 +300,8 @@ marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const 
     marlaas_status_t rc;
     if ((rc = make_map(&tmSrc, src, T, D, ld, BK, BM)) != MARLAAS_OK) return rc;
     if ((rc = make_map(&tmStore, store, (int64_t)pool->cap * pool->RP, D, sld, BK, 16)) != MARLAAS_OK) return rc;
-    MARLAAS_CUDA_TRY(cudaMemsetAsync(out, 0, sizeof(float) * (size_t)T * pool->RP, st));
+    if (!chained) MARLAAS_CUDA_TRY(cudaMemsetAsync(out, 0, sizeof(float) * (size_t)T * pool->RP, st));
+    g.chained = chained ? 1 : 0;
     constexpr size_t smem_bytes = 1024 + (size_t)SHRINK_STAGES * (A_STAGE_BYTES + SB_STAGE_BYTES) + 256;
     static bool attr_set[64] = {};
     if (pool->device >= 64 || !attr_set[pool->device]) {
@@ -306,10 +312,8 @@ marlaas_status_t launch_shrink_sm100(const marlaas_pool* pool, int64_t T, const 
     const int grid = g.num_m_tiles < pool->sm_count ? g.num_m_tiles : pool->sm_count;
     if (drop) g.drop = *drop;
     else memset(&g.drop, 0, sizeof(g.drop));
-    if (drop) k_shrink_sm100<true><<<grid, SHRINK_THREADS + DROP_EXTRA_THREADS, smem_bytes, st>>>(tmSrc, tmStore, g);
-    else k_shrink_sm100<false><<<grid, SHRINK_THREADS, smem_bytes, st>>>(tmSrc, tmStore, g);
-    MARLAAS_LAUNCH_CHECK("k_shrink_sm100");
-    return MARLAAS_OK;
+    return drop ? launch_link("k_shrink_sm100", k_shrink_sm100<true>, dim3((unsigned)grid), SHRINK_THREADS + DROP_EXTRA_THREADS, smem_bytes, chained, st, tmSrc, tmStore, g)
+                : launch_link("k_shrink_sm100", k_shrink_sm100<false>, dim3((unsigned)grid), SHRINK_THREADS, smem_bytes, chained, st, tmSrc, tmStore, g);
 }
 
 }  // namespace marlaas
