@@ -214,7 +214,8 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_forward(const NormArgs
             group_sum4(v, s_sums, par, W, g, wg, lane);
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                mean[b] = v[b] * inv_d;
+                // (divided: the sum of a constant row is exact, and its quotient the constant; times 1 / d it may miss by an ulp)
+                mean[b] = __fdiv_rn(v[b], (float)a.d);
                 v[b] = 0.f;
             }
         }
