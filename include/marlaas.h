@@ -411,7 +411,8 @@ enum { MARLAAS_HEAD_STATS = 4 };                           /* columns of marlaas
  * projections drops the same elements for all of them.
  * rates: fp32 [capacity] on the device, per slot; a rate that is not above 0 (or a NaN) drops nothing, one of 1 or more drops
  * everything (the adapter then gives nothing and gets zero gradients).  What a dropped element holds does not matter to the
- * adapters.  With rates of 0 the results are marlaas_lora_forward's and marlaas_lora_backward's up to the order of sums.
+ * adapters, and what the rows of a tenant's tokens hold (infinities and NaN too) reaches no other tenant's rows and gradients.
+ * With rates of 0 the results are marlaas_lora_forward's and marlaas_lora_backward's up to the order of sums.
  * Otherwise as those two calls, with h_save = (m_i o x_i) A_t; of the flags, HOST_TABLE, VALIDATE_SYNC and (backward)
  * ACCUMULATE apply.  Workspace: marlaas_lora_dropout_workspace_bytes, for both.  Adapter gradients of pools of more than 64
  * slots cannot be captured. */

@@ -203,7 +203,8 @@ bool adapter_gradients_fit(const marlaas_pool* pool, int64_t T, const marlaas_se
 }
 
 // dA and dB of all slots on one stream, for the plan, g and (T > 0) h in the workspace or as saved: what marlaas_lora_backward
-// does when it does not run them beside the dx product.  drop (only where adapter_gradients_fit): x is masked on its way.
+// does when it does not run them beside the dx product.  drop: what a token's rows hold reaches its own tenant's gradients alone, and x
+// is masked on its way if drop->rates is given (only where adapter_gradients_fit).
 marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
                                    float* const* dA_slots, float* const* dB_slots, const marlaas_segments_t* seg, const float* h,
                                    const Workspace& ws, bool acc, cudaStream_t st, const DropMask* drop) {
@@ -219,6 +220,8 @@ marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf
     if (tc_grad && (rc = launch_grad_plan(pool, T, ws, st, true)) != MARLAAS_OK) return rc;
     if (!fits && (rc = launch_slot_sort(pool, T, ws.tok_slot, ws.slot_count, ws.slot_offset, ws.perm, st, run_flag)) != MARLAAS_OK) return rc;
     std::vector<float*> part((size_t)pool->cap, nullptr);
+    DropMask rows_alone;                    // dy is not masked
+    memset(&rows_alone, 0, sizeof(rows_alone));
     for (int p = 0; p < NP; ++p) {
         if (tc_grad && p > 0) MARLAAS_CUDA_TRY(cudaMemsetAsync(ws.gflag + 2, 0, 2 * sizeof(int32_t), st));
         const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
@@ -239,7 +242,8 @@ marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf
             if (!inline_tables)
                 MARLAAS_CUDA_TRY(cudaMemcpyAsync(dev, part.data(), sizeof(float*) * (size_t)pool->cap, cudaMemcpyHostToDevice, st));
             if (tc_grad && (rc = launch_grad_sm100(pool, T, C, src, ld, r, dev, part.data(), which == 1, acc, ws, st, which == 0 ? ws.hm : ws.hm2,
-                                                   GRAD_PHASE_REDUCE | (inline_tables ? GRAD_PHASE_CHAINED : 0), which == 1 ? drop : nullptr)) != MARLAAS_OK) return rc;
+                                                   GRAD_PHASE_REDUCE | (inline_tables ? GRAD_PHASE_CHAINED : 0),
+                                                   drop && which == 0 ? &rows_alone : drop)) != MARLAAS_OK) return rc;
             if (!fits && (rc = launch_grad_reduce(pool, C, src, ld, r, ws.perm, ws.slot_offset, dev, which == 1, acc, st, run_flag)) != MARLAAS_OK)
                 return rc;
         }

@@ -474,9 +474,10 @@ marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, 
     const bool fits = adapter_gradients_fit(pool, T, seg, ws);
     if (want_dA && !fits && (rc = launch_drop_rows(pool, T, (const bf16*)x, ldx, mask, d.xd, st)) != MARLAAS_OK) return rc;
     if (want_dB && !h_saved && (rc = masked_shrink(&v, T, (const bf16*)x, ldx, ws, mask, ws.h, false, st)) != MARLAAS_OK) return rc;
+    const DropMask masked = {mask.tok_slot, nullptr, mask.key};
     if ((want_dA || want_dB) &&
         (rc = adapter_gradients(&v, T, fits ? (const bf16*)x : d.xd, fits ? ldx : pool->K, (const bf16*)dy, lddy, dA_slots, dB_slots, seg, h, ws, acc,
-                                st, fits ? &mask : nullptr)) != MARLAAS_OK)
+                                st, fits ? &mask : &masked)) != MARLAAS_OK)
         return rc;
     return finish(pool, flags, st);
 } catch (const std::exception& e) {

@@ -13,9 +13,10 @@
 // and writes the slot's gradient once.  If the batch interleaves tenants so finely that the copies would not
 // fit the workspace, a device flag routes the call to the CUDA-core reduction instead.
 //
-// For dA of the layer with dropout (DROP) the streamed rows of x are masked on their way: eight warps more zero the dropped elements
-// of every stage in shared memory before the MMA warp may use it, and the rows of the block's other tenants (8192 x 4096, 32 tenants
-// of rank 16: 37 us against 30 without masks; with the epilogue's warps doing half of it 48).
+// For the layer with dropout (DROP) the streamed rows are masked on their way: eight warps more zero the rows of the block's other
+// tenants in every stage in shared memory before the MMA warp may use it, since zeros of their r-vectors times an infinity or a NaN
+// would not be zeros, and for dA the dropped elements of x (8192 x 4096, 32 tenants of rank 16: 37 us against 30 without masks; with
+// the epilogue's warps doing half of it 48).
 #include <string.h>
 
 #include "dropout.cuh"
@@ -281,7 +282,7 @@ k_grad_sm100(const __grid_constant__ CUtensorMap tmSrc, const __grid_constant__ 
     // skewed batches still finish together; which CTA computes an item does not change its value.
     for (int t = threadIdx.x; t < g.cap; t += blockDim.x) s_cnt[t] = ((g.out_ptrs ? g.out_ptrs[t] : g.inl[t]) != nullptr && g.d_rank[t] > 0) ? g.ten_nblk[t] : -1;
     if (DROP)
-        for (int t = threadIdx.x; t < g.cap; t += blockDim.x) s_limit[t] = drop_limit(g.drop.rates[t]);
+        for (int t = threadIdx.x; t < g.cap; t += blockDim.x) s_limit[t] = g.drop.rates ? drop_limit(g.drop.rates[t]) : 0u;
     tc_fence_before();
     __syncthreads();
     for (int t = threadIdx.x; t < g.cap; t += blockDim.x) {

@@ -158,7 +158,7 @@ struct DropKey {
 // The masks of a kernel with dropout (dropout.cu).
 struct DropMask {
     const int32_t* tok_slot;           // [M]
-    const float* rates;                // [cap]
+    const float* rates;                // [cap]; grad_sm100.cu: NULL drops nothing, and the other tenants' rows alone are zeroed
     DropKey key;
 };
 // ---- kernels launched by api.cu ---------------------------------------------------------------------
@@ -327,7 +327,7 @@ marlaas_status_t launch_grad_copies(const marlaas_pool* pool, int64_t T, const W
 marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t C, const bf16* src, int64_t ld,
                                    const float* hg, float* const* out_ptrs, float* const* host_ptrs, bool transpose_out,
                                    bool accumulate, const Workspace& ws, cudaStream_t st, bf16* hm, int phases = GRAD_PHASE_COPIES | GRAD_PHASE_REDUCE,
-                                   const DropMask* drop = nullptr);      // rows of src masked on their way
+                                   const DropMask* drop = nullptr);      // rows of src masked on their way, those of other tenants zeroed
 // host_ptrs: the same table in host memory; pools of at most 64 slots pass it with the launch and never read out_ptrs
 
 // api.cu: the layer's steps, shared with its form with dropout (dropout.cu)
