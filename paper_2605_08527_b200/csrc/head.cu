@@ -383,7 +383,8 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: inv_temperature must be positive, finite and below 1.7e38", fn);
     if (!std::isfinite(grad_scale) || !std::isfinite(grad_scale * inv_temperature))
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: grad_scale is not finite", fn);
-    if (!dx && !logp && !stats) return fail(MARLAAS_ERR_INVALID_ARG, "%s: no output", fn);
+    // (an output of no tokens may have no address)
+    if (T > 0 && !dx && !logp && !stats) return fail(MARLAAS_ERR_INVALID_ARG, "%s: no output", fn);
     if (misaligned(logp, 4) || misaligned(stats, 4) || misaligned(weight, 4))
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: weight, logp or stats is misaligned", fn);
     if (logp && logp == weight) return fail(MARLAAS_ERR_INVALID_ARG, "%s: logp must not be one of the inputs", fn);

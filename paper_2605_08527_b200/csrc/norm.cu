@@ -735,7 +735,8 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
     const bool rms = (flags & MARLAAS_FLAG_RMS_NORM) != 0, host = (flags & MARLAAS_FLAG_HOST_TABLE) != 0;
     const bool accumulate = (flags & MARLAAS_FLAG_ACCUMULATE) != 0;
     if (misaligned(dgain, 16) || misaligned(dbias, 16)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: dgain or dbias is not 16-byte aligned", fn);
-    if (!dx && !dgain && !dbias) return fail(MARLAAS_ERR_INVALID_ARG, "%s: no output", fn);
+    // (a dx of no tokens may have no address)
+    if (T > 0 && !dx && !dgain && !dbias) return fail(MARLAAS_ERR_INVALID_ARG, "%s: no output", fn);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (T == 0) {
         MARLAAS_CUDA_TRY(cudaSetDevice(pool->device));
