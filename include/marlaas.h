@@ -466,6 +466,7 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
  *  - A row with a NaN or +inf logit gets NaN, and touches no other row; a logit of -inf has probability 0; a row whose logits
  *    are all -inf has no distribution: logp and dx are 0.
  * dx: bf16 [T][d] or NULL (no gradient: half the work and a smaller workspace); it may be x itself.  logp: fp32 [T] or NULL.
+ * No output may overlap an input otherwise.
  * stats (or NULL; then seg is not read): fp32 [capacity + 1][MARLAAS_HEAD_STATS], per slot (last row: slot -1) the sums over its
  * tokens of  w (-logp), w, -logp, 1;  written, or added to with MARLAAS_FLAG_ACCUMULATE, in a fixed order.
  * The exponentials in the workspace are those of a piece of the batch (512 MB, or 256 rows where those are more).  The probabilities

@@ -349,6 +349,18 @@ static HeadWorkspace carve_head(int64_t T, int64_t d, int64_t V, int32_t S, bool
     return w;
 }
 
+// The bytes of an argument (none, if it is not given).
+struct Span {
+    const char* name;
+    const void* p;
+    size_t bytes;
+};
+static Span matrix_span(const char* name, const void* p, int64_t rows, int64_t ld, int64_t cols) { return {name, p, 2 * (size_t)((rows - 1) * ld + cols)}; }
+static bool overlap(const Span& a, const Span& b) {
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
 static bool head_sizes_ok(int64_t T, int64_t d, int64_t V) {
@@ -387,7 +399,6 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
     if (T > 0 && !dx && !logp && !stats) return fail(MARLAAS_ERR_INVALID_ARG, "%s: no output", fn);
     if (misaligned(logp, 4) || misaligned(stats, 4) || misaligned(weight, 4))
         return fail(MARLAAS_ERR_INVALID_ARG, "%s: weight, logp or stats is misaligned", fn);
-    if (logp && logp == weight) return fail(MARLAAS_ERR_INVALID_ARG, "%s: logp must not be one of the inputs", fn);
     marlaas_status_t rc;
     if (stats && (rc = check_segments(fn, pool, T, seg, flags, nullptr)) != MARLAAS_OK) return rc;
     const bool accumulate = (flags & MARLAAS_FLAG_ACCUMULATE) != 0, host = stats && (flags & MARLAAS_FLAG_HOST_TABLE) != 0;
@@ -400,13 +411,18 @@ marlaas_status_t marlaas_head_cross_entropy(marlaas_pool_t* pool, int64_t T, int
         if ((rc = check_matrix(fn, "x", x, ldx, d)) != MARLAAS_OK) return rc;
         if ((rc = check_matrix(fn, "W", W, ldw, V)) != MARLAAS_OK) return rc;
         if (!targets || misaligned(targets, 4)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: targets is NULL or misaligned", fn);
-        if (dx) {
-            if ((rc = check_matrix(fn, "dx", dx, lddx, d)) != MARLAAS_OK) return rc;
-            const uintptr_t x0 = (uintptr_t)x, x1 = x0 + 2 * (size_t)((T - 1) * ldx + d);
-            const uintptr_t d0 = (uintptr_t)dx, d1 = d0 + 2 * (size_t)((T - 1) * lddx + d);
-            if (d0 < x1 && x0 < d1 && !(d0 == x0 && lddx == ldx))
-                return fail(MARLAAS_ERR_INVALID_ARG, "%s: dx overlaps x without being the same matrix", fn);
-        }
+        if (dx && (rc = check_matrix(fn, "dx", dx, lddx, d)) != MARLAAS_OK) return rc;
+        // dx may be x itself: rows are gathered before; other outputs are written while other CTAs still read inputs (of ignored tokens, in the first kernel)
+        const bool table = stats && !(flags & MARLAAS_FLAG_HOST_TABLE);
+        const Span outs[] = {matrix_span("dx", dx, T, lddx, d), {"logp", logp, 4 * (size_t)T},
+                             {"stats", stats, 4 * (size_t)MARLAAS_HEAD_STATS * ((size_t)pool->cap + 1)}};
+        const Span ins[] = {matrix_span("x", x, T, ldx, d), matrix_span("W", W, d, ldw, V), {"targets", targets, 4 * (size_t)T},
+                            {"weight", weight, 4 * (size_t)T}, {"the segment table", table ? off : nullptr, 4 * ((size_t)S + 1)},
+                            {"the segment table", table ? slot : nullptr, 4 * (size_t)S}};
+        for (const Span& o : outs)
+            for (const Span& i : ins)
+                if (overlap(o, i) && !(&o == outs && &i == ins && dx == x && lddx == ldx))
+                    return fail(MARLAAS_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, o.name, i.name);
         if (!workspace || misaligned(workspace, 256)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: workspace NULL or misaligned", fn);
         ws = carve_head(T, d, V, S, dx != nullptr, workspace);
         if (workspace_bytes < ws.total_bytes)
