@@ -186,28 +186,17 @@ marlaas_status_t reject_captured_tables(const char* fn, const marlaas_pool* pool
     return MARLAAS_OK;
 }
 
-// The pool's side stream and its events, on first use.
-marlaas_status_t make_side_stream(marlaas_pool* pool) {
-    if (pool->side) return MARLAAS_OK;
-    int lo = 0, hi = 0;
-    MARLAAS_CUDA_TRY(cudaDeviceGetStreamPriorityRange(&lo, &hi));
-    MARLAAS_CUDA_TRY(cudaStreamCreateWithPriority(&pool->side, cudaStreamNonBlocking, lo));   // lowest priority
-    MARLAAS_CUDA_TRY(cudaEventCreateWithFlags(&pool->ev_fork, cudaEventDisableTiming));
-    MARLAAS_CUDA_TRY(cudaEventCreateWithFlags(&pool->ev_join, cudaEventDisableTiming));
-    return MARLAAS_OK;
-}
-
 // Whether the tensor-core reductions' copies fit the workspace for certain, whatever the tokens' tenants.
 bool adapter_gradients_fit(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, const Workspace& ws) {
     return grad_sm100_eligible(pool, T) && cdiv(T, 64) + (int64_t)seg->num_segments <= (int64_t)ws.max_copies;
 }
 
-// dA and dB of all slots on one stream, for the plan, g and (T > 0) h in the workspace or as saved: what marlaas_lora_backward
-// does when it does not run them beside the dx product.  drop: what a token's rows hold reaches its own tenant's gradients alone, and x
+// dA and dB of all slots, for the plan, g and (T > 0) h in the workspace or as saved, kernel behind kernel on the caller's stream.
+// grad_plan_made: the blocks' lists in the workspace are an earlier call's.  drop: what a token's rows hold reaches its own tenant's gradients alone, and x
 // is masked on its way if drop->rates is given (only where adapter_gradients_fit).
 marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
                                    float* const* dA_slots, float* const* dB_slots, const marlaas_segments_t* seg, const float* h,
-                                   const Workspace& ws, bool acc, cudaStream_t st, const DropMask* drop) {
+                                   const Workspace& ws, bool acc, cudaStream_t st, const DropMask* drop, bool grad_plan_made) {
     marlaas_status_t rc;
     const int NP = pool->P;
     const size_t plane = (size_t)T * pool->RP;
@@ -217,17 +206,18 @@ marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf
     const bool inline_tables = fits && pool->cap <= 64;
     const int32_t* run_flag = tc_grad ? ws.gflag : nullptr;
     // (behind a copy or a clear nothing is launched ahead of time)
-    if (tc_grad && (rc = launch_grad_plan(pool, T, ws, st, true)) != MARLAAS_OK) return rc;
+    if (tc_grad && !grad_plan_made && (rc = launch_grad_plan(pool, T, ws, st, true)) != MARLAAS_OK) return rc;
     if (!fits && (rc = launch_slot_sort(pool, T, ws.tok_slot, ws.slot_count, ws.slot_offset, ws.perm, st, run_flag)) != MARLAAS_OK) return rc;
     std::vector<float*> part((size_t)pool->cap, nullptr);
     DropMask rows_alone;                    // dy is not masked
     memset(&rows_alone, 0, sizeof(rows_alone));
     for (int p = 0; p < NP; ++p) {
-        if (tc_grad && p > 0) MARLAAS_CUDA_TRY(cudaMemsetAsync(ws.gflag + 2, 0, 2 * sizeof(int32_t), st));
+        // (the plan's kernels clear the reductions' counters of work items, too)
+        if (tc_grad && (p > 0 || grad_plan_made)) MARLAAS_CUDA_TRY(cudaMemsetAsync(ws.gflag + 2, 0, 2 * sizeof(int32_t), st));
         const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
         const float *rB = h + p * plane, *rA = ws.g + p * plane;
         if (tc_grad && (rc = launch_grad_copies(pool, T, ws, dB_slots ? rB : rA, dB_slots ? ws.hm : ws.hm2, dA_slots && dB_slots ? rA : nullptr, ws.hm2,
-                                                p == 0 && fits, st)) != MARLAAS_OK) return rc;
+                                                p == 0 && fits && !grad_plan_made, st)) != MARLAAS_OK) return rc;
         for (int which = 0; which < 2; ++which) {       // dB, then dA
             float* const* all = which == 0 ? dB_slots : dA_slots;
             if (!all) continue;
@@ -555,18 +545,7 @@ marlaas_status_t marlaas_lora_backward(marlaas_pool_t* pool, int64_t T, const vo
             if (want_dB && dB_slots[s]) dB_part[s] = dB_slots[s] + r * (size_t)pool->part_begin[p];
         }
     };
-    // The adapter-gradient kernels read none of the dx GEMM's output: when they need no further pass over the workspace
-    // the GEMM uses (the saved h is given, the tensor-core reduction is certain to fit) they are issued on a side stream
-    // of the pool, forked here and joined at the end, so that their small planning and copy kernels run beside the
-    // GEMM instead of after it.
-    const bool tc_grad0 = tc_path && (want_dA || want_dB) && grad_sm100_eligible(pool, T);
-    const bool fits0 = tc_grad0 && cdiv(T, 64) + (int64_t)seg->num_segments <= (int64_t)ws.max_copies;
     const bool gemm2 = NP > 1 || gemm2_sm100_eligible(pool, T);
-    const bool overlap = fits0 && T > 0 && dx && (!want_dB || h_saved) && gemm2_sm100_eligible(pool, T) && pool->cap <= 64;
-    if (overlap) {
-        if ((rc = make_side_stream(pool)) != MARLAAS_OK) return rc;
-        MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_fork, st));
-    }
     if (T > 0 && dx && tc_path) {
         GemmOperands o;
         backward_operands(pool, T, (const bf16*)W, ldw, (const bf16*)dy, lddy, (bf16*)dx, lddx, ws, &o);
@@ -587,46 +566,13 @@ marlaas_status_t marlaas_lora_backward(marlaas_pool_t* pool, int64_t T, const vo
         const bool fits = tc_grad && nblk + (int64_t)seg->num_segments <= (int64_t)ws.max_copies;
         const bool inline_tables = fits && pool->cap <= 64;
         const int32_t* run_flag = tc_grad ? ws.gflag : nullptr;   // the CUDA-core kernels run only if the flag is set
-        if (overlap) {
-            cudaStream_t gs = pool->side;
-            MARLAAS_CUDA_TRY(cudaStreamWaitEvent(gs, pool->ev_fork, 0));
-            // whatever happens from here on, the side stream is joined again before the call returns: a forked stream left
-            // unjoined would invalidate a capture the caller's stream may be part of
-            auto side_work = [&]() -> marlaas_status_t {
-                marlaas_status_t r;
-                for (int p = 0; p < NP; ++p) {
-                    if (p == 0 && !(flags & MARLAAS_FLAG_REUSE_PLAN)) {
-                        if ((r = launch_grad_plan(pool, T, ws, gs)) != MARLAAS_OK) return r;
-                    } else {
-                        // the plan kernel also zeroes the reductions' work-item counters; a reused plan needs them zeroed again
-                        MARLAAS_CUDA_TRY(cudaMemsetAsync(ws.gflag + 2, 0, 2 * sizeof(int32_t), gs));
-                    }
-                    part_tables(p);
-                    float* const* dAp = NP == 1 ? dA_slots : dA_part.data();
-                    float* const* dBp = NP == 1 ? dB_slots : dB_part.data();
-                    const int64_t c0 = pool->part_begin[p], Np = pool->part_begin[p + 1] - c0;
-                    const bf16* dyp = (const bf16*)dy + c0;
-                    const float* hp = h_saved ? h_saved + p * plane : nullptr;
-                    const float* gp = ws.g + p * plane;
-                    // both sets of copies first (small kernels that fit beside the GEMM's CTAs), then the two reductions
-                    if (want_dB && (r = launch_grad_sm100(pool, T, Np, dyp, lddy, hp, nullptr, dBp, false, acc, ws,
-                                                          gs, ws.hm, GRAD_PHASE_COPIES)) != MARLAAS_OK) return r;
-                    if (want_dA && (r = launch_grad_sm100(pool, T, pool->K, (const bf16*)x, ldx, gp, nullptr, dAp, true, acc, ws,
-                                                          gs, ws.hm2, GRAD_PHASE_COPIES)) != MARLAAS_OK) return r;
-                    if (want_dB && (r = launch_grad_sm100(pool, T, Np, dyp, lddy, hp, nullptr, dBp, false, acc, ws,
-                                                          gs, ws.hm, GRAD_PHASE_REDUCE)) != MARLAAS_OK) return r;
-                    // the dA reduction reads x and its own copies (made above), nothing of the dB reduction: started behind it
-                    // as a programmatic dependent, its CTAs take the SMs that the dB reduction's CTAs leave one by one
-                    if (want_dA && (r = launch_grad_sm100(pool, T, pool->K, (const bf16*)x, ldx, gp, nullptr, dAp, true, acc, ws,
-                                                          gs, ws.hm2, GRAD_PHASE_REDUCE | (want_dB ? GRAD_PHASE_EARLY : 0))) != MARLAAS_OK) return r;
-                }
-                return MARLAAS_OK;
-            };
-            rc = side_work();
-            MARLAAS_CUDA_TRY(cudaEventRecord(pool->ev_join, gs));
-            MARLAAS_CUDA_TRY(cudaStreamWaitEvent(st, pool->ev_join, 0));
-            if (rc != MARLAAS_OK) return rc;
-            return finish(pool, flags, st);
+        // Batches of many rows whose h was kept: every kernel launched behind the one before it.  (Beside the dx product, on a
+        // second stream, they took nothing less of a step over one 4096 x 4096 projection and 4 % over a layer's seven; that form is
+        // left out, since one like it stopped making progress.)
+        if (inline_tables && dx && (!want_dB || h_saved) && gemm2_sm100_eligible(pool, T)) {
+            rc = adapter_gradients(pool, T, (const bf16*)x, ldx, (const bf16*)dy, lddy, dA_slots, dB_slots, seg, h_saved ? h_saved : ws.h, ws, acc, st, nullptr,
+                                   (flags & MARLAAS_FLAG_REUSE_PLAN) != 0);
+            return rc != MARLAAS_OK ? rc : finish(pool, flags, st);
         }
         if (tc_grad && !(flags & MARLAAS_FLAG_REUSE_PLAN) && (rc = launch_grad_plan(pool, T, ws, st)) != MARLAAS_OK) return rc;
         if (!fits && (rc = launch_slot_sort(pool, T, ws.tok_slot, ws.slot_count, ws.slot_offset, ws.perm, st, run_flag)) != MARLAAS_OK) return rc;

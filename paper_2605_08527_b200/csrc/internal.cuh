@@ -89,9 +89,6 @@ struct marlaas_pool {
     bool timing = false;
     std::vector<cudaEvent_t> timing_events;
     size_t timing_used = 0;
-    // backward: the adapter-gradient kernels run on a side stream beside the dx GEMM (created on first use)
-    cudaStream_t side = nullptr;
-    cudaEvent_t ev_fork = nullptr, ev_join = nullptr;
 };
 
 namespace marlaas {
@@ -319,8 +316,7 @@ bool grad_sm100_eligible(const marlaas_pool* pool, int64_t T);
 // chained (here and below): launched while the kernel before it in the stream still runs, it waits for that one's end
 marlaas_status_t launch_grad_plan(const marlaas_pool* pool, int64_t T, const Workspace& ws, cudaStream_t st, bool chained = false);
 // phases: build the masked hi/lo copies of the r-vectors into hm, reduce from hm, or both
-// GRAD_PHASE_EARLY: the reduction reads nothing the kernel before it in the stream writes and may start while that one ends
-enum { GRAD_PHASE_COPIES = 1, GRAD_PHASE_REDUCE = 2, GRAD_PHASE_EARLY = 4, GRAD_PHASE_CHAINED = 8 };
+enum { GRAD_PHASE_COPIES = 1, GRAD_PHASE_REDUCE = 2, GRAD_PHASE_CHAINED = 4 };
 // the copies of one r-vector, or of two (r1 may be NULL)
 marlaas_status_t launch_grad_copies(const marlaas_pool* pool, int64_t T, const Workspace& ws, const float* r0, bf16* hm0, const float* r1, bf16* hm1,
                                     bool chained, cudaStream_t st);
@@ -341,11 +337,10 @@ void forward_operands(const marlaas_pool* pool, int64_t T, const bf16* x, int64_
                       const Workspace& ws, GemmOperands* o);
 void backward_operands(const marlaas_pool* pool, int64_t T, const bf16* W, int64_t ldw, const bf16* dy, int64_t lddy, bf16* dx, int64_t lddx,
                        const Workspace& ws, GemmOperands* o);
-marlaas_status_t make_side_stream(marlaas_pool* pool);
 marlaas_status_t reject_captured_tables(const char* fn, const marlaas_pool* pool, cudaStream_t st);
 marlaas_status_t adapter_gradients(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* dy, int64_t lddy,
                                    float* const* dA_slots, float* const* dB_slots, const marlaas_segments_t* seg, const float* h,
-                                   const Workspace& ws, bool acc, cudaStream_t st, const DropMask* drop = nullptr);
+                                   const Workspace& ws, bool acc, cudaStream_t st, const DropMask* drop, bool grad_plan_made = false);
 bool adapter_gradients_fit(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, const Workspace& ws);
 // pool.cu: the pool with other scales of its slots, for the kernel launchers alone (no streams)
 void scaled_view(const marlaas_pool* pool, const float* d_scale, marlaas_pool* view);

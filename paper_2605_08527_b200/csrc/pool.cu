@@ -79,8 +79,6 @@ void scaled_view(const marlaas_pool* pool, const float* d_scale, marlaas_pool* v
     *v = *pool;
     v->d_scale = const_cast<float*>(d_scale);
     v->timing = false;
-    v->side = nullptr;
-    v->ev_fork = v->ev_join = nullptr;
 }
 
 StorageLayout storage_layout(int64_t K, int64_t N, int32_t RP, int32_t cap, int32_t parts) {
@@ -273,12 +271,8 @@ marlaas_status_t marlaas_kernel_timing_end(marlaas_pool_t* pool, float* gemm_ms,
 }
 
 marlaas_status_t marlaas_adapter_pool_destroy(marlaas_pool_t* pool) {
-    if (pool) {
+    if (pool)
         for (cudaEvent_t e : pool->timing_events) cudaEventDestroy(e);
-        if (pool->ev_fork) cudaEventDestroy(pool->ev_fork);
-        if (pool->ev_join) cudaEventDestroy(pool->ev_join);
-        if (pool->side) cudaStreamDestroy(pool->side);
-    }
     delete pool;
     return MARLAAS_OK;
 }
