@@ -128,8 +128,8 @@ marlaas_status_t make_plan(const marlaas_pool* pool, int64_t T, const marlaas_se
 
 // Shrink for the tensor-core path: batches with several 128-token tiles go through the tcgen05 kernel, small
 // (decode-shaped) batches through the per-token gather kernel, which spreads over more SMs.
-marlaas_status_t shrink(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D, const bf16* store, int64_t sld,
-                        const Workspace& ws, float* out, cudaStream_t st, bool out_is_zero) {
+static marlaas_status_t shrink(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D, const bf16* store, int64_t sld,
+                               const Workspace& ws, float* out, cudaStream_t st, bool out_is_zero = false) {
     if (T >= 512 && shrink_split_sm100_eligible(pool, T, D))
         return launch_shrink_split_sm100(pool, T, src, ld, D, store, sld, ws, out, st, out_is_zero);
     if (T >= 512) return launch_shrink_sm100(pool, T, src, ld, D, store, sld, ws, out, st);

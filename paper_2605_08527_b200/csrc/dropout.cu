@@ -338,8 +338,6 @@ static marlaas_status_t launch_drop_begin(const marlaas_pool* pool, const marlaa
     return MARLAAS_OK;
 }
 
-static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
-
 static marlaas_status_t check_drop(const char* fn, const marlaas_pool* pool, int64_t T, const marlaas_dropout_t* drop, uint32_t flags, uint32_t allowed,
                                    void* workspace, size_t workspace_bytes) {
     if (!pool) return fail(MARLAAS_ERR_INVALID_ARG, "%s: pool is NULL", fn);

@@ -209,7 +209,6 @@ struct GradArgs {
     int transpose_out, accumulate;
     int stages;            // pipeline steps in flight
     int32_t* status;
-    int T;
     int chained;           // launched while the kernel before it still runs: waits for its end
     DropMask drop;         // DROP
     float* inl[GRAD_INLINE_SLOTS];   // small pools: the pointer table travels with the launch (no host-to-device copy)
@@ -600,7 +599,6 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
     g.transpose_out = transpose_out ? 1 : 0;
     g.accumulate = accumulate ? 1 : 0;
     g.status = pool->d_status;
-    g.T = (int)T;
     const bool chained = (phases & GRAD_PHASE_CHAINED) != 0;
     g.chained = chained ? 1 : 0;
     if (drop) g.drop = *drop;

@@ -361,8 +361,6 @@ static bool overlap(const Span& a, const Span& b) {
     return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
 }
 
-static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
-
 static bool head_sizes_ok(int64_t T, int64_t d, int64_t V) {
     return T >= 0 && T < (1ll << 31) && d >= 8 && d <= MARLAAS_MAX_HEAD_WIDTH && d % 8 == 0 && V >= 1 && V <= MARLAAS_MAX_VOCABULARY;
 }

@@ -268,20 +268,8 @@ marlaas_status_t launch_head_few(const marlaas_pool* pool, int64_t T, int64_t d,
         MARLAAS_CUDA_TRY(cudaFuncSetAttribute(k_head_few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)HF_SMEM));
         if (pool->device < 64) attr_set[pool->device] = true;
     }
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // behind the gathering kernel
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)(g.tiles < pool->sm_count ? g.tiles : pool->sm_count));
-    cfg.blockDim = dim3(HF_THREADS);
-    cfg.dynamicSmemBytes = HF_SMEM;
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_head_few, tmW, tmX, g));
-    MARLAAS_LAUNCH_CHECK("k_head_few");
-    return MARLAAS_OK;
+    return launch_link("k_head_few", k_head_few, dim3((unsigned)(g.tiles < pool->sm_count ? g.tiles : pool->sm_count)), HF_THREADS, HF_SMEM, true, st,
+                       tmW, tmX, g);        // (behind the gathering kernel)
 }
 
 }  // namespace marlaas

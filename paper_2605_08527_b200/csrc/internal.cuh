@@ -140,6 +140,8 @@ struct Workspace {
 };
 Workspace carve_workspace(const marlaas_pool* pool, int64_t T, void* base);
 
+inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+
 // ---- argument checks and table staging (api.cu), shared by the exported calls -------------------------
 constexpr int32_t MAX_SEGMENTS = 1 << 30;      // of a batch, and groups: the kernels' 32-bit steps and bisections over them stay in range
 marlaas_status_t check_segments(const char* fn, const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg,
@@ -330,8 +332,6 @@ marlaas_status_t launch_grad_sm100(const marlaas_pool* pool, int64_t T, int64_t 
 marlaas_status_t check_matrix(const char* fn, const char* name, const void* p, int64_t ld, int64_t cols);
 marlaas_status_t make_plan(const marlaas_pool* pool, int64_t T, const marlaas_segments_t* seg, uint32_t flags,
                            const std::vector<int32_t>& host_tok_slot, const Workspace& ws, cudaStream_t st);
-marlaas_status_t shrink(const marlaas_pool* pool, int64_t T, const bf16* src, int64_t ld, int64_t D, const bf16* store, int64_t sld,
-                        const Workspace& ws, float* out, cudaStream_t st, bool out_is_zero = false);
 Workspace part_workspace(const marlaas_pool* pool, const Workspace& ws, int p, int64_t T);
 void forward_operands(const marlaas_pool* pool, int64_t T, const bf16* x, int64_t ldx, const bf16* W, int64_t ldw, bf16* y, int64_t ldy,
                       const Workspace& ws, GemmOperands* o);

@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_norm_backward(const NormArg
                     for (int j = 0; j < NV; ++j) {
                         unpack8(element(st, b, 0, j), x);
                         unpack8(element(st, b, 1, j), dy);
-                gains(j, gain);
+                        gains(j, gain);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             x[e] = __ffma2_rn(__fmul2_rn(dy[e], gain[e]), both(rstd[b]), RMS ? __fmul2_rn(x[e], both(k)) : __ffma2_rn(__fadd2_rn(x[e], both(-mean[b])), both(k), both(c)));
@@ -617,20 +617,9 @@ static marlaas_status_t launch_norm_t(const marlaas_pool* pool, const NormArgs& 
         MARLAAS_CUDA_TRY(cudaFuncSetAttribute(kb, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::min<size_t>(bwd * THREADS, 200 * 1024)));
         if (pool->device < 64) attr_set[pool->device] = true;
     }
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // backward: behind the order's kernels
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)(n.groups / n.G));
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (backward ? bwd : fwd) * THREADS;
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = a.perm ? 1 : 0;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, backward ? kb : kf, a, n.W, n.G));
-    MARLAAS_LAUNCH_CHECK(backward ? "k_norm_backward" : "k_norm_forward");
-    return MARLAAS_OK;
+    // (backward: behind the order's kernels, if there are any)
+    return launch_link(backward ? "k_norm_backward" : "k_norm_forward", backward ? kb : kf, dim3((unsigned)(n.groups / n.G)), (unsigned)threads,
+                       (backward ? bwd : fwd) * THREADS, a.perm != nullptr, st, a, n.W, n.G);
 }
 static marlaas_status_t launch_norm(const marlaas_pool* pool, NormArgs a, bool rms, bool backward, cudaStream_t st) {
     const NormPlan n = norm_plan(pool, a.T, a.d, backward);
@@ -640,8 +629,6 @@ static marlaas_status_t launch_norm(const marlaas_pool* pool, NormArgs a, bool r
     return n.NV == 2 ? NORM_GO(2, 256, 3) : NORM_GO(4, 512, 1);
 #undef NORM_GO
 }
-
-static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
 // An output matrix may be an input matrix itself, with the same leading dimension; any other overlap is refused.
 static marlaas_status_t check_overlap(const char* fn, const char* name, const void* out, int64_t ldo, const void* in, int64_t ldi,
@@ -690,9 +677,9 @@ size_t marlaas_layer_norm_workspace_bytes(const marlaas_pool_t* pool, int64_t T,
 }
 
 marlaas_status_t marlaas_layer_norm(marlaas_pool_t* pool, int64_t T, int64_t d, const void* x, int64_t ldx,
-                                            const marlaas_segments_t* seg, const float* gain, const float* bias, float eps, void* y,
-                                            int64_t ldy, float* mean, float* rstd, void* workspace, size_t workspace_bytes,
-                                            uint32_t flags, void* cuda_stream) try {
+                                    const marlaas_segments_t* seg, const float* gain, const float* bias, float eps, void* y,
+                                    int64_t ldy, float* mean, float* rstd, void* workspace, size_t workspace_bytes,
+                                    uint32_t flags, void* cuda_stream) try {
     const char* fn = "layer_norm";
     marlaas_status_t rc = check_norm(fn, pool, T, d, seg, gain, bias, flags,
                                      MARLAAS_FLAG_HOST_TABLE | MARLAAS_FLAG_VALIDATE_SYNC | MARLAAS_FLAG_RMS_NORM);
@@ -785,19 +772,9 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
         const int64_t ctas = cdiv(d, 128) * (pool->cap + 1);
         int warps = 8;
         while (warps < 32 && warps * 32 < n.groups && ctas * warps * 2 <= (int64_t)pool->sm_count * 64) warps *= 2;
-        cudaLaunchConfig_t cfg;
-        memset(&cfg, 0, sizeof(cfg));
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at[0].val.programmaticStreamSerializationAllowed = 1;
-        cfg.gridDim = dim3((unsigned)cdiv(d, 128), (unsigned)(pool->cap + 1));
-        cfg.blockDim = dim3((unsigned)(warps * 32));
-        cfg.dynamicSmemBytes = (size_t)warps * 32 * (2 * sizeof(float4) + sizeof(int2));
-        cfg.stream = st;
-        cfg.attrs = at;
-        cfg.numAttrs = 1;
-        MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_norm_reduce, a));
-        MARLAAS_LAUNCH_CHECK("k_norm_reduce");
+        rc = launch_link("k_norm_reduce", k_norm_reduce, dim3((unsigned)cdiv(d, 128), (unsigned)(pool->cap + 1)), (unsigned)(warps * 32),
+                         (size_t)warps * 32 * (2 * sizeof(float4) + sizeof(int2)), true, st, a);
+        if (rc != MARLAAS_OK) return rc;
     }
     return finish(pool, flags, st);
 } catch (const std::exception& e) {

@@ -138,25 +138,8 @@ marlaas_status_t launch_order(const marlaas_pool* pool, OrderArgs a, int32_t* sc
     k_order_count<<<nblk, B, smem, st>>>(a);
     MARLAAS_LAUNCH_CHECK("k_order_count");
     if (nblk == 1) return MARLAAS_OK;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(1);
-    cfg.blockDim = dim3(1024);
-    cfg.dynamicSmemBytes = sizeof(int) * ((size_t)a.nkeys + 1);
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_order_scan, a, nblk));
-    MARLAAS_LAUNCH_CHECK("k_order_scan");
-    cfg.gridDim = dim3((unsigned)nblk);
-    cfg.blockDim = dim3((unsigned)B);
-    cfg.dynamicSmemBytes = 0;
-    MARLAAS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_order_place, a));
-    MARLAAS_LAUNCH_CHECK("k_order_place");
-    return MARLAAS_OK;
+    const marlaas_status_t rc = launch_link("k_order_scan", k_order_scan, dim3(1), 1024, sizeof(int) * ((size_t)a.nkeys + 1), true, st, a, nblk);
+    return rc != MARLAAS_OK ? rc : launch_link("k_order_place", k_order_place, dim3((unsigned)nblk), (unsigned)B, 0, true, st, a);
 }
 
 }  // namespace marlaas

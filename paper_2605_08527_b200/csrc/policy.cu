@@ -421,8 +421,6 @@ static marlaas_status_t stage_tables(const marlaas_segments_t* seg, int32_t num_
     return MARLAAS_OK;
 }
 
-static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
-
 static marlaas_status_t check_rows(const char* fn, const char* name, const void* p, int64_t ld, int64_t V, int32_t dtype) {
     const int64_t per16 = dtype == MARLAAS_DTYPE_F32 ? 4 : 8;
     if (!p || misaligned(p, 16)) return fail(MARLAAS_ERR_INVALID_ARG, "%s: %s is NULL or not 16-byte aligned", fn, name);
