@@ -56,7 +56,9 @@ struct HeadArgs {
 };
 
 // A token that counts is copied to its row, of another one the outputs are cleared; a warp per place in the order.  Batches of at
-// most HEAD_SMALL_T tokens need no order made before (SMALL): a warp takes a token, and each CTA counts the tokens before its own.
+// most HEAD_SMALL_T tokens need no order made before (SMALL): a warp takes a token, and each CTA counts the tokens before its own,
+// which costs tokens^2 / 2048 loads where the order costs three kernels (whole calls, V = 1000, d = 1024, counted here and ordered
+// before: 1024 tokens 25 and 29 us, 4096 37 and 42, 8192 65 and 66, 16384 117 and 109).
 constexpr int HEAD_SMALL_T = 4096;
 template <bool SMALL>
 __global__ void __launch_bounds__(HEAD_THREADS) k_head_gather(const HeadArgs a, int32_t* perm, int32_t* active, int32_t* status) {
