@@ -266,9 +266,8 @@ marlaas_status_t marlaas_lora_forward_static_ws(marlaas_pool_t* pool, int64_t T,
  * MARLAAS_FLAG_ACCUMULATE every non-NULL slot is overwritten (tenants with no token in the batch get exact
  * zeros); with it the batch's contribution is added.  The sums over a tenant's tokens run over all of its
  * segments.  h_saved: what forward wrote to h_save for the same batch and adapters, or NULL = recompute.
- * Part of the work (the adapter-gradient kernels, when h_saved is given) may be issued on a stream that the pool
- * owns, forked from cuda_stream after the call's first kernels and joined to it before the call returns (events;
- * legal inside a stream capture): everything the call writes is ordered on cuda_stream as if issued there.  Inside a
+ * A row of x or dy with infinities or NaN may reach dA_t and dB_t of the other tenants that share a block of 64 tokens
+ * with it (the call with dropout below keeps them apart).  All work is issued on cuda_stream.  Inside a
  * stream capture, pools of more than 64 slots copy dA_slots / dB_slots with a memcpy node that keeps the HOST pointers:
  * the caller's tables must then stay alive and unchanged for every replay.  Calls on one pool are not to be issued from
  * several host threads at once. */
@@ -412,9 +411,14 @@ enum { MARLAAS_HEAD_STATS = 4 };                           /* columns of marlaas
  * rates: fp32 [capacity] on the device, per slot; a rate that is not above 0 (or a NaN) drops nothing, one of 1 or more drops
  * everything (the adapter then gives nothing and gets zero gradients).  What a dropped element holds does not matter to the
  * adapters, and what the rows of a tenant's tokens hold (infinities and NaN too) reaches no other tenant's rows and gradients.
- * With rates of 0 the results are marlaas_lora_forward's and marlaas_lora_backward's up to the order of sums.
+ * With rates of 0 the results are marlaas_lora_forward's and marlaas_lora_backward's up to the order of sums; as there, s'_t h and
+ * s'_t g are rounded to bf16 on their way into the second products, and from 512 tokens on dA and dB take h and g as the sum of two
+ * bf16 numbers each (2^-16 relative).
+ * Meant for supervised tuning.  A policy that answers without dropout is another function than the one that trains with it: its
+ * ratios are then not 1 in the first pass over a batch, and marlaas_head_cross_entropy's dx is not its policy gradient.
  * Otherwise as those two calls, with h_save = (m_i o x_i) A_t; of the flags, HOST_TABLE, VALIDATE_SYNC and (backward)
- * ACCUMULATE apply.  Workspace: marlaas_lora_dropout_workspace_bytes, for both.  Adapter gradients of pools of more than 64
+ * ACCUMULATE apply.  Workspace: marlaas_lora_dropout_workspace_bytes, for both; it has room for a copy of x beside the layer's
+ * own, for batches whose tenants mix finely and for rows of more than 96 K elements.  Adapter gradients of pools of more than 64
  * slots cannot be captured. */
 typedef struct marlaas_dropout {
     const float* rates;
@@ -436,7 +440,8 @@ marlaas_status_t marlaas_lora_backward_dropout(marlaas_pool_t* pool, int64_t T, 
  * var the population variance; with MARLAAS_FLAG_RMS_NORM mean_i = 0.  gain and bias (NULL = none) are fp32
  * [capacity + 1][d], 16-byte aligned; row `capacity` serves slot -1, and the tokens that an ill-formed device table leaves out
  * (reported by marlaas_check_status).  mean and rstd: fp32 [T] for the backward pass, each may be NULL.  y may be x itself.
- * A row of infinities or NaN gives NaN and touches no other row.  `pool` supplies the device, the slots and the status word.
+ * A row of infinities or NaN gives NaN and touches no other row; sums of a row's elements and of their squared deviations are fp32,
+ * so that rows of elements beyond about 1e17 leave its range.  `pool` supplies the device, the slots and the status word.
  * The workspace is used with MARLAAS_FLAG_HOST_TABLE alone (marlaas_layer_norm_workspace_bytes with backward = 0). */
 size_t marlaas_layer_norm_workspace_bytes(const marlaas_pool_t* pool, int64_t T, int64_t d, int32_t num_segments, int32_t backward);
 marlaas_status_t marlaas_layer_norm(marlaas_pool_t* pool, int64_t T, int64_t d, const void* x, int64_t ldx,
@@ -469,7 +474,9 @@ marlaas_status_t marlaas_layer_norm_backward(marlaas_pool_t* pool, int64_t T, in
  * No output may overlap an input otherwise.
  * stats (or NULL; then seg is not read): fp32 [capacity + 1][MARLAAS_HEAD_STATS], per slot (last row: slot -1) the sums over its
  * tokens of  w (-logp), w, -logp, 1;  written, or added to with MARLAAS_FLAG_ACCUMULATE, in a fixed order.
- * The exponentials in the workspace are those of a piece of the batch (512 MB, or 256 rows where those are more).  The probabilities
+ * The exponentials in the workspace are those of a piece of the batch (512 MB, or 256 rows where those are more); beside them it holds
+ * the counted rows of the whole batch (2 T d bytes), and with a gradient up to 192 MB of partial sums.  Logits and the exponentials'
+ * sums carry the tensor cores' fp32 sums and the hardware's exponential (about 2e-6 of a log-probability).  The probabilities
  * in the gradient's product are bf16, rounded twice on their way there (2^-8 relative each time); all sums are fp32. */
 size_t marlaas_head_cross_entropy_workspace_bytes(const marlaas_pool_t* pool, int64_t T, int64_t d, int64_t V, int32_t num_segments,
                                                   int32_t with_gradient);

@@ -6,8 +6,8 @@
 // rounded anew.  The layer's own kernels run with s'_t in the place of s_t; no masked copy of x is written but for batches whose
 // tenants mix too finely for the tensor-core reductions.
 // The products bound it, as they do the layer: forward 8192 x 4096 x 4096 with 32 tenants of rank 16 250 us (the product 180 at full
-// clocks, the masked shrink 40, of which the masks' random numbers are 8), backward 328 us (dx 188, its masks 8 of them; shrink 33;
-// the reductions 30 and 37).  All kernels of a call follow one another on the caller's stream: the reductions beside the dx product
+// clocks, the masked shrink 40, of which the masks' random numbers are 8), backward 320 us (dx 186, its masks 8 of them; shrink 33;
+// the reductions 35 and 42).  All kernels of a call follow one another on the caller's stream: the reductions beside the dx product
 // on a second stream measured 4 % less, but once in some 12000 calls under a deep queue that form stopped making progress.
 #include <string.h>
 
