@@ -412,8 +412,8 @@ enum { MARLAAS_HEAD_STATS = 4 };                           /* columns of marlaas
  * everything (the adapter then gives nothing and gets zero gradients).  What a dropped element holds does not matter to the
  * adapters, and what the rows of a tenant's tokens hold (infinities and NaN too) reaches no other tenant's rows and gradients.
  * With rates of 0 the results are marlaas_lora_forward's and marlaas_lora_backward's up to the order of sums; as there, s'_t h and
- * s'_t g are rounded to bf16 on their way into the second products, and from 512 tokens on dA and dB take h and g as the sum of two
- * bf16 numbers each (2^-16 relative).
+ * s'_t g are rounded to bf16 on their way into the second products, and from 512 tokens on h and g are the tensor cores' fp32 sums
+ * (2e-6 relative) and enter dA and dB as the sum of two bf16 numbers each (2^-16 relative).
  * Meant for supervised tuning.  A policy that answers without dropout is another function than the one that trains with it: its
  * ratios are then not 1 in the first pass over a batch, and marlaas_head_cross_entropy's dx is not its policy gradient.
  * Otherwise as those two calls, with h_save = (m_i o x_i) A_t; of the flags, HOST_TABLE, VALIDATE_SYNC and (backward)

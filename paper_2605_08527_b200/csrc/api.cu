@@ -567,8 +567,8 @@ marlaas_status_t marlaas_lora_backward(marlaas_pool_t* pool, int64_t T, const vo
         const bool inline_tables = fits && pool->cap <= 64;
         const int32_t* run_flag = tc_grad ? ws.gflag : nullptr;   // the CUDA-core kernels run only if the flag is set
         // Batches of many rows whose h was kept: every kernel launched behind the one before it.  (Beside the dx product, on a
-        // second stream, they took nothing less of a step over one 4096 x 4096 projection and 4 % over a layer's seven; that form is
-        // left out, since one like it stopped making progress.)
+        // second stream, a step over one 5120 x 5120 projection took as long and one over a layer's seven 4 % less; that form is left
+        // out, since one like it stopped making progress.)
         if (inline_tables && dx && (!want_dB || h_saved) && gemm2_sm100_eligible(pool, T)) {
             rc = adapter_gradients(pool, T, (const bf16*)x, ldx, (const bf16*)dy, lddy, dA_slots, dB_slots, seg, h_saved ? h_saved : ws.h, ws, acc, st, nullptr,
                                    (flags & MARLAAS_FLAG_REUSE_PLAN) != 0);
